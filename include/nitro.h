@@ -363,6 +363,98 @@ nitro_status nitro_prep_apply(nitro_prep* p, const uint8_t* x, int64_t n, int8_t
 nitro_status nitro_prep_stats(nitro_prep* p, int64_t* mu, int64_t* omega);
 void nitro_prep_destroy(nitro_prep* p);
 
+/* ---- Floating-point head --------------------------------------------------
+ * The paper's learning and output layers hold at most 64 classes and train on
+ * the integer RSS loss.  The calls below train and serve a classifier over
+ * many classes on the blocks' int8 activations (or on bf16 features): the
+ * softmax cross entropy of a linear head with its gradients, an orthogonalised
+ * update for its weights (or for the blocks' own int64 gradients), and the
+ * head's product with weights in 4 bits.  The paper has no counterpart to them.
+ *
+ * Matrices are row-major, with a row stride ld in elements (at least the
+ * columns).  bf16 data is passed as uint16_t or void.  Buffers need the alignment of their
+ * element type unless stated; rows at multiples of 16 bytes are faster.  All compute calls are
+ * asynchronous on `stream` and may be captured into a CUDA graph; a handle
+ * owns its workspace, sized at create, and must not be used by two streams at
+ * once.  The *_status calls synchronise the device and return the latched status
+ * (TIMEOUT, or ARG for a label out of range), and clear it if clear. */
+typedef enum { NITRO_BF16 = 0, NITRO_I8 = 1, NITRO_F32 = 2, NITRO_I64 = 3 } nitro_dtype;
+
+/* Softmax cross entropy of z = scale x W^T: x [rows x features] (NITRO_BF16 or
+ * NITRO_I8), W bf16 [classes x features], scale > 0 (int8 activations are integers;
+ * a scale brings their logits into range).  The logits are never kept: pieces of the
+ * classes are computed in both calls.
+ *
+ * forward: lse[i] = log sum_j exp z_ij and loss[i] = lse[i] - z_i,label (0 where the label is
+ * -1: the row is left out).  A label outside [-1, classes) latches BAD_LABEL
+ * and counts as -1.
+ * backward, from the lse of a forward on the same inputs and the loss gradient
+ * gout[i] of each row (NULL: 1): G_ij = gout_i scale (softmax(z_i)_j - [j = label_i]), zero in
+ * rows that are left out, rounded to bf16; dx = G W and dw = G^T x, bf16, either may
+ * be NULL.  Sums are in 32 bits, in an order that a shape fixes.  Rows that are left out
+ * put nothing into dw, whatever they hold; with rows = 0 dw is cleared.
+ * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], a stride
+ * below the features, another type, or a scale that is not above 0 (1e30 at most). */
+typedef struct nitro_xent nitro_xent;
+nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xent** out);
+nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w,
+                                int64_t ldw, const int32_t* labels, int rows, float scale, float* loss,
+                                float* lse, void* stream);
+nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w,
+                                 int64_t ldw, const int32_t* labels, int rows, float scale, const float* lse,
+                                 const float* gout, uint16_t* dx, int64_t lddx, uint16_t* dw, int64_t lddw,
+                                 void* stream);
+nitro_status nitro_xent_status(nitro_xent* h, int clear);
+void nitro_xent_destroy(nitro_xent* h);
+
+/* An update made orthogonal: X = M / (|M|_F + 1e-7), then `steps` times
+ * A = X X^T, X = a X + (b A + c A^2) X (on the shorter side), out = X in bf16.
+ * M: `count` matrices [rows x cols], stride_m elements apart, NITRO_BF16, NITRO_F32 or
+ * NITRO_I64 (weight gradients as nitro_block_grad_device gives them).  coef: (a, b, c), or NULL
+ * for (3.4445, -4.7750, 2.0315), which take every singular value to about 1 in
+ * five steps.  A matrix of zeros gives zeros.  out must not overlap M.
+ * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, max_count], steps
+ * outside [0, 100], strides below the sizes, another type, or coefficients under which a
+ * singular value in [0, 1] can pass 8 or |b s^2 + c s^4| 1024. */
+typedef struct nitro_orth nitro_orth;
+nitro_status nitro_orth_create(int max_count, int rows, int cols, nitro_orth** out);
+nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ldm, int64_t stride_m, int count,
+                            int steps, const float* coef, uint16_t* out, int64_t ldo, int64_t stride_o,
+                            void* stream);
+nitro_status nitro_orth_status(nitro_orth* h, int clear);
+void nitro_orth_destroy(nitro_orth* h);
+
+/* Microscaled 4-bit floating point: e2m1 values (0, 1/2, 1, 3/2, 2, 3, 4, 6 and their negatives)
+ * that share a power of two in blocks of 32 along a row (the last block of a row may be
+ * short).  A block's scale is 2^(floor(log2 max|v|) - 2), at least 2^-127, stored as the
+ * exponent + 127; a value goes to the nearest multiple, ties to the even code, 6 at most.
+ * A block that holds an infinity or NaN gets the scale 255, and all its values read as NaN.
+ *
+ * codes: [rows][blocks][16] bytes, blocks = ceil(cols / 32), value 2i of a block in the low
+ * half of byte i, zero past the last column.  scales: tiles of 128 rows x 4 blocks, 512
+ * bytes each, in the order [row tile][block tile]; row r, block j of a tile at
+ * (r % 32) 16 + (r / 32) 4 + j; places without a block hold 0.  nitro_mx4_bytes gives both sizes.
+ * Both buffers are 16-byte aligned.
+ *
+ * quantize: x [rows x cols], NITRO_BF16 or NITRO_F32.  dequantize: out in either type (exact but for
+ * bf16 below 2^-133); scale_values (may be NULL): the scales as fp32 [rows][blocks].
+ * linear: y [rows x out_features] = Q(x) W^T, NITRO_BF16 or NITRO_F32, for x [rows x in] as
+ * above, quantised on the way, and W [out_features x in] as codes and scales.  Exact products,
+ * 32-bit sums.  Errors: NITRO_ERR_ARG for null handles or pointers, sizes out of range, a
+ * stride below the columns, another type or a buffer that is not aligned. */
+typedef struct nitro_mx4 nitro_mx4;
+nitro_status nitro_mx4_bytes(int rows, int cols, size_t* codes, size_t* scales);
+nitro_status nitro_mx4_quantize(const void* x, int type, int64_t ldx, int rows, int cols, uint8_t* codes,
+                                uint8_t* scales, void* stream);
+nitro_status nitro_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, int rows, int cols, void* out,
+                                  int type, int64_t ldo, float* scale_values, void* stream);
+nitro_status nitro_mx4_create(int max_rows, int in, int out_features, nitro_mx4** out);
+nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t ldx, int rows,
+                              const uint8_t* w_codes, const uint8_t* w_scales, void* y, int y_type,
+                              int64_t ldy, void* stream);
+nitro_status nitro_mx4_status(nitro_mx4* h, int clear);
+void nitro_mx4_destroy(nitro_mx4* h);
+
 /* ---- Diagnostics (not part of the training step) -------------------------
  * Every kernel launch of the library is counted.  With profiling on, each
  * launch is also bracketed by CUDA events recorded on its own stream and

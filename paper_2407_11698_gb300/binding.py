@@ -19,6 +19,7 @@ NITRO_CONV3X3, NITRO_LINEAR = 0, 1
 NITRO_ROUND_FLOOR, NITRO_ROUND_TRUNC = 0, 1
 STATUS_BIT_OVERFLOW, STATUS_BIT_BAD_LABEL, STATUS_BIT_TIMEOUT = 1, 2, 4
 NITRO_CONTRACT_FWD, NITRO_CONTRACT_WGRAD, NITRO_CONTRACT_DGRAD = 0, 1, 2
+NITRO_BF16, NITRO_I8, NITRO_F32, NITRO_I64 = range(4)
 (NITRO_T_W, NITRO_T_DW, NITRO_T_WLR, NITRO_T_DWLR, NITRO_T_ACT, NITRO_T_REGION,
  NITRO_T_ARGMAX, NITRO_T_DELTA, NITRO_T_GRAD_L, NITRO_T_SSE, NITRO_T_LR_IN, NITRO_T_LR_ARGMAX,
  NITRO_T_STEP) = range(13)
@@ -127,7 +128,27 @@ def lib():
     L.nitro_prep_stats.argtypes = [_VP, ctypes.POINTER(ctypes.c_int64), ctypes.POINTER(ctypes.c_int64)]
     L.nitro_prep_destroy.argtypes = [_VP]
     L.nitro_prep_destroy.restype = None
-    for name in ("nitro_conv3x3_create", "nitro_conv3x3_contract", "nitro_conv3x3_status",
+    _I, _L, _F = ctypes.c_int, ctypes.c_int64, ctypes.c_float
+    _PS = ctypes.POINTER(ctypes.c_size_t)
+    L.nitro_xent_create.argtypes = [_I, _I, _I, ctypes.POINTER(_VP)]
+    L.nitro_xent_forward.argtypes = [_VP, _VP, _I, _L, _VP, _L, _VP, _I, _F, _VP, _VP, _VP]
+    L.nitro_xent_backward.argtypes = [_VP, _VP, _I, _L, _VP, _L, _VP, _I, _F, _VP, _VP, _VP, _L, _VP, _L, _VP]
+    L.nitro_orth_create.argtypes = [_I, _I, _I, ctypes.POINTER(_VP)]
+    L.nitro_orth_run.argtypes = [_VP, _VP, _I, _L, _L, _I, _I, ctypes.POINTER(_F), _VP, _L, _L, _VP]
+    L.nitro_mx4_bytes.argtypes = [_I, _I, _PS, _PS]
+    L.nitro_mx4_quantize.argtypes = [_VP, _I, _L, _I, _I, _VP, _VP, _VP]
+    L.nitro_mx4_dequantize.argtypes = [_VP, _VP, _I, _I, _VP, _I, _L, _VP, _VP]
+    L.nitro_mx4_create.argtypes = [_I, _I, _I, ctypes.POINTER(_VP)]
+    L.nitro_mx4_linear.argtypes = [_VP, _VP, _I, _L, _I, _VP, _VP, _VP, _I, _L, _VP]
+    for op in ("xent", "orth", "mx4"):
+        getattr(L, "nitro_%s_status" % op).argtypes = [_VP, _I]
+        getattr(L, "nitro_%s_status" % op).restype = _I
+        getattr(L, "nitro_%s_create" % op).restype = _I
+        getattr(L, "nitro_%s_destroy" % op).argtypes = [_VP]
+        getattr(L, "nitro_%s_destroy" % op).restype = None
+    for name in ("nitro_xent_forward", "nitro_xent_backward", "nitro_orth_run", "nitro_mx4_bytes",
+                 "nitro_mx4_quantize", "nitro_mx4_dequantize", "nitro_mx4_linear",
+                 "nitro_conv3x3_create", "nitro_conv3x3_contract", "nitro_conv3x3_status",
                  "nitro_gemm_create", "nitro_gemm_run", "nitro_gemm_status",
                  "nitro_prep_create", "nitro_prep_fit", "nitro_prep_apply", "nitro_prep_stats"):
         getattr(L, name).restype = ctypes.c_int
@@ -477,3 +498,180 @@ class IntPrep:
             self.close()
         except Exception:
             pass
+
+
+# ---------------------------------------------------------------- floating-point head
+def _dtype(t, allowed):
+    """The NITRO_* type of a torch tensor; ValueError if it is none of `allowed`."""
+    import torch
+    code = {torch.bfloat16: NITRO_BF16, torch.int8: NITRO_I8, torch.float32: NITRO_F32,
+            torch.int64: NITRO_I64}.get(t.dtype)
+    if code not in allowed:
+        raise ValueError("a tensor of type %s is not supported here" % t.dtype)
+    return code
+
+
+def _matrix(t, rows, cols, allowed, what):
+    """(type, row stride) of a CUDA matrix [rows x cols] whose rows are contiguous."""
+    if not t.is_cuda or t.dim() != 2 or tuple(t.shape) != (rows, cols):
+        raise ValueError("%s must be a CUDA tensor [%d x %d]" % (what, rows, cols))
+    if cols > 1 and t.stride(1) != 1:
+        raise ValueError("the rows of %s must be contiguous" % what)
+    # the stride of a lone row is never used
+    return _dtype(t, allowed), max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+
+
+def _vector(t, n, dtype, what):
+    import torch
+    if not t.is_cuda or t.dtype != getattr(torch, dtype) or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of %d %s" % (what, n, dtype))
+    return _ptr(t)
+
+
+class _Handle:
+    """A C handle of the operator `_op`: its status, and its end."""
+    _op = ""
+
+    def _create(self, *shape):
+        self.h = _VP()
+        name = "nitro_%s_create" % self._op
+        st = getattr(lib(), name)(*[int(v) for v in shape], ctypes.byref(self.h))
+        if st != NITRO_OK:
+            raise NitroError(st, name)
+
+    def status(self, clear=False):
+        return getattr(lib(), "nitro_%s_status" % self._op)(self.h, 1 if clear else 0)
+
+    def close(self):
+        if getattr(self, "h", None):
+            getattr(lib(), "nitro_%s_destroy" % self._op)(self.h)
+            self.h = None
+
+    def __del__(self):
+        try:
+            self.close()
+        except Exception:
+            pass
+
+
+class SoftmaxXent(_Handle):
+    """Softmax cross entropy of a linear head z = scale x W^T over many classes,
+    without keeping z.  x: bf16 or int8 [rows x features]; W: bf16 [classes x
+    features]; labels int32, -1 leaves a row out."""
+    _op = "xent"
+
+    def __init__(self, max_rows, features, classes):
+        self.features, self.classes = int(features), int(classes)
+        self._create(max_rows, features, classes)
+
+    def _inputs(self, x, w, labels):
+        n = x.shape[0]
+        xt, ldx = _matrix(x, n, self.features, (NITRO_BF16, NITRO_I8), "x")
+        _, ldw = _matrix(w, self.classes, self.features, (NITRO_BF16,), "w")
+        return n, [_ptr(x), xt, ldx, _ptr(w), ldw, _vector(labels, n, "int32", "labels"), n]
+
+    def forward(self, x, w, labels, loss, lse, scale=1.0, stream=None):
+        """Writes the rows' losses and log-sums (fp32 [rows]); returns loss."""
+        n, a = self._inputs(x, w, labels)
+        st = lib().nitro_xent_forward(self.h, *a, float(scale), _vector(loss, n, "float32", "loss"),
+                                      _vector(lse, n, "float32", "lse"), _stream_ptr(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_xent_forward")
+        return loss
+
+    def backward(self, x, w, labels, lse, gout=None, dx=None, dw=None, scale=1.0, stream=None):
+        """Writes dx [rows x features] and dw [classes x features] (bf16; either may be
+        None) from the lse of a forward on the same inputs; gout: the gradient of each
+        row's loss (fp32), None for ones."""
+        n, a = self._inputs(x, w, labels)
+        lddx = _matrix(dx, n, self.features, (NITRO_BF16,), "dx")[1] if dx is not None else self.features
+        lddw = _matrix(dw, self.classes, self.features, (NITRO_BF16,), "dw")[1] if dw is not None else self.features
+        st = lib().nitro_xent_backward(self.h, *a, float(scale), _vector(lse, n, "float32", "lse"),
+                                       None if gout is None else _vector(gout, n, "float32", "gout"),
+                                       _ptr(dx), lddx, _ptr(dw), lddw, _stream_ptr(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_xent_backward")
+        return dx, dw
+
+
+class Orthogonalizer(_Handle):
+    """Newton-Schulz orthogonalisation of up to max_count matrices [rows x cols]."""
+    _op = "orth"
+
+    def __init__(self, max_count, rows, cols):
+        self.rows, self.cols = int(rows), int(cols)
+        self._create(max_count, rows, cols)
+
+    def run(self, m, out, steps=5, coef=None, stream=None):
+        """m: [rows x cols] or [count x rows x cols] in bf16, fp32 or int64; out: bf16 of the
+        same shape.  coef: (a, b, c) of the step, None for the default."""
+        a, b = (t.unsqueeze(0) if t.dim() == 2 else t for t in (m, out))
+        if b.shape != a.shape or a.dim() != 3 or tuple(a.shape[1:]) != (self.rows, self.cols):
+            raise ValueError("m and out must be [count x %d x %d]" % (self.rows, self.cols))
+        n, ld = a.shape[0], [self.cols, self.cols]
+        types = [NITRO_BF16, NITRO_BF16]
+        if n:
+            types[0], ld[0] = _matrix(a[0], self.rows, self.cols, (NITRO_BF16, NITRO_F32, NITRO_I64), "m")
+            types[1], ld[1] = _matrix(b[0], self.rows, self.cols, (NITRO_BF16,), "out")
+        k = None if coef is None else (ctypes.c_float * 3)(*coef)
+        st = lib().nitro_orth_run(self.h, _ptr(m), types[0], ld[0], a.stride(0), n, int(steps), k, _ptr(out), ld[1],
+                                  b.stride(0), _stream_ptr(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_orth_run")
+        return out
+
+
+def mx4_bytes(rows, cols):
+    """(bytes of codes, bytes of scales) of a 4-bit matrix [rows x cols]."""
+    q, s = ctypes.c_size_t(), ctypes.c_size_t()
+    st = lib().nitro_mx4_bytes(int(rows), int(cols), ctypes.byref(q), ctypes.byref(s))
+    if st != NITRO_OK:
+        raise NitroError(st, "nitro_mx4_bytes")
+    return q.value, s.value
+
+
+def _mx4_buffers(codes, scales, rows, cols):
+    nq, ns = mx4_bytes(rows, cols)
+    return [_vector(codes, nq, "uint8", "codes"), _vector(scales, ns, "uint8", "scales")]
+
+
+def mx4_quantize(x, codes, scales, stream=None):
+    """x (bf16 or fp32) [rows x cols] as 4-bit codes and block scales (uint8, mx4_bytes)."""
+    rows, cols = x.shape
+    t, ld = _matrix(x, rows, cols, (NITRO_BF16, NITRO_F32), "x")
+    st = lib().nitro_mx4_quantize(_ptr(x), t, ld, rows, cols, *_mx4_buffers(codes, scales, rows, cols),
+                                  _stream_ptr(stream))
+    if st != NITRO_OK:
+        raise NitroError(st, "nitro_mx4_quantize")
+    return codes, scales
+
+
+def mx4_dequantize(codes, scales, out, scale_values=None, stream=None):
+    """The values as out (bf16 or fp32) [rows x cols]; scale_values: fp32 [rows x blocks] or None."""
+    rows, cols = out.shape
+    t, ld = _matrix(out, rows, cols, (NITRO_BF16, NITRO_F32), "out")
+    sv = None if scale_values is None else _vector(scale_values, rows * -(-cols // 32), "float32", "scale_values")
+    st = lib().nitro_mx4_dequantize(*_mx4_buffers(codes, scales, rows, cols), rows, cols, _ptr(out), t, ld, sv,
+                                    _stream_ptr(stream))
+    if st != NITRO_OK:
+        raise NitroError(st, "nitro_mx4_dequantize")
+    return out
+
+
+class Mx4Linear(_Handle):
+    """y = Q(x) W^T for x [rows x in] (quantised on the way) and 4-bit weights W [out x in]."""
+    _op = "mx4"
+
+    def __init__(self, max_rows, in_features, out_features):
+        self.in_features, self.out_features = int(in_features), int(out_features)
+        self._create(max_rows, in_features, out_features)
+
+    def run(self, x, codes, scales, y, stream=None):
+        n = x.shape[0]
+        xt, ldx = _matrix(x, n, self.in_features, (NITRO_BF16, NITRO_F32), "x")
+        yt, ldy = _matrix(y, n, self.out_features, (NITRO_BF16, NITRO_F32), "y")
+        st = lib().nitro_mx4_linear(self.h, _ptr(x), xt, ldx, n, *_mx4_buffers(codes, scales, self.out_features, self.in_features),
+                                    _ptr(y), yt, ldy, _stream_ptr(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_mx4_linear")
+        return y

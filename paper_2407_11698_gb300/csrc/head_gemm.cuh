@@ -1,0 +1,454 @@
+// The contraction kernel of the floating-point head: D = A B^T on the tcgen05 tensor
+// cores with 16-bit operands, 32-bit sums and an epilogue of the caller's.
+//
+// D[m][n] = sum over passes p and k of A_p[m][k] B_p[n][k].  Each operand is a tensor
+// map of rank 3 over planes of a matrix, stored either along K (inner dimension k) or
+// along M / N (inner dimension m or n); the planes are the matrices of a batch and, for
+// operands that are split into a high and a low half, the halves.  Everything past a
+// matrix's end reads as zero (the maps' bounds).
+//
+// One persistent CTA an SM: warp 0 loads tiles of 64 along K by TMA into a ring of
+// shared-memory stages, warp 1 issues the MMAs, warps 4..11 drain the sums from TMEM
+// through the epilogue (two warps a TMEM lane quadrant, half the columns each), while
+// the MMAs of the next tile fill the other of two accumulators.  CG = 2 pairs two CTAs
+// of a cluster on one 256-row tile: each loads its own 128 rows of A and half the
+// columns of B, and the MMAs that one thread of the pair issues read both halves.  That
+// halves the bytes of B an SM has to load and read for the same products, which is what
+// bounds the lone form (see the figures at pick_tile()).
+//
+// Every wait is bounded; on expiry the kernel raises TIMEOUT, drains its own copies and
+// MMAs in flight (bounded as well), frees TMEM and returns.
+#pragma once
+
+#include <cuda_bf16.h>
+#include <cuda_fp16.h>
+
+#include <algorithm>
+
+#include "prof.cuh"
+#include "tc_ptx.cuh"
+
+namespace nitro {
+namespace {
+
+constexpr int kHgThreads = 384;
+constexpr int kHgEpiWarp0 = 4, kHgEpiWarps = 8;
+constexpr int kHgBK = 64;                // K elements a stage: rows of 128 bytes
+constexpr uint64_t kDrainNs = 50000000ull;
+
+struct HgArgs {
+    int M, N;                  // valid rows and columns of D
+    int tiles_m, tiles_n, splits, batch, total;
+    int kb_total, kb_per_split;   // K blocks of a pass, of a split
+    int passes;                // 1, or 3: high x high, high x low, low x high halves
+    int planes_a, planes_b;    // planes a matrix of the batch has
+    int upper;                 // symmetric D: only tiles that reach the diagonal or lie right of it
+    int band;                  // row tiles that are walked together
+    uint32_t* status;
+};
+
+struct HgTile {
+    int m, n, split, batch, kb0, kb1;
+};
+
+template <int TM, int BN>
+__device__ __forceinline__ HgTile hg_decode(const HgArgs& g, int idx) {
+    HgTile t;
+    const int per = g.total / (g.splits * g.batch);
+    const int outer = idx / per;
+    idx -= outer * per;
+    t.split = outer % g.splits;
+    t.batch = outer / g.splits;
+    if (g.upper) {
+        int m = 0;
+        for (; m < g.tiles_m; ++m) {
+            const int row = g.tiles_n - m * TM / BN;
+            if (idx < row) break;
+            idx -= row;
+        }
+        t.m = m;
+        t.n = m * TM / BN + idx;
+    } else {
+        const int in_band = g.band * g.tiles_n;
+        const int b = idx / in_band;
+        const int rows = min(g.band, g.tiles_m - b * g.band);
+        const int r = idx - b * in_band;
+        t.n = r / rows;
+        t.m = b * g.band + r - t.n * rows;
+    }
+    t.kb0 = t.split * g.kb_per_split;
+    t.kb1 = min(g.kb_total, t.kb0 + g.kb_per_split);
+    return t;
+}
+
+template <int CG, int BN>
+struct HgCfg {
+    static constexpr int A_BYTES = 128 * 128;
+    static constexpr int B_ROWS = BN / CG;
+    static constexpr int B_BYTES = B_ROWS * 128;
+    static constexpr int STAGE = A_BYTES + B_BYTES;
+    static constexpr int S = STAGE > 40000 ? 4 : 6;
+    static constexpr int SMEM = S * STAGE + 1024 + 256;
+    static constexpr int TCOLS = 2 * BN;
+};
+
+// instruction descriptor of kind::f16 with f32 sums: both operands bf16 or both f16
+__host__ __device__ constexpr uint32_t hg_idesc(bool f16, int m, int n, bool a_mn, bool b_mn) {
+    return (1u << 4) | (f16 ? 0u : (1u << 7) | (1u << 10)) | (a_mn ? (1u << 15) : 0u) | (b_mn ? (1u << 16) : 0u) |
+           ((uint32_t)(n >> 3) << 17) | ((uint32_t)(m >> 4) << 24);
+}
+
+template <int CG>
+__device__ __forceinline__ void hg_tma(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1, int c2) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.3d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%3, %4, %5}], [%2];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1), "r"(c2)
+            : "memory");
+    else
+        tma_load_3d(dst, m, bar, c0, c1, c2);
+}
+template <int CG>
+__device__ __forceinline__ void hg_mma(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t accumulate) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %4, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::f16 [%0], %1, %2, %3, p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(accumulate)
+            : "memory");
+    else
+        umma_bf16(d, a, b, idesc, accumulate);
+}
+// arrives at `bar` (of both CTAs of a pair) once the MMAs issued so far are done
+template <int CG>
+__device__ __forceinline__ void hg_commit(uint32_t bar) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "tcgen05.commit.cta_group::2.mbarrier::arrive::one.shared::cluster.multicast::cluster.b64 [%0], %1;" ::"r"(bar),
+            "h"((uint16_t)3)
+            : "memory");
+    else
+        umma_commit(bar);
+}
+__device__ __forceinline__ void mbar_arrive_remote(uint32_t cluster_bar) {
+    asm volatile("mbarrier.arrive.release.cluster.shared::cluster.b64 _, [%0];" ::"r"(cluster_bar) : "memory");
+}
+__device__ __forceinline__ void tmem_ld32_nowait(uint32_t taddr, uint32_t* r) {
+    asm volatile(
+        "tcgen05.ld.sync.aligned.32x32b.x32.b32 {%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, "
+        "%15, %16, %17, %18, %19, %20, %21, %22, %23, %24, %25, %26, %27, %28, %29, %30, %31}, [%32];"
+        : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]), "=r"(r[7]), "=r"(r[8]),
+          "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]), "=r"(r[14]), "=r"(r[15]), "=r"(r[16]),
+          "=r"(r[17]), "=r"(r[18]), "=r"(r[19]), "=r"(r[20]), "=r"(r[21]), "=r"(r[22]), "=r"(r[23]), "=r"(r[24]),
+          "=r"(r[25]), "=r"(r[26]), "=r"(r[27]), "=r"(r[28]), "=r"(r[29]), "=r"(r[30]), "=r"(r[31])
+        : "r"(taddr));
+}
+// gives up after limit_ns without raising anything
+__device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64_t limit_ns) {
+    const uint64_t t0 = global_ns();
+    while (!mbar_try_wait(bar, parity) && global_ns() - t0 < limit_ns) {
+    }
+}
+
+// Epi: struct Args, and per tile and thread
+//   Epi(args, g, tile, row, col0, half)   row: this thread's row of D; col0: its first
+//       column, that of the tile's half 0 or 1
+//   void cols(c, v)                 v[0..32): columns col0 + c .. col0 + c + 31
+//   void done()
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16>
+__global__ void __launch_bounds__(kHgThreads, 1)
+    k_head_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const HgArgs g,
+                const __grid_constant__ typename Epi::Args ea) {
+    using C = HgCfg<CG, BN>;
+    constexpr int S = C::S, TM = 128 * CG;
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);
+    // bars: full [S], empty [S], tmem full [2], tmem empty [2], drain
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 5);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    const uint32_t bar0 = smem_u32(bars);
+    const auto full_bar = [&](int s) { return bar0 + 8u * s; };
+    const auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
+    const auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * S + b); };
+    const auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };
+    const uint32_t drain_bar = bar0 + 8u * (2 * S + 4);
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+
+    if (threadIdx.x == 0) {
+        for (int s = 0; s < S; ++s) {
+            mbar_init(full_bar(s), 1);
+            mbar_init(empty_bar(s), 1);
+        }
+        for (int b = 0; b < 2; ++b) {
+            mbar_init(tfull_bar(b), 1);
+            mbar_init(tempty_bar(b), CG * kHgEpiWarps);
+        }
+        mbar_init(drain_bar, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 2) {
+        if constexpr (CG == 2) {
+            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                         "r"(C::TCOLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+        } else {
+            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
+                         "r"(C::TCOLS)
+                         : "memory");
+            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+        }
+    }
+    if (warp == 0 && lane == 0) {
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmA)) : "memory");
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmB)) : "memory");
+    }
+    pdl_wait();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();   // the peer's barriers are set up
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    if (warp == 0) {
+        if (lane == 0) {
+            // ---------------- TMA producer: this CTA's rows of A and its share of B's
+            int st = 0, loaded = 0;
+            uint32_t ph = 1;
+            const uint32_t s0 = smem_u32(smem);
+            for (int tile = unit; tile < g.total; tile += units) {
+                const HgTile T = hg_decode<TM, BN>(g, tile);
+                const int m0 = T.m * TM + rank * 128, n0 = T.n * BN + rank * C::B_ROWS;
+                for (int p = 0; p < g.passes; ++p) {
+                    const int za = T.batch * g.planes_a + (p == 2), zb = T.batch * g.planes_b + (p == 1);
+                    for (int kb = T.kb0; kb < T.kb1; ++kb) {
+                        if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
+                        const uint32_t a_dst = s0 + st * C::STAGE, b_dst = a_dst + C::A_BYTES;
+                        uint32_t fb = full_bar(st);
+                        if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
+                        if constexpr (CG == 2) fb = remote_smem(fb, 0);
+                        if constexpr (AMN) {
+#pragma unroll
+                            for (int j = 0; j < 2; ++j)
+                                hg_tma<CG>(a_dst + j * 8192, &tmA, fb, m0 + 64 * j, kb * kHgBK, za);
+                        } else {
+                            hg_tma<CG>(a_dst, &tmA, fb, kb * kHgBK, m0, za);
+                        }
+                        if constexpr (BMN) {
+#pragma unroll
+                            for (int j = 0; j < C::B_ROWS / 64; ++j)
+                                hg_tma<CG>(b_dst + j * 8192, &tmB, fb, n0 + 64 * j, kb * kHgBK, zb);
+                        } else {
+                            hg_tma<CG>(b_dst, &tmB, fb, kb * kHgBK, n0, zb);
+                        }
+                        ++loaded;
+                        if (++st == S) {
+                            st = 0;
+                            ph ^= 1u;
+                        }
+                    }
+                }
+            }
+        producer_out:
+            // a wait gave up: the copies in flight land before shared memory is given back
+            if (*abort_flag) {
+                for (int k = max(0, loaded - S); k < loaded; ++k)
+                    mbar_drain(full_bar(k % S), (uint32_t)(k / S) & 1u, kDrainNs);
+            }
+        }
+    } else if (warp == 1) {
+        if (lane == 0 && rank == 0) {
+            // ---------------- MMA issuer
+            constexpr uint32_t idesc = hg_idesc(F16, TM, BN, AMN, BMN);
+            const uint32_t s0 = smem_u32(smem);
+            const uint64_t da0 = AMN ? desc_sw128_mn(s0, 8192) : desc_sw128(s0);
+            const uint64_t db0 = BMN ? desc_sw128_mn(s0 + C::A_BYTES, 8192) : desc_sw128(s0 + C::A_BYTES);
+            // a step of 16 along K: 32 bytes of a row, or 16 rows of 128 bytes
+            constexpr uint64_t kStepA = AMN ? 2048 >> 4 : 32 >> 4, kStepB = BMN ? 2048 >> 4 : 32 >> 4;
+            int st = 0, it = 0;
+            uint32_t ph = 0;
+            for (int tile = unit; tile < g.total; tile += units, ++it) {
+                const HgTile T = hg_decode<TM, BN>(g, tile);
+                const int buf = it & 1;
+                if (!mbar_wait(tempty_bar(buf), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, g.status)) break;
+                tc_fence_after();
+                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                const int blocks = g.passes * (T.kb1 - T.kb0);
+                bool ok = true;
+                for (int i = 0; i < blocks; ++i) {
+                    if (!(ok = mbar_wait(full_bar(st), ph, abort_flag, g.status))) break;
+                    tc_fence_after();
+                    const uint64_t so = (uint64_t)((uint32_t)(st * C::STAGE) >> 4);
+#pragma unroll
+                    for (int k = 0; k < kHgBK / 16; ++k)
+                        hg_mma<CG>(d, da0 + so + k * kStepA, db0 + so + k * kStepB, idesc, (i | k) != 0 ? 1u : 0u);
+                    hg_commit<CG>(empty_bar(st));
+                    if (++st == S) {
+                        st = 0;
+                        ph ^= 1u;
+                    }
+                }
+                if (!ok) break;
+                hg_commit<CG>(tfull_bar(buf));
+            }
+            if (*abort_flag) {   // MMAs in flight end before TMEM is freed
+                hg_commit<CG>(drain_bar);
+                mbar_drain(drain_bar, 0, kDrainNs);
+            }
+            pdl_trigger();
+        }
+    } else if (warp >= kHgEpiWarp0) {
+        // ---------------- epilogue
+        const int q = warp & 3, half = (warp - kHgEpiWarp0) >> 2;
+        int it = 0;
+        for (int tile = unit; tile < g.total; tile += units, ++it) {
+            const HgTile T = hg_decode<TM, BN>(g, tile);
+            const int buf = it & 1;
+            Epi epi(ea, g, T, T.m * TM + rank * 128 + q * 32 + lane, T.n * BN + half * (BN / 2), half);
+            const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it >> 1) & 1u, abort_flag, g.status);
+            if (!__all_sync(0xffffffffu, ok)) break;
+            tc_fence_after();
+            const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
+            uint32_t v[2][32];
+            tmem_ld32_nowait(src, v[0]);
+#pragma unroll
+            for (int c = 0; c < BN / 64; ++c) {
+                tmem_wait_ld<32>(v[c & 1]);
+                if (c + 1 < BN / 64) tmem_ld32_nowait(src + 32 * (c + 1), v[(c + 1) & 1]);
+                else {
+                    // the sums are in registers: the accumulator may be filled again
+                    tc_fence_before();
+                    __syncwarp();
+                    if (lane == 0) {
+                        if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
+                        else mbar_arrive(tempty_bar(buf));
+                    }
+                }
+                float* f = reinterpret_cast<float*>(v[c & 1]);
+                epi.cols(32 * c, f);
+            }
+            epi.done();
+        }
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();   // no copy, MMA or arrival of the pair is outstanding
+    if (warp == 2) {
+        tc_fence_after();
+        if constexpr (CG == 2)
+            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TCOLS) : "memory");
+        else
+            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TCOLS) : "memory");
+    }
+}
+
+// ------------------------------------------------------------------ host side
+// An operand: planes of a matrix with `outer` rows of `inner` 16-bit elements, ld apart.
+struct HgOperand {
+    const void* base;
+    int64_t inner, outer, ld, planes, plane;   // plane: elements from one plane to the next
+};
+
+inline bool hg_map(CUtensorMap* m, const HgOperand& o, bool f16, int box_outer) {
+    auto fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dim[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)o.planes};
+    cuuint64_t stride[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(o.planes > 1 ? o.plane : o.ld * o.outer) * 2};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_outer, 1}, step[3] = {1, 1, 1};
+    return fn(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base),
+              dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
+              CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
+
+struct HgProblem {
+    int64_t M, N, K;
+    int batch = 1, passes = 1, planes_a = 1, planes_b = 1, splits = 1;
+    bool upper = false;
+    uint32_t* status = nullptr;
+    int prof = 0;
+    double ops = 0, bytes = 0;
+};
+
+// Splits of K that have work when `want` are asked for.
+inline int hg_splits(int64_t K, int want) {
+    const int kb = (int)((K + kHgBK - 1) / kHgBK);
+    const int per = (kb + want - 1) / want;
+    return (kb + per - 1) / per;
+}
+
+// Tile of a product: CTAs that work on one (1 or 2) and columns.
+struct HgPick {
+    int cg, bn;
+};
+
+inline int hg_tiles(const HgProblem& p, HgPick t) {
+    const int tm = 128 * t.cg;
+    const int64_t rows = (p.M + tm - 1) / tm, cols = (p.N + t.bn - 1) / t.bn;
+    if (!p.upper) return (int)(rows * cols * p.batch);
+    int64_t n = 0;
+    for (int64_t m = 0; m < rows; ++m) n += cols - m * tm / t.bn;
+    return (int)(n * p.batch);
+}
+
+// A pair where its 256 x 256 tiles fill the GPU, else a lone CTA with the tile width that
+// gives every SM a tile.
+inline HgPick hg_pick(const HgProblem& p) {
+    const int sms = sm_count();
+    if (hg_tiles(p, {2, 256}) * p.splits >= sms / 2) return {2, 256};
+    if (hg_tiles(p, {1, 256}) * p.splits >= sms) return {1, 256};
+    return {1, 128};
+}
+
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16>
+cudaError_t hg_launch_as(const HgProblem& p, const HgOperand& a, const HgOperand& b, const typename Epi::Args& ea,
+                         cudaStream_t s) {
+    using C = HgCfg<CG, BN>;
+    CUtensorMap ma, mb;
+    if (!hg_map(&ma, a, F16, AMN ? 64 : 128) || !hg_map(&mb, b, F16, BMN ? 64 : C::B_ROWS)) return cudaErrorInvalidValue;
+    HgArgs g{};
+    g.M = (int)p.M;
+    g.N = (int)p.N;
+    g.tiles_m = (int)((p.M + 128 * CG - 1) / (128 * CG));
+    g.tiles_n = (int)((p.N + BN - 1) / BN);
+    g.batch = p.batch;
+    g.kb_total = (int)((p.K + kHgBK - 1) / kHgBK);
+    g.kb_per_split = (g.kb_total + p.splits - 1) / p.splits;
+    g.splits = (g.kb_total + g.kb_per_split - 1) / g.kb_per_split;
+    g.total = hg_tiles(p, {CG, BN}) * g.splits;
+    g.passes = p.passes;
+    g.planes_a = p.planes_a;
+    g.planes_b = p.planes_b;
+    g.upper = p.upper ? 1 : 0;
+    g.band = 2048 / (128 * CG);
+    g.status = p.status;
+    static std::atomic<uint64_t> ready{0};
+    int dev = 0;
+    const int sms = sm_count(&dev);
+    const auto kernel = k_head_gemm<Epi, CG, BN, AMN, BMN, F16>;
+    const cudaError_t e = once_per_device(ready, dev, [kernel] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+    });
+    if (e != cudaSuccess) return e;
+    const int grid = std::min(g.total, sms / CG) * CG;
+    ProfScope ps(p.prof, s, p.ops, p.bytes);
+    if constexpr (CG == 2) return launch_cluster(kernel, dim3(grid), kHgThreads, 2, s, C::SMEM, ma, mb, g, ea);
+    else return launch_k(kernel, dim3(grid), dim3(kHgThreads), C::SMEM, s, ma, mb, g, ea);
+}
+
+// D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K.
+template <class Epi, bool AMN, bool BMN, bool F16>
+cudaError_t hg_launch(const HgPick& t, const HgProblem& p, const HgOperand& a, const HgOperand& b,
+                      const typename Epi::Args& ea, cudaStream_t s) {
+    if (t.cg == 2) return hg_launch_as<Epi, 2, 256, AMN, BMN, F16>(p, a, b, ea, s);
+    if (t.bn == 256) return hg_launch_as<Epi, 1, 256, AMN, BMN, F16>(p, a, b, ea, s);
+    return hg_launch_as<Epi, 1, 128, AMN, BMN, F16>(p, a, b, ea, s);
+}
+
+}  // namespace
+}  // namespace nitro

@@ -1,0 +1,622 @@
+// Softmax cross entropy of a linear head over many classes: z = scale x W^T,
+// loss_i = log sum_j exp z_ij - z_i,label, and its gradients
+//   G_ij = gout_i scale (softmax(z_i)_j - [j = label_i]),   dx = G W,   dW = G^T x.
+//
+// The logits are never kept.  The forward's products leave, for every row and tile, the
+// maximum and the sum of exponentials of the tile's columns, and a second kernel joins
+// them.  The backward walks over pieces of the classes: the products again, G of the
+// piece in bf16 from the row's log-sum, then the two products with it; dx sums over the
+// pieces in 32 bits.  The products are those of k_head_gemm (head_gemm.cuh), 2 rows
+// features classes operations each: one in the forward, three in the backward, of which
+// one is the logits' second time.  Keeping them instead would write and read 8 bytes a
+// logit more in 32 bits (16-bit logits are off by 2^-9 of their size, far too much under
+// an exponential).
+//
+// Few rows and classes leave fewer tiles than SMs; then the logits' sum is split along
+// the features into 32-bit slices of a small workspace, which the row kernels add up.
+#include <new>
+#include <vector>
+
+#include "head_gemm.cuh"
+
+using namespace nitro;
+
+namespace nitro {
+namespace {
+
+constexpr float kLog2e = 1.4426950408889634f, kLn2 = 0.6931471805599453f;
+
+__device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
+    const __nv_bfloat162 p = __floats2bfloat162_rn(a, b);
+    return *reinterpret_cast<const uint32_t*>(&p);
+}
+
+// 32 floats -> bf16 at dst, n of them valid; vec: dst is 16-byte aligned
+__device__ __forceinline__ void store_bf16_32(uint16_t* dst, const float* v, int n, bool vec) {
+    if (vec && n >= 32) {
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            reinterpret_cast<uint4*>(dst)[j] = make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
+                                                          pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
+        return;
+    }
+#pragma unroll
+    for (int j = 0; j < 32; ++j)
+        if (j < n) dst[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+}
+
+// ------------------------------------------------------------------ epilogues
+// Row statistics of a tile in base 2: (max, sum of 2^(t - max)), t = z log2 e, and the
+// label's logit.  A thread holds one row, so nothing is exchanged.
+struct EpiStats {
+    struct Args {
+        const int32_t* labels;
+        float k2, scale;      // scale log2 e
+        float2* part;         // [2 tiles_n][rows]
+        float* zt;            // [rows]
+    };
+    const Args& a;
+    const HgArgs& g;
+    int row, col0, slot, lab;
+    float mx = -INFINITY, sum = 0.0f;
+    __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int half)
+        : a(a_), g(g_), row(row_), col0(col0_) {
+        slot = 2 * t.n + half;
+        lab = row < g.M ? a.labels[row] : -1;
+    }
+    __device__ __forceinline__ void cols(int c, float* v) {
+        const int n = g.N - (col0 + c);
+        if (n <= 0) return;
+        float m = -INFINITY;
+        if (n < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : -INFINITY;
+        }
+#pragma unroll
+        for (int j = 0; j < 32; ++j) m = fmaxf(m, v[j]);
+        m = fmaxf(mx, m * a.k2);
+        const float base = m == -INFINITY ? 0.0f : m;
+        float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+        for (int j = 0; j < 32; j += 4) {
+            s0 += exp2f(fmaf(v[j], a.k2, -base));
+            s1 += exp2f(fmaf(v[j + 1], a.k2, -base));
+            s2 += exp2f(fmaf(v[j + 2], a.k2, -base));
+            s3 += exp2f(fmaf(v[j + 3], a.k2, -base));
+        }
+        sum = sum * exp2f(mx - base) + ((s0 + s1) + (s2 + s3));
+        mx = m;
+        const int at = lab - (col0 + c);
+        if (at >= 0 && at < 32 && at < n) {
+            float z = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; ++j) z = j == at ? v[j] : z;
+            a.zt[row] = z * a.scale;
+        }
+    }
+    __device__ __forceinline__ void done() {
+        if (row < g.M) a.part[(int64_t)slot * g.M + row] = make_float2(mx, sum);
+    }
+};
+
+// G of a piece: gout scale (2^(z log2 e - lse log2 e) - [label]), rounded once to bf16, the
+// type that the products with it take (its rounding is as large as the one of the
+// gradients that come out).  Rows that are left out give zeros.
+struct EpiProb {
+    struct Args {
+        const int32_t* labels;
+        const float* lse;
+        const float* gout;    // or null: 1
+        float k2, scale;
+        int classes, v0;      // all classes, and the piece's first
+        uint16_t* G;          // [rows][ldg], ldg a multiple of 64
+        int64_t ldg;
+    };
+    const Args& a;
+    const HgArgs& g;
+    int row, col0, lab = -1;
+    float l2 = 0.0f, gi = 0.0f;
+    bool live = false;
+    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
+        : a(a_), g(g_), row(row_), col0(col0_) {
+        if (row < g.M) {
+            lab = a.labels[row];
+            live = lab >= 0 && lab < a.classes;
+            lab -= a.v0;
+            l2 = a.lse[row] * kLog2e;
+            gi = a.scale * (a.gout ? a.gout[row] : 1.0f);
+        }
+    }
+    __device__ __forceinline__ void cols(int c, float* v) {
+        const int col = col0 + c;
+        if (row >= g.M || col >= g.N) return;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) {
+            const float p = exp2f(fmaf(v[j], a.k2, -l2)) - (col + j == lab ? 1.0f : 0.0f);
+            v[j] = live ? gi * p : 0.0f;
+        }
+        store_bf16_32(a.G + (int64_t)row * a.ldg + col, v, 32, true);   // the row's padding may be written
+    }
+    __device__ __forceinline__ void done() {}
+};
+
+// 32-bit sums into slice `split` of c, or added to what it holds.
+struct EpiAcc {
+    struct Args {
+        float* c;
+        int64_t ldc, slice;   // ldc a multiple of 32
+        int add;
+    };
+    const Args& a;
+    const HgArgs& g;
+    int row, col0;
+    float* dst;
+    __device__ __forceinline__ EpiAcc(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int)
+        : a(a_), g(g_), row(row_), col0(col0_) {
+        dst = a.c + t.split * a.slice + (int64_t)row * a.ldc + col0;
+    }
+    __device__ __forceinline__ void cols(int c, float* v) {
+        if (row >= g.M || col0 + c >= a.ldc) return;
+        float4* p = reinterpret_cast<float4*>(dst + c);
+        if (a.add) {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                const float4 o = p[j];
+                v[4 * j] += o.x;
+                v[4 * j + 1] += o.y;
+                v[4 * j + 2] += o.z;
+                v[4 * j + 3] += o.w;
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < 8; ++j) p[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+    }
+    __device__ __forceinline__ void done() {}
+};
+
+struct EpiBf16 {
+    struct Args {
+        uint16_t* c;
+        int64_t ldc;
+        int vec;              // rows are 16-byte aligned
+    };
+    const Args& a;
+    const HgArgs& g;
+    int row, col0;
+    __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
+        : a(a_), g(g_), row(row_), col0(col0_) {}
+    __device__ __forceinline__ void cols(int c, float* v) {
+        const int n = g.N - (col0 + c);
+        if (row >= g.M || n <= 0) return;
+        store_bf16_32(a.c + (int64_t)row * a.ldc + col0 + c, v, n, a.vec != 0);
+    }
+    __device__ __forceinline__ void done() {}
+};
+
+// ------------------------------------------------------------------ row kernels
+struct RowOut {
+    const int32_t* labels;
+    float* loss;
+    float* lse;
+    uint32_t* status;
+    int classes;
+};
+__device__ __forceinline__ void write_row(const RowOut& o, int64_t row, float m2, float sum, float zt) {
+    const float lse = (m2 + log2f(sum)) * kLn2;
+    const int lab = o.labels[row];
+    const bool live = lab >= 0 && lab < o.classes;
+    if (!live && lab != -1) atomicOr(o.status, ST_BAD_LABEL);
+    o.lse[row] = lse;
+    o.loss[row] = live ? lse - zt : 0.0f;
+}
+
+// Joins a row's tiles: 32 rows a CTA, the tiles over its warps.
+__global__ void __launch_bounds__(256) k_xent_join(const float2* part, int parts, int rows, const float* zt, const RowOut o) {
+    __shared__ float2 sh[8][32];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    float m = -INFINITY, s = 0.0f;
+    const auto join = [&](float2 p) {
+        const float t = fmaxf(m, p.x), base = t == -INFINITY ? 0.0f : t;
+        s = s * exp2f(m - base) + p.y * exp2f(p.x - base);
+        // a NaN among the logits is in its tile's sum, not in the maximum
+        m = t;
+    };
+    if (row < rows)
+        for (int i = w; i < parts; i += 8) join(part[(int64_t)i * rows + row]);
+    sh[w][lane] = make_float2(m, s);
+    __syncthreads();
+    if (w == 0 && row < rows) {
+        for (int i = 1; i < 8; ++i) join(sh[i][lane]);
+        const int lab = o.labels[row];
+        write_row(o, row, m, s, lab >= 0 && lab < o.classes ? zt[row] : 0.0f);
+    }
+}
+
+// From logits in `slices` parts: a CTA a row.
+__global__ void __launch_bounds__(256) k_xent_rows(const float* z, int64_t ldz, int64_t slice, int slices, int classes,
+                                                   float k2, float scale, const RowOut o) {
+    __shared__ float sm[8], ss[8];
+    pdl_wait();
+    const int64_t row = blockIdx.x;
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
+    const float* zr = z + row * ldz;
+    float m = -INFINITY, s = 0.0f;
+    for (int j = threadIdx.x; j < classes; j += 256) {
+        float v = zr[j];
+        for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
+        const float t = fmaxf(m, v * k2), base = t == -INFINITY ? 0.0f : t;
+        s = s * exp2f(m - base) + exp2f(fmaf(v, k2, -base));
+        m = t;
+    }
+    const auto join = [&](float om, float os) {
+        const float t = fmaxf(m, om), base = t == -INFINITY ? 0.0f : t;
+        s = s * exp2f(m - base) + os * exp2f(om - base);
+        m = t;
+    };
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) {
+        const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
+        join(om, os);
+    }
+    if (lane == 0) {
+        sm[w] = m;
+        ss[w] = s;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        for (int i = 1; i < 8; ++i) join(sm[i], ss[i]);
+        const int lab = o.labels[row];
+        float zt = 0.0f;
+        if (lab >= 0 && lab < classes) {
+            zt = zr[lab];
+            for (int k = 1; k < slices; ++k) zt += zr[k * slice + lab];
+        }
+        write_row(o, row, m, s, zt * scale);
+    }
+}
+
+// G from logits in slices, as EpiProb writes it (all classes, one piece); padding zero.
+__global__ void __launch_bounds__(256) k_xent_probs(const float* z, int64_t ldz, int64_t slice, int slices,
+                                                    const EpiProb::Args a) {
+    pdl_wait();
+    const int64_t row = blockIdx.x;
+    const int lab = a.labels[row];
+    const bool live = lab >= 0 && lab < a.classes;
+    const float l2 = a.lse[row] * kLog2e, gi = a.scale * (a.gout ? a.gout[row] : 1.0f);
+    const float* zr = z + row * ldz;
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < a.ldg; j += gridDim.y * 256) {
+        float v = 0.0f;
+        if (j < a.classes && live) {
+            v = zr[j];
+            for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
+            v = gi * (exp2f(fmaf(v, a.k2, -l2)) - (j == lab ? 1.0f : 0.0f));
+        }
+        a.G[row * a.ldg + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    }
+}
+
+// dx in bf16 from the slices of its 32-bit sums.
+__global__ void __launch_bounds__(256) k_xent_dx(const float* c, int64_t ldc, int64_t slice, int slices, int features,
+                                                 uint16_t* dx, int64_t lddx) {
+    pdl_wait();
+    const int64_t row = blockIdx.x;
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < features; j += gridDim.y * 256) {
+        float v = c[row * ldc + j];
+        for (int k = 1; k < slices; ++k) v += c[k * slice + row * ldc + j];
+        dx[row * lddx + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    }
+}
+
+// Rows of x as bf16 with a stride of ldp (a multiple of 8; padding zero): int8 activations
+// are exact in bf16.  labels (may be null): rows that are left out become zeros, so that
+// an infinity or NaN in them meets no weight gradient (0 times it is NaN).
+template <typename T>
+__global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
+                                                   const int32_t* labels, int classes) {
+    pdl_wait();
+    const int64_t words = (int64_t)rows * (ldp / 8);
+    const bool vec = sizeof(T) == 2 ? (((uintptr_t)x | (uintptr_t)(ldx * 2)) & 15) == 0
+                                    : (((uintptr_t)x | (uintptr_t)ldx) & 7) == 0;
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) {
+        const int row = (int)(i / (ldp / 8)), c = (int)(i - (int64_t)row * (ldp / 8)) * 8;
+        uint4 v = make_uint4(0, 0, 0, 0);
+        const int lab = labels ? labels[row] : 0;
+        if (!labels || (lab >= 0 && lab < classes)) {
+            const T* src = x + row * ldx + c;
+            uint32_t* w = reinterpret_cast<uint32_t*>(&v);
+            if constexpr (sizeof(T) == 2) {
+                if (vec && c + 8 <= cols) v = *reinterpret_cast<const uint4*>(src);
+                else
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < cols) w[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+            } else {
+                uint32_t b[2] = {0x80808080u, 0x80808080u};   // bytes hold x + 128
+                if (vec && c + 8 <= cols) {
+                    const uint2 r = *reinterpret_cast<const uint2*>(src);
+                    b[0] ^= r.x;
+                    b[1] ^= r.y;
+                } else {
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < cols) b[j >> 2] ^= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
+                }
+#pragma unroll
+                for (int j = 0; j < 4; ++j) w[j] = bf16x2(b[j >> 1], 2 * (j & 1));
+            }
+        }
+        reinterpret_cast<uint4*>(out)[i] = v;
+    }
+}
+
+int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
+constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
+
+}  // namespace
+}  // namespace nitro
+
+struct nitro_xent {
+    int max_rows = 0, features = 0, classes = 0;
+    int64_t ldp = 0, g_elems = 0, acc_floats = 0;
+    uint16_t* xp = nullptr;     // [max_rows][ldp] bf16 copy of x
+    uint16_t* wp = nullptr;     // [classes][ldp] copy of W where its rows are not aligned for TMA
+    uint16_t* G = nullptr;
+    float* acc = nullptr;
+    float2* part = nullptr;
+    float* zt = nullptr;
+    uint32_t* status = nullptr;
+    std::vector<void*> allocs;
+};
+
+namespace {
+
+template <typename T>
+bool xalloc(nitro_xent* h, T** p, int64_t count) {
+    void* q = nullptr;
+    if (cudaMalloc(&q, (size_t)count * sizeof(T)) != cudaSuccess) return false;
+    h->allocs.push_back(q);
+    *p = static_cast<T*>(q);
+    return true;
+}
+
+#define TRY(expr)                                         \
+    do {                                                  \
+        if ((expr) != cudaSuccess) return NITRO_ERR_CUDA; \
+    } while (0)
+
+bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
+
+cudaError_t pack_x(const nitro_xent* h, const void* x, int type, int64_t ldx, int rows, uint16_t* out,
+                   const int32_t* labels, cudaStream_t s) {
+    const int64_t words = (int64_t)rows * (h->ldp / 8);
+    const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
+    ProfScope ps(K_XENT_PACK, s, 0.0, (double)rows * h->features * (type == NITRO_I8 ? 3 : 4));
+    if (type == NITRO_I8)
+        return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, h->features, out,
+                        h->ldp, labels, h->classes);
+    return launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, h->features, out,
+                    h->ldp, labels, h->classes);
+}
+
+// x and W as operands of the logits' product (K = features, both along K).
+nitro_status xent_operands(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
+                           int rows, const int32_t* labels, bool pack, cudaStream_t s, HgOperand* ox, HgOperand* ow) {
+    const int F = h->features;
+    if (pack || x_type == NITRO_I8 || !tma_rows(x, ldx)) {
+        TRY(pack_x(h, x, x_type, ldx, rows, h->xp, labels, s));
+        *ox = {h->xp, F, rows, h->ldp, 1, 0};
+    } else {
+        *ox = {x, F, rows, ldx, 1, 0};
+    }
+    if (!tma_rows(w, ldw)) {
+        const int64_t words = (int64_t)h->classes * (h->ldp / 8);
+        const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
+        ProfScope ps(K_XENT_PACK, s, 0.0, 4.0 * h->classes * F);
+        TRY(launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, w, ldw, h->classes, F, h->wp, h->ldp,
+                     (const int32_t*)nullptr, 0));
+        *ow = {h->wp, F, h->classes, h->ldp, 1, 0};
+    } else {
+        *ow = {w, F, h->classes, ldw, 1, 0};
+    }
+    return NITRO_OK;
+}
+
+bool xent_args(const nitro_xent* h, const void* x, int x_type, int64_t ldx, const void* w, int64_t ldw,
+               const int32_t* labels, int rows, float scale) {
+    if (!h || rows < 0 || rows > h->max_rows || (x_type != NITRO_BF16 && x_type != NITRO_I8)) return false;
+    if (ldx < h->features || ldw < h->features || !(scale > 0.0f) || scale > 1e30f) return false;
+    if (rows > 0 && (!x || !w || !labels)) return false;
+    return ((uintptr_t)w & 1) == 0 && (x_type == NITRO_I8 || ((uintptr_t)x & 1) == 0);
+}
+
+// Whether the logits go through slices, and how many: where 128 x 128 tiles are fewer than
+// half the SMs.
+int xent_slices(const nitro_xent* h, int rows) {
+    const int sms = sm_count();
+    HgProblem p{rows, h->classes, h->features};
+    const int tiles = hg_tiles(p, {1, 128});
+    if (2 * tiles > sms) return 0;
+    const int64_t most = h->acc_floats / (rows * round_up(h->classes, 32));
+    const int want = (int)std::min<int64_t>({(int64_t)(sms / tiles), most, (int64_t)((h->features + 127) / 128)});
+    return want < 2 ? 0 : hg_splits(h->features, want);
+}
+
+cudaError_t xent_logit_slices(nitro_xent* h, const HgOperand& ox, const HgOperand& ow, int rows, int slices, cudaStream_t s) {
+    HgProblem p{rows, h->classes, h->features};
+    p.splits = slices;
+    p.status = h->status;
+    p.prof = K_XENT_LOGITS;
+    p.ops = 2.0 * rows * h->classes * h->features;
+    const int64_t ldz = round_up(h->classes, 32);
+    const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
+    return hg_launch<EpiAcc, false, false, false>({1, 128}, p, ox, ow, ea, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xent** out) {
+    if (!out) return NITRO_ERR_ARG;
+    *out = nullptr;
+    if (max_rows < 1 || features < 1 || classes < 1 || max_rows > (1 << 20) || features > (1 << 17) ||
+        classes > (1 << 24) || (int64_t)max_rows * features > ((int64_t)1 << 34) ||
+        (int64_t)classes * features > ((int64_t)1 << 36))
+        return NITRO_ERR_ARG;
+    nitro_xent* h = new (std::nothrow) nitro_xent();
+    if (!h) return NITRO_ERR_CUDA;
+    h->max_rows = max_rows;
+    h->features = features;
+    h->classes = classes;
+    h->ldp = round_up(features, 8);
+    h->g_elems = std::min(max_rows * round_up(classes, 64), std::max(kGElems, (int64_t)max_rows * 256));
+    h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
+    const int64_t parts = 2 * ((classes + 127) / 128);
+    const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
+                    xalloc(h, &h->G, h->g_elems) && xalloc(h, &h->acc, h->acc_floats) &&
+                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->status, 1) && cudaMemset(h->status, 0, 4) == cudaSuccess;
+    if (!ok) {
+        nitro_xent_destroy(h);
+        return NITRO_ERR_CUDA;
+    }
+    *out = h;
+    return NITRO_OK;
+}
+
+nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
+                                const int32_t* labels, int rows, float scale, float* loss, float* lse, void* stream) {
+    if (!xent_args(h, x, x_type, ldx, w, ldw, labels, rows, scale)) return NITRO_ERR_ARG;
+    if (rows == 0) return NITRO_OK;
+    if (!loss || !lse) return NITRO_ERR_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    HgOperand ox, ow;
+    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, nullptr, false, s, &ox, &ow);
+    if (st != NITRO_OK) return st;
+    const RowOut ro{labels, loss, lse, h->status, h->classes};
+    const int slices = xent_slices(h, rows);
+    if (slices) {
+        TRY(xent_logit_slices(h, ox, ow, rows, slices, s));
+        const int64_t ldz = round_up(h->classes, 32);
+        ProfScope ps(K_XENT_ROWS, s, 0.0, 4.0 * slices * rows * h->classes);
+        TRY(launch_k(k_xent_rows, dim3(rows), dim3(256), 0, s, (const float*)h->acc, ldz, rows * ldz, slices, h->classes,
+                     scale * kLog2e, scale, ro));
+        return NITRO_OK;
+    }
+    HgProblem p{rows, h->classes, h->features};
+    p.status = h->status;
+    p.prof = K_XENT_LOGITS;
+    p.ops = 2.0 * rows * h->classes * h->features;
+    const HgPick t = hg_pick(p);
+    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, h->zt};
+    TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
+    const int parts = 2 * ((h->classes + t.bn - 1) / t.bn);
+    ProfScope ps(K_XENT_ROWS, s, 0.0, 8.0 * parts * rows);
+    TRY(launch_k(k_xent_join, dim3((rows + 31) / 32), dim3(256), 0, s, (const float2*)h->part, parts, rows,
+                 (const float*)h->zt, ro));
+    return NITRO_OK;
+}
+
+nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
+                                 const int32_t* labels, int rows, float scale, const float* lse, const float* gout,
+                                 uint16_t* dx, int64_t lddx, uint16_t* dw, int64_t lddw, void* stream) {
+    if (!xent_args(h, x, x_type, ldx, w, ldw, labels, rows, scale)) return NITRO_ERR_ARG;
+    if ((dx && (lddx < h->features || ((uintptr_t)dx & 1))) || (dw && (lddw < h->features || ((uintptr_t)dw & 1))))
+        return NITRO_ERR_ARG;
+    if (rows > 0 && !lse) return NITRO_ERR_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int F = h->features, V = h->classes;
+    if (rows == 0) {   // an empty batch has a weight gradient of zero
+        for (int64_t v = 0; dw && v < V; v += lddw == F ? V : 1)
+            TRY(cudaMemsetAsync(dw + v * lddw, 0, sizeof(uint16_t) * F * (size_t)(lddw == F ? V : 1), s));
+        return NITRO_OK;
+    }
+    if (!dx && !dw) return NITRO_OK;
+    HgOperand ox, ow;
+    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, labels, true, s, &ox, &ow);
+    if (st != NITRO_OK) return st;
+    const float k2 = scale * kLog2e;
+    const int slices = xent_slices(h, rows);
+    int64_t piece = std::min<int64_t>(round_up(V, 64), h->g_elems / rows / 64 * 64);
+    if (piece < V) piece = piece / 256 * 256;
+    // dx: slices along the classes where its tiles leave SMs idle
+    HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
+    const int64_t ldc = round_up(F, 32);
+    int dsplit = 1;
+    {
+        const int tiles = hg_tiles(pd, {1, 128}), sms = sm_count();
+        if (2 * tiles <= sms)
+            dsplit = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(sms / tiles), h->acc_floats / (rows * ldc), pd.K / 256}));
+        dsplit = hg_splits(pd.K, dsplit);
+    }
+    for (int64_t v0 = 0; v0 < V; v0 += piece) {
+        const int64_t n = std::min<int64_t>(piece, V - v0);
+        HgOperand wp = ow;
+        wp.base = static_cast<const uint16_t*>(ow.base) + v0 * ow.ld;
+        wp.outer = n;
+        const EpiProb::Args ep{labels, lse, gout, k2, scale, V, (int)v0, h->G, round_up(n, 64)};
+        if (slices && piece >= V) {
+            TRY(xent_logit_slices(h, ox, ow, rows, slices, s));
+            const int64_t ldz = round_up(V, 32);
+            ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * slices + 2.0) * rows * V);
+            TRY(launch_k(k_xent_probs, dim3(rows, (unsigned)std::min<int64_t>(8, (ep.ldg + 255) / 256)), dim3(256), 0, s,
+                         (const float*)h->acc, ldz, rows * ldz, slices, ep));
+        } else {
+            HgProblem p{rows, n, F};
+            p.status = h->status;
+            p.prof = K_XENT_LOGITS;
+            p.ops = 2.0 * rows * n * F;
+            TRY((hg_launch<EpiProb, false, false, false>(hg_pick(p), p, ox, wp, ep, s)));
+        }
+        const HgOperand G{h->G, n, rows, ep.ldg, 1, 0};
+        if (dx) {
+            HgProblem p{rows, F, n};
+            p.status = h->status;
+            p.prof = K_XENT_DX;
+            p.ops = 2.0 * rows * n * F;
+            p.splits = hg_splits(n, dsplit);
+            const HgPick t = dsplit > 1 ? HgPick{1, 128} : hg_pick(p);
+            if (piece >= V && dsplit == 1) {
+                const EpiBf16::Args eb{dx, lddx, tma_rows(dx, lddx)};
+                TRY((hg_launch<EpiBf16, false, true, false>(t, p, G, wp, eb, s)));
+            } else {
+                // a last piece with fewer slices adds to the first ones
+                const EpiAcc::Args ea{h->acc, ldc, rows * ldc, v0 > 0};
+                TRY((hg_launch<EpiAcc, false, true, false>(t, p, G, wp, ea, s)));
+            }
+        }
+        if (dw) {
+            HgProblem p{n, F, rows};
+            p.status = h->status;
+            p.prof = K_XENT_DW;
+            p.ops = 2.0 * rows * n * F;
+            const EpiBf16::Args eb{dw + v0 * lddw, lddw, tma_rows(dw, lddw)};
+            TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, G, ox, eb, s)));
+        }
+    }
+    if (dx && (piece < V || dsplit > 1)) {
+        ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * dsplit + 2.0) * rows * F);
+        TRY(launch_k(k_xent_dx, dim3(rows, (unsigned)std::min(8, (F + 255) / 256)), dim3(256), 0, s, (const float*)h->acc,
+                     ldc, rows * ldc, dsplit, F, dx, lddx));
+    }
+    return NITRO_OK;
+}
+
+nitro_status nitro_xent_status(nitro_xent* h, int clear) {
+    if (!h) return NITRO_ERR_ARG;
+    uint32_t bits = 0;
+    if (cudaDeviceSynchronize() != cudaSuccess ||
+        cudaMemcpy(&bits, h->status, 4, cudaMemcpyDeviceToHost) != cudaSuccess ||
+        (clear && cudaMemset(h->status, 0, 4) != cudaSuccess))
+        return NITRO_ERR_CUDA;
+    return bits & ST_TIMEOUT ? NITRO_ERR_TIMEOUT : bits & ST_BAD_LABEL ? NITRO_ERR_ARG : NITRO_OK;
+}
+
+void nitro_xent_destroy(nitro_xent* h) {
+    if (!h) return;
+    cudaDeviceSynchronize();
+    for (void* p : h->allocs) cudaFree(p);
+    delete h;
+}
+
+}  // extern "C"

@@ -38,6 +38,18 @@ enum KernelId : int {
     K_LRPOOL_TO_DELTA,
     K_TC_PROBE,
     K_TC_LIN_WGRAD,
+    K_XENT_PACK,
+    K_XENT_LOGITS,
+    K_XENT_ROWS,
+    K_XENT_DX,
+    K_XENT_DW,
+    K_ORTH_PACK,
+    K_ORTH_GRAM,
+    K_ORTH_SQUARE,
+    K_ORTH_UPDATE,
+    K_MX4_QUANTIZE,
+    K_MX4_DEQUANTIZE,
+    K_MX4_LINEAR,
     K_COUNT
 };
 
