@@ -501,31 +501,44 @@ class IntPrep:
 
 
 # ---------------------------------------------------------------- floating-point head
-def _dtype(t, allowed):
-    """The NITRO_* type of a torch tensor; ValueError if it is none of `allowed`."""
-    import torch
-    code = {torch.bfloat16: NITRO_BF16, torch.int8: NITRO_I8, torch.float32: NITRO_F32,
-            torch.int64: NITRO_I64}.get(t.dtype)
-    if code not in allowed:
-        raise ValueError("a tensor of type %s is not supported here" % t.dtype)
-    return code
+_codes = {}     # torch dtype -> NITRO_* type (int32 and uint8: codes of this module's own)
+_INT32, _UINT8 = -1, -2
+
+
+def _code(t):
+    """The type of a torch tensor as a code; None if the library knows none."""
+    c = _codes.get(t.dtype)
+    if c is None and not _codes:
+        import torch
+        _codes.update({torch.bfloat16: NITRO_BF16, torch.int8: NITRO_I8, torch.float32: NITRO_F32,
+                       torch.int64: NITRO_I64, torch.int32: _INT32, torch.uint8: _UINT8})
+        c = _codes.get(t.dtype)
+    return c
 
 
 def _matrix(t, rows, cols, allowed, what):
-    """(type, row stride) of a CUDA matrix [rows x cols] whose rows are contiguous."""
-    if not t.is_cuda or t.dim() != 2 or tuple(t.shape) != (rows, cols):
+    """(address, type, row stride) of a CUDA matrix [rows x cols] whose rows are contiguous."""
+    if not t.is_cuda or t.shape != (rows, cols):
         raise ValueError("%s must be a CUDA tensor [%d x %d]" % (what, rows, cols))
-    if cols > 1 and t.stride(1) != 1:
+    ld, step = t.stride()
+    if step != 1 and cols > 1:
         raise ValueError("the rows of %s must be contiguous" % what)
+    code = _code(t)
+    if code not in allowed:
+        raise ValueError("%s cannot be of type %s" % (what, t.dtype))
     # the stride of a lone row is never used
-    return _dtype(t, allowed), max(t.stride(0), cols) if rows <= 1 else t.stride(0)
+    return t.data_ptr(), code, max(ld, cols) if rows <= 1 else ld
 
 
-def _vector(t, n, dtype, what):
-    import torch
-    if not t.is_cuda or t.dtype != getattr(torch, dtype) or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor of %d %s" % (what, n, dtype))
-    return _ptr(t)
+def _vector(t, n, code, what):
+    if not t.is_cuda or _code(t) != code or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of %d values of its type (not %s)"
+                         % (what, n, t.dtype))
+    return t.data_ptr()
+
+
+_X, _W, _ORTH = (NITRO_BF16, NITRO_I8), (NITRO_BF16,), (NITRO_BF16, NITRO_F32, NITRO_I64)
+_MX4 = (NITRO_BF16, NITRO_F32)
 
 
 class _Handle:
@@ -566,15 +579,15 @@ class SoftmaxXent(_Handle):
 
     def _inputs(self, x, w, labels):
         n = x.shape[0]
-        xt, ldx = _matrix(x, n, self.features, (NITRO_BF16, NITRO_I8), "x")
-        _, ldw = _matrix(w, self.classes, self.features, (NITRO_BF16,), "w")
-        return n, [_ptr(x), xt, ldx, _ptr(w), ldw, _vector(labels, n, "int32", "labels"), n]
+        xp, xt, ldx = _matrix(x, n, self.features, _X, "x")
+        wp, _, ldw = _matrix(w, self.classes, self.features, _W, "w")
+        return n, (xp, xt, ldx, wp, ldw, _vector(labels, n, _INT32, "labels"), n)
 
     def forward(self, x, w, labels, loss, lse, scale=1.0, stream=None):
         """Writes the rows' losses and log-sums (fp32 [rows]); returns loss."""
         n, a = self._inputs(x, w, labels)
-        st = lib().nitro_xent_forward(self.h, *a, float(scale), _vector(loss, n, "float32", "loss"),
-                                      _vector(lse, n, "float32", "lse"), _stream_ptr(stream))
+        st = lib().nitro_xent_forward(self.h, *a, scale, _vector(loss, n, NITRO_F32, "loss"),
+                                      _vector(lse, n, NITRO_F32, "lse"), _stream_ptr(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_xent_forward")
         return loss
@@ -584,11 +597,15 @@ class SoftmaxXent(_Handle):
         None) from the lse of a forward on the same inputs; gout: the gradient of each
         row's loss (fp32), None for ones."""
         n, a = self._inputs(x, w, labels)
-        lddx = _matrix(dx, n, self.features, (NITRO_BF16,), "dx")[1] if dx is not None else self.features
-        lddw = _matrix(dw, self.classes, self.features, (NITRO_BF16,), "dw")[1] if dw is not None else self.features
-        st = lib().nitro_xent_backward(self.h, *a, float(scale), _vector(lse, n, "float32", "lse"),
-                                       None if gout is None else _vector(gout, n, "float32", "gout"),
-                                       _ptr(dx), lddx, _ptr(dw), lddw, _stream_ptr(stream))
+        dxp = dwp = None
+        lddx = lddw = self.features
+        if dx is not None:
+            dxp, _, lddx = _matrix(dx, n, self.features, _W, "dx")
+        if dw is not None:
+            dwp, _, lddw = _matrix(dw, self.classes, self.features, _W, "dw")
+        st = lib().nitro_xent_backward(self.h, *a, scale, _vector(lse, n, NITRO_F32, "lse"),
+                                       None if gout is None else _vector(gout, n, NITRO_F32, "gout"),
+                                       dxp, lddx, dwp, lddw, _stream_ptr(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_xent_backward")
         return dx, dw
@@ -605,16 +622,17 @@ class Orthogonalizer(_Handle):
     def run(self, m, out, steps=5, coef=None, stream=None):
         """m: [rows x cols] or [count x rows x cols] in bf16, fp32 or int64; out: bf16 of the
         same shape.  coef: (a, b, c) of the step, None for the default."""
-        a, b = (t.unsqueeze(0) if t.dim() == 2 else t for t in (m, out))
-        if b.shape != a.shape or a.dim() != 3 or tuple(a.shape[1:]) != (self.rows, self.cols):
+        a, b = (m.unsqueeze(0), out.unsqueeze(0)) if m.dim() == 2 and out.dim() == 2 else (m, out)
+        n = a.shape[0]
+        if a.dim() != 3 or b.shape != a.shape or a.shape != (n, self.rows, self.cols):
             raise ValueError("m and out must be [count x %d x %d]" % (self.rows, self.cols))
-        n, ld = a.shape[0], [self.cols, self.cols]
-        types = [NITRO_BF16, NITRO_BF16]
+        mt = ot = NITRO_BF16
+        ldm = ldo = self.cols
         if n:
-            types[0], ld[0] = _matrix(a[0], self.rows, self.cols, (NITRO_BF16, NITRO_F32, NITRO_I64), "m")
-            types[1], ld[1] = _matrix(b[0], self.rows, self.cols, (NITRO_BF16,), "out")
+            _, mt, ldm = _matrix(a[0], self.rows, self.cols, _ORTH, "m")
+            _, ot, ldo = _matrix(b[0], self.rows, self.cols, _W, "out")
         k = None if coef is None else (ctypes.c_float * 3)(*coef)
-        st = lib().nitro_orth_run(self.h, _ptr(m), types[0], ld[0], a.stride(0), n, int(steps), k, _ptr(out), ld[1],
+        st = lib().nitro_orth_run(self.h, a.data_ptr(), mt, ldm, a.stride(0), n, steps, k, b.data_ptr(), ldo,
                                   b.stride(0), _stream_ptr(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_orth_run")
@@ -622,25 +640,22 @@ class Orthogonalizer(_Handle):
 
 
 def mx4_bytes(rows, cols):
-    """(bytes of codes, bytes of scales) of a 4-bit matrix [rows x cols]."""
-    q, s = ctypes.c_size_t(), ctypes.c_size_t()
-    st = lib().nitro_mx4_bytes(int(rows), int(cols), ctypes.byref(q), ctypes.byref(s))
-    if st != NITRO_OK:
-        raise NitroError(st, "nitro_mx4_bytes")
-    return q.value, s.value
+    """(bytes of codes, bytes of scales) of a 4-bit matrix [rows x cols]: nitro_mx4_bytes."""
+    blocks = -(-cols // 32)
+    return rows * blocks * 16, -(-rows // 128) * -(-blocks // 4) * 512
 
 
 def _mx4_buffers(codes, scales, rows, cols):
     nq, ns = mx4_bytes(rows, cols)
-    return [_vector(codes, nq, "uint8", "codes"), _vector(scales, ns, "uint8", "scales")]
+    return _vector(codes, nq, _UINT8, "codes"), _vector(scales, ns, _UINT8, "scales")
 
 
 def mx4_quantize(x, codes, scales, stream=None):
     """x (bf16 or fp32) [rows x cols] as 4-bit codes and block scales (uint8, mx4_bytes)."""
     rows, cols = x.shape
-    t, ld = _matrix(x, rows, cols, (NITRO_BF16, NITRO_F32), "x")
-    st = lib().nitro_mx4_quantize(_ptr(x), t, ld, rows, cols, *_mx4_buffers(codes, scales, rows, cols),
-                                  _stream_ptr(stream))
+    xp, t, ld = _matrix(x, rows, cols, _MX4, "x")
+    q, s = _mx4_buffers(codes, scales, rows, cols)
+    st = lib().nitro_mx4_quantize(xp, t, ld, rows, cols, q, s, _stream_ptr(stream))
     if st != NITRO_OK:
         raise NitroError(st, "nitro_mx4_quantize")
     return codes, scales
@@ -649,10 +664,10 @@ def mx4_quantize(x, codes, scales, stream=None):
 def mx4_dequantize(codes, scales, out, scale_values=None, stream=None):
     """The values as out (bf16 or fp32) [rows x cols]; scale_values: fp32 [rows x blocks] or None."""
     rows, cols = out.shape
-    t, ld = _matrix(out, rows, cols, (NITRO_BF16, NITRO_F32), "out")
-    sv = None if scale_values is None else _vector(scale_values, rows * -(-cols // 32), "float32", "scale_values")
-    st = lib().nitro_mx4_dequantize(*_mx4_buffers(codes, scales, rows, cols), rows, cols, _ptr(out), t, ld, sv,
-                                    _stream_ptr(stream))
+    op, t, ld = _matrix(out, rows, cols, _MX4, "out")
+    q, s = _mx4_buffers(codes, scales, rows, cols)
+    sv = None if scale_values is None else _vector(scale_values, rows * -(-cols // 32), NITRO_F32, "scale_values")
+    st = lib().nitro_mx4_dequantize(q, s, rows, cols, op, t, ld, sv, _stream_ptr(stream))
     if st != NITRO_OK:
         raise NitroError(st, "nitro_mx4_dequantize")
     return out
@@ -668,10 +683,10 @@ class Mx4Linear(_Handle):
 
     def run(self, x, codes, scales, y, stream=None):
         n = x.shape[0]
-        xt, ldx = _matrix(x, n, self.in_features, (NITRO_BF16, NITRO_F32), "x")
-        yt, ldy = _matrix(y, n, self.out_features, (NITRO_BF16, NITRO_F32), "y")
-        st = lib().nitro_mx4_linear(self.h, _ptr(x), xt, ldx, n, *_mx4_buffers(codes, scales, self.out_features, self.in_features),
-                                    _ptr(y), yt, ldy, _stream_ptr(stream))
+        xp, xt, ldx = _matrix(x, n, self.in_features, _MX4, "x")
+        yp, yt, ldy = _matrix(y, n, self.out_features, _MX4, "y")
+        q, s = _mx4_buffers(codes, scales, self.out_features, self.in_features)
+        st = lib().nitro_mx4_linear(self.h, xp, xt, ldx, n, q, s, yp, yt, ldy, _stream_ptr(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_mx4_linear")
         return y

@@ -1,11 +1,12 @@
 // The contraction kernel of the floating-point head: D = A B^T on the tcgen05 tensor
 // cores with 16-bit operands, 32-bit sums and an epilogue of the caller's.
 //
-// D[m][n] = sum over passes p and k of A_p[m][k] B_p[n][k].  Each operand is a tensor
-// map of rank 3 over planes of a matrix, stored either along K (inner dimension k) or
-// along M / N (inner dimension m or n); the planes are the matrices of a batch and, for
-// operands that are split into a high and a low half, the halves.  Everything past a
-// matrix's end reads as zero (the maps' bounds).
+// D[m][n] = sum_k A[m][k] B[n][k].  Each operand is a tensor map of rank 3 over planes of a
+// matrix, stored either along K (inner dimension k) or along M / N (inner dimension m or n).
+// An operand may be split into a high and a low half (HA, HB = 2 planes a matrix); then
+// D = high high + high low + low high, each half loaded once.  The planes of a batch's
+// matrices follow one another.  Everything past a matrix's end reads as zero (the maps'
+// bounds).
 //
 // One persistent CTA an SM: warp 0 loads tiles of 64 along K by TMA into a ring of
 // shared-memory stages, warp 1 issues the MMAs, warps 4..11 drain the sums from TMEM
@@ -24,6 +25,7 @@
 #include <cuda_fp16.h>
 
 #include <algorithm>
+#include <cstdint>
 
 #include "prof.cuh"
 #include "tc_ptx.cuh"
@@ -40,8 +42,7 @@ struct HgArgs {
     int M, N;                  // valid rows and columns of D
     int tiles_m, tiles_n, splits, batch, total;
     int kb_total, kb_per_split;   // K blocks of a pass, of a split
-    int passes;                // 1, or 3: high x high, high x low, low x high halves
-    int planes_a, planes_b;    // planes a matrix of the batch has
+    int planes_a, planes_b;    // planes that a matrix of the batch has
     int upper;                 // symmetric D: only tiles that reach the diagonal or lie right of it
     int band;                  // row tiles that are walked together
     uint32_t* status;
@@ -81,13 +82,13 @@ __device__ __forceinline__ HgTile hg_decode(const HgArgs& g, int idx) {
     return t;
 }
 
-template <int CG, int BN>
+template <int CG, int BN, int HA, int HB>
 struct HgCfg {
     static constexpr int A_BYTES = 128 * 128;
     static constexpr int B_ROWS = BN / CG;
     static constexpr int B_BYTES = B_ROWS * 128;
-    static constexpr int STAGE = A_BYTES + B_BYTES;
-    static constexpr int S = STAGE > 40000 ? 4 : 6;
+    static constexpr int STAGE = HA * A_BYTES + HB * B_BYTES;
+    static constexpr int S = 229376 / STAGE < 8 ? 229376 / STAGE : 8;      // 2 to 8
     static constexpr int SMEM = S * STAGE + 1024 + 256;
     static constexpr int TCOLS = 2 * BN;
 };
@@ -151,16 +152,36 @@ __device__ __forceinline__ void mbar_drain(uint32_t bar, uint32_t parity, uint64
     }
 }
 
+// TMEM columns: taken (their address goes to shared memory) and given back by one warp, of
+// both CTAs where they work as a pair
+template <int CG>
+__device__ __forceinline__ void hg_tmem_alloc(uint32_t slot, uint32_t cols) {
+    if constexpr (CG == 2) {
+        asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
+    } else {
+        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(slot), "r"(cols) : "memory");
+        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
+    }
+}
+template <int CG>
+__device__ __forceinline__ void hg_tmem_free(uint32_t tmem, uint32_t cols) {
+    if constexpr (CG == 2)
+        asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+    else
+        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
+}
+
 // Epi: struct Args, and per tile and thread
 //   Epi(args, g, tile, row, col0, half)   row: this thread's row of D; col0: its first
 //       column, that of the tile's half 0 or 1
 //   void cols(c, v)                 v[0..32): columns col0 + c .. col0 + c + 31
 //   void done()
-template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16>
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB>
 __global__ void __launch_bounds__(kHgThreads, 1)
     k_head_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const HgArgs g,
                 const __grid_constant__ typename Epi::Args ea) {
-    using C = HgCfg<CG, BN>;
+    using C = HgCfg<CG, BN, HA, HB>;
     constexpr int S = C::S, TM = 128 * CG;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -191,19 +212,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) {
-        if constexpr (CG == 2) {
-            asm volatile("tcgen05.alloc.cta_group::2.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                         "r"(C::TCOLS)
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::2.sync.aligned;" ::: "memory");
-        } else {
-            asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                         "r"(C::TCOLS)
-                         : "memory");
-            asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-        }
-    }
+    if (warp == 2) hg_tmem_alloc<CG>(smem_u32(tmem_slot), C::TCOLS);
     if (warp == 0 && lane == 0) {
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmA)) : "memory");
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&tmB)) : "memory");
@@ -224,33 +233,39 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             for (int tile = unit; tile < g.total; tile += units) {
                 const HgTile T = hg_decode<TM, BN>(g, tile);
                 const int m0 = T.m * TM + rank * 128, n0 = T.n * BN + rank * C::B_ROWS;
-                for (int p = 0; p < g.passes; ++p) {
-                    const int za = T.batch * g.planes_a + (p == 2), zb = T.batch * g.planes_b + (p == 1);
-                    for (int kb = T.kb0; kb < T.kb1; ++kb) {
-                        if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
-                        const uint32_t a_dst = s0 + st * C::STAGE, b_dst = a_dst + C::A_BYTES;
-                        uint32_t fb = full_bar(st);
-                        if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
-                        if constexpr (CG == 2) fb = remote_smem(fb, 0);
+                for (int kb = T.kb0; kb < T.kb1; ++kb) {
+                    if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
+                    const uint32_t a_dst = s0 + st * C::STAGE, b_dst = a_dst + HA * C::A_BYTES;
+                    uint32_t fb = full_bar(st);
+                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
+                    if constexpr (CG == 2) fb = remote_smem(fb, 0);
+#pragma unroll
+                    for (int h = 0; h < HA; ++h) {
+                        const uint32_t dst = a_dst + h * C::A_BYTES;
+                        const int z = T.batch * g.planes_a + h;
                         if constexpr (AMN) {
 #pragma unroll
-                            for (int j = 0; j < 2; ++j)
-                                hg_tma<CG>(a_dst + j * 8192, &tmA, fb, m0 + 64 * j, kb * kHgBK, za);
+                            for (int j = 0; j < 2; ++j) hg_tma<CG>(dst + j * 8192, &tmA, fb, m0 + 64 * j, kb * kHgBK, z);
                         } else {
-                            hg_tma<CG>(a_dst, &tmA, fb, kb * kHgBK, m0, za);
+                            hg_tma<CG>(dst, &tmA, fb, kb * kHgBK, m0, z);
                         }
+                    }
+#pragma unroll
+                    for (int h = 0; h < HB; ++h) {
+                        const uint32_t dst = b_dst + h * C::B_BYTES;
+                        const int z = T.batch * g.planes_b + h;
                         if constexpr (BMN) {
 #pragma unroll
                             for (int j = 0; j < C::B_ROWS / 64; ++j)
-                                hg_tma<CG>(b_dst + j * 8192, &tmB, fb, n0 + 64 * j, kb * kHgBK, zb);
+                                hg_tma<CG>(dst + j * 8192, &tmB, fb, n0 + 64 * j, kb * kHgBK, z);
                         } else {
-                            hg_tma<CG>(b_dst, &tmB, fb, kb * kHgBK, n0, zb);
+                            hg_tma<CG>(dst, &tmB, fb, kb * kHgBK, n0, z);
                         }
-                        ++loaded;
-                        if (++st == S) {
-                            st = 0;
-                            ph ^= 1u;
-                        }
+                    }
+                    ++loaded;
+                    if (++st == S) {
+                        st = 0;
+                        ph ^= 1u;
                     }
                 }
             }
@@ -267,7 +282,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             constexpr uint32_t idesc = hg_idesc(F16, TM, BN, AMN, BMN);
             const uint32_t s0 = smem_u32(smem);
             const uint64_t da0 = AMN ? desc_sw128_mn(s0, 8192) : desc_sw128(s0);
-            const uint64_t db0 = BMN ? desc_sw128_mn(s0 + C::A_BYTES, 8192) : desc_sw128(s0 + C::A_BYTES);
+            const uint64_t db0 = BMN ? desc_sw128_mn(s0 + HA * C::A_BYTES, 8192) : desc_sw128(s0 + HA * C::A_BYTES);
             // a step of 16 along K: 32 bytes of a row, or 16 rows of 128 bytes
             constexpr uint64_t kStepA = AMN ? 2048 >> 4 : 32 >> 4, kStepB = BMN ? 2048 >> 4 : 32 >> 4;
             int st = 0, it = 0;
@@ -278,15 +293,20 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                 if (!mbar_wait(tempty_bar(buf), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, g.status)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
-                const int blocks = g.passes * (T.kb1 - T.kb0);
                 bool ok = true;
-                for (int i = 0; i < blocks; ++i) {
+                for (int kb = T.kb0; kb < T.kb1; ++kb) {
                     if (!(ok = mbar_wait(full_bar(st), ph, abort_flag, g.status))) break;
                     tc_fence_after();
                     const uint64_t so = (uint64_t)((uint32_t)(st * C::STAGE) >> 4);
 #pragma unroll
-                    for (int k = 0; k < kHgBK / 16; ++k)
-                        hg_mma<CG>(d, da0 + so + k * kStepA, db0 + so + k * kStepB, idesc, (i | k) != 0 ? 1u : 0u);
+                    for (int h = 0; h < HA + HB - 1; ++h) {
+                        // high high, high low, low high
+                        const uint64_t da = da0 + so + (h >= HB ? C::A_BYTES >> 4 : 0);
+                        const uint64_t db = db0 + so + (h > 0 && h < HB ? C::B_BYTES >> 4 : 0);
+#pragma unroll
+                        for (int k = 0; k < kHgBK / 16; ++k)
+                            hg_mma<CG>(d, da + k * kStepA, db + k * kStepB, idesc, kb > T.kb0 || (h | k) != 0 ? 1u : 0u);
+                    }
                     hg_commit<CG>(empty_bar(st));
                     if (++st == S) {
                         st = 0;
@@ -341,10 +361,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
     if constexpr (CG == 2) cluster_barrier();   // no copy, MMA or arrival of the pair is outstanding
     if (warp == 2) {
         tc_fence_after();
-        if constexpr (CG == 2)
-            asm volatile("tcgen05.dealloc.cta_group::2.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TCOLS) : "memory");
-        else
-            asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TCOLS) : "memory");
+        hg_tmem_free<CG>(tmem, C::TCOLS);
     }
 }
 
@@ -368,7 +385,8 @@ inline bool hg_map(CUtensorMap* m, const HgOperand& o, bool f16, int box_outer) 
 
 struct HgProblem {
     int64_t M, N, K;
-    int batch = 1, passes = 1, planes_a = 1, planes_b = 1, splits = 1;
+    int batch = 1, planes_a = 1, planes_b = 1;
+    int products = 1;          // of halves: 1 to 3 (for the choice of a form)
     bool upper = false;
     uint32_t* status = nullptr;
     int prof = 0;
@@ -382,33 +400,51 @@ inline int hg_splits(int64_t K, int want) {
     return (kb + per - 1) / per;
 }
 
-// Tile of a product: CTAs that work on one (1 or 2) and columns.
+// How a product runs: CTAs that work on a tile (1 or 2), its columns, and splits of K.
 struct HgPick {
-    int cg, bn;
+    int cg, bn, splits;
 };
 
-inline int hg_tiles(const HgProblem& p, HgPick t) {
-    const int tm = 128 * t.cg;
-    const int64_t rows = (p.M + tm - 1) / tm, cols = (p.N + t.bn - 1) / t.bn;
-    if (!p.upper) return (int)(rows * cols * p.batch);
+inline int64_t hg_tiles(const HgProblem& p, int cg, int bn) {
+    const int tm = 128 * cg;
+    const int64_t rows = (p.M + tm - 1) / tm, cols = (p.N + bn - 1) / bn;
+    if (!p.upper) return rows * cols * p.batch;
     int64_t n = 0;
-    for (int64_t m = 0; m < rows; ++m) n += cols - m * tm / t.bn;
-    return (int)(n * p.batch);
+    for (int64_t m = 0; m < rows; ++m) n += cols - m * tm / bn;
+    return n * p.batch;
 }
 
-// A pair where its 256 x 256 tiles fill the GPU, else a lone CTA with the tile width that
-// gives every SM a tile.
-inline HgPick hg_pick(const HgProblem& p) {
+// The cheapest in clocks of its busiest SM: rounds of tiles times K blocks times a block's
+// clocks, and for splits (at most max_splits) what joining their sums in 32 bits costs.  A
+// block's clocks are those of its loads, about 53 bytes a clock into an SM's shared memory
+// (256 x 256 by a pair: 32 KB in 600 clocks, of which the MMAs need 512; 256 x 128 by a pair:
+// 24 KB in 550, MMAs 256; measured on 8192 x 2048 x 16384).
+inline HgPick hg_pick(const HgProblem& p, int max_splits = 1) {
     const int sms = sm_count();
-    if (hg_tiles(p, {2, 256}) * p.splits >= sms / 2) return {2, 256};
-    if (hg_tiles(p, {1, 256}) * p.splits >= sms) return {1, 256};
-    return {1, 128};
+    static const struct { int cg, bn, clocks; } kForms[] = {{2, 256, 600}, {2, 128, 500}, {1, 256, 930}, {1, 128, 620}};
+    HgPick best{2, 256, 1};
+    int64_t least = INT64_MAX;
+    const int64_t kb = (p.K + kHgBK - 1) / kHgBK;
+    for (const auto& f : kForms) {
+        const int64_t tiles = hg_tiles(p, f.cg, f.bn), units = sms / f.cg;
+        for (int w = 1; w <= max_splits && w <= kb; ++w) {
+            const int s = hg_splits(p.K, w);
+            if (s != w) continue;
+            int64_t c = (tiles * s + units - 1) / units * ((kb + s - 1) / s * p.products * f.clocks + 1500);
+            if (s > 1) c += 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500;
+            if (c < least) {
+                least = c;
+                best = {f.cg, f.bn, s};
+            }
+        }
+    }
+    return best;
 }
 
-template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16>
-cudaError_t hg_launch_as(const HgProblem& p, const HgOperand& a, const HgOperand& b, const typename Epi::Args& ea,
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB>
+cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, const HgOperand& b, const typename Epi::Args& ea,
                          cudaStream_t s) {
-    using C = HgCfg<CG, BN>;
+    using C = HgCfg<CG, BN, HA, HB>;
     CUtensorMap ma, mb;
     if (!hg_map(&ma, a, F16, AMN ? 64 : 128) || !hg_map(&mb, b, F16, BMN ? 64 : C::B_ROWS)) return cudaErrorInvalidValue;
     HgArgs g{};
@@ -418,10 +454,9 @@ cudaError_t hg_launch_as(const HgProblem& p, const HgOperand& a, const HgOperand
     g.tiles_n = (int)((p.N + BN - 1) / BN);
     g.batch = p.batch;
     g.kb_total = (int)((p.K + kHgBK - 1) / kHgBK);
-    g.kb_per_split = (g.kb_total + p.splits - 1) / p.splits;
+    g.kb_per_split = (g.kb_total + splits - 1) / splits;
     g.splits = (g.kb_total + g.kb_per_split - 1) / g.kb_per_split;
-    g.total = hg_tiles(p, {CG, BN}) * g.splits;
-    g.passes = p.passes;
+    g.total = (int)hg_tiles(p, CG, BN) * g.splits;
     g.planes_a = p.planes_a;
     g.planes_b = p.planes_b;
     g.upper = p.upper ? 1 : 0;
@@ -430,7 +465,7 @@ cudaError_t hg_launch_as(const HgProblem& p, const HgOperand& a, const HgOperand
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
     const int sms = sm_count(&dev);
-    const auto kernel = k_head_gemm<Epi, CG, BN, AMN, BMN, F16>;
+    const auto kernel = k_head_gemm<Epi, CG, BN, AMN, BMN, F16, HA, HB>;
     const cudaError_t e = once_per_device(ready, dev, [kernel] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
@@ -441,13 +476,15 @@ cudaError_t hg_launch_as(const HgProblem& p, const HgOperand& a, const HgOperand
     else return launch_k(kernel, dim3(grid), dim3(kHgThreads), C::SMEM, s, ma, mb, g, ea);
 }
 
-// D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K.
-template <class Epi, bool AMN, bool BMN, bool F16>
+// D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K; HA, HB:
+// halves of the operands.
+template <class Epi, bool AMN, bool BMN, bool F16, int HA = 1, int HB = 1>
 cudaError_t hg_launch(const HgPick& t, const HgProblem& p, const HgOperand& a, const HgOperand& b,
                       const typename Epi::Args& ea, cudaStream_t s) {
-    if (t.cg == 2) return hg_launch_as<Epi, 2, 256, AMN, BMN, F16>(p, a, b, ea, s);
-    if (t.bn == 256) return hg_launch_as<Epi, 1, 256, AMN, BMN, F16>(p, a, b, ea, s);
-    return hg_launch_as<Epi, 1, 128, AMN, BMN, F16>(p, a, b, ea, s);
+    if (t.cg == 2 && t.bn == 256) return hg_launch_as<Epi, 2, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
+    if (t.cg == 2) return hg_launch_as<Epi, 2, 128, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
+    if (t.bn == 256) return hg_launch_as<Epi, 1, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
+    return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
 }
 
 }  // namespace

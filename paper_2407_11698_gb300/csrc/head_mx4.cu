@@ -9,7 +9,7 @@
 // Scales: tiles of 128 rows x 4 blocks, 512 bytes each, ordered [row tile][block tile];
 // row r, block j of a tile at (r % 32) 16 + (r / 32) 4 + j.  That is the order in which
 // the tensor cores take scales from TMEM, so a tile goes from global memory to shared
-// memory by one bulk copy and on to TMEM by one tcgen05.cp.
+// memory as one run of bytes and on to TMEM by one tcgen05.cp.
 //
 // The product runs on tcgen05.mma kind::mxf4 (products and scales exact, 32-bit sums).
 #include <new>
@@ -20,8 +20,7 @@
 #include <algorithm>
 #include <type_traits>
 
-#include "prof.cuh"
-#include "tc_ptx.cuh"
+#include "head_gemm.cuh"
 
 using namespace nitro;
 
@@ -38,12 +37,6 @@ __device__ __forceinline__ int64_t scale_at(int64_t row, int j, int tiles) {
     return ((row >> 7) * tiles + (j >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (j & 3);
 }
 
-template <typename T>
-__device__ __forceinline__ float to_float(T v) {
-    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)v << 16);
-    else return v;
-}
-
 // two values -> two e2m1 codes in a byte, b in the high half; nearest, ties to even, at most 6
 __device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
     uint32_t r;
@@ -51,110 +44,166 @@ __device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
     return r;
 }
 
-// Four threads a block, eight values each.  The grid covers the scales' padding too.
+constexpr int kMxInFlight = 4;      // loads of a thread in flight
+
+// eight values as loaded
+template <typename T>
+struct Raw8 {
+    uint4 w[sizeof(T) / 2];
+    __device__ __forceinline__ float get(int j) const {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+        if constexpr (sizeof(T) == 2) return __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
+        else return __uint_as_float(u[j]);
+    }
+};
+template <typename T>
+__device__ __forceinline__ Raw8<T> load8(const T* src, int n, bool vec) {
+    Raw8<T> r;
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = make_uint4(0, 0, 0, 0);
+    if (vec && n >= 8) {
+#pragma unroll
+        for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = reinterpret_cast<const uint4*>(src)[j];
+    } else {
+        uint32_t* u = reinterpret_cast<uint32_t*>(r.w);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            if (j >= n) continue;
+            if constexpr (sizeof(T) == 2) u[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+            else u[j] = __float_as_uint(src[j]);
+        }
+    }
+    return r;
+}
+
+// Two threads a block, sixteen values each, two such loads in flight.  The grid covers the
+// scales' padding too.  Bound by memory: MX4Q_MEASURED
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc,
                                                       int blocks, int64_t rows_pad, int vec) {
     pdl_wait();
-    const int tiles = (blocks + 3) / 4;
-    const int64_t per_row = (int64_t)tiles * 16, n = rows_pad * per_row;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per_row;
-        const int part = (int)(i - row * per_row), blk = part >> 2, c = part * 8;
-        float v[8];
+    const int tiles = (blocks + 3) / 4, per = tiles * 8;
+    const int64_t n = rows_pad * per, step = (int64_t)gridDim.x * 256;
+    RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, step, per);
+    for (int64_t base = blockIdx.x * (int64_t)256; base < n; base += 2 * step) {
+        Raw8<T> raw[2][2];
+        int64_t row[2];
+        int part[2];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
-        if (row < rows && c < cols) {
-            const T* src = x + row * ldx + c;
-            if (vec && c + 8 <= cols) {
-                if constexpr (sizeof(T) == 2) {
-                    const uint4 w = *reinterpret_cast<const uint4*>(src);
-                    const uint32_t u[4] = {w.x, w.y, w.z, w.w};
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        v[2 * j] = __uint_as_float(u[j] << 16);
-                        v[2 * j + 1] = __uint_as_float(u[j] & 0xffff0000u);
-                    }
-                } else {
-                    const float4 a = reinterpret_cast<const float4*>(src)[0], b = reinterpret_cast<const float4*>(src)[1];
-                    v[0] = a.x, v[1] = a.y, v[2] = a.z, v[3] = a.w, v[4] = b.x, v[5] = b.y, v[6] = b.z, v[7] = b.w;
-                }
-            } else {
-#pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < cols) v[j] = to_float(src[j]);
-            }
+        for (int u = 0; u < 2; ++u) {
+            row[u] = at.row;
+            part[u] = at.part;
+            const int c = at.part * 16;
+            const T* src = x + at.row * ldx + c;
+            const int left = at.row < rows ? cols - c : 0;
+            raw[u][0] = load8(src, left, vec != 0);
+            raw[u][1] = load8(src + 8, left - 8, vec != 0);
+            at.next();
         }
-        // magnitudes as integers keep their order, and a NaN is the largest
-        uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 8; ++j) top = max(top, __float_as_uint(v[j]) & 0x7fffffffu);
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-        top = max(top, __shfl_xor_sync(0xffffffffu, top, 2));
-        // exponent + 127 of the scale: that of the largest less 2, at least 0; 255: not finite
-        const uint32_t e = top >> 23;
-        const uint32_t s = e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
-        // 2^(127 - s): 254 - s as an exponent field (s = 254 cannot be)
-        const float inv = __uint_as_float((254u - min(s, 253u)) << 23);
-        uint32_t w = 0;
+        for (int u = 0; u < 2; ++u) {
+            // magnitudes as integers keep their order, and a NaN is the largest
+            uint32_t top = 0;
 #pragma unroll
-        for (int j = 0; j < 4; ++j) w |= e2m1x2(v[2 * j] * inv, v[2 * j + 1] * inv) << (8 * j);
-        if (row < rows && blk < blocks) *reinterpret_cast<uint32_t*>(q + (row * blocks + blk) * 16 + (part & 3) * 4) = w;
-        if ((part & 3) == 0) sc[scale_at(row, blk, tiles)] = row < rows && blk < blocks ? (uint8_t)s : 0;
+            for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(raw[u][j >> 3].get(j & 7)) & 0x7fffffffu);
+            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+            // exponent + 127 of the scale: that of the largest less 2, at least 0; 255: not finite
+            const uint32_t e = top >> 23;
+            const uint32_t s = e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
+            // 2^(127 - s): 254 - s as an exponent field (s = 254 cannot be)
+            const float inv = __uint_as_float((254u - min(s, 253u)) << 23);
+            uint32_t w[2] = {0, 0};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                w[j >> 2] |= e2m1x2(raw[u][j >> 2].get(2 * (j & 3)) * inv, raw[u][j >> 2].get(2 * (j & 3) + 1) * inv) << (8 * (j & 3));
+            const int blk = part[u] >> 1;
+            const bool in = row[u] < rows && blk < blocks;
+            if (in) *reinterpret_cast<uint2*>(q + (row[u] * blocks + blk) * 16 + (part[u] & 1) * 8) = make_uint2(w[0], w[1]);
+            if ((part[u] & 1) == 0 && row[u] < rows_pad) sc[scale_at(row[u], blk, tiles)] = in ? (uint8_t)s : 0;
+        }
     }
 }
 
-__device__ __forceinline__ float e2m1_value(uint32_t code) {
-    // magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6: twice that in half a byte each
-    const float m = 0.5f * (float)((0xc8643210u >> (4 * (code & 7))) & 15u);
-    return code & 8 ? -m : m;
-}
+// a scale as a value
 __device__ __forceinline__ float e8m0_value(uint32_t s) {
     return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
+}
+// codes 2i and 2i + 1 of a word as two bf16: their halves looked up byte by byte (the
+// magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6 are 0000 3f00 3f80 3fc0 4000 4040 4080 40c0)
+__device__ __forceinline__ uint32_t e2m1_bf16x2(uint32_t w, int i) {
+    const uint32_t c = w >> (8 * i), sel = (c & 7u) | (c & 0x70u);
+    const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, sel), lo = __byte_perm(0xc0800000u, 0xc0804000u, sel);
+    return __byte_perm(lo, hi, 0x5140) | (c & 8u) << 12 | (c & 0x80u) << 24;
 }
 
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const uint8_t* sc, int rows, int cols, int blocks,
                                                         T* out, int64_t ldo, float* scales, int vec) {
     pdl_wait();
-    const int tiles = (blocks + 3) / 4;
-    const int64_t per_row = (int64_t)blocks * 4, n = rows * per_row;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < n; i += (int64_t)gridDim.x * 256) {
-        const int64_t row = i / per_row;
-        const int part = (int)(i - row * per_row), blk = part >> 2, c = part * 8;
-        const uint32_t w = *reinterpret_cast<const uint32_t*>(q + i * 4);
-        const float s = e8m0_value(sc[scale_at(row, blk, tiles)]);
-        if (scales && (part & 3) == 0) scales[row * blocks + blk] = s;
-        float v[8];
+    const int tiles = (blocks + 3) / 4, per = blocks * 4;
+    const int64_t step = (int64_t)gridDim.x * 256;
+    RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, step, per);
+    while (at.row < rows) {
+        uint32_t w[kMxInFlight], s[kMxInFlight];
+        int64_t row[kMxInFlight];
+        int part[kMxInFlight];
 #pragma unroll
-        for (int j = 0; j < 8; ++j) v[j] = e2m1_value((w >> (4 * j)) & 15u) * s;
-        T* dst = out + row * ldo + c;
-        if constexpr (sizeof(T) == 2) {
-            uint32_t u[4];
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const __nv_bfloat162 p = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
-                u[j] = *reinterpret_cast<const uint32_t*>(&p);
+        for (int u = 0; u < kMxInFlight; ++u) {
+            row[u] = at.row;
+            part[u] = at.part;
+            if (at.row < rows) {
+                w[u] = *reinterpret_cast<const uint32_t*>(q + (at.row * per + at.part) * 4);
+                s[u] = sc[scale_at(at.row, at.part >> 2, tiles)];
             }
-            if (vec && c + 8 <= cols) *reinterpret_cast<uint4*>(dst) = make_uint4(u[0], u[1], u[2], u[3]);
-            else
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < cols) dst[j] = (uint16_t)(u[j >> 1] >> (16 * (j & 1)));
-        } else {
-            if (vec && c + 8 <= cols) {
-                reinterpret_cast<float4*>(dst)[0] = make_float4(v[0], v[1], v[2], v[3]);
-                reinterpret_cast<float4*>(dst)[1] = make_float4(v[4], v[5], v[6], v[7]);
-            } else
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < cols) dst[j] = v[j];
+            at.next();
+        }
+#pragma unroll
+        for (int u = 0; u < kMxInFlight; ++u) {
+            if (row[u] >= rows) continue;
+            const int blk = part[u] >> 2, c = part[u] * 8;
+            const float f = e8m0_value(s[u]);
+            if (scales && (part[u] & 3) == 0) scales[row[u] * blocks + blk] = f;
+            T* dst = out + row[u] * ldo + c;
+            uint32_t v[4];      // two values each, as bf16
+#pragma unroll
+            for (int j = 0; j < 4; ++j) v[j] = e2m1_bf16x2(w[u], j);
+            if constexpr (sizeof(T) == 2) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const __nv_bfloat162 p = __floats2bfloat162_rn(__uint_as_float(v[j] << 16) * f, __uint_as_float(v[j] & 0xffff0000u) * f);
+                    v[j] = *reinterpret_cast<const uint32_t*>(&p);
+                }
+                if (vec && c + 8 <= cols) *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
+                else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < cols) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+                }
+            } else {
+                float o[8];
+#pragma unroll
+                for (int j = 0; j < 8; ++j) o[j] = __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16) * f;
+                if (vec && c + 8 <= cols) {
+                    reinterpret_cast<float4*>(dst)[0] = make_float4(o[0], o[1], o[2], o[3]);
+                    reinterpret_cast<float4*>(dst)[1] = make_float4(o[4], o[5], o[6], o[7]);
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 8; ++j)
+                        if (c + j < cols) dst[j] = o[j];
+                }
+            }
         }
     }
 }
 
 // ------------------------------------------------------------------ product
-// D[p][q] = sum_k P[p][k] Q[q][k], 128 rows of P (TMEM lanes) x BN rows of Q (columns) a
-// tile.  SWAP: P is W and Q the features, for few samples: a tile then has 128 weights'
-// rows and as few columns as there are samples, and the weights stream past once.
+// D[p][q] = sum_k P[p][k] Q[q][k], 128 CG rows of P (TMEM lanes) x BN rows of Q (columns) a
+// tile, 256 elements of K (128 bytes) a stage.  SWAP: P is W and Q the features, for few
+// samples: a tile then has 128 of W's rows and as few columns as there are samples, and the
+// weights stream past once.  CG = 2 pairs two CTAs on 256 x 256 (see head_gemm.cuh): at the
+// 4-bit rate the MMAs of a stage take a third of the time of its loads, so what counts is
+// products a byte loaded.  A pair's accumulator and scales fill TMEM, so its drain waits for
+// the next tile's MMAs, but not for its loads.
 constexpr int kMxThreads = 384, kMxEpiWarp0 = 4, kMxEpiWarps = 8;
 
 struct MxArgs {
@@ -162,47 +211,67 @@ struct MxArgs {
     int tiles_p, tiles_q, splits, total, band;
     int k64;                 // steps of 64 along K
     int stages, stages_per_split;
-    const uint8_t *sp, *sq;  // scales
-    int tiles_k;             // scale tiles along K
     void* y;                 // output, or slices of 32-bit partial sums
     int64_t ldy, slice;
     int out;                 // 0 bf16, 1 fp32
     int vec;                 // rows of y are 16-byte aligned
     uint32_t* status;
 };
-
-template <int BN>
-struct MxCfg {
-    static constexpr int P_BYTES = 128 * 128, Q_BYTES = BN * 128;
-    static constexpr int STAGE = P_BYTES + Q_BYTES + 2048;    // and 1 KB of scales each
-    static constexpr int S = BN >= 128 ? 6 : 8;
-    static constexpr int SMEM = S * STAGE + 1024 + 256;
-    static constexpr int SF = 2 * BN;                          // TMEM columns of the scales: 2 x 16
-    static constexpr int TCOLS = 2 * BN + 32 <= 128 ? 128 : 2 * BN + 32 <= 256 ? 256 : 512;
+struct MxMaps {
+    CUtensorMap p, q, sp, sq;      // codes, scale tiles
 };
 
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes, uint32_t bar) {
-    asm volatile("cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(dst),
-                 "l"(src), "r"(bytes), "r"(bar)
-                 : "memory");
+template <int CG, int BN>
+struct MxCfg {
+    static constexpr int P_BYTES = 128 * 128, Q_ROWS = BN / CG, Q_BYTES = Q_ROWS * 128;
+    static constexpr int QT = BN > 128 ? 2 : 1;               // scale tiles of 128 rows a tile's columns take
+    static constexpr int SF_BYTES = 1024 + QT * 1024;
+    static constexpr int STAGE = P_BYTES + Q_BYTES + SF_BYTES;
+    static constexpr int S = BN >= 128 ? 6 : 8;
+    static constexpr int SMEM = S * STAGE + 1024 + 256;
+    static constexpr int NBUF = CG == 2 ? 1 : 2;               // accumulators
+    static constexpr int SF = NBUF * BN, SF_COLS = 8 + 8 * QT; // TMEM columns of a stage's scales, for two stages
+    static constexpr int TCOLS = SF + 2 * SF_COLS <= 128 ? 128 : SF + 2 * SF_COLS <= 256 ? 256 : 512;
+};
+
+template <int CG>
+__device__ __forceinline__ void mx_tma(uint32_t dst, const CUtensorMap* m, uint32_t bar, int c0, int c1) {
+    if constexpr (CG == 2)
+        asm volatile(
+            "cp.async.bulk.tensor.2d.cta_group::2.shared::cluster.global.mbarrier::complete_tx::bytes"
+            " [%0], [%1, {%3, %4}], [%2];" ::"r"(dst),
+            "l"(reinterpret_cast<uint64_t>(m)), "r"(bar), "r"(c0), "r"(c1)
+            : "memory");
+    else
+        tma_load_2d(dst, m, bar, c0, c1);
 }
 // 32 rows of 16 bytes (a scale tile) -> four TMEM columns, the same for every lane quadrant
+template <int CG>
 __device__ __forceinline__ void copy_scales(uint32_t taddr, uint32_t saddr) {
     const uint64_t d = (uint64_t)((saddr & 0x3FFFFu) >> 4) | (uint64_t)(128 >> 4) << 32 | (uint64_t)1 << 46;
-    asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
+    if constexpr (CG == 2) asm volatile("tcgen05.cp.cta_group::2.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
+    else asm volatile("tcgen05.cp.cta_group::1.32x128b.warpx4 [%0], %1;" ::"r"(taddr), "l"(d) : "memory");
 }
-// kind::mxf4, e2m1 operands, e8m0 scales of 32; half: which two of a scale word's four bytes
+template <int CG>
 __device__ __forceinline__ void mma_mxf4(uint32_t d, uint64_t a, uint64_t b, uint32_t idesc, uint32_t sa, uint32_t sb,
                                          uint32_t accumulate) {
-    asm volatile(
-        "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
-        " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
-        "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
-        : "memory");
+    if constexpr (CG == 2)
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::2.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            : "memory");
+    else
+        asm volatile(
+            "{\n .reg .pred p;\n setp.ne.b32 p, %6, 0;\n"
+            " tcgen05.mma.cta_group::1.kind::mxf4.block_scale.scale_vec::2X [%0], %1, %2, %3, [%4], [%5], p;\n}\n" ::"r"(d),
+            "l"(a), "l"(b), "r"(idesc), "r"(sa), "r"(sb), "r"(accumulate)
+            : "memory");
 }
-__host__ __device__ constexpr uint32_t mx_idesc(int n, int half) {
-    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) | (8u << 24) |
-           ((uint32_t)(2 * half) << 29);
+// kind::mxf4, e2m1 operands, e8m0 scales of 32; half: which two of a scale word's four bytes
+__host__ __device__ constexpr uint32_t mx_idesc(int m, int n, int half) {
+    return ((uint32_t)(2 * half) << 4) | (1u << 7) | (1u << 10) | ((uint32_t)(n >> 3) << 17) | (1u << 23) |
+           ((uint32_t)(m >> 4) << 24) | ((uint32_t)(2 * half) << 29);
 }
 
 struct MxTile {
@@ -221,10 +290,9 @@ __device__ __forceinline__ MxTile mx_decode(const MxArgs& g, int idx) {
     return t;
 }
 
-template <int BN, bool SWAP>
-__global__ void __launch_bounds__(kMxThreads, 1)
-    k_mx4_gemm(const __grid_constant__ CUtensorMap tmP, const __grid_constant__ CUtensorMap tmQ, const MxArgs g) {
-    using C = MxCfg<BN>;
+template <int CG, int BN, bool SWAP>
+__global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constant__ MxMaps maps, const MxArgs g) {
+    using C = MxCfg<CG, BN>;
     constexpr int S = C::S;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
@@ -239,6 +307,8 @@ __global__ void __launch_bounds__(kMxThreads, 1)
     const auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * S + b); };
     const auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };
     const uint32_t drain_bar = bar0 + 8u * (2 * S + 4);
+    const int rank = CG == 2 ? (int)cluster_rank() : 0;
+    const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
             mbar_init(full_bar(s), 1);
@@ -246,21 +316,19 @@ __global__ void __launch_bounds__(kMxThreads, 1)
         }
         for (int b = 0; b < 2; ++b) {
             mbar_init(tfull_bar(b), 1);
-            mbar_init(tempty_bar(b), kMxEpiWarps);
+            mbar_init(tempty_bar(b), CG * kMxEpiWarps);
         }
         mbar_init(drain_bar, 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
-    if (warp == 2) {
-        asm volatile("tcgen05.alloc.cta_group::1.sync.aligned.shared::cta.b32 [%0], %1;" ::"r"(smem_u32(tmem_slot)),
-                     "r"(C::TCOLS)
-                     : "memory");
-        asm volatile("tcgen05.relinquish_alloc_permit.cta_group::1.sync.aligned;" ::: "memory");
-    }
+    if (warp == 2) hg_tmem_alloc<CG>(smem_u32(tmem_slot), C::TCOLS);
+    if (warp == 0 && lane < 4)
+        asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.p + lane)) : "memory");
     pdl_wait();
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
     tc_fence_after();
     const uint32_t tmem = *tmem_slot;
 
@@ -268,20 +336,20 @@ __global__ void __launch_bounds__(kMxThreads, 1)
         if (lane == 0) {
             int st = 0, loaded = 0;
             uint32_t ph = 1;
-            for (int tile = blockIdx.x; tile < g.total; tile += gridDim.x) {
+            for (int tile = unit; tile < g.total; tile += units) {
                 const MxTile T = mx_decode(g, tile);
-                const uint8_t* sp = g.sp + (int64_t)T.p * g.tiles_k * 512;
-                const uint8_t* sq = g.sq + (int64_t)(T.q * BN / 128) * g.tiles_k * 512;
+                const int p0 = T.p * 128 * CG + rank * 128, q0 = T.q * BN;
                 for (int k = T.s0; k < T.s1; ++k) {
                     if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
-                    const uint32_t dp = s0 + st * (C::P_BYTES + C::Q_BYTES), dq = dp + C::P_BYTES, ds = sf0 + st * 2048;
-                    const uint32_t fb = full_bar(st);
-                    const uint32_t sb = (uint32_t)min(2, g.tiles_k - 2 * k) * 512u;
-                    mbar_expect_tx(fb, C::P_BYTES + C::Q_BYTES + 2 * sb);
-                    tma_load_2d(dp, &tmP, fb, k * 128, T.p * 128);
-                    tma_load_2d(dq, &tmQ, fb, k * 128, T.q * BN);
-                    bulk_load(ds, sp + (int64_t)k * 1024, sb, fb);
-                    bulk_load(ds + 1024, sq + (int64_t)k * 1024, sb, fb);
+                    const uint32_t dp = s0 + st * (C::P_BYTES + C::Q_BYTES), dq = dp + C::P_BYTES, ds = sf0 + st * C::SF_BYTES;
+                    uint32_t fb = full_bar(st);
+                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
+                    if constexpr (CG == 2) fb = remote_smem(fb, 0);
+                    mx_tma<CG>(dp, &maps.p, fb, k * 128, p0);
+                    mx_tma<CG>(dq, &maps.q, fb, k * 128, q0 + rank * C::Q_ROWS);
+                    // both CTAs of a pair hold the scales of all columns
+                    mx_tma<CG>(ds, &maps.sp, fb, k * 256, p0 / 128);
+                    mx_tma<CG>(ds + 1024, &maps.sq, fb, k * 256, q0 / 128);
                     ++loaded;
                     if (++st == S) {
                         st = 0;
@@ -291,21 +359,19 @@ __global__ void __launch_bounds__(kMxThreads, 1)
             }
         producer_out:
             if (*abort_flag) {
-                const uint64_t t0 = global_ns();
                 for (int k = max(0, loaded - S); k < loaded; ++k)
-                    while (!mbar_try_wait(full_bar(k % S), (uint32_t)(k / S) & 1u) && global_ns() - t0 < 50000000ull) {
-                    }
+                    mbar_drain(full_bar(k % S), (uint32_t)(k / S) & 1u, kDrainNs);
             }
         }
     } else if (warp == 1) {
-        if (lane == 0) {
+        if (lane == 0 && rank == 0) {
             const uint64_t dp0 = desc_sw128(s0), dq0 = desc_sw128(s0 + C::P_BYTES);
             int st = 0, it = 0, n = 0;
             uint32_t ph = 0;
-            for (int tile = blockIdx.x; tile < g.total; tile += gridDim.x, ++it) {
+            for (int tile = unit; tile < g.total; tile += units, ++it) {
                 const MxTile T = mx_decode(g, tile);
-                const int buf = it & 1;
-                if (!mbar_wait(tempty_bar(buf), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, g.status)) break;
+                const int buf = it % C::NBUF;
+                if (!mbar_wait(tempty_bar(buf), ((uint32_t)(it / C::NBUF) & 1u) ^ 1u, abort_flag, g.status)) break;
                 tc_fence_after();
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 bool ok = true;
@@ -313,52 +379,48 @@ __global__ void __launch_bounds__(kMxThreads, 1)
                     if (!(ok = mbar_wait(full_bar(st), ph, abort_flag, g.status))) break;
                     tc_fence_after();
                     const int steps = min(4, g.k64 - 4 * k);
-                    const uint32_t sf = tmem + C::SF + 16u * (n & 1), ds = sf0 + st * 2048;
-                    copy_scales(sf, ds);
-                    copy_scales(sf + 8, ds + 1024);
-                    if (steps > 2) {
-                        copy_scales(sf + 4, ds + 512);
-                        copy_scales(sf + 12, ds + 1536);
+                    const uint32_t sp = tmem + C::SF + C::SF_COLS * (n & 1), sq = sp + 8, ds = sf0 + st * C::SF_BYTES;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        copy_scales<CG>(sp + 4 * j, ds + 512 * j);
+#pragma unroll
+                        for (int r = 0; r < C::QT; ++r) copy_scales<CG>(sq + 4 * (C::QT * j + r), ds + 1024 + 1024 * r + 512 * j);
                     }
                     const uint64_t so = (uint64_t)((uint32_t)(st * (C::P_BYTES + C::Q_BYTES)) >> 4);
-                    // where the columns' tile starts inside a scale tile of 128 rows: 32 rows a TMEM column
-                    const uint32_t q32 = BN < 128 ? (uint32_t)((T.q * BN) & 127) >> 5 : 0u;
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         if (j < steps)
-                            mma_mxf4(d, dp0 + so + 2 * j, dq0 + so + 2 * j, mx_idesc(BN, j & 1), sf + 4u * (j >> 1),
-                                     sf + 8 + 4u * (j >> 1) + q32, (k > T.s0 || j > 0) ? 1u : 0u);
-                    umma_commit(empty_bar(st));
+                            mma_mxf4<CG>(d, dp0 + so + 2 * j, dq0 + so + 2 * j, mx_idesc(128 * CG, BN, j & 1), sp + 4u * (j >> 1),
+                                         sq + 4u * C::QT * (j >> 1), (k > T.s0 || j > 0) ? 1u : 0u);
+                    hg_commit<CG>(empty_bar(st));
                     if (++st == S) {
                         st = 0;
                         ph ^= 1u;
                     }
                 }
                 if (!ok) break;
-                umma_commit(tfull_bar(buf));
+                hg_commit<CG>(tfull_bar(buf));
             }
             if (*abort_flag) {
-                umma_commit(drain_bar);
-                const uint64_t t0 = global_ns();
-                while (!mbar_try_wait(drain_bar, 0) && global_ns() - t0 < 50000000ull) {
-                }
+                hg_commit<CG>(drain_bar);
+                mbar_drain(drain_bar, 0, kDrainNs);
             }
             pdl_trigger();
         }
     } else if (warp >= kMxEpiWarp0) {
         const int q = warp & 3, half = (warp - kMxEpiWarp0) >> 2;
         int it = 0;
-        for (int tile = blockIdx.x; tile < g.total; tile += gridDim.x, ++it) {
+        for (int tile = unit; tile < g.total; tile += units, ++it) {
             const MxTile T = mx_decode(g, tile);
-            const int buf = it & 1;
-            const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it >> 1) & 1u, abort_flag, g.status);
+            const int buf = it % C::NBUF;
+            const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it / C::NBUF) & 1u, abort_flag, g.status);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
-            const int row = T.p * 128 + q * 32 + lane, col0 = T.q * BN + half * (BN / 2);
+            const int row = T.p * 128 * CG + rank * 128 + q * 32 + lane, col0 = T.q * BN + half * (BN / 2);
             const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
             float* yf = static_cast<float*>(g.y) + T.split * g.slice;
             uint16_t* yb = static_cast<uint16_t*>(g.y);
-#pragma unroll
+#pragma unroll 4
             for (int c = 0; c < BN / 2; c += 16) {
                 uint32_t v[16];
                 tmem_ld16_nowait(src + c, v);
@@ -366,7 +428,10 @@ __global__ void __launch_bounds__(kMxThreads, 1)
                 if (c + 16 == BN / 2) {
                     tc_fence_before();
                     __syncwarp();
-                    if (lane == 0) mbar_arrive(tempty_bar(buf));
+                    if (lane == 0) {
+                        if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
+                        else mbar_arrive(tempty_bar(buf));
+                    }
                 }
                 const int n = g.Q - (col0 + c);
                 if (row >= g.P || n <= 0) continue;
@@ -414,9 +479,10 @@ __global__ void __launch_bounds__(kMxThreads, 1)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if constexpr (CG == 2) cluster_barrier();
     if (warp == 2) {
         tc_fence_after();
-        asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(C::TCOLS) : "memory");
+        hg_tmem_free<CG>(tmem, C::TCOLS);
     }
 }
 
@@ -444,29 +510,51 @@ bool mx_map(CUtensorMap* m, const uint8_t* codes, int64_t rows, int64_t pitch, i
               CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
               CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
 }
+// scale tiles as rows of words, two tiles along K a box; those past the end read as zero
+bool mx_scale_map(CUtensorMap* m, const uint8_t* scales, int64_t rows, int64_t tiles_k, int box_tiles) {
+    auto fn = encode_fn();
+    if (!fn) return false;
+    cuuint64_t dim[2] = {(cuuint64_t)tiles_k * 128, (cuuint64_t)((rows + 127) / 128)}, stride[1] = {(cuuint64_t)tiles_k * 512};
+    cuuint32_t box[2] = {256, (cuuint32_t)box_tiles}, step[2] = {1, 1};
+    return fn(m, CU_TENSOR_MAP_DATA_TYPE_UINT32, 2, const_cast<uint8_t*>(scales), dim, stride, box, step,
+              CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_NONE, CU_TENSOR_MAP_L2_PROMOTION_L2_256B,
+              CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
+}
 
-template <int BN, bool SWAP>
-cudaError_t mx_launch(const uint8_t* p, int64_t np, const uint8_t* q, int64_t nq, int64_t pitch, MxArgs g, double ops,
-                      double bytes, cudaStream_t s) {
-    using C = MxCfg<BN>;
-    CUtensorMap mp, mq;
-    if (!mx_map(&mp, p, np, pitch, 128) || !mx_map(&mq, q, nq, pitch, BN)) return cudaErrorInvalidValue;
+struct MxOperand {
+    const uint8_t *codes, *scales;
+    int64_t rows;
+};
+
+template <int CG, int BN, bool SWAP>
+cudaError_t mx_launch(const MxOperand& p, const MxOperand& q, int in, MxArgs g, double ops, double bytes, cudaStream_t s) {
+    using C = MxCfg<CG, BN>;
+    MxMaps m;
+    const int64_t pitch = blocks_of(in) * 16, tiles_k = (blocks_of(in) + 3) / 4;
+    if (!mx_map(&m.p, p.codes, p.rows, pitch, 128) || !mx_map(&m.q, q.codes, q.rows, pitch, C::Q_ROWS) ||
+        !mx_scale_map(&m.sp, p.scales, p.rows, tiles_k, 1) || !mx_scale_map(&m.sq, q.scales, q.rows, tiles_k, C::QT))
+        return cudaErrorInvalidValue;
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
     const int sms = sm_count(&dev);
     const cudaError_t e = once_per_device(ready, dev, [] {
-        return cudaFuncSetAttribute(k_mx4_gemm<BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        return cudaFuncSetAttribute(k_mx4_gemm<CG, BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
     if (e != cudaSuccess) return e;
+    const int grid = std::min(g.total, sms / CG) * CG;
     ProfScope ps(K_MX4_LINEAR, s, ops, bytes);
-    return launch_k(k_mx4_gemm<BN, SWAP>, dim3(std::min(g.total, sms)), dim3(kMxThreads), C::SMEM, s, mp, mq, g);
+    if constexpr (CG == 2) return launch_cluster(k_mx4_gemm<CG, BN, SWAP>, dim3(grid), kMxThreads, 2, s, C::SMEM, m, g);
+    else return launch_k(k_mx4_gemm<CG, BN, SWAP>, dim3(grid), dim3(kMxThreads), C::SMEM, s, m, g);
 }
+
+// CTAs for n items: one an item and thread while few, then what the SMs hold at once
+int mx_grid(int64_t n) { return (int)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 8); }
 
 template <typename T>
 cudaError_t quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc, cudaStream_t s) {
     const int blocks = (int)blocks_of(cols);
-    const int64_t pad = round_up(rows, 128), n = pad * ((blocks + 3) / 4) * 16;
-    const int grid = (int)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 16);
+    const int64_t pad = round_up(rows, 128), n = pad * ((blocks + 3) / 4) * 8;
+    const int grid = mx_grid(n);
     const int vec = ((uintptr_t)x & 15) == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
     ProfScope ps(K_MX4_QUANTIZE, s, 0.0, (double)rows * cols * (sizeof(T) + 17.0 / 32.0));
     return launch_k(k_mx4_quantize<T>, dim3(grid), dim3(256), 0, s, x, ldx, rows, cols, q, sc, blocks, pad, vec);
@@ -526,7 +614,7 @@ nitro_status nitro_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, i
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int blocks = (int)blocks_of(cols);
     const int64_t n = (int64_t)rows * blocks * 4;
-    const int grid = (int)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 16);
+    const int grid = mx_grid(n);
     const int size = type == NITRO_BF16 ? 2 : 4;
     const int vec = ((uintptr_t)out & 15) == 0 && ldo * size % 16 == 0;
     ProfScope ps(K_MX4_DEQUANTIZE, s, 0.0, (double)rows * cols * (size + 17.0 / 32.0));
@@ -577,49 +665,59 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (x_type == NITRO_BF16) TRY(quantize((const uint16_t*)x, ldx, rows, h->in, h->xq, h->xs, s));
     else TRY(quantize((const float*)x, ldx, rows, h->in, h->xq, h->xs, s));
-    const int64_t pitch = blocks_of(h->in) * 16;
+    // Few samples: W's rows along the lanes.  Else pairs, or 128 x 128 tiles where those finish
+    // earlier: a stage takes a lone CTA and a pair the same time (32 KB into an SM).
     const bool swap = rows <= 64;
-    const int bn = rows <= 32 ? 32 : rows <= 64 ? 64 : 128;
     const int sms = sm_count();
     MxArgs g{};
     g.P = swap ? h->out : rows;
     g.Q = swap ? rows : h->out;
-    g.tiles_p = (g.P + 127) / 128;
-    g.tiles_q = (g.Q + bn - 1) / bn;
-    g.band = 16;
+    g.band = 8;
     g.k64 = (h->in + 63) / 64;
     g.stages = (g.k64 + 3) / 4;
-    g.tiles_k = (int)((blocks_of(h->in) + 3) / 4);
-    g.sp = swap ? w_scales : h->xs;
-    g.sq = swap ? h->xs : w_scales;
     g.status = h->status;
-    // K is shared out where that shortens the longest CTA's work
-    const int64_t tiles = (int64_t)g.tiles_p * g.tiles_q;
     const int64_t ldp = round_up(h->out, 4);
-    int best = 1;
-    int64_t cost = (tiles + sms - 1) / sms * g.stages;
-    for (int k = 2; k <= 16 && k <= g.stages && k * rows * ldp <= kPartFloats; ++k) {
-        const int per = (g.stages + k - 1) / k, real = (g.stages + per - 1) / per;
-        const int64_t c = (tiles * real + sms - 1) / sms * per + 3;    // and joining them: about three stages
-        if (c < cost) {
-            cost = c;
-            best = real;
+    int cg = 1, bn = 0, splits = 1;
+    int64_t cost = INT64_MAX;
+    const auto consider = [&](int c, int n) {
+        // K is shared out where that shortens the longest CTA's work
+        const int64_t tiles = (int64_t)((g.P + 128 * c - 1) / (128 * c)) * ((g.Q + n - 1) / n), units = sms / c;
+        for (int k = 1; k <= 16 && k <= g.stages && (k == 1 || k * rows * ldp <= kPartFloats); ++k) {
+            const int per = (g.stages + k - 1) / k;
+            if ((g.stages + per - 1) / per != k) continue;
+            // in stages: two for a tile's ends, four to join splits
+            const int64_t t = (tiles * k + units - 1) / units * (per + 2) + (k > 1 ? 4 : 0);
+            if (t < cost) {
+                cost = t;
+                cg = c;
+                bn = n;
+                splits = k;
+            }
         }
+    };
+    if (swap) {
+        consider(1, rows <= 32 ? 32 : 64);
+    } else {
+        consider(2, 256);
+        consider(1, 128);
     }
-    g.stages_per_split = (g.stages + best - 1) / best;
-    g.splits = (g.stages + g.stages_per_split - 1) / g.stages_per_split;
-    g.total = (int)(tiles * g.splits);
-    g.y = g.splits > 1 ? h->part : y;
-    g.ldy = g.splits > 1 ? ldp : ldy;
+    g.tiles_p = (g.P + 128 * cg - 1) / (128 * cg);
+    g.tiles_q = (g.Q + bn - 1) / bn;
+    g.stages_per_split = (g.stages + splits - 1) / splits;
+    g.splits = splits;
+    g.total = g.tiles_p * g.tiles_q * splits;
+    g.y = splits > 1 ? h->part : y;
+    g.ldy = splits > 1 ? ldp : ldy;
     g.slice = rows * ldp;
-    g.out = g.splits > 1 || y_type == NITRO_F32;
-    g.vec = g.splits > 1 || (((uintptr_t)y & 15) == 0 && ldy * (y_type == NITRO_F32 ? 4 : 2) % 16 == 0);
+    g.out = splits > 1 || y_type == NITRO_F32;
+    g.vec = splits > 1 || (((uintptr_t)y & 15) == 0 && ldy * (y_type == NITRO_F32 ? 4 : 2) % 16 == 0);
     const double ops = 2.0 * rows * h->in * h->out;
     const double bytes = (double)code_bytes(h->out, h->in) * 17 / 16 + code_bytes(rows, h->in) + 2.0 * rows * h->out;
-    const uint8_t *p = swap ? w_codes : h->xq, *q = swap ? h->xq : w_codes;
-    if (bn == 32) TRY((mx_launch<32, true>(p, g.P, q, g.Q, pitch, g, ops, bytes, s)));
-    else if (bn == 64) TRY((mx_launch<64, true>(p, g.P, q, g.Q, pitch, g, ops, bytes, s)));
-    else TRY((mx_launch<128, false>(p, g.P, q, g.Q, pitch, g, ops, bytes, s)));
+    const MxOperand x_op{h->xq, h->xs, rows}, w_op{w_codes, w_scales, h->out};
+    if (bn == 32) TRY((mx_launch<1, 32, true>(w_op, x_op, h->in, g, ops, bytes, s)));
+    else if (bn == 64) TRY((mx_launch<1, 64, true>(w_op, x_op, h->in, g, ops, bytes, s)));
+    else if (cg == 1) TRY((mx_launch<1, 128, false>(x_op, w_op, h->in, g, ops, bytes, s)));
+    else TRY((mx_launch<2, 256, false>(x_op, w_op, h->in, g, ops, bytes, s)));
     if (g.splits > 1) {
         const int64_t n = (int64_t)rows * h->out;
         ProfScope ps(K_MX4_LINEAR, s, 0.0, (4.0 * g.splits + 2.0) * n);

@@ -1,6 +1,7 @@
 // Softmax cross entropy of a linear head over many classes: z = scale x W^T,
 // loss_i = log sum_j exp z_ij - z_i,label, and its gradients
-//   G_ij = gout_i scale (softmax(z_i)_j - [j = label_i]),   dx = G W,   dW = G^T x.
+//   G_ij = softmax(z_i)_j - [j = label_i],   dx_i = gout_i scale (G W)_i,
+//   dW = scale sum_i gout_i G_i^T x_i.
 //
 // The logits are never kept.  The forward's products leave, for every row and tile, the
 // maximum and the sum of exponentials of the tile's columns, and a second kernel joins
@@ -99,23 +100,23 @@ struct EpiStats {
     }
 };
 
-// G of a piece: gout scale (2^(z log2 e - lse log2 e) - [label]), rounded once to bf16, the
-// type that the products with it take (its rounding is as large as the one of the
-// gradients that come out).  Rows that are left out give zeros.
+// softmax - onehot of a piece, rounded once to bf16, the type that the products with it
+// take.  The row's factor gout scale is left to their ends (dx) and to x (dw): multiplied
+// in here, the -1 at the label, exact in bf16 and most of a row's weight, would be rounded
+// as well, alike in every row.  Rows that are left out give zeros.
 struct EpiProb {
     struct Args {
         const int32_t* labels;
         const float* lse;
-        const float* gout;    // or null: 1
-        float k2, scale;
+        float k2;
         int classes, v0;      // all classes, and the piece's first
         uint16_t* G;          // [rows][ldg], ldg a multiple of 64
-        int64_t ldg;
+        int64_t ldg, low;     // low: from G to what its rounding left over, 0: not kept
     };
     const Args& a;
     const HgArgs& g;
     int row, col0, lab = -1;
-    float l2 = 0.0f, gi = 0.0f;
+    float l2 = 0.0f;
     bool live = false;
     __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
         : a(a_), g(g_), row(row_), col0(col0_) {
@@ -124,18 +125,25 @@ struct EpiProb {
             live = lab >= 0 && lab < a.classes;
             lab -= a.v0;
             l2 = a.lse[row] * kLog2e;
-            gi = a.scale * (a.gout ? a.gout[row] : 1.0f);
         }
     }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = col0 + c;
         if (row >= g.M || col >= g.N) return;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const float p = exp2f(fmaf(v[j], a.k2, -l2)) - (col + j == lab ? 1.0f : 0.0f);
-            v[j] = live ? gi * p : 0.0f;
+        for (int j = 0; j < 32; ++j) v[j] = live ? exp2f(fmaf(v[j], a.k2, -l2)) : 0.0f;
+        const int at = lab - col;
+        if (live && at >= 0 && at < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] -= j == at ? 1.0f : 0.0f;
         }
-        store_bf16_32(a.G + (int64_t)row * a.ldg + col, v, 32, true);   // the row's padding may be written
+        uint16_t* dst = a.G + (int64_t)row * a.ldg + col;
+        store_bf16_32(dst, v, 32, true);   // the row's padding may be written
+        if (a.low) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
+            store_bf16_32(dst + a.low, v, 32, true);
+        }
     }
     __device__ __forceinline__ void done() {}
 };
@@ -179,15 +187,22 @@ struct EpiBf16 {
         uint16_t* c;
         int64_t ldc;
         int vec;              // rows are 16-byte aligned
+        const float* factor;  // of the row, or of all rows
+        int one;
     };
     const Args& a;
     const HgArgs& g;
     int row, col0;
+    float f = 0.0f;
     __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
-        : a(a_), g(g_), row(row_), col0(col0_) {}
+        : a(a_), g(g_), row(row_), col0(col0_) {
+        if (row < g.M) f = a.factor[a.one ? 0 : row];
+    }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int n = g.N - (col0 + c);
         if (row >= g.M || n <= 0) return;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] *= f;
         store_bf16_32(a.c + (int64_t)row * a.ldc + col0 + c, v, n, a.vec != 0);
     }
     __device__ __forceinline__ void done() {}
@@ -276,60 +291,113 @@ __global__ void __launch_bounds__(256) k_xent_rows(const float* z, int64_t ldz, 
     }
 }
 
-// G from logits in slices, as EpiProb writes it (all classes, one piece); padding zero.
+// softmax - onehot from logits in slices, as EpiProb writes it (all classes, one piece).
 __global__ void __launch_bounds__(256) k_xent_probs(const float* z, int64_t ldz, int64_t slice, int slices,
                                                     const EpiProb::Args a) {
     pdl_wait();
     const int64_t row = blockIdx.x;
     const int lab = a.labels[row];
     const bool live = lab >= 0 && lab < a.classes;
-    const float l2 = a.lse[row] * kLog2e, gi = a.scale * (a.gout ? a.gout[row] : 1.0f);
+    const float l2 = a.lse[row] * kLog2e;
     const float* zr = z + row * ldz;
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < a.ldg; j += gridDim.y * 256) {
-        float v = 0.0f;
-        if (j < a.classes && live) {
-            v = zr[j];
-            for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
-            v = gi * (exp2f(fmaf(v, a.k2, -l2)) - (j == lab ? 1.0f : 0.0f));
-        }
-        a.G[row * a.ldg + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    for (int j = blockIdx.y * 256 + threadIdx.x; j < a.classes; j += gridDim.y * 256) {
+        float v = zr[j];
+        for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
+        v = live ? exp2f(fmaf(v, a.k2, -l2)) - (j == lab ? 1.0f : 0.0f) : 0.0f;
+        const __nv_bfloat16 r = __float2bfloat16_rn(v);
+        a.G[row * a.ldg + j] = __bfloat16_as_ushort(r);
+        if (a.low) a.G[a.low + row * a.ldg + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v - __bfloat162float(r)));
     }
 }
 
-// dx in bf16 from the slices of its 32-bit sums.
+// dx in bf16 from the slices of its 32-bit sums, four columns a thread.
 __global__ void __launch_bounds__(256) k_xent_dx(const float* c, int64_t ldc, int64_t slice, int slices, int features,
-                                                 uint16_t* dx, int64_t lddx) {
+                                                 const float* factor, uint16_t* dx, int64_t lddx, int vec) {
     pdl_wait();
     const int64_t row = blockIdx.x;
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < features; j += gridDim.y * 256) {
-        float v = c[row * ldc + j];
-        for (int k = 1; k < slices; ++k) v += c[k * slice + row * ldc + j];
-        dx[row * lddx + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    const float f = factor[row];
+    for (int j = (blockIdx.y * 256 + threadIdx.x) * 4; j < features; j += gridDim.y * 1024) {
+        float4 v = *reinterpret_cast<const float4*>(c + row * ldc + j);      // ldc holds the padding
+        for (int k = 1; k < slices; ++k) {
+            const float4 o = *reinterpret_cast<const float4*>(c + k * slice + row * ldc + j);
+            v.x += o.x, v.y += o.y, v.z += o.z, v.w += o.w;
+        }
+        const uint32_t w[2] = {pack_bf16(v.x * f, v.y * f), pack_bf16(v.z * f, v.w * f)};
+        uint16_t* dst = dx + row * lddx + j;
+        if (vec && j + 4 <= features) *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+        else {
+#pragma unroll
+            for (int k = 0; k < 4; ++k)
+                if (j + k < features) dst[k] = (uint16_t)(w[k >> 1] >> (16 * (k & 1)));
+        }
     }
 }
 
+// What the backward takes of x and gout: rows that are left out become zeros, so that an
+// infinity or NaN in them meets no weight gradient (0 times it is NaN); the others
+// x gout_i / ref, ref = gout of the first row that has one, so that under a mean, where all
+// are alike, x stays what it is.  factor[0] = scale ref, factor[1 + i] = scale gout_i.
+struct PackGrad {
+    const int32_t* labels;     // or null: a plain copy
+    const float* gout;         // or null: 1
+    float* factor;
+    float scale;
+    int classes;
+};
+
 // Rows of x as bf16 with a stride of ldp (a multiple of 8; padding zero): int8 activations
-// are exact in bf16.  labels (may be null): rows that are left out become zeros, so that
-// an infinity or NaN in them meets no weight gradient (0 times it is NaN).
+// are exact in bf16.
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
-                                                   const int32_t* labels, int classes) {
+                                                   const PackGrad pg) {
+    __shared__ int first;
     pdl_wait();
-    const int64_t words = (int64_t)rows * (ldp / 8);
+    float ref = 1.0f;
+    if (pg.labels && pg.gout) {
+        if (threadIdx.x == 0) first = rows;
+        __syncthreads();
+        for (int r = 0; r < rows; r += 256) {
+            const int i = r + threadIdx.x;
+            bool has = false;
+            if (i < rows) {
+                const int lab = pg.labels[i];
+                has = lab >= 0 && lab < pg.classes && pg.gout[i] != 0.0f;
+            }
+            if (has) atomicMin(&first, i);
+            if (__syncthreads_or(has)) break;
+        }
+        ref = first < rows ? pg.gout[first] : 0.0f;
+    }
+    if (pg.labels && blockIdx.x == 0 && threadIdx.x == 0) pg.factor[0] = pg.scale * ref;
+    const int per = (int)(ldp / 8);
+    const int64_t words = (int64_t)rows * per, step = (int64_t)gridDim.x * 256;
     const bool vec = sizeof(T) == 2 ? (((uintptr_t)x | (uintptr_t)(ldx * 2)) & 15) == 0
                                     : (((uintptr_t)x | (uintptr_t)ldx) & 7) == 0;
-    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < words; i += (int64_t)gridDim.x * 256) {
-        const int row = (int)(i / (ldp / 8)), c = (int)(i - (int64_t)row * (ldp / 8)) * 8;
+    RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, step, per);
+    for (int64_t i = blockIdx.x * (int64_t)256 + threadIdx.x; i < words; i += step, at.next()) {
+        const int64_t row = at.row;
+        const int c = at.part * 8;
         uint4 v = make_uint4(0, 0, 0, 0);
-        const int lab = labels ? labels[row] : 0;
-        if (!labels || (lab >= 0 && lab < classes)) {
+        bool live = true;
+        float f = 1.0f;
+        if (pg.labels) {
+            const int lab = pg.labels[row];
+            live = lab >= 0 && lab < pg.classes;
+            const float go = live ? (pg.gout ? pg.gout[row] : 1.0f) : 0.0f;
+            f = go == ref ? 1.0f : go / ref;
+            live = live && go != 0.0f;
+            if (c == 0) pg.factor[1 + row] = pg.scale * go;
+        }
+        if (live) {
             const T* src = x + row * ldx + c;
             uint32_t* w = reinterpret_cast<uint32_t*>(&v);
             if constexpr (sizeof(T) == 2) {
                 if (vec && c + 8 <= cols) v = *reinterpret_cast<const uint4*>(src);
-                else
+                else {
+#pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (c + j < cols) w[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+                }
             } else {
                 uint32_t b[2] = {0x80808080u, 0x80808080u};   // bytes hold x + 128
                 if (vec && c + 8 <= cols) {
@@ -337,11 +405,17 @@ __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int 
                     b[0] ^= r.x;
                     b[1] ^= r.y;
                 } else {
+#pragma unroll
                     for (int j = 0; j < 8; ++j)
                         if (c + j < cols) b[j >> 2] ^= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
                 }
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = bf16x2(b[j >> 1], 2 * (j & 1));
+            }
+            if (f != 1.0f) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    w[j] = pack_bf16(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
             }
         }
         reinterpret_cast<uint4*>(out)[i] = v;
@@ -349,6 +423,10 @@ __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int 
 }
 
 int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
+
+// Up to this many rows G is kept as two bf16 halves: the rounding of one entry, up to 2^-8 of
+// it, can be most of a lone row's error, and averages out over more.
+constexpr int kRowsWithLow = 32;
 
 constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
@@ -359,12 +437,14 @@ constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at mos
 struct nitro_xent {
     int max_rows = 0, features = 0, classes = 0;
     int64_t ldp = 0, g_elems = 0, acc_floats = 0;
-    uint16_t* xp = nullptr;     // [max_rows][ldp] bf16 copy of x
+    uint16_t* xp = nullptr;     // [max_rows][ldp] bf16 copy of x where TMA cannot take its rows
+    uint16_t* xg = nullptr;     // and as dw's product takes it, see PackGrad
     uint16_t* wp = nullptr;     // [classes][ldp] copy of W where its rows are not aligned for TMA
     uint16_t* G = nullptr;
     float* acc = nullptr;
     float2* part = nullptr;
     float* zt = nullptr;
+    float* factor = nullptr;    // [1 + max_rows], see PackGrad
     uint32_t* status = nullptr;
     std::vector<void*> allocs;
 };
@@ -387,34 +467,30 @@ bool xalloc(nitro_xent* h, T** p, int64_t count) {
 
 bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
-cudaError_t pack_x(const nitro_xent* h, const void* x, int type, int64_t ldx, int rows, uint16_t* out,
-                   const int32_t* labels, cudaStream_t s) {
-    const int64_t words = (int64_t)rows * (h->ldp / 8);
+cudaError_t pack_rows(const void* x, int type, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
+                      const PackGrad& pg, cudaStream_t s) {
+    const int64_t words = rows * (ldp / 8);
     const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
-    ProfScope ps(K_XENT_PACK, s, 0.0, (double)rows * h->features * (type == NITRO_I8 ? 3 : 4));
+    ProfScope ps(K_XENT_PACK, s, 0.0, (double)rows * cols * (type == NITRO_I8 ? 3 : 4));
     if (type == NITRO_I8)
-        return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, h->features, out,
-                        h->ldp, labels, h->classes);
-    return launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, h->features, out,
-                    h->ldp, labels, h->classes);
+        return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp, pg);
+    return launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, cols, out, ldp, pg);
 }
 
-// x and W as operands of the logits' product (K = features, both along K).
+// x and W as operands of the logits' product (K = features, both along K); copies where
+// TMA cannot take their rows.
 nitro_status xent_operands(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
-                           int rows, const int32_t* labels, bool pack, cudaStream_t s, HgOperand* ox, HgOperand* ow) {
+                           int rows, cudaStream_t s, HgOperand* ox, HgOperand* ow) {
     const int F = h->features;
-    if (pack || x_type == NITRO_I8 || !tma_rows(x, ldx)) {
-        TRY(pack_x(h, x, x_type, ldx, rows, h->xp, labels, s));
+    const PackGrad copy{};
+    if (x_type == NITRO_I8 || !tma_rows(x, ldx)) {
+        TRY(pack_rows(x, x_type, ldx, rows, F, h->xp, h->ldp, copy, s));
         *ox = {h->xp, F, rows, h->ldp, 1, 0};
     } else {
         *ox = {x, F, rows, ldx, 1, 0};
     }
     if (!tma_rows(w, ldw)) {
-        const int64_t words = (int64_t)h->classes * (h->ldp / 8);
-        const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
-        ProfScope ps(K_XENT_PACK, s, 0.0, 4.0 * h->classes * F);
-        TRY(launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, w, ldw, h->classes, F, h->wp, h->ldp,
-                     (const int32_t*)nullptr, 0));
+        TRY(pack_rows(w, NITRO_BF16, ldw, h->classes, F, h->wp, h->ldp, copy, s));
         *ow = {h->wp, F, h->classes, h->ldp, 1, 0};
     } else {
         *ow = {w, F, h->classes, ldw, 1, 0};
@@ -430,27 +506,20 @@ bool xent_args(const nitro_xent* h, const void* x, int x_type, int64_t ldx, cons
     return ((uintptr_t)w & 1) == 0 && (x_type == NITRO_I8 || ((uintptr_t)x & 1) == 0);
 }
 
-// Whether the logits go through slices, and how many: where 128 x 128 tiles are fewer than
-// half the SMs.
-int xent_slices(const nitro_xent* h, int rows) {
-    const int sms = sm_count();
-    HgProblem p{rows, h->classes, h->features};
-    const int tiles = hg_tiles(p, {1, 128});
-    if (2 * tiles > sms) return 0;
-    const int64_t most = h->acc_floats / (rows * round_up(h->classes, 32));
-    const int want = (int)std::min<int64_t>({(int64_t)(sms / tiles), most, (int64_t)((h->features + 127) / 128)});
-    return want < 2 ? 0 : hg_splits(h->features, want);
+// How the logits' product of `classes` classes runs; splits only for a piece of all classes.
+HgPick logits_pick(const nitro_xent* h, int rows, int64_t classes) {
+    const HgProblem p{rows, classes, h->features};
+    int64_t most = 1;
+    if (classes == h->classes) most = std::min<int64_t>(16, h->acc_floats / (rows * round_up(classes, 32)));
+    return hg_pick(p, (int)std::max<int64_t>(1, most));
 }
 
-cudaError_t xent_logit_slices(nitro_xent* h, const HgOperand& ox, const HgOperand& ow, int rows, int slices, cudaStream_t s) {
-    HgProblem p{rows, h->classes, h->features};
-    p.splits = slices;
+HgProblem logits_problem(const nitro_xent* h, int rows, int64_t classes) {
+    HgProblem p{rows, classes, h->features};
     p.status = h->status;
     p.prof = K_XENT_LOGITS;
-    p.ops = 2.0 * rows * h->classes * h->features;
-    const int64_t ldz = round_up(h->classes, 32);
-    const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
-    return hg_launch<EpiAcc, false, false, false>({1, 128}, p, ox, ow, ea, s);
+    p.ops = 2.0 * rows * classes * h->features;
+    return p;
 }
 
 }  // namespace
@@ -470,12 +539,13 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     h->features = features;
     h->classes = classes;
     h->ldp = round_up(features, 8);
-    h->g_elems = std::min(max_rows * round_up(classes, 64), std::max(kGElems, (int64_t)max_rows * 256));
+    h->g_elems = std::max(std::min(max_rows * round_up(classes, 64), std::max(kGElems, (int64_t)max_rows * 256)),
+                          2 * std::min(max_rows, kRowsWithLow) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
     const int64_t parts = 2 * ((classes + 127) / 128);
-    const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
+    const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->xg, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
                     xalloc(h, &h->G, h->g_elems) && xalloc(h, &h->acc, h->acc_floats) &&
-                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->status, 1) && cudaMemset(h->status, 0, 4) == cudaSuccess;
+                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->factor, max_rows + 1) && xalloc(h, &h->status, 1) && cudaMemset(h->status, 0, 4) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -491,23 +561,20 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     if (!loss || !lse) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     HgOperand ox, ow;
-    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, nullptr, false, s, &ox, &ow);
+    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
     if (st != NITRO_OK) return st;
     const RowOut ro{labels, loss, lse, h->status, h->classes};
-    const int slices = xent_slices(h, rows);
-    if (slices) {
-        TRY(xent_logit_slices(h, ox, ow, rows, slices, s));
+    const HgPick t = logits_pick(h, rows, h->classes);
+    const HgProblem p = logits_problem(h, rows, h->classes);
+    if (t.splits > 1) {
         const int64_t ldz = round_up(h->classes, 32);
-        ProfScope ps(K_XENT_ROWS, s, 0.0, 4.0 * slices * rows * h->classes);
-        TRY(launch_k(k_xent_rows, dim3(rows), dim3(256), 0, s, (const float*)h->acc, ldz, rows * ldz, slices, h->classes,
+        const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
+        TRY((hg_launch<EpiAcc, false, false, false>(t, p, ox, ow, ea, s)));
+        ProfScope ps(K_XENT_ROWS, s, 0.0, 4.0 * t.splits * rows * h->classes);
+        TRY(launch_k(k_xent_rows, dim3(rows), dim3(256), 0, s, (const float*)h->acc, ldz, rows * ldz, t.splits, h->classes,
                      scale * kLog2e, scale, ro));
         return NITRO_OK;
     }
-    HgProblem p{rows, h->classes, h->features};
-    p.status = h->status;
-    p.prof = K_XENT_LOGITS;
-    p.ops = 2.0 * rows * h->classes * h->features;
-    const HgPick t = hg_pick(p);
     const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, h->zt};
     TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
     const int parts = 2 * ((h->classes + t.bn - 1) / t.bn);
@@ -533,71 +600,74 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
     }
     if (!dx && !dw) return NITRO_OK;
     HgOperand ox, ow;
-    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, labels, true, s, &ox, &ow);
+    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
     if (st != NITRO_OK) return st;
-    const float k2 = scale * kLog2e;
-    const int slices = xent_slices(h, rows);
-    int64_t piece = std::min<int64_t>(round_up(V, 64), h->g_elems / rows / 64 * 64);
+    const PackGrad pg{labels, gout, h->factor, scale, V};
+    TRY(pack_rows(x, x_type, ldx, rows, F, h->xg, h->ldp, pg, s));
+    const HgOperand og{h->xg, F, rows, h->ldp, 1, 0};
+    const int halves = rows <= kRowsWithLow ? 2 : 1;
+    int64_t piece = std::min<int64_t>(round_up(V, 64), h->g_elems / halves / rows / 64 * 64);
     if (piece < V) piece = piece / 256 * 256;
-    // dx: slices along the classes where its tiles leave SMs idle
-    HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
+    // dx: in slices along the classes where its tiles leave SMs idle
     const int64_t ldc = round_up(F, 32);
-    int dsplit = 1;
-    {
-        const int tiles = hg_tiles(pd, {1, 128}), sms = sm_count();
-        if (2 * tiles <= sms)
-            dsplit = (int)std::max<int64_t>(1, std::min<int64_t>({(int64_t)(sms / tiles), h->acc_floats / (rows * ldc), pd.K / 256}));
-        dsplit = hg_splits(pd.K, dsplit);
-    }
+    HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
+    pd.products = halves;
+    const HgPick td = hg_pick(pd, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
+    const bool direct = piece >= V && td.splits == 1;
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int64_t n = std::min<int64_t>(piece, V - v0);
         HgOperand wp = ow;
         wp.base = static_cast<const uint16_t*>(ow.base) + v0 * ow.ld;
         wp.outer = n;
-        const EpiProb::Args ep{labels, lse, gout, k2, scale, V, (int)v0, h->G, round_up(n, 64)};
-        if (slices && piece >= V) {
-            TRY(xent_logit_slices(h, ox, ow, rows, slices, s));
+        const EpiProb::Args ep{labels, lse, scale * kLog2e, V, (int)v0, h->G, round_up(n, 64),
+                                halves == 2 ? rows * round_up(n, 64) : 0};
+        const HgPick tl = logits_pick(h, rows, n);
+        const HgProblem pl = logits_problem(h, rows, n);
+        if (tl.splits > 1) {
             const int64_t ldz = round_up(V, 32);
-            ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * slices + 2.0) * rows * V);
-            TRY(launch_k(k_xent_probs, dim3(rows, (unsigned)std::min<int64_t>(8, (ep.ldg + 255) / 256)), dim3(256), 0, s,
-                         (const float*)h->acc, ldz, rows * ldz, slices, ep));
+            const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
+            TRY((hg_launch<EpiAcc, false, false, false>(tl, pl, ox, wp, ea, s)));
+            ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * tl.splits + 2.0) * rows * V);
+            TRY(launch_k(k_xent_probs, dim3(rows, (unsigned)std::min<int64_t>(8, (V + 255) / 256)), dim3(256), 0, s,
+                         (const float*)h->acc, ldz, rows * ldz, tl.splits, ep));
         } else {
-            HgProblem p{rows, n, F};
-            p.status = h->status;
-            p.prof = K_XENT_LOGITS;
-            p.ops = 2.0 * rows * n * F;
-            TRY((hg_launch<EpiProb, false, false, false>(hg_pick(p), p, ox, wp, ep, s)));
+            TRY((hg_launch<EpiProb, false, false, false>(tl, pl, ox, wp, ep, s)));
         }
-        const HgOperand G{h->G, n, rows, ep.ldg, 1, 0};
+        const HgOperand G{h->G, n, rows, ep.ldg, halves, rows * ep.ldg};
         if (dx) {
             HgProblem p{rows, F, n};
+            p.planes_a = halves;
             p.status = h->status;
             p.prof = K_XENT_DX;
             p.ops = 2.0 * rows * n * F;
-            p.splits = hg_splits(n, dsplit);
-            const HgPick t = dsplit > 1 ? HgPick{1, 128} : hg_pick(p);
-            if (piece >= V && dsplit == 1) {
-                const EpiBf16::Args eb{dx, lddx, tma_rows(dx, lddx)};
-                TRY((hg_launch<EpiBf16, false, true, false>(t, p, G, wp, eb, s)));
+            if (direct) {
+                const EpiBf16::Args eb{dx, lddx, tma_rows(dx, lddx), h->factor + 1, 0};
+                if (halves == 2) TRY((hg_launch<EpiBf16, false, true, false, 2, 1>(td, p, G, wp, eb, s)));
+                else TRY((hg_launch<EpiBf16, false, true, false>(td, p, G, wp, eb, s)));
             } else {
-                // a last piece with fewer slices adds to the first ones
+                // a shorter last piece has as many slices or fewer: it adds to the first ones
+                const HgPick t{td.cg, td.bn, hg_splits(n, td.splits)};
                 const EpiAcc::Args ea{h->acc, ldc, rows * ldc, v0 > 0};
-                TRY((hg_launch<EpiAcc, false, true, false>(t, p, G, wp, ea, s)));
+                if (halves == 2) TRY((hg_launch<EpiAcc, false, true, false, 2, 1>(t, p, G, wp, ea, s)));
+                else TRY((hg_launch<EpiAcc, false, true, false>(t, p, G, wp, ea, s)));
             }
         }
         if (dw) {
             HgProblem p{n, F, rows};
+            p.planes_a = p.products = halves;
             p.status = h->status;
             p.prof = K_XENT_DW;
             p.ops = 2.0 * rows * n * F;
-            const EpiBf16::Args eb{dw + v0 * lddw, lddw, tma_rows(dw, lddw)};
-            TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, G, ox, eb, s)));
+            const EpiBf16::Args eb{dw + v0 * lddw, lddw, tma_rows(dw, lddw), h->factor, 1};
+            if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p), p, G, og, eb, s)));
+            else TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, G, og, eb, s)));
         }
     }
-    if (dx && (piece < V || dsplit > 1)) {
-        ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * dsplit + 2.0) * rows * F);
-        TRY(launch_k(k_xent_dx, dim3(rows, (unsigned)std::min(8, (F + 255) / 256)), dim3(256), 0, s, (const float*)h->acc,
-                     ldc, rows * ldc, dsplit, F, dx, lddx));
+    if (dx && !direct) {
+        ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * td.splits + 2.0) * rows * F);
+        TRY(launch_k(k_xent_dx, dim3(rows, (unsigned)std::min(8, (F + 1023) / 1024)), dim3(256), 0, s, (const float*)h->acc,
+                     ldc, rows * ldc, td.splits, F, (const float*)h->factor + 1, dx, lddx,
+                     (int)(((uintptr_t)dx & 7) == 0 && lddx % 4 == 0)));
     }
     return NITRO_OK;
 }

@@ -179,6 +179,26 @@ __host__ __device__ __forceinline__ int limb_count(uint32_t m) {
 }
 
 #ifdef __CUDACC__
+// Positions (row, part) of a grid-wide walk over rows of `per` parts, without a division a step.
+struct RowWalk {
+    int64_t row, drow;
+    int part, dpart, per;
+    __device__ __forceinline__ RowWalk(int64_t first, int64_t step, int per_) : per(per_) {
+        row = first / per;
+        part = (int)(first - row * per);
+        drow = step / per;
+        dpart = (int)(step - drow * per);
+    }
+    __device__ __forceinline__ void next() {
+        row += drow;
+        part += dpart;
+        if (part >= per) {
+            part -= per;
+            ++row;
+        }
+    }
+};
+
 // two int8 values v (bytes i, i + 1 of a word whose bytes hold v + 128) -> two bf16:
 // 2^23 + (v + 128) is the float 0x4B0000xx, and subtracting 2^23 + 128 leaves v
 // exactly, whose upper half is its bf16
