@@ -17,6 +17,10 @@
 // halves the bytes of B an SM has to load and read for the same products, which is what
 // bounds the lone form (see the figures at pick_tile()).
 //
+// KS > 1 gives a tile's K to a cluster of KS (2 or 4) lone CTAs, where there are few tiles:
+// their sums meet in distributed shared memory, a slice of the columns for each CTA, are
+// added in the CTAs' order, and every CTA takes its slice through the epilogue.
+//
 // Every wait is bounded; on expiry the kernel raises TIMEOUT, drains its own copies and
 // MMAs in flight (bounded as well), frees TMEM and returns.
 #pragma once
@@ -173,11 +177,13 @@ __device__ __forceinline__ void hg_tmem_free(uint32_t tmem, uint32_t cols) {
 }
 
 // Epi: struct Args, and per tile and thread
-//   Epi(args, g, tile, row, col0, half)   row: this thread's row of D; col0: its first
-//       column, that of the tile's half 0 or 1
-//   void cols(c, v)                 v[0..32): columns col0 + c .. col0 + c + 31
+//   Epi(args, g, tile, row, col0, width, slot)   row: this thread's row of D; col0, width: its
+//       columns, slot: which part of the tile's columns that is (BN / width parts)
+//   void fetch(c)           starts loading what cols(c) needs (called for c = 0; cols(c)
+//                           calls it for the next)
+//   void cols(c, v)         v[0..32): columns col0 + c .. col0 + c + 31
 //   void done()
-template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB>
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB, int KS>
 __global__ void __launch_bounds__(kHgThreads, 1)
     k_head_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const HgArgs g,
                 const __grid_constant__ typename Epi::Args ea) {
@@ -197,7 +203,15 @@ __global__ void __launch_bounds__(kHgThreads, 1)
     const auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };
     const uint32_t drain_bar = bar0 + 8u * (2 * S + 4);
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
-    const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
+    static_assert(KS == 1 || (CG == 1 && BN == 128), "a tile's K is shared out among lone CTAs");
+    // a cluster that shares a tile's K: its CTAs are the tile's splits
+    const int part = KS > 1 ? (int)cluster_rank() : 0;
+    int unit = (int)blockIdx.x / (KS > 1 ? KS : CG);
+    if constexpr (KS > 1) {
+        const int tiles = g.total / (KS * g.batch);
+        unit += (unit / tiles * (KS - 1) + part) * tiles;
+    }
+    const int units = KS > 1 ? g.total : (int)gridDim.x / CG;
 
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
@@ -329,36 +343,85 @@ __global__ void __launch_bounds__(kHgThreads, 1)
         for (int tile = unit; tile < g.total; tile += units, ++it) {
             const HgTile T = hg_decode<TM, BN>(g, tile);
             const int buf = it & 1;
-            Epi epi(ea, g, T, T.m * TM + rank * 128 + q * 32 + lane, T.n * BN + half * (BN / 2), half);
-            const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it >> 1) & 1u, abort_flag, g.status);
-            if (!__all_sync(0xffffffffu, ok)) break;
-            tc_fence_after();
-            const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
-            uint32_t v[2][32];
-            tmem_ld32_nowait(src, v[0]);
+            const int row = T.m * TM + rank * 128 + q * 32 + lane;
+            if constexpr (KS > 1) {
+                constexpr int W = BN / KS;                       // columns of a CTA's slice
+                float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
+                Epi epi(ea, g, T, row, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half);
+                const bool mine = 32 * half < W;
+                if (mine) epi.fetch(0);
+                bool ok = mbar_wait(tfull_bar(buf), 0, abort_flag, g.status);
+                ok = __all_sync(0xffffffffu, ok);
+                tc_fence_after();
+                cluster_barrier();       // every CTA's MMAs have read their operands
+                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (BN / 2));
 #pragma unroll
-            for (int c = 0; c < BN / 64; ++c) {
-                tmem_wait_ld<32>(v[c & 1]);
-                if (c + 1 < BN / 64) tmem_ld32_nowait(src + 32 * (c + 1), v[(c + 1) & 1]);
-                else {
-                    // the sums are in registers: the accumulator may be filled again
-                    tc_fence_before();
+                for (int c = 0; c < BN / 2; c += 32) {
+                    uint32_t v[32];
                     __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
-                        else mbar_arrive(tempty_bar(buf));
-                    }
+                    tmem_ld32_nowait(src + c, v);
+                    tmem_wait_ld<32>(v);
+                    const int col = half * (BN / 2) + c;
+                    const uint32_t to = remote_smem(smem_u32(stage + (part * (W / 4) + (col % W) / 4) * 128 + q * 32 + lane), col / W);
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) st_remote4(to + j * 2048, v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 }
-                float* f = reinterpret_cast<float*>(v[c & 1]);
-                epi.cols(32 * c, f);
+                cluster_barrier();
+                if (mine && ok) {
+                    float v[32];
+#pragma unroll
+                    for (int j = 0; j < 8; ++j) {
+                        float4 s = stage[(8 * half + j) * 128 + q * 32 + lane];
+#pragma unroll
+                        for (int k = 1; k < KS; ++k) {
+                            const float4 o = stage[(k * (W / 4) + 8 * half + j) * 128 + q * 32 + lane];
+                            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+                        }
+                        v[4 * j] = s.x, v[4 * j + 1] = s.y, v[4 * j + 2] = s.z, v[4 * j + 3] = s.w;
+                    }
+                    epi.cols(0, v);
+                    epi.done();
+                }
+            } else {
+                Epi epi(ea, g, T, row, T.n * BN + half * (BN / 2), BN / 2, half);
+                epi.fetch(0);
+                const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it >> 1) & 1u, abort_flag, g.status);
+                if (!__all_sync(0xffffffffu, ok)) break;
+                tc_fence_after();
+                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
+                uint32_t v[2][32];
+                tmem_ld32_nowait(src, v[0]);
+#pragma unroll
+                for (int c = 0; c < BN / 64; ++c) {
+                    __syncwarp();
+                    tmem_wait_ld<32>(v[c & 1]);
+                    if (c + 1 < BN / 64) tmem_ld32_nowait(src + 32 * (c + 1), v[(c + 1) & 1]);
+                    else {
+                        // the sums are in registers: the accumulator may be filled again
+                        tc_fence_before();
+                        __syncwarp();
+                        if (lane == 0) {
+                            if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
+                            else mbar_arrive(tempty_bar(buf));
+                        }
+                    }
+                    epi.cols(32 * c, reinterpret_cast<float*>(v[c & 1]));
+                }
+                epi.done();
             }
-            epi.done();
+        }
+    }
+    if constexpr (KS > 1) {
+        if (warp < kHgEpiWarp0) {    // the two of the epilogue's exchange
+            __syncwarp();
+            cluster_barrier();
+            cluster_barrier();
         }
     }
     __syncwarp();
     tc_fence_before();
     __syncthreads();
-    if constexpr (CG == 2) cluster_barrier();   // no copy, MMA or arrival of the pair is outstanding
+    if constexpr (CG == 2 || KS > 1) cluster_barrier();   // no copy, MMA or arrival of the pair is outstanding
     if (warp == 2) {
         tc_fence_after();
         hg_tmem_free<CG>(tmem, C::TCOLS);
@@ -402,7 +465,8 @@ inline int hg_splits(int64_t K, int want) {
 
 // How a product runs: CTAs that work on a tile (1 or 2), its columns, and splits of K.
 struct HgPick {
-    int cg, bn, splits;
+    int cg, bn, splits;        // splits: slices of the caller's
+    int ks = 1;                // CTAs of a cluster that share a tile's K
 };
 
 inline int64_t hg_tiles(const HgProblem& p, int cg, int bn) {
@@ -431,17 +495,27 @@ inline HgPick hg_pick(const HgProblem& p, int max_splits = 1) {
             const int s = hg_splits(p.K, w);
             if (s != w) continue;
             int64_t c = (tiles * s + units - 1) / units * ((kb + s - 1) / s * p.products * f.clocks + 1500);
+            if (f.cg == 2) c += 2500;      // a pair's launch and its barriers
             if (s > 1) c += 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500;
             if (c < least) {
                 least = c;
                 best = {f.cg, f.bn, s};
             }
         }
+        // or shared out in a cluster: its barriers and the exchange
+        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 4; s *= 2) {
+            if (hg_splits(p.K, s) != s) continue;
+            const int64_t c = (tiles * s + units - 1) / units * ((kb + s - 1) / s * p.products * f.clocks + 1500) + 4500;
+            if (c < least) {
+                least = c;
+                best = {1, 128, 1, s};
+            }
+        }
     }
     return best;
 }
 
-template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB>
+template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB, int KS = 1>
 cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, const HgOperand& b, const typename Epi::Args& ea,
                          cudaStream_t s) {
     using C = HgCfg<CG, BN, HA, HB>;
@@ -465,14 +539,15 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
     const int sms = sm_count(&dev);
-    const auto kernel = k_head_gemm<Epi, CG, BN, AMN, BMN, F16, HA, HB>;
+    const auto kernel = k_head_gemm<Epi, CG, BN, AMN, BMN, F16, HA, HB, KS>;
     const cudaError_t e = once_per_device(ready, dev, [kernel] {
         return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
     if (e != cudaSuccess) return e;
     const int grid = std::min(g.total, sms / CG) * CG;
     ProfScope ps(p.prof, s, p.ops, p.bytes);
-    if constexpr (CG == 2) return launch_cluster(kernel, dim3(grid), kHgThreads, 2, s, C::SMEM, ma, mb, g, ea);
+    if constexpr (KS > 1) return launch_cluster(kernel, dim3(g.total), kHgThreads, KS, s, C::SMEM, ma, mb, g, ea);
+    else if constexpr (CG == 2) return launch_cluster(kernel, dim3(grid), kHgThreads, 2, s, C::SMEM, ma, mb, g, ea);
     else return launch_k(kernel, dim3(grid), dim3(kHgThreads), C::SMEM, s, ma, mb, g, ea);
 }
 
@@ -481,6 +556,9 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
 template <class Epi, bool AMN, bool BMN, bool F16, int HA = 1, int HB = 1>
 cudaError_t hg_launch(const HgPick& t, const HgProblem& p, const HgOperand& a, const HgOperand& b,
                       const typename Epi::Args& ea, cudaStream_t s) {
+    // (a K too short for the cluster goes to lone CTAs)
+    if (t.ks == 2 && hg_splits(p.K, 2) == 2) return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB, 2>(2, p, a, b, ea, s);
+    if (t.ks == 4 && hg_splits(p.K, 4) == 4) return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB, 4>(4, p, a, b, ea, s);
     if (t.cg == 2 && t.bn == 256) return hg_launch_as<Epi, 2, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
     if (t.cg == 2) return hg_launch_as<Epi, 2, 128, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
     if (t.bn == 256) return hg_launch_as<Epi, 1, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);

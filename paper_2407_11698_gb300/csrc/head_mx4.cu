@@ -422,6 +422,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
             uint16_t* yb = static_cast<uint16_t*>(g.y);
 #pragma unroll 4
             for (int c = 0; c < BN / 2; c += 16) {
+                __syncwarp();
                 uint32_t v[16];
                 tmem_ld16_nowait(src + c, v);
                 tmem_wait_ld<16>(v);

@@ -29,47 +29,46 @@ namespace {
 constexpr float kNormEps = 1e-7f;
 constexpr int kNormCtas = 1024;     // partial sums of squares a matrix, at most
 
-// v -> its high and low half
-__device__ __forceinline__ void split_half(float v, __half* hi, __half* lo) {
-    *hi = __float2half_rn(v);
-    *lo = __float2half_rn(v - __half2float(*hi));
-}
-__device__ __forceinline__ uint32_t pack_half(__half a, __half b) {
-    return (uint32_t)__half_as_ushort(a) | (uint32_t)__half_as_ushort(b) << 16;
+__device__ __forceinline__ float2 halves2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
+// two values -> a word of their high and a word of their low halves.  Pairs, since the
+// conversion of two floats to a pair is one instruction at a higher rate than that of one
+// (32 columns a thread through the steps' sums: 3300 clocks, now HALVES_MEASURED).
+__device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint32_t* lo) {
+    const __half2 h = __floats2half2_rn(a, b);
+    const float2 back = __half22float2(h);
+    const __half2 l = __floats2half2_rn(a - back.x, b - back.y);
+    *hi = *reinterpret_cast<const uint32_t*>(&h);
+    *lo = *reinterpret_cast<const uint32_t*>(&l);
 }
 // 32 floats as high (and low, if lo) halves at an 64-byte aligned place
-__device__ __forceinline__ void store_halves(uint16_t* hi, uint16_t* lo, const float* v) {
+__device__ __forceinline__ void store_halves(uint16_t* hi, uint16_t* lo, const uint32_t* h, const uint32_t* l) {
 #pragma unroll
     for (int j = 0; j < 4; ++j) {
-        uint32_t h[4], l[4];
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            __half h0, h1, l0, l1;
-            split_half(v[8 * j + 2 * k], &h0, &l0);
-            split_half(v[8 * j + 2 * k + 1], &h1, &l1);
-            h[k] = pack_half(h0, h1);
-            l[k] = pack_half(l0, l1);
-        }
-        reinterpret_cast<uint4*>(hi)[j] = make_uint4(h[0], h[1], h[2], h[3]);
-        if (lo) reinterpret_cast<uint4*>(lo)[j] = make_uint4(l[0], l[1], l[2], l[3]);
+        reinterpret_cast<uint4*>(hi)[j] = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
+        if (lo) reinterpret_cast<uint4*>(lo)[j] = make_uint4(l[4 * j], l[4 * j + 1], l[4 * j + 2], l[4 * j + 3]);
     }
 }
-// adds f times the 32 values held at hi (+ lo)
-__device__ __forceinline__ void add_halves(const uint16_t* hi, const uint16_t* lo, float f, float* v) {
+// 32 values held as halves, loaded ahead of their use
+struct Halves32 {
+    uint4 h[4], l[4];
+    __device__ __forceinline__ void load(const uint16_t* hi, const uint16_t* lo) {
 #pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const uint4 h = reinterpret_cast<const uint4*>(hi)[j];
-        const uint4 l = lo ? reinterpret_cast<const uint4*>(lo)[j] : make_uint4(0, 0, 0, 0);
-        const uint32_t hw[4] = {h.x, h.y, h.z, h.w}, lw[4] = {l.x, l.y, l.z, l.w};
-#pragma unroll
-        for (int k = 0; k < 4; ++k) {
-            const float2 a = __half22float2(*reinterpret_cast<const __half2*>(&hw[k]));
-            const float2 b = __half22float2(*reinterpret_cast<const __half2*>(&lw[k]));
-            v[8 * j + 2 * k] = fmaf(f, a.x + b.x, v[8 * j + 2 * k]);
-            v[8 * j + 2 * k + 1] = fmaf(f, a.y + b.y, v[8 * j + 2 * k + 1]);
+        for (int j = 0; j < 4; ++j) {
+            h[j] = reinterpret_cast<const uint4*>(hi)[j];
+            l[j] = lo ? reinterpret_cast<const uint4*>(lo)[j] : make_uint4(0, 0, 0, 0);
         }
     }
-}
+    // v = g v + f times the values
+    __device__ __forceinline__ void join(float g, float f, float* v) const {
+        const uint32_t *hw = reinterpret_cast<const uint32_t*>(h), *lw = reinterpret_cast<const uint32_t*>(l);
+#pragma unroll
+        for (int j = 0; j < 16; ++j) {
+            const float2 a = halves2(hw[j]), b = halves2(lw[j]);
+            v[2 * j] = fmaf(f, a.x + b.x, v[2 * j] * g);
+            v[2 * j + 1] = fmaf(f, a.y + b.y, v[2 * j + 1] * g);
+        }
+    }
+};
 
 // Planes of a tensor of the batch: high at base + 2 b plane, low one plane further.
 struct Planes {
@@ -88,40 +87,53 @@ struct EpiSym {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0;
+    int row, col0, width;
     uint16_t *hi, *lo;
     const uint16_t* add = nullptr;
     float f;
-    __device__ __forceinline__ EpiSym(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int)
-        : a(a_), g(g_), row(row_), col0(col0_) {
+    Halves32 old;
+    __device__ __forceinline__ EpiSym(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int width_, int)
+        : a(a_), g(g_), row(row_), col0(col0_), width(width_) {
         hi = a.out.base + 2 * t.batch * a.out.plane;
         lo = a.low ? hi + a.out.plane : nullptr;
         f = a.f;
         if (a.scale) f *= a.scale[t.batch] * a.scale[t.batch];
         if (a.add.base) add = a.add.base + 2 * t.batch * a.add.plane + (int64_t)row * a.add.ld;
     }
+    __device__ __forceinline__ bool skip(int col) const { return row >= g.M || col >= g.N || col + 31 < row; }
+    __device__ __forceinline__ void fetch(int c) {
+        const int col = col0 + c;
+        if (add && !skip(col)) old.load(add + col, a.low_add ? add + a.add.plane + col : nullptr);
+    }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = col0 + c;
-        if (row >= g.M || col >= g.N || col + 31 < row) return;
+        if (!skip(col)) {
+            if (add) old.join(f, a.fa, v);
+            else {
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= f;
-        if (add) add_halves(add + col, a.low_add ? add + a.add.plane + col : nullptr, a.fa, v);
+                for (int j = 0; j < 32; ++j) v[j] *= f;
+            }
+        }
+        if (c + 32 < width) fetch(c + 32);
+        if (skip(col)) return;
+        uint32_t h[16], l[16];
+#pragma unroll
+        for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
         if (col > row) {
             // the padding of a row may be written
-            uint16_t* h = hi + (int64_t)row * a.out.ld + col;
-            store_halves(h, lo ? lo + (h - hi) : nullptr, v);
+            uint16_t* at = hi + (int64_t)row * a.out.ld + col;
+            store_halves(at, lo ? lo + (at - hi) : nullptr, h, l);
         }
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             const int cj = col + j;
             if (cj < row || cj >= g.N) continue;
-            __half h, l;
-            split_half(v[j], &h, &l);
-            hi[(int64_t)cj * a.out.ld + row] = __half_as_ushort(h);
-            if (lo) lo[(int64_t)cj * a.out.ld + row] = __half_as_ushort(l);
+            const uint16_t hj = (uint16_t)(h[j >> 1] >> (16 * (j & 1))), lj = (uint16_t)(l[j >> 1] >> (16 * (j & 1)));
+            hi[(int64_t)cj * a.out.ld + row] = hj;
+            if (lo) lo[(int64_t)cj * a.out.ld + row] = lj;
             if (col <= row) {
-                hi[(int64_t)row * a.out.ld + cj] = __half_as_ushort(h);
-                if (lo) lo[(int64_t)row * a.out.ld + cj] = __half_as_ushort(l);
+                hi[(int64_t)row * a.out.ld + cj] = hj;
+                if (lo) lo[(int64_t)row * a.out.ld + cj] = lj;
             }
         }
     }
@@ -141,24 +153,32 @@ struct EpiUpdate {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0, batch;
+    int row, col0, width, batch;
     float f, fx;
-    __device__ __forceinline__ EpiUpdate(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int)
-        : a(a_), g(g_), row(row_), col0(col0_), batch(t.batch) {
+    Halves32 old;
+    __device__ __forceinline__ EpiUpdate(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int width_, int)
+        : a(a_), g(g_), row(row_), col0(col0_), width(width_), batch(t.batch) {
         const float k = a.scale ? a.scale[batch] : 1.0f;
         f = a.f * k;
         fx = a.fx * k;
     }
+    __device__ __forceinline__ void fetch(int c) {
+        if (row >= g.M || col0 + c >= g.N) return;
+        const uint16_t* x = a.x.base + 2 * batch * a.x.plane + (int64_t)row * a.x.ld + col0 + c;
+        old.load(x, a.low_x ? x + a.x.plane : nullptr);
+    }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = col0 + c;
-        if (row >= g.M || col >= g.N) return;
-#pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] *= f;
-        const uint16_t* x = a.x.base + 2 * batch * a.x.plane + (int64_t)row * a.x.ld + col;
-        add_halves(x, a.low_x ? x + a.x.plane : nullptr, fx, v);
+        const bool skip = row >= g.M || col >= g.N;
+        if (!skip) old.join(f, fx, v);
+        if (c + 32 < width) fetch(c + 32);
+        if (skip) return;
         if (!a.last) {
             uint16_t* o = a.out.base + 2 * batch * a.out.plane + (int64_t)row * a.out.ld + col;
-            store_halves(o, a.low ? o + a.out.plane : nullptr, v);
+            uint32_t h[16], l[16];
+#pragma unroll
+            for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
+            store_halves(o, a.low ? o + a.out.plane : nullptr, h, l);
             return;
         }
         uint16_t* o = a.last + batch * a.stride_last + (int64_t)row * a.ld_last + col;
@@ -289,13 +309,8 @@ __global__ void __launch_bounds__(256) k_orth_pack(const T* m, int64_t ld, int64
             if (to[u] < 0) continue;
             uint32_t h[E / 2], l[E / 2];
 #pragma unroll
-            for (int j = 0; j < E / 2; ++j) {
-                __half h0, h1, l0, l1;
-                split_half(as_float(r[u].v[2 * j]) * f, &h0, &l0);
-                split_half(as_float(r[u].v[2 * j + 1]) * f, &h1, &l1);
-                h[j] = pack_half(h0, h1);
-                l[j] = pack_half(l0, l1);
-            }
+            for (int j = 0; j < E / 2; ++j)
+                split_pair(as_float(r[u].v[2 * j]) * f, as_float(r[u].v[2 * j + 1]) * f, &h[j], &l[j]);
             const auto put = [](uint16_t* p, const uint32_t* w) {
                 if constexpr (E == 8) *reinterpret_cast<uint4*>(p) = make_uint4(w[0], w[1], w[2], w[3]);
                 else if constexpr (E == 4) *reinterpret_cast<uint2*>(p) = make_uint2(w[0], w[1]);
@@ -319,6 +334,369 @@ __global__ void __launch_bounds__(256) k_orth_copy(Planes x, float mul, int low,
         const uint16_t* p = hi + r * x.ld + c;
         const float v = (__half2float(__ushort_as_half(p[0])) + (low ? __half2float(__ushort_as_half(p[x.plane])) : 0.0f)) * mul;
         out[blockIdx.y * stride + r * ld + c] = __bfloat16_as_ushort(__float2bfloat16_rn(v));
+    }
+}
+
+// ------------------------------------------------------------------ small matrices
+// All steps in one launch for matrices whose shorter side m is at most 128: a cluster of
+// C CTAs holds X (m x n, the transpose of a tall matrix) in shared memory, n / C columns each,
+// as the 64-column blocks of 128-byte rows that the MMAs read along K (A = X X^T) and
+// across it (B X) alike.  Every CTA has all of A and B.  A step is three batches of MMAs,
+// each followed by its sums' way through the registers into the next one's operands; for
+// C > 1 the parts of A meet by column slices in distributed shared memory, are added in the
+// CTAs' order, and go back to all.  Bound by the latency of that chain: ORTH_SMALL_MEASURED
+// A wait that gives up latches TIMEOUT; the CTA then goes through the rest without waiting, so
+// that the cluster's barriers and stores stay matched.
+constexpr int kOsThreads = 512;      // four warps a TMEM lane quadrant, a quarter of the columns each
+
+struct OsArgs {
+    const void* m;
+    int64_t ld, stride;
+    uint16_t* out;
+    int64_t ld_out, stride_out;
+    int rows, cols;          // of M
+    int tall;
+    int mp;                  // m rounded up to 32
+    int nb;                  // blocks of 64 columns a CTA holds
+    int steps;
+    int exact_first;         // X0's low halves are zero
+    int vec, vec_out;        // rows of M and of the result are 16-byte aligned
+    float mul, fa, fs, fsa, fu, fux, fu_last, fux_last;
+    uint32_t* status;
+};
+
+// byte offset of 16-byte chunk j of row r in a block of 128-byte rows (128-byte swizzle)
+__device__ __forceinline__ uint32_t sw_chunk(int r, int j) { return (uint32_t)(r * 128 + ((j ^ (r & 7)) << 4)); }
+
+template <typename T, int C>
+__global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
+    extern __shared__ uint8_t smem_raw[];
+    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    const int sb = (a.mp + 63) / 64;                     // blocks of A and B
+    uint8_t* xh = smem;                                  // [nb] blocks of 16 KB, then their low halves
+    uint8_t* xl = xh + a.nb * 16384;
+    uint8_t* sh = xl + a.nb * 16384;                     // A, then B
+    uint8_t* sl = sh + sb * 16384;
+    uint8_t* tail = sl + sb * 16384;
+    uint64_t* bar = reinterpret_cast<uint64_t*>(tail);
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 1);
+    volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
+    float* parts = reinterpret_cast<float*>(tail + 64);  // [16] warps, then [8] CTAs
+    const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
+    const int rank = C > 1 ? (int)cluster_rank() : 0;
+    const int64_t mat = blockIdx.x / C;
+    const int m = a.tall ? a.cols : a.rows, n = a.tall ? a.rows : a.cols;
+    const int c0 = rank * a.nb * 64;                     // this CTA's first column of X
+    const int nc = max(0, min(a.nb * 64, n - c0));
+    const uint32_t bar_a = smem_u32(bar);
+    if (tid == 0) {
+        mbar_init(bar_a, 1);
+        *abort_flag = 0;
+        asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
+    }
+    if (warp == 0) hg_tmem_alloc<1>(smem_u32(tmem_slot), 512);
+    for (int i = tid; i < a.nb * 2048; i += kOsThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+    pdl_wait();
+    tc_fence_before();
+    __syncthreads();
+    tc_fence_after();
+    const uint32_t tmem = *tmem_slot;
+
+    // ---------------- norm and first planes
+    // 16 bytes of M at a time; until the norm is known, the bits of a value (fp32) wait in its
+    // places in the two planes
+    constexpr int E = Vec16<T>::E;
+    const T* src = static_cast<const T*>(a.m) + mat * a.stride + (a.tall ? c0 * a.ld : c0);
+    const int len = a.tall ? m : nc, lines = a.tall ? nc : m;      // of this CTA's slice as it lies in memory
+    float s = 0.0f;
+    if (len > 0) {
+        RowWalk at(tid, kOsThreads, (len + E - 1) / E);
+        while (at.row < lines) {
+            constexpr int U = 4;
+            Vec16<T> v[U];
+            int line[U], pos[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                line[u] = at.row < lines ? (int)at.row : -1;
+                pos[u] = at.part * E;
+                v[u].load(src + at.row * a.ld + at.part * E, at.row < lines ? len - at.part * E : 0, a.vec != 0);
+                at.next();
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                if (line[u] < 0) continue;
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    if (pos[u] + j >= len) continue;
+                    const float f = as_float(v[u].v[j]);
+                    s = fmaf(f, f, s);
+                    const int r = a.tall ? pos[u] + j : line[u], c = a.tall ? line[u] : pos[u] + j;
+                    const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(r, (c & 63) >> 3) + (c & 7) * 2;
+                    *reinterpret_cast<uint16_t*>(xh + o) = (uint16_t)(__float_as_uint(f) >> 16);
+                    *reinterpret_cast<uint16_t*>(xl + o) = (uint16_t)__float_as_uint(f);
+                }
+            }
+        }
+    }
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    if (lane == 0) parts[warp] = s;
+    __syncthreads();
+    s = 0.0f;
+    for (int w = 0; w < 16; ++w) s += parts[w];
+    if constexpr (C > 1) {
+        cluster_barrier();       // every CTA of the cluster runs
+        if (tid < C) {
+            const uint32_t to = remote_smem(smem_u32(parts + 16 + rank), (uint32_t)tid);
+            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(s) : "memory");
+        }
+        cluster_barrier();
+        s = 0.0f;
+        for (int r = 0; r < C; ++r) s += parts[16 + r];
+    }
+    const float eps = sizeof(T) == 8 ? kNormEps * 0x1p-32f : kNormEps;
+    const float full = 1.0f / (sqrtf(s) + eps);
+    int e;
+    float left = frexpf(full, &e);           // see k_orth_pack
+    float f0 = ldexpf(a.mul, e);
+    if (!(isfinite(full) && full > 0.0f)) {
+        left = 1.0f;
+        f0 = a.mul * full;
+    }
+    for (int i = tid; i < a.nb * 1024; i += kOsThreads) {
+        const uint4 hv = reinterpret_cast<const uint4*>(xh)[i], lv = reinterpret_cast<const uint4*>(xl)[i];
+        const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
+        uint32_t hw[4], lw[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            split_pair(__uint_as_float(__byte_perm(lr[j], hr[j], 0x5410)) * f0, __uint_as_float(__byte_perm(lr[j], hr[j], 0x7632)) * f0,
+                       &hw[j], &lw[j]);
+        reinterpret_cast<uint4*>(xh)[i] = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+        reinterpret_cast<uint4*>(xl)[i] = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+    }
+
+    // ---------------- steps
+    const int q = warp & 3, half = warp >> 2, row = q * 32 + lane;
+    const uint32_t lanes = (uint32_t)(q * 32) << 16;
+    const uint32_t d_a = tmem, d_s = tmem + 128, d_u = tmem + 256;
+    uint32_t phase = 0;
+    bool dead = false;
+    // operands are in shared memory: the MMAs of a batch, and their end
+    const auto batch = [&](auto issue) {
+        asm volatile("fence.proxy.async;" ::: "memory");
+        tc_fence_before();
+        __syncthreads();
+        if (tid == 0 && !*abort_flag) {
+            tc_fence_after();
+            issue();
+            umma_commit(bar_a);
+        }
+        __syncwarp();
+        dead = dead || !mbar_wait(bar_a, phase, abort_flag, a.status);
+        dead = __any_sync(0xffffffffu, dead);
+        phase ^= 1u;
+        tc_fence_after();
+    };
+    // high high, high low and low high products of two operands whose low halves lie lo_a and lo_b bytes on
+    const auto products = [&](uint32_t d, uint64_t da, uint64_t db, uint32_t lo_a, uint32_t lo_b, bool with_lo_a, bool with_lo_b,
+                              uint32_t idesc, int ks, auto step_a, auto step_b) {
+        uint32_t acc = 0;
+        for (int h = 0; h < 3; ++h) {
+            if ((h == 1 && !with_lo_b) || (h == 2 && !with_lo_a)) continue;
+            const uint64_t pa = da + (h == 2 ? lo_a >> 4 : 0), pb = db + (h == 1 ? lo_b >> 4 : 0);
+            for (int k = 0; k < ks; ++k) {
+                umma_bf16(d, pa + step_a(k), pb + step_b(k), idesc, acc);
+                acc = 1;
+            }
+        }
+    };
+    const auto along = [](int k) { return (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * (32 >> 4)); };
+    const auto across = [](int k) { return (uint64_t)(k * (2048 >> 4)); };
+    const uint32_t id_s = hg_idesc(true, 128, a.mp, false, false), id_u = hg_idesc(true, 128, a.nb * 64, false, true);
+    const uint32_t xh_a = smem_u32(xh), sh_a = smem_u32(sh);
+    const uint32_t x_lo = (uint32_t)a.nb * 16384, s_lo = (uint32_t)sb * 16384;
+    const int s0 = half * (a.mp / 4), s1 = s0 + a.mp / 4;        // this thread's columns of A and B,
+    const int u0 = half * (a.nb * 16), u1 = u0 + a.nb * 16;      // and of X
+    // body(column, eight sums) over a thread's columns, 32 of them loaded together
+    const auto columns = [&](uint32_t d, int from, int to, auto body) {
+        for (int c = from; c < to; c += 32) {
+            uint32_t v[4][8];
+            __syncwarp();
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c + 8 * u < to) tmem_ld8_nowait(d + lanes + c + 8 * u, v[u]);
+            tmem_wait_ld<8>(v[0]);
+            reg_touch8(v[1]);
+            reg_touch8(v[2]);
+            reg_touch8(v[3]);
+#pragma unroll
+            for (int u = 0; u < 4; ++u)
+                if (c + 8 * u < to) body(c + 8 * u, v[u]);
+        }
+    };
+
+    for (int i = 0; i < a.steps; ++i) {
+        const bool low = a.steps - i > 2, low_x = low && !(i == 0 && a.exact_first);
+        const float k0 = i == 0 ? left : 1.0f;
+        // A = X X^T
+        batch([&] { products(d_a, desc_sw128(xh_a), desc_sw128(xh_a), x_lo, x_lo, low_x, low_x, id_s, a.nb * 4, along, along); });
+        const float fa = a.fa * k0 * k0;
+        if constexpr (C == 1) {
+            columns(d_a, s0, s1, [&](int c, const uint32_t* v) {
+                uint32_t hw[4], lw[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+                    split_pair(__uint_as_float(v[2 * j]) * fa, __uint_as_float(v[2 * j + 1]) * fa, &hw[j], &lw[j]);
+                const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
+                *reinterpret_cast<uint4*>(sh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+            });
+        } else {
+            // slices of cw columns: [source][row][cw] floats where A and B lie, free until then
+            const int cw = a.mp / C;
+            const uint32_t stage = smem_u32(sh);
+            cluster_barrier();               // no CTA's MMAs read its B any more
+            columns(d_a, s0, s1, [&](int c, const uint32_t* v) {
+                if (row >= a.mp) return;
+#pragma unroll
+                for (int j = 0; j < 2; ++j) {
+                    const int col = c + 4 * j, to = col / cw;
+                    st_remote4(remote_smem(stage + (uint32_t)(((rank * 128 + row) * cw + col - to * cw) * 4), (uint32_t)to), v[4 * j],
+                               v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+                }
+            });
+            cluster_barrier();
+            const int quads = cw / 4;
+            constexpr int U = 8 / C;         // 128 rows x 32 / C quads of columns at most
+            float4 mine[U];
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int idx = tid + u * kOsThreads;
+                mine[u] = make_float4(0, 0, 0, 0);
+                if (idx >= a.mp * quads) continue;
+                const int r = idx / quads, col = (idx - r * quads) * 4;
+                for (int k = 0; k < C; ++k) {
+                    const float4 o = *reinterpret_cast<const float4*>(sh + (((k * 128 + r) * cw + col) * 4));
+                    mine[u].x += o.x, mine[u].y += o.y, mine[u].z += o.z, mine[u].w += o.w;
+                }
+            }
+            cluster_barrier();               // every slice is read
+#pragma unroll
+            for (int u = 0; u < U; ++u) {
+                const int idx = tid + u * kOsThreads;
+                if (idx >= a.mp * quads) continue;
+                const int r = idx / quads, col = rank * cw + (idx - r * quads) * 4;
+                uint32_t hw[2], lw[2];
+                split_pair(mine[u].x * fa, mine[u].y * fa, &hw[0], &lw[0]);
+                split_pair(mine[u].z * fa, mine[u].w * fa, &hw[1], &lw[1]);
+                const uint32_t o = (uint32_t)(col >> 6) * 16384 + sw_chunk(r, (col & 63) >> 3) + (col & 7) * 2;
+#pragma unroll
+                for (int k = 0; k < C; ++k) {
+                    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(remote_smem(sh_a + o, (uint32_t)k)),
+                                 "r"(hw[0]), "r"(hw[1])
+                                 : "memory");
+                    asm volatile("st.shared::cluster.v2.b32 [%0], {%1, %2};" ::"r"(remote_smem(sh_a + s_lo + o, (uint32_t)k)),
+                                 "r"(lw[0]), "r"(lw[1])
+                                 : "memory");
+                }
+            }
+            asm volatile("fence.proxy.async;" ::: "memory");
+            cluster_barrier();
+        }
+        // B = b A + c A^2
+        batch([&] { products(d_s, desc_sw128(sh_a), desc_sw128(sh_a), s_lo, s_lo, low, low, id_s, a.mp / 16, along, along); });
+        columns(d_s, s0, s1, [&](int c, const uint32_t* v) {
+            const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
+            const uint4 hv = *reinterpret_cast<const uint4*>(sh + o);
+            const uint4 lv = low ? *reinterpret_cast<const uint4*>(sl + o) : make_uint4(0, 0, 0, 0);
+            const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
+            uint32_t hw[4], lw[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = halves2(hr[j]), y = halves2(lr[j]);
+                split_pair(fmaf(a.fsa, x.x + y.x, __uint_as_float(v[2 * j]) * a.fs),
+                           fmaf(a.fsa, x.y + y.y, __uint_as_float(v[2 * j + 1]) * a.fs), &hw[j], &lw[j]);
+            }
+            *reinterpret_cast<uint4*>(sh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+            *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+        });
+        // X = a X + B X
+        batch([&] {
+            products(d_u, desc_sw128(sh_a), desc_sw128_mn(xh_a, 16384), s_lo, x_lo, low, low_x, id_u, a.mp / 16, along, across);
+        });
+        const bool last = i + 1 == a.steps;
+        const float fu = (last ? a.fu_last : a.fu) * k0, fux = (last ? a.fux_last : a.fux) * k0;
+        columns(d_u, u0, u1, [&](int c, const uint32_t* v) {
+            if (row >= m || c >= nc) return;
+            const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
+            const uint4 hv = *reinterpret_cast<const uint4*>(xh + o);
+            // where the products take the high halves alone, so does a X: the step is then exact
+            // for a rounded X, and rounding moves a singular value near 1 by 1.5 times itself,
+            // not by a - p' = 5 times
+            const uint4 lv = low ? *reinterpret_cast<const uint4*>(xl + o) : make_uint4(0, 0, 0, 0);
+            const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
+            float f[8];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float2 x = halves2(hr[j]), y = halves2(lr[j]);
+                f[2 * j] = fmaf(fux, x.x + y.x, __uint_as_float(v[2 * j]) * fu);
+                f[2 * j + 1] = fmaf(fux, x.y + y.y, __uint_as_float(v[2 * j + 1]) * fu);
+            }
+            if (!last) {
+                uint32_t hw[4], lw[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) split_pair(f[2 * j], f[2 * j + 1], &hw[j], &lw[j]);
+                *reinterpret_cast<uint4*>(xh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
+                *reinterpret_cast<uint4*>(xl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                return;
+            }
+            uint32_t w[4];      // the result, where X's high halves were
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
+                w[j] = *reinterpret_cast<const uint32_t*>(&p);
+            }
+            *reinterpret_cast<uint4*>(xh + o) = make_uint4(w[0], w[1], w[2], w[3]);
+        });
+    }
+    // ---------------- result: lanes along the rows of memory
+    __syncthreads();
+    uint16_t* dst = a.out + mat * a.stride_out + (a.tall ? c0 * a.ld_out : c0);
+    const auto at_x = [&](int r, int c) { return (uint32_t)(c >> 6) * 16384 + sw_chunk(r, (c & 63) >> 3) + (c & 7) * 2; };
+    if (len > 0 && !a.tall && a.vec_out) {
+        const int per = (nc + 7) / 8;
+        RowWalk at(tid, kOsThreads, per);
+        for (; at.row < m; at.next()) {
+            const int r = (int)at.row, c = at.part * 8;
+            const uint4 w = *reinterpret_cast<const uint4*>(xh + at_x(r, c));
+            uint16_t* p = dst + r * a.ld_out + c;
+            if (c + 8 <= nc) {
+                *reinterpret_cast<uint4*>(p) = w;
+            } else {
+                const uint32_t u[4] = {w.x, w.y, w.z, w.w};
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < nc) p[j] = (uint16_t)(u[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+    } else if (len > 0) {
+        RowWalk at(tid, kOsThreads, len);
+        for (; at.row < lines; at.next()) {
+            const int r = a.tall ? at.part : (int)at.row, c = a.tall ? (int)at.row : at.part;
+            dst[at.row * a.ld_out + at.part] = *reinterpret_cast<const uint16_t*>(xh + at_x(r, c));
+        }
+    }
+    if (dead && tid == 0) {      // MMAs in flight end before TMEM is freed
+        umma_commit(bar_a);
+        mbar_drain(bar_a, phase, kDrainNs);
+    }
+    __syncwarp();
+    tc_fence_before();
+    __syncthreads();
+    if constexpr (C > 1) cluster_barrier();
+    if (warp == 0) {
+        tc_fence_after();
+        hg_tmem_free<1>(tmem, 512);
     }
 }
 
@@ -359,12 +737,25 @@ float half_scale(double top) { return (float)std::ldexp(1.0, 15 - (int)std::ceil
 // |b s^2 + c s^4|; false where they leave the range that fp16 planes hold.
 bool orth_range(const float* k, int steps, double* top, double* top_b) {
     double hi = 1.0, all = 1.0, bmax = 0.0;
+    const double a = k[0], b = k[1], c = k[2];
+    const auto p = [=](double s2) { return b * s2 + c * s2 * s2; };
+    if (!(std::fabs(a) < 1e6 && std::fabs(b) < 1e6 && std::fabs(c) < 1e6)) return false;
     for (int i = 0; i < steps; ++i) {
+        // s (a + b s^2 + c s^4) and b s^2 + c s^4 on [0, hi]: at its end and where they turn
+        const double end = hi * hi, disc = 9 * b * b - 20 * a * c;
+        double at[4] = {end, -1, -1, -1};
+        if (c != 0) at[3] = -b / (2 * c);
+        if (c != 0 && disc >= 0) {
+            at[1] = (-3 * b + std::sqrt(disc)) / (10 * c);
+            at[2] = (-3 * b - std::sqrt(disc)) / (10 * c);
+        } else if (c == 0 && b != 0) {
+            at[1] = -a / (3 * b);
+        }
         double next = 0.0;
-        for (int j = 0; j <= 4096; ++j) {
-            const double s = hi * j / 4096, s2 = s * s, p = k[1] * s2 + (double)k[2] * s2 * s2;
-            next = std::max(next, std::fabs(s * (k[0] + p)));
-            bmax = std::max(bmax, std::fabs(p));
+        for (const double s2 : at) {
+            if (!(s2 >= 0 && s2 <= end)) continue;
+            next = std::max(next, std::sqrt(s2) * std::fabs(a + p(s2)));
+            bmax = std::max(bmax, std::fabs(p(s2)));
         }
         if (i + 1 < steps) all = std::max(all, next);
         hi = next;
@@ -396,6 +787,44 @@ nitro_status orth_first(nitro_orth* h, const T* m, int64_t ld, int64_t stride, i
     TRY(launch_k(k_orth_pack<T>, dim3(grid, count), dim3(256), 0, s, m, ld, stride, h->rows, h->cols, (const float*)h->part,
                  parts, mul, h->x[0], low ? 1 : 0, vec, h->scale));
     return NITRO_OK;
+}
+
+// The one-launch form: its cluster size, or 0 where it does not apply.  Up to 256 columns a
+// CTA (128 KB of halves).
+int small_cluster(const nitro_orth* h) {
+    if (h->small > 128) return 0;
+    const int big = std::max(h->rows, h->cols);
+    for (int c = 1; c <= 8; c *= 2)
+        if (big <= 256 * c) return c;
+    return 0;
+}
+
+template <typename T, int C>
+cudaError_t small_launch(const OsArgs& a, int count, cudaStream_t s) {
+    static std::atomic<uint64_t> ready{0};
+    int dev = 0;
+    sm_count(&dev);
+    const int sb = (a.mp + 63) / 64;
+    const size_t smem = (size_t)(2 * a.nb + 2 * sb) * 16384 + 1024 + 256;
+    const cudaError_t e = once_per_device(ready, dev, [] {
+        return cudaFuncSetAttribute(k_orth_small<T, C>, cudaFuncAttributeMaxDynamicSharedMemorySize, 12 * 16384 + 1280);
+    });
+    if (e != cudaSuccess) return e;
+    if constexpr (C > 1) return launch_cluster(k_orth_small<T, C>, dim3((unsigned)count * C), kOsThreads, C, s, smem, a);
+    else return launch_k(k_orth_small<T, C>, dim3((unsigned)count), dim3(kOsThreads), smem, s, a);
+}
+
+template <typename T>
+cudaError_t small_run(int c, OsArgs a, int count, cudaStream_t s) {
+    const int m = std::min(a.rows, a.cols), n = std::max(a.rows, a.cols);
+    a.mp = (int)round_up(m, 32);
+    a.nb = (n + 64 * c - 1) / (64 * c);
+    switch (c) {
+        case 1: return small_launch<T, 1>(a, count, s);
+        case 2: return small_launch<T, 2>(a, count, s);
+        case 4: return small_launch<T, 4>(a, count, s);
+        default: return small_launch<T, 8>(a, count, s);
+    }
 }
 
 HgOperand operand(const Planes& p, int64_t inner, int64_t outer, int count) {
@@ -450,6 +879,17 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
     const int64_t big = std::max(h->rows, h->cols);
     const float sx = half_scale(top), sa = half_scale(top * top), sb = half_scale(top_b);
     const bool low0 = m_type != NITRO_BF16 && (steps == 0 || orth_halves(0, steps));
+    if (const int c = steps > 0 ? small_cluster(h) : 0) {
+        const OsArgs a{m, ldm, stride_m, out, ldo, stride_o, h->rows, h->cols, tall, 0, 0, steps, m_type == NITRO_BF16,
+                       ((uintptr_t)m & 15) == 0 && ldm * size % 16 == 0 && stride_m * size % 16 == 0,
+                       ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && stride_o % 8 == 0, sx,
+                       sa / (sx * sx), k[2] * sb / (sa * sa), k[1] * sb / sa, 1.0f / sb, k[0],
+                       1.0f / (sb * sx), k[0] / sx, h->status};
+        ProfScope ps(K_ORTH_SMALL, s, (double)count * steps * n * n * (3.0 * big + n), (double)count * n * big * (size + 2));
+        TRY(m_type == NITRO_BF16 ? small_run<uint16_t>(c, a, count, s)
+            : m_type == NITRO_F32 ? small_run<float>(c, a, count, s) : small_run<int64_t>(c, a, count, s));
+        return NITRO_OK;
+    }
     nitro_status st;
     if (m_type == NITRO_BF16) st = orth_first(h, (const uint16_t*)m, ldm, stride_m, count, sx, low0, s);
     else if (m_type == NITRO_F32) st = orth_first(h, (const float*)m, ldm, stride_m, count, sx, low0, s);

@@ -13,8 +13,8 @@
 // logit more in 32 bits (16-bit logits are off by 2^-9 of their size, far too much under
 // an exponential).
 //
-// Few rows and classes leave fewer tiles than SMs; then the logits' sum is split along
-// the features into 32-bit slices of a small workspace, which the row kernels add up.
+// Where dx has fewer tiles than SMs its sum is split along the classes into 32-bit slices of
+// a small workspace, or shared out in a cluster (head_gemm.cuh), as the logits' is.
 #include <new>
 #include <vector>
 
@@ -53,18 +53,20 @@ struct EpiStats {
     struct Args {
         const int32_t* labels;
         float k2, scale;      // scale log2 e
-        float2* part;         // [2 tiles_n][rows]
+        float2* part;         // [per tiles_n][rows]
+        int per;              // parts that a tile's columns are taken in
         float* zt;            // [rows]
     };
     const Args& a;
     const HgArgs& g;
     int row, col0, slot, lab;
     float mx = -INFINITY, sum = 0.0f;
-    __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int half)
+    __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int, int slot_)
         : a(a_), g(g_), row(row_), col0(col0_) {
-        slot = 2 * t.n + half;
+        slot = a.per * t.n + slot_;
         lab = row < g.M ? a.labels[row] : -1;
     }
+    __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
         const int n = g.N - (col0 + c);
         if (n <= 0) return;
@@ -118,7 +120,7 @@ struct EpiProb {
     int row, col0, lab = -1;
     float l2 = 0.0f;
     bool live = false;
-    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
+    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int, int)
         : a(a_), g(g_), row(row_), col0(col0_) {
         if (row < g.M) {
             lab = a.labels[row];
@@ -127,6 +129,7 @@ struct EpiProb {
             l2 = a.lse[row] * kLog2e;
         }
     }
+    __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = col0 + c;
         if (row >= g.M || col >= g.N) return;
@@ -159,10 +162,11 @@ struct EpiAcc {
     const HgArgs& g;
     int row, col0;
     float* dst;
-    __device__ __forceinline__ EpiAcc(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int)
+    __device__ __forceinline__ EpiAcc(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int, int)
         : a(a_), g(g_), row(row_), col0(col0_) {
         dst = a.c + t.split * a.slice + (int64_t)row * a.ldc + col0;
     }
+    __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
         if (row >= g.M || col0 + c >= a.ldc) return;
         float4* p = reinterpret_cast<float4*>(dst + c);
@@ -194,10 +198,11 @@ struct EpiBf16 {
     const HgArgs& g;
     int row, col0;
     float f = 0.0f;
-    __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int)
+    __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int, int)
         : a(a_), g(g_), row(row_), col0(col0_) {
         if (row < g.M) f = a.factor[a.one ? 0 : row];
     }
+    __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
         const int n = g.N - (col0 + c);
         if (row >= g.M || n <= 0) return;
@@ -245,68 +250,6 @@ __global__ void __launch_bounds__(256) k_xent_join(const float2* part, int parts
         for (int i = 1; i < 8; ++i) join(sh[i][lane]);
         const int lab = o.labels[row];
         write_row(o, row, m, s, lab >= 0 && lab < o.classes ? zt[row] : 0.0f);
-    }
-}
-
-// From logits in `slices` parts: a CTA a row.
-__global__ void __launch_bounds__(256) k_xent_rows(const float* z, int64_t ldz, int64_t slice, int slices, int classes,
-                                                   float k2, float scale, const RowOut o) {
-    __shared__ float sm[8], ss[8];
-    pdl_wait();
-    const int64_t row = blockIdx.x;
-    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5;
-    const float* zr = z + row * ldz;
-    float m = -INFINITY, s = 0.0f;
-    for (int j = threadIdx.x; j < classes; j += 256) {
-        float v = zr[j];
-        for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
-        const float t = fmaxf(m, v * k2), base = t == -INFINITY ? 0.0f : t;
-        s = s * exp2f(m - base) + exp2f(fmaf(v, k2, -base));
-        m = t;
-    }
-    const auto join = [&](float om, float os) {
-        const float t = fmaxf(m, om), base = t == -INFINITY ? 0.0f : t;
-        s = s * exp2f(m - base) + os * exp2f(om - base);
-        m = t;
-    };
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float om = __shfl_xor_sync(0xffffffffu, m, d), os = __shfl_xor_sync(0xffffffffu, s, d);
-        join(om, os);
-    }
-    if (lane == 0) {
-        sm[w] = m;
-        ss[w] = s;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int i = 1; i < 8; ++i) join(sm[i], ss[i]);
-        const int lab = o.labels[row];
-        float zt = 0.0f;
-        if (lab >= 0 && lab < classes) {
-            zt = zr[lab];
-            for (int k = 1; k < slices; ++k) zt += zr[k * slice + lab];
-        }
-        write_row(o, row, m, s, zt * scale);
-    }
-}
-
-// softmax - onehot from logits in slices, as EpiProb writes it (all classes, one piece).
-__global__ void __launch_bounds__(256) k_xent_probs(const float* z, int64_t ldz, int64_t slice, int slices,
-                                                    const EpiProb::Args a) {
-    pdl_wait();
-    const int64_t row = blockIdx.x;
-    const int lab = a.labels[row];
-    const bool live = lab >= 0 && lab < a.classes;
-    const float l2 = a.lse[row] * kLog2e;
-    const float* zr = z + row * ldz;
-    for (int j = blockIdx.y * 256 + threadIdx.x; j < a.classes; j += gridDim.y * 256) {
-        float v = zr[j];
-        for (int k = 1; k < slices; ++k) v += zr[k * slice + j];
-        v = live ? exp2f(fmaf(v, a.k2, -l2)) - (j == lab ? 1.0f : 0.0f) : 0.0f;
-        const __nv_bfloat16 r = __float2bfloat16_rn(v);
-        a.G[row * a.ldg + j] = __bfloat16_as_ushort(r);
-        if (a.low) a.G[a.low + row * a.ldg + j] = __bfloat16_as_ushort(__float2bfloat16_rn(v - __bfloat162float(r)));
     }
 }
 
@@ -506,14 +449,6 @@ bool xent_args(const nitro_xent* h, const void* x, int x_type, int64_t ldx, cons
     return ((uintptr_t)w & 1) == 0 && (x_type == NITRO_I8 || ((uintptr_t)x & 1) == 0);
 }
 
-// How the logits' product of `classes` classes runs; splits only for a piece of all classes.
-HgPick logits_pick(const nitro_xent* h, int rows, int64_t classes) {
-    const HgProblem p{rows, classes, h->features};
-    int64_t most = 1;
-    if (classes == h->classes) most = std::min<int64_t>(16, h->acc_floats / (rows * round_up(classes, 32)));
-    return hg_pick(p, (int)std::max<int64_t>(1, most));
-}
-
 HgProblem logits_problem(const nitro_xent* h, int rows, int64_t classes) {
     HgProblem p{rows, classes, h->features};
     p.status = h->status;
@@ -542,7 +477,7 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     h->g_elems = std::max(std::min(max_rows * round_up(classes, 64), std::max(kGElems, (int64_t)max_rows * 256)),
                           2 * std::min(max_rows, kRowsWithLow) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
-    const int64_t parts = 2 * ((classes + 127) / 128);
+    const int64_t parts = 4 * ((classes + 127) / 128);
     const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->xg, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
                     xalloc(h, &h->G, h->g_elems) && xalloc(h, &h->acc, h->acc_floats) &&
                     xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->factor, max_rows + 1) && xalloc(h, &h->status, 1) && cudaMemset(h->status, 0, 4) == cudaSuccess;
@@ -564,20 +499,11 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
     if (st != NITRO_OK) return st;
     const RowOut ro{labels, loss, lse, h->status, h->classes};
-    const HgPick t = logits_pick(h, rows, h->classes);
     const HgProblem p = logits_problem(h, rows, h->classes);
-    if (t.splits > 1) {
-        const int64_t ldz = round_up(h->classes, 32);
-        const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
-        TRY((hg_launch<EpiAcc, false, false, false>(t, p, ox, ow, ea, s)));
-        ProfScope ps(K_XENT_ROWS, s, 0.0, 4.0 * t.splits * rows * h->classes);
-        TRY(launch_k(k_xent_rows, dim3(rows), dim3(256), 0, s, (const float*)h->acc, ldz, rows * ldz, t.splits, h->classes,
-                     scale * kLog2e, scale, ro));
-        return NITRO_OK;
-    }
-    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, h->zt};
+    const HgPick t = hg_pick(p);
+    const int per = t.ks > 1 ? 4 : 2, parts = per * ((h->classes + t.bn - 1) / t.bn);
+    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, per, h->zt};
     TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
-    const int parts = 2 * ((h->classes + t.bn - 1) / t.bn);
     ProfScope ps(K_XENT_ROWS, s, 0.0, 8.0 * parts * rows);
     TRY(launch_k(k_xent_join, dim3((rows + 31) / 32), dim3(256), 0, s, (const float2*)h->part, parts, rows,
                  (const float*)h->zt, ro));
@@ -621,18 +547,8 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         wp.outer = n;
         const EpiProb::Args ep{labels, lse, scale * kLog2e, V, (int)v0, h->G, round_up(n, 64),
                                 halves == 2 ? rows * round_up(n, 64) : 0};
-        const HgPick tl = logits_pick(h, rows, n);
         const HgProblem pl = logits_problem(h, rows, n);
-        if (tl.splits > 1) {
-            const int64_t ldz = round_up(V, 32);
-            const EpiAcc::Args ea{h->acc, ldz, rows * ldz, 0};
-            TRY((hg_launch<EpiAcc, false, false, false>(tl, pl, ox, wp, ea, s)));
-            ProfScope ps(K_XENT_ROWS, s, 0.0, (4.0 * tl.splits + 2.0) * rows * V);
-            TRY(launch_k(k_xent_probs, dim3(rows, (unsigned)std::min<int64_t>(8, (V + 255) / 256)), dim3(256), 0, s,
-                         (const float*)h->acc, ldz, rows * ldz, tl.splits, ep));
-        } else {
-            TRY((hg_launch<EpiProb, false, false, false>(tl, pl, ox, wp, ep, s)));
-        }
+        TRY((hg_launch<EpiProb, false, false, false>(hg_pick(pl), pl, ox, wp, ep, s)));
         const HgOperand G{h->G, n, rows, ep.ldg, halves, rows * ep.ldg};
         if (dx) {
             HgProblem p{rows, F, n};
@@ -646,7 +562,7 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
                 else TRY((hg_launch<EpiBf16, false, true, false>(td, p, G, wp, eb, s)));
             } else {
                 // a shorter last piece has as many slices or fewer: it adds to the first ones
-                const HgPick t{td.cg, td.bn, hg_splits(n, td.splits)};
+                const HgPick t{td.cg, td.bn, hg_splits(n, td.splits), td.ks};
                 const EpiAcc::Args ea{h->acc, ldc, rows * ldc, v0 > 0};
                 if (halves == 2) TRY((hg_launch<EpiAcc, false, true, false, 2, 1>(t, p, G, wp, ea, s)));
                 else TRY((hg_launch<EpiAcc, false, true, false>(t, p, G, wp, ea, s)));

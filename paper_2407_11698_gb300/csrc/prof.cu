@@ -45,7 +45,8 @@ const char* const kNames[K_COUNT] = {
     "tc_pack_weights", "tc_pack_input", "tc_pack_delta", "prep_sum", "prep_mad",
     "prep_apply", "lr_pool", "lrpool_to_delta", "tc_timeout_probe", "tc_linear_wgrad",
     "xent_pack", "xent_logits", "xent_rows", "xent_dx", "xent_dw", "orth_pack", "orth_gram",
-    "orth_square", "orth_update", "mx4_quantize", "mx4_dequantize", "mx4_linear"};
+    "orth_square", "orth_update", "orth_small",
+    "mx4_quantize", "mx4_dequantize", "mx4_linear"};
 
 }  // namespace
 

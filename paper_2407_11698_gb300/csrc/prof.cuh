@@ -47,6 +47,7 @@ enum KernelId : int {
     K_ORTH_GRAM,
     K_ORTH_SQUARE,
     K_ORTH_UPDATE,
+    K_ORTH_SMALL,
     K_MX4_QUANTIZE,
     K_MX4_DEQUANTIZE,
     K_MX4_LINEAR,
