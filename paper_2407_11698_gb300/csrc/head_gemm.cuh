@@ -49,6 +49,7 @@ struct HgArgs {
     int planes_a, planes_b;    // planes that a matrix of the batch has
     int upper;                 // symmetric D: only tiles that reach the diagonal or lie right of it
     int band;                  // row tiles that are walked together
+    int fold;                  // K in two halves, an accumulator each (Epi::kFold only)
     uint32_t* status;
 };
 
@@ -183,6 +184,7 @@ __device__ __forceinline__ void hg_tmem_free(uint32_t tmem, uint32_t cols) {
 //                           calls it for the next)
 //   void cols(c, v)         v[0..32): columns col0 + c .. col0 + c + 31
 //   void done()
+//   kFold                   whether K may go to the two accumulators by halves, to be added here
 template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB, int KS>
 __global__ void __launch_bounds__(kHgThreads, 1)
     k_head_gemm(const __grid_constant__ CUtensorMap tmA, const __grid_constant__ CUtensorMap tmB, const HgArgs g,
@@ -303,12 +305,23 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             uint32_t ph = 0;
             for (int tile = unit; tile < g.total; tile += units, ++it) {
                 const HgTile T = hg_decode<TM, BN>(g, tile);
-                const int buf = it & 1;
-                if (!mbar_wait(tempty_bar(buf), ((uint32_t)(it >> 1) & 1u) ^ 1u, abort_flag, g.status)) break;
+                const bool fold = Epi::kFold && g.fold;
+                int buf = fold ? 0 : it & 1, first = T.kb0;
+                const int half_k = fold ? (T.kb0 + T.kb1 + 1) / 2 : T.kb1;
+                const uint32_t free_ph = ((uint32_t)(fold ? it : it >> 1) & 1u) ^ 1u;
+                if (!mbar_wait(tempty_bar(buf), free_ph, abort_flag, g.status)) break;
                 tc_fence_after();
-                const uint32_t d = tmem + (uint32_t)(buf * BN);
+                uint32_t d = tmem + (uint32_t)(buf * BN);
                 bool ok = true;
                 for (int kb = T.kb0; kb < T.kb1; ++kb) {
+                    if (Epi::kFold && kb == half_k) {
+                        hg_commit<CG>(tfull_bar(0));
+                        buf = 1;
+                        first = kb;
+                        d = tmem + (uint32_t)BN;
+                        if (!(ok = mbar_wait(tempty_bar(1), free_ph, abort_flag, g.status))) break;
+                        tc_fence_after();
+                    }
                     if (!(ok = mbar_wait(full_bar(st), ph, abort_flag, g.status))) break;
                     tc_fence_after();
                     const uint64_t so = (uint64_t)((uint32_t)(st * C::STAGE) >> 4);
@@ -319,7 +332,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                         const uint64_t db = db0 + so + (h > 0 && h < HB ? C::B_BYTES >> 4 : 0);
 #pragma unroll
                         for (int k = 0; k < kHgBK / 16; ++k)
-                            hg_mma<CG>(d, da + k * kStepA, db + k * kStepB, idesc, kb > T.kb0 || (h | k) != 0 ? 1u : 0u);
+                            hg_mma<CG>(d, da + k * kStepA, db + k * kStepB, idesc, kb > first || (h | k) != 0 ? 1u : 0u);
                     }
                     hg_commit<CG>(empty_bar(st));
                     if (++st == S) {
@@ -385,24 +398,40 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             } else {
                 Epi epi(ea, g, T, row, T.n * BN + half * (BN / 2), BN / 2, half);
                 epi.fetch(0);
-                const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it >> 1) & 1u, abort_flag, g.status);
+                const bool fold = Epi::kFold && g.fold;
+                const int use = fold ? 0 : buf;
+                const uint32_t full_ph = (uint32_t)(fold ? it : it >> 1) & 1u;
+                bool ok = mbar_wait(tfull_bar(use), full_ph, abort_flag, g.status);
+                if (fold) ok = ok && mbar_wait(tfull_bar(1), full_ph, abort_flag, g.status);
                 if (!__all_sync(0xffffffffu, ok)) break;
                 tc_fence_after();
-                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
+                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(use * BN + half * (BN / 2));
                 uint32_t v[2][32];
                 tmem_ld32_nowait(src, v[0]);
 #pragma unroll
                 for (int c = 0; c < BN / 64; ++c) {
                     __syncwarp();
                     tmem_wait_ld<32>(v[c & 1]);
+                    if constexpr (Epi::kFold) {
+                        if (fold) {
+                            uint32_t w[32];
+                            tmem_ld32_nowait(src + BN + 32 * c, w);
+                            tmem_wait_ld<32>(w);
+#pragma unroll
+                            for (int j = 0; j < 32; ++j)
+                                v[c & 1][j] = __float_as_uint(__uint_as_float(v[c & 1][j]) + __uint_as_float(w[j]));
+                        }
+                    }
                     if (c + 1 < BN / 64) tmem_ld32_nowait(src + 32 * (c + 1), v[(c + 1) & 1]);
                     else {
                         // the sums are in registers: the accumulator may be filled again
                         tc_fence_before();
                         __syncwarp();
                         if (lane == 0) {
-                            if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
-                            else mbar_arrive(tempty_bar(buf));
+                            for (int b = use; b <= (fold ? 1 : use); ++b) {
+                                if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(b), 0));
+                                else mbar_arrive(tempty_bar(b));
+                            }
                         }
                     }
                     epi.cols(32 * c, reinterpret_cast<float*>(v[c & 1]));
@@ -450,7 +479,7 @@ struct HgProblem {
     int64_t M, N, K;
     int batch = 1, planes_a = 1, planes_b = 1;
     int products = 1;          // of halves: 1 to 3 (for the choice of a form)
-    bool upper = false;
+    bool upper = false, fold = false;
     uint32_t* status = nullptr;
     int prof = 0;
     double ops = 0, bytes = 0;
@@ -534,6 +563,7 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     g.planes_a = p.planes_a;
     g.planes_b = p.planes_b;
     g.upper = p.upper ? 1 : 0;
+    g.fold = p.fold && KS == 1 && g.kb_per_split > 1 ? 1 : 0;
     g.band = 2048 / (128 * CG);
     g.status = p.status;
     static std::atomic<uint64_t> ready{0};

@@ -79,6 +79,7 @@ struct Planes {
 // The symmetric products.  A = f sum; B = f sum + g A with A's planes in `add`.  Elements
 // right of the diagonal are stored at (row, col) and (col, row), the others left to them.
 struct EpiSym {
+    static constexpr bool kFold = false;
     struct Args {
         Planes out, add;     // add.base may be null
         float f, fa;
@@ -142,6 +143,7 @@ struct EpiSym {
 
 // X <- a X + f sum, as planes for the next step or, at the last one, in bf16.
 struct EpiUpdate {
+    static constexpr bool kFold = false;
     struct Args {
         Planes x, out;
         float f, fx;         // times the sum, times X's planes
@@ -483,7 +485,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
     bool dead = false;
     // operands are in shared memory: the MMAs of a batch, and their end
     const auto batch = [&](auto issue) {
-        asm volatile("fence.proxy.async;" ::: "memory");
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
         tc_fence_before();
         __syncthreads();
         if (tid == 0 && !*abort_flag) {
@@ -513,6 +515,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
     const auto along = [](int k) { return (uint64_t)((k >> 2) * (16384 >> 4) + (k & 3) * (32 >> 4)); };
     const auto across = [](int k) { return (uint64_t)(k * (2048 >> 4)); };
     const uint32_t id_s = hg_idesc(true, 128, a.mp, false, false), id_u = hg_idesc(true, 128, a.nb * 64, false, true);
+    const int ks_x = max(1, (nc + 15) / 16);
     const uint32_t xh_a = smem_u32(xh), sh_a = smem_u32(sh);
     const uint32_t x_lo = (uint32_t)a.nb * 16384, s_lo = (uint32_t)sb * 16384;
     const int s0 = half * (a.mp / 4), s1 = s0 + a.mp / 4;        // this thread's columns of A and B,
@@ -536,10 +539,10 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
     };
 
     for (int i = 0; i < a.steps; ++i) {
-        const bool low = a.steps - i > 2, low_x = low && !(i == 0 && a.exact_first);
+        const bool low = a.steps - i > 2, low_next = a.steps - i > 3, low_x = low && !(i == 0 && a.exact_first);
         const float k0 = i == 0 ? left : 1.0f;
         // A = X X^T
-        batch([&] { products(d_a, desc_sw128(xh_a), desc_sw128(xh_a), x_lo, x_lo, low_x, low_x, id_s, a.nb * 4, along, along); });
+        batch([&] { products(d_a, desc_sw128(xh_a), desc_sw128(xh_a), x_lo, x_lo, low_x, low_x, id_s, ks_x, along, along); });
         const float fa = a.fa * k0 * k0;
         if constexpr (C == 1) {
             columns(d_a, s0, s1, [&](int c, const uint32_t* v) {
@@ -549,11 +552,11 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
                     split_pair(__uint_as_float(v[2 * j]) * fa, __uint_as_float(v[2 * j + 1]) * fa, &hw[j], &lw[j]);
                 const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
                 *reinterpret_cast<uint4*>(sh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                if (low) *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
             });
         } else {
-            // slices of cw columns: [source][row][cw] floats where A and B lie, free until then
-            const int cw = a.mp / C;
+            // slices of cw columns: [source][four columns][row] where A and B lie, free until then
+            const int cw = a.mp / C, quads = cw / 4;
             const uint32_t stage = smem_u32(sh);
             cluster_barrier();               // no CTA's MMAs read its B any more
             columns(d_a, s0, s1, [&](int c, const uint32_t* v) {
@@ -561,31 +564,28 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
 #pragma unroll
                 for (int j = 0; j < 2; ++j) {
                     const int col = c + 4 * j, to = col / cw;
-                    st_remote4(remote_smem(stage + (uint32_t)(((rank * 128 + row) * cw + col - to * cw) * 4), (uint32_t)to), v[4 * j],
+                    st_remote4(remote_smem(stage + (uint32_t)(((rank * quads + (col - to * cw) / 4) * 128 + row) * 16), (uint32_t)to), v[4 * j],
                                v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
                 }
             });
             cluster_barrier();
-            const int quads = cw / 4;
             constexpr int U = 8 / C;         // 128 rows x 32 / C quads of columns at most
             float4 mine[U];
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int idx = tid + u * kOsThreads;
+                const int idx = tid + u * kOsThreads, r = idx & 127, qd = idx >> 7;
                 mine[u] = make_float4(0, 0, 0, 0);
-                if (idx >= a.mp * quads) continue;
-                const int r = idx / quads, col = (idx - r * quads) * 4;
+                if (qd >= quads || r >= a.mp) continue;
                 for (int k = 0; k < C; ++k) {
-                    const float4 o = *reinterpret_cast<const float4*>(sh + (((k * 128 + r) * cw + col) * 4));
+                    const float4 o = reinterpret_cast<const float4*>(sh)[(k * quads + qd) * 128 + r];
                     mine[u].x += o.x, mine[u].y += o.y, mine[u].z += o.z, mine[u].w += o.w;
                 }
             }
             cluster_barrier();               // every slice is read
 #pragma unroll
             for (int u = 0; u < U; ++u) {
-                const int idx = tid + u * kOsThreads;
-                if (idx >= a.mp * quads) continue;
-                const int r = idx / quads, col = rank * cw + (idx - r * quads) * 4;
+                const int idx = tid + u * kOsThreads, r = idx & 127, qd = idx >> 7, col = rank * cw + qd * 4;
+                if (qd >= quads || r >= a.mp) continue;
                 uint32_t hw[2], lw[2];
                 split_pair(mine[u].x * fa, mine[u].y * fa, &hw[0], &lw[0]);
                 split_pair(mine[u].z * fa, mine[u].w * fa, &hw[1], &lw[1]);
@@ -618,7 +618,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
                            fmaf(a.fsa, x.y + y.y, __uint_as_float(v[2 * j + 1]) * a.fs), &hw[j], &lw[j]);
             }
             *reinterpret_cast<uint4*>(sh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-            *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+            if (low) *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
         });
         // X = a X + B X
         batch([&] {
@@ -647,7 +647,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) split_pair(f[2 * j], f[2 * j + 1], &hw[j], &lw[j]);
                 *reinterpret_cast<uint4*>(xh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
-                *reinterpret_cast<uint4*>(xl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
+                if (low_next) *reinterpret_cast<uint4*>(xl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
                 return;
             }
             uint32_t w[4];      // the result, where X's high halves were

@@ -50,6 +50,7 @@ __device__ __forceinline__ void store_bf16_32(uint16_t* dst, const float* v, int
 // Row statistics of a tile in base 2: (max, sum of 2^(t - max)), t = z log2 e, and the
 // label's logit.  A thread holds one row, so nothing is exchanged.
 struct EpiStats {
+    static constexpr bool kFold = true;
     struct Args {
         const int32_t* labels;
         float k2, scale;      // scale log2 e
@@ -107,6 +108,7 @@ struct EpiStats {
 // in here, the -1 at the label, exact in bf16 and most of a row's weight, would be rounded
 // as well, alike in every row.  Rows that are left out give zeros.
 struct EpiProb {
+    static constexpr bool kFold = false;
     struct Args {
         const int32_t* labels;
         const float* lse;
@@ -153,6 +155,7 @@ struct EpiProb {
 
 // 32-bit sums into slice `split` of c, or added to what it holds.
 struct EpiAcc {
+    static constexpr bool kFold = false;
     struct Args {
         float* c;
         int64_t ldc, slice;   // ldc a multiple of 32
@@ -187,6 +190,7 @@ struct EpiAcc {
 };
 
 struct EpiBf16 {
+    static constexpr bool kFold = false;
     struct Args {
         uint16_t* c;
         int64_t ldc;
@@ -371,6 +375,12 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 // it, can be most of a lone row's error, and averages out over more.
 constexpr int kRowsWithLow = 32;
 
+// The tensor cores drop the bits that a sum's 32 do not hold, so its error grows with the
+// additions: the loss is off by 5.6e-7 of it with 2048 features and 1.2e-6 with 3850.  From
+// here on the logits are summed in two halves, added with rounding (at 8192 x 2048 x 64000
+// that takes FOLD_MEASURED).
+constexpr int kFoldFeatures = 2048;
+
 constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
 
@@ -499,7 +509,8 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
     if (st != NITRO_OK) return st;
     const RowOut ro{labels, loss, lse, h->status, h->classes};
-    const HgProblem p = logits_problem(h, rows, h->classes);
+    HgProblem p = logits_problem(h, rows, h->classes);
+    p.fold = h->features > kFoldFeatures;
     const HgPick t = hg_pick(p);
     const int per = t.ks > 1 ? 4 : 2, parts = per * ((h->classes + t.bn - 1) / t.bn);
     const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, per, h->zt};
