@@ -93,8 +93,8 @@ struct HgCfg {
     static constexpr int B_ROWS = BN / CG;
     static constexpr int B_BYTES = B_ROWS * 128;
     static constexpr int STAGE = HA * A_BYTES + HB * B_BYTES;
-    static constexpr int S = 229376 / STAGE < 8 ? 229376 / STAGE : 8;      // 2 to 8
-    static constexpr int SMEM = S * STAGE + 1024 + 256;
+    static constexpr int S = 212992 / STAGE < 8 ? 212992 / STAGE : 8;      // 2 to 8
+    static constexpr int SMEM = S * STAGE + kHgEpiWarps * 2048 + 1024 + 256;
     static constexpr int TCOLS = 2 * BN;
 };
 
@@ -177,12 +177,73 @@ __device__ __forceinline__ void hg_tmem_free(uint32_t tmem, uint32_t cols) {
         asm volatile("tcgen05.dealloc.cta_group::1.sync.aligned.b32 %0, %1;" ::"r"(tmem), "r"(cols) : "memory");
 }
 
+// TMEM gives a thread a row.  Global memory wants a warp's accesses in few lines: 32 rows of 16
+// bytes each are 32 lines an instruction, and cost the epilogues of 128 x 128 tiles 6 us.
+// So rows go through 2 KB of the warp's own: 32 rows x 64 bytes, as four 16-byte chunks of the
+// thread's row (mine) or spread over the lanes so that eight rows' 64 bytes are one
+// instruction (line(i): row 8 i + lane / 4, chunk lane % 4).
+struct HgStage {
+    uint4* at;
+    int lane;
+    __device__ __forceinline__ uint4& slot(int row, int j) const { return at[row * 4 + (j ^ ((row >> 1) & 3))]; }
+    __device__ __forceinline__ void to_lines(uint4* v) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) slot(lane, j) = v[j];
+        __syncwarp();
+#pragma unroll
+        for (int i = 0; i < 4; ++i) v[i] = slot(8 * i + (lane >> 2), lane & 3);
+        __syncwarp();
+    }
+    __device__ __forceinline__ void to_mine(uint4* v) const {
+#pragma unroll
+        for (int i = 0; i < 4; ++i) slot(8 * i + (lane >> 2), lane & 3) = v[i];
+        __syncwarp();
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = slot(lane, j);
+        __syncwarp();
+    }
+    __device__ __forceinline__ int line_row(int i) const { return 8 * i + (lane >> 2); }
+    __device__ __forceinline__ int line_chunk() const { return lane & 3; }
+};
+
+// A thread's part of a tile: its row, the first row of its warp, its columns (width of them)
+// and which part of the tile's columns that is.
+struct HgPart {
+    int row, row0, col0, width, slot;
+    HgStage stage;
+};
+
+// 32 rows x 32 16-bit values, a thread's row in w[16], to rows row0.. of a matrix at
+// column col; rows below `rows`, columns below `cols` (vec: rows 16-byte aligned).  All lanes.
+__device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, uint16_t* base, int64_t ld, int col, int rows,
+                                           int cols, bool vec) {
+    uint4 v[4];
+#pragma unroll
+    for (int j = 0; j < 4; ++j) v[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    p.stage.to_lines(v);
+    const int c = col + 8 * p.stage.line_chunk();
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const int row = p.row0 + p.stage.line_row(i);
+        if (row >= rows || c >= cols) continue;
+        uint16_t* dst = base + (int64_t)row * ld + c;
+        if (vec && c + 8 <= cols) {
+            *reinterpret_cast<uint4*>(dst) = v[i];
+        } else {
+            const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j)
+                if (c + j < cols) dst[j] = (uint16_t)(u[j >> 1] >> (16 * (j & 1)));
+        }
+    }
+}
+
 // Epi: struct Args, and per tile and thread
-//   Epi(args, g, tile, row, col0, width, slot)   row: this thread's row of D; col0, width: its
-//       columns, slot: which part of the tile's columns that is (BN / width parts)
+//   Epi(args, g, tile, part)
 //   void fetch(c)           starts loading what cols(c) needs (called for c = 0; cols(c)
 //                           calls it for the next)
-//   void cols(c, v)         v[0..32): columns col0 + c .. col0 + c + 31
+//   void cols(c, v)         v[0..32): columns col0 + c .. col0 + c + 31 of the thread's row; all
+//                           lanes call it, rows and columns past the end among them
 //   void done()
 //   kFold                   whether K may go to the two accumulators by halves, to be added here
 template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB, int KS>
@@ -193,7 +254,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
     constexpr int S = C::S, TM = 128 * CG;
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE + kHgEpiWarps * 2048);
     // bars: full [S], empty [S], tmem full [2], tmem empty [2], drain
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 5);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
@@ -356,11 +417,13 @@ __global__ void __launch_bounds__(kHgThreads, 1)
         for (int tile = unit; tile < g.total; tile += units, ++it) {
             const HgTile T = hg_decode<TM, BN>(g, tile);
             const int buf = it & 1;
-            const int row = T.m * TM + rank * 128 + q * 32 + lane;
+            const int row0 = T.m * TM + rank * 128 + q * 32;
+            const HgStage hs{reinterpret_cast<uint4*>(smem + S * C::STAGE) + (warp - kHgEpiWarp0) * 128, lane};
             if constexpr (KS > 1) {
                 constexpr int W = BN / KS;                       // columns of a CTA's slice
                 float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
-                Epi epi(ea, g, T, row, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half);
+                const HgPart hp{row0 + lane, row0, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half, hs};
+                Epi epi(ea, g, T, hp);
                 const bool mine = 32 * half < W;
                 if (mine) epi.fetch(0);
                 bool ok = mbar_wait(tfull_bar(buf), 0, abort_flag, g.status);
@@ -396,7 +459,8 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                     epi.done();
                 }
             } else {
-                Epi epi(ea, g, T, row, T.n * BN + half * (BN / 2), BN / 2, half);
+                const HgPart hp{row0 + lane, row0, T.n * BN + half * (BN / 2), BN / 2, half, hs};
+                Epi epi(ea, g, T, hp);
                 epi.fetch(0);
                 const bool fold = Epi::kFold && g.fold;
                 const int use = fold ? 0 : buf;
@@ -478,7 +542,6 @@ inline bool hg_map(CUtensorMap* m, const HgOperand& o, bool f16, int box_outer) 
 struct HgProblem {
     int64_t M, N, K;
     int batch = 1, planes_a = 1, planes_b = 1;
-    int products = 1;          // of halves: 1 to 3 (for the choice of a form)
     bool upper = false, fold = false;
     uint32_t* status = nullptr;
     int prof = 0;
@@ -507,39 +570,36 @@ inline int64_t hg_tiles(const HgProblem& p, int cg, int bn) {
     return n * p.batch;
 }
 
-// The cheapest in clocks of its busiest SM: rounds of tiles times K blocks times a block's
-// clocks, and for splits (at most max_splits) what joining their sums in 32 bits costs.  A
-// block's clocks are those of its loads, about 53 bytes a clock into an SM's shared memory
-// (256 x 256 by a pair: 32 KB in 600 clocks, of which the MMAs need 512; 256 x 128 by a pair:
-// 24 KB in 550, MMAs 256; measured on 8192 x 2048 x 16384).
-inline HgPick hg_pick(const HgProblem& p, int max_splits = 1) {
+// The cheapest in clocks of its busiest SM: rounds of tiles times a tile's K blocks, each of
+// which takes as long as its MMAs (2 BN clocks a product of halves) or its loads, about 53
+// bytes a clock into an SM's shared memory (a pair's 256 x 256: 32 KB in 600 clocks against
+// 512 of MMAs; its 256 x 128: 24 KB in 550 against 256; measured on 8192 x 2048 x 16384).
+// Splits into the caller's slices (at most max_splits) or over a cluster pay for their joining.
+inline HgPick hg_pick(const HgProblem& p, int ha = 1, int hb = 1, int max_splits = 1) {
     const int sms = sm_count();
-    static const struct { int cg, bn, clocks; } kForms[] = {{2, 256, 600}, {2, 128, 500}, {1, 256, 930}, {1, 128, 620}};
+    static const struct { int cg, bn; } kForms[] = {{2, 256}, {2, 128}, {1, 256}, {1, 128}};
     HgPick best{2, 256, 1};
     int64_t least = INT64_MAX;
     const int64_t kb = (p.K + kHgBK - 1) / kHgBK;
     for (const auto& f : kForms) {
         const int64_t tiles = hg_tiles(p, f.cg, f.bn), units = sms / f.cg;
-        for (int w = 1; w <= max_splits && w <= kb; ++w) {
-            const int s = hg_splits(p.K, w);
-            if (s != w) continue;
-            int64_t c = (tiles * s + units - 1) / units * ((kb + s - 1) / s * p.products * f.clocks + 1500);
-            if (f.cg == 2) c += 2500;      // a pair's launch and its barriers
-            if (s > 1) c += 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500;
+        const int64_t mma = 2 * f.bn * (ha + hb - 1), load = (ha * 16384 + hb * (f.bn / f.cg) * 128) / 53 + 30;
+        const int64_t clocks = std::max(mma, load);
+        const auto cost = [&](int s) {
+            // and a tile's way through TMEM, most of it beside the next tile's MMAs; a pair's barriers
+            return (tiles * s + units - 1) / units * ((kb + s - 1) / s * clocks + 6 * f.bn) + (f.cg == 2 ? 2500 : 0);
+        };
+        const auto take = [&](int64_t c, HgPick t) {
             if (c < least) {
                 least = c;
-                best = {f.cg, f.bn, s};
+                best = t;
             }
-        }
-        // or shared out in a cluster: its barriers and the exchange
-        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 4; s *= 2) {
-            if (hg_splits(p.K, s) != s) continue;
-            const int64_t c = (tiles * s + units - 1) / units * ((kb + s - 1) / s * p.products * f.clocks + 1500) + 4500;
-            if (c < least) {
-                least = c;
-                best = {1, 128, 1, s};
-            }
-        }
+        };
+        for (int s = 1; s <= max_splits && s <= kb; ++s)
+            if (hg_splits(p.K, s) == s)
+                take(cost(s) + (s > 1 ? 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500 : 0), {f.cg, f.bn, s});
+        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 4; s *= 2)
+            if (hg_splits(p.K, s) == s) take(cost(s) + 3000, {1, 128, 1, s});
     }
     return best;
 }

@@ -40,26 +40,25 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint3
     *hi = *reinterpret_cast<const uint32_t*>(&h);
     *lo = *reinterpret_cast<const uint32_t*>(&l);
 }
-// 32 floats as high (and low, if lo) halves at an 64-byte aligned place
-__device__ __forceinline__ void store_halves(uint16_t* hi, uint16_t* lo, const uint32_t* h, const uint32_t* l) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        reinterpret_cast<uint4*>(hi)[j] = make_uint4(h[4 * j], h[4 * j + 1], h[4 * j + 2], h[4 * j + 3]);
-        if (lo) reinterpret_cast<uint4*>(lo)[j] = make_uint4(l[4 * j], l[4 * j + 1], l[4 * j + 2], l[4 * j + 3]);
-    }
-}
-// 32 values held as halves, loaded ahead of their use
+// 32 x 32 values of a warp held as halves, loaded ahead of their use (lines, see HgStage)
 struct Halves32 {
     uint4 h[4], l[4];
-    __device__ __forceinline__ void load(const uint16_t* hi, const uint16_t* lo) {
+    // rows below `rows` of a matrix at column col; lo may be null
+    __device__ __forceinline__ void load(const HgPart& p, const uint16_t* hi, const uint16_t* lo, int64_t ld, int col, int rows) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            h[j] = reinterpret_cast<const uint4*>(hi)[j];
-            l[j] = lo ? reinterpret_cast<const uint4*>(lo)[j] : make_uint4(0, 0, 0, 0);
+        for (int i = 0; i < 4; ++i) {
+            const int row = p.row0 + p.stage.line_row(i);
+            const int64_t at = (int64_t)row * ld + col + 8 * p.stage.line_chunk();
+            h[i] = l[i] = make_uint4(0, 0, 0, 0);
+            if (row >= rows) continue;
+            h[i] = *reinterpret_cast<const uint4*>(hi + at);
+            if (lo) l[i] = *reinterpret_cast<const uint4*>(lo + at);
         }
     }
-    // v = g v + f times the values
-    __device__ __forceinline__ void join(float g, float f, float* v) const {
+    // v = g v + f times the thread's row
+    __device__ __forceinline__ void join(const HgPart& p, bool low, float g, float f, float* v) {
+        p.stage.to_mine(h);
+        if (low) p.stage.to_mine(l);
         const uint32_t *hw = reinterpret_cast<const uint32_t*>(h), *lw = reinterpret_cast<const uint32_t*>(l);
 #pragma unroll
         for (int j = 0; j < 16; ++j) {
@@ -88,53 +87,71 @@ struct EpiSym {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0, width;
+    const HgPart& p;
     uint16_t *hi, *lo;
     const uint16_t* add = nullptr;
     float f;
     Halves32 old;
-    __device__ __forceinline__ EpiSym(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int width_, int)
-        : a(a_), g(g_), row(row_), col0(col0_), width(width_) {
+    __device__ __forceinline__ EpiSym(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p_) : a(a_), g(g_), p(p_) {
         hi = a.out.base + 2 * t.batch * a.out.plane;
         lo = a.low ? hi + a.out.plane : nullptr;
         f = a.f;
         if (a.scale) f *= a.scale[t.batch] * a.scale[t.batch];
-        if (a.add.base) add = a.add.base + 2 * t.batch * a.add.plane + (int64_t)row * a.add.ld;
+        if (a.add.base) add = a.add.base + 2 * t.batch * a.add.plane;
     }
-    __device__ __forceinline__ bool skip(int col) const { return row >= g.M || col >= g.N || col + 31 < row; }
+    // no column of the warp's rows is right of the diagonal
+    __device__ __forceinline__ bool skip(int col) const { return col >= g.N || col + 31 < p.row0; }
     __device__ __forceinline__ void fetch(int c) {
-        const int col = col0 + c;
-        if (add && !skip(col)) old.load(add + col, a.low_add ? add + a.add.plane + col : nullptr);
+        const int col = p.col0 + c;
+        if (add && !skip(col)) old.load(p, add, a.low_add ? add + a.add.plane : nullptr, a.add.ld, col, g.M);
     }
     __device__ __forceinline__ void cols(int c, float* v) {
-        const int col = col0 + c;
-        if (!skip(col)) {
-            if (add) old.join(f, a.fa, v);
+        const int col = p.col0 + c, row = p.row;
+        const bool none = skip(col);
+        if (!none) {
+            if (add) old.join(p, a.low_add != 0, f, a.fa, v);
             else {
 #pragma unroll
                 for (int j = 0; j < 32; ++j) v[j] *= f;
             }
         }
-        if (c + 32 < width) fetch(c + 32);
-        if (skip(col)) return;
+        if (c + 32 < p.width) fetch(c + 32);
+        if (none) return;
         uint32_t h[16], l[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
-        if (col > row) {
-            // the padding of a row may be written
-            uint16_t* at = hi + (int64_t)row * a.out.ld + col;
-            store_halves(at, lo ? lo + (at - hi) : nullptr, h, l);
+        if (col > p.row0 + 31) {
+            // all right of the diagonal: rows, and as columns two rows a store (lanes 2i and 2i + 1
+            // swap, one takes the even columns, the other the odd); paddings may be written
+            const int odd = p.stage.lane & 1;
+            const int64_t to = (int64_t)(col + odd) * a.out.ld + (row - odd);
+            const auto mirror = [&](uint16_t* plane, const uint32_t* w) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) {
+                    const uint32_t other = __shfl_xor_sync(0xffffffffu, w[j], 1);
+                    const uint32_t pair = odd ? __byte_perm(other, w[j], 0x7632) : __byte_perm(w[j], other, 0x5410);
+                    if (row - odd < g.M && col + 2 * j + odd < g.N)
+                        *reinterpret_cast<uint32_t*>(plane + to + 2 * j * a.out.ld) = pair;
+                }
+            };
+            mirror(hi, h);
+            hg_store16(p, h, hi, a.out.ld, col, g.M, (int)a.out.ld, true);
+            if (lo) {
+                mirror(lo, l);
+                hg_store16(p, l, lo, a.out.ld, col, g.M, (int)a.out.ld, true);
+            }
+            return;
         }
 #pragma unroll
         for (int j = 0; j < 32; ++j) {
             const int cj = col + j;
-            if (cj < row || cj >= g.N) continue;
+            if (cj < row || cj >= g.N || row >= g.M) continue;
             const uint16_t hj = (uint16_t)(h[j >> 1] >> (16 * (j & 1))), lj = (uint16_t)(l[j >> 1] >> (16 * (j & 1)));
             hi[(int64_t)cj * a.out.ld + row] = hj;
-            if (lo) lo[(int64_t)cj * a.out.ld + row] = lj;
-            if (col <= row) {
-                hi[(int64_t)row * a.out.ld + cj] = hj;
-                if (lo) lo[(int64_t)row * a.out.ld + cj] = lj;
+            hi[(int64_t)row * a.out.ld + cj] = hj;
+            if (lo) {
+                lo[(int64_t)cj * a.out.ld + row] = lj;
+                lo[(int64_t)row * a.out.ld + cj] = lj;
             }
         }
     }
@@ -155,52 +172,42 @@ struct EpiUpdate {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0, width, batch;
+    const HgPart& p;
+    int batch;
     float f, fx;
     Halves32 old;
-    __device__ __forceinline__ EpiUpdate(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int width_, int)
-        : a(a_), g(g_), row(row_), col0(col0_), width(width_), batch(t.batch) {
+    __device__ __forceinline__ EpiUpdate(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p_)
+        : a(a_), g(g_), p(p_), batch(t.batch) {
         const float k = a.scale ? a.scale[batch] : 1.0f;
         f = a.f * k;
         fx = a.fx * k;
     }
     __device__ __forceinline__ void fetch(int c) {
-        if (row >= g.M || col0 + c >= g.N) return;
-        const uint16_t* x = a.x.base + 2 * batch * a.x.plane + (int64_t)row * a.x.ld + col0 + c;
-        old.load(x, a.low_x ? x + a.x.plane : nullptr);
+        if (p.col0 + c >= g.N) return;
+        const uint16_t* x = a.x.base + 2 * batch * a.x.plane;
+        old.load(p, x, a.low_x ? x + a.x.plane : nullptr, a.x.ld, p.col0 + c, g.M);
     }
     __device__ __forceinline__ void cols(int c, float* v) {
-        const int col = col0 + c;
-        const bool skip = row >= g.M || col >= g.N;
-        if (!skip) old.join(f, fx, v);
-        if (c + 32 < width) fetch(c + 32);
-        if (skip) return;
+        const int col = p.col0 + c;
+        const bool none = col >= g.N;
+        if (!none) old.join(p, a.low_x != 0, f, fx, v);
+        if (c + 32 < p.width) fetch(c + 32);
+        if (none) return;
+        uint32_t h[16], l[16];
         if (!a.last) {
-            uint16_t* o = a.out.base + 2 * batch * a.out.plane + (int64_t)row * a.out.ld + col;
-            uint32_t h[16], l[16];
 #pragma unroll
             for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
-            store_halves(o, a.low ? o + a.out.plane : nullptr, h, l);
+            uint16_t* o = a.out.base + 2 * batch * a.out.plane;      // a row's padding may be written
+            hg_store16(p, h, o, a.out.ld, col, g.M, (int)a.out.ld, true);
+            if (a.low) hg_store16(p, l, o + a.out.plane, a.out.ld, col, g.M, (int)a.out.ld, true);
             return;
         }
-        uint16_t* o = a.last + batch * a.stride_last + (int64_t)row * a.ld_last + col;
-        const int n = g.N - col;
-        if (a.vec && n >= 32) {
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                uint32_t w[4];
-#pragma unroll
-                for (int k = 0; k < 4; ++k) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(v[8 * j + 2 * k], v[8 * j + 2 * k + 1]);
-                    w[k] = *reinterpret_cast<const uint32_t*>(&p);
-                }
-                reinterpret_cast<uint4*>(o)[j] = make_uint4(w[0], w[1], w[2], w[3]);
-            }
-        } else {
-#pragma unroll
-            for (int j = 0; j < 32; ++j)
-                if (j < n) o[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+        for (int j = 0; j < 16; ++j) {
+            const __nv_bfloat162 w = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
+            h[j] = *reinterpret_cast<const uint32_t*>(&w);
         }
+        hg_store16(p, h, a.last + batch * a.stride_last, a.ld_last, col, g.M, g.N, a.vec != 0);
     }
     __device__ __forceinline__ void done() {}
 };
@@ -914,35 +921,34 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
         p.M = p.N = n;
         p.K = big;
         p.upper = true;
-        p.products = low_x ? 3 : 1;
+        const HgPick tg = low_x ? hg_pick(p, 2, 2) : hg_pick(p);
         p.prof = K_ORTH_GRAM;
         p.ops = (double)count * n * n * big;
         const float* g0 = i == 0 ? h->scale : nullptr;
         const EpiSym::Args ga{h->a, {nullptr, 0, 0}, sa / (sx * sx), 0.0f, low, 0, g0};
-        if (tall && low_x) TRY((hg_launch<EpiSym, true, true, true, 2, 2>(hg_pick(p), p, ox, ox, ga, s)));
-        else if (tall) TRY((hg_launch<EpiSym, true, true, true>(hg_pick(p), p, ox, ox, ga, s)));
-        else if (low_x) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(hg_pick(p), p, ox, ox, ga, s)));
-        else TRY((hg_launch<EpiSym, false, false, true>(hg_pick(p), p, ox, ox, ga, s)));
+        if (tall && low_x) TRY((hg_launch<EpiSym, true, true, true, 2, 2>(tg, p, ox, ox, ga, s)));
+        else if (tall) TRY((hg_launch<EpiSym, true, true, true>(tg, p, ox, ox, ga, s)));
+        else if (low_x) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(tg, p, ox, ox, ga, s)));
+        else TRY((hg_launch<EpiSym, false, false, true>(tg, p, ox, ox, ga, s)));
         // B = b A + c A^2
         p.K = n;
-        p.products = low ? 3 : 1;
         p.prof = K_ORTH_SQUARE;
         p.ops = (double)count * n * n * n;
         const EpiSym::Args gb{h->b, h->a, k[2] * sb / (sa * sa), k[1] * sb / sa, low, low, nullptr};
-        if (low) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(hg_pick(p), p, oa, oa, gb, s)));
+        if (low) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(hg_pick(p, 2, 2), p, oa, oa, gb, s)));
         else TRY((hg_launch<EpiSym, false, false, true>(hg_pick(p), p, oa, oa, gb, s)));
         // X
         p.M = h->rows;
         p.N = h->cols;
         p.upper = false;
-        p.products = 1 + low + (low && low_x);
         p.prof = K_ORTH_UPDATE;
         p.ops = 2.0 * count * n * n * big;
         const bool last = i + 1 == steps;
         const float so = last ? 1.0f : sx;
         const EpiUpdate::Args gu{x, h->x[(i + 1) & 1], so / (sb * sx), k[0] * so / sx, low_x, low_next, last ? out : nullptr,
                                  ldo, stride_o, ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && (count == 1 || stride_o % 8 == 0), g0};
-        const HgPick t = hg_pick(p);
+        const int hb = 1 + low, hx = 1 + (low && low_x);
+        const HgPick t = tall ? hg_pick(p, hx, hb) : hg_pick(p, hb, hx);
         if (tall && low && low_x) TRY((hg_launch<EpiUpdate, false, false, true, 2, 2>(t, p, ox, ob, gu, s)));
         else if (tall && low) TRY((hg_launch<EpiUpdate, false, false, true, 1, 2>(t, p, ox, ob, gu, s)));
         else if (tall) TRY((hg_launch<EpiUpdate, false, false, true>(t, p, ox, ob, gu, s)));

@@ -32,18 +32,9 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
-// 32 floats -> bf16 at dst, n of them valid; vec: dst is 16-byte aligned
-__device__ __forceinline__ void store_bf16_32(uint16_t* dst, const float* v, int n, bool vec) {
-    if (vec && n >= 32) {
+__device__ __forceinline__ void pack_bf16_32(const float* v, uint32_t* w) {
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            reinterpret_cast<uint4*>(dst)[j] = make_uint4(pack_bf16(v[8 * j], v[8 * j + 1]), pack_bf16(v[8 * j + 2], v[8 * j + 3]),
-                                                          pack_bf16(v[8 * j + 4], v[8 * j + 5]), pack_bf16(v[8 * j + 6], v[8 * j + 7]));
-        return;
-    }
-#pragma unroll
-    for (int j = 0; j < 32; ++j)
-        if (j < n) dst[j] = __bfloat16_as_ushort(__float2bfloat16_rn(v[j]));
+    for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
 }
 
 // ------------------------------------------------------------------ epilogues
@@ -62,9 +53,9 @@ struct EpiStats {
     const HgArgs& g;
     int row, col0, slot, lab;
     float mx = -INFINITY, sum = 0.0f;
-    __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int, int slot_)
-        : a(a_), g(g_), row(row_), col0(col0_) {
-        slot = a.per * t.n + slot_;
+    __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p)
+        : a(a_), g(g_), row(p.row), col0(p.col0) {
+        slot = a.per * t.n + p.slot;
         lab = row < g.M ? a.labels[row] : -1;
     }
     __device__ __forceinline__ void fetch(int) {}
@@ -119,22 +110,22 @@ struct EpiProb {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0, lab = -1;
+    const HgPart& p;
+    int lab = -1;
     float l2 = 0.0f;
     bool live = false;
-    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int, int)
-        : a(a_), g(g_), row(row_), col0(col0_) {
-        if (row < g.M) {
-            lab = a.labels[row];
+    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, const HgPart& p_) : a(a_), g(g_), p(p_) {
+        if (p.row < g.M) {
+            lab = a.labels[p.row];
             live = lab >= 0 && lab < a.classes;
             lab -= a.v0;
-            l2 = a.lse[row] * kLog2e;
+            l2 = a.lse[p.row] * kLog2e;
         }
     }
     __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
-        const int col = col0 + c;
-        if (row >= g.M || col >= g.N) return;
+        const int col = p.col0 + c;
+        if (col >= g.N) return;
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = live ? exp2f(fmaf(v[j], a.k2, -l2)) : 0.0f;
         const int at = lab - col;
@@ -142,12 +133,14 @@ struct EpiProb {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] -= j == at ? 1.0f : 0.0f;
         }
-        uint16_t* dst = a.G + (int64_t)row * a.ldg + col;
-        store_bf16_32(dst, v, 32, true);   // the row's padding may be written
+        uint32_t w[16];
+        pack_bf16_32(v, w);
+        hg_store16(p, w, a.G, a.ldg, col, g.M, (int)a.ldg, true);   // a row's padding may be written
         if (a.low) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] -= __bfloat162float(__float2bfloat16_rn(v[j]));
-            store_bf16_32(dst + a.low, v, 32, true);
+            for (int j = 0; j < 32; ++j) v[j] -= __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+            pack_bf16_32(v, w);
+            hg_store16(p, w, a.G + a.low, a.ldg, col, g.M, (int)a.ldg, true);
         }
     }
     __device__ __forceinline__ void done() {}
@@ -163,28 +156,36 @@ struct EpiAcc {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0;
-    float* dst;
-    __device__ __forceinline__ EpiAcc(const Args& a_, const HgArgs& g_, const HgTile& t, int row_, int col0_, int, int)
-        : a(a_), g(g_), row(row_), col0(col0_) {
-        dst = a.c + t.split * a.slice + (int64_t)row * a.ldc + col0;
+    const HgPart& p;
+    float* base;
+    float4 old[8];         // lines of two 16-column halves
+    __device__ __forceinline__ EpiAcc(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p_) : a(a_), g(g_), p(p_) {
+        base = a.c + t.split * a.slice + p.col0;
     }
-    __device__ __forceinline__ void fetch(int) {}
+    __device__ __forceinline__ float4* line(int c, int k) const {
+        const int row = p.row0 + p.stage.line_row(k & 3);
+        if (row >= g.M || p.col0 + c >= a.ldc) return nullptr;
+        return reinterpret_cast<float4*>(base + (int64_t)row * a.ldc + c + 16 * (k >> 2) + 4 * p.stage.line_chunk());
+    }
+    __device__ __forceinline__ void fetch(int c) {
+        if (!a.add) return;
+#pragma unroll
+        for (int k = 0; k < 8; ++k)
+            if (const float4* q = line(c, k)) old[k] = *q;
+    }
     __device__ __forceinline__ void cols(int c, float* v) {
-        if (row >= g.M || col0 + c >= a.ldc) return;
-        float4* p = reinterpret_cast<float4*>(dst + c);
+        uint4* w = reinterpret_cast<uint4*>(v);
+        p.stage.to_lines(w);
+        p.stage.to_lines(w + 4);
+        float4* f = reinterpret_cast<float4*>(v);
         if (a.add) {
 #pragma unroll
-            for (int j = 0; j < 8; ++j) {
-                const float4 o = p[j];
-                v[4 * j] += o.x;
-                v[4 * j + 1] += o.y;
-                v[4 * j + 2] += o.z;
-                v[4 * j + 3] += o.w;
-            }
+            for (int k = 0; k < 8; ++k) f[k].x += old[k].x, f[k].y += old[k].y, f[k].z += old[k].z, f[k].w += old[k].w;
         }
+        if (c + 32 < p.width) fetch(c + 32);
 #pragma unroll
-        for (int j = 0; j < 8; ++j) p[j] = make_float4(v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
+        for (int k = 0; k < 8; ++k)
+            if (float4* q = line(c, k)) *q = f[k];
     }
     __device__ __forceinline__ void done() {}
 };
@@ -200,19 +201,19 @@ struct EpiBf16 {
     };
     const Args& a;
     const HgArgs& g;
-    int row, col0;
+    const HgPart& p;
     float f = 0.0f;
-    __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, int row_, int col0_, int, int)
-        : a(a_), g(g_), row(row_), col0(col0_) {
-        if (row < g.M) f = a.factor[a.one ? 0 : row];
+    __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, const HgPart& p_) : a(a_), g(g_), p(p_) {
+        if (p.row < g.M) f = a.factor[a.one ? 0 : p.row];
     }
     __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
-        const int n = g.N - (col0 + c);
-        if (row >= g.M || n <= 0) return;
+        if (p.col0 + c >= g.N) return;
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] *= f;
-        store_bf16_32(a.c + (int64_t)row * a.ldc + col0 + c, v, n, a.vec != 0);
+        uint32_t w[16];
+        pack_bf16_32(v, w);
+        hg_store16(p, w, a.c, a.ldc, p.col0 + c, g.M, g.N, a.vec != 0);
     }
     __device__ __forceinline__ void done() {}
 };
@@ -547,9 +548,8 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
     if (piece < V) piece = piece / 256 * 256;
     // dx: in slices along the classes where its tiles leave SMs idle
     const int64_t ldc = round_up(F, 32);
-    HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
-    pd.products = halves;
-    const HgPick td = hg_pick(pd, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
+    const HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
+    const HgPick td = hg_pick(pd, halves, 1, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
     const bool direct = piece >= V && td.splits == 1;
     for (int64_t v0 = 0; v0 < V; v0 += piece) {
         const int64_t n = std::min<int64_t>(piece, V - v0);
@@ -581,12 +581,12 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         }
         if (dw) {
             HgProblem p{n, F, rows};
-            p.planes_a = p.products = halves;
+            p.planes_a = halves;
             p.status = h->status;
             p.prof = K_XENT_DW;
             p.ops = 2.0 * rows * n * F;
             const EpiBf16::Args eb{dw + v0 * lddw, lddw, tma_rows(dw, lddw), h->factor, 1};
-            if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p), p, G, og, eb, s)));
+            if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p, 2), p, G, og, eb, s)));
             else TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, G, og, eb, s)));
         }
     }
