@@ -209,14 +209,14 @@ struct HgStage {
 // A thread's part of a tile: its row, the first row of its warp, its columns (width of them)
 // and which part of the tile's columns that is.
 struct HgPart {
-    int row, row0, col0, width, slot;
+    int row, row0, rows, col0, width, slot;      // rows: below which rows are valid
     HgStage stage;
 };
 
 // 32 rows x 32 16-bit values, a thread's row in w[16], to rows row0.. of a matrix at
-// column col; rows below `rows`, columns below `cols` (vec: rows 16-byte aligned).  All lanes.
-__device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, uint16_t* base, int64_t ld, int col, int rows,
-                                           int cols, bool vec) {
+// column col; valid rows, columns below `cols` (vec: rows 16-byte aligned).  All lanes.
+__device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, uint16_t* base, int64_t ld, int col, int cols,
+                                           bool vec) {
     uint4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
@@ -225,7 +225,7 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
         const int row = p.row0 + p.stage.line_row(i);
-        if (row >= rows || c >= cols) continue;
+        if (row >= p.rows || c >= cols) continue;
         uint16_t* dst = base + (int64_t)row * ld + c;
         if (vec && c + 8 <= cols) {
             *reinterpret_cast<uint4*>(dst) = v[i];
@@ -419,90 +419,106 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             const int buf = it & 1;
             const int row0 = T.m * TM + rank * 128 + q * 32;
             const HgStage hs{reinterpret_cast<uint4*>(smem + S * C::STAGE) + (warp - kHgEpiWarp0) * 128, lane};
-            if constexpr (KS > 1) {
-                constexpr int W = BN / KS;                       // columns of a CTA's slice
-                float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
-                const HgPart hp{row0 + lane, row0, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half, hs};
-                Epi epi(ea, g, T, hp);
-                const bool mine = 32 * half < W;
-                if (mine) epi.fetch(0);
-                bool ok = mbar_wait(tfull_bar(buf), 0, abort_flag, g.status);
-                ok = __all_sync(0xffffffffu, ok);
-                tc_fence_after();
-                cluster_barrier();       // every CTA's MMAs have read their operands
-                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (BN / 2));
-#pragma unroll
-                for (int c = 0; c < BN / 2; c += 32) {
-                    uint32_t v[32];
-                    __syncwarp();
-                    tmem_ld32_nowait(src + c, v);
-                    tmem_wait_ld<32>(v);
-                    const int col = half * (BN / 2) + c;
-                    const uint32_t to = remote_smem(smem_u32(stage + (part * (W / 4) + (col % W) / 4) * 128 + q * 32 + lane), col / W);
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) st_remote4(to + j * 2048, v[4 * j], v[4 * j + 1], v[4 * j + 2], v[4 * j + 3]);
-                }
-                cluster_barrier();
-                if (mine && ok) {
-                    float v[32];
-#pragma unroll
-                    for (int j = 0; j < 8; ++j) {
-                        float4 s = stage[(8 * half + j) * 128 + q * 32 + lane];
-#pragma unroll
-                        for (int k = 1; k < KS; ++k) {
-                            const float4 o = stage[(k * (W / 4) + 8 * half + j) * 128 + q * 32 + lane];
-                            s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
-                        }
-                        v[4 * j] = s.x, v[4 * j + 1] = s.y, v[4 * j + 2] = s.z, v[4 * j + 3] = s.w;
-                    }
-                    epi.cols(0, v);
-                    epi.done();
-                }
-            } else {
-                const HgPart hp{row0 + lane, row0, T.n * BN + half * (BN / 2), BN / 2, half, hs};
-                Epi epi(ea, g, T, hp);
-                epi.fetch(0);
-                const bool fold = Epi::kFold && g.fold;
-                const int use = fold ? 0 : buf;
-                const uint32_t full_ph = (uint32_t)(fold ? it : it >> 1) & 1u;
-                bool ok = mbar_wait(tfull_bar(use), full_ph, abort_flag, g.status);
-                if (fold) ok = ok && mbar_wait(tfull_bar(1), full_ph, abort_flag, g.status);
-                if (!__all_sync(0xffffffffu, ok)) break;
-                tc_fence_after();
-                const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(use * BN + half * (BN / 2));
-                uint32_t v[2][32];
-                tmem_ld32_nowait(src, v[0]);
-#pragma unroll
-                for (int c = 0; c < BN / 64; ++c) {
-                    __syncwarp();
-                    tmem_wait_ld<32>(v[c & 1]);
-                    if constexpr (Epi::kFold) {
-                        if (fold) {
+            // The first tile's columns are gone through once before its sums are there, with no valid
+            // row: the epilogue's instructions are then cached.  A launch runs each for the first time,
+            // and 32 columns took 2.5 to 3.8 us, mostly waiting for them.  For the same reason the
+            // columns are a rolled loop.
+#pragma unroll 1
+            for (int dry = it == 0; dry >= 0; --dry) {
+                asm volatile("" : "+r"(dry));
+                if constexpr (KS > 1) {
+                    constexpr int W = BN / KS;                       // columns of a CTA's slice
+                    float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
+                    const HgPart hp{row0 + lane, row0, dry ? 0 : g.M, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half, hs};
+                    Epi epi(ea, g, T, hp);
+                    const bool mine = 32 * half < W;
+                    bool ok = true;
+                    float v[32] = {};
+                    if (!dry) {
+                        if (mine) epi.fetch(0);
+                        ok = mbar_wait(tfull_bar(buf), 0, abort_flag, g.status);
+                        ok = __all_sync(0xffffffffu, ok);
+                        tc_fence_after();
+                        cluster_barrier();       // every CTA's MMAs have read their operands
+                        const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(half * (BN / 2));
+#pragma unroll 1
+                        for (int c = 0; c < BN / 2; c += 32) {
                             uint32_t w[32];
-                            tmem_ld32_nowait(src + BN + 32 * c, w);
+                            __syncwarp();
+                            tmem_ld32_nowait(src + c, w);
                             tmem_wait_ld<32>(w);
+                            const int col = half * (BN / 2) + c;
+                            const uint32_t to =
+                                remote_smem(smem_u32(stage + (part * (W / 4) + (col % W) / 4) * 128 + q * 32 + lane), col / W);
 #pragma unroll
-                            for (int j = 0; j < 32; ++j)
-                                v[c & 1][j] = __float_as_uint(__uint_as_float(v[c & 1][j]) + __uint_as_float(w[j]));
+                            for (int j = 0; j < 8; ++j) st_remote4(to + j * 2048, w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
                         }
-                    }
-                    if (c + 1 < BN / 64) tmem_ld32_nowait(src + 32 * (c + 1), v[(c + 1) & 1]);
-                    else {
-                        // the sums are in registers: the accumulator may be filled again
-                        tc_fence_before();
-                        __syncwarp();
-                        if (lane == 0) {
-                            for (int b = use; b <= (fold ? 1 : use); ++b) {
-                                if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(b), 0));
-                                else mbar_arrive(tempty_bar(b));
+                        cluster_barrier();
+                        if (mine) {
+#pragma unroll
+                            for (int j = 0; j < 8; ++j) {
+                                float4 s = stage[(8 * half + j) * 128 + q * 32 + lane];
+#pragma unroll
+                                for (int k = 1; k < KS; ++k) {
+                                    const float4 o = stage[(k * (W / 4) + 8 * half + j) * 128 + q * 32 + lane];
+                                    s.x += o.x, s.y += o.y, s.z += o.z, s.w += o.w;
+                                }
+                                v[4 * j] = s.x, v[4 * j + 1] = s.y, v[4 * j + 2] = s.z, v[4 * j + 3] = s.w;
                             }
                         }
                     }
-                    epi.cols(32 * c, reinterpret_cast<float*>(v[c & 1]));
+                    if (mine && ok) {
+                        epi.cols(0, v);
+                        if (!dry) epi.done();
+                    }
+                } else {
+                    const HgPart hp{row0 + lane, row0, dry ? 0 : g.M, T.n * BN + half * (BN / 2), BN / 2, half, hs};
+                    Epi epi(ea, g, T, hp);
+                    const bool fold = Epi::kFold && g.fold;
+                    const int use = fold ? 0 : buf;
+                    if (!dry) {
+                        epi.fetch(0);
+                        const uint32_t full_ph = (uint32_t)(fold ? it : it >> 1) & 1u;
+                        bool ok = mbar_wait(tfull_bar(use), full_ph, abort_flag, g.status);
+                        if (fold) ok = ok && mbar_wait(tfull_bar(1), full_ph, abort_flag, g.status);
+                        if (!__all_sync(0xffffffffu, ok)) goto epilogue_out;
+                        tc_fence_after();
+                    }
+                    const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(use * BN + half * (BN / 2));
+                    const int end = dry ? 32 : BN / 2;
+#pragma unroll 1
+                    for (int c = 0; c < end; c += 32) {
+                        uint32_t v[32];
+                        __syncwarp();
+                        tmem_ld32_nowait(src + c, v);
+                        tmem_wait_ld<32>(v);
+                        if constexpr (Epi::kFold) {
+                            if (fold) {
+                                uint32_t w[32];
+                                tmem_ld32_nowait(src + BN + c, w);
+                                tmem_wait_ld<32>(w);
+#pragma unroll
+                                for (int j = 0; j < 32; ++j) v[j] = __float_as_uint(__uint_as_float(v[j]) + __uint_as_float(w[j]));
+                            }
+                        }
+                        if (!dry && c + 32 == BN / 2) {
+                            // the sums are in registers: the accumulator may be filled again
+                            tc_fence_before();
+                            __syncwarp();
+                            if (lane == 0) {
+                                for (int b = use; b <= (fold ? 1 : use); ++b) {
+                                    if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(b), 0));
+                                    else mbar_arrive(tempty_bar(b));
+                                }
+                            }
+                        }
+                        epi.cols(c, reinterpret_cast<float*>(v));
+                    }
+                    if (!dry) epi.done();
                 }
-                epi.done();
             }
         }
+    epilogue_out:;
     }
     if constexpr (KS > 1) {
         if (warp < kHgEpiWarp0) {    // the two of the epilogue's exchange

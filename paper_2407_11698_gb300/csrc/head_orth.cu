@@ -43,14 +43,14 @@ __device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint3
 // 32 x 32 values of a warp held as halves, loaded ahead of their use (lines, see HgStage)
 struct Halves32 {
     uint4 h[4], l[4];
-    // rows below `rows` of a matrix at column col; lo may be null
-    __device__ __forceinline__ void load(const HgPart& p, const uint16_t* hi, const uint16_t* lo, int64_t ld, int col, int rows) {
+    // valid rows of a matrix at column col; lo may be null
+    __device__ __forceinline__ void load(const HgPart& p, const uint16_t* hi, const uint16_t* lo, int64_t ld, int col) {
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const int row = p.row0 + p.stage.line_row(i);
             const int64_t at = (int64_t)row * ld + col + 8 * p.stage.line_chunk();
             h[i] = l[i] = make_uint4(0, 0, 0, 0);
-            if (row >= rows) continue;
+            if (row >= p.rows) continue;
             h[i] = *reinterpret_cast<const uint4*>(hi + at);
             if (lo) l[i] = *reinterpret_cast<const uint4*>(lo + at);
         }
@@ -75,8 +75,8 @@ struct Planes {
     int64_t ld, plane;      // ld a multiple of 64
 };
 
-// The symmetric products.  A = f sum; B = f sum + g A with A's planes in `add`.  Elements
-// right of the diagonal are stored at (row, col) and (col, row), the others left to them.
+// The symmetric products.  A = f sum; B = f sum + fa A with A's planes in `add`.  Blocks of
+// 32 x 32 right of the diagonal are stored at (row, col) and (col, row).
 struct EpiSym {
     static constexpr bool kFold = false;
     struct Args {
@@ -103,7 +103,7 @@ struct EpiSym {
     __device__ __forceinline__ bool skip(int col) const { return col >= g.N || col + 31 < p.row0; }
     __device__ __forceinline__ void fetch(int c) {
         const int col = p.col0 + c;
-        if (add && !skip(col)) old.load(p, add, a.low_add ? add + a.add.plane : nullptr, a.add.ld, col, g.M);
+        if (add && !skip(col)) old.load(p, add, a.low_add ? add + a.add.plane : nullptr, a.add.ld, col);
     }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = p.col0 + c, row = p.row;
@@ -120,40 +120,25 @@ struct EpiSym {
         uint32_t h[16], l[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
-        if (col > p.row0 + 31) {
-            // all right of the diagonal: rows, and as columns two rows a store (lanes 2i and 2i + 1
-            // swap, one takes the even columns, the other the odd); paddings may be written
-            const int odd = p.stage.lane & 1;
-            const int64_t to = (int64_t)(col + odd) * a.out.ld + (row - odd);
-            const auto mirror = [&](uint16_t* plane, const uint32_t* w) {
+        hg_store16(p, h, hi, a.out.ld, col, (int)a.out.ld, true);     // paddings may be written
+        if (lo) hg_store16(p, l, lo, a.out.ld, col, (int)a.out.ld, true);
+        // a block on the diagonal (both start at multiples of 32) holds both of its halves
+        if (col == p.row0) return;
+        // and as columns, two rows a store: lanes 2i and 2i + 1 swap, one takes the even
+        // columns, the other the odd
+        const int odd = p.stage.lane & 1;
+        const int64_t to = (int64_t)(col + odd) * a.out.ld + (row - odd);
+        const auto mirror = [&](uint16_t* plane, const uint32_t* w) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) {
-                    const uint32_t other = __shfl_xor_sync(0xffffffffu, w[j], 1);
-                    const uint32_t pair = odd ? __byte_perm(other, w[j], 0x7632) : __byte_perm(w[j], other, 0x5410);
-                    if (row - odd < g.M && col + 2 * j + odd < g.N)
-                        *reinterpret_cast<uint32_t*>(plane + to + 2 * j * a.out.ld) = pair;
-                }
-            };
-            mirror(hi, h);
-            hg_store16(p, h, hi, a.out.ld, col, g.M, (int)a.out.ld, true);
-            if (lo) {
-                mirror(lo, l);
-                hg_store16(p, l, lo, a.out.ld, col, g.M, (int)a.out.ld, true);
+            for (int j = 0; j < 16; ++j) {
+                const uint32_t other = __shfl_xor_sync(0xffffffffu, w[j], 1);
+                const uint32_t pair = odd ? __byte_perm(other, w[j], 0x7632) : __byte_perm(w[j], other, 0x5410);
+                if (row - odd < p.rows && col + 2 * j + odd < g.N)
+                    *reinterpret_cast<uint32_t*>(plane + to + 2 * j * a.out.ld) = pair;
             }
-            return;
-        }
-#pragma unroll
-        for (int j = 0; j < 32; ++j) {
-            const int cj = col + j;
-            if (cj < row || cj >= g.N || row >= g.M) continue;
-            const uint16_t hj = (uint16_t)(h[j >> 1] >> (16 * (j & 1))), lj = (uint16_t)(l[j >> 1] >> (16 * (j & 1)));
-            hi[(int64_t)cj * a.out.ld + row] = hj;
-            hi[(int64_t)row * a.out.ld + cj] = hj;
-            if (lo) {
-                lo[(int64_t)cj * a.out.ld + row] = lj;
-                lo[(int64_t)row * a.out.ld + cj] = lj;
-            }
-        }
+        };
+        mirror(hi, h);
+        if (lo) mirror(lo, l);
     }
     __device__ __forceinline__ void done() {}
 };
@@ -185,7 +170,7 @@ struct EpiUpdate {
     __device__ __forceinline__ void fetch(int c) {
         if (p.col0 + c >= g.N) return;
         const uint16_t* x = a.x.base + 2 * batch * a.x.plane;
-        old.load(p, x, a.low_x ? x + a.x.plane : nullptr, a.x.ld, p.col0 + c, g.M);
+        old.load(p, x, a.low_x ? x + a.x.plane : nullptr, a.x.ld, p.col0 + c);
     }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = p.col0 + c;
@@ -198,8 +183,8 @@ struct EpiUpdate {
 #pragma unroll
             for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
             uint16_t* o = a.out.base + 2 * batch * a.out.plane;      // a row's padding may be written
-            hg_store16(p, h, o, a.out.ld, col, g.M, (int)a.out.ld, true);
-            if (a.low) hg_store16(p, l, o + a.out.plane, a.out.ld, col, g.M, (int)a.out.ld, true);
+            hg_store16(p, h, o, a.out.ld, col, (int)a.out.ld, true);
+            if (a.low) hg_store16(p, l, o + a.out.plane, a.out.ld, col, (int)a.out.ld, true);
             return;
         }
 #pragma unroll
@@ -207,7 +192,7 @@ struct EpiUpdate {
             const __nv_bfloat162 w = __floats2bfloat162_rn(v[2 * j], v[2 * j + 1]);
             h[j] = *reinterpret_cast<const uint32_t*>(&w);
         }
-        hg_store16(p, h, a.last + batch * a.stride_last, a.ld_last, col, g.M, g.N, a.vec != 0);
+        hg_store16(p, h, a.last + batch * a.stride_last, a.ld_last, col, g.N, a.vec != 0);
     }
     __device__ __forceinline__ void done() {}
 };

@@ -56,7 +56,7 @@ struct EpiStats {
     __device__ __forceinline__ EpiStats(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p)
         : a(a_), g(g_), row(p.row), col0(p.col0) {
         slot = a.per * t.n + p.slot;
-        lab = row < g.M ? a.labels[row] : -1;
+        lab = row < p.rows ? a.labels[row] : -1;
     }
     __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
@@ -115,7 +115,7 @@ struct EpiProb {
     float l2 = 0.0f;
     bool live = false;
     __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, const HgPart& p_) : a(a_), g(g_), p(p_) {
-        if (p.row < g.M) {
+        if (p.row < p.rows) {
             lab = a.labels[p.row];
             live = lab >= 0 && lab < a.classes;
             lab -= a.v0;
@@ -135,12 +135,12 @@ struct EpiProb {
         }
         uint32_t w[16];
         pack_bf16_32(v, w);
-        hg_store16(p, w, a.G, a.ldg, col, g.M, (int)a.ldg, true);   // a row's padding may be written
+        hg_store16(p, w, a.G, a.ldg, col, (int)a.ldg, true);   // a row's padding may be written
         if (a.low) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] -= __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
             pack_bf16_32(v, w);
-            hg_store16(p, w, a.G + a.low, a.ldg, col, g.M, (int)a.ldg, true);
+            hg_store16(p, w, a.G + a.low, a.ldg, col, (int)a.ldg, true);
         }
     }
     __device__ __forceinline__ void done() {}
@@ -164,7 +164,7 @@ struct EpiAcc {
     }
     __device__ __forceinline__ float4* line(int c, int k) const {
         const int row = p.row0 + p.stage.line_row(k & 3);
-        if (row >= g.M || p.col0 + c >= a.ldc) return nullptr;
+        if (row >= p.rows || p.col0 + c >= a.ldc) return nullptr;
         return reinterpret_cast<float4*>(base + (int64_t)row * a.ldc + c + 16 * (k >> 2) + 4 * p.stage.line_chunk());
     }
     __device__ __forceinline__ void fetch(int c) {
@@ -204,7 +204,7 @@ struct EpiBf16 {
     const HgPart& p;
     float f = 0.0f;
     __device__ __forceinline__ EpiBf16(const Args& a_, const HgArgs& g_, const HgTile&, const HgPart& p_) : a(a_), g(g_), p(p_) {
-        if (p.row < g.M) f = a.factor[a.one ? 0 : p.row];
+        if (p.row < p.rows) f = a.factor[a.one ? 0 : p.row];
     }
     __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
@@ -213,7 +213,7 @@ struct EpiBf16 {
         for (int j = 0; j < 32; ++j) v[j] *= f;
         uint32_t w[16];
         pack_bf16_32(v, w);
-        hg_store16(p, w, a.c, a.ldc, p.col0 + c, g.M, g.N, a.vec != 0);
+        hg_store16(p, w, a.c, a.ldc, p.col0 + c, g.N, a.vec != 0);
     }
     __device__ __forceinline__ void done() {}
 };
