@@ -408,14 +408,14 @@ nitro_status nitro_xent_status(nitro_xent* h, int clear);
 void nitro_xent_destroy(nitro_xent* h);
 
 /* An update made orthogonal: X = M / (|M|_F + 1e-7), then `steps` times
- * A = X X^T, X = a X + (b A + c A^2) X (on the shorter side), out = X in bf16.
+ * A = X X^T, X = (a I + b A + c A^2) X (on the shorter side), out = X in bf16.
  * M: `count` matrices [rows x cols], stride_m elements apart, NITRO_BF16, NITRO_F32 or
  * NITRO_I64 (weight gradients as nitro_block_grad_device gives them).  coef: (a, b, c), or NULL
  * for (3.4445, -4.7750, 2.0315), which take every singular value to about 1 in
  * five steps.  A matrix of zeros gives zeros.  out must not overlap M.
  * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, max_count], steps
  * outside [0, 100], strides below the sizes, another type, or coefficients under which a
- * singular value in [0, 1] can pass 8 or |b s^2 + c s^4| 1024. */
+ * singular value in [0, 1] can pass 8 or |a + b s^2 + c s^4| 1024. */
 typedef struct nitro_orth nitro_orth;
 nitro_status nitro_orth_create(int max_count, int rows, int cols, nitro_orth** out);
 nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ldm, int64_t stride_m, int count,

@@ -414,7 +414,8 @@ __global__ void __launch_bounds__(kHgThreads, 1)
         // ---------------- epilogue
         const int q = warp & 3, half = (warp - kHgEpiWarp0) >> 2;
         int it = 0;
-        for (int tile = unit; tile < g.total; tile += units, ++it) {
+        bool alive = true;
+        for (int tile = unit; tile < g.total && alive; tile += units, ++it) {
             const HgTile T = hg_decode<TM, BN>(g, tile);
             const int buf = it & 1;
             const int row0 = T.m * TM + rank * 128 + q * 32;
@@ -481,7 +482,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                         const uint32_t full_ph = (uint32_t)(fold ? it : it >> 1) & 1u;
                         bool ok = mbar_wait(tfull_bar(use), full_ph, abort_flag, g.status);
                         if (fold) ok = ok && mbar_wait(tfull_bar(1), full_ph, abort_flag, g.status);
-                        if (!__all_sync(0xffffffffu, ok)) goto epilogue_out;
+                        if (!(alive = __all_sync(0xffffffffu, ok))) break;
                         tc_fence_after();
                     }
                     const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(use * BN + half * (BN / 2));
@@ -518,7 +519,6 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                 }
             }
         }
-    epilogue_out:;
     }
     if constexpr (KS > 1) {
         if (warp < kHgEpiWarp0) {    // the two of the epilogue's exchange

@@ -1,10 +1,10 @@
 // An update made orthogonal by Newton-Schulz steps: X0 = M / (|M|_F + 1e-7), then
-//   A = X X^T,   X <- a X + (b A + c A^2) X
-// (A = X^T X and X <- a X + X (b A + c A^2) where M has more rows than columns), which
+//   A = X X^T,   B = a I + b A + c A^2,   X <- B X
+// (A = X^T X and X <- X B where M has more rows than columns), which
 // moves every singular value s to a s + b s^3 + c s^5 and leaves the singular vectors.
 //
 // The products run on k_head_gemm (head_gemm.cuh) in fp16 with 32-bit sums.  X, A and
-// B = b A + c A^2 are kept times powers of two that put the largest value each can take
+// B are kept times powers of two that put the largest value each can take
 // below fp16's largest.  A value is two fp16 halves, v = high + low (22 bits and more),
 // and a product of two such tensors is three, high high + high low + low high: a step
 // multiplies what rounding adds outside M's own directions by a = 3.4 each, so an error
@@ -75,13 +75,13 @@ struct Planes {
     int64_t ld, plane;      // ld a multiple of 64
 };
 
-// The symmetric products.  A = f sum; B = f sum + fa A with A's planes in `add`.  Blocks of
+// The symmetric products.  A = f sum; B = f sum + fa A + diag I with A's planes in `add`.  Blocks of
 // 32 x 32 right of the diagonal are stored at (row, col) and (col, row).
 struct EpiSym {
     static constexpr bool kFold = false;
     struct Args {
         Planes out, add;     // add.base may be null
-        float f, fa;
+        float f, fa, diag;   // diag: added on the diagonal
         int low, low_add;    // whether out gets, and add has, low halves
         const float* scale;  // of the matrix's planes, or null (1): A takes its square
     };
@@ -117,6 +117,10 @@ struct EpiSym {
         }
         if (c + 32 < p.width) fetch(c + 32);
         if (none) return;
+        if (col == p.row0) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] += j == p.stage.lane ? a.diag : 0.0f;
+        }
         uint32_t h[16], l[16];
 #pragma unroll
         for (int j = 0; j < 16; ++j) split_pair(v[2 * j], v[2 * j + 1], &h[j], &l[j]);
@@ -143,13 +147,13 @@ struct EpiSym {
     __device__ __forceinline__ void done() {}
 };
 
-// X <- a X + f sum, as planes for the next step or, at the last one, in bf16.
+// X <- f sum, as planes for the next step or, at the last one, in bf16.
 struct EpiUpdate {
     static constexpr bool kFold = false;
     struct Args {
-        Planes x, out;
-        float f, fx;         // times the sum, times X's planes
-        int low_x, low;
+        Planes out;
+        float f;
+        int low;
         uint16_t* last;      // or null
         int64_t ld_last, stride_last;
         int vec;
@@ -159,25 +163,17 @@ struct EpiUpdate {
     const HgArgs& g;
     const HgPart& p;
     int batch;
-    float f, fx;
-    Halves32 old;
+    float f;
     __device__ __forceinline__ EpiUpdate(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p_)
         : a(a_), g(g_), p(p_), batch(t.batch) {
-        const float k = a.scale ? a.scale[batch] : 1.0f;
-        f = a.f * k;
-        fx = a.fx * k;
+        f = a.scale ? a.f * a.scale[batch] : a.f;
     }
-    __device__ __forceinline__ void fetch(int c) {
-        if (p.col0 + c >= g.N) return;
-        const uint16_t* x = a.x.base + 2 * batch * a.x.plane;
-        old.load(p, x, a.low_x ? x + a.x.plane : nullptr, a.x.ld, p.col0 + c);
-    }
+    __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
         const int col = p.col0 + c;
-        const bool none = col >= g.N;
-        if (!none) old.join(p, a.low_x != 0, f, fx, v);
-        if (c + 32 < p.width) fetch(c + 32);
-        if (none) return;
+        if (col >= g.N) return;
+#pragma unroll
+        for (int j = 0; j < 32; ++j) v[j] *= f;
         uint32_t h[16], l[16];
         if (!a.last) {
 #pragma unroll
@@ -355,7 +351,7 @@ struct OsArgs {
     int steps;
     int exact_first;         // X0's low halves are zero
     int vec, vec_out;        // rows of M and of the result are 16-byte aligned
-    float mul, fa, fs, fsa, fu, fux, fu_last, fux_last;
+    float mul, fa, fs, fsa, diag, fu, fu_last;
     uint32_t* status;
 };
 
@@ -595,7 +591,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
             asm volatile("fence.proxy.async;" ::: "memory");
             cluster_barrier();
         }
-        // B = b A + c A^2
+        // B = a I + b A + c A^2
         batch([&] { products(d_s, desc_sw128(sh_a), desc_sw128(sh_a), s_lo, s_lo, low, low, id_s, a.mp / 16, along, along); });
         columns(d_s, s0, s1, [&](int c, const uint32_t* v) {
             const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
@@ -606,34 +602,25 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const float2 x = halves2(hr[j]), y = halves2(lr[j]);
-                split_pair(fmaf(a.fsa, x.x + y.x, __uint_as_float(v[2 * j]) * a.fs),
-                           fmaf(a.fsa, x.y + y.y, __uint_as_float(v[2 * j + 1]) * a.fs), &hw[j], &lw[j]);
+                const int at = row - c - 2 * j;
+                split_pair(fmaf(a.fsa, x.x + y.x, __uint_as_float(v[2 * j]) * a.fs) + (at == 0 ? a.diag : 0.0f),
+                           fmaf(a.fsa, x.y + y.y, __uint_as_float(v[2 * j + 1]) * a.fs) + (at == 1 ? a.diag : 0.0f), &hw[j], &lw[j]);
             }
             *reinterpret_cast<uint4*>(sh + o) = make_uint4(hw[0], hw[1], hw[2], hw[3]);
             if (low) *reinterpret_cast<uint4*>(sl + o) = make_uint4(lw[0], lw[1], lw[2], lw[3]);
         });
-        // X = a X + B X
+        // X = B X
         batch([&] {
             products(d_u, desc_sw128(sh_a), desc_sw128_mn(xh_a, 16384), s_lo, x_lo, low, low_x, id_u, a.mp / 16, along, across);
         });
         const bool last = i + 1 == a.steps;
-        const float fu = (last ? a.fu_last : a.fu) * k0, fux = (last ? a.fux_last : a.fux) * k0;
+        const float fu = (last ? a.fu_last : a.fu) * k0;
         columns(d_u, u0, u1, [&](int c, const uint32_t* v) {
             if (row >= m || c >= nc) return;
             const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(row, (c & 63) >> 3);
-            const uint4 hv = *reinterpret_cast<const uint4*>(xh + o);
-            // where the products take the high halves alone, so does a X: the step is then exact
-            // for a rounded X, and rounding moves a singular value near 1 by 1.5 times itself,
-            // not by a - p' = 5 times
-            const uint4 lv = low ? *reinterpret_cast<const uint4*>(xl + o) : make_uint4(0, 0, 0, 0);
-            const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
             float f[8];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float2 x = halves2(hr[j]), y = halves2(lr[j]);
-                f[2 * j] = fmaf(fux, x.x + y.x, __uint_as_float(v[2 * j]) * fu);
-                f[2 * j + 1] = fmaf(fux, x.y + y.y, __uint_as_float(v[2 * j + 1]) * fu);
-            }
+            for (int j = 0; j < 8; ++j) f[j] = __uint_as_float(v[j]) * fu;
             if (!last) {
                 uint32_t hw[4], lw[4];
 #pragma unroll
@@ -726,16 +713,16 @@ bool oalloc(nitro_orth* h, T** p, int64_t count) {
 float half_scale(double top) { return (float)std::ldexp(1.0, 15 - (int)std::ceil(std::log2(std::max(top, 1e-6)))); }
 
 // The largest singular value that can occur before each step (from 1), and the largest
-// |b s^2 + c s^4|; false where they leave the range that fp16 planes hold.
+// |a + b s^2 + c s^4|; false where they leave the range that fp16 planes hold.
 bool orth_range(const float* k, int steps, double* top, double* top_b) {
     double hi = 1.0, all = 1.0, bmax = 0.0;
     const double a = k[0], b = k[1], c = k[2];
-    const auto p = [=](double s2) { return b * s2 + c * s2 * s2; };
+    const auto p = [=](double s2) { return a + b * s2 + c * s2 * s2; };
     if (!(std::fabs(a) < 1e6 && std::fabs(b) < 1e6 && std::fabs(c) < 1e6)) return false;
     for (int i = 0; i < steps; ++i) {
-        // s (a + b s^2 + c s^4) and b s^2 + c s^4 on [0, hi]: at its end and where they turn
+        // s (a + b s^2 + c s^4) and a + b s^2 + c s^4 on [0, hi]: at its ends and where they turn
         const double end = hi * hi, disc = 9 * b * b - 20 * a * c;
-        double at[4] = {end, -1, -1, -1};
+        double at[5] = {end, -1, -1, -1, 0};
         if (c != 0) at[3] = -b / (2 * c);
         if (c != 0 && disc >= 0) {
             at[1] = (-3 * b + std::sqrt(disc)) / (10 * c);
@@ -746,7 +733,7 @@ bool orth_range(const float* k, int steps, double* top, double* top_b) {
         double next = 0.0;
         for (const double s2 : at) {
             if (!(s2 >= 0 && s2 <= end)) continue;
-            next = std::max(next, std::sqrt(s2) * std::fabs(a + p(s2)));
+            next = std::max(next, std::sqrt(s2) * std::fabs(p(s2)));
             bmax = std::max(bmax, std::fabs(p(s2)));
         }
         if (i + 1 < steps) all = std::max(all, next);
@@ -755,7 +742,7 @@ bool orth_range(const float* k, int steps, double* top, double* top_b) {
     }
     // rounding moves a value past its bound a little
     *top = 1.01 * all;
-    *top_b = 1.01 * bmax + 1e-3;
+    *top_b = 1.01 * bmax;
     return true;
 }
 
@@ -875,8 +862,8 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
         const OsArgs a{m, ldm, stride_m, out, ldo, stride_o, h->rows, h->cols, tall, 0, 0, steps, m_type == NITRO_BF16,
                        ((uintptr_t)m & 15) == 0 && ldm * size % 16 == 0 && stride_m * size % 16 == 0,
                        ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && stride_o % 8 == 0, sx,
-                       sa / (sx * sx), k[2] * sb / (sa * sa), k[1] * sb / sa, 1.0f / sb, k[0],
-                       1.0f / (sb * sx), k[0] / sx, h->status};
+                       sa / (sx * sx), k[2] * sb / (sa * sa), k[1] * sb / sa, k[0] * sb, 1.0f / sb,
+                       1.0f / (sb * sx), h->status};
         ProfScope ps(K_ORTH_SMALL, s, (double)count * steps * n * n * (3.0 * big + n), (double)count * n * big * (size + 2));
         TRY(m_type == NITRO_BF16 ? small_run<uint16_t>(c, a, count, s)
             : m_type == NITRO_F32 ? small_run<float>(c, a, count, s) : small_run<int64_t>(c, a, count, s));
@@ -910,16 +897,16 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
         p.prof = K_ORTH_GRAM;
         p.ops = (double)count * n * n * big;
         const float* g0 = i == 0 ? h->scale : nullptr;
-        const EpiSym::Args ga{h->a, {nullptr, 0, 0}, sa / (sx * sx), 0.0f, low, 0, g0};
+        const EpiSym::Args ga{h->a, {nullptr, 0, 0}, sa / (sx * sx), 0.0f, 0.0f, low, 0, g0};
         if (tall && low_x) TRY((hg_launch<EpiSym, true, true, true, 2, 2>(tg, p, ox, ox, ga, s)));
         else if (tall) TRY((hg_launch<EpiSym, true, true, true>(tg, p, ox, ox, ga, s)));
         else if (low_x) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(tg, p, ox, ox, ga, s)));
         else TRY((hg_launch<EpiSym, false, false, true>(tg, p, ox, ox, ga, s)));
-        // B = b A + c A^2
+        // B = a I + b A + c A^2
         p.K = n;
         p.prof = K_ORTH_SQUARE;
         p.ops = (double)count * n * n * n;
-        const EpiSym::Args gb{h->b, h->a, k[2] * sb / (sa * sa), k[1] * sb / sa, low, low, nullptr};
+        const EpiSym::Args gb{h->b, h->a, k[2] * sb / (sa * sa), k[1] * sb / sa, k[0] * sb, low, low, nullptr};
         if (low) TRY((hg_launch<EpiSym, false, false, true, 2, 2>(hg_pick(p, 2, 2), p, oa, oa, gb, s)));
         else TRY((hg_launch<EpiSym, false, false, true>(hg_pick(p), p, oa, oa, gb, s)));
         // X
@@ -930,8 +917,8 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
         p.ops = 2.0 * count * n * n * big;
         const bool last = i + 1 == steps;
         const float so = last ? 1.0f : sx;
-        const EpiUpdate::Args gu{x, h->x[(i + 1) & 1], so / (sb * sx), k[0] * so / sx, low_x, low_next, last ? out : nullptr,
-                                 ldo, stride_o, ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && (count == 1 || stride_o % 8 == 0), g0};
+        const EpiUpdate::Args gu{h->x[(i + 1) & 1], so / (sb * sx), low_next, last ? out : nullptr, ldo, stride_o,
+                                 ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && (count == 1 || stride_o % 8 == 0), g0};
         const int hb = 1 + low, hx = 1 + (low && low_x);
         const HgPick t = tall ? hg_pick(p, hx, hb) : hg_pick(p, hb, hx);
         if (tall && low && low_x) TRY((hg_launch<EpiUpdate, false, false, true, 2, 2>(t, p, ox, ob, gu, s)));
