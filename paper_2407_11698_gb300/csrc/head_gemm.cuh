@@ -245,6 +245,8 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
 //   void cols(c, v)         v[0..32): columns col0 + c .. col0 + c + 31 of the thread's row; all
 //                           lanes call it, rows and columns past the end among them
 //   void done()
+//   kTail                   whether tail(args, g, shared word) follows, called by every thread once the CTA's
+//                           tiles are done
 //   kFold                   whether K may go to the two accumulators by halves, to be added here
 template <class Epi, int CG, int BN, bool AMN, bool BMN, bool F16, int HA, int HB, int KS>
 __global__ void __launch_bounds__(kHgThreads, 1)
@@ -530,6 +532,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
     __syncwarp();
     tc_fence_before();
     __syncthreads();
+    if constexpr (Epi::kTail) Epi::tail(ea, g, reinterpret_cast<int*>(tmem_slot + 2));
     if constexpr (CG == 2 || KS > 1) cluster_barrier();   // no copy, MMA or arrival of the pair is outstanding
     if (warp == 2) {
         tc_fence_after();

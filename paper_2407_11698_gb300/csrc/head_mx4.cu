@@ -37,23 +37,54 @@ __device__ __forceinline__ int64_t scale_at(int64_t row, int j, int tiles) {
     return ((row >> 7) * tiles + (j >> 2)) * 512 + (row & 31) * 16 + ((row >> 5) & 3) * 4 + (j & 3);
 }
 
-// two values -> two e2m1 codes in a byte, b in the high half; nearest, ties to even, at most 6
-__device__ __forceinline__ uint32_t e2m1x2(float a, float b) {
+// eight values -> eight e2m1 codes, v[0] lowest; nearest, ties to even, at most 6
+__device__ __forceinline__ uint32_t e2m1x8(const float* v) {
     uint32_t r;
-    asm("{\n .reg .b8 t;\n cvt.rn.satfinite.e2m1x2.f32 t, %2, %1;\n cvt.u32.u8 %0, t;\n}\n" : "=r"(r) : "f"(a), "f"(b));
+    asm("{\n .reg .b8 a, b, c, d;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 a, %2, %1;\n cvt.rn.satfinite.e2m1x2.f32 b, %4, %3;\n"
+        " cvt.rn.satfinite.e2m1x2.f32 c, %6, %5;\n cvt.rn.satfinite.e2m1x2.f32 d, %8, %7;\n"
+        " mov.b32 %0, {a, b, c, d};\n}\n"
+        : "=r"(r)
+        : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return r;
 }
-
-constexpr int kMxInFlight = 4;      // loads of a thread in flight
 
 // eight values as loaded
 template <typename T>
 struct Raw8 {
     uint4 w[sizeof(T) / 2];
-    __device__ __forceinline__ float get(int j) const {
+    // the largest magnitude's bits (magnitudes as integers keep their order, and a NaN is the largest)
+    __device__ __forceinline__ uint32_t top() const {
         const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
-        if constexpr (sizeof(T) == 2) return __uint_as_float(j & 1 ? u[j >> 1] & 0xffff0000u : u[j >> 1] << 16);
-        else return __uint_as_float(u[j]);
+        if constexpr (sizeof(T) == 2) {
+            const uint32_t m = __vmaxu2(__vmaxu2(u[0] & 0x7fff7fffu, u[1] & 0x7fff7fffu),
+                                        __vmaxu2(u[2] & 0x7fff7fffu, u[3] & 0x7fff7fffu));
+            return max(m << 16, m & 0xffff0000u);
+        } else {
+            uint32_t m = 0;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) m = max(m, u[j] & 0x7fffffffu);
+            return m;
+        }
+    }
+    // times 2^k, the float `f`: exact where it matters (below the smallest normal it is 0 as a code)
+    __device__ __forceinline__ uint32_t codes(float f) const {
+        const uint32_t* u = reinterpret_cast<const uint32_t*>(w);
+        float v[8];
+        if constexpr (sizeof(T) == 2) {
+            const __nv_bfloat162 k = __float2bfloat162_rn(f);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&u[j]), k);
+                const uint32_t b = *reinterpret_cast<const uint32_t*>(&p);
+                v[2 * j] = __uint_as_float(b << 16);
+                v[2 * j + 1] = __uint_as_float(b & 0xffff0000u);
+            }
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(u[j]) * f;
+        }
+        return e2m1x8(v);
     }
 };
 template <typename T>
@@ -64,7 +95,7 @@ __device__ __forceinline__ Raw8<T> load8(const T* src, int n, bool vec) {
     if (vec && n >= 8) {
 #pragma unroll
         for (int j = 0; j < (int)sizeof(T) / 2; ++j) r.w[j] = reinterpret_cast<const uint4*>(src)[j];
-    } else {
+    } else if (n > 0) {
         uint32_t* u = reinterpret_cast<uint32_t*>(r.w);
 #pragma unroll
         for (int j = 0; j < 8; ++j) {
@@ -75,9 +106,17 @@ __device__ __forceinline__ Raw8<T> load8(const T* src, int n, bool vec) {
     }
     return r;
 }
+// a block's scale as stored, from its largest magnitude's bits: that exponent less 2, at
+// least 0; 255: not finite
+__device__ __forceinline__ uint32_t scale_code(uint32_t top) {
+    const uint32_t e = top >> 23;
+    return e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
+}
+// 2^(127 - s), what a block's values are multiplied by: 254 - s as an exponent (s = 254 cannot be)
+__device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - min(s, 253u)) << 23); }
 
 // Two threads a block, sixteen values each, two such loads in flight.  The grid covers the
-// scales' padding too.  Bound by memory: MX4Q_MEASURED
+// scales' padding too.  MX4Q_MEASURED
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc,
                                                       int blocks, int64_t rows_pad, int vec) {
@@ -102,23 +141,14 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, i
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            // magnitudes as integers keep their order, and a NaN is the largest
-            uint32_t top = 0;
-#pragma unroll
-            for (int j = 0; j < 16; ++j) top = max(top, __float_as_uint(raw[u][j >> 3].get(j & 7)) & 0x7fffffffu);
+            uint32_t top = max(raw[u][0].top(), raw[u][1].top());
             top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
-            // exponent + 127 of the scale: that of the largest less 2, at least 0; 255: not finite
-            const uint32_t e = top >> 23;
-            const uint32_t s = e == 255u ? 255u : (e > 2u ? e - 2u : 0u);
-            // 2^(127 - s): 254 - s as an exponent field (s = 254 cannot be)
-            const float inv = __uint_as_float((254u - min(s, 253u)) << 23);
-            uint32_t w[2] = {0, 0};
-#pragma unroll
-            for (int j = 0; j < 8; ++j)
-                w[j >> 2] |= e2m1x2(raw[u][j >> 2].get(2 * (j & 3)) * inv, raw[u][j >> 2].get(2 * (j & 3) + 1) * inv) << (8 * (j & 3));
+            const uint32_t s = scale_code(top);
+            const float inv = scale_inverse(s);
+            const uint2 w = make_uint2(raw[u][0].codes(inv), raw[u][1].codes(inv));
             const int blk = part[u] >> 1;
             const bool in = row[u] < rows && blk < blocks;
-            if (in) *reinterpret_cast<uint2*>(q + (row[u] * blocks + blk) * 16 + (part[u] & 1) * 8) = make_uint2(w[0], w[1]);
+            if (in) *reinterpret_cast<uint2*>(q + (row[u] * blocks + blk) * 16 + (part[u] & 1) * 8) = w;
             if ((part[u] & 1) == 0 && row[u] < rows_pad) sc[scale_at(row[u], blk, tiles)] = in ? (uint8_t)s : 0;
         }
     }
@@ -128,67 +158,80 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, i
 __device__ __forceinline__ float e8m0_value(uint32_t s) {
     return s == 255u ? __uint_as_float(0x7fc00000u) : s == 0u ? __uint_as_float(0x00400000u) : __uint_as_float(s << 23);
 }
-// codes 2i and 2i + 1 of a word as two bf16: their halves looked up byte by byte (the
-// magnitudes 0, 1/2, 1, 3/2, 2, 3, 4, 6 are 0000 3f00 3f80 3fc0 4000 4040 4080 40c0)
-__device__ __forceinline__ uint32_t e2m1_bf16x2(uint32_t w, int i) {
-    const uint32_t c = w >> (8 * i), sel = (c & 7u) | (c & 0x70u);
+// Codes 4h to 4h + 3 of a word as two words of two bf16 each: the halves of the magnitudes 0,
+// 1/2, 1, 3/2, 2, 3, 4, 6 (0000 3f00 3f80 3fc0 4000 4040 4080 40c0) looked up byte by byte, four
+// codes a look-up, and the codes' sign bits.
+__device__ __forceinline__ void e2m1_bf16x4(uint32_t w, int h, uint32_t* out) {
+    const uint32_t sel = (w >> (16 * h)) & 0x7777u;
     const uint32_t hi = __byte_perm(0x3f3f3f00u, 0x40404040u, sel), lo = __byte_perm(0xc0800000u, 0xc0804000u, sel);
-    return __byte_perm(lo, hi, 0x5140) | (c & 8u) << 12 | (c & 0x80u) << 24;
+    // bytes 1 and 3: the one that has a code's sign on top
+    const uint32_t up = w << 4;
+    out[0] = __byte_perm(lo, hi, 0x5140) | (__byte_perm(up, w, h ? 0x6020 : 0x4000) & 0x80008000u);
+    out[1] = __byte_perm(lo, hi, 0x7362) | (__byte_perm(up, w, h ? 0x7030 : 0x5010) & 0x80008000u);
 }
 
+// Sixteen values a thread, two loads in flight.  MX4D_MEASURED
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const uint8_t* sc, int rows, int cols, int blocks,
                                                         T* out, int64_t ldo, float* scales, int vec) {
     pdl_wait();
-    const int tiles = (blocks + 3) / 4, per = blocks * 4;
+    const int tiles = (blocks + 3) / 4, per = blocks * 2;
     const int64_t step = (int64_t)gridDim.x * 256;
     RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, step, per);
+    const uint2* src = reinterpret_cast<const uint2*>(q) + blockIdx.x * (int64_t)256 + threadIdx.x;
     while (at.row < rows) {
-        uint32_t w[kMxInFlight], s[kMxInFlight];
-        int64_t row[kMxInFlight];
-        int part[kMxInFlight];
+        uint2 w[2];
+        uint32_t s[2];
+        int64_t row[2];
+        int part[2];
 #pragma unroll
-        for (int u = 0; u < kMxInFlight; ++u) {
+        for (int u = 0; u < 2; ++u, src += step) {
             row[u] = at.row;
             part[u] = at.part;
             if (at.row < rows) {
-                w[u] = *reinterpret_cast<const uint32_t*>(q + (at.row * per + at.part) * 4);
-                s[u] = sc[scale_at(at.row, at.part >> 2, tiles)];
+                w[u] = *src;
+                s[u] = sc[scale_at(at.row, at.part >> 1, tiles)];
             }
             at.next();
         }
 #pragma unroll
-        for (int u = 0; u < kMxInFlight; ++u) {
+        for (int u = 0; u < 2; ++u) {
             if (row[u] >= rows) continue;
-            const int blk = part[u] >> 2, c = part[u] * 8;
+            const int c = part[u] * 16;
             const float f = e8m0_value(s[u]);
-            if (scales && (part[u] & 3) == 0) scales[row[u] * blocks + blk] = f;
+            if (scales && (part[u] & 1) == 0) scales[row[u] * blocks + (part[u] >> 1)] = f;
             T* dst = out + row[u] * ldo + c;
-            uint32_t v[4];      // two values each, as bf16
-#pragma unroll
-            for (int j = 0; j < 4; ++j) v[j] = e2m1_bf16x2(w[u], j);
+            uint32_t v[8];      // two values each, as bf16
+            e2m1_bf16x4(w[u].x, 0, v);
+            e2m1_bf16x4(w[u].x, 1, v + 2);
+            e2m1_bf16x4(w[u].y, 0, v + 4);
+            e2m1_bf16x4(w[u].y, 1, v + 6);
             if constexpr (sizeof(T) == 2) {
+                const __nv_bfloat162 k = __float2bfloat162_rn(f);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const __nv_bfloat162 p = __floats2bfloat162_rn(__uint_as_float(v[j] << 16) * f, __uint_as_float(v[j] & 0xffff0000u) * f);
+                for (int j = 0; j < 8; ++j) {
+                    const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[j]), k);
                     v[j] = *reinterpret_cast<const uint32_t*>(&p);
                 }
-                if (vec && c + 8 <= cols) *reinterpret_cast<uint4*>(dst) = make_uint4(v[0], v[1], v[2], v[3]);
-                else {
+                if (vec && c + 16 <= cols) {
+                    reinterpret_cast<uint4*>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
+                    reinterpret_cast<uint4*>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
+                } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                    for (int j = 0; j < 16; ++j)
                         if (c + j < cols) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
                 }
             } else {
-                float o[8];
+                float o[16];
 #pragma unroll
-                for (int j = 0; j < 8; ++j) o[j] = __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16) * f;
-                if (vec && c + 8 <= cols) {
-                    reinterpret_cast<float4*>(dst)[0] = make_float4(o[0], o[1], o[2], o[3]);
-                    reinterpret_cast<float4*>(dst)[1] = make_float4(o[4], o[5], o[6], o[7]);
+                for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16) * f;
+                if (vec && c + 16 <= cols) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+                        reinterpret_cast<float4*>(dst)[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
                 } else {
 #pragma unroll
-                    for (int j = 0; j < 8; ++j)
+                    for (int j = 0; j < 16; ++j)
                         if (c + j < cols) dst[j] = o[j];
                 }
             }
@@ -202,7 +245,9 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
 // samples: a tile then has 128 of W's rows and as few columns as there are samples, and the
 // weights stream past once.  CG = 2 pairs two CTAs on 256 x 256 (see head_gemm.cuh): at the
 // 4-bit rate the MMAs of a stage take a third of the time of its loads, so what counts is
-// products a byte loaded.  A pair's accumulator and scales fill TMEM, so its drain waits for
+// products a byte loaded.  FX (bf16 or fp32, for SWAP): Q's codes and scales are not loaded but made by
+// the epilogue warps from the features themselves, stage by stage, which saves the launch
+// that would quantise them; every CTA does so for its own, so it is for few rows.  A pair's accumulator and scales fill TMEM, so its drain waits for
 // the next tile's MMAs, but not for its loads.
 constexpr int kMxThreads = 384, kMxEpiWarp0 = 4, kMxEpiWarps = 8;
 
@@ -216,10 +261,15 @@ struct MxArgs {
     int out;                 // 0 bf16, 1 fp32
     int vec;                 // rows of y are 16-byte aligned
     uint32_t* status;
+    const void* x;           // FX: the features [Q][in]
+    int64_t ldx;
+    int in, vec_x;
 };
 struct MxMaps {
     CUtensorMap p, q, sp, sq;      // codes, scale tiles
 };
+
+struct NoFx {};
 
 template <int CG, int BN>
 struct MxCfg {
@@ -227,8 +277,8 @@ struct MxCfg {
     static constexpr int QT = BN > 128 ? 2 : 1;               // scale tiles of 128 rows a tile's columns take
     static constexpr int SF_BYTES = 1024 + QT * 1024;
     static constexpr int STAGE = P_BYTES + Q_BYTES + SF_BYTES;
-    static constexpr int S = BN >= 128 ? 6 : 8;
-    static constexpr int SMEM = S * STAGE + 1024 + 256;
+    static constexpr int S = CG == 2 ? 5 : BN == 128 ? 6 : 8;
+    static constexpr int SMEM = S * STAGE + kMxEpiWarps * 2048 + 1024 + 256;
     static constexpr int NBUF = CG == 2 ? 1 : 2;               // accumulators
     static constexpr int SF = NBUF * BN, SF_COLS = 8 + 8 * QT; // TMEM columns of a stage's scales, for two stages
     static constexpr int TCOLS = SF + 2 * SF_COLS <= 128 ? 128 : SF + 2 * SF_COLS <= 256 ? 256 : 512;
@@ -290,14 +340,16 @@ __device__ __forceinline__ MxTile mx_decode(const MxArgs& g, int idx) {
     return t;
 }
 
-template <int CG, int BN, bool SWAP>
+template <int CG, int BN, bool SWAP, typename FX>
 __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constant__ MxMaps maps, const MxArgs g) {
     using C = MxCfg<CG, BN>;
     constexpr int S = C::S;
+    constexpr bool kFx = !std::is_same_v<FX, NoFx>;
+    static_assert(!kFx || (SWAP && BN == 32), "features in the kernel: for few rows");
     extern __shared__ uint8_t smem_raw[];
     uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
-    // stages of operands (1024-byte aligned), then the scales
-    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE);
+    // stages of operands (1024-byte aligned), the scales, the warps' own 2 KB
+    uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE + kMxEpiWarps * 2048);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 5);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -311,7 +363,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
     const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
     if (threadIdx.x == 0) {
         for (int s = 0; s < S; ++s) {
-            mbar_init(full_bar(s), 1);
+            mbar_init(full_bar(s), kFx ? 2 : 1);
             mbar_init(empty_bar(s), 1);
         }
         for (int b = 0; b < 2; ++b) {
@@ -323,6 +375,10 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
     if (warp == 2) hg_tmem_alloc<CG>(smem_u32(tmem_slot), C::TCOLS);
+    if constexpr (kFx) {     // rows past the last one stay zero
+        for (int i = threadIdx.x; i < S * C::STAGE / 16; i += kMxThreads) reinterpret_cast<uint4*>(smem)[i] = make_uint4(0, 0, 0, 0);
+        asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+    }
     if (warp == 0 && lane < 4)
         asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(&maps.p + lane)) : "memory");
     pdl_wait();
@@ -343,13 +399,15 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                     if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
                     const uint32_t dp = s0 + st * (C::P_BYTES + C::Q_BYTES), dq = dp + C::P_BYTES, ds = sf0 + st * C::SF_BYTES;
                     uint32_t fb = full_bar(st);
-                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
+                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, kFx ? C::P_BYTES + 1024 : CG * C::STAGE);
                     if constexpr (CG == 2) fb = remote_smem(fb, 0);
                     mx_tma<CG>(dp, &maps.p, fb, k * 128, p0);
-                    mx_tma<CG>(dq, &maps.q, fb, k * 128, q0 + rank * C::Q_ROWS);
-                    // both CTAs of a pair hold the scales of all columns
                     mx_tma<CG>(ds, &maps.sp, fb, k * 256, p0 / 128);
-                    mx_tma<CG>(ds + 1024, &maps.sq, fb, k * 256, q0 / 128);
+                    if constexpr (!kFx) {
+                        mx_tma<CG>(dq, &maps.q, fb, k * 128, q0 + rank * C::Q_ROWS);
+                        // both CTAs of a pair hold the scales of all columns
+                        mx_tma<CG>(ds + 1024, &maps.sq, fb, k * 256, q0 / 128);
+                    }
                     ++loaded;
                     if (++st == S) {
                         st = 0;
@@ -409,35 +467,82 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
         }
     } else if (warp >= kMxEpiWarp0) {
         const int q = warp & 3, half = (warp - kMxEpiWarp0) >> 2;
-        int it = 0;
+        const HgStage hs{reinterpret_cast<uint4*>(smem + S * C::STAGE) + (warp - kMxEpiWarp0) * 128, lane};
+        int it = 0, made = 0;       // made: stages of the tiles before
         for (int tile = unit; tile < g.total; tile += units, ++it) {
             const MxTile T = mx_decode(g, tile);
             const int buf = it % C::NBUF;
+            if constexpr (kFx) {
+                // Every eighth stage is this warp's, so that the loads' latencies overlap (all
+                // warps on each stage took 16.5 us where two launches take 14.4): sixteen values a
+                // thread, two threads a block, two rows at a time, four of those in flight.
+                const int part = lane & 15, r0 = lane >> 4, blk = part >> 1;
+                const FX* x = static_cast<const FX*>(g.x);
+                bool ok = true;
+                for (int k = T.s0 + warp - kMxEpiWarp0; k < T.s1 && ok; k += kMxEpiWarps) {
+                    const int n = made + k - T.s0, st = n % S, c = k * 256 + part * 16;
+                    uint8_t* dq = smem + st * (C::P_BYTES + C::Q_BYTES) + C::P_BYTES;
+                    uint8_t* ds = smem + S * (C::P_BYTES + C::Q_BYTES) + st * C::SF_BYTES + 1024;
+                    for (int rb = 0; rb < g.Q; rb += 8) {
+                        Raw8<FX> raw[4][2];
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int r = rb + 2 * u + r0, left = r < g.Q ? g.in - c : 0;
+                            const FX* src = x + r * g.ldx + c;
+                            raw[u][0] = load8(src, left, g.vec_x != 0);
+                            raw[u][1] = load8(src + 8, left - 8, g.vec_x != 0);
+                        }
+                        if (rb == 0) {
+                            ok = mbar_wait(empty_bar(st), ((uint32_t)(n / S) & 1u) ^ 1u, abort_flag, g.status);
+                            if (!(ok = __all_sync(0xffffffffu, ok))) break;
+                        }
+#pragma unroll
+                        for (int u = 0; u < 4; ++u) {
+                            const int r = rb + 2 * u + r0;
+                            uint32_t top = max(raw[u][0].top(), raw[u][1].top());
+                            top = max(top, __shfl_xor_sync(0xffffffffu, top, 1));
+                            const uint32_t s = scale_code(top);
+                            const float inv = scale_inverse(s);
+                            const uint2 w = make_uint2(raw[u][0].codes(inv), raw[u][1].codes(inv));
+                            if (r >= g.Q) continue;
+                            *reinterpret_cast<uint2*>(dq + r * 128 + ((blk ^ (r & 7)) << 4) + (part & 1) * 8) = w;
+                            if ((part & 1) == 0) ds[(blk >> 2) * 512 + r * 16 + (blk & 3)] = (uint8_t)s;
+                        }
+                        __syncwarp();
+                    }
+                    asm volatile("fence.proxy.async.shared::cta;" ::: "memory");
+                    __syncwarp();
+                    if (lane == 0 && ok) mbar_arrive(full_bar(st));
+                }
+                if (!ok) break;
+                made += T.s1 - T.s0;
+            }
             const bool ok = mbar_wait(tfull_bar(buf), (uint32_t)(it / C::NBUF) & 1u, abort_flag, g.status);
             if (!__all_sync(0xffffffffu, ok)) break;
             tc_fence_after();
-            const int row = T.p * 128 * CG + rank * 128 + q * 32 + lane, col0 = T.q * BN + half * (BN / 2);
+            const int row0 = T.p * 128 * CG + rank * 128 + q * 32, row = row0 + lane, col0 = T.q * BN + half * (BN / 2);
             const uint32_t src = tmem + ((uint32_t)(q * 32) << 16) + (uint32_t)(buf * BN + half * (BN / 2));
             float* yf = static_cast<float*>(g.y) + T.split * g.slice;
             uint16_t* yb = static_cast<uint16_t*>(g.y);
-#pragma unroll 4
-            for (int c = 0; c < BN / 2; c += 16) {
+            const auto release = [&] {
+                tc_fence_before();
                 __syncwarp();
-                uint32_t v[16];
-                tmem_ld16_nowait(src + c, v);
-                tmem_wait_ld<16>(v);
-                if (c + 16 == BN / 2) {
-                    tc_fence_before();
-                    __syncwarp();
-                    if (lane == 0) {
-                        if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
-                        else mbar_arrive(tempty_bar(buf));
-                    }
+                if (lane == 0) {
+                    if constexpr (CG == 2) mbar_arrive_remote(remote_smem(tempty_bar(buf), 0));
+                    else mbar_arrive(tempty_bar(buf));
                 }
-                const int n = g.Q - (col0 + c);
-                if (row >= g.P || n <= 0) continue;
-                const float* f = reinterpret_cast<const float*>(v);
-                if constexpr (SWAP) {
+            };
+            if constexpr (SWAP) {
+#pragma unroll 1
+                for (int c = 0; c < BN / 2; c += 16) {
+                    uint32_t v[16];
+                    __syncwarp();
+                    tmem_ld16_nowait(src + c, v);
+                    tmem_wait_ld<16>(v);
+                    if (c + 16 == BN / 2) release();
+                    const int n = g.Q - (col0 + c);
+                    if (row >= g.P || n <= 0) continue;
+                    const float* f = reinterpret_cast<const float*>(v);
 #pragma unroll
                     for (int j = 0; j < 16; ++j) {
                         if (j >= n) continue;
@@ -445,32 +550,53 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                         if (g.out) yf[at] = f[j];
                         else yb[at] = __bfloat16_as_ushort(__float2bfloat16_rn(f[j]));
                     }
+                }
+            } else {
+                // all columns in bf16 leave TMEM before the first is stored, so that the next tile's
+                // MMAs wait no longer than for that
+                constexpr int N = BN / 64;
+                const HgPart hp{row, row0, g.P, col0, BN / 2, half, hs};
+                if (!g.out) {
+                    uint32_t w[N][16];
+#pragma unroll
+                    for (int c = 0; c < N; ++c) {
+                        uint32_t v[32];
+                        __syncwarp();
+                        tmem_ld32_nowait(src + 32 * c, v);
+                        tmem_wait_ld<32>(v);
+#pragma unroll
+                        for (int j = 0; j < 16; ++j) {
+                            const __nv_bfloat162 p = __floats2bfloat162_rn(__uint_as_float(v[2 * j]), __uint_as_float(v[2 * j + 1]));
+                            w[c][j] = *reinterpret_cast<const uint32_t*>(&p);
+                        }
+                    }
+                    release();
+#pragma unroll
+                    for (int c = 0; c < N; ++c)
+                        if (col0 + 32 * c < g.Q) hg_store16(hp, w[c], yb, g.ldy, col0 + 32 * c, g.Q, g.vec != 0);
                 } else {
-                    const int64_t at = (int64_t)row * g.ldy + col0 + c;
-                    if (g.out) {
-                        if (g.vec && n >= 16) {
+#pragma unroll 1
+                    for (int c = 0; c < BN / 2; c += 32) {
+                        uint4 v[8];
+                        __syncwarp();
+                        tmem_ld32_nowait(src + c, reinterpret_cast<uint32_t*>(v));
+                        tmem_wait_ld<32>(reinterpret_cast<uint32_t*>(v));
+                        if (c + 32 == BN / 2) release();
+                        hs.to_lines(v);
+                        hs.to_lines(v + 4);
 #pragma unroll
-                            for (int j = 0; j < 4; ++j)
-                                reinterpret_cast<float4*>(yf + at)[j] = make_float4(f[4 * j], f[4 * j + 1], f[4 * j + 2], f[4 * j + 3]);
-                        } else {
+                        for (int k = 0; k < 8; ++k) {
+                            const int r = row0 + hs.line_row(k & 3), cc = col0 + c + 16 * (k >> 2) + 4 * hs.line_chunk();
+                            if (r >= g.P || cc >= g.Q) continue;
+                            float* dst = yf + (int64_t)r * g.ldy + cc;
+                            if (g.vec && cc + 4 <= g.Q) {
+                                *reinterpret_cast<uint4*>(dst) = v[k];
+                            } else {
+                                const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
 #pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (j < n) yf[at + j] = f[j];
-                        }
-                    } else {
-                        uint32_t w[8];
-#pragma unroll
-                        for (int j = 0; j < 8; ++j) {
-                            const __nv_bfloat162 p = __floats2bfloat162_rn(f[2 * j], f[2 * j + 1]);
-                            w[j] = *reinterpret_cast<const uint32_t*>(&p);
-                        }
-                        if (g.vec && n >= 16) {
-                            reinterpret_cast<uint4*>(yb + at)[0] = make_uint4(w[0], w[1], w[2], w[3]);
-                            reinterpret_cast<uint4*>(yb + at)[1] = make_uint4(w[4], w[5], w[6], w[7]);
-                        } else {
-#pragma unroll
-                            for (int j = 0; j < 16; ++j)
-                                if (j < n) yb[at + j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+                                for (int j = 0; j < 4; ++j)
+                                    if (cc + j < g.Q) dst[j] = __uint_as_float(u[j]);
+                            }
                         }
                     }
                 }
@@ -527,25 +653,30 @@ struct MxOperand {
     int64_t rows;
 };
 
-template <int CG, int BN, bool SWAP>
+template <int CG, int BN, bool SWAP, typename FX = NoFx>
 cudaError_t mx_launch(const MxOperand& p, const MxOperand& q, int in, MxArgs g, double ops, double bytes, cudaStream_t s) {
     using C = MxCfg<CG, BN>;
     MxMaps m;
     const int64_t pitch = blocks_of(in) * 16, tiles_k = (blocks_of(in) + 3) / 4;
-    if (!mx_map(&m.p, p.codes, p.rows, pitch, 128) || !mx_map(&m.q, q.codes, q.rows, pitch, C::Q_ROWS) ||
-        !mx_scale_map(&m.sp, p.scales, p.rows, tiles_k, 1) || !mx_scale_map(&m.sq, q.scales, q.rows, tiles_k, C::QT))
-        return cudaErrorInvalidValue;
+    if (!mx_map(&m.p, p.codes, p.rows, pitch, 128) || !mx_scale_map(&m.sp, p.scales, p.rows, tiles_k, 1)) return cudaErrorInvalidValue;
+    if (std::is_same_v<FX, NoFx>) {
+        if (!mx_map(&m.q, q.codes, q.rows, pitch, C::Q_ROWS) || !mx_scale_map(&m.sq, q.scales, q.rows, tiles_k, C::QT))
+            return cudaErrorInvalidValue;
+    } else {
+        m.q = m.p;      // not read
+        m.sq = m.sp;
+    }
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
     const int sms = sm_count(&dev);
     const cudaError_t e = once_per_device(ready, dev, [] {
-        return cudaFuncSetAttribute(k_mx4_gemm<CG, BN, SWAP>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
+        return cudaFuncSetAttribute(k_mx4_gemm<CG, BN, SWAP, FX>, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM);
     });
     if (e != cudaSuccess) return e;
     const int grid = std::min(g.total, sms / CG) * CG;
     ProfScope ps(K_MX4_LINEAR, s, ops, bytes);
-    if constexpr (CG == 2) return launch_cluster(k_mx4_gemm<CG, BN, SWAP>, dim3(grid), kMxThreads, 2, s, C::SMEM, m, g);
-    else return launch_k(k_mx4_gemm<CG, BN, SWAP>, dim3(grid), dim3(kMxThreads), C::SMEM, s, m, g);
+    if constexpr (CG == 2) return launch_cluster(k_mx4_gemm<CG, BN, SWAP, FX>, dim3(grid), kMxThreads, 2, s, C::SMEM, m, g);
+    else return launch_k(k_mx4_gemm<CG, BN, SWAP, FX>, dim3(grid), dim3(kMxThreads), C::SMEM, s, m, g);
 }
 
 // CTAs for n items: one an item and thread while few, then what the SMs hold at once
@@ -614,7 +745,7 @@ nitro_status nitro_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, i
         return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int blocks = (int)blocks_of(cols);
-    const int64_t n = (int64_t)rows * blocks * 4;
+    const int64_t n = (int64_t)rows * blocks * 2;
     const int grid = mx_grid(n);
     const int size = type == NITRO_BF16 ? 2 : 4;
     const int vec = ((uintptr_t)out & 15) == 0 && ldo * size % 16 == 0;
@@ -664,8 +795,12 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
     if (rows == 0) return NITRO_OK;
     if (!w_codes || !w_scales || ((uintptr_t)w_codes & 15) || ((uintptr_t)w_scales & 15)) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (x_type == NITRO_BF16) TRY(quantize((const uint16_t*)x, ldx, rows, h->in, h->xq, h->xs, s));
-    else TRY(quantize((const float*)x, ldx, rows, h->in, h->xq, h->xs, s));
+    // up to this many rows the product's CTAs quantise them themselves
+    const bool inside = rows <= 32;
+    if (!inside) {
+        if (x_type == NITRO_BF16) TRY(quantize((const uint16_t*)x, ldx, rows, h->in, h->xq, h->xs, s));
+        else TRY(quantize((const float*)x, ldx, rows, h->in, h->xq, h->xs, s));
+    }
     // Few samples: W's rows along the lanes.  Else pairs, or 128 x 128 tiles where those finish
     // earlier: a stage takes a lone CTA and a pair the same time (32 KB into an SM).
     const bool swap = rows <= 64;
@@ -697,7 +832,7 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
         }
     };
     if (swap) {
-        consider(1, rows <= 32 ? 32 : 64);
+        consider(1, inside ? 32 : 64);
     } else {
         consider(2, 256);
         consider(1, 128);
@@ -715,7 +850,12 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
     const double ops = 2.0 * rows * h->in * h->out;
     const double bytes = (double)code_bytes(h->out, h->in) * 17 / 16 + code_bytes(rows, h->in) + 2.0 * rows * h->out;
     const MxOperand x_op{h->xq, h->xs, rows}, w_op{w_codes, w_scales, h->out};
-    if (bn == 32) TRY((mx_launch<1, 32, true>(w_op, x_op, h->in, g, ops, bytes, s)));
+    g.x = x;
+    g.ldx = ldx;
+    g.in = h->in;
+    g.vec_x = ((uintptr_t)x & 15) == 0 && ldx * (x_type == NITRO_F32 ? 4 : 2) % 16 == 0;
+    if (inside && x_type == NITRO_BF16) TRY((mx_launch<1, 32, true, uint16_t>(w_op, x_op, h->in, g, ops, bytes, s)));
+    else if (inside) TRY((mx_launch<1, 32, true, float>(w_op, x_op, h->in, g, ops, bytes, s)));
     else if (bn == 64) TRY((mx_launch<1, 64, true>(w_op, x_op, h->in, g, ops, bytes, s)));
     else if (cg == 1) TRY((mx_launch<1, 128, false>(x_op, w_op, h->in, g, ops, bytes, s)));
     else TRY((mx_launch<2, 256, false>(x_op, w_op, h->in, g, ops, bytes, s)));

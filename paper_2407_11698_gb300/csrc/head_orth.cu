@@ -78,7 +78,7 @@ struct Planes {
 // The symmetric products.  A = f sum; B = f sum + fa A + diag I with A's planes in `add`.  Blocks of
 // 32 x 32 right of the diagonal are stored at (row, col) and (col, row).
 struct EpiSym {
-    static constexpr bool kFold = false;
+    static constexpr bool kFold = false, kTail = false;
     struct Args {
         Planes out, add;     // add.base may be null
         float f, fa, diag;   // diag: added on the diagonal
@@ -149,7 +149,7 @@ struct EpiSym {
 
 // X <- f sum, as planes for the next step or, at the last one, in bf16.
 struct EpiUpdate {
-    static constexpr bool kFold = false;
+    static constexpr bool kFold = false, kTail = false;
     struct Args {
         Planes out;
         float f;

@@ -38,16 +38,45 @@ __device__ __forceinline__ void pack_bf16_32(const float* v, uint32_t* w) {
 }
 
 // ------------------------------------------------------------------ epilogues
+struct RowOut {
+    const int32_t* labels;
+    float* loss;
+    float* lse;
+    uint32_t* status;
+    int classes;
+};
+__device__ __forceinline__ void write_row(const RowOut& o, int64_t row, float m2, float sum, float zt) {
+    const float lse = (m2 + log2f(sum)) * kLn2;
+    const int lab = o.labels[row];
+    const bool live = lab >= 0 && lab < o.classes;
+    if (!live && lab != -1) atomicOr(o.status, ST_BAD_LABEL);
+    o.lse[row] = lse;
+    o.loss[row] = live ? lse - zt : 0.0f;
+}
+
+// (max, sum of 2^(t - max)) pairs into one.  A NaN among the logits is in a sum, not in a maximum.
+struct MaxSum {
+    float m = -INFINITY, s = 0.0f;
+    __device__ __forceinline__ void join(float om, float os) {
+        const float t = fmaxf(m, om), base = t == -INFINITY ? 0.0f : t;
+        s = s * exp2f(m - base) + os * exp2f(om - base);
+        m = t;
+    }
+};
+
 // Row statistics of a tile in base 2: (max, sum of 2^(t - max)), t = z log2 e, and the
 // label's logit.  A thread holds one row, so nothing is exchanged.
 struct EpiStats {
-    static constexpr bool kFold = true;
+    static constexpr bool kFold = true, kTail = true;
     struct Args {
         const int32_t* labels;
         float k2, scale;      // scale log2 e
         float2* part;         // [per tiles_n][rows]
         int per;              // parts that a tile's columns are taken in
         float* zt;            // [rows]
+        uint32_t* ticket;     // zero before and after
+        int parts;            // few parts of few rows: the last CTA joins them, else 0
+        RowOut out;
     };
     const Args& a;
     const HgArgs& g;
@@ -92,6 +121,36 @@ struct EpiStats {
     __device__ __forceinline__ void done() {
         if (row < g.M) a.part[(int64_t)slot * g.M + row] = make_float2(mx, sum);
     }
+    // the last CTA joins the parts
+    static __device__ __forceinline__ void tail(const Args& a, const HgArgs& g, int* word) {
+        if (!a.parts) return;
+        __threadfence();
+        __syncthreads();
+        if (threadIdx.x == 0) *word = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
+        __syncthreads();
+        if (!*word) return;
+        __threadfence();
+        if (threadIdx.x == 0) *a.ticket = 0;
+        // 8 or 32 lanes a row, so that the rows' loads are under way together
+        const int width = g.M >= kHgThreads / 8 ? 8 : 32, sub = threadIdx.x & (width - 1);
+        for (int r0 = 0; r0 < g.M; r0 += kHgThreads / width) {
+            const int row = r0 + threadIdx.x / width;
+            MaxSum v;
+            if (row < g.M) {
+#pragma unroll 4
+                for (int i = sub; i < a.parts; i += width) {
+                    const float2 p = __ldcg(a.part + (int64_t)i * g.M + row);
+                    v.join(p.x, p.y);
+                }
+            }
+            for (int d = width >> 1; d > 0; d >>= 1)
+                v.join(__shfl_xor_sync(0xffffffffu, v.m, d), __shfl_xor_sync(0xffffffffu, v.s, d));
+            if (sub == 0 && row < g.M) {
+                const int lab = a.out.labels[row];
+                write_row(a.out, row, v.m, v.s, lab >= 0 && lab < a.out.classes ? __ldcg(a.zt + row) : 0.0f);
+            }
+        }
+    }
 };
 
 // softmax - onehot of a piece, rounded once to bf16, the type that the products with it
@@ -99,7 +158,7 @@ struct EpiStats {
 // in here, the -1 at the label, exact in bf16 and most of a row's weight, would be rounded
 // as well, alike in every row.  Rows that are left out give zeros.
 struct EpiProb {
-    static constexpr bool kFold = false;
+    static constexpr bool kFold = false, kTail = false;
     struct Args {
         const int32_t* labels;
         const float* lse;
@@ -148,7 +207,7 @@ struct EpiProb {
 
 // 32-bit sums into slice `split` of c, or added to what it holds.
 struct EpiAcc {
-    static constexpr bool kFold = false;
+    static constexpr bool kFold = false, kTail = false;
     struct Args {
         float* c;
         int64_t ldc, slice;   // ldc a multiple of 32
@@ -191,7 +250,7 @@ struct EpiAcc {
 };
 
 struct EpiBf16 {
-    static constexpr bool kFold = false;
+    static constexpr bool kFold = false, kTail = false;
     struct Args {
         uint16_t* c;
         int64_t ldc;
@@ -219,42 +278,23 @@ struct EpiBf16 {
 };
 
 // ------------------------------------------------------------------ row kernels
-struct RowOut {
-    const int32_t* labels;
-    float* loss;
-    float* lse;
-    uint32_t* status;
-    int classes;
-};
-__device__ __forceinline__ void write_row(const RowOut& o, int64_t row, float m2, float sum, float zt) {
-    const float lse = (m2 + log2f(sum)) * kLn2;
-    const int lab = o.labels[row];
-    const bool live = lab >= 0 && lab < o.classes;
-    if (!live && lab != -1) atomicOr(o.status, ST_BAD_LABEL);
-    o.lse[row] = lse;
-    o.loss[row] = live ? lse - zt : 0.0f;
-}
-
 // Joins a row's tiles: 32 rows a CTA, the tiles over its warps.
 __global__ void __launch_bounds__(256) k_xent_join(const float2* part, int parts, int rows, const float* zt, const RowOut o) {
     __shared__ float2 sh[8][32];
     pdl_wait();
     const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
-    float m = -INFINITY, s = 0.0f;
-    const auto join = [&](float2 p) {
-        const float t = fmaxf(m, p.x), base = t == -INFINITY ? 0.0f : t;
-        s = s * exp2f(m - base) + p.y * exp2f(p.x - base);
-        // a NaN among the logits is in its tile's sum, not in the maximum
-        m = t;
-    };
+    MaxSum v;
     if (row < rows)
-        for (int i = w; i < parts; i += 8) join(part[(int64_t)i * rows + row]);
-    sh[w][lane] = make_float2(m, s);
+        for (int i = w; i < parts; i += 8) {
+            const float2 p = part[(int64_t)i * rows + row];
+            v.join(p.x, p.y);
+        }
+    sh[w][lane] = make_float2(v.m, v.s);
     __syncthreads();
     if (w == 0 && row < rows) {
-        for (int i = 1; i < 8; ++i) join(sh[i][lane]);
+        for (int i = 1; i < 8; ++i) v.join(sh[i][lane].x, sh[i][lane].y);
         const int lab = o.labels[row];
-        write_row(o, row, m, s, lab >= 0 && lab < o.classes ? zt[row] : 0.0f);
+        write_row(o, row, v.m, v.s, lab >= 0 && lab < o.classes ? zt[row] : 0.0f);
     }
 }
 
@@ -295,9 +335,10 @@ struct PackGrad {
 
 // Rows of x as bf16 with a stride of ldp (a multiple of 8; padding zero): int8 activations
 // are exact in bf16.
+// plain (may be null): the rows as they are, as well.
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
-                                                   const PackGrad pg) {
+                                                   const PackGrad pg, uint16_t* plain) {
     __shared__ int first;
     pdl_wait();
     float ref = 1.0f;
@@ -336,7 +377,7 @@ __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int 
             live = live && go != 0.0f;
             if (c == 0) pg.factor[1 + row] = pg.scale * go;
         }
-        if (live) {
+        if (live || plain) {
             const T* src = x + row * ldx + c;
             uint32_t* w = reinterpret_cast<uint32_t*>(&v);
             if constexpr (sizeof(T) == 2) {
@@ -360,7 +401,9 @@ __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int 
 #pragma unroll
                 for (int j = 0; j < 4; ++j) w[j] = bf16x2(b[j >> 1], 2 * (j & 1));
             }
-            if (f != 1.0f) {
+            if (plain) reinterpret_cast<uint4*>(plain)[i] = v;
+            if (!live) v = make_uint4(0, 0, 0, 0);
+            else if (f != 1.0f) {
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
                     w[j] = pack_bf16(__uint_as_float(w[j] << 16) * f, __uint_as_float(w[j] & 0xffff0000u) * f);
@@ -382,6 +425,10 @@ constexpr int kRowsWithLow = 32;
 // that takes FOLD_MEASURED).
 constexpr int kFoldFeatures = 2048;
 
+// Parts of all rows that the forward's last CTA still joins by itself; more go to a launch of
+// their own (4 rows x 512 x 10000: 14 us with that launch, now JOIN_MEASURED).
+constexpr int64_t kPartsInOne = 4096;
+
 constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
 
@@ -399,7 +446,7 @@ struct nitro_xent {
     float2* part = nullptr;
     float* zt = nullptr;
     float* factor = nullptr;    // [1 + max_rows], see PackGrad
-    uint32_t* status = nullptr;
+    uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
     std::vector<void*> allocs;
 };
 
@@ -422,34 +469,24 @@ bool xalloc(nitro_xent* h, T** p, int64_t count) {
 bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld % 8 == 0; }
 
 cudaError_t pack_rows(const void* x, int type, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
-                      const PackGrad& pg, cudaStream_t s) {
+                      const PackGrad& pg, cudaStream_t s, uint16_t* plain = nullptr) {
     const int64_t words = rows * (ldp / 8);
     const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
     ProfScope ps(K_XENT_PACK, s, 0.0, (double)rows * cols * (type == NITRO_I8 ? 3 : 4));
     if (type == NITRO_I8)
-        return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp, pg);
-    return launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, cols, out, ldp, pg);
+        return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp, pg,
+                        plain);
+    return launch_k(k_xent_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, cols, out, ldp, pg,
+                    plain);
 }
 
-// x and W as operands of the logits' product (K = features, both along K); copies where
-// TMA cannot take their rows.
-nitro_status xent_operands(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
-                           int rows, cudaStream_t s, HgOperand* ox, HgOperand* ow) {
-    const int F = h->features;
-    const PackGrad copy{};
-    if (x_type == NITRO_I8 || !tma_rows(x, ldx)) {
-        TRY(pack_rows(x, x_type, ldx, rows, F, h->xp, h->ldp, copy, s));
-        *ox = {h->xp, F, rows, h->ldp, 1, 0};
-    } else {
-        *ox = {x, F, rows, ldx, 1, 0};
-    }
-    if (!tma_rows(w, ldw)) {
-        TRY(pack_rows(w, NITRO_BF16, ldw, h->classes, F, h->wp, h->ldp, copy, s));
-        *ow = {h->wp, F, h->classes, h->ldp, 1, 0};
-    } else {
-        *ow = {w, F, h->classes, ldw, 1, 0};
-    }
-    return NITRO_OK;
+bool copies(const void* x, int type, int64_t ldx) { return type == NITRO_I8 || !tma_rows(x, ldx); }
+
+// W as an operand along K; a copy where TMA cannot take its rows.
+cudaError_t w_operand(nitro_xent* h, const uint16_t* w, int64_t ldw, cudaStream_t s, HgOperand* ow) {
+    const bool copy = copies(w, NITRO_BF16, ldw);
+    *ow = {copy ? h->wp : w, h->features, h->classes, copy ? h->ldp : ldw, 1, 0};
+    return copy ? pack_rows(w, NITRO_BF16, ldw, h->classes, h->features, h->wp, h->ldp, PackGrad{}, s) : cudaSuccess;
 }
 
 bool xent_args(const nitro_xent* h, const void* x, int x_type, int64_t ldx, const void* w, int64_t ldw,
@@ -491,7 +528,7 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     const int64_t parts = 4 * ((classes + 127) / 128);
     const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->xg, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
                     xalloc(h, &h->G, h->g_elems) && xalloc(h, &h->acc, h->acc_floats) &&
-                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->factor, max_rows + 1) && xalloc(h, &h->status, 1) && cudaMemset(h->status, 0, 4) == cudaSuccess;
+                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->factor, max_rows + 1) && xalloc(h, &h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -506,16 +543,21 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     if (rows == 0) return NITRO_OK;
     if (!loss || !lse) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    HgOperand ox, ow;
-    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
-    if (st != NITRO_OK) return st;
+    HgOperand ox{x, h->features, rows, ldx, 1, 0}, ow;
+    if (copies(x, x_type, ldx)) {
+        TRY(pack_rows(x, x_type, ldx, rows, h->features, h->xp, h->ldp, PackGrad{}, s));
+        ox = {h->xp, h->features, rows, h->ldp, 1, 0};
+    }
+    TRY(w_operand(h, w, ldw, s, &ow));
     const RowOut ro{labels, loss, lse, h->status, h->classes};
     HgProblem p = logits_problem(h, rows, h->classes);
     p.fold = h->features > kFoldFeatures;
     const HgPick t = hg_pick(p);
     const int per = t.ks > 1 ? 4 : 2, parts = per * ((h->classes + t.bn - 1) / t.bn);
-    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, per, h->zt};
+    const bool few = (int64_t)parts * rows <= kPartsInOne;
+    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, per, h->zt, h->status + 1, few ? parts : 0, ro};
     TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
+    if (few) return NITRO_OK;
     ProfScope ps(K_XENT_ROWS, s, 0.0, 8.0 * parts * rows);
     TRY(launch_k(k_xent_join, dim3((rows + 31) / 32), dim3(256), 0, s, (const float2*)h->part, parts, rows,
                  (const float*)h->zt, ro));
@@ -537,11 +579,12 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         return NITRO_OK;
     }
     if (!dx && !dw) return NITRO_OK;
-    HgOperand ox, ow;
-    const nitro_status st = xent_operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow);
-    if (st != NITRO_OK) return st;
+    HgOperand ox{x, F, rows, ldx, 1, 0}, ow;
+    const bool copy = copies(x, x_type, ldx);
+    if (copy) ox = {h->xp, F, rows, h->ldp, 1, 0};
     const PackGrad pg{labels, gout, h->factor, scale, V};
-    TRY(pack_rows(x, x_type, ldx, rows, F, h->xg, h->ldp, pg, s));
+    TRY(pack_rows(x, x_type, ldx, rows, F, h->xg, h->ldp, pg, s, copy ? h->xp : nullptr));
+    TRY(w_operand(h, w, ldw, s, &ow));
     const HgOperand og{h->xg, F, rows, h->ldp, 1, 0};
     const int halves = rows <= kRowsWithLow ? 2 : 1;
     int64_t piece = std::min<int64_t>(round_up(V, 64), h->g_elems / halves / rows / 64 * 64);

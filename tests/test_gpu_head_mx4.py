@@ -215,3 +215,28 @@ def test_refusals():
     with pytest.raises(nb.NitroError):
         nb.mx4_quantize(x, odd, s)                              # codes not 16-byte aligned
     h.close()
+
+
+def test_extreme_blocks_in_bf16():
+    x = torch.zeros(6, 32, dtype=torch.bfloat16, device="cuda")
+    x[1] = 2.0 ** -133                              # the smallest subnormal
+    x[2, 5], x[2, 6] = 2.0 ** -126, -2.0 ** -128
+    x[3] = 3.0e38
+    x[4, 3] = float("inf")
+    x[5, 3] = float("nan")
+    v, sv, _, _ = _round_trip(x)
+    want, scales = _define(x)
+    assert _same(v, want) and _same(sv, scales)
+    # values down to 2^-128 are multiples of bf16's smallest
+    assert _same(_round_trip(x, "bf16")[0], want)
+
+
+@pytest.mark.parametrize("rows", [1, 2, 17, 32])
+@pytest.mark.parametrize("dtype", ["bf16", "f32"])
+@pytest.mark.parametrize("k, pad", [(40, 0), (255, 3), (513, 8), (3000, 1)])
+def test_few_rows(rows, dtype, k, pad):
+    # quantised inside the product: the same bits as quantised before it
+    g = torch.Generator(device="cuda").manual_seed(rows + k)
+    x = (torch.randn(rows, k + pad, generator=g, device="cuda") * 5).to(DT[dtype])[:, :k]
+    (q, s), wv = _weights(300, k, 8)
+    _check(x, _linear(x, q, s, 300), wv)
