@@ -51,12 +51,15 @@ __device__ __forceinline__ uint64_t global_ns() {
 // register-split (setmaxnreg) regions of the contraction kernel.
 __device__ __forceinline__ bool mbar_wait_slow(uint32_t bar, uint32_t parity, volatile int* abort_flag,
                                             uint32_t* status, uint64_t limit_ns) {
-    const uint64_t t0 = global_ns();
+    // the timer is read from the 64th try on: a read takes longer than most waits
+    uint64_t t0 = 0;
     for (uint32_t i = 1;; ++i) {
         if (mbar_try_wait(bar, parity)) return true;
         if ((i & 63) == 0) {
             if (*abort_flag) return false;
-            if (global_ns() - t0 > limit_ns) {
+            const uint64_t now = global_ns();
+            if (t0 == 0) t0 = now;
+            if (now - t0 > limit_ns) {
                 *abort_flag = 1;
                 atomicOr(status, ST_TIMEOUT);
                 return false;
