@@ -277,8 +277,8 @@ struct MxCfg {
     static constexpr int QT = BN > 128 ? 2 : 1;               // scale tiles of 128 rows a tile's columns take
     static constexpr int SF_BYTES = 1024 + QT * 1024;
     static constexpr int STAGE = P_BYTES + Q_BYTES + SF_BYTES;
-    static constexpr int S = CG == 2 ? 5 : BN == 128 ? 6 : 8;
-    static constexpr int SMEM = S * STAGE + kMxEpiWarps * 2048 + 1024 + 256;
+    static constexpr int S = BN >= 128 ? 6 : 8;
+    static constexpr int SMEM = S * STAGE + kMxEpiWarps * 2048 + 256;
     static constexpr int NBUF = CG == 2 ? 1 : 2;               // accumulators
     static constexpr int SF = NBUF * BN, SF_COLS = 8 + 8 * QT; // TMEM columns of a stage's scales, for two stages
     static constexpr int TCOLS = SF + 2 * SF_COLS <= 128 ? 128 : SF + 2 * SF_COLS <= 256 ? 256 : 512;
@@ -346,8 +346,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
     constexpr int S = C::S;
     constexpr bool kFx = !std::is_same_v<FX, NoFx>;
     static_assert(!kFx || (SWAP && BN == 32), "features in the kernel: for few rows");
-    extern __shared__ uint8_t smem_raw[];
-    uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) & ~(uintptr_t)1023);
+    extern __shared__ __align__(1024) uint8_t smem[];
     // stages of operands (1024-byte aligned), the scales, the warps' own 2 KB
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE + kMxEpiWarps * 2048);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 5);
@@ -679,14 +678,13 @@ cudaError_t mx_launch(const MxOperand& p, const MxOperand& q, int in, MxArgs g, 
     else return launch_k(k_mx4_gemm<CG, BN, SWAP, FX>, dim3(grid), dim3(kMxThreads), C::SMEM, s, m, g);
 }
 
-// CTAs for n items: one an item and thread while few, then what the SMs hold at once
-int mx_grid(int64_t n) { return (int)std::min<int64_t>((n + 255) / 256, (int64_t)sm_count() * 8); }
 
 template <typename T>
 cudaError_t quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc, cudaStream_t s) {
     const int blocks = (int)blocks_of(cols);
     const int64_t pad = round_up(rows, 128), n = pad * ((blocks + 3) / 4) * 8;
-    const int grid = mx_grid(n);
+    static std::atomic<int> resident{0};
+    const int grid = one_wave(k_mx4_quantize<T>, resident, n);
     const int vec = ((uintptr_t)x & 15) == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
     ProfScope ps(K_MX4_QUANTIZE, s, 0.0, (double)rows * cols * (sizeof(T) + 17.0 / 32.0));
     return launch_k(k_mx4_quantize<T>, dim3(grid), dim3(256), 0, s, x, ldx, rows, cols, q, sc, blocks, pad, vec);
@@ -746,7 +744,9 @@ nitro_status nitro_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, i
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int blocks = (int)blocks_of(cols);
     const int64_t n = (int64_t)rows * blocks * 2;
-    const int grid = mx_grid(n);
+    static std::atomic<int> resident[2];
+    const int grid = type == NITRO_BF16 ? one_wave(k_mx4_dequantize<uint16_t>, resident[0], n)
+                                        : one_wave(k_mx4_dequantize<float>, resident[1], n);
     const int size = type == NITRO_BF16 ? 2 : 4;
     const int vec = ((uintptr_t)out & 15) == 0 && ldo * size % 16 == 0;
     ProfScope ps(K_MX4_DEQUANTIZE, s, 0.0, (double)rows * cols * (size + 17.0 / 32.0));

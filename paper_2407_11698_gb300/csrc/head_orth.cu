@@ -754,14 +754,16 @@ nitro_status orth_first(nitro_orth* h, const T* m, int64_t ld, int64_t stride, i
     const int64_t n = (int64_t)h->rows * h->cols;
     constexpr int E = Vec16<T>::E;
     const int vec = ((uintptr_t)m & 15) == 0 && ld % E == 0 && (count == 1 || stride % E == 0);
-    const int most = 8 * sm_count() / count + 1;
-    const int parts = (int)std::min<int64_t>(std::min(kNormCtas, most), (n / E + 255) / 256 + 1);
+    static std::atomic<int> resident[2];
+    const int64_t items = h->rows * (h->x[0].ld / E);
+    // one wave for all matrices together
+    const auto share = [count](int grid) { return std::max(1, grid / count); };
+    const int parts = std::min(kNormCtas, share(one_wave(k_orth_norm<T>, resident[0], (items + 3) / 4 * count)));
     {
         ProfScope ps(K_ORTH_PACK, s, 0.0, (double)sizeof(T) * n * count);
         TRY(launch_k(k_orth_norm<T>, dim3(parts, count), dim3(256), 0, s, m, ld, stride, h->rows, h->cols, h->part, vec));
     }
-    const int64_t items = h->rows * (h->x[0].ld / E);
-    const int grid = (int)std::min<int64_t>((items + 255) / 256, most);
+    const int grid = share(one_wave(k_orth_pack<T>, resident[1], (items + 3) / 4 * count));
     ProfScope ps(K_ORTH_PACK, s, 0.0, (double)(sizeof(T) + (low ? 4 : 2)) * n * count);
     TRY(launch_k(k_orth_pack<T>, dim3(grid, count), dim3(256), 0, s, m, ld, stride, h->rows, h->cols, (const float*)h->part,
                  parts, mul, h->x[0], low ? 1 : 0, vec, h->scale));

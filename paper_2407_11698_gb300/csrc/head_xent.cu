@@ -470,8 +470,9 @@ bool tma_rows(const void* p, int64_t ld) { return ((uintptr_t)p & 15) == 0 && ld
 
 cudaError_t pack_rows(const void* x, int type, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
                       const PackGrad& pg, cudaStream_t s, uint16_t* plain = nullptr) {
+    static std::atomic<int> resident[2];
     const int64_t words = rows * (ldp / 8);
-    const int grid = (int)std::min<int64_t>((words + 255) / 256, (int64_t)sm_count() * 8);
+    const int grid = type == NITRO_I8 ? one_wave(k_xent_pack<int8_t>, resident[0], words) : one_wave(k_xent_pack<uint16_t>, resident[1], words);
     ProfScope ps(K_XENT_PACK, s, 0.0, (double)rows * cols * (type == NITRO_I8 ? 3 : 4));
     if (type == NITRO_I8)
         return launch_k(k_xent_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp, pg,

@@ -184,6 +184,15 @@ struct RowWalk {
     int64_t row, drow;
     int part, dpart, per;
     __device__ __forceinline__ RowWalk(int64_t first, int64_t step, int per_) : per(per_) {
+        if (((first | step) >> 31) == 0) {     // a 64-bit division is some hundred instructions
+            const uint32_t p = (uint32_t)per, f = (uint32_t)first, s = (uint32_t)step;
+            const uint32_t r = f / p, d = s / p;
+            row = r;
+            part = (int)(f - r * p);
+            drow = d;
+            dpart = (int)(s - d * p);
+            return;
+        }
         row = first / per;
         part = (int)(first - row * per);
         drow = step / per;

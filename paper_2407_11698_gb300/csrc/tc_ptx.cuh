@@ -242,5 +242,22 @@ inline int sm_count(int* device = nullptr) {
     return n;
 }
 
+// CTAs of 256 threads for `items` of a grid-stride kernel, one a thread, and no more than the
+// SMs hold at once by their registers (a second wave of a third of the CTAs costs as much as
+// the first).  resident: the kernel's CTAs an SM, looked up once.
+template <typename K>
+inline int one_wave(K* kernel, std::atomic<int>& resident, int64_t items) {
+    int r = resident.load(std::memory_order_relaxed);
+    if (r == 0) {
+        cudaFuncAttributes fa{};
+        const bool ok = cudaFuncGetAttributes(&fa, kernel) == cudaSuccess && fa.numRegs > 0;
+        const int per = ok ? 65536 / (256 * ((fa.numRegs + 7) / 8 * 8)) : 4;
+        r = per < 1 ? 1 : per > 8 ? 8 : per;
+        resident.store(r, std::memory_order_relaxed);
+    }
+    const int64_t want = (items + 255) / 256, most = (int64_t)sm_count() * r;
+    return (int)(want < most ? want : most);
+}
+
 }  // namespace
 }  // namespace nitro
