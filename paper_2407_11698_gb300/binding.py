@@ -518,23 +518,29 @@ def _code(t):
 
 def _matrix(t, rows, cols, allowed, what):
     """(address, type, row stride) of a CUDA matrix [rows x cols] whose rows are contiguous."""
-    if not t.is_cuda or t.shape != (rows, cols):
-        raise ValueError("%s must be a CUDA tensor [%d x %d]" % (what, rows, cols))
+    code = _codes.get(t.dtype) if _codes else _code(t)
+    if code not in allowed or not t.is_cuda or t.shape != (rows, cols):
+        raise ValueError("%s must be a CUDA tensor [%d x %d] of a supported type, not %s %s on %s"
+                         % (what, rows, cols, tuple(t.shape), t.dtype, t.device))
     ld, step = t.stride()
     if step != 1 and cols > 1:
         raise ValueError("the rows of %s must be contiguous" % what)
-    code = _code(t)
-    if code not in allowed:
-        raise ValueError("%s cannot be of type %s" % (what, t.dtype))
     # the stride of a lone row is never used
     return t.data_ptr(), code, max(ld, cols) if rows <= 1 else ld
 
 
 def _vector(t, n, code, what):
-    if not t.is_cuda or _code(t) != code or t.numel() != n or not t.is_contiguous():
-        raise ValueError("%s must be a contiguous CUDA tensor of %d values of its type (not %s)"
-                         % (what, n, t.dtype))
+    if (_codes.get(t.dtype) if _codes else _code(t)) != code or not t.is_cuda or t.numel() != n or not t.is_contiguous():
+        raise ValueError("%s must be a contiguous CUDA tensor of %d values of its type, not %s %s on %s"
+                         % (what, n, tuple(t.shape), t.dtype, t.device))
     return t.data_ptr()
+
+
+def _stream_int(stream):
+    """A stream's handle as a number, which ctypes takes for a pointer."""
+    if stream is None:
+        return _current_stream()
+    return stream.cuda_stream if hasattr(stream, "cuda_stream") else int(stream)
 
 
 _X, _W, _ORTH = (NITRO_BF16, NITRO_I8), (NITRO_BF16,), (NITRO_BF16, NITRO_F32, NITRO_I64)
@@ -587,7 +593,7 @@ class SoftmaxXent(_Handle):
         """Writes the rows' losses and log-sums (fp32 [rows]); returns loss."""
         n, a = self._inputs(x, w, labels)
         st = lib().nitro_xent_forward(self.h, *a, scale, _vector(loss, n, NITRO_F32, "loss"),
-                                      _vector(lse, n, NITRO_F32, "lse"), _stream_ptr(stream))
+                                      _vector(lse, n, NITRO_F32, "lse"), _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_xent_forward")
         return loss
@@ -605,7 +611,7 @@ class SoftmaxXent(_Handle):
             dwp, _, lddw = _matrix(dw, self.classes, self.features, _W, "dw")
         st = lib().nitro_xent_backward(self.h, *a, scale, _vector(lse, n, NITRO_F32, "lse"),
                                        None if gout is None else _vector(gout, n, NITRO_F32, "gout"),
-                                       dxp, lddx, dwp, lddw, _stream_ptr(stream))
+                                       dxp, lddx, dwp, lddw, _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_xent_backward")
         return dx, dw
@@ -633,7 +639,7 @@ class Orthogonalizer(_Handle):
             _, ot, ldo = _matrix(b[0], self.rows, self.cols, _W, "out")
         k = None if coef is None else (ctypes.c_float * 3)(*coef)
         st = lib().nitro_orth_run(self.h, a.data_ptr(), mt, ldm, a.stride(0), n, steps, k, b.data_ptr(), ldo,
-                                  b.stride(0), _stream_ptr(stream))
+                                  b.stride(0), _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_orth_run")
         return out
@@ -655,7 +661,7 @@ def mx4_quantize(x, codes, scales, stream=None):
     rows, cols = x.shape
     xp, t, ld = _matrix(x, rows, cols, _MX4, "x")
     q, s = _mx4_buffers(codes, scales, rows, cols)
-    st = lib().nitro_mx4_quantize(xp, t, ld, rows, cols, q, s, _stream_ptr(stream))
+    st = lib().nitro_mx4_quantize(xp, t, ld, rows, cols, q, s, _stream_int(stream))
     if st != NITRO_OK:
         raise NitroError(st, "nitro_mx4_quantize")
     return codes, scales
@@ -667,7 +673,7 @@ def mx4_dequantize(codes, scales, out, scale_values=None, stream=None):
     op, t, ld = _matrix(out, rows, cols, _MX4, "out")
     q, s = _mx4_buffers(codes, scales, rows, cols)
     sv = None if scale_values is None else _vector(scale_values, rows * -(-cols // 32), NITRO_F32, "scale_values")
-    st = lib().nitro_mx4_dequantize(q, s, rows, cols, op, t, ld, sv, _stream_ptr(stream))
+    st = lib().nitro_mx4_dequantize(q, s, rows, cols, op, t, ld, sv, _stream_int(stream))
     if st != NITRO_OK:
         raise NitroError(st, "nitro_mx4_dequantize")
     return out
@@ -686,7 +692,7 @@ class Mx4Linear(_Handle):
         xp, xt, ldx = _matrix(x, n, self.in_features, _MX4, "x")
         yp, yt, ldy = _matrix(y, n, self.out_features, _MX4, "y")
         q, s = _mx4_buffers(codes, scales, self.out_features, self.in_features)
-        st = lib().nitro_mx4_linear(self.h, xp, xt, ldx, n, q, s, yp, yt, ldy, _stream_ptr(stream))
+        st = lib().nitro_mx4_linear(self.h, xp, xt, ldx, n, q, s, yp, yt, ldy, _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_mx4_linear")
         return y
