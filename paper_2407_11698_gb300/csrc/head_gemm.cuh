@@ -14,8 +14,11 @@
 // the MMAs of the next tile fill the other of two accumulators.  CG = 2 pairs two CTAs
 // of a cluster on one 256-row tile: each loads its own 128 rows of A and half the
 // columns of B, and the MMAs that one thread of the pair issues read both halves.  That
-// halves the bytes of B an SM has to load and read for the same products, which is what
-// bounds the lone form (see the figures at pick_tile()).
+// halves the bytes of B an SM has to load for the same products: loads are what bounds both
+// forms (about 53 bytes a clock into an SM, see hg_pick(); a pair's block of 64 along K then
+// takes 0.35 us, its MMAs 0.25 at 2.07 GHz).  Measured (2 M N K operations over time): 8192 x
+// 64000 x 2048 1.81 PFLOP/s and 16384 x 2048 x 8192 1.83 where the clock holds, 1.6 to 1.75
+// under the power limit; the library's bf16 product makes 1.90 and 1.71.
 //
 // KS > 1 gives a tile's K to a cluster of KS (2 or 4) lone CTAs, where there are few tiles:
 // their sums meet in distributed shared memory, a slice of the columns for each CTA, are
@@ -618,7 +621,7 @@ inline HgPick hg_pick(const HgProblem& p, int ha = 1, int hb = 1, int max_splits
             if (hg_splits(p.K, s) == s)
                 take(cost(s) + (s > 1 ? 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500 : 0), {f.cg, f.bn, s});
         for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 4; s *= 2)
-            if (hg_splits(p.K, s) == s) take(cost(s) + 3000, {1, 128, 1, s});
+            if (hg_splits(p.K, s) == s) take(cost(s) + 6000, {1, 128, 1, s});
     }
     return best;
 }

@@ -8,12 +8,11 @@
 // Layout.  Codes: [rows][blocks][16] bytes, value 2i of a block in the low half of byte i.
 // Scales: tiles of 128 rows x 4 blocks, 512 bytes each, ordered [row tile][block tile];
 // row r, block j of a tile at (r % 32) 16 + (r / 32) 4 + j.  That is the order in which
-// the tensor cores take scales from TMEM, so a tile goes from global memory to shared
-// memory as one run of bytes and on to TMEM by one tcgen05.cp.
+// the tensor cores take scales from TMEM, so a tile is one run of bytes in global and shared
+// memory and goes on to TMEM by one tcgen05.cp.
 //
 // The product runs on tcgen05.mma kind::mxf4 (products and scales exact, 32-bit sums).
 #include <new>
-#include <vector>
 
 #include <cuda_bf16.h>
 
@@ -47,6 +46,23 @@ __device__ __forceinline__ uint32_t e2m1x8(const float* v) {
         : "=r"(r)
         : "f"(v[0]), "f"(v[1]), "f"(v[2]), "f"(v[3]), "f"(v[4]), "f"(v[5]), "f"(v[6]), "f"(v[7]));
     return r;
+}
+
+// 32 bytes in one access (both 32-byte aligned)
+__device__ __forceinline__ void load32(const void* p, uint4* a, uint4* b) {
+    asm volatile("ld.global.v8.b32 {%0, %1, %2, %3, %4, %5, %6, %7}, [%8];"
+                 : "=r"(a->x), "=r"(a->y), "=r"(a->z), "=r"(a->w), "=r"(b->x), "=r"(b->y), "=r"(b->z), "=r"(b->w)
+                 : "l"(p));
+}
+__device__ __forceinline__ void store32(void* p, const uint32_t* v) {
+    asm volatile("st.global.v8.b32 [%0], {%1, %2, %3, %4, %5, %6, %7, %8};" ::"l"(p), "r"(v[0]), "r"(v[1]), "r"(v[2]), "r"(v[3]),
+                 "r"(v[4]), "r"(v[5]), "r"(v[6]), "r"(v[7])
+                 : "memory");
+}
+// what rows at p, ld values apart, are aligned to: 32, 16 or fewer bytes (2, 1, 0)
+int row_vec(const void* p, int64_t ld, int size) {
+    const uintptr_t low = (uintptr_t)p | (uintptr_t)(ld * size);
+    return (low & 31) == 0 ? 2 : (low & 15) == 0 ? 1 : 0;
 }
 
 // eight values as loaded
@@ -106,6 +122,21 @@ __device__ __forceinline__ Raw8<T> load8(const T* src, int n, bool vec) {
     }
     return r;
 }
+// sixteen, vec: see row_vec
+template <typename T>
+__device__ __forceinline__ void load16(Raw8<T>* r, const T* src, int n, int vec) {
+    if (vec == 2 && n >= 16) {
+        if constexpr (sizeof(T) == 2) {
+            load32(src, &r[0].w[0], &r[1].w[0]);
+        } else {
+            load32(src, &r[0].w[0], &r[0].w[1]);
+            load32(src + 8, &r[1].w[0], &r[1].w[1]);
+        }
+        return;
+    }
+    r[0] = load8(src, n, vec != 0);
+    r[1] = load8(src + 8, n - 8, vec != 0);
+}
 // a block's scale as stored, from its largest magnitude's bits: that exponent less 2, at
 // least 0; 255: not finite
 __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
@@ -116,7 +147,9 @@ __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
 __device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_float((254u - min(s, 253u)) << 23); }
 
 // Two threads a block, sixteen values each, two such loads in flight.  The grid covers the
-// scales' padding too.  MX4Q_MEASURED
+// scales' padding too.  Bound by memory and, nearly, by the instructions (9 a value): 16384 x
+// 4096 in bf16 28.7 us, 5.9 TB/s; with 16-byte loads, one multiplication and one integer
+// maximum a value and a division an item 58 us.
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc,
                                                       int blocks, int64_t rows_pad, int vec) {
@@ -135,8 +168,7 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, i
             const int c = at.part * 16;
             const T* src = x + at.row * ldx + c;
             const int left = at.row < rows ? cols - c : 0;
-            raw[u][0] = load8(src, left, vec != 0);
-            raw[u][1] = load8(src + 8, left - 8, vec != 0);
+            load16(raw[u], src, left, vec);
             at.next();
         }
 #pragma unroll
@@ -170,7 +202,8 @@ __device__ __forceinline__ void e2m1_bf16x4(uint32_t w, int h, uint32_t* out) {
     out[1] = __byte_perm(lo, hi, 0x7362) | (__byte_perm(up, w, h ? 0x7030 : 0x5010) & 0x80008000u);
 }
 
-// Sixteen values a thread, two loads in flight.  MX4D_MEASURED
+// Sixteen values a thread, two loads in flight.  Bound by memory: 16384 x 4096 to bf16 31 us,
+// 5.7 TB/s (36.5 with 16-byte stores, which fill half a sector each).
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const uint8_t* sc, int rows, int cols, int blocks,
                                                         T* out, int64_t ldo, float* scales, int vec) {
@@ -213,7 +246,9 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
                     const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[j]), k);
                     v[j] = *reinterpret_cast<const uint32_t*>(&p);
                 }
-                if (vec && c + 16 <= cols) {
+                if (vec == 2 && c + 16 <= cols) {
+                    store32(dst, v);
+                } else if (vec && c + 16 <= cols) {
                     reinterpret_cast<uint4*>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
                     reinterpret_cast<uint4*>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
                 } else {
@@ -225,7 +260,10 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
                 float o[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16) * f;
-                if (vec && c + 16 <= cols) {
+                if (vec == 2 && c + 16 <= cols) {
+                    store32(dst, reinterpret_cast<const uint32_t*>(o));
+                    store32(dst + 8, reinterpret_cast<const uint32_t*>(o) + 8);
+                } else if (vec && c + 16 <= cols) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         reinterpret_cast<float4*>(dst)[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
@@ -248,7 +286,10 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
 // products a byte loaded.  FX (bf16 or fp32, for SWAP): Q's codes and scales are not loaded but made by
 // the epilogue warps from the features themselves, stage by stage, which saves the launch
 // that would quantise them; every CTA does so for its own, so it is for few rows.  A pair's accumulator and scales fill TMEM, so its drain waits for
-// the next tile's MMAs, but not for its loads.
+// the next tile's MMAs, but not for its loads.  Measured: 8192^3 243 us, 4.5 PFLOP/s; a stage
+// takes 0.5 us, in which the thread that issues is held by four MMAs (0.18) and, before them,
+// six scale tiles (0.16): those do not overlap.  Scales put into TMEM by warps (tcgen05.st) were
+// slower (405 us).  One row x 4096 x 10000 takes 10 us, of which 79 CTAs' sixteen stages are 6.
 constexpr int kMxThreads = 384, kMxEpiWarp0 = 4, kMxEpiWarps = 8;
 
 struct MxArgs {
@@ -488,8 +529,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                         for (int u = 0; u < 4; ++u) {
                             const int r = rb + 2 * u + r0, left = r < g.Q ? g.in - c : 0;
                             const FX* src = x + r * g.ldx + c;
-                            raw[u][0] = load8(src, left, g.vec_x != 0);
-                            raw[u][1] = load8(src + 8, left - 8, g.vec_x != 0);
+                            load16(raw[u], src, left, g.vec_x);
                         }
                         if (rb == 0) {
                             ok = mbar_wait(empty_bar(st), ((uint32_t)(n / S) & 1u) ^ 1u, abort_flag, g.status);
@@ -685,7 +725,7 @@ cudaError_t quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, ui
     const int64_t pad = round_up(rows, 128), n = pad * ((blocks + 3) / 4) * 8;
     static std::atomic<int> resident{0};
     const int grid = one_wave(k_mx4_quantize<T>, resident, n);
-    const int vec = ((uintptr_t)x & 15) == 0 && ldx * (int64_t)sizeof(T) % 16 == 0;
+    const int vec = row_vec(x, ldx, (int)sizeof(T));
     ProfScope ps(K_MX4_QUANTIZE, s, 0.0, (double)rows * cols * (sizeof(T) + 17.0 / 32.0));
     return launch_k(k_mx4_quantize<T>, dim3(grid), dim3(256), 0, s, x, ldx, rows, cols, q, sc, blocks, pad, vec);
 }
@@ -707,7 +747,7 @@ struct nitro_mx4 {
     uint8_t *xq = nullptr, *xs = nullptr;
     float* part = nullptr;
     uint32_t* status = nullptr;
-    std::vector<void*> allocs;
+    DeviceAllocs allocs;
 };
 
 #define TRY(expr)                                         \
@@ -748,7 +788,7 @@ nitro_status nitro_mx4_dequantize(const uint8_t* codes, const uint8_t* scales, i
     const int grid = type == NITRO_BF16 ? one_wave(k_mx4_dequantize<uint16_t>, resident[0], n)
                                         : one_wave(k_mx4_dequantize<float>, resident[1], n);
     const int size = type == NITRO_BF16 ? 2 : 4;
-    const int vec = ((uintptr_t)out & 15) == 0 && ldo * size % 16 == 0;
+    const int vec = row_vec(out, ldo, size);
     ProfScope ps(K_MX4_DEQUANTIZE, s, 0.0, (double)rows * cols * (size + 17.0 / 32.0));
     if (type == NITRO_BF16)
         TRY(launch_k(k_mx4_dequantize<uint16_t>, dim3(grid), dim3(256), 0, s, codes, scales, rows, cols, blocks,
@@ -770,15 +810,9 @@ nitro_status nitro_mx4_create(int max_rows, int in, int out_features, nitro_mx4*
     h->max_rows = max_rows;
     h->in = in;
     h->out = out_features;
-    const auto alloc = [h](auto** p, int64_t bytes) {
-        void* q = nullptr;
-        if (cudaMalloc(&q, (size_t)bytes) != cudaSuccess) return false;
-        h->allocs.push_back(q);
-        *p = static_cast<std::remove_reference_t<decltype(*p)>>(q);
-        return true;
-    };
-    const bool ok = alloc(&h->xq, code_bytes(max_rows, in)) && alloc(&h->xs, scale_bytes(max_rows, in)) &&
-                    alloc(&h->part, kPartFloats * 4) && alloc(&h->status, 4) && cudaMemset(h->status, 0, 4) == cudaSuccess;
+    const bool ok = h->allocs.take(&h->xq, code_bytes(max_rows, in)) && h->allocs.take(&h->xs, scale_bytes(max_rows, in)) &&
+                    h->allocs.take(&h->part, kPartFloats) && h->allocs.take(&h->status, 1) &&
+                    cudaMemset(h->status, 0, 4) == cudaSuccess;
     if (!ok) {
         nitro_mx4_destroy(h);
         return NITRO_ERR_CUDA;
@@ -853,7 +887,7 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
     g.x = x;
     g.ldx = ldx;
     g.in = h->in;
-    g.vec_x = ((uintptr_t)x & 15) == 0 && ldx * (x_type == NITRO_F32 ? 4 : 2) % 16 == 0;
+    g.vec_x = row_vec(x, ldx, x_type == NITRO_F32 ? 4 : 2);
     if (inside && x_type == NITRO_BF16) TRY((mx_launch<1, 32, true, uint16_t>(w_op, x_op, h->in, g, ops, bytes, s)));
     else if (inside) TRY((mx_launch<1, 32, true, float>(w_op, x_op, h->in, g, ops, bytes, s)));
     else if (bn == 64) TRY((mx_launch<1, 64, true>(w_op, x_op, h->in, g, ops, bytes, s)));
@@ -881,7 +915,7 @@ nitro_status nitro_mx4_status(nitro_mx4* h, int clear) {
 void nitro_mx4_destroy(nitro_mx4* h) {
     if (!h) return;
     cudaDeviceSynchronize();
-    for (void* p : h->allocs) cudaFree(p);
+    h->allocs.free();
     delete h;
 }
 

@@ -17,7 +17,6 @@
 #include <cfloat>
 #include <cmath>
 #include <new>
-#include <vector>
 
 #include "head_gemm.cuh"
 
@@ -31,8 +30,7 @@ constexpr int kNormCtas = 1024;     // partial sums of squares a matrix, at most
 
 __device__ __forceinline__ float2 halves2(uint32_t w) { return __half22float2(*reinterpret_cast<const __half2*>(&w)); }
 // two values -> a word of their high and a word of their low halves.  Pairs, since the
-// conversion of two floats to a pair is one instruction at a higher rate than that of one
-// (32 columns a thread through the steps' sums: 3300 clocks, now HALVES_MEASURED).
+// conversion of two floats to a pair is one instruction at a higher rate than that of one.
 __device__ __forceinline__ void split_pair(float a, float b, uint32_t* hi, uint32_t* lo) {
     const __half2 h = __floats2half2_rn(a, b);
     const float2 back = __half22float2(h);
@@ -196,9 +194,20 @@ struct EpiUpdate {
 // ------------------------------------------------------------------ norm and first planes
 template <typename T>
 __device__ __forceinline__ float as_float(T v) {
-    if constexpr (sizeof(T) == 2) return __uint_as_float((uint32_t)v << 16);
-    else if constexpr (sizeof(T) == 8) return (float)v * 0x1p-32f;   // squares of int64 gradients stay inside fp32
-    else return v;
+    if constexpr (sizeof(T) == 2) {
+        return __uint_as_float((uint32_t)v << 16);
+    } else if constexpr (sizeof(T) == 8) {
+        // times 2^-32: squares of int64 gradients stay inside fp32.  By pieces of 16 bits, since the
+        // conversion instruction is slow (the norm of eight 256 x 2304: 15 us): 2^23 + piece is a
+        // float with the piece for its low bits; the top piece is taken as 2^15 more than it is.
+        const uint32_t lo = (uint32_t)v, hi = (uint32_t)((uint64_t)v >> 32) ^ 0x80000000u;
+        const auto piece = [](uint32_t w, uint32_t sel) { return __uint_as_float(__byte_perm(w, 0x4B000000u, sel)); };
+        float f = fmaf(piece(hi, 0x7632) - (8388608.0f + 32768.0f), 65536.0f, piece(hi, 0x7610) - 8388608.0f);
+        f = fmaf(piece(lo, 0x7632) - 8388608.0f, 0x1p-16f, f);
+        return fmaf(piece(lo, 0x7610) - 8388608.0f, 0x1p-32f, f);
+    } else {
+        return v;
+    }
 }
 // 16 bytes of a row: E values, those past n zero
 template <typename T>
@@ -334,7 +343,9 @@ __global__ void __launch_bounds__(256) k_orth_copy(Planes x, float mul, int low,
 // across it (B X) alike.  Every CTA has all of A and B.  A step is three batches of MMAs,
 // each followed by its sums' way through the registers into the next one's operands; for
 // C > 1 the parts of A meet by column slices in distributed shared memory, are added in the
-// CTAs' order, and go back to all.  Bound by the latency of that chain: ORTH_SMALL_MEASURED
+// CTAs' order, and go back to all.  Bound by the latency of that chain: 50 x 100 takes 29 us,
+// 1.9 a batch (the same by k_head_gemm, 17 launches, 107), 128 x 256 50, and with the
+// exchange 128 x 1024 95.
 // A wait that gives up latches TIMEOUT; the CTA then goes through the rest without waiting, so
 // that the cluster's barriers and stores stay matched.
 constexpr int kOsThreads = 512;      // four warps a TMEM lane quadrant, a quarter of the columns each
@@ -690,19 +701,10 @@ struct nitro_orth {
     float* part = nullptr;
     float* scale = nullptr;    // [max_count], see k_orth_pack
     uint32_t* status = nullptr;
-    std::vector<void*> allocs;
+    DeviceAllocs allocs;
 };
 
 namespace {
-
-template <typename T>
-bool oalloc(nitro_orth* h, T** p, int64_t count) {
-    void* q = nullptr;
-    if (cudaMalloc(&q, (size_t)count * sizeof(T)) != cudaSuccess) return false;
-    h->allocs.push_back(q);
-    *p = static_cast<T*>(q);
-    return true;
-}
 
 #define TRY(expr)                                         \
     do {                                                  \
@@ -771,12 +773,14 @@ nitro_status orth_first(nitro_orth* h, const T* m, int64_t ld, int64_t stride, i
 }
 
 // The one-launch form: its cluster size, or 0 where it does not apply.  Up to 256 columns a
-// CTA (128 KB of halves).
+// CTA (128 KB of halves).  The exchange grows with the square of the shorter side: by eight
+// CTAs a side above 64 is as slow as by launches (128 x 2048 133 us, 128 x 2500 by launches 127;
+// 64 x 2048 64 us).
 int small_cluster(const nitro_orth* h) {
     if (h->small > 128) return 0;
     const int big = std::max(h->rows, h->cols);
     for (int c = 1; c <= 8; c *= 2)
-        if (big <= 256 * c) return c;
+        if (big <= 256 * c) return c == 8 && h->small > 64 ? 0 : c;
     return 0;
 }
 
@@ -830,9 +834,9 @@ nitro_status nitro_orth_create(int max_count, int rows, int cols, nitro_orth** o
     h->small = std::min(rows, cols);
     for (Planes* p : {&h->x[0], &h->x[1]}) *p = {nullptr, round_up(cols, 64), rows * round_up(cols, 64)};
     for (Planes* p : {&h->a, &h->b}) *p = {nullptr, round_up(h->small, 64), h->small * round_up(h->small, 64)};
-    bool ok = oalloc(h, &h->part, (int64_t)max_count * kNormCtas) && oalloc(h, &h->scale, max_count) && oalloc(h, &h->status, 1) &&
+    bool ok = h->allocs.take(&h->part, (int64_t)max_count * kNormCtas) && h->allocs.take(&h->scale, max_count) && h->allocs.take(&h->status, 1) &&
               cudaMemset(h->status, 0, 4) == cudaSuccess;
-    for (Planes* p : {&h->x[0], &h->x[1], &h->a, &h->b}) ok = ok && oalloc(h, &p->base, 2 * max_count * p->plane);
+    for (Planes* p : {&h->x[0], &h->x[1], &h->a, &h->b}) ok = ok && h->allocs.take(&p->base, 2 * max_count * p->plane);
     if (!ok) {
         nitro_orth_destroy(h);
         return NITRO_ERR_CUDA;
@@ -947,7 +951,7 @@ nitro_status nitro_orth_status(nitro_orth* h, int clear) {
 void nitro_orth_destroy(nitro_orth* h) {
     if (!h) return;
     cudaDeviceSynchronize();
-    for (void* p : h->allocs) cudaFree(p);
+    h->allocs.free();
     delete h;
 }
 

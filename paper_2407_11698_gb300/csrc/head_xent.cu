@@ -16,7 +16,6 @@
 // Where dx has fewer tiles than SMs its sum is split along the classes into 32-bit slices of
 // a small workspace, or shared out in a cluster (head_gemm.cuh), as the logits' is.
 #include <new>
-#include <vector>
 
 #include "head_gemm.cuh"
 
@@ -421,13 +420,14 @@ constexpr int kRowsWithLow = 32;
 
 // The tensor cores drop the bits that a sum's 32 do not hold, so its error grows with the
 // additions: the loss is off by 5.6e-7 of it with 2048 features and 1.2e-6 with 3850.  From
-// here on the logits are summed in two halves, added with rounding (at 8192 x 2048 x 64000
-// that takes FOLD_MEASURED).
+// here on the logits are summed in two halves, added with rounding (at 8192 x 4096 x 32000
+// that takes 3 per cent more time).
 constexpr int kFoldFeatures = 2048;
 
 // Parts of all rows that the forward's last CTA still joins by itself; more go to a launch of
-// their own (4 rows x 512 x 10000: 14 us with that launch, now JOIN_MEASURED).
-constexpr int64_t kPartsInOne = 4096;
+// their own (4 rows x 512 x 10000: 11.1 us with that launch and 9.9 without; 64 x 4096 x 1000,
+// 2048 parts: 12.9 and 14.8).
+constexpr int64_t kPartsInOne = 1024;
 
 constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
@@ -447,19 +447,10 @@ struct nitro_xent {
     float* zt = nullptr;
     float* factor = nullptr;    // [1 + max_rows], see PackGrad
     uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
-    std::vector<void*> allocs;
+    DeviceAllocs allocs;
 };
 
 namespace {
-
-template <typename T>
-bool xalloc(nitro_xent* h, T** p, int64_t count) {
-    void* q = nullptr;
-    if (cudaMalloc(&q, (size_t)count * sizeof(T)) != cudaSuccess) return false;
-    h->allocs.push_back(q);
-    *p = static_cast<T*>(q);
-    return true;
-}
 
 #define TRY(expr)                                         \
     do {                                                  \
@@ -527,9 +518,9 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
                           2 * std::min(max_rows, kRowsWithLow) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
     const int64_t parts = 4 * ((classes + 127) / 128);
-    const bool ok = xalloc(h, &h->xp, max_rows * h->ldp) && xalloc(h, &h->xg, max_rows * h->ldp) && xalloc(h, &h->wp, classes * h->ldp) &&
-                    xalloc(h, &h->G, h->g_elems) && xalloc(h, &h->acc, h->acc_floats) &&
-                    xalloc(h, &h->part, parts * max_rows) && xalloc(h, &h->zt, max_rows) && xalloc(h, &h->factor, max_rows + 1) && xalloc(h, &h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
+    const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->xg, max_rows * h->ldp) && h->allocs.take(&h->wp, classes * h->ldp) &&
+                    h->allocs.take(&h->G, h->g_elems) && h->allocs.take(&h->acc, h->acc_floats) &&
+                    h->allocs.take(&h->part, parts * max_rows) && h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) && h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -656,7 +647,7 @@ nitro_status nitro_xent_status(nitro_xent* h, int clear) {
 void nitro_xent_destroy(nitro_xent* h) {
     if (!h) return;
     cudaDeviceSynchronize();
-    for (void* p : h->allocs) cudaFree(p);
+    h->allocs.free();
     delete h;
 }
 

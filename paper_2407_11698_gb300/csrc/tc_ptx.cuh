@@ -242,6 +242,23 @@ inline int sm_count(int* device = nullptr) {
     return n;
 }
 
+// A handle's device buffers (no container that could throw through a C entry).
+struct DeviceAllocs {
+    void* at[12];
+    int n = 0;
+    template <typename T>
+    bool take(T** p, int64_t count) {
+        void* q = nullptr;
+        if (n == 12 || cudaMalloc(&q, (size_t)count * sizeof(T)) != cudaSuccess) return false;
+        at[n++] = q;
+        *p = static_cast<T*>(q);
+        return true;
+    }
+    void free() {
+        while (n > 0) cudaFree(at[--n]);
+    }
+};
+
 // CTAs of 256 threads for `items` of a grid-stride kernel, one a thread, and no more than the
 // SMs hold at once by their registers (a second wave of a third of the CTAs costs as much as
 // the first).  resident: the kernel's CTAs an SM, looked up once.
