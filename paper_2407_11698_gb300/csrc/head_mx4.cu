@@ -286,11 +286,16 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
 // products a byte loaded.  FX (bf16 or fp32, for SWAP): Q's codes and scales are not loaded but made by
 // the epilogue warps from the features themselves, stage by stage, which saves the launch
 // that would quantise them; every CTA does so for its own, so it is for few rows.  A pair's accumulator and scales fill TMEM, so its drain waits for
-// the next tile's MMAs, but not for its loads.  Measured: 8192^3 243 us, 4.5 PFLOP/s; a stage
-// takes 0.5 us, in which the thread that issues is held by four MMAs (0.18) and, before them,
-// six scale tiles (0.16): those do not overlap.  Scales put into TMEM by warps (tcgen05.st) were
-// slower (405 us).  One row x 4096 x 10000 takes 10 us, of which 79 CTAs' sixteen stages are 6.
+// the next tile's MMAs, but not for its loads.
+//
+// Scales go from shared memory to TMEM by tcgen05.cp, 34 ns a tile of 512 bytes, which hold the
+// thread that issues them; with six of them before a stage's four MMAs (45 ns each) in one thread a
+// stage took 0.5 us (8192^3: 243 us).  So a thread of its own issues them, up to four stages ahead.
+// Measured: 8192^3 204 us, 5.4 PFLOP/s, 0.41 us a stage of 35 KB a CTA, bound by its loads; one
+// row x 4096 x 10000 10 us, of which 79 CTAs' sixteen stages are 6.  (Scales put into TMEM by
+// warps, tcgen05.st: 405 us.)
 constexpr int kMxThreads = 384, kMxEpiWarp0 = 4, kMxEpiWarps = 8;
+constexpr int kMxScaleBufs = 4;      // stages whose scales are in TMEM
 
 struct MxArgs {
     int P, Q;                // valid rows
@@ -321,8 +326,10 @@ struct MxCfg {
     static constexpr int S = BN >= 128 ? 6 : 8;
     static constexpr int SMEM = S * STAGE + kMxEpiWarps * 2048 + 256;
     static constexpr int NBUF = CG == 2 ? 1 : 2;               // accumulators
-    static constexpr int SF = NBUF * BN, SF_COLS = 8 + 8 * QT; // TMEM columns of a stage's scales, for two stages
-    static constexpr int TCOLS = SF + 2 * SF_COLS <= 128 ? 128 : SF + 2 * SF_COLS <= 256 ? 256 : 512;
+    static constexpr int SF = NBUF * BN, SF_COLS = 8 + 8 * QT; // TMEM columns of a stage's scales
+    static constexpr int SF_END = SF + kMxScaleBufs * SF_COLS;
+    static constexpr int TCOLS = SF_END <= 128 ? 128 : SF_END <= 256 ? 256 : 512;
+    static_assert(SF_END <= 512, "TMEM");
 };
 
 template <int CG>
@@ -390,7 +397,8 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
     extern __shared__ __align__(1024) uint8_t smem[];
     // stages of operands (1024-byte aligned), the scales, the warps' own 2 KB
     uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S * C::STAGE + kMxEpiWarps * 2048);
-    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 5);
+    // barriers: full [S], empty [S], tmem full [2], empty [2], drain [2], scales in [4] and out of use [4]
+    uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 2 * S + 6 + 2 * kMxScaleBufs);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const uint32_t bar0 = smem_u32(bars), s0 = smem_u32(smem), sf0 = s0 + S * (C::P_BYTES + C::Q_BYTES);
@@ -398,7 +406,9 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
     const auto empty_bar = [&](int s) { return bar0 + 8u * (S + s); };
     const auto tfull_bar = [&](int b) { return bar0 + 8u * (2 * S + b); };
     const auto tempty_bar = [&](int b) { return bar0 + 8u * (2 * S + 2 + b); };
-    const uint32_t drain_bar = bar0 + 8u * (2 * S + 4);
+    const auto drain_bar = [&](int i) { return bar0 + 8u * (2 * S + 4 + i); };
+    const auto sin_bar = [&](int b) { return bar0 + 8u * (2 * S + 6 + b); };
+    const auto sout_bar = [&](int b) { return bar0 + 8u * (2 * S + 6 + kMxScaleBufs + b); };
     const int rank = CG == 2 ? (int)cluster_rank() : 0;
     const int unit = (int)blockIdx.x / CG, units = (int)gridDim.x / CG;
     if (threadIdx.x == 0) {
@@ -410,7 +420,12 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
             mbar_init(tfull_bar(b), 1);
             mbar_init(tempty_bar(b), CG * kMxEpiWarps);
         }
-        mbar_init(drain_bar, 1);
+        for (int b = 0; b < kMxScaleBufs; ++b) {
+            mbar_init(sin_bar(b), 1);
+            mbar_init(sout_bar(b), 1);
+        }
+        mbar_init(drain_bar(0), 1);
+        mbar_init(drain_bar(1), 1);
         *abort_flag = 0;
         asm volatile("fence.mbarrier_init.release.cluster;" ::: "memory");
     }
@@ -474,16 +489,13 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                 const uint32_t d = tmem + (uint32_t)(buf * BN);
                 bool ok = true;
                 for (int k = T.s0; k < T.s1; ++k, ++n) {
-                    if (!(ok = mbar_wait(full_bar(st), ph, abort_flag, g.status))) break;
+                    const int sbuf = n % kMxScaleBufs;
+                    ok = mbar_wait(full_bar(st), ph, abort_flag, g.status) &&
+                         mbar_wait(sin_bar(sbuf), (uint32_t)(n / kMxScaleBufs) & 1u, abort_flag, g.status);
+                    if (!ok) break;
                     tc_fence_after();
                     const int steps = min(4, g.k64 - 4 * k);
-                    const uint32_t sp = tmem + C::SF + C::SF_COLS * (n & 1), sq = sp + 8, ds = sf0 + st * C::SF_BYTES;
-#pragma unroll
-                    for (int j = 0; j < 2; ++j) {
-                        copy_scales<CG>(sp + 4 * j, ds + 512 * j);
-#pragma unroll
-                        for (int r = 0; r < C::QT; ++r) copy_scales<CG>(sq + 4 * (C::QT * j + r), ds + 1024 + 1024 * r + 512 * j);
-                    }
+                    const uint32_t sp = tmem + C::SF + C::SF_COLS * sbuf, sq = sp + 8;
                     const uint64_t so = (uint64_t)((uint32_t)(st * (C::P_BYTES + C::Q_BYTES)) >> 4);
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
@@ -491,6 +503,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                             mma_mxf4<CG>(d, dp0 + so + 2 * j, dq0 + so + 2 * j, mx_idesc(128 * CG, BN, j & 1), sp + 4u * (j >> 1),
                                          sq + 4u * C::QT * (j >> 1), (k > T.s0 || j > 0) ? 1u : 0u);
                     hg_commit<CG>(empty_bar(st));
+                    hg_commit<CG>(sout_bar(sbuf));
                     if (++st == S) {
                         st = 0;
                         ph ^= 1u;
@@ -500,10 +513,43 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                 hg_commit<CG>(tfull_bar(buf));
             }
             if (*abort_flag) {
-                hg_commit<CG>(drain_bar);
-                mbar_drain(drain_bar, 0, kDrainNs);
+                hg_commit<CG>(drain_bar(0));
+                mbar_drain(drain_bar(0), 0, kDrainNs);
             }
             pdl_trigger();
+        }
+    } else if (warp == 3) {
+        if (lane == 0 && rank == 0) {
+            // ---------------- scales to TMEM, ahead of the MMAs
+            int st = 0, n = 0;
+            uint32_t ph = 0;
+            bool ok = true;
+            for (int tile = unit; tile < g.total && ok; tile += units) {
+                const MxTile T = mx_decode(g, tile);
+                for (int k = T.s0; k < T.s1; ++k, ++n) {
+                    const int sbuf = n % kMxScaleBufs;
+                    ok = mbar_wait(full_bar(st), ph, abort_flag, g.status) &&
+                         mbar_wait(sout_bar(sbuf), ((uint32_t)(n / kMxScaleBufs) & 1u) ^ 1u, abort_flag, g.status);
+                    if (!ok) break;
+                    tc_fence_after();
+                    const uint32_t sp = tmem + C::SF + C::SF_COLS * sbuf, sq = sp + 8, ds = sf0 + st * C::SF_BYTES;
+#pragma unroll
+                    for (int j = 0; j < 2; ++j) {
+                        copy_scales<CG>(sp + 4 * j, ds + 512 * j);
+#pragma unroll
+                        for (int r = 0; r < C::QT; ++r) copy_scales<CG>(sq + 4 * (C::QT * j + r), ds + 1024 + 1024 * r + 512 * j);
+                    }
+                    hg_commit<CG>(sin_bar(sbuf));
+                    if (++st == S) {
+                        st = 0;
+                        ph ^= 1u;
+                    }
+                }
+            }
+            if (*abort_flag) {
+                hg_commit<CG>(drain_bar(1));
+                mbar_drain(drain_bar(1), 0, kDrainNs);
+            }
         }
     } else if (warp >= kMxEpiWarp0) {
         const int q = warp & 3, half = (warp - kMxEpiWarp0) >> 2;
