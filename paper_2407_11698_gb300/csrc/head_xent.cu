@@ -13,6 +13,8 @@
 // logit more in 32 bits (16-bit logits are off by 2^-9 of their size, far too much under
 // an exponential).
 //
+// A forward of a few rows, a server's, runs on the CUDA cores (k_xent_few).
+//
 // Where dx has fewer tiles than SMs its sum is split along the classes into 32-bit slices of
 // a small workspace, or shared out in a cluster (head_gemm.cuh), as the logits' is.
 #include <new>
@@ -43,14 +45,17 @@ struct RowOut {
     float* lse;
     uint32_t* status;
     int classes;
+    float k2;              // scale log2 e
 };
+// zt: the label's product.  The loss is small where the label's logit is the largest, so it is not taken from
+// lse, whose rounding (2.4e-7 at 7) would be all of it, but from the logit's distance to the maximum.
 __device__ __forceinline__ void write_row(const RowOut& o, int64_t row, float m2, float sum, float zt) {
-    const float lse = (m2 + log2f(sum)) * kLn2;
+    const float l2 = log2f(sum), lse = (m2 + l2) * kLn2;
     const int lab = o.labels[row];
     const bool live = lab >= 0 && lab < o.classes;
     if (!live && lab != -1) atomicOr(o.status, ST_BAD_LABEL);
     o.lse[row] = lse;
-    o.loss[row] = live ? lse - zt : 0.0f;
+    o.loss[row] = live ? (l2 - fmaf(zt, o.k2, -m2)) * kLn2 : 0.0f;
 }
 
 // (max, sum of 2^(t - max)) pairs into one.  A NaN among the logits is in a sum, not in a maximum.
@@ -63,13 +68,46 @@ struct MaxSum {
     }
 };
 
+// Every thread of every CTA, its parts and label logits written: the last CTA to come here joins the
+// rows' parts [parts][rows].  ticket: zero before and after; word: the CTA's own, in shared memory.
+template <int THREADS>
+__device__ __forceinline__ void join_as_last(const float2* part, int parts, int rows, const float* zt, uint32_t* ticket,
+                                             const RowOut& out, int* word) {
+    __threadfence();
+    __syncthreads();
+    if (threadIdx.x == 0) *word = atomicAdd(ticket, 1u) == gridDim.x - 1;
+    __syncthreads();
+    if (!*word) return;
+    __threadfence();
+    if (threadIdx.x == 0) *ticket = 0;
+    // 8 or 32 lanes a row, so that the rows' loads are under way together
+    const int width = rows >= THREADS / 8 ? 8 : 32, sub = threadIdx.x & (width - 1);
+    for (int r0 = 0; r0 < rows; r0 += THREADS / width) {
+        const int row = r0 + threadIdx.x / width;
+        MaxSum v;
+        if (row < rows) {
+#pragma unroll 4
+            for (int i = sub; i < parts; i += width) {
+                const float2 p = __ldcg(part + (int64_t)i * rows + row);
+                v.join(p.x, p.y);
+            }
+        }
+        for (int d = width >> 1; d > 0; d >>= 1)
+            v.join(__shfl_xor_sync(0xffffffffu, v.m, d), __shfl_xor_sync(0xffffffffu, v.s, d));
+        if (sub == 0 && row < rows) {
+            const int lab = out.labels[row];
+            write_row(out, row, v.m, v.s, lab >= 0 && lab < out.classes ? __ldcg(zt + row) : 0.0f);
+        }
+    }
+}
+
 // Row statistics of a tile in base 2: (max, sum of 2^(t - max)), t = z log2 e, and the
-// label's logit.  A thread holds one row, so nothing is exchanged.
+// label's product.  A thread holds one row, so nothing is exchanged.
 struct EpiStats {
     static constexpr bool kFold = true, kTail = true;
     struct Args {
         const int32_t* labels;
-        float k2, scale;      // scale log2 e
+        float k2;             // scale log2 e
         float2* part;         // [per tiles_n][rows]
         int per;              // parts that a tile's columns are taken in
         float* zt;            // [rows]
@@ -114,7 +152,7 @@ struct EpiStats {
             float z = 0.0f;
 #pragma unroll
             for (int j = 0; j < 32; ++j) z = j == at ? v[j] : z;
-            a.zt[row] = z * a.scale;
+            a.zt[row] = z;
         }
     }
     __device__ __forceinline__ void done() {
@@ -122,33 +160,7 @@ struct EpiStats {
     }
     // the last CTA joins the parts
     static __device__ __forceinline__ void tail(const Args& a, const HgArgs& g, int* word) {
-        if (!a.parts) return;
-        __threadfence();
-        __syncthreads();
-        if (threadIdx.x == 0) *word = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
-        __syncthreads();
-        if (!*word) return;
-        __threadfence();
-        if (threadIdx.x == 0) *a.ticket = 0;
-        // 8 or 32 lanes a row, so that the rows' loads are under way together
-        const int width = g.M >= kHgThreads / 8 ? 8 : 32, sub = threadIdx.x & (width - 1);
-        for (int r0 = 0; r0 < g.M; r0 += kHgThreads / width) {
-            const int row = r0 + threadIdx.x / width;
-            MaxSum v;
-            if (row < g.M) {
-#pragma unroll 4
-                for (int i = sub; i < a.parts; i += width) {
-                    const float2 p = __ldcg(a.part + (int64_t)i * g.M + row);
-                    v.join(p.x, p.y);
-                }
-            }
-            for (int d = width >> 1; d > 0; d >>= 1)
-                v.join(__shfl_xor_sync(0xffffffffu, v.m, d), __shfl_xor_sync(0xffffffffu, v.s, d));
-            if (sub == 0 && row < g.M) {
-                const int lab = a.out.labels[row];
-                write_row(a.out, row, v.m, v.s, lab >= 0 && lab < a.out.classes ? __ldcg(a.zt + row) : 0.0f);
-            }
-        }
+        if (a.parts) join_as_last<kHgThreads>(a.part, a.parts, g.M, a.zt, a.ticket, a.out, word);
     }
 };
 
@@ -275,6 +287,149 @@ struct EpiBf16 {
     }
     __device__ __forceinline__ void done() {}
 };
+
+// ------------------------------------------------------------------ few rows
+// The forward of up to kFewRows rows on the CUDA cores: W's bytes bound it, and a sum that is
+// rounded at every step is nearer than the tensor cores', which cut off: with one to four rows
+// a confident row's small loss is all there is to be off from (4096 features, 1000 classes:
+// up to 2.9e-6 of the loss on the tensor cores, 3e-7 here).  One launch, no copies and no tensor maps:
+// 4 x 512 x 10000 6.8 us (9.6 on the tensor cores; W's 10 MB from L2), 4 x 4096 x 64000 111 us (W at 4.7 TB/s).
+//
+// A warp takes C classes (over ks warps of a CTA by pieces of 256 features, where there are few), R
+// rows at a time in registers; x comes from L1 after the first class.  Its sums are
+// exchanged so that each lane ends with one (row, class), whose statistics it keeps.
+struct FewArgs {
+    int64_t ldx, ldw;
+    int rows, features, ks;
+    float2* part;          // [CTAs][rows]
+    float* zt;
+    uint32_t* ticket;
+    RowOut out;
+};
+
+// Eight elements of a row of a piece of 256: VEC takes eight in a row, 16 bytes (8 of int8), else every 32nd
+template <typename T, bool VEC, bool WHOLE>
+__device__ __forceinline__ void few_load(const T* row, int piece, int lane, int features, float* v) {
+    if constexpr (VEC && WHOLE) {
+        const T* at = row + piece + 8 * lane;
+        if constexpr (sizeof(T) == 2) {
+            const uint4 u = __ldg(reinterpret_cast<const uint4*>(at));
+            const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
+        } else {
+            const uint2 u = __ldg(reinterpret_cast<const uint2*>(at));
+#pragma unroll
+            for (int j = 0; j < 8; ++j) v[j] = (float)(int8_t)((j < 4 ? u.x : u.y) >> (8 * (j & 3)));
+        }
+    } else {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            const int col = piece + (VEC ? 8 * lane + j : 32 * j + lane);
+            v[j] = 0.0f;
+            if (WHOLE || col < features) {
+                if constexpr (sizeof(T) == 2) v[j] = __uint_as_float((uint32_t)__ldg(row + col) << 16);
+                else v[j] = (float)__ldg(row + col);
+            }
+        }
+    }
+}
+
+template <typename T, int R, int C, bool VEC, bool WHOLE>
+__device__ __forceinline__ void few_step(const T* const* x, const uint16_t* const* w, int piece, int lane, int features,
+                                         float (*acc)[C]) {
+    float wv[C][8];
+#pragma unroll
+    for (int c = 0; c < C; ++c) few_load<uint16_t, VEC, WHOLE>(w[c], piece, lane, features, wv[c]);
+#pragma unroll
+    for (int r = 0; r < R; ++r) {
+        float xv[8];
+        few_load<T, VEC, WHOLE>(x[r], piece, lane, features, xv);
+#pragma unroll
+        for (int c = 0; c < C; ++c)
+#pragma unroll
+            for (int j = 0; j < 8; ++j) acc[r][c] = fmaf(xv[j], wv[c][j], acc[r][c]);
+    }
+}
+
+// v[0..N) summed over the warp's lanes; a lane gets the sum number lane / (32 / N)
+template <int N>
+__device__ __forceinline__ float few_sum(float* v, int lane) {
+    int bit = 16;
+#pragma unroll
+    for (int h = N / 2; h > 0; h >>= 1, bit >>= 1) {
+        const bool up = lane & bit;
+#pragma unroll
+        for (int i = 0; i < h; ++i) {
+            const float give = up ? v[i] : v[i + h], keep = up ? v[i + h] : v[i];
+            v[i] = keep + __shfl_xor_sync(0xffffffffu, give, bit);
+        }
+    }
+    for (; bit > 0; bit >>= 1) v[0] += __shfl_xor_sync(0xffffffffu, v[0], bit);
+    return v[0];
+}
+
+template <typename T, int R, int C, bool VEC>
+__global__ void __launch_bounds__(256, 2) k_xent_few(const T* x, const uint16_t* w, const FewArgs a) {
+    constexpr int N = R * C, kLanes = 32 / N;     // lanes that hold the same sum
+    __shared__ float sums[2][8][N];
+    __shared__ float2 rows_sh[8][R];
+    __shared__ int last;
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = warp % a.ks, per = 8 / a.ks;
+    const int groups = (a.out.classes + C - 1) / C, row = lane / kLanes / C;
+    const bool mine = sub == 0 && lane % kLanes == 0 && row < a.rows;
+    const int lab = mine ? a.out.labels[row] : -1;
+    const T* xr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) xr[r] = x + min(r, a.rows - 1) * a.ldx;
+    MaxSum st;
+    int turn = 0;
+    for (int g0 = blockIdx.x * per; g0 < groups; g0 += gridDim.x * per, turn ^= 1) {
+        const int first = (g0 + warp / a.ks) * C;
+        float acc[R][C];
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i / C][i % C] = 0.0f;
+        if (first < a.out.classes) {
+            const uint16_t* wr[C];
+#pragma unroll
+            for (int c = 0; c < C; ++c) wr[c] = w + min(first + c, a.out.classes - 1) * a.ldw;
+            int piece = sub * 256;
+#pragma unroll 2
+            for (; piece + 256 <= a.features; piece += a.ks * 256)
+                few_step<T, R, C, VEC, true>(xr, wr, piece, lane, a.features, acc);
+            if (piece < a.features) few_step<T, R, C, VEC, false>(xr, wr, piece, lane, a.features, acc);
+        }
+        float z = few_sum<N>(&acc[0][0], lane);
+        if (a.ks > 1) {
+            if (lane % kLanes == 0) sums[turn][warp][lane / kLanes] = z;
+            __syncthreads();       // the other turn's sums are read by now
+            if (mine) {
+                z = sums[turn][warp][lane / kLanes];
+                for (int k = 1; k < a.ks; ++k) z += sums[turn][warp + k][lane / kLanes];
+            }
+        }
+        const int cls = first + lane / kLanes % C;
+        if (mine && cls < a.out.classes) {
+            const float t = z * a.out.k2;
+            st.join(t, exp2f(fmaf(z, a.out.k2, -t)));     // what t's rounding left over: see write_row()
+            if (cls == lab) a.zt[row] = z;
+        }
+    }
+    // over the lanes of a row, the warps, and then the CTAs
+#pragma unroll
+    for (int d = 1; d < kLanes * C; d <<= 1)
+        st.join(__shfl_xor_sync(0xffffffffu, st.m, d), __shfl_xor_sync(0xffffffffu, st.s, d));
+    if (lane % (kLanes * C) == 0) rows_sh[warp][row] = make_float2(st.m, st.s);
+    __syncthreads();
+    if (threadIdx.x < a.rows) {
+        MaxSum v;
+        for (int i = 0; i < 8; ++i) v.join(rows_sh[i][threadIdx.x].x, rows_sh[i][threadIdx.x].y);
+        a.part[(int64_t)blockIdx.x * a.rows + threadIdx.x] = make_float2(v.m, v.s);
+    }
+    join_as_last<256>(a.part, gridDim.x, a.rows, a.zt, a.ticket, a.out, &last);
+}
 
 // ------------------------------------------------------------------ row kernels
 // Joins a row's tiles: 32 rows a CTA, the tiles over its warps.
@@ -429,6 +584,14 @@ constexpr int kFoldFeatures = 2048;
 // 2048 parts: 12.9 and 14.8).
 constexpr int64_t kPartsInOne = 1024;
 
+// The forward takes up to kFewRows rows to k_xent_few, from five on only where the head is small or
+// TMA cannot take W.  us, k_xent_few and the tensor cores: 4 rows x 512 x 10000 6.8 and 9.6, x 4096
+// x 64000 111 and 127; 8 rows x 4096 x 1000 8.2 and 12.2, x 512 x 10000 8.9 and 10.2, but x 1000 x 20011
+// 20.7 and 16.4 to 19; the same with W's rows at odd addresses 23.8 and 32.2.
+constexpr int kFewRows = 8;
+constexpr int64_t kFewProducts = (int64_t)8 << 20;
+constexpr int kFewCtas = 512;      // at most
+
 constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
 
@@ -497,6 +660,34 @@ HgProblem logits_problem(const nitro_xent* h, int rows, int64_t classes) {
     return p;
 }
 
+template <typename T, int R, int C>
+cudaError_t few_as(bool vec, const void* x, const uint16_t* w, const FewArgs& a, int grid, cudaStream_t s) {
+    return vec ? launch_k(k_xent_few<T, R, C, true>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a)
+               : launch_k(k_xent_few<T, R, C, false>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a);
+}
+template <typename T>
+cudaError_t few_rows(bool vec, int c, const void* x, const uint16_t* w, const FewArgs& a, int grid, cudaStream_t s) {
+    if (c == 4) return a.rows <= 1 ? few_as<T, 1, 4>(vec, x, w, a, grid, s) : a.rows <= 4 ? few_as<T, 4, 4>(vec, x, w, a, grid, s) : few_as<T, 8, 4>(vec, x, w, a, grid, s);
+    return a.rows <= 1 ? few_as<T, 1, 1>(vec, x, w, a, grid, s) : a.rows <= 4 ? few_as<T, 4, 1>(vec, x, w, a, grid, s) : few_as<T, 8, 1>(vec, x, w, a, grid, s);
+}
+
+cudaError_t forward_few(nitro_xent* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
+                        const RowOut& ro, cudaStream_t s) {
+    // two CTAs an SM; four classes a warp where that leaves no warp idle, else one, and its features
+    // over as many warps as are free
+    const int ctas = std::min(2 * sm_count(), kFewCtas), warps = 8 * ctas, pieces = (h->features + 255) / 256;
+    const int c = (int64_t)((h->classes + 3) / 4) * std::min(8, pieces) >= warps / 2 ? 4 : 1;
+    const int groups = (h->classes + c - 1) / c;
+    int ks = 1;
+    while (ks < 8 && 2 * ks <= pieces && (int64_t)groups * 2 * ks <= warps) ks *= 2;
+    const FewArgs a{ldx, ldw, rows, h->features, ks, h->part, h->zt, h->status + 1, ro};
+    const int grid = std::min(ctas, (groups + 8 / ks - 1) / (8 / ks));
+    const bool i8 = x_type == NITRO_I8;
+    const bool vec = tma_rows(w, ldw) && (i8 ? ((uintptr_t)x & 7) == 0 && ldx % 8 == 0 : tma_rows(x, ldx));
+    ProfScope ps(K_XENT_LOGITS, s, 2.0 * rows * h->classes * h->features, 2.0 * h->classes * h->features);
+    return i8 ? few_rows<int8_t>(vec, c, x, w, a, grid, s) : few_rows<uint16_t>(vec, c, x, w, a, grid, s);
+}
+
 }  // namespace
 
 extern "C" {
@@ -520,7 +711,7 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     const int64_t parts = 4 * ((classes + 127) / 128);
     const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->xg, max_rows * h->ldp) && h->allocs.take(&h->wp, classes * h->ldp) &&
                     h->allocs.take(&h->G, h->g_elems) && h->allocs.take(&h->acc, h->acc_floats) &&
-                    h->allocs.take(&h->part, parts * max_rows) && h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) && h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
+                    h->allocs.take(&h->part, std::max<int64_t>(parts * max_rows, kFewCtas * kFewRows)) && h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) && h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -535,19 +726,23 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     if (rows == 0) return NITRO_OK;
     if (!loss || !lse) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const RowOut ro{labels, loss, lse, h->status, h->classes, scale * kLog2e};
+    if (rows <= kFewRows && (rows <= 4 || (int64_t)h->classes * h->features <= kFewProducts || copies(w, NITRO_BF16, ldw))) {
+        TRY(forward_few(h, x, x_type, ldx, w, ldw, rows, ro, s));
+        return NITRO_OK;
+    }
     HgOperand ox{x, h->features, rows, ldx, 1, 0}, ow;
     if (copies(x, x_type, ldx)) {
         TRY(pack_rows(x, x_type, ldx, rows, h->features, h->xp, h->ldp, PackGrad{}, s));
         ox = {h->xp, h->features, rows, h->ldp, 1, 0};
     }
     TRY(w_operand(h, w, ldw, s, &ow));
-    const RowOut ro{labels, loss, lse, h->status, h->classes};
     HgProblem p = logits_problem(h, rows, h->classes);
     p.fold = h->features > kFoldFeatures;
     const HgPick t = hg_pick(p);
     const int per = t.ks > 1 ? 4 : 2, parts = per * ((h->classes + t.bn - 1) / t.bn);
     const bool few = (int64_t)parts * rows <= kPartsInOne;
-    const EpiStats::Args ea{labels, scale * kLog2e, scale, h->part, per, h->zt, h->status + 1, few ? parts : 0, ro};
+    const EpiStats::Args ea{labels, scale * kLog2e, h->part, per, h->zt, h->status + 1, few ? parts : 0, ro};
     TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
     if (few) return NITRO_OK;
     ProfScope ps(K_XENT_ROWS, s, 0.0, 8.0 * parts * rows);
