@@ -610,6 +610,7 @@ struct nitro_xent {
     float* zt = nullptr;
     float* factor = nullptr;    // [1 + max_rows], see PackGrad
     uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
+    bool clean = false;         // the ticket, see clear_once
     DeviceAllocs allocs;
 };
 
@@ -709,9 +710,13 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
                           2 * std::min(max_rows, kRowsWithLow) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
     const int64_t parts = 4 * ((classes + 127) / 128);
-    const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->xg, max_rows * h->ldp) && h->allocs.take(&h->wp, classes * h->ldp) &&
-                    h->allocs.take(&h->G, h->g_elems) && h->allocs.take(&h->acc, h->acc_floats) &&
-                    h->allocs.take(&h->part, std::max<int64_t>(parts * max_rows, kFewCtas * kFewRows)) && h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) && h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 8) == cudaSuccess;
+    // the status word is latched from here on; the ticket is cleared by the first forward
+    const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->xg, max_rows * h->ldp) &&
+                    h->allocs.take(&h->wp, classes * h->ldp) && h->allocs.take(&h->G, h->g_elems) &&
+                    h->allocs.take(&h->acc, h->acc_floats) &&
+                    h->allocs.take(&h->part, std::max<int64_t>(parts * max_rows, kFewCtas * kFewRows)) &&
+                    h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) &&
+                    h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 4) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -726,6 +731,7 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     if (rows == 0) return NITRO_OK;
     if (!loss || !lse) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    TRY(clear_once(h->clean, h->status + 1, 4, s));
     const RowOut ro{labels, loss, lse, h->status, h->classes, scale * kLog2e};
     if (rows <= kFewRows && (rows <= 4 || (int64_t)h->classes * h->features <= kFewProducts || copies(w, NITRO_BF16, ldw))) {
         TRY(forward_few(h, x, x_type, ldx, w, ldw, rows, ro, s));
