@@ -20,9 +20,9 @@
 // 64000 x 2048 1.81 PFLOP/s and 16384 x 2048 x 8192 1.83 where the clock holds, 1.6 to 1.75
 // under the power limit; the library's bf16 product makes 1.90 and 1.71.
 //
-// KS > 1 gives a tile's K to a cluster of KS (2 or 4) lone CTAs, where there are few tiles:
-// their sums meet in distributed shared memory, a slice of the columns for each CTA, are
-// added in the CTAs' order, and every CTA takes its slice through the epilogue.
+// KS > 1 gives a tile's K to a cluster of KS (2, 4 or 8) lone CTAs, where there are few tiles:
+// their sums meet in distributed shared memory, a slice of the columns for each CTA (of eight, for
+// the first four), are added in the CTAs' order, and taken through the epilogue there.
 //
 // Every wait is bounded; on expiry the kernel raises TIMEOUT, drains its own copies and
 // MMAs in flight (bounded as well), frees TMEM and returns.
@@ -205,6 +205,17 @@ struct HgStage {
         for (int j = 0; j < 4; ++j) v[j] = slot(lane, j);
         __syncwarp();
     }
+    // rows of unaligned matrices go out value by value, a row an instruction (or two of fp32): put, then value(row, j)
+    __device__ __forceinline__ void put(const uint4* v) const {
+#pragma unroll
+        for (int j = 0; j < 4; ++j) slot(lane, j) = v[j];
+        __syncwarp();
+    }
+    template <typename T>
+    __device__ __forceinline__ T value(int row, int j) const {
+        constexpr int E = 16 / (int)sizeof(T);
+        return reinterpret_cast<const T*>(&slot(row, j / E))[j % E];
+    }
     __device__ __forceinline__ int line_row(int i) const { return 8 * i + (lane >> 2); }
     __device__ __forceinline__ int line_chunk() const { return lane & 3; }
 };
@@ -223,6 +234,17 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
     uint4 v[4];
 #pragma unroll
     for (int j = 0; j < 4; ++j) v[j] = make_uint4(w[4 * j], w[4 * j + 1], w[4 * j + 2], w[4 * j + 3]);
+    if (!vec) {
+        // (eight values a lane at the lines' places are eight stores to 32 sectors each: the gradient of 6008 x 2337 took 76 us, now 33)
+        p.stage.put(v);
+        const int rows = min(32, p.rows - p.row0), c = col + p.stage.lane;
+        uint16_t* dst = base + (int64_t)p.row0 * ld + c;
+#pragma unroll 4
+        for (int r = 0; r < rows; ++r, dst += ld)
+            if (c < cols) *dst = p.stage.value<uint16_t>(r, p.stage.lane);
+        __syncwarp();
+        return;
+    }
     p.stage.to_lines(v);
     const int c = col + 8 * p.stage.line_chunk();
 #pragma unroll
@@ -230,7 +252,7 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
         const int row = p.row0 + p.stage.line_row(i);
         if (row >= p.rows || c >= cols) continue;
         uint16_t* dst = base + (int64_t)row * ld + c;
-        if (vec && c + 8 <= cols) {
+        if (c + 8 <= cols) {
             *reinterpret_cast<uint4*>(dst) = v[i];
         } else {
             const uint32_t u[4] = {v[i].x, v[i].y, v[i].z, v[i].w};
@@ -433,11 +455,11 @@ __global__ void __launch_bounds__(kHgThreads, 1)
             for (int dry = it == 0; dry >= 0; --dry) {
                 asm volatile("" : "+r"(dry));
                 if constexpr (KS > 1) {
-                    constexpr int W = BN / KS;                       // columns of a CTA's slice
+                    constexpr int W = KS > 4 ? 32 : BN / KS;         // columns of a CTA's slice
                     float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
                     const HgPart hp{row0 + lane, row0, dry ? 0 : g.M, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half, hs};
                     Epi epi(ea, g, T, hp);
-                    const bool mine = 32 * half < W;
+                    const bool mine = part < BN / W && 32 * half < W;
                     bool ok = true;
                     float v[32] = {};
                     if (!dry) {
@@ -620,8 +642,8 @@ inline HgPick hg_pick(const HgProblem& p, int ha = 1, int hb = 1, int max_splits
         for (int s = 1; s <= max_splits && s <= kb; ++s)
             if (hg_splits(p.K, s) == s)
                 take(cost(s) + (s > 1 ? 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500 : 0), {f.cg, f.bn, s});
-        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 4; s *= 2)
-            if (hg_splits(p.K, s) == s) take(cost(s) + 6000, {1, 128, 1, s});
+        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 8 && (s < 8 || 8 * tiles <= sms / 8 * 7); s *= 2)
+            if (hg_splits(p.K, s) == s) take(cost(s) + 6000 + (s == 8 ? 1000 : 0), {1, 128, 1, s});
     }
     return best;
 }
@@ -673,6 +695,7 @@ cudaError_t hg_launch(const HgPick& t, const HgProblem& p, const HgOperand& a, c
     // (a K too short for the cluster goes to lone CTAs)
     if (t.ks == 2 && hg_splits(p.K, 2) == 2) return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB, 2>(2, p, a, b, ea, s);
     if (t.ks == 4 && hg_splits(p.K, 4) == 4) return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB, 4>(4, p, a, b, ea, s);
+    if (t.ks == 8 && hg_splits(p.K, 8) == 8) return hg_launch_as<Epi, 1, 128, AMN, BMN, F16, HA, HB, 8>(8, p, a, b, ea, s);
     if (t.cg == 2 && t.bn == 256) return hg_launch_as<Epi, 2, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
     if (t.cg == 2) return hg_launch_as<Epi, 2, 128, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);
     if (t.bn == 256) return hg_launch_as<Epi, 1, 256, AMN, BMN, F16, HA, HB>(t.splits, p, a, b, ea, s);

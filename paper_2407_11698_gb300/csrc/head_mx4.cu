@@ -667,6 +667,20 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                         tmem_ld32_nowait(src + c, reinterpret_cast<uint32_t*>(v));
                         tmem_wait_ld<32>(reinterpret_cast<uint32_t*>(v));
                         if (c + 32 == BN / 2) release();
+                        if (!g.vec) {      // see hg_store16()
+                            const int rows = min(32, g.P - row0);
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                const int cc = col0 + c + 16 * h + (lane & 15);
+                                hs.put(v + 4 * h);
+                                float* dst = yf + (int64_t)(row0 + (lane >> 4)) * g.ldy + cc;
+#pragma unroll 4
+                                for (int r = lane >> 4; r < rows; r += 2, dst += 2 * g.ldy)
+                                    if (cc < g.Q) *dst = hs.value<float>(r, lane & 15);
+                                __syncwarp();
+                            }
+                            continue;
+                        }
                         hs.to_lines(v);
                         hs.to_lines(v + 4);
 #pragma unroll
@@ -674,7 +688,7 @@ __global__ void __launch_bounds__(kMxThreads, 1) k_mx4_gemm(const __grid_constan
                             const int r = row0 + hs.line_row(k & 3), cc = col0 + c + 16 * (k >> 2) + 4 * hs.line_chunk();
                             if (r >= g.P || cc >= g.Q) continue;
                             float* dst = yf + (int64_t)r * g.ldy + cc;
-                            if (g.vec && cc + 4 <= g.Q) {
+                            if (cc + 4 <= g.Q) {
                                 *reinterpret_cast<uint4*>(dst) = v[k];
                             } else {
                                 const uint32_t u[4] = {v[k].x, v[k].y, v[k].z, v[k].w};
