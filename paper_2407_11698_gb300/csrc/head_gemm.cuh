@@ -246,12 +246,16 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
         return;
     }
     p.stage.to_lines(v);
-    const int c = col + 8 * p.stage.line_chunk();
+    const int c = col + 8 * p.stage.line_chunk(), row = p.row0 + p.stage.line_row(0);
+    uint16_t* dst = base + (int64_t)row * ld + c;
+    if (p.row0 + 32 <= p.rows && col + 32 <= cols) {       // nearly all
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
-        const int row = p.row0 + p.stage.line_row(i);
-        if (row >= p.rows || c >= cols) continue;
-        uint16_t* dst = base + (int64_t)row * ld + c;
+        for (int i = 0; i < 4; ++i, dst += 8 * ld) *reinterpret_cast<uint4*>(dst) = v[i];
+        return;
+    }
+#pragma unroll
+    for (int i = 0; i < 4; ++i, dst += 8 * ld) {
+        if (row + 8 * i >= p.rows || c >= cols) continue;
         if (c + 8 <= cols) {
             *reinterpret_cast<uint4*>(dst) = v[i];
         } else {

@@ -33,6 +33,14 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
     return *reinterpret_cast<const uint32_t*>(&p);
 }
 
+// 2^t of an exponential's argument, below 2^-126 zero: one instruction, where exp2f has four (a logit's
+// part of an epilogue then is half as long)
+__device__ __forceinline__ float ex2(float t) {
+    float r;
+    asm("ex2.approx.ftz.f32 %0, %1;" : "=f"(r) : "f"(t));
+    return r;
+}
+
 __device__ __forceinline__ void pack_bf16_32(const float* v, uint32_t* w) {
 #pragma unroll
     for (int j = 0; j < 16; ++j) w[j] = pack_bf16(v[2 * j], v[2 * j + 1]);
@@ -128,22 +136,24 @@ struct EpiStats {
     __device__ __forceinline__ void cols(int c, float* v) {
         const int n = g.N - (col0 + c);
         if (n <= 0) return;
-        float m = -INFINITY;
+        float top[8];
         if (n < 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : -INFINITY;
         }
 #pragma unroll
-        for (int j = 0; j < 32; ++j) m = fmaxf(m, v[j]);
-        m = fmaxf(mx, m * a.k2);
+        for (int j = 0; j < 8; ++j) top[j] = fmaxf(fmaxf(v[j], v[j + 8]), fmaxf(v[j + 16], v[j + 24]));
+#pragma unroll
+        for (int j = 0; j < 4; ++j) top[j] = fmaxf(top[j], top[j + 4]);
+        const float m = fmaxf(mx, fmaxf(fmaxf(top[0], top[1]), fmaxf(top[2], top[3])) * a.k2);
         const float base = m == -INFINITY ? 0.0f : m;
         float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
 #pragma unroll
         for (int j = 0; j < 32; j += 4) {
-            s0 += exp2f(fmaf(v[j], a.k2, -base));
-            s1 += exp2f(fmaf(v[j + 1], a.k2, -base));
-            s2 += exp2f(fmaf(v[j + 2], a.k2, -base));
-            s3 += exp2f(fmaf(v[j + 3], a.k2, -base));
+            s0 += ex2(fmaf(v[j], a.k2, -base));
+            s1 += ex2(fmaf(v[j + 1], a.k2, -base));
+            s2 += ex2(fmaf(v[j + 2], a.k2, -base));
+            s3 += ex2(fmaf(v[j + 3], a.k2, -base));
         }
         sum = sum * exp2f(mx - base) + ((s0 + s1) + (s2 + s3));
         mx = m;
@@ -197,19 +207,24 @@ struct EpiProb {
         const int col = p.col0 + c;
         if (col >= g.N) return;
 #pragma unroll
-        for (int j = 0; j < 32; ++j) v[j] = live ? exp2f(fmaf(v[j], a.k2, -l2)) : 0.0f;
+        for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(v[j], a.k2, -l2));
         const int at = lab - col;
         if (live && at >= 0 && at < 32) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] -= j == at ? 1.0f : 0.0f;
         }
         uint32_t w[16];
-        pack_bf16_32(v, w);
+        const auto pack = [&] {
+            pack_bf16_32(v, w);
+#pragma unroll
+            for (int j = 0; j < 16; ++j) w[j] = live ? w[j] : 0u;
+        };
+        pack();
         hg_store16(p, w, a.G, a.ldg, col, (int)a.ldg, true);   // a row's padding may be written
         if (a.low) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] -= __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-            pack_bf16_32(v, w);
+            pack();
             hg_store16(p, w, a.G + a.low, a.ldg, col, (int)a.ldg, true);
         }
     }
