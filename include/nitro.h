@@ -395,7 +395,7 @@ typedef enum { NITRO_BF16 = 0, NITRO_I8 = 1, NITRO_F32 = 2, NITRO_I64 = 3 } nitr
  * is rounded to bf16 on the way to dw: nothing where all gout are alike, as under a mean.)  Sums are
  * in 32 bits, in an order that the sizes fix.  Rows that are left out put nothing into
  * dw, whatever they hold; with rows = 0 dw is cleared.
- * Workspace: copies of x and W as bf16, G of a piece (at most 256 MB, or 256 classes) and
+ * Workspace: copies of x and W as bf16, G of a piece (at most 512 MB, or 256 classes) and
  * 64 MB or rows x features of 32-bit sums.
  * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], a stride
  * below the features, another type, or a scale that is not above 0 (1e30 at most). */

@@ -607,7 +607,10 @@ constexpr int kFewRows = 8;
 constexpr int64_t kFewProducts = (int64_t)8 << 20;
 constexpr int kFewCtas = 512;      // at most
 
-constexpr int64_t kGElems = (int64_t)128 << 20;     // G of a piece: at most 256 MB where that is 256 columns or more
+// G of a piece: at most 512 MB where that is 256 columns or more.  A piece costs its products' last rounds
+// and dx's 32-bit sums a pass: 8192 x 2048 x 64000 takes 4.76 ms in pieces of 256 MB, 4.70 of 512, 4.65 of 1 GB, 5.3
+// of 64 MB, which would stay in L2; 8000 x 300 x 30000 715, 686, 686 and 990 us.
+constexpr int64_t kGElems = (int64_t)256 << 20;
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
 
 }  // namespace
