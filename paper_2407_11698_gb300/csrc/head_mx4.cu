@@ -137,6 +137,41 @@ __device__ __forceinline__ void load16(Raw8<T>* r, const T* src, int n, int vec)
     r[0] = load8(src, n, vec != 0);
     r[1] = load8(src + 8, n - 8, vec != 0);
 }
+// Rows at odd addresses.  A lane's sixteen values by sixteen accesses of its own would be 32 sectors
+// each; here half a warp takes sixteen values together, two lanes' an instruction, and they change
+// hands in shared memory (`box`: a warp's 32 x 16 values).  All lanes call; `n` of a lane's values
+// are in its row, none if not above 0.  16384 x 4097 in bf16: to 4 bits 73 -> 67 us, back 401 -> 62.
+template <typename T>
+__device__ __forceinline__ void lanes_load16(T* box, int lane, const T* src, int n, Raw8<T>* r) {
+    T v[16];
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int of = 2 * i + (lane >> 4);
+        const T* at = reinterpret_cast<const T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(src), of));
+        v[i] = (lane & 15) < __shfl_sync(0xffffffffu, n, of) ? at[lane & 15] : (T)0;
+    }
+#pragma unroll
+    for (int i = 0; i < 16; ++i) box[(2 * i + (lane >> 4)) * 16 + (lane & 15)] = v[i];
+    __syncwarp();
+    const uint4* mine = reinterpret_cast<const uint4*>(box + lane * 16);
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T); ++j) r[j / (sizeof(T) / 2)].w[j % (sizeof(T) / 2)] = mine[j];
+    __syncwarp();
+}
+template <typename T>
+__device__ __forceinline__ void lanes_store16(T* box, int lane, T* dst, int n, const uint4* v) {
+    uint4* mine = reinterpret_cast<uint4*>(box + lane * 16);
+#pragma unroll
+    for (int j = 0; j < (int)sizeof(T); ++j) mine[j] = v[j];
+    __syncwarp();
+#pragma unroll
+    for (int i = 0; i < 16; ++i) {
+        const int of = 2 * i + (lane >> 4);
+        T* at = reinterpret_cast<T*>(__shfl_sync(0xffffffffu, reinterpret_cast<unsigned long long>(dst), of));
+        if ((lane & 15) < __shfl_sync(0xffffffffu, n, of)) at[lane & 15] = box[of * 16 + (lane & 15)];
+    }
+    __syncwarp();
+}
 // a block's scale as stored, from its largest magnitude's bits: that exponent less 2, at
 // least 0; 255: not finite
 __device__ __forceinline__ uint32_t scale_code(uint32_t top) {
@@ -153,6 +188,7 @@ __device__ __forceinline__ float scale_inverse(uint32_t s) { return __uint_as_fl
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, int rows, int cols, uint8_t* q, uint8_t* sc,
                                                       int blocks, int64_t rows_pad, int vec) {
+    __shared__ __align__(16) T box[8][512];
     pdl_wait();
     const int tiles = (blocks + 3) / 4, per = tiles * 8;
     const int64_t n = rows_pad * per, step = (int64_t)gridDim.x * 256;
@@ -168,7 +204,8 @@ __global__ void __launch_bounds__(256) k_mx4_quantize(const T* x, int64_t ldx, i
             const int c = at.part * 16;
             const T* src = x + at.row * ldx + c;
             const int left = at.row < rows ? cols - c : 0;
-            load16(raw[u], src, left, vec);
+            if (vec) load16(raw[u], src, left, vec);
+            else lanes_load16(box[threadIdx.x >> 5], threadIdx.x & 31, src, left, raw[u]);
             at.next();
         }
 #pragma unroll
@@ -207,14 +244,15 @@ __device__ __forceinline__ void e2m1_bf16x4(uint32_t w, int h, uint32_t* out) {
 template <typename T>
 __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const uint8_t* sc, int rows, int cols, int blocks,
                                                         T* out, int64_t ldo, float* scales, int vec) {
+    __shared__ __align__(16) T box[8][512];
     pdl_wait();
     const int tiles = (blocks + 3) / 4, per = blocks * 2;
     const int64_t step = (int64_t)gridDim.x * 256;
     RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, step, per);
     const uint2* src = reinterpret_cast<const uint2*>(q) + blockIdx.x * (int64_t)256 + threadIdx.x;
-    while (at.row < rows) {
-        uint2 w[2];
-        uint32_t s[2];
+    while (__any_sync(0xffffffffu, at.row < rows)) {
+        uint2 w[2] = {};
+        uint32_t s[2] = {};
         int64_t row[2];
         int part[2];
 #pragma unroll
@@ -229,12 +267,13 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
         }
 #pragma unroll
         for (int u = 0; u < 2; ++u) {
-            if (row[u] >= rows) continue;
+            const bool in = row[u] < rows;
+            if (vec && !in) continue;
             const int c = part[u] * 16;
             const float f = e8m0_value(s[u]);
-            if (scales && (part[u] & 1) == 0) scales[row[u] * blocks + (part[u] >> 1)] = f;
+            if (in && scales && (part[u] & 1) == 0) scales[row[u] * blocks + (part[u] >> 1)] = f;
             T* dst = out + row[u] * ldo + c;
-            uint32_t v[8];      // two values each, as bf16
+            __align__(16) uint32_t v[8];      // two values each, as bf16
             e2m1_bf16x4(w[u].x, 0, v);
             e2m1_bf16x4(w[u].x, 1, v + 2);
             e2m1_bf16x4(w[u].y, 0, v + 4);
@@ -246,9 +285,11 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
                     const __nv_bfloat162 p = __hmul2(*reinterpret_cast<const __nv_bfloat162*>(&v[j]), k);
                     v[j] = *reinterpret_cast<const uint32_t*>(&p);
                 }
-                if (vec == 2 && c + 16 <= cols) {
+                if (!vec) {
+                    lanes_store16(box[threadIdx.x >> 5], threadIdx.x & 31, dst, in ? cols - c : 0, reinterpret_cast<const uint4*>(v));
+                } else if (vec == 2 && c + 16 <= cols) {
                     store32(dst, v);
-                } else if (vec && c + 16 <= cols) {
+                } else if (c + 16 <= cols) {
                     reinterpret_cast<uint4*>(dst)[0] = make_uint4(v[0], v[1], v[2], v[3]);
                     reinterpret_cast<uint4*>(dst)[1] = make_uint4(v[4], v[5], v[6], v[7]);
                 } else {
@@ -257,13 +298,15 @@ __global__ void __launch_bounds__(256) k_mx4_dequantize(const uint8_t* q, const 
                         if (c + j < cols) dst[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
                 }
             } else {
-                float o[16];
+                __align__(16) float o[16];
 #pragma unroll
                 for (int j = 0; j < 16; ++j) o[j] = __uint_as_float(j & 1 ? v[j >> 1] & 0xffff0000u : v[j >> 1] << 16) * f;
-                if (vec == 2 && c + 16 <= cols) {
+                if (!vec) {
+                    lanes_store16(box[threadIdx.x >> 5], threadIdx.x & 31, dst, in ? cols - c : 0, reinterpret_cast<const uint4*>(o));
+                } else if (vec == 2 && c + 16 <= cols) {
                     store32(dst, reinterpret_cast<const uint32_t*>(o));
                     store32(dst + 8, reinterpret_cast<const uint32_t*>(o) + 8);
-                } else if (vec && c + 16 <= cols) {
+                } else if (c + 16 <= cols) {
 #pragma unroll
                     for (int j = 0; j < 4; ++j)
                         reinterpret_cast<float4*>(dst)[j] = make_float4(o[4 * j], o[4 * j + 1], o[4 * j + 2], o[4 * j + 3]);
