@@ -673,7 +673,7 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     g.upper = p.upper ? 1 : 0;
     g.fold = p.fold && KS == 1 && g.kb_per_split > 1 ? 1 : 0;
     // row tiles whose A stays in L2 while B goes past them once: 40 MB (8192 x 64000 x 2048 in
-    // bands of 2048 rows read B, 262 MB, four times: a step 5.55 ms, now 5.48, under the power limit)
+    // bands of 2048 rows read B, 262 MB, four times: a step 5.55 ms, with these 5.48, under the power limit)
     g.band = (int)std::min<int64_t>(64, std::max<int64_t>(4, ((int64_t)40 << 20) / ((int64_t)128 * CG * HA * 2 * p.K)));
     g.status = p.status;
     static std::atomic<uint64_t> ready{0};

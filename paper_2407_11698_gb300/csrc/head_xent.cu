@@ -589,13 +589,13 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 constexpr int kRowsWithLow = 32;
 
 // The tensor cores drop the bits that a sum's 32 do not hold, so its error grows with the
-// additions: the loss is off by 5.6e-7 of it with 2048 features and 1.2e-6 with 3850.  From
+// additions: the loss is off by 5.6e-7 of it with 2048 features and, in one sum, 1.2e-6 with 3850.  From
 // here on the logits are summed in two halves, added with rounding (at 8192 x 4096 x 32000
 // that takes 3 per cent more time).
 constexpr int kFoldFeatures = 2048;
 
 // Parts of all rows that the forward's last CTA still joins by itself; more go to a launch of
-// their own (4 rows x 512 x 10000: 11.1 us with that launch and 9.9 without; 64 x 4096 x 1000,
+// their own (4 rows x 512 x 10000, taken here: 11.1 us with that launch and 9.9 without; 64 x 4096 x 1000,
 // 2048 parts: 12.9 and 14.8).
 constexpr int64_t kPartsInOne = 1024;
 
