@@ -958,8 +958,10 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
         for (int k = 1; k <= 16 && k <= g.stages && (k == 1 || k * rows * ldp <= kPartFloats); ++k) {
             const int per = (g.stages + k - 1) / k;
             if ((g.stages + per - 1) / per != k) continue;
-            // in stages: two for a tile's ends, four to join splits
-            const int64_t t = (tiles * k + units - 1) / units * (per + 2) + (k > 1 ? 4 : 0);
+            // in stages: two for a tile's ends, eight to join splits (by four 300 x 4096 x 4096 took a split and
+            // 19.7 us, now 14.8, and 500 x 2048 x 2048 15.8, now 11.3; by twelve 16 x 4096 x 4096 loses one
+            // that is worth having, 9.1 against 11.5)
+            const int64_t t = (tiles * k + units - 1) / units * (per + 2) + (k > 1 ? 8 : 0);
             if (t < cost) {
                 cost = t;
                 cg = c;
