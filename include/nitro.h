@@ -391,7 +391,7 @@ typedef enum { NITRO_BF16 = 0, NITRO_I8 = 1, NITRO_F32 = 2, NITRO_I64 = 3 } nitr
  * backward, from the lse of a forward on the same inputs and the loss gradient
  * gout[i] of each row (NULL: 1): G_ij = softmax(z_i)_j - [j = label_i], zero in rows that are
  * left out, rounded to bf16 (up to 32 rows: kept as two bf16 halves); dx_i = gout_i scale (G W)_i
- * and dw = scale sum_i gout_i G_i^T x_i, bf16, either may be NULL.  (x_i gout_i / gout_first
+ * and dw = scale sum_i gout_i G_i^T x_i, bf16, either may be NULL.  (x_i gout_i / max |gout|
  * is rounded to bf16 on the way to dw: nothing where all gout are alike, as under a mean.)  Sums are
  * in 32 bits, in an order that the sizes fix.  Rows that are left out put nothing into
  * dw, whatever they hold; with rows = 0 dw is cleared.

@@ -492,7 +492,8 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* c, int64_t ldc, in
 
 // What the backward takes of x and gout: rows that are left out become zeros, so that an
 // infinity or NaN in them meets no weight gradient (0 times it is NaN); the others
-// x gout_i / ref, ref = gout of the first row that has one, so that under a mean, where all
+// x gout_i / ref, ref = the largest |gout| of the rows with a label, so that no factor is above 1 whatever the
+// gradients' range (a quotient by a smaller one can pass bf16), and under a mean, where all
 // are alike, x stays what it is.  factor[0] = scale ref, factor[1 + i] = scale gout_i.
 struct PackGrad {
     const int32_t* labels;     // or null: a plain copy
@@ -500,7 +501,36 @@ struct PackGrad {
     float* factor;
     float scale;
     int classes;
+    const float* tops;         // the largest |gout| of parts of the rows, or null: the rows are gone through
+    int n_tops;
+    // |gout| of a row, 0 where it is left out
+    __device__ __forceinline__ float size(int64_t row) const {
+        const int lab = labels[row];
+        return lab >= 0 && lab < classes ? fabsf(gout[row]) : 0.0f;
+    }
 };
+
+// The largest of the threads' values (none negative; a NaN counts for nothing), in every thread of 256.
+__device__ __forceinline__ float block_max(float v) {
+    __shared__ float sh[8];
+#pragma unroll
+    for (int d = 16; d > 0; d >>= 1) v = fmaxf(v, __shfl_xor_sync(0xffffffffu, v, d));
+    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = v;
+    __syncthreads();
+    v = sh[0];
+#pragma unroll
+    for (int w = 1; w < 8; ++w) v = fmaxf(v, sh[w]);
+    return v;
+}
+
+// The largest |gout| of a CTA's rows, for batches of more rows than every CTA of k_xent_pack should go through.
+__global__ void __launch_bounds__(256) k_xent_top(const PackGrad pg, int rows, float* tops) {
+    pdl_wait();
+    float v = 0.0f;
+    for (int i = blockIdx.x * 256 + threadIdx.x; i < rows; i += gridDim.x * 256) v = fmaxf(v, pg.size(i));
+    v = block_max(v);
+    if (threadIdx.x == 0) tops[blockIdx.x] = v;
+}
 
 // Rows of x as bf16 with a stride of ldp (a multiple of 8; padding zero): int8 activations
 // are exact in bf16.
@@ -508,23 +538,15 @@ struct PackGrad {
 template <typename T>
 __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int rows, int cols, uint16_t* out, int64_t ldp,
                                                    const PackGrad pg, uint16_t* plain) {
-    __shared__ int first;
     pdl_wait();
     float ref = 1.0f;
     if (pg.labels && pg.gout) {
-        if (threadIdx.x == 0) first = rows;
-        __syncthreads();
-        for (int r = 0; r < rows; r += 256) {
-            const int i = r + threadIdx.x;
-            bool has = false;
-            if (i < rows) {
-                const int lab = pg.labels[i];
-                has = lab >= 0 && lab < pg.classes && pg.gout[i] != 0.0f;
-            }
-            if (has) atomicMin(&first, i);
-            if (__syncthreads_or(has)) break;
-        }
-        ref = first < rows ? pg.gout[first] : 0.0f;
+        float v = 0.0f;
+        if (pg.tops)
+            for (int i = threadIdx.x; i < pg.n_tops; i += 256) v = fmaxf(v, pg.tops[i]);
+        else
+            for (int i = threadIdx.x; i < rows; i += 256) v = fmaxf(v, pg.size(i));
+        ref = block_max(v);
     }
     if (pg.labels && blockIdx.x == 0 && threadIdx.x == 0) pg.factor[0] = pg.scale * ref;
     const int per = (int)(ldp / 8);
@@ -542,7 +564,7 @@ __global__ void __launch_bounds__(256) k_xent_pack(const T* x, int64_t ldx, int 
             const int lab = pg.labels[row];
             live = lab >= 0 && lab < pg.classes;
             const float go = live ? (pg.gout ? pg.gout[row] : 1.0f) : 0.0f;
-            f = go == ref ? 1.0f : go / ref;
+            f = go == ref ? 1.0f : go == -ref ? -1.0f : go / ref;      // (an infinity among them, too)
             live = live && go != 0.0f;
             if (c == 0) pg.factor[1 + row] = pg.scale * go;
         }
@@ -607,6 +629,11 @@ constexpr int kFewRows = 8;
 constexpr int64_t kFewProducts = (int64_t)8 << 20;
 constexpr int kFewCtas = 512;      // at most
 
+// Rows that every CTA of k_xent_pack goes through for the largest |gout|; more are gone through once, by a launch
+// of up to kTopCtas.
+constexpr int kRowsInPack = 1024;
+constexpr int kTopCtas = 64;
+
 // G of a piece: at most 512 MB where that is 256 columns or more.  A piece costs its products' last rounds
 // and dx's 32-bit sums a pass: 8192 x 2048 x 64000 takes 4.76 ms in pieces of 256 MB, 4.70 of 512, 4.65 of 1 GB, 5.3
 // of 64 MB, which would stay in L2; 8000 x 300 x 30000 715, 686, 686 and 990 us.
@@ -626,7 +653,7 @@ struct nitro_xent {
     float* acc = nullptr;
     float2* part = nullptr;
     float* zt = nullptr;
-    float* factor = nullptr;    // [1 + max_rows], see PackGrad
+    float* factor = nullptr;    // [1 + max_rows], see PackGrad, and [kTopCtas]
     uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
     bool clean = false;         // the ticket, see clear_once
     DeviceAllocs allocs;
@@ -733,7 +760,7 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
                     h->allocs.take(&h->wp, classes * h->ldp) && h->allocs.take(&h->G, h->g_elems) &&
                     h->allocs.take(&h->acc, h->acc_floats) &&
                     h->allocs.take(&h->part, std::max<int64_t>(parts * max_rows, kFewCtas * kFewRows)) &&
-                    h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1) &&
+                    h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1 + kTopCtas) &&
                     h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 4) == cudaSuccess;
     if (!ok) {
         nitro_xent_destroy(h);
@@ -793,7 +820,14 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
     HgOperand ox{x, F, rows, ldx, 1, 0}, ow;
     const bool copy = copies(x, x_type, ldx);
     if (copy) ox = {h->xp, F, rows, h->ldp, 1, 0};
-    const PackGrad pg{labels, gout, h->factor, scale, V};
+    PackGrad pg{labels, gout, h->factor, scale, V, nullptr, 0};
+    if (gout && rows > kRowsInPack) {
+        float* tops = h->factor + 1 + h->max_rows;
+        pg.n_tops = std::min(kTopCtas, (rows + 255) / 256);
+        ProfScope ps(K_XENT_PACK, s, 0.0, 8.0 * rows);
+        TRY(launch_k(k_xent_top, dim3(pg.n_tops), dim3(256), 0, s, pg, rows, tops));
+        pg.tops = tops;
+    }
     TRY(pack_rows(x, x_type, ldx, rows, F, h->xg, h->ldp, pg, s, copy ? h->xp : nullptr));
     TRY(w_operand(h, w, ldw, s, &ow));
     const HgOperand og{h->xg, F, rows, h->ldp, 1, 0};
