@@ -389,14 +389,16 @@ typedef enum { NITRO_BF16 = 0, NITRO_I8 = 1, NITRO_F32 = 2, NITRO_I64 = 3 } nitr
  * -1: the row is left out).  A label outside [-1, classes) latches BAD_LABEL
  * and counts as -1.
  * backward, from the lse of a forward on the same inputs and the loss gradient
- * gout[i] of each row (NULL: 1): G_ij = softmax(z_i)_j - [j = label_i], zero in rows that are
+ * gout[i] of each row (NULL: 1): G_ij = softmax(z_i)_j - [j = label_i] (at the label minus the sum of the
+ * others, which does not cancel in confident rows), zero in rows that are
  * left out, rounded to bf16 (up to 32 rows: kept as two bf16 halves); dx_i = gout_i scale (G W)_i
  * and dw = scale sum_i gout_i G_i^T x_i, bf16, either may be NULL.  (x_i gout_i / max |gout|
  * is rounded to bf16 on the way to dw: nothing where all gout are alike, as under a mean.)  Sums are
  * in 32 bits, in an order that the sizes fix.  Rows that are left out put nothing into
  * dw, whatever they hold; with rows = 0 dw is cleared.
- * Workspace: copies of x and W as bf16, G of a piece (at most 512 MB, or 256 classes) and
- * 64 MB or rows x features of 32-bit sums.
+ * Workspace: copies of x and W as bf16, G (rows x classes in bf16, twice that of up to 32 rows; at most
+ * 4 GB, beyond which the classes go in pieces and the logits are computed a third time), row statistics of
+ * 8 bytes a row and 32 classes, and 64 MB or rows x features of 32-bit sums.
  * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], a stride
  * below the features, another type, or a scale that is not above 0 (1e30 at most). */
 typedef struct nitro_xent nitro_xent;

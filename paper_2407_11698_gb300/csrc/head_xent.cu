@@ -178,40 +178,61 @@ struct EpiStats {
 // take.  The row's factor gout scale is left to their ends (dx) and to x (dw): multiplied
 // in here, the -1 at the label, exact in bf16 and most of a row's weight, would be rounded
 // as well, alike in every row.  Rows that are left out give zeros.
+//
+// The label's entry is minus the sum of the row's other entries.  As the label's exponential less one it would
+// be off by the rounding of lse, 2^-24 |lse| and more, which is all of it and many times its size in a
+// confident row (loss 1e-6 at lse 20).  So a tile leaves the sum of its columns, the label's apart, and
+// k_xent_label writes the entry (part), or it is there already (rest).
 struct EpiProb {
-    static constexpr bool kFold = false, kTail = false;
+    static constexpr bool kFold = true, kTail = false;
     struct Args {
         const int32_t* labels;
         const float* lse;
         float k2;
         int classes, v0;      // all classes, and the piece's first
-        uint16_t* G;          // [rows][ldg], ldg a multiple of 64
+        uint16_t* G;          // [rows][ldg], ldg a multiple of 64, or null: the sums alone
         int64_t ldg, low;     // low: from G to what its rounding left over, 0: not kept
+        float* part;          // [per tiles_n][rows] sums, or null
+        int per;              // parts that a tile's columns are taken in
+        const float* rest;    // [rows] the sums over all classes, where part is null
     };
     const Args& a;
     const HgArgs& g;
     const HgPart& p;
-    int lab = -1;
-    float l2 = 0.0f;
+    int lab = -1, slot;
+    float l2 = 0.0f, entry = 0.0f, sum = 0.0f;
     bool live = false;
-    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile&, const HgPart& p_) : a(a_), g(g_), p(p_) {
+    __device__ __forceinline__ EpiProb(const Args& a_, const HgArgs& g_, const HgTile& t, const HgPart& p_)
+        : a(a_), g(g_), p(p_), slot(a_.per * t.n + p_.slot) {
         if (p.row < p.rows) {
             lab = a.labels[p.row];
             live = lab >= 0 && lab < a.classes;
             lab -= a.v0;
             l2 = a.lse[p.row] * kLog2e;
+            if (a.rest) entry = -a.rest[p.row];
         }
     }
     __device__ __forceinline__ void fetch(int) {}
     __device__ __forceinline__ void cols(int c, float* v) {
-        const int col = p.col0 + c;
-        if (col >= g.N) return;
+        const int col = p.col0 + c, n = g.N - col;
+        if (n <= 0) return;
 #pragma unroll
         for (int j = 0; j < 32; ++j) v[j] = ex2(fmaf(v[j], a.k2, -l2));
+        if (n < 32) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] = j < n ? v[j] : 0.0f;
+        }
         const int at = lab - col;
         if (live && at >= 0 && at < 32) {
 #pragma unroll
-            for (int j = 0; j < 32; ++j) v[j] -= j == at ? 1.0f : 0.0f;
+            for (int j = 0; j < 32; ++j) v[j] = j == at ? entry : v[j];
+        }
+        if (a.part) {
+            float s0 = 0.0f, s1 = 0.0f, s2 = 0.0f, s3 = 0.0f;
+#pragma unroll
+            for (int j = 0; j < 32; j += 4) s0 += v[j], s1 += v[j + 1], s2 += v[j + 2], s3 += v[j + 3];
+            sum += (s0 + s1) + (s2 + s3);
+            if (!a.G) return;
         }
         uint32_t w[16];
         const auto pack = [&] {
@@ -228,7 +249,9 @@ struct EpiProb {
             hg_store16(p, w, a.G + a.low, a.ldg, col, (int)a.ldg, true);
         }
     }
-    __device__ __forceinline__ void done() {}
+    __device__ __forceinline__ void done() {
+        if (a.part && p.row < p.rows) a.part[(int64_t)slot * g.M + p.row] = sum;
+    }
 };
 
 // 32-bit sums into slice `split` of c, or added to what it holds.
@@ -467,6 +490,32 @@ __global__ void __launch_bounds__(256) k_xent_join(const float2* part, int parts
     }
 }
 
+// The label's entry of G from the sums of its row's other entries, or those sums alone (rest): 32 rows a
+// CTA, the parts over its warps.
+__global__ void __launch_bounds__(256) k_xent_label(const float* part, int parts, int rows, const int32_t* labels, int classes,
+                                                    uint16_t* G, int64_t ldg, int64_t low, float* rest) {
+    __shared__ float sh[8][32];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, w = threadIdx.x >> 5, row = blockIdx.x * 32 + lane;
+    float v = 0.0f;
+    if (row < rows)
+        for (int i = w; i < parts; i += 8) v += part[(int64_t)i * rows + row];
+    sh[w][lane] = v;
+    __syncthreads();
+    if (w != 0 || row >= rows) return;
+    for (int i = 1; i < 8; ++i) v += sh[i][lane];
+    if (rest) {
+        rest[row] = v;
+        return;
+    }
+    const int lab = labels[row];
+    if (lab < 0 || lab >= classes) return;
+    const __nv_bfloat16 h = __float2bfloat16_rn(-v);
+    uint16_t* at = G + row * ldg + lab;
+    *at = __bfloat16_as_ushort(h);
+    if (low) at[low] = __bfloat16_as_ushort(__float2bfloat16_rn(-v - __bfloat162float(h)));
+}
+
 // dx in bf16 from the slices of its 32-bit sums, four columns a thread.
 __global__ void __launch_bounds__(256) k_xent_dx(const float* c, int64_t ldc, int64_t slice, int slices, int features,
                                                  const float* factor, uint16_t* dx, int64_t lddx, int vec) {
@@ -634,10 +683,10 @@ constexpr int kFewCtas = 512;      // at most
 constexpr int kRowsInPack = 1024;
 constexpr int kTopCtas = 64;
 
-// G of a piece: at most 512 MB where that is 256 columns or more.  A piece costs its products' last rounds
-// and dx's 32-bit sums a pass: 8192 x 2048 x 64000 takes 4.76 ms in pieces of 256 MB, 4.70 of 512, 4.65 of 1 GB, 5.3
-// of 64 MB, which would stay in L2; 8000 x 300 x 30000 715, 686, 686 and 990 us.
-constexpr int64_t kGElems = (int64_t)256 << 20;
+// G: at most 4 GB.  Beyond that the classes go in pieces, whose rows' sums have to be known before the first
+// piece's products: the logits are then taken a third time, and dx's 32-bit sums are read and written
+// again by every piece.
+constexpr int64_t kGElems = (int64_t)1 << 31;
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices beyond one: at most 64 MB together
 
 }  // namespace
@@ -652,7 +701,7 @@ struct nitro_xent {
     uint16_t* G = nullptr;
     float* acc = nullptr;
     float2* part = nullptr;
-    float* zt = nullptr;
+    float* zt = nullptr;        // [max_rows] the forward's label logits, the backward's sums (EpiProb::Args::rest)
     float* factor = nullptr;    // [1 + max_rows], see PackGrad, and [kTopCtas]
     uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
     bool clean = false;         // the ticket, see clear_once
@@ -751,8 +800,7 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     h->features = features;
     h->classes = classes;
     h->ldp = round_up(features, 8);
-    h->g_elems = std::max(std::min(max_rows * round_up(classes, 64), std::max(kGElems, (int64_t)max_rows * 256)),
-                          2 * std::min(max_rows, kRowsWithLow) * round_up(classes, 64));
+    h->g_elems = std::min(kGElems, std::max(max_rows, 2 * std::min(max_rows, kRowsWithLow)) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
     const int64_t parts = 4 * ((classes + 127) / 128);
     // the status word is latched from here on; the ticket is cleared by the first forward
@@ -833,7 +881,28 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
     const HgOperand og{h->xg, F, rows, h->ldp, 1, 0};
     const int halves = rows <= kRowsWithLow ? 2 : 1;
     int64_t piece = std::min<int64_t>(round_up(V, 64), h->g_elems / halves / rows / 64 * 64);
-    if (piece < V) piece = piece / 256 * 256;
+    // the logits of n classes through EpiProb, and what follows from its sums
+    float* sums = reinterpret_cast<float*>(h->part);
+    const auto softmax = [&](const HgOperand& wp, int64_t n, EpiProb::Args ep) -> nitro_status {
+        HgProblem p = logits_problem(h, rows, n);
+        p.fold = F > kFoldFeatures;         // as in the forward
+        const HgPick t = hg_pick(p);
+        ep.per = t.ks > 1 ? 4 : 2;
+        TRY((hg_launch<EpiProb, false, false, false>(t, p, ox, wp, ep, s)));
+        if (!ep.part) return NITRO_OK;
+        const int parts = ep.per * (int)((n + t.bn - 1) / t.bn);
+        ProfScope ps(K_XENT_ROWS, s, 0.0, 4.0 * parts * rows);
+        TRY(launch_k(k_xent_label, dim3((rows + 31) / 32), dim3(256), 0, s, (const float*)sums, parts, rows, labels, V, ep.G, ep.ldg,
+                     ep.low, ep.G ? nullptr : h->zt));
+        return NITRO_OK;
+    };
+    EpiProb::Args ep{labels, lse, scale * kLog2e, V, 0, nullptr, 0, 0, sums, 0, nullptr};
+    if (piece < V) {
+        piece = piece / 256 * 256;
+        if (const nitro_status st = softmax(ow, V, ep)) return st;
+        ep.part = nullptr;
+        ep.rest = h->zt;
+    }
     // dx: in slices along the classes where its tiles leave SMs idle
     const int64_t ldc = round_up(F, 32);
     const HgProblem pd{rows, F, std::min<int64_t>(piece, V)};
@@ -844,10 +913,11 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         HgOperand wp = ow;
         wp.base = static_cast<const uint16_t*>(ow.base) + v0 * ow.ld;
         wp.outer = n;
-        const EpiProb::Args ep{labels, lse, scale * kLog2e, V, (int)v0, h->G, round_up(n, 64),
-                                halves == 2 ? rows * round_up(n, 64) : 0};
-        const HgProblem pl = logits_problem(h, rows, n);
-        TRY((hg_launch<EpiProb, false, false, false>(hg_pick(pl), pl, ox, wp, ep, s)));
+        ep.v0 = (int)v0;
+        ep.G = h->G;
+        ep.ldg = round_up(n, 64);
+        ep.low = halves == 2 ? rows * ep.ldg : 0;
+        if (const nitro_status st = softmax(wp, n, ep)) return st;
         const HgOperand G{h->G, n, rows, ep.ldg, halves, rows * ep.ldg};
         if (dx) {
             HgProblem p{rows, F, n};
