@@ -849,7 +849,7 @@ struct nitro_mx4 {
     int max_rows = 0, in = 0, out = 0;
     uint8_t *xq = nullptr, *xs = nullptr;
     float* part = nullptr;
-    uint32_t* status = nullptr;
+    StatusWord status;
     DeviceAllocs allocs;
 };
 
@@ -914,8 +914,7 @@ nitro_status nitro_mx4_create(int max_rows, int in, int out_features, nitro_mx4*
     h->in = in;
     h->out = out_features;
     const bool ok = h->allocs.take(&h->xq, code_bytes(max_rows, in)) && h->allocs.take(&h->xs, scale_bytes(max_rows, in)) &&
-                    h->allocs.take(&h->part, kPartFloats) && h->allocs.take(&h->status, 1) &&
-                    cudaMemset(h->status, 0, 4) == cudaSuccess;
+                    h->allocs.take(&h->part, kPartFloats) && h->status.take();
     if (!ok) {
         nitro_mx4_destroy(h);
         return NITRO_ERR_CUDA;
@@ -948,7 +947,7 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
     g.band = 8;
     g.k64 = (h->in + 63) / 64;
     g.stages = (g.k64 + 3) / 4;
-    g.status = h->status;
+    g.status = h->status.at;
     const int64_t ldp = round_up(h->out, 4);
     int cg = 1, bn = 0, splits = 1;
     int64_t cost = INT64_MAX;
@@ -1010,10 +1009,7 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
 nitro_status nitro_mx4_status(nitro_mx4* h, int clear) {
     if (!h) return NITRO_ERR_ARG;
     uint32_t bits = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess ||
-        cudaMemcpy(&bits, h->status, 4, cudaMemcpyDeviceToHost) != cudaSuccess ||
-        (clear && cudaMemset(h->status, 0, 4) != cudaSuccess))
-        return NITRO_ERR_CUDA;
+    if (!h->status.read(clear != 0, &bits)) return NITRO_ERR_CUDA;
     return bits & ST_TIMEOUT ? NITRO_ERR_TIMEOUT : NITRO_OK;
 }
 
@@ -1021,6 +1017,7 @@ void nitro_mx4_destroy(nitro_mx4* h) {
     if (!h) return;
     cudaDeviceSynchronize();
     h->allocs.free();
+    h->status.free();
     delete h;
 }
 

@@ -700,7 +700,7 @@ struct nitro_orth {
     Planes x[2], a, b;
     float* part = nullptr;
     float* scale = nullptr;    // [max_count], see k_orth_pack
-    uint32_t* status = nullptr;
+    StatusWord status;
     DeviceAllocs allocs;
 };
 
@@ -834,8 +834,7 @@ nitro_status nitro_orth_create(int max_count, int rows, int cols, nitro_orth** o
     h->small = std::min(rows, cols);
     for (Planes* p : {&h->x[0], &h->x[1]}) *p = {nullptr, round_up(cols, 64), rows * round_up(cols, 64)};
     for (Planes* p : {&h->a, &h->b}) *p = {nullptr, round_up(h->small, 64), h->small * round_up(h->small, 64)};
-    bool ok = h->allocs.take(&h->part, (int64_t)max_count * kNormCtas) && h->allocs.take(&h->scale, max_count) && h->allocs.take(&h->status, 1) &&
-              cudaMemset(h->status, 0, 4) == cudaSuccess;
+    bool ok = h->allocs.take(&h->part, (int64_t)max_count * kNormCtas) && h->allocs.take(&h->scale, max_count) && h->status.take();
     for (Planes* p : {&h->x[0], &h->x[1], &h->a, &h->b}) ok = ok && h->allocs.take(&p->base, 2 * max_count * p->plane);
     if (!ok) {
         nitro_orth_destroy(h);
@@ -869,7 +868,7 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
                        ((uintptr_t)m & 15) == 0 && ldm * size % 16 == 0 && stride_m * size % 16 == 0,
                        ((uintptr_t)out & 15) == 0 && ldo % 8 == 0 && stride_o % 8 == 0, sx,
                        sa / (sx * sx), k[2] * sb / (sa * sa), k[1] * sb / sa, k[0] * sb, 1.0f / sb,
-                       1.0f / (sb * sx), h->status};
+                       1.0f / (sb * sx), h->status.at};
         ProfScope ps(K_ORTH_SMALL, s, (double)count * steps * n * n * (3.0 * big + n), (double)count * n * big * (size + 2));
         TRY(m_type == NITRO_BF16 ? small_run<uint16_t>(c, a, count, s)
             : m_type == NITRO_F32 ? small_run<float>(c, a, count, s) : small_run<int64_t>(c, a, count, s));
@@ -893,7 +892,7 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
         HgProblem p;
         p.batch = count;
         p.planes_a = p.planes_b = 2;
-        p.status = h->status;
+        p.status = h->status.at;
         const HgOperand ox = operand(x, h->cols, h->rows, count), oa = operand(h->a, n, n, count), ob = operand(h->b, n, n, count);
         // A.  A bf16 matrix is held exactly by the first step's high halves.
         p.M = p.N = n;
@@ -941,10 +940,7 @@ nitro_status nitro_orth_run(nitro_orth* h, const void* m, int m_type, int64_t ld
 nitro_status nitro_orth_status(nitro_orth* h, int clear) {
     if (!h) return NITRO_ERR_ARG;
     uint32_t bits = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess ||
-        cudaMemcpy(&bits, h->status, 4, cudaMemcpyDeviceToHost) != cudaSuccess ||
-        (clear && cudaMemset(h->status, 0, 4) != cudaSuccess))
-        return NITRO_ERR_CUDA;
+    if (!h->status.read(clear != 0, &bits)) return NITRO_ERR_CUDA;
     return bits & ST_TIMEOUT ? NITRO_ERR_TIMEOUT : NITRO_OK;
 }
 
@@ -952,6 +948,7 @@ void nitro_orth_destroy(nitro_orth* h) {
     if (!h) return;
     cudaDeviceSynchronize();
     h->allocs.free();
+    h->status.free();
     delete h;
 }
 

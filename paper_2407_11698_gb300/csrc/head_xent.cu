@@ -703,8 +703,9 @@ struct nitro_xent {
     float2* part = nullptr;
     float* zt = nullptr;        // [max_rows] the forward's label logits, the backward's sums (EpiProb::Args::rest)
     float* factor = nullptr;    // [1 + max_rows], see PackGrad, and [kTopCtas]
-    uint32_t* status = nullptr; // [0] status, [1] ticket of the forward's CTAs
+    uint32_t* ticket = nullptr; // of the forward's CTAs
     bool clean = false;         // the ticket, see clear_once
+    StatusWord status;
     DeviceAllocs allocs;
 };
 
@@ -749,7 +750,7 @@ bool xent_args(const nitro_xent* h, const void* x, int x_type, int64_t ldx, cons
 
 HgProblem logits_problem(const nitro_xent* h, int rows, int64_t classes) {
     HgProblem p{rows, classes, h->features};
-    p.status = h->status;
+    p.status = h->status.at;
     p.prof = K_XENT_LOGITS;
     p.ops = 2.0 * rows * classes * h->features;
     return p;
@@ -775,7 +776,7 @@ cudaError_t forward_few(nitro_xent* h, const void* x, int x_type, int64_t ldx, c
     const int groups = (h->classes + c - 1) / c;
     int ks = 1;
     while (ks < 8 && 2 * ks <= pieces && (int64_t)groups * 2 * ks <= warps) ks *= 2;
-    const FewArgs a{ldx, ldw, rows, h->features, ks, h->part, h->zt, h->status + 1, ro};
+    const FewArgs a{ldx, ldw, rows, h->features, ks, h->part, h->zt, h->ticket, ro};
     const int grid = std::min(ctas, (groups + 8 / ks - 1) / (8 / ks));
     const bool i8 = x_type == NITRO_I8;
     const bool vec = tma_rows(w, ldw) && (i8 ? ((uintptr_t)x & 7) == 0 && ldx % 8 == 0 : tma_rows(x, ldx));
@@ -803,13 +804,13 @@ nitro_status nitro_xent_create(int max_rows, int features, int classes, nitro_xe
     h->g_elems = std::min(kGElems, std::max(max_rows, 2 * std::min(max_rows, kRowsWithLow)) * round_up(classes, 64));
     h->acc_floats = std::max(max_rows * round_up(features, 32), kAccFloats);
     const int64_t parts = 4 * ((classes + 127) / 128);
-    // the status word is latched from here on; the ticket is cleared by the first forward
+    // (the ticket is cleared by the first forward)
     const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->xg, max_rows * h->ldp) &&
                     h->allocs.take(&h->wp, classes * h->ldp) && h->allocs.take(&h->G, h->g_elems) &&
                     h->allocs.take(&h->acc, h->acc_floats) &&
                     h->allocs.take(&h->part, std::max<int64_t>(parts * max_rows, kFewCtas * kFewRows)) &&
                     h->allocs.take(&h->zt, max_rows) && h->allocs.take(&h->factor, max_rows + 1 + kTopCtas) &&
-                    h->allocs.take(&h->status, 2) && cudaMemset(h->status, 0, 4) == cudaSuccess;
+                    h->allocs.take(&h->ticket, 1) && h->status.take();
     if (!ok) {
         nitro_xent_destroy(h);
         return NITRO_ERR_CUDA;
@@ -824,8 +825,8 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     if (rows == 0) return NITRO_OK;
     if (!loss || !lse) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    TRY(clear_once(h->clean, h->status + 1, 4, s));
-    const RowOut ro{labels, loss, lse, h->status, h->classes, scale * kLog2e};
+    TRY(clear_once(h->clean, h->ticket, 4, s));
+    const RowOut ro{labels, loss, lse, h->status.at, h->classes, scale * kLog2e};
     if (rows <= kFewRows && (rows <= 4 || (int64_t)h->classes * h->features <= kFewProducts || copies(w, NITRO_BF16, ldw))) {
         TRY(forward_few(h, x, x_type, ldx, w, ldw, rows, ro, s));
         return NITRO_OK;
@@ -841,7 +842,7 @@ nitro_status nitro_xent_forward(nitro_xent* h, const void* x, int x_type, int64_
     const HgPick t = hg_pick(p);
     const int per = t.ks > 1 ? 4 : 2, parts = per * ((h->classes + t.bn - 1) / t.bn);
     const bool few = (int64_t)parts * rows <= kPartsInOne;
-    const EpiStats::Args ea{labels, scale * kLog2e, h->part, per, h->zt, h->status + 1, few ? parts : 0, ro};
+    const EpiStats::Args ea{labels, scale * kLog2e, h->part, per, h->zt, h->ticket, few ? parts : 0, ro};
     TRY((hg_launch<EpiStats, false, false, false>(t, p, ox, ow, ea, s)));
     if (few) return NITRO_OK;
     ProfScope ps(K_XENT_ROWS, s, 0.0, 8.0 * parts * rows);
@@ -922,7 +923,7 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         if (dx) {
             HgProblem p{rows, F, n};
             p.planes_a = halves;
-            p.status = h->status;
+            p.status = h->status.at;
             p.prof = K_XENT_DX;
             p.ops = 2.0 * rows * n * F;
             if (direct) {
@@ -940,7 +941,7 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
         if (dw) {
             HgProblem p{n, F, rows};
             p.planes_a = halves;
-            p.status = h->status;
+            p.status = h->status.at;
             p.prof = K_XENT_DW;
             p.ops = 2.0 * rows * n * F;
             const EpiBf16::Args eb{dw + v0 * lddw, lddw, tma_rows(dw, lddw), h->factor, 1};
@@ -960,10 +961,7 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
 nitro_status nitro_xent_status(nitro_xent* h, int clear) {
     if (!h) return NITRO_ERR_ARG;
     uint32_t bits = 0;
-    if (cudaDeviceSynchronize() != cudaSuccess ||
-        cudaMemcpy(&bits, h->status, 4, cudaMemcpyDeviceToHost) != cudaSuccess ||
-        (clear && cudaMemset(h->status, 0, 4) != cudaSuccess))
-        return NITRO_ERR_CUDA;
+    if (!h->status.read(clear != 0, &bits)) return NITRO_ERR_CUDA;
     return bits & ST_TIMEOUT ? NITRO_ERR_TIMEOUT : bits & ST_BAD_LABEL ? NITRO_ERR_ARG : NITRO_OK;
 }
 
@@ -971,6 +969,7 @@ void nitro_xent_destroy(nitro_xent* h) {
     if (!h) return;
     cudaDeviceSynchronize();
     h->allocs.free();
+    h->status.free();
     delete h;
 }
 

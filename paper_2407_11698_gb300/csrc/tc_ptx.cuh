@@ -259,6 +259,33 @@ struct DeviceAllocs {
     }
 };
 
+// A handle's latched status, in pinned host memory: it is clear when take() returns, and again when read() has cleared
+// it, without an operation on any stream.  (A clear on the default stream can wait there behind other
+// work, and erase what calls on another stream latch in the meantime.)  Kernels reach it over
+// the bus, only when they raise a bit.
+struct StatusWord {
+    uint32_t* at = nullptr;
+    bool take() {
+        void* q = nullptr;
+        if (cudaMallocHost(&q, sizeof(uint32_t)) != cudaSuccess) return false;
+        at = static_cast<uint32_t*>(q);
+        *at = 0;
+        return true;
+    }
+    // waits for the device
+    bool read(bool clear, uint32_t* bits) {
+        if (cudaDeviceSynchronize() != cudaSuccess) return false;
+        volatile uint32_t* w = at;
+        *bits = *w;
+        if (clear) *w = 0;
+        return true;
+    }
+    void free() {
+        if (at) cudaFreeHost(at);
+        at = nullptr;
+    }
+};
+
 // CTAs of 256 threads for `items` of a grid-stride kernel, one a thread, and no more than the
 // SMs hold at once by their registers (a second wave of a third of the CTAs costs as much as
 // the first).  resident: the kernel's CTAs an SM, looked up once.
