@@ -155,7 +155,10 @@ struct EpiStats {
             s2 += ex2(fmaf(v[j + 2], a.k2, -base));
             s3 += ex2(fmaf(v[j + 3], a.k2, -base));
         }
-        sum = sum * exp2f(mx - base) + ((s0 + s1) + (s2 + s3));
+        // A term is 1 at most but for the rounding of its maximum, which moves it by a factor of up to 2 below 2^24; a
+        // sum above 64 is that of masked classes (2^31 and more, where the factor is past the range)
+        const float s = (s0 + s1) + (s2 + s3);
+        sum = sum * exp2f(mx - base) + (s > 64.0f ? 1.0f : s);
         mx = m;
         const int at = lab - (col0 + c);
         if (at >= 0 && at < 32 && at < n) {
@@ -451,7 +454,10 @@ __global__ void __launch_bounds__(256, 2) k_xent_few(const T* x, const uint16_t*
         const int cls = first + lane / kLanes % C;
         if (mine && cls < a.out.classes) {
             const float t = z * a.out.k2;
-            st.join(t, exp2f(fmaf(z, a.out.k2, -t)));     // what t's rounding left over: see write_row()
+            // what t's rounding left over: see write_row().  A masked class may have a t that is not finite, or
+            // one of 2^31 and more, whose rounding alone is past an exponential's range.
+            const float rest = exp2f(fmaf(z, a.out.k2, -t));
+            if (t != -INFINITY) st.join(t, rest > 2.0f ? 1.0f : rest);
             if (cls == lab) a.zt[row] = z;
         }
     }
