@@ -462,7 +462,9 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                     constexpr int W = KS > 4 ? 32 : BN / KS;         // columns of a CTA's slice
                     float4* stage = reinterpret_cast<float4*>(smem); // [KS][W / 4][128], where the operands were
                     const HgPart hp{row0 + lane, row0, dry ? 0 : g.M, T.n * BN + part * W + 32 * half, 32, (part * W >> 5) + half, hs};
-                    Epi epi(ea, g, T, hp);
+                    HgTile whole = T;            // what arrives at the epilogue is the sum of all splits
+                    whole.split = 0;
+                    Epi epi(ea, g, whole, hp);
                     const bool mine = part < BN / W && 32 * half < W;
                     bool ok = true;
                     float v[32] = {};
