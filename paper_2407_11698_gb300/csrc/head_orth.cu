@@ -230,40 +230,71 @@ struct Vec16 {
 };
 constexpr int kOrthInFlight = 4;    // loads of a thread in flight
 
-// Sum of squares of a matrix, a partial of each CTA (blockIdx.y: the matrix).
+// Squares of fp32 and bf16 values from 1.8e19 on do not fit 32 bits.  So a sum that is not finite is taken again, of
+// the values times 2^-96: 2^33 squares of the largest then sum up to 2^97, and where a sum has passed 2^128 the
+// values that count are above 2^47.  (The sum of values that are not finite stays so; int64 values
+// are scaled anyway.)
+constexpr float kFar = 0x1p-96f;
+constexpr int kFarBits = 96;
+__device__ __forceinline__ bool is_far(float s) { return !(s <= FLT_MAX); }
+
+// 1 / (norm + eps) as left 2^e, left in [1/2, 1), from the sum of squares s (far: of the values times kFar); false
+// where that is not finite or zero: left is then 1 and *whole the factor itself.
 template <typename T>
-__global__ void __launch_bounds__(256) k_orth_norm(const T* m, int64_t ld, int64_t stride, int rows, int cols, float* part,
+__device__ __forceinline__ bool norm_inverse(float s, bool far, float* left, int* e, float* whole) {
+    // int64 values were taken times 2^-32, so is the 1e-7; beside far values it is nothing
+    const float eps = far ? 0.0f : sizeof(T) == 8 ? kNormEps * 0x1p-32f : kNormEps;
+    const float full = 1.0f / (sqrtf(s) + eps);
+    *left = frexpf(full, e);
+    *e -= far ? kFarBits : 0;
+    *whole = full;
+    if (isfinite(full) && full > 0.0f) return true;
+    *left = 1.0f;
+    return false;
+}
+
+// Sum of squares of a matrix, a partial of each CTA (blockIdx.y: the matrix): x that of the values, y of them
+// times kFar.
+template <typename T>
+__global__ void __launch_bounds__(256) k_orth_norm(const T* m, int64_t ld, int64_t stride, int rows, int cols, float2* part,
                                                    int vec) {
     constexpr int E = Vec16<T>::E;
-    __shared__ float sh[8];
+    __shared__ float sh[2][8];
     pdl_wait();
     const T* src = m + blockIdx.y * stride;
-    RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, (int64_t)gridDim.x * 256, (cols + E - 1) / E);
-    float s[kOrthInFlight] = {};
-    while (at.row < rows) {
-        Vec16<T> r[kOrthInFlight];
+    // the CTA's sum of the squares of values times f, in every thread
+    const auto sum = [&](float f, float* warps) {
+        RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, (int64_t)gridDim.x * 256, (cols + E - 1) / E);
+        float s[kOrthInFlight] = {};
+        while (at.row < rows) {
+            Vec16<T> r[kOrthInFlight];
 #pragma unroll
-        for (int u = 0; u < kOrthInFlight; ++u) {
-            r[u].load(src + at.row * ld + at.part * E, at.row < rows ? cols - at.part * E : 0, vec != 0);
-            at.next();
-        }
-#pragma unroll
-        for (int u = 0; u < kOrthInFlight; ++u)
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float v = as_float(r[u].v[j]);
-                s[u] = fmaf(v, v, s[u]);
+            for (int u = 0; u < kOrthInFlight; ++u) {
+                r[u].load(src + at.row * ld + at.part * E, at.row < rows ? cols - at.part * E : 0, vec != 0);
+                at.next();
             }
-    }
-    float t = (s[0] + s[1]) + (s[2] + s[3]);
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-    if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = t;
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        for (int w = 1; w < 8; ++w) t += sh[w];
-        part[blockIdx.y * kNormCtas + blockIdx.x] = t;
-    }
+            for (int u = 0; u < kOrthInFlight; ++u)
+#pragma unroll
+                for (int j = 0; j < E; ++j) {
+                    const float v = as_float(r[u].v[j]) * f;
+                    s[u] = fmaf(v, v, s[u]);
+                }
+        }
+        float t = (s[0] + s[1]) + (s[2] + s[3]);
+#pragma unroll
+        for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+        if ((threadIdx.x & 31) == 0) warps[threadIdx.x >> 5] = t;
+        __syncthreads();
+        t = warps[0];
+        for (int w = 1; w < 8; ++w) t += warps[w];
+        return t;
+    };
+    float2 t;
+    t.x = sum(1.0f, sh[0]);
+    t.y = t.x * kFar * kFar;
+    if (sizeof(T) < 8 && is_far(t.x)) t.y = sum(kFar, sh[1]);
+    if (threadIdx.x == 0) part[blockIdx.y * kNormCtas + blockIdx.x] = t;
 }
 
 // X0 as planes (padding columns zero).  The planes hold M times the power of two that puts
@@ -272,25 +303,26 @@ __global__ void __launch_bounds__(256) k_orth_norm(const T* m, int64_t ld, int64
 // bits: their low halves are zero, and the first step leaves them out.
 template <typename T>
 __global__ void __launch_bounds__(256) k_orth_pack(const T* m, int64_t ld, int64_t stride, int rows, int cols,
-                                                   const float* part, int parts, float mul, Planes out, int low, int vec, float* scale) {
+                                                   const float2* part, int parts, float mul, Planes out, int low, int vec, float* scale) {
     constexpr int E = Vec16<T>::E;
-    __shared__ float sh[8];
+    __shared__ float2 sh[8];
     pdl_wait();
-    float s = 0.0f;
-    for (int i = threadIdx.x; i < parts; i += 256) s += part[blockIdx.y * kNormCtas + i];
+    float2 s = make_float2(0.0f, 0.0f);
+    for (int i = threadIdx.x; i < parts; i += 256) {
+        const float2 o = part[blockIdx.y * kNormCtas + i];
+        s.x += o.x, s.y += o.y;
+    }
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
+    for (int d = 16; d > 0; d >>= 1) s.x += __shfl_xor_sync(0xffffffffu, s.x, d), s.y += __shfl_xor_sync(0xffffffffu, s.y, d);
     if ((threadIdx.x & 31) == 0) sh[threadIdx.x >> 5] = s;
     __syncthreads();
-    s = 0.0f;
-    for (int w = 0; w < 8; ++w) s += sh[w];
-    // int64 values were taken times 2^-32, so is the 1e-7
-    const float eps = sizeof(T) == 8 ? kNormEps * 0x1p-32f : kNormEps;
-    const float full = 1.0f / (sqrtf(s) + eps);
+    s = make_float2(0.0f, 0.0f);
+    for (int w = 0; w < 8; ++w) s.x += sh[w].x, s.y += sh[w].y;
+    const bool far = sizeof(T) < 8 && is_far(s.x);
     int e;
-    const float left = frexpf(full, &e);      // in [1/2, 1); a norm that is not finite leaves 0 or NaN
-    const float f = isfinite(full) && full > 0.0f ? ldexpf(mul, e) : mul * full;
-    if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = isfinite(full) && full > 0.0f ? left : 1.0f;
+    float left, full;
+    const float f = norm_inverse<T>(far ? s.y : s.x, far, &left, &e, &full) ? ldexpf(mul, e) : mul * full;
+    if (blockIdx.x == 0 && threadIdx.x == 0) scale[blockIdx.y] = left;
     const T* src = m + blockIdx.y * stride;
     uint16_t* hi = out.base + 2 * blockIdx.y * out.plane;
     RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, (int64_t)gridDim.x * 256, (int)(out.ld / E));
@@ -439,31 +471,41 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
             }
         }
     }
+    // over the threads and the cluster
+    const auto total = [&](float t) {
 #pragma unroll
-    for (int d = 16; d > 0; d >>= 1) s += __shfl_xor_sync(0xffffffffu, s, d);
-    if (lane == 0) parts[warp] = s;
-    __syncthreads();
-    s = 0.0f;
-    for (int w = 0; w < 16; ++w) s += parts[w];
-    if constexpr (C > 1) {
-        cluster_barrier();       // every CTA of the cluster runs
-        if (tid < C) {
-            const uint32_t to = remote_smem(smem_u32(parts + 16 + rank), (uint32_t)tid);
-            asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(s) : "memory");
+        for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
+        if (lane == 0) parts[warp] = t;
+        __syncthreads();
+        t = 0.0f;
+        for (int w = 0; w < 16; ++w) t += parts[w];
+        if constexpr (C > 1) {
+            cluster_barrier();       // every CTA of the cluster runs, and has read what an earlier total left
+            if (tid < C) {
+                const uint32_t to = remote_smem(smem_u32(parts + 16 + rank), (uint32_t)tid);
+                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(t) : "memory");
+            }
+            cluster_barrier();
+            t = 0.0f;
+            for (int r = 0; r < C; ++r) t += parts[16 + r];
         }
-        cluster_barrier();
+        return t;
+    };
+    s = total(s);
+    const bool far = sizeof(T) < 8 && is_far(s);     // alike in the whole cluster
+    if (far) {
+        __syncthreads();             // the warps' parts are read
         s = 0.0f;
-        for (int r = 0; r < C; ++r) s += parts[16 + r];
+        for (int i = tid; i < a.nb * 8192; i += kOsThreads) {
+            const uint32_t hi = reinterpret_cast<const uint16_t*>(xh)[i], lo = reinterpret_cast<const uint16_t*>(xl)[i];
+            const float v = __uint_as_float(hi << 16 | lo) * kFar;
+            s = fmaf(v, v, s);
+        }
+        s = total(s);
     }
-    const float eps = sizeof(T) == 8 ? kNormEps * 0x1p-32f : kNormEps;
-    const float full = 1.0f / (sqrtf(s) + eps);
     int e;
-    float left = frexpf(full, &e);           // see k_orth_pack
-    float f0 = ldexpf(a.mul, e);
-    if (!(isfinite(full) && full > 0.0f)) {
-        left = 1.0f;
-        f0 = a.mul * full;
-    }
+    float left, full, f0;            // see k_orth_pack
+    f0 = norm_inverse<T>(s, far, &left, &e, &full) ? ldexpf(a.mul, e) : a.mul * full;
     for (int i = tid; i < a.nb * 1024; i += kOsThreads) {
         const uint4 hv = reinterpret_cast<const uint4*>(xh)[i], lv = reinterpret_cast<const uint4*>(xl)[i];
         const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
@@ -698,7 +740,7 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 struct nitro_orth {
     int max_count = 0, rows = 0, cols = 0, small = 0;   // small = min(rows, cols)
     Planes x[2], a, b;
-    float* part = nullptr;
+    float2* part = nullptr;    // [max_count][kNormCtas], see k_orth_norm
     float* scale = nullptr;    // [max_count], see k_orth_pack
     StatusWord status;
     DeviceAllocs allocs;
@@ -767,7 +809,7 @@ nitro_status orth_first(nitro_orth* h, const T* m, int64_t ld, int64_t stride, i
     }
     const int grid = share(one_wave(k_orth_pack<T>, resident[1], (items + 3) / 4 * count));
     ProfScope ps(K_ORTH_PACK, s, 0.0, (double)(sizeof(T) + (low ? 4 : 2)) * n * count);
-    TRY(launch_k(k_orth_pack<T>, dim3(grid, count), dim3(256), 0, s, m, ld, stride, h->rows, h->cols, (const float*)h->part,
+    TRY(launch_k(k_orth_pack<T>, dim3(grid, count), dim3(256), 0, s, m, ld, stride, h->rows, h->cols, (const float2*)h->part,
                  parts, mul, h->x[0], low ? 1 : 0, vec, h->scale));
     return NITRO_OK;
 }
