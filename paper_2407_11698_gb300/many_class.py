@@ -35,6 +35,7 @@ class ManyClassHead:
         self.loss_op = nb.SoftmaxXent(max_rows, features, classes)
         self.orth_op = nb.Orthogonalizer(1, classes, features)
         self.serve_op = None
+        self.stale = True                                # whether the 4-bit weights are of an older W
 
     def step(self, x, labels):
         """One training step on x int8 [rows x features], labels int32 (-1: left out); returns
@@ -50,7 +51,7 @@ class ManyClassHead:
         self.orth_op.run(self.m, self.update)
         self.master.add_(self.update, alpha=-self.lr * math.sqrt(max(self.classes, self.features)))
         self.w.copy_(self.master)
-        self.serve_op = None                             # its 4-bit weights are of the old W
+        self.stale = True
         return loss.sum() / live
 
     def logits(self, x):
@@ -63,8 +64,10 @@ class ManyClassHead:
             nq, ns = nb.mx4_bytes(self.classes, self.features)
             self.q = torch.empty(nq, dtype=torch.uint8, device=x.device)
             self.s = torch.empty(ns, dtype=torch.uint8, device=x.device)
-            nb.mx4_quantize(self.w, self.q, self.s)
             self.serve_op = nb.Mx4Linear(self.max_rows, self.features, self.classes)
+        if self.stale:
+            nb.mx4_quantize(self.w, self.q, self.s)
+            self.stale = False
         y = torch.empty(x.shape[0], self.classes, dtype=torch.float32, device=x.device)
         self.serve_op.run(x.to(torch.bfloat16), self.q, self.s, y)
         return y * self.scale
