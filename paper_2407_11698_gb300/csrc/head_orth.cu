@@ -230,8 +230,8 @@ struct Vec16 {
 };
 constexpr int kOrthInFlight = 4;    // loads of a thread in flight
 
-// Squares of fp32 and bf16 values from 1.8e19 on do not fit 32 bits.  So a sum that is not finite is taken again, of
-// the values times 2^-96: 2^33 squares of the largest then sum up to 2^97, and where a sum has passed 2^128 the
+// Squares of fp32 and bf16 values from 1.8e19 on do not fit 32 bits.  Where their sum is not finite, that of
+// the values times 2^-96 is taken: 2^33 squares of the largest then sum up to 2^97, and where a sum has passed 2^128 the
 // values that count are above 2^47.  (The sum of values that are not finite stays so; int64 values
 // are scaled anyway.)
 constexpr float kFar = 0x1p-96f;
@@ -254,7 +254,7 @@ __device__ __forceinline__ bool norm_inverse(float s, bool far, float* left, int
 }
 
 // Sum of squares of a matrix, a partial of each CTA (blockIdx.y: the matrix): x that of the values, y of them
-// times kFar.
+// times kFar, for which a CTA whose sum is not finite goes through its values again.
 template <typename T>
 __global__ void __launch_bounds__(256) k_orth_norm(const T* m, int64_t ld, int64_t stride, int rows, int cols, float2* part,
                                                    int vec) {
@@ -414,7 +414,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
     uint64_t* bar = reinterpret_cast<uint64_t*>(tail);
     uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bar + 1);
     volatile int* abort_flag = reinterpret_cast<volatile int*>(tmem_slot + 1);
-    float* parts = reinterpret_cast<float*>(tail + 64);  // [16] warps, then [8] CTAs
+    float2* parts = reinterpret_cast<float2*>(tail + 64);  // [16] warps, then [8] CTAs
     const int tid = threadIdx.x, warp = tid >> 5, lane = tid & 31;
     const int rank = C > 1 ? (int)cluster_rank() : 0;
     const int64_t mat = blockIdx.x / C;
@@ -441,7 +441,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
     constexpr int E = Vec16<T>::E;
     const T* src = static_cast<const T*>(a.m) + mat * a.stride + (a.tall ? c0 * a.ld : c0);
     const int len = a.tall ? m : nc, lines = a.tall ? nc : m;      // of this CTA's slice as it lies in memory
-    float s = 0.0f;
+    float s = 0.0f, sf = 0.0f;       // sums of squares, of the values and of them times kFar
     if (len > 0) {
         RowWalk at(tid, kOsThreads, (len + E - 1) / E);
         while (at.row < lines) {
@@ -463,6 +463,7 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
                     if (pos[u] + j >= len) continue;
                     const float f = as_float(v[u].v[j]);
                     s = fmaf(f, f, s);
+                    if (sizeof(T) < 8) sf = fmaf(f * kFar, f * kFar, sf);
                     const int r = a.tall ? pos[u] + j : line[u], c = a.tall ? line[u] : pos[u] + j;
                     const uint32_t o = (uint32_t)(c >> 6) * 16384 + sw_chunk(r, (c & 63) >> 3) + (c & 7) * 2;
                     *reinterpret_cast<uint16_t*>(xh + o) = (uint16_t)(__float_as_uint(f) >> 16);
@@ -471,41 +472,29 @@ __global__ void __launch_bounds__(kOsThreads, 1) k_orth_small(const OsArgs a) {
             }
         }
     }
-    // over the threads and the cluster
-    const auto total = [&](float t) {
 #pragma unroll
-        for (int d = 16; d > 0; d >>= 1) t += __shfl_xor_sync(0xffffffffu, t, d);
-        if (lane == 0) parts[warp] = t;
-        __syncthreads();
-        t = 0.0f;
-        for (int w = 0; w < 16; ++w) t += parts[w];
-        if constexpr (C > 1) {
-            cluster_barrier();       // every CTA of the cluster runs, and has read what an earlier total left
-            if (tid < C) {
-                const uint32_t to = remote_smem(smem_u32(parts + 16 + rank), (uint32_t)tid);
-                asm volatile("st.shared::cluster.f32 [%0], %1;" ::"r"(to), "f"(t) : "memory");
-            }
-            cluster_barrier();
-            t = 0.0f;
-            for (int r = 0; r < C; ++r) t += parts[16 + r];
-        }
-        return t;
-    };
-    s = total(s);
-    const bool far = sizeof(T) < 8 && is_far(s);     // alike in the whole cluster
-    if (far) {
-        __syncthreads();             // the warps' parts are read
-        s = 0.0f;
-        for (int i = tid; i < a.nb * 8192; i += kOsThreads) {
-            const uint32_t hi = reinterpret_cast<const uint16_t*>(xh)[i], lo = reinterpret_cast<const uint16_t*>(xl)[i];
-            const float v = __uint_as_float(hi << 16 | lo) * kFar;
-            s = fmaf(v, v, s);
-        }
-        s = total(s);
+    for (int d = 16; d > 0; d >>= 1) {
+        s += __shfl_xor_sync(0xffffffffu, s, d);
+        if (sizeof(T) < 8) sf += __shfl_xor_sync(0xffffffffu, sf, d);
     }
+    if (lane == 0) parts[warp] = make_float2(s, sf);
+    __syncthreads();
+    s = sf = 0.0f;
+    for (int w = 0; w < 16; ++w) s += parts[w].x, sf += parts[w].y;
+    if constexpr (C > 1) {
+        cluster_barrier();       // every CTA of the cluster runs
+        if (tid < C) {
+            const uint32_t to = remote_smem(smem_u32(parts + 16 + rank), (uint32_t)tid);
+            asm volatile("st.shared::cluster.v2.f32 [%0], {%1, %2};" ::"r"(to), "f"(s), "f"(sf) : "memory");
+        }
+        cluster_barrier();
+        s = sf = 0.0f;
+        for (int r = 0; r < C; ++r) s += parts[16 + r].x, sf += parts[16 + r].y;
+    }
+    const bool far = sizeof(T) < 8 && is_far(s);
     int e;
-    float left, full, f0;            // see k_orth_pack
-    f0 = norm_inverse<T>(s, far, &left, &e, &full) ? ldexpf(a.mul, e) : a.mul * full;
+    float left, full;            // see k_orth_pack
+    const float f0 = norm_inverse<T>(far ? sf : s, far, &left, &e, &full) ? ldexpf(a.mul, e) : a.mul * full;
     for (int i = tid; i < a.nb * 1024; i += kOsThreads) {
         const uint4 hv = reinterpret_cast<const uint4*>(xh)[i], lv = reinterpret_cast<const uint4*>(xl)[i];
         const uint32_t hr[4] = {hv.x, hv.y, hv.z, hv.w}, lr[4] = {lv.x, lv.y, lv.z, lv.w};
