@@ -545,6 +545,13 @@ __global__ void __launch_bounds__(256) k_xent_dx(const float* c, int64_t ldc, in
     }
 }
 
+// A weight gradient of zeros (of an empty batch) into rows ld apart.
+__global__ void __launch_bounds__(256) k_xent_zero(uint16_t* dw, int64_t ld, int64_t rows, int cols) {
+    pdl_wait();
+    RowWalk at(blockIdx.x * (int64_t)256 + threadIdx.x, (int64_t)gridDim.x * 256, cols);
+    for (; at.row < rows; at.next()) dw[at.row * ld + at.part] = 0;
+}
+
 // What the backward takes of x and gout: rows that are left out become zeros, so that an
 // infinity or NaN in them meets no weight gradient (0 times it is NaN); the others
 // x gout_i / ref, ref = the largest |gout| of the rows with a label, so that no factor is above 1 whatever the
@@ -867,8 +874,13 @@ nitro_status nitro_xent_backward(nitro_xent* h, const void* x, int x_type, int64
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int F = h->features, V = h->classes;
     if (rows == 0) {   // an empty batch has a weight gradient of zero
-        for (int64_t v = 0; dw && v < V; v += lddw == F ? V : 1)
-            TRY(cudaMemsetAsync(dw + v * lddw, 0, sizeof(uint16_t) * F * (size_t)(lddw == F ? V : 1), s));
+        if (dw && lddw == F) {
+            TRY(cudaMemsetAsync(dw, 0, sizeof(uint16_t) * (size_t)V * F, s));
+        } else if (dw) {
+            static std::atomic<int> resident{0};
+            ProfScope ps(K_XENT_DW, s, 0.0, 2.0 * V * F);
+            TRY(launch_k(k_xent_zero, dim3(one_wave(k_xent_zero, resident, (int64_t)V * F)), dim3(256), 0, s, dw, lddw, (int64_t)V, F));
+        }
         return NITRO_OK;
     }
     if (!dx && !dw) return NITRO_OK;
