@@ -35,7 +35,7 @@ namespace {
 template <typename T>
 bool dalloc(std::vector<void*>& allocs, T** p, size_t count) {
     void* q = nullptr;
-    if (cudaMalloc(&q, (count ? count : 1) * sizeof(T)) != cudaSuccess) return false;
+    if (!allocated(cudaMalloc(&q, (count ? count : 1) * sizeof(T)))) return false;
     allocs.push_back(q);
     *p = static_cast<T*>(q);
     return true;

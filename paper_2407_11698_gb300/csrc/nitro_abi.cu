@@ -85,7 +85,7 @@ template <typename T>
 bool dalloc(nitro_block* b, T** p, size_t count) {
     void* q = nullptr;
     if (count == 0) count = 1;
-    if (cudaMalloc(&q, count * sizeof(T)) != cudaSuccess) return false;
+    if (!allocated(cudaMalloc(&q, count * sizeof(T)))) return false;
     b->allocs.push_back(q);
     *p = static_cast<T*>(q);
     return true;
@@ -280,7 +280,7 @@ nitro_status nitro_init_block(const nitro_block_desc* desc, uint64_t seed, void*
     if (ok) {
         b->sse = reinterpret_cast<unsigned long long*>(b->words + sse_word(desc->n_layers));
         void* h = nullptr;
-        ok = cudaMallocHost(&h, sizeof(uint32_t) * n_words(desc->n_layers)) == cudaSuccess;
+        ok = allocated(cudaMallocHost(&h, sizeof(uint32_t) * n_words(desc->n_layers)));
         if (ok) {
             b->host_allocs.push_back(h);
             b->words_host = static_cast<uint32_t*>(h);

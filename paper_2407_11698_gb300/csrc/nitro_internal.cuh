@@ -426,6 +426,14 @@ inline cudaError_t once_per_device(std::atomic<uint64_t>& done, int dev, F&& f) 
     return e;
 }
 
+// Whether an allocation was made.  One that was refused leaves an error behind, which the next launch of anybody would
+// take for its own: it is taken back.
+inline bool allocated(cudaError_t e) {
+    if (e == cudaSuccess) return true;
+    cudaGetLastError();
+    return false;
+}
+
 // Clears n bytes on s the first time that a handle runs; its kernels keep them clean from
 // then on.  (A clear at creation would queue on the default stream, and could still be
 // waiting there when the handle is used on another; a stream of its own to wait for

@@ -322,7 +322,7 @@ nitro_status nitro_prep_create(nitro_prep** out) {
     int dev = 0;
     bool ok = cudaGetDevice(&dev) == cudaSuccess &&
               cudaDeviceGetAttribute(&p->sms, cudaDevAttrMultiProcessorCount, dev) == cudaSuccess &&
-              cudaMalloc(&p->st, sizeof(PrepState) + (size_t)p->sms * kCtasPerSm * 32) == cudaSuccess;
+              allocated(cudaMalloc(&p->st, sizeof(PrepState) + (size_t)p->sms * kCtasPerSm * 32));
     if (!ok) {
         if (p->st) cudaFree(p->st);
         delete p;

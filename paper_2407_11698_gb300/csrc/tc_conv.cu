@@ -1555,7 +1555,7 @@ inline int grid1d(int64_t n) {
 template <typename T>
 bool dalloc(std::vector<void*>& allocs, T** p, size_t count) {
     void* q = nullptr;
-    if (cudaMalloc(&q, (count ? count : 1) * sizeof(T)) != cudaSuccess) return false;
+    if (!allocated(cudaMalloc(&q, (count ? count : 1) * sizeof(T)))) return false;
     allocs.push_back(q);
     *p = static_cast<T*>(q);
     return true;
@@ -1702,7 +1702,7 @@ bool tc_layer_init(TcLayer& t, const LayerGeom& g, int max_batch, bool has_dgrad
     if (ok && (t.fwd || t.dgrad)) ok = dalloc(allocs, &t.w_planes, (size_t)kMaxLimbs * nwk);
     if (ok) {
         void* h = nullptr;
-        ok = cudaMallocHost(&h, 2 * sizeof(uint32_t)) == cudaSuccess;
+        ok = allocated(cudaMallocHost(&h, 2 * sizeof(uint32_t)));
         if (ok) {
             host_allocs.push_back(h);
             t.max_host = static_cast<uint32_t*>(h);
@@ -1736,7 +1736,7 @@ bool tc_linear_init(TcLayer& t, const LayerGeom& g, int max_batch, uint16_t* act
     bool ok = dalloc(allocs, &t.d_nhwc, (size_t)kMaxLimbs * max_batch * g.cout);
     if (ok) {
         void* h = nullptr;
-        ok = cudaMallocHost(&h, 2 * sizeof(uint32_t)) == cudaSuccess;
+        ok = allocated(cudaMallocHost(&h, 2 * sizeof(uint32_t)));
         if (ok) {
             host_allocs.push_back(h);
             t.max_host = static_cast<uint32_t*>(h);

@@ -249,7 +249,7 @@ struct DeviceAllocs {
     template <typename T>
     bool take(T** p, int64_t count) {
         void* q = nullptr;
-        if (n == 12 || cudaMalloc(&q, (size_t)count * sizeof(T)) != cudaSuccess) return false;
+        if (n == 12 || !allocated(cudaMalloc(&q, (size_t)count * sizeof(T)))) return false;
         at[n++] = q;
         *p = static_cast<T*>(q);
         return true;
@@ -267,7 +267,7 @@ struct StatusWord {
     uint32_t* at = nullptr;
     bool take() {
         void* q = nullptr;
-        if (cudaMallocHost(&q, sizeof(uint32_t)) != cudaSuccess) return false;
+        if (!allocated(cudaMallocHost(&q, sizeof(uint32_t)))) return false;
         at = static_cast<uint32_t*>(q);
         *at = 0;
         return true;
