@@ -5,13 +5,14 @@
 //
 // The logits are never kept.  The forward's products leave, for every row and tile, the
 // maximum and the sum of exponentials of the tile's columns, and a second kernel joins
-// them.  The backward walks over pieces of the classes: the products again, G of the
-// piece in bf16 from the row's log-sum, then the two products with it; dx sums over the
-// pieces in 32 bits.  The products are those of k_head_gemm (head_gemm.cuh), 2 rows
-// features classes operations each: one in the forward, three in the backward, of which
-// one is the logits' second time.  Keeping them instead would write and read 8 bytes a
-// logit more in 32 bits (16-bit logits are off by 2^-9 of their size, far too much under
-// an exponential).
+// them.  The backward takes the products again, writes G in bf16 from the row's log-sum, the label's
+// entry from the row's other ones (EpiProb), and takes the two products with it.  Where G would pass 4 GB it goes by
+// pieces of the classes, over which dx sums in 32 bits.  The products are those of k_head_gemm
+// (head_gemm.cuh), 2 rows features classes operations each: one in the forward, three in the
+// backward, of which one is the logits' second time, a fifth to a quarter of a step.  (Two calls share nothing but
+// lse.  One call for both could keep exponentials of the distance to a tile's maximum, 2 bytes a
+// logit in fp16, instead; 32-bit logits would be 4, and 16-bit ones are off by 2^-9 of their size, far too
+// much under an exponential.)
 //
 // A forward of a few rows, a server's, runs on the CUDA cores (k_xent_few).
 //
@@ -673,9 +674,10 @@ int64_t round_up(int64_t v, int64_t to) { return (v + to - 1) / to * to; }
 constexpr int kRowsWithLow = 32;
 
 // The tensor cores drop the bits that a sum's 32 do not hold, so its error grows with the
-// additions: the loss is off by 5.6e-7 of it with 2048 features and, in one sum, 1.2e-6 with 3850.  From
-// here on the logits are summed in two halves, added with rounding (at 8192 x 4096 x 32000
-// that takes 3 per cent more time).
+// additions.  The loss of some hundred rows is off, of its size, in one sum by 3.6e-7 with 1024 features, 5.4e-7 with 1536,
+// 7.2e-7 with 2000, 9.1e-7 with 2560, 1.25e-6 with 3500 and 1.46e-6 with 4096; in two halves, added with
+// rounding, by half of that.  Halves from here on keep it below 7.5e-7 up to 4096 features; at 8192 x 4096 x
+// 32000 they take 3 per cent more time.
 constexpr int kFoldFeatures = 2048;
 
 // Parts of all rows that the forward's last CTA still joins by itself; more go to a launch of
@@ -692,8 +694,9 @@ constexpr int64_t kFewProducts = (int64_t)8 << 20;
 constexpr int kFewCtas = 512;      // at most
 
 // Rows that every CTA of k_xent_pack goes through for the largest |gout|; more are gone through once, by a launch
-// of up to kTopCtas.
-constexpr int kRowsInPack = 1024;
+// of up to kTopCtas.  A backward for dw of 512 features and 64 classes, us, gone through by every CTA and by a launch:
+// 1000 rows 18.9 and 19.3, 2000 20.3 and 20.3, 4000 22.3 and 21.9, 8192 26.6 and 25.3, 65536 131 and 96.
+constexpr int kRowsInPack = 2048;
 constexpr int kTopCtas = 64;
 
 // G: at most 4 GB.  Beyond that the classes go in pieces, whose rows' sums have to be known before the first
