@@ -461,6 +461,85 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
 nitro_status nitro_mx4_status(nitro_mx4* h, int clear);
 void nitro_mx4_destroy(nitro_mx4* h);
 
+/* Activations of the two operators below: u, max(u, 0), u / (1 + exp(-u)), and u times the
+ * normal distribution at u. */
+typedef enum { NITRO_ACT_NONE = 0, NITRO_ACT_RELU = 1, NITRO_ACT_SILU = 2, NITRO_ACT_GELU = 3 } nitro_act;
+
+/* Group norm with an activation on channels-last maps x [samples x pixels x channels]: mean and
+ * variance (over the count, no correction) of a sample's group of channels / groups neighbouring channels over all
+ * pixels, h = (x - mean) / sqrt(var + eps), u = gamma h + beta, y = act(u).  gamma, beta:
+ * fp32 [channels], NULL for ones, zeros.  x: NITRO_I8 (a block's activations), NITRO_BF16 or NITRO_F32; pixels
+ * ldx elements apart, samples stride_x.
+ *
+ * forward: y in NITRO_BF16 or NITRO_F32; mean, rstd (1 / sqrt(var + eps)): fp32 [samples x groups], both or neither NULL.
+ * y may be x itself where type and strides are the same, and must not overlap it otherwise.
+ * backward, from mean and rstd of a forward on the same inputs and dy (NITRO_BF16 or NITRO_F32, y_type, as is dx):
+ * dx, dgamma and dbeta (fp32 [channels], summed over samples and pixels, overwritten); any may be NULL.
+ * dx may be dy itself likewise, but not x.
+ * Statistics and sums are in 32 bits or more, in an order that the sizes fix.  With samples = 0 dgamma and dbeta are
+ * cleared.  Errors: NITRO_ERR_ARG for null handles or pointers, samples outside [0, max_samples],
+ * pixels outside [1, max_pixels], strides below the sizes (stride_x below pixels ldx with more than one sample), eps
+ * that is not above 0 and finite, another type or activation; at create sizes below 1,
+ * channels above 8192 or not a multiple of groups, more than 2^31 - 1 pixels, more than 65535 samples, or
+ * more than 2^38 values. */
+typedef struct nitro_gnorm nitro_gnorm;
+nitro_status nitro_gnorm_create(int max_samples, int max_pixels, int channels, int groups, nitro_gnorm** out);
+nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int64_t ldx, int64_t stride_x, int samples,
+                                 int pixels, const float* gamma, const float* beta, float eps, int act, void* y,
+                                 int y_type, int64_t ldy, int64_t stride_y, float* mean, float* rstd, void* stream);
+nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int64_t ldx, int64_t stride_x, int samples,
+                                  int pixels, const float* gamma, const float* beta, const float* mean,
+                                  const float* rstd, int act, const void* dy, int y_type, int64_t lddy,
+                                  int64_t stride_dy, void* dx, int64_t lddx, int64_t stride_dx, float* dgamma,
+                                  float* dbeta, void* stream);
+nitro_status nitro_gnorm_status(nitro_gnorm* h, int clear);
+void nitro_gnorm_destroy(nitro_gnorm* h);
+
+/* A gated feed-forward block: z = scale x W^T for x [rows x features] (NITRO_BF16 or NITRO_I8) and W bf16
+ * [2 hidden x features], the gate's rows first; with a = z's first `hidden` columns and b the others
+ * out = act(a) b, bf16 [rows x hidden].  The projection back is the caller's next matrix (of nitro_xent_*, say).
+ *
+ * forward: saved, fp32 [rows x 2 hidden] without gaps, gets z for a backward (NULL: not kept).
+ * backward, from saved and the gradient dout (bf16): D = [dout b act'(a), dout act(a)], dx = scale D W and
+ * dw = scale D^T x, bf16; either may be NULL.  D is rounded to bf16 (up to 32 rows: kept as two
+ * bf16 halves).  Sums are in 32 bits, in an order that the sizes fix.  With rows = 0 dw is cleared.
+ * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], strides below the sizes, another type
+ * or activation, or a scale that is not above 0 (1e30 at most). */
+typedef struct nitro_glu nitro_glu;
+nitro_status nitro_glu_create(int max_rows, int features, int hidden, nitro_glu** out);
+nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
+                               int rows, float scale, int act, uint16_t* out, int64_t ldo, float* saved, void* stream);
+nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw,
+                                int rows, float scale, int act, const float* saved, const uint16_t* dout,
+                                int64_t lddout, uint16_t* dx, int64_t lddx, uint16_t* dw, int64_t lddw, void* stream);
+nitro_status nitro_glu_status(nitro_glu* h, int clear);
+void nitro_glu_destroy(nitro_glu* h);
+
+/* The norm over many gradients, sqrt of the sum of the squares of all their values, and the gradients scaled by
+ * min(1, max_norm / norm).  The matrices are named at create, which lays out the work on the device; their
+ * values are read by every run.  in: [rows x cols], NITRO_BF16, NITRO_F32 or NITRO_I64 (nitro_block_grad_device), rows ld_in
+ * elements apart; out (NULL: this one is not written): the same type, ld_out apart, may be `in` itself with the
+ * same ld.  The pointers must stay valid while the handle runs.
+ *
+ * run: norm (fp32, one value) is written, and with max_norm > 0 every out = in min(1, max_norm / norm), rounded once;
+ * with max_norm = 0 the norm alone is taken.  A sum of squares that is not finite (its norm is written: NaN or infinity)
+ * scales by 1.  A norm beyond fp32 or the squares' range is no such sum: squares are taken in three ranges.  The sum is
+ * in 64 bits over values' sums in 32, in an order that the handle's sizes fix.
+ * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, 2^20], sizes below 0, strides below the columns
+ * (with rows above 1), another type, int64 with an out, more than 2^40 values, an out that overlaps another
+ * matrix, or in otherwise than by being it; max_norm below 0 or NaN, or above 0 where no matrix has an out. */
+typedef struct nitro_clip nitro_clip;
+typedef struct {
+    const void* in;
+    void* out;
+    int64_t rows, cols, ld_in, ld_out;
+    int type;
+} nitro_clip_matrix;
+nitro_status nitro_clip_create(const nitro_clip_matrix* list, int count, nitro_clip** out);
+nitro_status nitro_clip_run(nitro_clip* h, float max_norm, float* norm, void* stream);
+nitro_status nitro_clip_status(nitro_clip* h, int clear);
+void nitro_clip_destroy(nitro_clip* h);
+
 /* ---- Diagnostics (not part of the training step) -------------------------
  * Every kernel launch of the library is counted.  With profiling on, each
  * launch is also bracketed by CUDA events recorded on its own stream and

@@ -20,6 +20,7 @@ NITRO_ROUND_FLOOR, NITRO_ROUND_TRUNC = 0, 1
 STATUS_BIT_OVERFLOW, STATUS_BIT_BAD_LABEL, STATUS_BIT_TIMEOUT = 1, 2, 4
 NITRO_CONTRACT_FWD, NITRO_CONTRACT_WGRAD, NITRO_CONTRACT_DGRAD = 0, 1, 2
 NITRO_BF16, NITRO_I8, NITRO_F32, NITRO_I64 = range(4)
+NITRO_ACT_NONE, NITRO_ACT_RELU, NITRO_ACT_SILU, NITRO_ACT_GELU = range(4)
 (NITRO_T_W, NITRO_T_DW, NITRO_T_WLR, NITRO_T_DWLR, NITRO_T_ACT, NITRO_T_REGION,
  NITRO_T_ARGMAX, NITRO_T_DELTA, NITRO_T_GRAD_L, NITRO_T_SSE, NITRO_T_LR_IN, NITRO_T_LR_ARGMAX,
  NITRO_T_STEP) = range(13)
@@ -35,6 +36,12 @@ TENSOR_DTYPE = {
 class nitro_layer_desc(ctypes.Structure):
     _fields_ = [("kind", ctypes.c_int), ("cin", ctypes.c_int), ("cout", ctypes.c_int),
                 ("h", ctypes.c_int), ("w", ctypes.c_int), ("pool2x2", ctypes.c_int)]
+
+
+class nitro_clip_matrix(ctypes.Structure):
+    _fields_ = [("in_", ctypes.c_void_p), ("out", ctypes.c_void_p), ("rows", ctypes.c_int64),
+                ("cols", ctypes.c_int64), ("ld_in", ctypes.c_int64), ("ld_out", ctypes.c_int64),
+                ("type", ctypes.c_int)]
 
 
 class nitro_block_desc(ctypes.Structure):
@@ -140,7 +147,16 @@ def lib():
     L.nitro_mx4_dequantize.argtypes = [_VP, _VP, _I, _I, _VP, _I, _L, _VP, _VP]
     L.nitro_mx4_create.argtypes = [_I, _I, _I, ctypes.POINTER(_VP)]
     L.nitro_mx4_linear.argtypes = [_VP, _VP, _I, _L, _I, _VP, _VP, _VP, _I, _L, _VP]
-    for op in ("xent", "orth", "mx4"):
+    L.nitro_gnorm_create.argtypes = [_I, _I, _I, _I, ctypes.POINTER(_VP)]
+    L.nitro_gnorm_forward.argtypes = [_VP, _VP, _I, _L, _L, _I, _I, _VP, _VP, _F, _I, _VP, _I, _L, _L, _VP, _VP, _VP]
+    L.nitro_gnorm_backward.argtypes = [_VP, _VP, _I, _L, _L, _I, _I, _VP, _VP, _VP, _VP, _I, _VP, _I, _L, _L, _VP, _L, _L, _VP,
+                                       _VP, _VP]
+    L.nitro_glu_create.argtypes = [_I, _I, _I, ctypes.POINTER(_VP)]
+    L.nitro_glu_forward.argtypes = [_VP, _VP, _I, _L, _VP, _L, _I, _F, _I, _VP, _L, _VP, _VP]
+    L.nitro_glu_backward.argtypes = [_VP, _VP, _I, _L, _VP, _L, _I, _F, _I, _VP, _VP, _L, _VP, _L, _VP, _L, _VP]
+    L.nitro_clip_create.argtypes = [ctypes.POINTER(nitro_clip_matrix), _I, ctypes.POINTER(_VP)]
+    L.nitro_clip_run.argtypes = [_VP, _F, _VP, _VP]
+    for op in ("xent", "orth", "mx4", "gnorm", "glu", "clip"):
         getattr(L, "nitro_%s_status" % op).argtypes = [_VP, _I]
         getattr(L, "nitro_%s_status" % op).restype = _I
         getattr(L, "nitro_%s_create" % op).restype = _I
@@ -148,6 +164,7 @@ def lib():
         getattr(L, "nitro_%s_destroy" % op).restype = None
     for name in ("nitro_xent_forward", "nitro_xent_backward", "nitro_orth_run", "nitro_mx4_bytes",
                  "nitro_mx4_quantize", "nitro_mx4_dequantize", "nitro_mx4_linear",
+                 "nitro_gnorm_forward", "nitro_gnorm_backward", "nitro_glu_forward", "nitro_glu_backward", "nitro_clip_run",
                  "nitro_conv3x3_create", "nitro_conv3x3_contract", "nitro_conv3x3_status",
                  "nitro_gemm_create", "nitro_gemm_run", "nitro_gemm_status",
                  "nitro_prep_create", "nitro_prep_fit", "nitro_prep_apply", "nitro_prep_stats"):
@@ -696,3 +713,162 @@ class Mx4Linear(_Handle):
         if st != NITRO_OK:
             raise NitroError(st, "nitro_mx4_linear")
         return y
+
+
+def _map(t, shape, allowed, what):
+    """(address, type, pixel stride, sample stride) of a CUDA map [samples x pixels x channels] whose channels are
+    contiguous."""
+    code = _code(t)
+    if code not in allowed or not t.is_cuda or t.shape != shape:
+        raise ValueError("%s must be a CUDA tensor %s of a supported type, not %s %s on %s"
+                         % (what, list(shape), tuple(t.shape), t.dtype, t.device))
+    n, p, c = shape
+    stride, ld, step = t.stride()
+    if step != 1 and c > 1:
+        raise ValueError("the channels of %s must be contiguous" % what)
+    # the strides of a lone pixel or sample are never used
+    if p <= 1:
+        ld = c
+    return t.data_ptr(), code, ld, stride if n > 1 else p * ld
+
+
+_GN_X, _GN_Y = (NITRO_I8, NITRO_BF16, NITRO_F32), (NITRO_BF16, NITRO_F32)
+
+
+class GroupNorm(_Handle):
+    """Group norm with an activation (NITRO_ACT_*) on channels-last maps [samples x pixels x channels];
+    gamma and beta: fp32 [channels], None for ones and zeros."""
+    _op = "gnorm"
+
+    def __init__(self, max_samples, max_pixels, channels, groups):
+        self.channels, self.groups = int(channels), int(groups)
+        self._create(max_samples, max_pixels, channels, groups)
+
+    def _param(self, t, what):
+        return None if t is None else _vector(t, self.channels, NITRO_F32, what)
+
+    def _stat(self, t, n, what):
+        return None if t is None else _vector(t, n * self.groups, NITRO_F32, what)
+
+    def forward(self, x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, act=NITRO_ACT_NONE, stream=None):
+        """Writes y (bf16 or fp32) and, if given, mean and rstd (fp32 [samples x groups]); x: int8, bf16 or fp32."""
+        n, p = x.shape[0], x.shape[1]
+        shape = (n, p, self.channels)
+        xp, xt, ldx, sx = _map(x, shape, _GN_X, "x")
+        yp, yt, ldy, sy = _map(y, shape, _GN_Y, "y")
+        st = lib().nitro_gnorm_forward(self.h, xp, xt, ldx, sx, n, p, self._param(gamma, "gamma"), self._param(beta, "beta"),
+                                       eps, act, yp, yt, ldy, sy, self._stat(mean, n, "mean"), self._stat(rstd, n, "rstd"),
+                                       _stream_int(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_gnorm_forward")
+        return y
+
+    def backward(self, x, gamma, beta, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, act=NITRO_ACT_NONE, stream=None):
+        """Writes dx (of dy's type), dgamma and dbeta (fp32 [channels]), each unless None, from mean and rstd of a
+        forward on the same inputs."""
+        n, p = x.shape[0], x.shape[1]
+        shape = (n, p, self.channels)
+        xp, xt, ldx, sx = _map(x, shape, _GN_X, "x")
+        gp, gt, ldg, sg = _map(dy, shape, _GN_Y, "dy")
+        dp, _, ldd, sd = (None, gt, ldg, sg) if dx is None else _map(dx, shape, (gt,), "dx")
+        st = lib().nitro_gnorm_backward(self.h, xp, xt, ldx, sx, n, p, self._param(gamma, "gamma"), self._param(beta, "beta"),
+                                        self._stat(mean, n, "mean"), self._stat(rstd, n, "rstd"), act, gp, gt, ldg, sg, dp, ldd, sd,
+                                        self._param(dgamma, "dgamma"), self._param(dbeta, "dbeta"), _stream_int(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_gnorm_backward")
+        return dx, dgamma, dbeta
+
+
+class GatedLinear(_Handle):
+    """out = act(a) b of z = [a b] = scale x W^T, W bf16 [2 hidden x features], the gate's rows first; x: bf16 or
+    int8 [rows x features]."""
+    _op = "glu"
+
+    def __init__(self, max_rows, features, hidden):
+        self.features, self.hidden = int(features), int(hidden)
+        self._create(max_rows, features, hidden)
+
+    def _inputs(self, x, w, scale, act):
+        n = x.shape[0]
+        xp, xt, ldx = _matrix(x, n, self.features, _X, "x")
+        wp, _, ldw = _matrix(w, 2 * self.hidden, self.features, _W, "w")
+        return n, (xp, xt, ldx, wp, ldw, n, scale, act)
+
+    def forward(self, x, w, out, saved=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
+        """Writes out (bf16 [rows x hidden]) and, for a backward, z to saved (fp32 [rows x 2 hidden])."""
+        n, a = self._inputs(x, w, scale, act)
+        op, _, ldo = _matrix(out, n, self.hidden, _W, "out")
+        st = lib().nitro_glu_forward(self.h, *a, op, ldo,
+                                     None if saved is None else _vector(saved, 2 * n * self.hidden, NITRO_F32, "saved"),
+                                     _stream_int(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_glu_forward")
+        return out
+
+    def backward(self, x, w, saved, dout, dx=None, dw=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
+        """Writes dx [rows x features] and dw [2 hidden x features] (bf16; either may be None) from the
+        gradient dout (bf16 [rows x hidden]) and the saved of a forward on the same inputs."""
+        n, a = self._inputs(x, w, scale, act)
+        gp, _, ldg = _matrix(dout, n, self.hidden, _W, "dout")
+        dxp = dwp = None
+        lddx = lddw = self.features
+        if dx is not None:
+            dxp, _, lddx = _matrix(dx, n, self.features, _W, "dx")
+        if dw is not None:
+            dwp, _, lddw = _matrix(dw, 2 * self.hidden, self.features, _W, "dw")
+        st = lib().nitro_glu_backward(self.h, *a, _vector(saved, 2 * n * self.hidden, NITRO_F32, "saved"), gp, ldg, dxp, lddx,
+                                      dwp, lddw, _stream_int(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_glu_backward")
+        return dx, dw
+
+
+class GradClip(_Handle):
+    """The norm over the values of all `grads` (bf16, fp32, or int64 where it is not scaled), and each scaled by
+    min(1, max_norm / norm) into its tensor of `outs` (None: not written; grads themselves: in
+    place).  Tensors are contiguous, or matrices with contiguous rows.  The handle keeps them and reads their
+    values at every run."""
+    _op = "clip"
+
+    def __init__(self, grads, outs=None):
+        grads = list(grads)
+        outs = [None] * len(grads) if outs is None else list(outs)
+        if len(outs) != len(grads):
+            raise ValueError("as many outs as grads")
+        self.tensors = grads, outs
+        table = (nitro_clip_matrix * max(1, len(grads)))()
+        for m, g, o in zip(table, grads, outs):
+            code = _code(g)
+            if code not in _ORTH or not g.is_cuda:
+                raise ValueError("gradients must be CUDA tensors of a supported type, not %s on %s" % (g.dtype, g.device))
+            if o is not None and (o.shape != g.shape or o.dtype != g.dtype or not o.is_cuda):
+                raise ValueError("an out must be as its gradient, %s %s, not %s %s on %s"
+                                 % (tuple(g.shape), g.dtype, tuple(o.shape), o.dtype, o.device))
+            both = (g,) if o is None else (g, o)
+            if all(t.is_contiguous() for t in both):
+                m.rows, m.cols = 1, g.numel()
+                m.ld_in = m.ld_out = m.cols
+            elif g.dim() == 2:
+                m.rows, m.cols = g.shape
+                for t in both:
+                    if t.stride(1) != 1 and m.cols > 1:
+                        raise ValueError("the rows of a matrix must be contiguous")
+                m.ld_in, m.ld_out = g.stride(0), both[-1].stride(0)
+            else:
+                raise ValueError("a gradient must be contiguous, or a matrix with contiguous rows")
+            m.in_, m.type = g.data_ptr(), code
+            m.out = None if o is None else o.data_ptr()
+        self.h = _VP()
+        st = lib().nitro_clip_create(table, len(grads), ctypes.byref(self.h))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_clip_create")
+
+    def run(self, norm, max_norm=None, stream=None):
+        """Writes the norm (fp32, one value) and with max_norm (above 0) the outs; returns norm."""
+        if max_norm is not None and not max_norm > 0:
+            raise ValueError("max_norm must be above 0")
+        st = lib().nitro_clip_run(self.h, 0.0 if max_norm is None else max_norm, _vector(norm, 1, NITRO_F32, "norm"),
+                                  _stream_int(stream))
+        if st != NITRO_OK:
+            raise NitroError(st, "nitro_clip_run")
+        return norm

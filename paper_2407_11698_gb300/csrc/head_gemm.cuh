@@ -267,6 +267,11 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
     }
 }
 
+// Whether an epilogue takes two planes of B in turns of 16 rows: columns 32 i .. 32 i + 15 of D are then rows
+// 16 i .. 16 i + 15 of the first plane, and the 16 columns after them the same rows of the second.
+template <class Epi>
+constexpr bool hg_pairs = false;
+
 // Epi: struct Args, and per tile and thread
 //   Epi(args, g, tile, part)
 //   void fetch(c)           starts loading what cols(c) needs (called for c = 0; cols(c)
@@ -366,6 +371,10 @@ __global__ void __launch_bounds__(kHgThreads, 1)
 #pragma unroll
                             for (int j = 0; j < C::B_ROWS / 64; ++j)
                                 hg_tma<CG>(dst + j * 8192, &tmB, fb, n0 + 64 * j, kb * kHgBK, z);
+                        } else if constexpr (hg_pairs<Epi>) {
+#pragma unroll
+                            for (int j = 0; j < C::B_ROWS / 32; ++j)
+                                hg_tma<CG>(dst + j * 4096, &tmB, fb, kb * kHgBK, n0 / 2 + 16 * j, 0);
                         } else {
                             hg_tma<CG>(dst, &tmB, fb, kb * kHgBK, n0, z);
                         }
@@ -578,12 +587,12 @@ struct HgOperand {
     int64_t inner, outer, ld, planes, plane;   // plane: elements from one plane to the next
 };
 
-inline bool hg_map(CUtensorMap* m, const HgOperand& o, bool f16, int box_outer) {
+inline bool hg_map(CUtensorMap* m, const HgOperand& o, bool f16, int box_outer, int box_planes = 1) {
     auto fn = encode_fn();
     if (!fn) return false;
     cuuint64_t dim[3] = {(cuuint64_t)o.inner, (cuuint64_t)o.outer, (cuuint64_t)o.planes};
     cuuint64_t stride[2] = {(cuuint64_t)o.ld * 2, (cuuint64_t)(o.planes > 1 ? o.plane : o.ld * o.outer) * 2};
-    cuuint32_t box[3] = {64, (cuuint32_t)box_outer, 1}, step[3] = {1, 1, 1};
+    cuuint32_t box[3] = {64, (cuuint32_t)box_outer, (cuuint32_t)box_planes}, step[3] = {1, 1, 1};
     return fn(m, f16 ? CU_TENSOR_MAP_DATA_TYPE_FLOAT16 : CU_TENSOR_MAP_DATA_TYPE_BFLOAT16, 3, const_cast<void*>(o.base),
               dim, stride, box, step, CU_TENSOR_MAP_INTERLEAVE_NONE, CU_TENSOR_MAP_SWIZZLE_128B,
               CU_TENSOR_MAP_L2_PROMOTION_L2_256B, CU_TENSOR_MAP_FLOAT_OOB_FILL_NONE) == CUDA_SUCCESS;
@@ -659,7 +668,9 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
                          cudaStream_t s) {
     using C = HgCfg<CG, BN, HA, HB>;
     CUtensorMap ma, mb;
-    if (!hg_map(&ma, a, F16, AMN ? 64 : 128) || !hg_map(&mb, b, F16, BMN ? 64 : C::B_ROWS)) return cudaErrorInvalidValue;
+    static_assert(!hg_pairs<Epi> || (!BMN && HB == 1), "pairs of planes go along K");
+    if (!hg_map(&ma, a, F16, AMN ? 64 : 128)) return cudaErrorInvalidValue;
+    if (!(hg_pairs<Epi> ? hg_map(&mb, b, F16, 16, 2) : hg_map(&mb, b, F16, BMN ? 64 : C::B_ROWS))) return cudaErrorInvalidValue;
     HgArgs g{};
     g.M = (int)p.M;
     g.N = (int)p.N;

@@ -1,0 +1,483 @@
+// A gated feed-forward block: z = scale x W^T, W's first `hidden` rows the gate's, out = act(a) b with
+// z = [a b], and its gradients
+//   D = [dout b act'(a), dout act(a)],   dx = scale D W,   dW = scale D^T x.
+//
+// The forward is one product (head_gemm.cuh) whose tiles hold gate and up columns in turns of 16, so that the
+// epilogue has both of a unit in one thread: z goes through memory only as what the backward keeps of it, 32 bits a
+// value (8 rows hidden bytes each way, beside 12 rows hidden features operations; 16 bits would
+// put a rounding of 2^-9 under both gradients, and taking the products again costs a third of a step).
+// The backward writes D in bf16, which both products with it take.  4 rows hidden features operations forward and
+// 8 backward.  Few rows run on the CUDA cores, where W's bytes bound them (k_glu_few).
+#include <new>
+
+#include "head_act.cuh"
+
+using namespace nitro;
+
+namespace nitro {
+namespace {
+
+// out and saved of a tile: columns come in turns of 16 gates and the 16 ups of the same units.
+struct EpiGlu {
+    static constexpr bool kFold = true, kTail = false;
+    struct Args {
+        uint16_t* out;
+        int64_t ldo;
+        float* saved;         // or null
+        int vec, vec_saved;   // rows are 16-byte aligned
+        int hidden, act;
+        float scale;
+    };
+    const Args& a;
+    const HgPart& p;
+    uint32_t kept[8];         // 16 units' outputs, until the next 16 fill their line of 64 bytes
+    __device__ __forceinline__ EpiGlu(const Args& a_, const HgArgs&, const HgTile&, const HgPart& p_) : a(a_), p(p_) {}
+    __device__ __forceinline__ void fetch(int) {}
+    // 16 values of each row, a thread's in v, to columns col.. of saved
+    __device__ __forceinline__ void save(const float* v, int unit, float* base) const {
+        uint4 w[4];
+#pragma unroll
+        for (int j = 0; j < 4; ++j)
+            w[j] = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
+        const int64_t ld = 2 * (int64_t)a.hidden;
+        if (a.vec_saved) {
+            p.stage.to_lines(w);
+            const int c = unit + 4 * p.stage.line_chunk(), row = p.row0 + p.stage.line_row(0);
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (row + 8 * i < p.rows && c < a.hidden) *reinterpret_cast<uint4*>(base + (row + 8 * i) * ld + c) = w[i];
+            return;
+        }
+        p.stage.put(w);
+        const int rows = min(32, p.rows - p.row0), c = unit + (p.stage.lane & 15);
+        for (int r = p.stage.lane >> 4; r < rows; r += 2)
+            if (c < a.hidden) base[(p.row0 + r) * ld + c] = p.stage.value<float>(r, p.stage.lane & 15);
+        __syncwarp();
+    }
+    __device__ __forceinline__ void cols(int c, float* v) {
+        const int unit = (p.col0 + c) >> 1;
+        if (unit < a.hidden) {
+#pragma unroll
+            for (int j = 0; j < 32; ++j) v[j] *= a.scale;
+            if (a.saved) {
+                save(v, unit, a.saved);
+                save(v + 16, unit, a.saved + a.hidden);
+            }
+            with_act(a.act, [&](auto act) {
+#pragma unroll
+                for (int j = 0; j < 16; ++j) v[j] = act_value<decltype(act)::value>(v[j]) * v[16 + j];
+            });
+        }
+        uint32_t w[16];
+#pragma unroll
+        for (int j = 0; j < 8; ++j) w[8 + j] = pack_bf16(v[2 * j], v[2 * j + 1]);
+        if (p.width == 32) {     // a cluster's slice: the thread's row alone
+            if (p.row >= p.rows || unit >= a.hidden) return;
+            uint16_t* dst = a.out + p.row * a.ldo + unit;
+            if (a.vec && unit + 16 <= a.hidden) {
+                reinterpret_cast<uint4*>(dst)[0] = make_uint4(w[8], w[9], w[10], w[11]);
+                reinterpret_cast<uint4*>(dst)[1] = make_uint4(w[12], w[13], w[14], w[15]);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 16; ++j)
+                    if (unit + j < a.hidden) dst[j] = (uint16_t)(w[8 + (j >> 1)] >> (16 * (j & 1)));
+            }
+        } else if (c & 32) {
+            if (unit - 16 >= a.hidden) return;
+#pragma unroll
+            for (int j = 0; j < 8; ++j) w[j] = kept[j];
+            hg_store16(p, w, a.out, a.ldo, unit - 16, a.hidden, a.vec != 0);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 8; ++j) kept[j] = w[8 + j];
+        }
+    }
+    __device__ __forceinline__ void done() {}
+};
+template <>
+constexpr bool hg_pairs<EpiGlu> = true;
+
+// ------------------------------------------------------------------ few rows
+// A warp takes C units, so 2 C rows of W (over ks warps of a CTA by pieces of 256 features, where there are few), and R
+// rows of x; its sums are exchanged so that each lane ends with one (row, unit, half).
+struct FewGluArgs {
+    int64_t ldx, ldw, ldo;
+    int rows, features, hidden, ks, act;
+    uint16_t* out;
+    float* saved;          // or null
+    float scale;
+};
+
+template <typename T, int R, int C, bool VEC>
+__global__ void __launch_bounds__(256, 2) k_glu_few(const T* x, const uint16_t* w, const FewGluArgs a) {
+    constexpr int N = 2 * R * C, kLanes = 32 / N;     // lanes that hold the same sum
+    __shared__ float sums[2][8][N];
+    pdl_wait();
+    const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
+    const int sub = warp % a.ks, per = 8 / a.ks;
+    const int groups = (a.hidden + C - 1) / C;
+    const T* xr[R];
+#pragma unroll
+    for (int r = 0; r < R; ++r) xr[r] = x + min(r, a.rows - 1) * a.ldx;
+    int turn = 0;
+    for (int g0 = blockIdx.x * per; g0 < groups; g0 += gridDim.x * per, turn ^= 1) {
+        const int first = (g0 + warp / a.ks) * C;
+        float acc[R][2 * C];
+#pragma unroll
+        for (int i = 0; i < N; ++i) acc[i / (2 * C)][i % (2 * C)] = 0.0f;
+        if (first < a.hidden) {
+            const uint16_t* wr[2 * C];
+#pragma unroll
+            for (int c = 0; c < 2 * C; ++c)
+                wr[c] = w + (min(first + c % C, a.hidden - 1) + (int64_t)(c / C) * a.hidden) * a.ldw;
+            int piece = sub * 256;
+            for (; piece + 256 <= a.features; piece += a.ks * 256)
+                few_step<T, R, 2 * C, VEC, true>(xr, wr, piece, lane, a.features, acc);
+            if (piece < a.features) few_step<T, R, 2 * C, VEC, false>(xr, wr, piece, lane, a.features, acc);
+        }
+        float z = few_sum<N>(&acc[0][0], lane);
+        if (a.ks > 1) {
+            if (lane % kLanes == 0) sums[turn][warp][lane / kLanes] = z;
+            __syncthreads();       // the other turn's sums are read by now
+            if (sub == 0) {
+                z = sums[turn][warp][lane / kLanes];
+                for (int k = 1; k < a.ks; ++k) z += sums[turn][warp + k][lane / kLanes];
+            }
+        }
+        z *= a.scale;
+        const float up = __shfl_down_sync(0xffffffffu, z, C * kLanes);
+        const int i = lane / kLanes, row = i / (2 * C), unit = first + i % C;
+        if (sub == 0 && lane % kLanes == 0 && row < a.rows && unit < a.hidden) {
+            const bool gate = i % (2 * C) < C;
+            if (a.saved) a.saved[(int64_t)row * 2 * a.hidden + (gate ? 0 : a.hidden) + unit] = z;
+            if (gate) {
+                float v = 0.0f;
+                with_act(a.act, [&](auto act) { v = act_value<decltype(act)::value>(z); });
+                a.out[row * a.ldo + unit] = __bfloat16_as_ushort(__float2bfloat16_rn(v * up));
+            }
+        }
+    }
+}
+
+// ------------------------------------------------------------------ elementwise
+// Rows as bf16 with a stride of ldp (a multiple of 8): int8 activations are exact in bf16.
+template <typename T>
+__global__ void __launch_bounds__(256) k_glu_pack(const T* x, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp) {
+    pdl_wait();
+    const int per = (int)(ldp / 8);
+    const int64_t words = rows * per, step = (int64_t)gridDim.x * 256, first = blockIdx.x * (int64_t)256 + threadIdx.x;
+    const bool vec = (((uintptr_t)x | (uintptr_t)(ldx * sizeof(T))) & (8 * sizeof(T) - 1)) == 0;
+    RowWalk at(first, step, per);
+    for (int64_t i = first; i < words; i += step, at.next()) {
+        const int c = at.part * 8;
+        const T* src = x + at.row * ldx + c;
+        uint32_t w[4] = {0, 0, 0, 0};
+        if constexpr (sizeof(T) == 2) {
+            if (vec && c + 8 <= cols) {
+                *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src);
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < cols) w[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+            }
+        } else {
+            uint32_t b[2] = {0x80808080u, 0x80808080u};   // bytes hold x + 128
+            if (vec && c + 8 <= cols) {
+                const uint2 r = *reinterpret_cast<const uint2*>(src);
+                b[0] ^= r.x;
+                b[1] ^= r.y;
+            } else {
+#pragma unroll
+                for (int j = 0; j < 8; ++j)
+                    if (c + j < cols) b[j >> 2] ^= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
+            }
+#pragma unroll
+            for (int j = 0; j < 4; ++j) w[j] = bf16x2(b[j >> 1], 2 * (j & 1));
+        }
+        reinterpret_cast<uint4*>(out)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+    }
+}
+
+// D [rows][ldd] from saved and dout, and what its rounding left over `low` elements on (0: not kept): four units a
+// thread where rows are aligned (VEC), else one.
+template <bool VEC>
+__global__ void __launch_bounds__(256) k_glu_grad(const float* saved, const uint16_t* dout, int64_t lddout, int64_t rows, int hidden,
+                                                  int act, uint16_t* D, int64_t ldd, int64_t low) {
+    pdl_wait();
+    constexpr int E = VEC ? 4 : 1;
+    const int per = hidden / E;
+    const int64_t items = rows * per, step = (int64_t)gridDim.x * 256, first = blockIdx.x * (int64_t)256 + threadIdx.x;
+    RowWalk at(first, step, per);
+    for (int64_t i = first; i < items; i += step, at.next()) {
+        const int c = at.part * E;
+        const float* z = saved + at.row * 2 * hidden + c;
+        float a[E], b[E], g[E], da[E], db[E];
+        if constexpr (VEC) {
+            *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(z);
+            *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(z + hidden);
+            const uint2 u = *reinterpret_cast<const uint2*>(dout + at.row * lddout + c);
+            g[0] = __uint_as_float(u.x << 16), g[1] = __uint_as_float(u.x & 0xffff0000u);
+            g[2] = __uint_as_float(u.y << 16), g[3] = __uint_as_float(u.y & 0xffff0000u);
+        } else {
+            a[0] = z[0], b[0] = z[hidden], g[0] = __uint_as_float((uint32_t)dout[at.row * lddout + c] << 16);
+        }
+        with_act(act, [&](auto k) {
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                const float2 v = act_slope<decltype(k)::value>(a[j]);
+                da[j] = g[j] * b[j] * v.y;
+                db[j] = g[j] * v.x;
+            }
+        });
+        uint16_t* dst = D + at.row * ldd + c;
+        for (int half = 0;; ++half) {
+            uint16_t ha[E], hb[E];
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                ha[j] = __bfloat16_as_ushort(__float2bfloat16_rn(da[j]));
+                hb[j] = __bfloat16_as_ushort(__float2bfloat16_rn(db[j]));
+            }
+            if constexpr (VEC) {
+                *reinterpret_cast<uint2*>(dst) = make_uint2(ha[0] | (uint32_t)ha[1] << 16, ha[2] | (uint32_t)ha[3] << 16);
+                *reinterpret_cast<uint2*>(dst + hidden) = make_uint2(hb[0] | (uint32_t)hb[1] << 16, hb[2] | (uint32_t)hb[3] << 16);
+            } else {
+                dst[0] = ha[0];
+                dst[hidden] = hb[0];
+            }
+            if (low == 0 || half == 1) break;
+#pragma unroll
+            for (int j = 0; j < E; ++j) {
+                da[j] -= __uint_as_float((uint32_t)ha[j] << 16);
+                db[j] -= __uint_as_float((uint32_t)hb[j] << 16);
+            }
+            dst += low;
+        }
+    }
+}
+
+// Up to this many rows D is kept as two bf16 halves: the rounding of one entry, up to 2^-8 of
+// it, can be most of a lone row's error, and averages out over more.
+constexpr int kRowsWithLow = 32;
+// Sums in two accumulators, added with rounding, from here on: the tensor cores cut off what 32 bits do not hold.
+constexpr int kFoldFeatures = 2048;
+constexpr int kFewRows = 4;
+constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices of dx: at most 64 MB together
+
+}  // namespace
+}  // namespace nitro
+
+struct nitro_glu {
+    int max_rows = 0, features = 0, hidden = 0;
+    int64_t ldp = 0, ldd = 0, acc_floats = 0;
+    uint16_t* xp = nullptr;     // [max_rows][ldp] bf16 copy of x where TMA cannot take its rows
+    uint16_t* wp = nullptr;     // [2 hidden][ldp] copy of W likewise
+    uint16_t* D = nullptr;
+    float* acc = nullptr;
+    StatusWord status;
+    DeviceAllocs allocs;
+};
+
+namespace {
+
+bool copies(const void* x, int type, int64_t ldx) { return type == NITRO_I8 || !tma_rows(x, ldx); }
+
+cudaError_t pack(const void* x, int type, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp, cudaStream_t s) {
+    static std::atomic<int> resident[2];
+    const int64_t words = rows * (ldp / 8);
+    const bool i8 = type == NITRO_I8;
+    const int grid = i8 ? one_wave(k_glu_pack<int8_t>, resident[0], words) : one_wave(k_glu_pack<uint16_t>, resident[1], words);
+    ProfScope ps(K_GLU_PACK, s, 0.0, (double)rows * cols * (i8 ? 3 : 4));
+    return i8 ? launch_k(k_glu_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp)
+              : launch_k(k_glu_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, cols, out, ldp);
+}
+
+// x and W as operands along K; copies where TMA cannot take their rows.
+cudaError_t operands(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
+                     cudaStream_t s, HgOperand* ox, HgOperand* ow) {
+    cudaError_t e = cudaSuccess;
+    *ox = {x, h->features, rows, ldx, 1, 0};
+    if (copies(x, x_type, ldx)) {
+        e = pack(x, x_type, ldx, rows, h->features, h->xp, h->ldp, s);
+        *ox = {h->xp, h->features, rows, h->ldp, 1, 0};
+    }
+    *ow = {w, h->features, 2 * (int64_t)h->hidden, ldw, 1, 0};
+    if (e == cudaSuccess && copies(w, NITRO_BF16, ldw)) {
+        e = pack(w, NITRO_BF16, ldw, 2 * (int64_t)h->hidden, h->features, h->wp, h->ldp, s);
+        *ow = {h->wp, h->features, 2 * (int64_t)h->hidden, h->ldp, 1, 0};
+    }
+    return e;
+}
+
+bool glu_args(const nitro_glu* h, const void* x, int x_type, int64_t ldx, const void* w, int64_t ldw, int rows, float scale,
+              int act) {
+    if (!h || rows < 0 || rows > h->max_rows || (x_type != NITRO_BF16 && x_type != NITRO_I8) || !act_known(act)) return false;
+    if (ldx < h->features || ldw < h->features || !(scale > 0.0f) || scale > 1e30f) return false;
+    if (rows > 0 && (!x || !w)) return false;
+    return ((uintptr_t)w & 1) == 0 && (x_type == NITRO_I8 || ((uintptr_t)x & 1) == 0);
+}
+
+template <typename T, int R, int C>
+cudaError_t few_as(bool vec, const void* x, const uint16_t* w, const FewGluArgs& a, int grid, cudaStream_t s) {
+    return vec ? launch_k(k_glu_few<T, R, C, true>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a)
+               : launch_k(k_glu_few<T, R, C, false>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a);
+}
+
+cudaError_t forward_few(const nitro_glu* h, const void* x, int x_type, const uint16_t* w, FewGluArgs a, cudaStream_t s) {
+    constexpr int C = 4;
+    // two CTAs an SM; a warp's features over as many warps as are free
+    const int ctas = 2 * sm_count(), warps = 8 * ctas, pieces = (h->features + 255) / 256;
+    const int groups = (h->hidden + C - 1) / C;
+    a.ks = 1;
+    while (a.ks < 8 && 2 * a.ks <= pieces && (int64_t)groups * 2 * a.ks <= warps) a.ks *= 2;
+    const int per = 8 / a.ks, grid = std::min(ctas, (groups + per - 1) / per);
+    const bool i8 = x_type == NITRO_I8;
+    const bool vec = tma_rows(w, a.ldw) && (i8 ? ((uintptr_t)x & 7) == 0 && a.ldx % 8 == 0 : tma_rows(x, a.ldx));
+    ProfScope ps(K_GLU_FWD, s, 4.0 * a.rows * h->hidden * h->features, 4.0 * h->hidden * h->features);
+    if (i8) return a.rows <= 1 ? few_as<int8_t, 1, C>(vec, x, w, a, grid, s) : few_as<int8_t, 4, C>(vec, x, w, a, grid, s);
+    return a.rows <= 1 ? few_as<uint16_t, 1, C>(vec, x, w, a, grid, s) : few_as<uint16_t, 4, C>(vec, x, w, a, grid, s);
+}
+
+}  // namespace
+
+extern "C" {
+
+nitro_status nitro_glu_create(int max_rows, int features, int hidden, nitro_glu** out) {
+    if (!out) return NITRO_ERR_ARG;
+    *out = nullptr;
+    if (max_rows < 1 || features < 1 || hidden < 1 || max_rows > (1 << 20) || features > (1 << 17) || hidden > (1 << 20) ||
+        (int64_t)max_rows * std::max(features, hidden) > ((int64_t)1 << 34) || (int64_t)hidden * features > ((int64_t)1 << 34))
+        return NITRO_ERR_ARG;
+    nitro_glu* h = new (std::nothrow) nitro_glu();
+    if (!h) return NITRO_ERR_CUDA;
+    h->max_rows = max_rows;
+    h->features = features;
+    h->hidden = hidden;
+    h->ldp = round_up(features, 8);
+    h->ldd = round_up(2 * (int64_t)hidden, 8);
+    h->acc_floats = std::min(16 * max_rows * round_up(features, 32), kAccFloats);
+    const bool ok = h->allocs.take(&h->xp, max_rows * h->ldp) && h->allocs.take(&h->wp, 2 * hidden * h->ldp) &&
+                    h->allocs.take(&h->D, std::max(max_rows, 2 * std::min(max_rows, kRowsWithLow)) * h->ldd) &&
+                    h->allocs.take(&h->acc, h->acc_floats) && h->status.take();
+    if (!ok) {
+        nitro_glu_destroy(h);
+        return NITRO_ERR_CUDA;
+    }
+    *out = h;
+    return NITRO_OK;
+}
+
+nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
+                               float scale, int act, uint16_t* out, int64_t ldo, float* saved, void* stream) {
+    if (!glu_args(h, x, x_type, ldx, w, ldw, rows, scale, act) || ldo < h->hidden) return NITRO_ERR_ARG;
+    if (((uintptr_t)out & 1) || ((uintptr_t)saved & 3)) return NITRO_ERR_ARG;
+    if (rows == 0) return NITRO_OK;
+    if (!out) return NITRO_ERR_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    if (rows <= kFewRows) {
+        TRY(forward_few(h, x, x_type, w, FewGluArgs{ldx, ldw, ldo, rows, h->features, h->hidden, 1, act, out, saved, scale}, s));
+        return NITRO_OK;
+    }
+    HgOperand ox, ow;
+    TRY(operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow));
+    ow = {ow.base, ow.inner, h->hidden, ow.ld, 2, h->hidden * ow.ld};
+    HgProblem p{rows, 2 * round_up(h->hidden, 16), h->features};
+    p.status = h->status.at;
+    p.prof = K_GLU_FWD;
+    p.ops = 4.0 * rows * h->hidden * h->features;
+    p.fold = h->features > kFoldFeatures;
+    const EpiGlu::Args ea{out, ldo, saved, tma_rows(out, ldo), ((uintptr_t)saved & 15) == 0 && h->hidden % 4 == 0, h->hidden, act, scale};
+    TRY((hg_launch<EpiGlu, false, false, false>(hg_pick(p), p, ox, ow, ea, s)));
+    return NITRO_OK;
+}
+
+nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
+                                float scale, int act, const float* saved, const uint16_t* dout, int64_t lddout, uint16_t* dx,
+                                int64_t lddx, uint16_t* dw, int64_t lddw, void* stream) {
+    if (!glu_args(h, x, x_type, ldx, w, ldw, rows, scale, act) || lddout < h->hidden) return NITRO_ERR_ARG;
+    if ((dx && (lddx < h->features || ((uintptr_t)dx & 1))) || (dw && (lddw < h->features || ((uintptr_t)dw & 1))))
+        return NITRO_ERR_ARG;
+    if (rows > 0 && (!saved || !dout || ((uintptr_t)saved & 3) || ((uintptr_t)dout & 1))) return NITRO_ERR_ARG;
+    const cudaStream_t s = static_cast<cudaStream_t>(stream);
+    const int F = h->features;
+    const int64_t H2 = 2 * (int64_t)h->hidden;
+    if (rows == 0) {   // an empty batch has a weight gradient of zero
+        if (dw && lddw == F) {
+            TRY(cudaMemsetAsync(dw, 0, sizeof(uint16_t) * (size_t)(H2 * F), s));
+        } else if (dw) {
+            static std::atomic<int> resident{0};
+            ProfScope ps(K_GLU_DW, s, 0.0, 2.0 * H2 * F);
+            TRY(launch_k(k_head_zero, dim3(one_wave(k_head_zero, resident, H2 * F)), dim3(256), 0, s, dw, lddw, H2, F));
+        }
+        return NITRO_OK;
+    }
+    if (!dx && !dw) return NITRO_OK;
+    const int halves = rows <= kRowsWithLow ? 2 : 1;
+    const int64_t plane = rows * h->ldd;
+    {
+        static std::atomic<int> resident[2];
+        const bool vec = h->hidden % 4 == 0 && ((uintptr_t)saved & 15) == 0 && ((uintptr_t)dout & 7) == 0 && lddout % 4 == 0;
+        const int64_t items = rows * (int64_t)(h->hidden / (vec ? 4 : 1));
+        ProfScope ps(K_GLU_GRAD, s, 0.0, 14.0 * rows * h->hidden);
+        const int64_t low = halves == 2 ? plane : 0;
+        if (vec)
+            TRY(launch_k(k_glu_grad<true>, dim3(one_wave(k_glu_grad<true>, resident[0], items)), dim3(256), 0, s, saved, dout, lddout,
+                         (int64_t)rows, h->hidden, act, h->D, h->ldd, low));
+        else
+            TRY(launch_k(k_glu_grad<false>, dim3(one_wave(k_glu_grad<false>, resident[1], items)), dim3(256), 0, s, saved, dout, lddout,
+                         (int64_t)rows, h->hidden, act, h->D, h->ldd, low));
+    }
+    HgOperand ox, ow;
+    TRY(operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow));
+    const HgOperand D{h->D, H2, rows, h->ldd, halves, plane};
+    if (dx) {
+        HgProblem p{rows, F, H2};
+        p.planes_a = halves;
+        p.status = h->status.at;
+        p.prof = K_GLU_DX;
+        p.ops = 4.0 * rows * h->hidden * F;
+        // in slices along the hidden units where its tiles leave SMs idle
+        const int64_t ldc = round_up(F, 32);
+        const HgPick t = hg_pick(p, halves, 1, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
+        if (t.splits == 1) {
+            const EpiBf16::Args eb{dx, lddx, tma_rows(dx, lddx), nullptr, 0, scale};
+            if (halves == 2) TRY((hg_launch<EpiBf16, false, true, false, 2, 1>(t, p, D, ow, eb, s)));
+            else TRY((hg_launch<EpiBf16, false, true, false>(t, p, D, ow, eb, s)));
+        } else {
+            const EpiAcc::Args ea{h->acc, ldc, rows * ldc, 0};
+            if (halves == 2) TRY((hg_launch<EpiAcc, false, true, false, 2, 1>(t, p, D, ow, ea, s)));
+            else TRY((hg_launch<EpiAcc, false, true, false>(t, p, D, ow, ea, s)));
+            ProfScope ps(K_GLU_DX, s, 0.0, (4.0 * t.splits + 2.0) * rows * F);
+            TRY(launch_k(k_head_slices, dim3(rows, (unsigned)std::min(8, (F + 1023) / 1024)), dim3(256), 0, s, (const float*)h->acc, ldc,
+                         rows * ldc, t.splits, F, (const float*)nullptr, scale, dx, lddx,
+                         (int)(((uintptr_t)dx & 7) == 0 && lddx % 4 == 0)));
+        }
+    }
+    if (dw) {
+        HgProblem p{H2, F, rows};
+        p.planes_a = halves;
+        p.status = h->status.at;
+        p.prof = K_GLU_DW;
+        p.ops = 4.0 * rows * h->hidden * F;
+        const EpiBf16::Args eb{dw, lddw, tma_rows(dw, lddw), nullptr, 0, scale};
+        if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p, 2), p, D, ox, eb, s)));
+        else TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, D, ox, eb, s)));
+    }
+    return NITRO_OK;
+}
+
+nitro_status nitro_glu_status(nitro_glu* h, int clear) {
+    if (!h) return NITRO_ERR_ARG;
+    uint32_t bits = 0;
+    if (!h->status.read(clear != 0, &bits)) return NITRO_ERR_CUDA;
+    return bits & ST_TIMEOUT ? NITRO_ERR_TIMEOUT : NITRO_OK;
+}
+
+void nitro_glu_destroy(nitro_glu* h) {
+    if (!h) return;
+    cudaDeviceSynchronize();
+    h->allocs.free();
+    h->status.free();
+    delete h;
+}
+
+}  // extern "C"

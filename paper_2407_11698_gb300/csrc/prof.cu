@@ -46,7 +46,8 @@ const char* const kNames[K_COUNT] = {
     "prep_apply", "lr_pool", "lrpool_to_delta", "tc_timeout_probe", "tc_linear_wgrad",
     "xent_pack", "xent_logits", "xent_rows", "xent_dx", "xent_dw", "orth_pack", "orth_gram",
     "orth_square", "orth_update", "orth_small",
-    "mx4_quantize", "mx4_dequantize", "mx4_linear"};
+    "mx4_quantize", "mx4_dequantize", "mx4_linear",
+    "glu_pack", "glu_fwd", "glu_grad", "glu_dx", "glu_dw", "gnorm_fwd", "gnorm_bwd", "gnorm_params", "clip"};
 
 }  // namespace
 

@@ -51,6 +51,15 @@ enum KernelId : int {
     K_MX4_QUANTIZE,
     K_MX4_DEQUANTIZE,
     K_MX4_LINEAR,
+    K_GLU_PACK,
+    K_GLU_FWD,
+    K_GLU_GRAD,
+    K_GLU_DX,
+    K_GLU_DW,
+    K_GNORM_FWD,
+    K_GNORM_BWD,
+    K_GNORM_PARAMS,
+    K_CLIP,
     K_COUNT
 };
 
