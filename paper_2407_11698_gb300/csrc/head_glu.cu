@@ -65,7 +65,10 @@ struct EpiGlu {
             }
             with_act(a.act, [&](auto act) {
 #pragma unroll
-                for (int j = 0; j < 16; ++j) v[j] = act_value<decltype(act)::value>(v[j]) * v[16 + j];
+                for (int j = 0; j < 16; j += 2) {
+                    const float2 r = mul2(act_value<decltype(act)::value>(make_float2(v[j], v[j + 1])), make_float2(v[16 + j], v[17 + j]));
+                    v[j] = r.x, v[j + 1] = r.y;
+                }
             });
         }
         uint32_t w[16];
@@ -223,10 +226,15 @@ __global__ void __launch_bounds__(256) k_glu_grad(const float* saved, const uint
         }
         with_act(act, [&](auto k) {
 #pragma unroll
-            for (int j = 0; j < E; ++j) {
-                const float2 v = act_slope<decltype(k)::value>(a[j]);
-                da[j] = g[j] * b[j] * v.y;
+            for (int j = 0; j < E; j += 2) {
+                float2 v;
+                const float2 d = act_slope<decltype(k)::value>(make_float2(a[j], E > 1 ? a[j + 1] : 0.0f), &v);
+                da[j] = g[j] * b[j] * d.x;
                 db[j] = g[j] * v.x;
+                if (E > 1) {
+                    da[j + 1] = g[j + 1] * b[j + 1] * d.y;
+                    db[j + 1] = g[j + 1] * v.y;
+                }
             }
         });
         uint16_t* dst = D + at.row * ldd + c;

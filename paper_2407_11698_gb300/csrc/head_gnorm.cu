@@ -20,20 +20,22 @@ namespace {
 
 constexpr int kGnThreads = 256;
 constexpr int kGnBatch = 1024;                 // samples of a launch, at most
-constexpr int kGnCtas = 1216;                  // CTAs of a launch, unless there are more samples (eight an SM)
+constexpr int kGnCtas = 608;                   // CTAs of a launch of two passes, unless there are more samples (four an SM)
 constexpr int64_t kGnBatchBytes = (int64_t)64 << 20;
 constexpr int kGnChannels = 8192;
 
-// V values of a row as fp32; rows are aligned to V values
+// V values of a row as fp32 pairs (of one value: itself and 0); rows are aligned to V values
 template <typename T, int V>
 struct Vals {
-    static constexpr int W = V * (int)sizeof(T) / 4;      // words
-    static __device__ __forceinline__ void load(const T* p, float* v) {
+    static constexpr int N = (V + 1) / 2;
+    static __device__ __forceinline__ void load(const T* p, float2* v) {
         if constexpr (V == 1) {
-            if constexpr (sizeof(T) == 1) v[0] = (float)(*reinterpret_cast<const int8_t*>(p));
-            else if constexpr (sizeof(T) == 2) v[0] = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
-            else v[0] = *reinterpret_cast<const float*>(p);
+            v[0].y = 0.0f;
+            if constexpr (sizeof(T) == 1) v[0].x = (float)(*reinterpret_cast<const int8_t*>(p));
+            else if constexpr (sizeof(T) == 2) v[0].x = __uint_as_float((uint32_t)*reinterpret_cast<const uint16_t*>(p) << 16);
+            else v[0].x = *reinterpret_cast<const float*>(p);
         } else {
+            constexpr int W = V * (int)sizeof(T) / 4;      // words
             uint32_t w[W];
             if constexpr (W % 4 == 0) {
 #pragma unroll
@@ -44,24 +46,31 @@ struct Vals {
                 w[0] = *reinterpret_cast<const uint32_t*>(p);
             }
 #pragma unroll
-            for (int j = 0; j < V; ++j) {
-                if constexpr (sizeof(T) == 1)          // 2^23 + (v + 128) as a float has v + 128 in its low byte
-                    v[j] = __uint_as_float(__byte_perm(w[j >> 2] ^ 0x80808080u, 0x4B000000u, 0x7540 + (j & 3))) - 8388736.0f;
-                else if constexpr (sizeof(T) == 2) v[j] = __uint_as_float(j & 1 ? w[j >> 1] & 0xffff0000u : w[j >> 1] << 16);
-                else v[j] = __uint_as_float(w[j]);
+            for (int j = 0; j < N; ++j) {
+                if constexpr (sizeof(T) == 1) {        // 2^23 + (v + 128) as a float has v + 128 in its low byte
+                    const uint32_t b = w[j >> 1] ^ 0x80808080u;
+                    v[j] = add2(make_float2(__uint_as_float(__byte_perm(b, 0x4B000000u, 0x7540 + 2 * (j & 1))),
+                                            __uint_as_float(__byte_perm(b, 0x4B000000u, 0x7541 + 2 * (j & 1)))),
+                                pair(-8388736.0f));
+                } else if constexpr (sizeof(T) == 2) {
+                    v[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+                } else {
+                    v[j] = make_float2(__uint_as_float(w[2 * j]), __uint_as_float(w[2 * j + 1]));
+                }
             }
         }
     }
-    static __device__ __forceinline__ void store(T* p, const float* v) {
+    static __device__ __forceinline__ void store(T* p, const float2* v) {
         if constexpr (V == 1) {
-            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p) = __bfloat16_as_ushort(__float2bfloat16_rn(v[0]));
-            else *reinterpret_cast<float*>(p) = v[0];
+            if constexpr (sizeof(T) == 2) *reinterpret_cast<uint16_t*>(p) = __bfloat16_as_ushort(__float2bfloat16_rn(v[0].x));
+            else *reinterpret_cast<float*>(p) = v[0].x;
         } else {
+            constexpr int W = V * (int)sizeof(T) / 4;
             uint32_t w[W];
 #pragma unroll
-            for (int i = 0; i < W; ++i) {
-                if constexpr (sizeof(T) == 2) w[i] = pack_bf16(v[2 * i], v[2 * i + 1]);
-                else w[i] = __float_as_uint(v[i]);
+            for (int j = 0; j < N; ++j) {
+                if constexpr (sizeof(T) == 2) w[j] = pack_bf16(v[j].x, v[j].y);
+                else w[2 * j] = __float_as_uint(v[j].x), w[2 * j + 1] = __float_as_uint(v[j].y);
             }
             if constexpr (W % 4 == 0) {
 #pragma unroll
@@ -72,7 +81,118 @@ struct Vals {
         }
     }
 };
+// f(j, group) for V channels from c on, with one division
+template <int V, class F>
+__device__ __forceinline__ void each_channel(int c, int per, F&& f) {
+    int g = c / per, r = c - g * per;
+#pragma unroll
+    for (int j = 0; j < V; ++j) {
+        f(j, g);
+        if (++r == per) r = 0, ++g;
+    }
+}
+__device__ __forceinline__ float& at2(float2* v, int j) { return j & 1 ? v[j >> 1].y : v[j >> 1].x; }
 
+// A thread's channels: statistics of their groups, gamma and beta
+template <int V>
+struct GnChannels {
+    static constexpr int N = (V + 1) / 2;
+    float2 m[N], r[N], gamma[N], beta[N];
+    __device__ __forceinline__ void params(int c, const float* g, const float* b) {
+#pragma unroll
+        for (int j = 0; j < 2 * N; ++j) {
+            at2(gamma, j) = g && j < V ? g[c + j] : 1.0f;
+            at2(beta, j) = b && j < V ? b[c + j] : 0.0f;
+        }
+    }
+    // statistics of a sample's groups
+    __device__ __forceinline__ void stats(int c, int per, const float* mean, const float* rstd) {
+        m[N - 1].y = r[N - 1].y = 0.0f;
+        each_channel<V>(c, per, [&](int j, int g) {
+            at2(m, j) = mean[g];
+            at2(r, j) = rstd[g];
+        });
+    }
+    // act(gamma r (x - m) + beta), r times gamma in r
+    template <int ACT>
+    __device__ __forceinline__ void apply(float2* x) const {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = act_value<ACT>(fma2(sub2(x[j], m[j]), r[j], beta[j]));
+    }
+    // x to h, dy to du
+    template <int ACT>
+    __device__ __forceinline__ void slopes(float2* x, float2* dy) const {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            float2 value;
+            x[j] = mul2(sub2(x[j], m[j]), r[j]);
+            dy[j] = mul2(dy[j], act_slope<ACT>(fma2(gamma[j], x[j], beta[j]), &value));
+        }
+    }
+    // dx = r (gamma du - u - h v) of group means u and v, as (gamma r) du - (x - m) r^2 v - r u: to gamma, r and beta
+    __device__ __forceinline__ void to_dx(const float2* u, const float2* v) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            gamma[j] = mul2(gamma[j], r[j]);
+            beta[j] = mul2(mul2(r[j], u[j]), pair(-1.0f));
+            r[j] = mul2(mul2(r[j], mul2(r[j], v[j])), pair(-1.0f));
+        }
+    }
+    __device__ __forceinline__ void dx(float2* x, const float2* du) const {
+#pragma unroll
+        for (int j = 0; j < N; ++j) x[j] = fma2(du[j], gamma[j], fma2(sub2(x[j], m[j]), r[j], beta[j]));
+    }
+};
+
+// (count, mean, sum of squared distances) joined with another's
+struct Moments {
+    float n = 0.0f, m = 0.0f, q = 0.0f;
+    __device__ __forceinline__ void add(float on, float om, float oq) {
+        const float t = n + on, w = t > 0.0f ? on * rcp(t) : 0.0f, diff = om - m;
+        q += oq + diff * diff * (n * w);
+        m = fmaf(diff, w, m);
+        n = t;
+    }
+    // with those of the lanes at distances first .. last (powers of two)
+    __device__ __forceinline__ void join(int first, int last) {
+        for (int d = first; d <= last; d <<= 1)
+            add(__shfl_xor_sync(0xffffffffu, n, d), __shfl_xor_sync(0xffffffffu, m, d), __shfl_xor_sync(0xffffffffu, q, d));
+    }
+};
+
+// Sums of a thread's values in V channels, from its first ones on
+template <int V>
+struct Sums {
+    static constexpr int N = (V + 1) / 2;
+    float2 k[N], sum[N], sq[N];
+    __device__ __forceinline__ Sums() {
+#pragma unroll
+        for (int j = 0; j < N; ++j) k[j] = sum[j] = sq[j] = pair(0.0f);
+    }
+    __device__ __forceinline__ void add(const float2* v) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float2 d = sub2(v[j], k[j]);
+            sum[j] = add2(sum[j], d);
+            sq[j] = fma2(d, d, sq[j]);
+        }
+    }
+    // to means, from origin(group) on, in sum and squared distances in sq, of n values
+    template <class F>
+    __device__ __forceinline__ void finish(float n, int c, int per, F&& origin) {
+        const float one = n > 0.0f ? rcp(n) : 0.0f;
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float2 m = mul2(sum[j], pair(one));
+            sq[j] = fma2(mul2(m, pair(-1.0f)), sum[j], sq[j]);
+            sq[j] = make_float2(sq[j].x < 0.0f ? 0.0f : sq[j].x, sq[j].y < 0.0f ? 0.0f : sq[j].y);     // (a NaN stays)
+            sum[j] = m;
+        }
+        each_channel<V>(c, per, [&](int j, int g) { at2(sum, j) = n > 0.0f ? at2(sum, j) + (at2(k, j) - origin(g)) : 0.0f; });
+    }
+};
+
+// ------------------------------------------------------------------ two passes
 // What is common to the four passes.
 struct GnShape {
     int pixels, channels, groups, per;   // per: channels of a group
@@ -100,25 +220,6 @@ struct GnPlace {
     }
 };
 
-// A warp's (count, mean, squared distances) triples into one: count-weighted.  cnt may be zero.
-__device__ __forceinline__ void gn_join(float& n, float& mean, float& m2) {
-#pragma unroll
-    for (int d = 16; d > 0; d >>= 1) {
-        const float on = __shfl_xor_sync(0xffffffffu, n, d), om = __shfl_xor_sync(0xffffffffu, mean, d),
-                    o2 = __shfl_xor_sync(0xffffffffu, m2, d);
-        const float t = n + on, w = t > 0.0f ? on / t : 0.0f, diff = om - mean;
-        m2 += o2 + diff * diff * n * w;
-        mean = fmaf(diff, w, mean);
-        n = t;
-    }
-}
-__device__ __forceinline__ void gn_add(float& n, float& mean, float& m2, float on, float om, float o2) {
-    const float t = n + on, w = t > 0.0f ? on / t : 0.0f, diff = om - mean;
-    m2 += o2 + diff * diff * n * w;
-    mean = fmaf(diff, w, mean);
-    n = t;
-}
-
 // Every thread of a sample's CTAs, their parts written: true in the last to come here.
 __device__ __forceinline__ bool gn_last(uint32_t* ticket, int chunks, int* word) {
     if (chunks == 1) {
@@ -139,7 +240,7 @@ __device__ __forceinline__ bool gn_last(uint32_t* ticket, int chunks, int* word)
 
 // mean and rstd of a sample's groups.  Dynamic shared memory: two values a channel.
 template <typename X, int V>
-__global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx, int64_t sx, const GnShape s, float eps, float2* part,
+__global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx, int64_t sx, const GnShape s, float eps, float2* parts,
                                                          uint32_t* ticket, float* mean, float* rstd) {
     extern __shared__ float chan[];                   // [channels] means, [channels] squared distances
     __shared__ float red[2][kGnThreads * V];          // [rows][slab's channels]
@@ -150,88 +251,65 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
     const int width = s.vecs * V;
     x += sample * sx;
     const auto origin = [&](int g) {         // what a group's means are taken from
-        float k;
+        float2 k;
         Vals<X, 1>::load(x + g * s.per, &k);
-        return k;
+        return k.x;
     };
     for (int slab = 0; slab < s.slabs; ++slab) {
         const int c = at.channel<V>(s, slab);
         if (c >= 0) {
-            float k[V], sum[V], sq[V];
-#pragma unroll
-            for (int j = 0; j < V; ++j) sum[j] = sq[j] = k[j] = 0.0f;
+            Sums<V> t;
             const X* src = x + (int64_t)(p0 + at.row) * ldx + c;
-            if (at.row < np) Vals<X, V>::load(src, k);
+            if (at.row < np) Vals<X, V>::load(src, t.k);
             const int64_t step = s.rows * ldx;
-#pragma unroll 4
+#pragma unroll 8
             for (int p = at.row; p < np; p += s.rows, src += step) {
-                float v[V];
+                float2 v[Sums<V>::N];
                 Vals<X, V>::load(src, v);
-#pragma unroll
-                for (int j = 0; j < V; ++j) {
-                    const float d = v[j] - k[j];
-                    sum[j] += d;
-                    sq[j] = fmaf(d, d, sq[j]);
-                }
+                t.add(v);
             }
-            const float n = (float)((np - at.row + s.rows - 1) / s.rows);       // 0 for rows past the chunk
+            t.finish((float)max(0, (np - at.row + s.rows - 1) / s.rows), c, s.per, origin);      // 0 for rows past the chunk
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                const float m = at.row < np ? sum[j] / n : 0.0f;
-                red[0][at.row * width + at.vec * V + j] = (k[j] - origin((c + j) / s.per)) + m;
-                red[1][at.row * width + at.vec * V + j] = fmaxf(fmaf(-m, sum[j], sq[j]), 0.0f);
+                red[0][at.row * width + at.vec * V + j] = at2(t.sum, j);
+                red[1][at.row * width + at.vec * V + j] = at2(t.sq, j);
             }
         }
         __syncthreads();
         for (int i = threadIdx.x; i < width; i += blockDim.x) {
             const int ch = slab * width + i;
             if (ch >= s.channels) break;
-            float n = 0.0f, m = 0.0f, m2 = 0.0f;
+            Moments a;
             for (int r = 0; r < min(s.rows, np); ++r)
-                gn_add(n, m, m2, (float)((np - r + s.rows - 1) / s.rows), red[0][r * width + i], red[1][r * width + i]);
-            chan[ch] = m;
-            chan[s.channels + ch] = m2;
+                a.add((float)((np - r + s.rows - 1) / s.rows), red[0][r * width + i], red[1][r * width + i]);
+            chan[ch] = a.m;
+            chan[s.channels + ch] = a.q;
         }
         __syncthreads();
     }
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    part += (int64_t)sample * s.chunks * s.groups;
+    parts += (int64_t)sample * s.chunks * s.groups;
     for (int g = warp; g < s.groups; g += warps) {
-        float n = 0.0f, m = 0.0f, m2 = 0.0f;
-        for (int c = lane; c < s.per; c += 32) gn_add(n, m, m2, (float)np, chan[g * s.per + c], chan[s.channels + g * s.per + c]);
-        gn_join(n, m, m2);
-        if (lane == 0) part[(int64_t)blockIdx.x * s.groups + g] = make_float2(m, m2);
+        Moments a;
+        for (int c = lane; c < s.per; c += 32) a.add((float)np, chan[g * s.per + c], chan[s.channels + g * s.per + c]);
+        a.join(1, 16);
+        if (lane == 0) parts[(int64_t)blockIdx.x * s.groups + g] = make_float2(a.m, a.q);
     }
     if (!gn_last(ticket + sample, s.chunks, &word)) return;
     for (int g = warp; g < s.groups; g += warps) {
-        float n = 0.0f, m = 0.0f, m2 = 0.0f;
+        Moments a;
+#pragma unroll 4
         for (int i = lane; i < s.chunks; i += 32) {
-            const float2 v = __ldcg(part + (int64_t)i * s.groups + g);
-            gn_add(n, m, m2, (float)(min(s.chunk, s.pixels - i * s.chunk)) * (float)s.per, v.x, v.y);
+            const float2 v = __ldcg(parts + (int64_t)i * s.groups + g);
+            a.add((float)(min(s.chunk, s.pixels - i * s.chunk)) * (float)s.per, v.x, v.y);
         }
-        gn_join(n, m, m2);
+        a.join(1, 16);
         if (lane == 0) {
-            mean[(int64_t)sample * s.groups + g] = origin(g) + m;
-            rstd[(int64_t)sample * s.groups + g] = 1.0f / sqrtf(m2 / n + eps);
+            mean[(int64_t)sample * s.groups + g] = origin(g) + a.m;
+            rstd[(int64_t)sample * s.groups + g] = 1.0f / sqrtf(a.q / a.n + eps);
         }
     }
 }
-
-// A thread's channels: statistics of their groups, gamma and beta
-template <int V>
-struct GnChannels {
-    float m[V], r[V], gamma[V], beta[V];
-    __device__ __forceinline__ void load(const GnShape& s, int c, const float* mean, const float* rstd) {
-#pragma unroll
-        for (int j = 0; j < V; ++j) {
-            const int g = (c + j) / s.per;
-            m[j] = mean[g];
-            r[j] = rstd[g];
-            gamma[j] = s.gamma ? s.gamma[c + j] : 1.0f;
-            beta[j] = s.beta ? s.beta[c + j] : 0.0f;
-        }
-    }
-};
 
 template <typename X, typename Y, int V>
 __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx, int64_t sx, const GnShape s, const float* mean,
@@ -243,40 +321,31 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
         const int c = at.channel<V>(s, slab);
         if (c < 0) continue;
         GnChannels<V> ch;
-        ch.load(s, c, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+        ch.params(c, s.gamma, s.beta);
+        ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
 #pragma unroll
-        for (int j = 0; j < V; ++j) ch.r[j] *= ch.gamma[j];
+        for (int j = 0; j < ch.N; ++j) ch.r[j] = mul2(ch.r[j], ch.gamma[j]);
         const X* src = x + sample * sx + (int64_t)(p0 + at.row) * ldx + c;
         Y* dst = y + sample * sy + (int64_t)(p0 + at.row) * ldy + c;
+        const int64_t xs = s.rows * ldx, ys = s.rows * ldy;
         with_act(s.act, [&](auto act) {
 #pragma unroll 4
-            for (int p = at.row; p < np; p += s.rows, src += s.rows * ldx, dst += s.rows * ldy) {
-                float v[V];
+            for (int p = at.row; p < np; p += s.rows, src += xs, dst += ys) {
+                float2 v[ch.N];
                 Vals<X, V>::load(src, v);
-#pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = act_value<decltype(act)::value>(fmaf(v[j] - ch.m[j], ch.r[j], ch.beta[j]));
+                ch.template apply<decltype(act)::value>(v);
                 Vals<Y, V>::store(dst, v);
             }
         });
     }
 }
 
-// du and h of V values
-template <int ACT, int V>
-__device__ __forceinline__ void gn_slopes(const GnChannels<V>& ch, float* x, float* dy) {
-#pragma unroll
-    for (int j = 0; j < V; ++j) {
-        x[j] = (x[j] - ch.m[j]) * ch.r[j];
-        dy[j] *= act_slope<ACT>(fmaf(ch.gamma[j], x[j], ch.beta[j])).y;
-    }
-}
-
 // Sums over a chunk: of du and du h for each channel (part_c [sample][chunk][2][channels]), and over a sample's
 // groups of gamma du and gamma du h, divided by their count (means [sample][groups]).
 template <typename X, typename Y, int V>
-__global__ void __launch_bounds__(kGnThreads) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
-                                                        const GnShape s, const float* mean, const float* rstd, float* part_c,
-                                                        float2* part, uint32_t* ticket, float2* means) {
+__global__ void __launch_bounds__(kGnThreads, 2) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
+                                                           const GnShape s, const float* mean, const float* rstd, float* part_c,
+                                                           float2* parts, uint32_t* ticket, float2* means) {
     __shared__ float red[2][kGnThreads * V];
     __shared__ int word;
     pdl_wait();
@@ -288,30 +357,32 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_sums(const X* x, int64_t ldx,
         const int c = at.channel<V>(s, slab);
         if (c >= 0) {
             GnChannels<V> ch;
-            ch.load(s, c, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
-            float a[V], b[V];
+            ch.params(c, s.gamma, s.beta);
+            ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+            float2 a[ch.N], b[ch.N];
 #pragma unroll
-            for (int j = 0; j < V; ++j) a[j] = b[j] = 0.0f;
+            for (int j = 0; j < ch.N; ++j) a[j] = b[j] = pair(0.0f);
             const X* src = x + sample * sx + (int64_t)(p0 + at.row) * ldx + c;
             const Y* grad = dy + sample * sdy + (int64_t)(p0 + at.row) * lddy + c;
+            const int64_t xs = s.rows * ldx, gs = s.rows * lddy;
             with_act(s.act, [&](auto act) {
-#pragma unroll 2
-                for (int p = at.row; p < np; p += s.rows, src += s.rows * ldx, grad += s.rows * lddy) {
-                    float v[V], g[V];
+#pragma unroll 4
+                for (int p = at.row; p < np; p += s.rows, src += xs, grad += gs) {
+                    float2 v[ch.N], g[ch.N];
                     Vals<X, V>::load(src, v);
                     Vals<Y, V>::load(grad, g);
-                    gn_slopes<decltype(act)::value, V>(ch, v, g);
+                    ch.template slopes<decltype(act)::value>(v, g);
 #pragma unroll
-                    for (int j = 0; j < V; ++j) {
-                        a[j] += g[j];
-                        b[j] = fmaf(g[j], v[j], b[j]);
+                    for (int j = 0; j < ch.N; ++j) {
+                        a[j] = add2(a[j], g[j]);
+                        b[j] = fma2(g[j], v[j], b[j]);
                     }
                 }
             });
 #pragma unroll
             for (int j = 0; j < V; ++j) {
-                red[0][at.row * width + at.vec * V + j] = a[j];
-                red[1][at.row * width + at.vec * V + j] = b[j];
+                red[0][at.row * width + at.vec * V + j] = at2(a, j);
+                red[1][at.row * width + at.vec * V + j] = at2(b, j);
             }
         }
         __syncthreads();
@@ -326,8 +397,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_sums(const X* x, int64_t ldx,
     }
     if (!means) return;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, warps = blockDim.x >> 5;
-    part += (int64_t)sample * s.chunks * s.groups;
-    __threadfence_block();
+    parts += (int64_t)sample * s.chunks * s.groups;
     for (int g = warp; g < s.groups; g += warps) {
         float a = 0.0f, b = 0.0f;
         for (int i = lane; i < s.per; i += 32) {
@@ -338,14 +408,15 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_sums(const X* x, int64_t ldx,
         }
 #pragma unroll
         for (int d = 16; d > 0; d >>= 1) a += __shfl_xor_sync(0xffffffffu, a, d), b += __shfl_xor_sync(0xffffffffu, b, d);
-        if (lane == 0) part[(int64_t)blockIdx.x * s.groups + g] = make_float2(a, b);
+        if (lane == 0) parts[(int64_t)blockIdx.x * s.groups + g] = make_float2(a, b);
     }
     if (!gn_last(ticket + sample, s.chunks, &word)) return;
     const float count = (float)s.pixels * (float)s.per;
     for (int g = warp; g < s.groups; g += warps) {
         float a = 0.0f, b = 0.0f;
+#pragma unroll 4
         for (int i = lane; i < s.chunks; i += 32) {
-            const float2 v = __ldcg(part + (int64_t)i * s.groups + g);
+            const float2 v = __ldcg(parts + (int64_t)i * s.groups + g);
             a += v.x;
             b += v.y;
         }
@@ -356,36 +427,422 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_sums(const X* x, int64_t ldx,
 }
 
 template <typename X, typename Y, int V>
-__global__ void __launch_bounds__(kGnThreads) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
-                                                      const GnShape s, const float* mean, const float* rstd, const float2* means,
-                                                      Y* dx, int64_t lddx, int64_t sdx) {
+__global__ void __launch_bounds__(kGnThreads, 2) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
+                                                         const GnShape s, const float* mean, const float* rstd, const float2* means,
+                                                         Y* dx, int64_t lddx, int64_t sdx) {
     pdl_wait();
     const int sample = blockIdx.y, p0 = blockIdx.x * s.chunk, p1 = min(s.pixels, p0 + s.chunk), np = p1 - p0;
     const GnPlace at(s);
     for (int slab = 0; slab < s.slabs; ++slab) {
         const int c = at.channel<V>(s, slab);
         if (c < 0) continue;
-        GnChannels<V> ch;
-        ch.load(s, c, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
-        float2 t[V];
-#pragma unroll
-        for (int j = 0; j < V; ++j) t[j] = means[(int64_t)sample * s.groups + (c + j) / s.per];
+        GnChannels<V> ch, to;
+        ch.params(c, s.gamma, s.beta);
+        ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+        to = ch;
+        {
+            float2 u[ch.N], v[ch.N];
+            u[ch.N - 1].y = v[ch.N - 1].y = 0.0f;
+            each_channel<V>(c, s.per, [&](int j, int g) {
+                const float2 t = means[(int64_t)sample * s.groups + g];
+                at2(u, j) = t.x;
+                at2(v, j) = t.y;
+            });
+            to.to_dx(u, v);
+        }
         const X* src = x + sample * sx + (int64_t)(p0 + at.row) * ldx + c;
         const Y* grad = dy + sample * sdy + (int64_t)(p0 + at.row) * lddy + c;
         Y* dst = dx + sample * sdx + (int64_t)(p0 + at.row) * lddx + c;
+        const int64_t xs = s.rows * ldx, gs = s.rows * lddy, ds = s.rows * lddx;
         with_act(s.act, [&](auto act) {
-#pragma unroll 2
-            for (int p = at.row; p < np; p += s.rows, src += s.rows * ldx, grad += s.rows * lddy, dst += s.rows * lddx) {
-                float v[V], g[V];
+#pragma unroll 4
+            for (int p = at.row; p < np; p += s.rows, src += xs, grad += gs, dst += ds) {
+                float2 v[ch.N], h[ch.N], g[ch.N];
                 Vals<X, V>::load(src, v);
                 Vals<Y, V>::load(grad, g);
-                gn_slopes<decltype(act)::value, V>(ch, v, g);
 #pragma unroll
-                for (int j = 0; j < V; ++j) v[j] = ch.r[j] * fmaf(-v[j], t[j].y, fmaf(ch.gamma[j], g[j], -t[j].x));
+                for (int j = 0; j < ch.N; ++j) h[j] = v[j];
+                ch.template slopes<decltype(act)::value>(h, g);
+                to.dx(v, g);
                 Vals<Y, V>::store(dst, v);
             }
         });
     }
+}
+
+// ------------------------------------------------------------------ one pass
+// Both directions in one launch with one pass over memory, where a cluster's shared memory holds a slab of a sample: whole
+// groups, `width` channels at all pixels, shared out over ks CTAs by pixels.  A thread copies its own vectors to
+// shared memory and alone reads them there, so nothing waits for them but itself; channels' sums meet in the
+// warp's lanes, over the CTA's warps, and over the cluster's shared memory.
+//
+// Lanes: 2^k >= width / V to a pixel (those past the width idle), so the lanes of a channel are found by shuffles.
+constexpr int kGnWarps = kGnThreads / 32;
+struct GnOne {
+    int pixels, channels, groups, per;
+    int width, slabs, ks;                // channels of a slab, slabs of a sample, CTAs of a cluster
+    int vecs, lanes;                     // vectors of a slab's pixel, and lanes
+    int chunk, steps;                    // pixels of a CTA, of which a thread takes every (256 / lanes)th
+    int act;
+    const float* gamma;                  // or null
+    const float* beta;                   // or null
+};
+
+// A vector's place in shared memory: planes of 16 bytes a thread (or less, the vector itself)
+template <typename T, int V>
+struct Slots {
+    static constexpr int BYTES = V * (int)sizeof(T), PLANE = BYTES < 16 ? BYTES : 16, PLANES = BYTES / PLANE;
+    static constexpr int STEP = kGnThreads * BYTES;          // from a thread's vector to its next
+    static __device__ __forceinline__ uint8_t* first(uint8_t* base) { return base + (int)threadIdx.x * PLANE; }
+    // Place: whose places the vector takes, its own or those of wider values that replace it later
+    template <class Place = Slots>
+    static __device__ __forceinline__ void fetch(uint8_t* to, const T* src) {
+        if constexpr (PLANE < 4) {
+            *reinterpret_cast<T*>(to) = *src;
+        } else {
+#pragma unroll
+            for (int i = 0; i < PLANES; ++i) {
+                const uint32_t dst = smem_u32(to + i * kGnThreads * Place::PLANE);
+                const char* s = reinterpret_cast<const char*>(src) + i * PLANE;
+                if constexpr (PLANE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(s) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(s), "n"(PLANE) : "memory");
+            }
+        }
+    }
+    template <class Place = Slots>
+    static __device__ __forceinline__ void get(const uint8_t* from, float2* v) {
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i)
+            Vals<T, V / PLANES>::load(reinterpret_cast<const T*>(from + i * kGnThreads * Place::PLANE), v + i * (V / PLANES / 2));
+    }
+    static __device__ __forceinline__ void put(uint8_t* to, const float2* v) {
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i)
+            Vals<T, V / PLANES>::store(reinterpret_cast<T*>(to + i * kGnThreads * PLANE), v + i * (V / PLANES / 2));
+    }
+};
+// A thread's copies go in up to kGnStages groups, so that the first are taken while the others are under way
+constexpr int kGnStages = 4;
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+__device__ __forceinline__ void copies_landed(int stage) {
+    if (stage == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
+    else if (stage == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
+    else if (stage == 2) asm volatile("cp.async.wait_group 1;" ::: "memory");
+    else asm volatile("cp.async.wait_group 0;" ::: "memory");
+}
+
+__device__ __forceinline__ float ld_remote(const float* p, uint32_t rank) {
+    float v;
+    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_smem(smem_u32(p), rank)) : "memory");
+    return v;
+}
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+
+// A thread's part of a slab
+struct GnPart {
+    int sample, rank, c, g0, row, rows, np;       // first channel (-1: idle lane), the slab's first group, first pixel of the chunk's, step, pixels
+    int count, stage;                             // pixels that the thread takes, of a stage
+    int64_t p0;
+    __device__ __forceinline__ GnPart(const GnOne& s, int v) {
+        const int unit = blockIdx.x / s.ks, slab = unit % s.slabs, lane = threadIdx.x & 31, per_warp = 32 / s.lanes;
+        rank = blockIdx.x - unit * s.ks;
+        sample = unit / s.slabs;
+        const int vec = lane & (s.lanes - 1);
+        row = (threadIdx.x >> 5) * per_warp + lane / s.lanes;
+        rows = kGnWarps * per_warp;
+        c = vec < s.vecs ? slab * s.width + vec * v : -1;
+        g0 = slab * (s.width / s.per);
+        p0 = (int64_t)rank * s.chunk;
+        np = max(0, min(s.chunk, s.pixels - rank * s.chunk));
+        count = c >= 0 && row < np ? (np - row + rows - 1) / rows : 0;
+        stage = (s.steps + kGnStages - 1) / kGnStages;
+    }
+};
+
+template <typename X, typename Y, int V>
+__global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ldx, int64_t sx, const GnOne s, float eps, float* mean,
+                                                          float* rstd, Y* y, int64_t ldy, int64_t sy) {
+    using SX = Slots<X, V>;
+    constexpr int N = (V + 1) / 2;
+    extern __shared__ __align__(16) uint8_t data[];
+    const int gs = s.width / s.per;
+    float* warp_m = reinterpret_cast<float*>(data + (s.steps * SX::STEP + 15) / 16 * 16);      // [warps][entries] means, from the group's origin
+    float* warp_q = warp_m + kGnWarps * s.width;                                               // and squared distances
+    float* group = warp_q + kGnWarps * s.width;                                                // [3][groups of the slab]: counts, means, distances
+    float* stat = group + 3 * gs;                                                              // [2][groups]: origin, then mean; rstd
+    __shared__ float warp_n[kGnWarps];
+    pdl_wait();
+    const GnPart at(s, V);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    x += at.sample * sx;
+    uint8_t* slot = SX::first(data);
+    {
+        const X* src = x + (at.p0 + at.row) * ldx + at.c;
+        const int64_t step = at.rows * ldx;
+        uint8_t* to = slot;
+        for (int k = 0, i = 0; k < kGnStages; ++k) {
+            const int end = min(at.count, (k + 1) * at.stage);
+#pragma unroll 4
+            for (; i < end; ++i, src += step, to += SX::STEP) SX::fetch(to, src);
+            copies_group();
+        }
+    }
+    const auto origin = [&](int g) {         // what a group's means are taken from
+        float2 k;
+        Vals<X, 1>::load(x + g * s.per, &k);
+        return k.x;
+    };
+    // (read before the first y is written, which may be x itself)
+    for (int g = threadIdx.x; g < gs; g += kGnThreads) stat[g] = origin(at.g0 + g);
+    GnChannels<V> ch;
+    if (at.c >= 0) ch.params(at.c, s.gamma, s.beta);
+    Sums<V> t;
+    {
+        const uint8_t* from = slot;
+        for (int k = 0, i = 0; k < kGnStages; ++k) {
+            copies_landed(k);
+            if (k == 0 && at.count > 0) SX::get(slot, t.k);
+            const int end = min(at.count, (k + 1) * at.stage);
+#pragma unroll 4
+            for (; i < end; ++i, from += SX::STEP) {
+                float2 v[N];
+                SX::get(from, v);
+                t.add(v);
+            }
+        }
+    }
+    __syncthreads();                         // the origins are there
+    float n = (float)at.count;
+    if (at.c >= 0) t.finish(n, at.c, s.per, [&](int g) { return stat[g - at.g0]; });
+    // A vector of one group goes on as one entry, others channel by channel
+    const bool whole = s.per % V == 0;
+    const int entry = whole ? V : 1;         // channels of an entry
+    if (whole) {
+        float2 m = t.sum[0];
+#pragma unroll
+        for (int j = 1; j < N; ++j) m = add2(m, t.sum[j]);
+        Moments a;
+        a.n = n * V;
+        a.m = V == 1 ? m.x : (m.x + m.y) * (1.0f / V);
+        float2 q = pair(0.0f);
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            const float2 d = sub2(t.sum[j], pair(a.m));
+            q = add2(q, fma2(mul2(d, d), pair(n), t.sq[j]));
+        }
+        a.q = V == 1 ? t.sq[0].x : q.x + q.y;
+        if (n == 0.0f) a = Moments();
+        a.join(s.lanes, 16);
+        if (lane < s.vecs) {
+            warp_m[warp * s.width + lane] = a.m;
+            warp_q[warp * s.width + lane] = a.q;
+            if (lane == 0) warp_n[warp] = a.n;
+        }
+    } else {
+        float cn = n;
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            Moments a;
+            a.n = n, a.m = at2(t.sum, j), a.q = at2(t.sq, j);
+            a.join(s.lanes, 16);
+            if (lane < s.vecs) {
+                warp_m[warp * s.width + lane * V + j] = a.m;
+                warp_q[warp * s.width + lane * V + j] = a.q;
+            }
+            cn = a.n;
+        }
+        if (lane == 0) warp_n[warp] = cn;
+    }
+    __syncthreads();
+    // a group's entries: those of a warp to a lane of eight
+    for (int g0 = 0; g0 < gs; g0 += kGnThreads / kGnWarps) {
+        const int g = g0 + threadIdx.x / kGnWarps, w = threadIdx.x % kGnWarps, per = s.per / entry;
+        Moments a;
+        if (g < gs)
+            for (int i = 0; i < per; ++i) a.add(warp_n[w], warp_m[w * s.width + g * per + i], warp_q[w * s.width + g * per + i]);
+        a.join(1, kGnWarps / 2);
+        if (g < gs && w == 0) group[g] = a.n, group[gs + g] = a.m, group[2 * gs + g] = a.q;
+    }
+    if (s.ks > 1) cluster_barrier();
+    else __syncthreads();
+    for (int g = threadIdx.x; g < gs; g += kGnThreads) {
+        Moments a;
+        if (s.ks == 1) a.n = group[g], a.m = group[gs + g], a.q = group[2 * gs + g];
+        else
+            for (int r = 0; r < s.ks; ++r) a.add(ld_remote(group + g, r), ld_remote(group + gs + g, r), ld_remote(group + 2 * gs + g, r));
+        const float mu = stat[g] + a.m, rs = 1.0f / sqrtf(a.q / a.n + eps);
+        stat[g] = mu;
+        stat[gs + g] = rs;
+        if (at.rank == 0 && mean) {
+            mean[(int64_t)at.sample * s.groups + at.g0 + g] = mu;
+            rstd[(int64_t)at.sample * s.groups + at.g0 + g] = rs;
+        }
+    }
+    if (s.ks > 1) cluster_arrive();          // this CTA has read its peers' shared memory
+    __syncthreads();
+    if (at.count > 0) {
+        ch.stats(at.c, s.per, stat - at.g0, stat + gs - at.g0);
+#pragma unroll
+        for (int j = 0; j < N; ++j) ch.r[j] = mul2(ch.r[j], ch.gamma[j]);
+        Y* dst = y + at.sample * sy + (at.p0 + at.row) * ldy + at.c;
+        const int64_t step = at.rows * ldy;
+        const uint8_t* from = slot;
+        with_act(s.act, [&](auto act) {
+#pragma unroll 4
+            for (int i = 0; i < at.count; ++i, from += SX::STEP, dst += step) {
+                float2 v[N];
+                SX::get(from, v);
+                ch.template apply<decltype(act)::value>(v);
+                Vals<Y, V>::store(dst, v);
+            }
+        });
+    }
+    if (s.ks > 1) cluster_wait();            // and they this one's
+}
+
+// The gradients: du replaces dy in shared memory, in 32 bits, so that the slopes are taken once.  sums: of du and
+// du h for each sample and channel [sample][2][channels], or null.  dx may be null.
+template <typename X, typename Y, int V>
+__global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
+                                                               const GnOne s, const float* mean, const float* rstd, float* sums, Y* dx,
+                                                               int64_t lddx, int64_t sdx) {
+    using SX = Slots<X, V>;
+    using SY = Slots<Y, V>;
+    using SD = Slots<float, V>;
+    constexpr int N = (V + 1) / 2;
+    extern __shared__ __align__(16) uint8_t data[];
+    const int xb = (s.steps * SX::STEP + 15) / 16 * 16, gs = s.width / s.per;
+    uint8_t* grads = data + xb;
+    float* warp_s = reinterpret_cast<float*>(grads + s.steps * SD::STEP);      // [2][warps][width]
+    float* chan = warp_s + 2 * kGnWarps * s.width;                             // [2][width]
+    float* means = chan + 2 * s.width;                                         // [2][groups]
+    pdl_wait();
+    const GnPart at(s, V);
+    const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
+    uint8_t *xslot = SX::first(data), *gslot = SD::first(grads);
+    {
+        const X* src = x + at.sample * sx + (at.p0 + at.row) * ldx + at.c;
+        const Y* grad = dy + at.sample * sdy + (at.p0 + at.row) * lddy + at.c;
+        const int64_t xs = at.rows * ldx, ys = at.rows * lddy;
+        uint8_t *tx = xslot, *tg = gslot;
+        for (int k = 0, i = 0; k < kGnStages; ++k) {
+            const int end = min(at.count, (k + 1) * at.stage);
+#pragma unroll 2
+            for (; i < end; ++i, src += xs, grad += ys, tx += SX::STEP, tg += SD::STEP) {
+                SX::fetch(tx, src);
+                SY::template fetch<SD>(tg, grad);
+            }
+            copies_group();
+        }
+    }
+    GnChannels<V> ch;
+    float2 a[N], b[N];
+#pragma unroll
+    for (int j = 0; j < N; ++j) a[j] = b[j] = pair(0.0f);
+    if (at.c >= 0) {
+        ch.params(at.c, s.gamma, s.beta);
+        ch.stats(at.c, s.per, mean + (int64_t)at.sample * s.groups, rstd + (int64_t)at.sample * s.groups);
+    }
+    with_act(s.act, [&](auto act) {
+        const uint8_t* tx = xslot;
+        uint8_t* tg = gslot;
+        for (int k = 0, i = 0; k < kGnStages; ++k) {
+            copies_landed(k);
+            const int end = min(at.count, (k + 1) * at.stage);
+#pragma unroll 2
+            for (; i < end; ++i, tx += SX::STEP, tg += SD::STEP) {
+                float2 v[N], du[N];
+                SX::get(tx, v);
+                SY::template get<SD>(tg, du);
+                ch.template slopes<decltype(act)::value>(v, du);
+#pragma unroll
+                for (int j = 0; j < N; ++j) {
+                    a[j] = add2(a[j], du[j]);
+                    b[j] = fma2(du[j], v[j], b[j]);
+                }
+                SD::put(tg, du);
+            }
+        }
+    });
+    for (int d = s.lanes; d < 32; d <<= 1) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            a[j] = add2(a[j], make_float2(__shfl_xor_sync(0xffffffffu, a[j].x, d), V > 1 ? __shfl_xor_sync(0xffffffffu, a[j].y, d) : 0.0f));
+            b[j] = add2(b[j], make_float2(__shfl_xor_sync(0xffffffffu, b[j].x, d), V > 1 ? __shfl_xor_sync(0xffffffffu, b[j].y, d) : 0.0f));
+        }
+    }
+    if (lane < s.vecs) {
+#pragma unroll
+        for (int j = 0; j < V; ++j) {
+            warp_s[warp * s.width + lane * V + j] = at2(a, j);
+            warp_s[(kGnWarps + warp) * s.width + lane * V + j] = at2(b, j);
+        }
+    }
+    __syncthreads();
+    for (int i = threadIdx.x; i < 2 * s.width; i += kGnThreads) {
+        const int half = i >= s.width, c = i - half * s.width;
+        float v = 0.0f;
+#pragma unroll
+        for (int w = 0; w < kGnWarps; ++w) v += warp_s[(half * kGnWarps + w) * s.width + c];
+        chan[i] = v;
+    }
+    if (s.ks > 1) {
+        cluster_barrier();
+        // all ranks' sums, in their order, to where the warps' were
+        for (int i = threadIdx.x; i < 2 * s.width; i += kGnThreads) {
+            float v = 0.0f;
+            for (int r = 0; r < s.ks; ++r) v += ld_remote(chan + i, r);
+            warp_s[i] = v;
+        }
+        cluster_arrive();          // this CTA has read its peers' shared memory
+    }
+    __syncthreads();
+    const float* total = s.ks > 1 ? warp_s : chan;
+    const int c0 = at.g0 * s.per;
+    if (sums && at.rank == 0)
+        for (int i = threadIdx.x; i < 2 * s.width; i += kGnThreads) {
+            const int half = i >= s.width;
+            sums[((int64_t)at.sample * 2 + half) * s.channels + c0 + i - half * s.width] = total[i];
+        }
+    if (dx) {
+        const float one = 1.0f / ((float)s.pixels * (float)s.per);
+        for (int g0 = 0; g0 < gs; g0 += kGnThreads / 8) {        // eight lanes a group
+            const int g = g0 + threadIdx.x / 8;
+            float u = 0.0f, v = 0.0f;
+            if (g < gs)
+                for (int i = threadIdx.x % 8; i < s.per; i += 8) {
+                    const int c = g * s.per + i;
+                    const float k = s.gamma ? s.gamma[c0 + c] : 1.0f;
+                    u = fmaf(k, total[c], u);
+                    v = fmaf(k, total[s.width + c], v);
+                }
+#pragma unroll
+            for (int d = 4; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d), v += __shfl_xor_sync(0xffffffffu, v, d);
+            if (g < gs && threadIdx.x % 8 == 0) means[g] = u * one, means[gs + g] = v * one;
+        }
+        __syncthreads();
+        if (at.count > 0) {
+            a[N - 1].y = b[N - 1].y = 0.0f;
+            each_channel<V>(at.c, s.per, [&](int j, int g) {
+                at2(a, j) = means[g - at.g0];
+                at2(b, j) = means[gs + g - at.g0];
+            });
+            ch.to_dx(a, b);
+            Y* dst = dx + at.sample * sdx + (at.p0 + at.row) * lddx + at.c;
+            const int64_t step = at.rows * lddx;
+            const uint8_t *tx = xslot, *tg = gslot;
+#pragma unroll 4
+            for (int i = 0; i < at.count; ++i, tx += SX::STEP, tg += SD::STEP, dst += step) {
+                float2 v[N], du[N];
+                SX::get(tx, v);
+                SD::get(tg, du);
+                ch.dx(v, du);
+                Vals<Y, V>::store(dst, v);
+            }
+        }
+    }
+    if (s.ks > 1) cluster_wait();            // and they this one's
 }
 
 // dgamma and dbeta from the chunks' sums [rows][2][channels]: 32 channels a CTA, the rows over its warps.
@@ -455,7 +912,7 @@ GnShape shape(const nitro_gnorm* h, int pixels, int samples, int v, int act, con
     s.slabs = (vecs + kGnThreads - 1) / kGnThreads;
     s.vecs = (vecs + s.slabs - 1) / s.slabs;
     s.rows = kGnThreads / s.vecs;
-    // eight CTAs an SM in all, of eight steps at least
+    // four CTAs an SM in all, of eight steps at least
     const int want = std::max(1, std::min(kGnCtas / samples, (pixels + 8 * s.rows - 1) / (8 * s.rows)));
     s.chunk = (pixels + want - 1) / want;
     s.chunks = (pixels + s.chunk - 1) / s.chunk;
@@ -510,6 +967,68 @@ int batch_size(const nitro_gnorm* h, int pixels, int bytes_a_value) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, h->batch));
 }
 
+// How a call runs in one pass, or ks = 0: x_bytes, dy_bytes: of a value in shared memory; ctas: that an SM should hold.
+// The narrowest slab of whole groups whose rows are lines of 64 bytes of x, or of 32 where there are few CTAs; the least CTAs that hold it; and more
+// of them while SMs are idle.
+GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size, int value_bytes, int ctas, int act, const float* gamma,
+               const float* beta, int* smem) {
+    GnOne s{};
+    s.pixels = pixels;
+    s.channels = h->channels;
+    s.groups = h->groups;
+    s.per = h->channels / h->groups;
+    s.act = act;
+    s.gamma = gamma;
+    s.beta = beta;
+    const int sms = sm_count();
+    const auto fit = [&](int m, int ks, int budget) {      // m groups a slab
+        s.width = m * s.per;
+        s.slabs = h->groups / m;
+        s.ks = ks;
+        s.vecs = s.width / v;
+        for (s.lanes = 1; s.lanes < s.vecs;) s.lanes *= 2;
+        const int rows = kGnThreads / s.lanes;
+        s.chunk = (pixels + ks - 1) / ks;
+        s.steps = (s.chunk + rows - 1) / rows;
+        const int64_t bytes = (int64_t)s.steps * kGnThreads * v * value_bytes + 32 + 4 * (2 * kGnWarps + 2) * (int64_t)s.width + 20 * m;
+        *smem = (int)bytes;
+        return bytes <= budget;
+    };
+    const auto slab_ok = [&](int m) { return h->groups % m == 0 && m * s.per % v == 0 && m * s.per / v <= 32; };
+    // groups of a slab whose rows have `line` bytes, else as many as there may be
+    const auto slab = [&](int line) {
+        int best = 0;
+        for (int m = 1; m <= h->groups && m * s.per <= 32 * v; ++m) {
+            if (!slab_ok(m)) continue;
+            best = m;
+            if (m * s.per * x_size >= line) break;
+        }
+        return best;
+    };
+    if (slab(64) == 0) return GnOne{};
+    const int widest = (int64_t)samples * (h->groups / slab(64)) >= sms ? 64 : 32;
+    const int share = 226 * 1024 / ctas - 1024;
+    for (int budget : {share, 110 * 1024, 224 * 1024})
+        for (int line = widest; line >= 16; line /= 2)
+            for (int ks = 1; ks <= 8; ks *= 2) {
+                if (!fit(slab(line), ks, budget) || (int64_t)samples * s.slabs * 8 > INT32_MAX) continue;
+                const int least = ks;
+                while (ks < 8 && (int64_t)samples * s.slabs * ks * 2 <= 2 * sms && s.steps > 2 * (ks / least)) ks *= 2;
+                if (ks > least) fit(slab(line), ks, budget);
+                return s;
+            }
+    return GnOne{};
+}
+
+template <typename K>
+cudaError_t one_ready(K* kernel, std::atomic<uint64_t>& ready) {
+    int dev = 0;
+    sm_count(&dev);
+    return once_per_device(ready, dev, [kernel] {
+        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
+    });
+}
+
 }  // namespace
 
 extern "C" {
@@ -551,6 +1070,26 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     TRY(clear_once(h->clean, h->ticket, sizeof(uint32_t) * h->batch, s));
     const int v = pick_v(h, samples, {mx, my}), C = h->channels;
+    int smem = 0;
+    const GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), type_size(x_type), 3, act, gamma, beta, &smem);
+    if (one.ks) {
+        TRY(with_x(x_type, [&](auto xt) {
+            using X = decltype(xt);
+            return with_y(y_type, [&](auto yt) {
+                using Y = decltype(yt);
+                return with_v(v, [&](auto vt) {
+                    constexpr int V = decltype(vt)::value;
+                    static std::atomic<uint64_t> ready{0};
+                    const cudaError_t e = one_ready(k_gn_one<X, Y, V>, ready);
+                    if (e != cudaSuccess) return e;
+                    ProfScope ps(K_GNORM_FWD, s, 0.0, (double)samples * pixels * C * (sizeof(X) + sizeof(Y)));
+                    return launch_cluster(k_gn_one<X, Y, V>, dim3((unsigned)(samples * one.slabs * one.ks)), kGnThreads, one.ks, s, smem,
+                                          (const X*)x, ldx, stride_x, one, eps, mean, rstd, (Y*)y, ldy, stride_y);
+                });
+            });
+        }));
+        return NITRO_OK;
+    }
     const int batch = batch_size(h, pixels, type_size(x_type) + type_size(y_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
@@ -610,6 +1149,38 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
     if (!dx && !dgamma && !dbeta) return NITRO_OK;
     TRY(clear_once(h->clean, h->ticket, sizeof(uint32_t) * h->batch, s));
     const int v = pick_v(h, samples, {mx, mdy, mdx});
+    int smem = 0;
+    const GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), type_size(x_type) + 4, 2, act, gamma, beta, &smem);
+    if (one.ks) {
+        // the sums of at most a batch's samples are kept at a time
+        const int most = dgamma || dbeta ? std::max(kGnCtas, kGnBatch) : samples;
+        for (int s0 = 0; s0 < samples; s0 += most) {
+            const int n = std::min(most, samples - s0);
+            TRY(with_x(x_type, [&](auto xt) {
+                using X = decltype(xt);
+                return with_y(y_type, [&](auto yt) {
+                    using Y = decltype(yt);
+                    return with_v(v, [&](auto vt) {
+                        constexpr int V = decltype(vt)::value;
+                        static std::atomic<uint64_t> ready{0};
+                        const cudaError_t e = one_ready(k_gn_one_back<X, Y, V>, ready);
+                        if (e != cudaSuccess) return e;
+                        ProfScope ps(K_GNORM_BWD, s, 0.0, (double)n * pixels * C * (sizeof(X) + (dx ? 2 : 1) * sizeof(Y)));
+                        return launch_cluster(k_gn_one_back<X, Y, V>, dim3((unsigned)(n * one.slabs * one.ks)), kGnThreads, one.ks, s, smem,
+                                              sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0), lddy, stride_dy, one,
+                                              mean + (int64_t)s0 * h->groups, rstd + (int64_t)s0 * h->groups,
+                                              dgamma || dbeta ? h->part_c : nullptr,
+                                              dx ? const_cast<Y*>(sample_at<Y>(mdx, s0)) : nullptr, lddx, stride_dx);
+                    });
+                });
+            }));
+            if (dgamma || dbeta) {
+                ProfScope ps(K_GNORM_PARAMS, s, 0.0, 8.0 * n * C);
+                TRY(launch_k(k_gn_params, dim3((C + 31) / 32, 2), dim3(1024), 0, s, (const float*)h->part_c, n, C, dgamma, dbeta, (int)(s0 > 0)));
+            }
+        }
+        return NITRO_OK;
+    }
     const int batch = batch_size(h, pixels, type_size(x_type) + (dx ? 2 : 1) * type_size(y_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
