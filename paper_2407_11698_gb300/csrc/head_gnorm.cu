@@ -81,34 +81,51 @@ struct Vals {
         }
     }
 };
-// f(j, group) for V channels from c on, with one division
-template <int V, class F>
-__device__ __forceinline__ void each_channel(int c, int per, F&& f) {
-    int g = c / per, r = c - g * per;
+// A channel's group and its place there; per: channels of a group
+struct GnGroup {
+    int g, r, per;
+    // f(j, group) for V channels from there on; alike: they are of one group
+    template <int V, class F>
+    __device__ __forceinline__ void each(bool alike, F&& f) const {
+        int gj = g, rj = r;
 #pragma unroll
-    for (int j = 0; j < V; ++j) {
-        f(j, g);
-        if (++r == per) r = 0, ++g;
+        for (int j = 0; j < V; ++j) {
+            f(j, gj);
+            if (!alike && ++rj == per) rj = 0, ++gj;
+        }
     }
-}
+};
 __device__ __forceinline__ float& at2(float2* v, int j) { return j & 1 ? v[j >> 1].y : v[j >> 1].x; }
 
 // A thread's channels: statistics of their groups, gamma and beta
 template <int V>
 struct GnChannels {
     static constexpr int N = (V + 1) / 2;
-    float2 m[N], r[N], gamma[N], beta[N];
-    __device__ __forceinline__ void params(int c, const float* g, const float* b) {
+    alignas(16) float2 gamma[N + (N & 1)], beta[N + (N & 1)];
+    float2 m[N], r[N];
+    static __device__ __forceinline__ void param(const float* p, float none, int c, float2* v) {
+        if (p && V > 1 && ((uintptr_t)p & 15) == 0) {
 #pragma unroll
-        for (int j = 0; j < 2 * N; ++j) {
-            at2(gamma, j) = g && j < V ? g[c + j] : 1.0f;
-            at2(beta, j) = b && j < V ? b[c + j] : 0.0f;
+            for (int j = 0; j < N; j += 2) *reinterpret_cast<float4*>(v + j) = *reinterpret_cast<const float4*>(p + c + 2 * j);
+        } else {
+#pragma unroll
+            for (int j = 0; j < 2 * N; ++j) at2(v, j) = p && j < V ? p[c + j] : none;
         }
     }
+    __device__ __forceinline__ void params(int c, const float* g, const float* b) {
+        param(g, 1.0f, c, gamma);
+        param(b, 0.0f, c, beta);
+    }
     // statistics of a sample's groups
-    __device__ __forceinline__ void stats(int c, int per, const float* mean, const float* rstd) {
+    __device__ __forceinline__ void stats(const GnGroup& at, bool alike, const float* mean, const float* rstd) {
+        if (alike) {
+            const float a = mean[at.g], b = rstd[at.g];
+#pragma unroll
+            for (int j = 0; j < N; ++j) m[j] = pair(a), r[j] = pair(b);
+            return;
+        }
         m[N - 1].y = r[N - 1].y = 0.0f;
-        each_channel<V>(c, per, [&](int j, int g) {
+        at.each<V>(false, [&](int j, int g) {
             at2(m, j) = mean[g];
             at2(r, j) = rstd[g];
         });
@@ -179,7 +196,7 @@ struct Sums {
     }
     // to means, from origin(group) on, in sum and squared distances in sq, of n values
     template <class F>
-    __device__ __forceinline__ void finish(float n, int c, int per, F&& origin) {
+    __device__ __forceinline__ void finish(float n, const GnGroup& at, bool alike, F&& origin) {
         const float one = n > 0.0f ? rcp(n) : 0.0f;
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -188,7 +205,8 @@ struct Sums {
             sq[j] = make_float2(sq[j].x < 0.0f ? 0.0f : sq[j].x, sq[j].y < 0.0f ? 0.0f : sq[j].y);     // (a NaN stays)
             sum[j] = m;
         }
-        each_channel<V>(c, per, [&](int j, int g) { at2(sum, j) = n > 0.0f ? at2(sum, j) + (at2(k, j) - origin(g)) : 0.0f; });
+        const float first = origin(at.g);
+        at.each<V>(alike, [&](int j, int g) { at2(sum, j) = n > 0.0f ? at2(sum, j) + (at2(k, j) - (alike ? first : origin(g))) : 0.0f; });
     }
 };
 
@@ -217,6 +235,10 @@ struct GnPlace {
     __device__ __forceinline__ int channel(const GnShape& s, int i) const {
         const int c = (i * s.vecs + vec) * V;
         return live && c < s.channels ? c : -1;
+    }
+    __device__ __forceinline__ GnGroup group(const GnShape& s, int c) const {
+        const int g = c / s.per;
+        return {g, c - g * s.per, s.per};
     }
 };
 
@@ -268,7 +290,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
                 Vals<X, V>::load(src, v);
                 t.add(v);
             }
-            t.finish((float)max(0, (np - at.row + s.rows - 1) / s.rows), c, s.per, origin);      // 0 for rows past the chunk
+            t.finish((float)max(0, (np - at.row + s.rows - 1) / s.rows), at.group(s, c), s.per % V == 0, origin);      // 0 for rows past the chunk
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 red[0][at.row * width + at.vec * V + j] = at2(t.sum, j);
@@ -322,7 +344,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
         if (c < 0) continue;
         GnChannels<V> ch;
         ch.params(c, s.gamma, s.beta);
-        ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+        ch.stats(at.group(s, c), s.per % V == 0, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
 #pragma unroll
         for (int j = 0; j < ch.N; ++j) ch.r[j] = mul2(ch.r[j], ch.gamma[j]);
         const X* src = x + sample * sx + (int64_t)(p0 + at.row) * ldx + c;
@@ -358,7 +380,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_sums(const X* x, int64_t l
         if (c >= 0) {
             GnChannels<V> ch;
             ch.params(c, s.gamma, s.beta);
-            ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+            ch.stats(at.group(s, c), s.per % V == 0, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
             float2 a[ch.N], b[ch.N];
 #pragma unroll
             for (int j = 0; j < ch.N; ++j) a[j] = b[j] = pair(0.0f);
@@ -438,12 +460,12 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_dx(const X* x, int64_t ldx
         if (c < 0) continue;
         GnChannels<V> ch, to;
         ch.params(c, s.gamma, s.beta);
-        ch.stats(c, s.per, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
+        ch.stats(at.group(s, c), s.per % V == 0, mean + (int64_t)sample * s.groups, rstd + (int64_t)sample * s.groups);
         to = ch;
         {
             float2 u[ch.N], v[ch.N];
             u[ch.N - 1].y = v[ch.N - 1].y = 0.0f;
-            each_channel<V>(c, s.per, [&](int j, int g) {
+            at.group(s, c).template each<V>(s.per % V == 0, [&](int j, int g) {
                 const float2 t = means[(int64_t)sample * s.groups + g];
                 at2(u, j) = t.x;
                 at2(v, j) = t.y;
@@ -480,9 +502,11 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_dx(const X* x, int64_t ldx
 constexpr int kGnWarps = kGnThreads / 32;
 struct GnOne {
     int pixels, channels, groups, per;
-    int width, slabs, ks;                // channels of a slab, slabs of a sample, CTAs of a cluster
-    int vecs, lanes;                     // vectors of a slab's pixel, and lanes
+    int width, gs, slabs, ks;            // channels and groups of a slab, slabs of a sample, CTAs of a cluster
+    int vecs, lane_log;                  // vectors of a slab's pixel, and the lanes' logarithm
     int chunk, steps;                    // pixels of a CTA, of which a thread takes every (256 / lanes)th
+    int alike, entries;                  // vectors are of one group each; a group's vectors, or its channels where they are not
+    FloorDiv32 by_per;
     int act;
     const float* gamma;                  // or null
     const float* beta;                   // or null
@@ -536,29 +560,33 @@ __device__ __forceinline__ float ld_remote(const float* p, uint32_t rank) {
     asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_smem(smem_u32(p), rank)) : "memory");
     return v;
 }
-__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.release;" ::: "memory"); }
-__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait.acquire;" ::: "memory"); }
+// (nothing is handed over: peers learn that their shared memory has been read)
+__device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
+__device__ __forceinline__ void cluster_wait() { asm volatile("barrier.cluster.wait;" ::: "memory"); }
 
-// A thread's part of a slab
+// A thread's part of a slab.  Grid: (slabs ks, samples)
 struct GnPart {
-    int sample, rank, c, g0, row, rows, np;       // first channel (-1: idle lane), the slab's first group, first pixel of the chunk's, step, pixels
+    int sample, rank, c, g0, row, rows;           // first channel (-1: idle lane), the slab's first group, first pixel of the chunk's, step
     int count, stage;                             // pixels that the thread takes, of a stage
     int64_t p0;
+    GnGroup group;                                // of the first channel
     __device__ __forceinline__ GnPart(const GnOne& s, int v) {
-        const int unit = blockIdx.x / s.ks, slab = unit % s.slabs, lane = threadIdx.x & 31, per_warp = 32 / s.lanes;
-        rank = blockIdx.x - unit * s.ks;
-        sample = unit / s.slabs;
-        const int vec = lane & (s.lanes - 1);
-        row = (threadIdx.x >> 5) * per_warp + lane / s.lanes;
-        rows = kGnWarps * per_warp;
-        c = vec < s.vecs ? slab * s.width + vec * v : -1;
-        g0 = slab * (s.width / s.per);
+        const int slab = blockIdx.x / (unsigned)s.ks, vec = threadIdx.x & ((1 << s.lane_log) - 1);
+        rank = blockIdx.x - slab * s.ks;
+        sample = blockIdx.y;
+        row = threadIdx.x >> s.lane_log;
+        rows = kGnThreads >> s.lane_log;
+        const int first = slab * s.width + min(vec, s.vecs - 1) * v, g = s.by_per.udiv(first);
+        group = {g, first - g * s.per, s.per};
+        c = vec < s.vecs ? first : -1;
+        g0 = slab * s.gs;
         p0 = (int64_t)rank * s.chunk;
-        np = max(0, min(s.chunk, s.pixels - rank * s.chunk));
-        count = c >= 0 && row < np ? (np - row + rows - 1) / rows : 0;
+        const int np = min(s.chunk, s.pixels - rank * s.chunk);
+        count = c >= 0 && row < np ? (np - row + rows - 1) >> (8 - s.lane_log) : 0;
         stage = (s.steps + kGnStages - 1) / kGnStages;
     }
 };
+static_assert(kGnThreads == 256, "rows are 256 / lanes");
 
 template <typename X, typename Y, int V>
 __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ldx, int64_t sx, const GnOne s, float eps, float* mean,
@@ -566,7 +594,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     using SX = Slots<X, V>;
     constexpr int N = (V + 1) / 2;
     extern __shared__ __align__(16) uint8_t data[];
-    const int gs = s.width / s.per;
+    const int gs = s.gs, lanes = 1 << s.lane_log;
     float* warp_m = reinterpret_cast<float*>(data + (s.steps * SX::STEP + 15) / 16 * 16);      // [warps][entries] means, from the group's origin
     float* warp_q = warp_m + kGnWarps * s.width;                                               // and squared distances
     float* group = warp_q + kGnWarps * s.width;                                                // [3][groups of the slab]: counts, means, distances
@@ -614,11 +642,9 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     }
     __syncthreads();                         // the origins are there
     float n = (float)at.count;
-    if (at.c >= 0) t.finish(n, at.c, s.per, [&](int g) { return stat[g - at.g0]; });
+    t.finish(n, at.group, s.alike, [&](int g) { return stat[g - at.g0]; });
     // A vector of one group goes on as one entry, others channel by channel
-    const bool whole = s.per % V == 0;
-    const int entry = whole ? V : 1;         // channels of an entry
-    if (whole) {
+    if (s.alike) {
         float2 m = t.sum[0];
 #pragma unroll
         for (int j = 1; j < N; ++j) m = add2(m, t.sum[j]);
@@ -633,7 +659,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
         }
         a.q = V == 1 ? t.sq[0].x : q.x + q.y;
         if (n == 0.0f) a = Moments();
-        a.join(s.lanes, 16);
+        a.join(lanes, 16);
         if (lane < s.vecs) {
             warp_m[warp * s.width + lane] = a.m;
             warp_q[warp * s.width + lane] = a.q;
@@ -645,7 +671,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
         for (int j = 0; j < V; ++j) {
             Moments a;
             a.n = n, a.m = at2(t.sum, j), a.q = at2(t.sq, j);
-            a.join(s.lanes, 16);
+            a.join(lanes, 16);
             if (lane < s.vecs) {
                 warp_m[warp * s.width + lane * V + j] = a.m;
                 warp_q[warp * s.width + lane * V + j] = a.q;
@@ -657,7 +683,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     __syncthreads();
     // a group's entries: those of a warp to a lane of eight
     for (int g0 = 0; g0 < gs; g0 += kGnThreads / kGnWarps) {
-        const int g = g0 + threadIdx.x / kGnWarps, w = threadIdx.x % kGnWarps, per = s.per / entry;
+        const int g = g0 + threadIdx.x / kGnWarps, w = threadIdx.x % kGnWarps, per = s.entries;
         Moments a;
         if (g < gs)
             for (int i = 0; i < per; ++i) a.add(warp_n[w], warp_m[w * s.width + g * per + i], warp_q[w * s.width + g * per + i]);
@@ -682,7 +708,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     if (s.ks > 1) cluster_arrive();          // this CTA has read its peers' shared memory
     __syncthreads();
     if (at.count > 0) {
-        ch.stats(at.c, s.per, stat - at.g0, stat + gs - at.g0);
+        ch.stats(at.group, s.alike, stat - at.g0, stat + gs - at.g0);
 #pragma unroll
         for (int j = 0; j < N; ++j) ch.r[j] = mul2(ch.r[j], ch.gamma[j]);
         Y* dst = y + at.sample * sy + (at.p0 + at.row) * ldy + at.c;
@@ -712,7 +738,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
     using SD = Slots<float, V>;
     constexpr int N = (V + 1) / 2;
     extern __shared__ __align__(16) uint8_t data[];
-    const int xb = (s.steps * SX::STEP + 15) / 16 * 16, gs = s.width / s.per;
+    const int xb = (s.steps * SX::STEP + 15) / 16 * 16, gs = s.gs;
     uint8_t* grads = data + xb;
     float* warp_s = reinterpret_cast<float*>(grads + s.steps * SD::STEP);      // [2][warps][width]
     float* chan = warp_s + 2 * kGnWarps * s.width;                             // [2][width]
@@ -742,7 +768,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
     for (int j = 0; j < N; ++j) a[j] = b[j] = pair(0.0f);
     if (at.c >= 0) {
         ch.params(at.c, s.gamma, s.beta);
-        ch.stats(at.c, s.per, mean + (int64_t)at.sample * s.groups, rstd + (int64_t)at.sample * s.groups);
+        ch.stats(at.group, s.alike, mean + (int64_t)at.sample * s.groups, rstd + (int64_t)at.sample * s.groups);
     }
     with_act(s.act, [&](auto act) {
         const uint8_t* tx = xslot;
@@ -765,7 +791,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
             }
         }
     });
-    for (int d = s.lanes; d < 32; d <<= 1) {
+    for (int d = 1 << s.lane_log; d < 32; d <<= 1) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
             a[j] = add2(a[j], make_float2(__shfl_xor_sync(0xffffffffu, a[j].x, d), V > 1 ? __shfl_xor_sync(0xffffffffu, a[j].y, d) : 0.0f));
@@ -824,7 +850,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
         __syncthreads();
         if (at.count > 0) {
             a[N - 1].y = b[N - 1].y = 0.0f;
-            each_channel<V>(at.c, s.per, [&](int j, int g) {
+            at.group.template each<V>(s.alike, [&](int j, int g) {
                 at2(a, j) = means[g - at.g0];
                 at2(b, j) = means[gs + g - at.g0];
             });
@@ -977,17 +1003,21 @@ GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size,
     s.channels = h->channels;
     s.groups = h->groups;
     s.per = h->channels / h->groups;
+    s.by_per = FloorDiv32::make(s.per);
     s.act = act;
     s.gamma = gamma;
     s.beta = beta;
     const int sms = sm_count();
     const auto fit = [&](int m, int ks, int budget) {      // m groups a slab
         s.width = m * s.per;
+        s.gs = m;
         s.slabs = h->groups / m;
         s.ks = ks;
         s.vecs = s.width / v;
-        for (s.lanes = 1; s.lanes < s.vecs;) s.lanes *= 2;
-        const int rows = kGnThreads / s.lanes;
+        s.alike = s.per % v == 0;
+        s.entries = s.alike ? s.per / v : s.per;
+        for (s.lane_log = 0; 1 << s.lane_log < s.vecs;) ++s.lane_log;
+        const int rows = kGnThreads >> s.lane_log;
         s.chunk = (pixels + ks - 1) / ks;
         s.steps = (s.chunk + rows - 1) / rows;
         const int64_t bytes = (int64_t)s.steps * kGnThreads * v * value_bytes + 32 + 4 * (2 * kGnWarps + 2) * (int64_t)s.width + 20 * m;
@@ -1011,7 +1041,7 @@ GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size,
     for (int budget : {share, 110 * 1024, 224 * 1024})
         for (int line = widest; line >= 16; line /= 2)
             for (int ks = 1; ks <= 8; ks *= 2) {
-                if (!fit(slab(line), ks, budget) || (int64_t)samples * s.slabs * 8 > INT32_MAX) continue;
+                if (!fit(slab(line), ks, budget)) continue;
                 const int least = ks;
                 while (ks < 8 && (int64_t)samples * s.slabs * ks * 2 <= 2 * sms && s.steps > 2 * (ks / least)) ks *= 2;
                 if (ks > least) fit(slab(line), ks, budget);
@@ -1083,7 +1113,7 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
                     const cudaError_t e = one_ready(k_gn_one<X, Y, V>, ready);
                     if (e != cudaSuccess) return e;
                     ProfScope ps(K_GNORM_FWD, s, 0.0, (double)samples * pixels * C * (sizeof(X) + sizeof(Y)));
-                    return launch_cluster(k_gn_one<X, Y, V>, dim3((unsigned)(samples * one.slabs * one.ks)), kGnThreads, one.ks, s, smem,
+                    return launch_cluster(k_gn_one<X, Y, V>, dim3(one.slabs * one.ks, samples), kGnThreads, one.ks, s, smem,
                                           (const X*)x, ldx, stride_x, one, eps, mean, rstd, (Y*)y, ldy, stride_y);
                 });
             });
@@ -1166,7 +1196,7 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
                         const cudaError_t e = one_ready(k_gn_one_back<X, Y, V>, ready);
                         if (e != cudaSuccess) return e;
                         ProfScope ps(K_GNORM_BWD, s, 0.0, (double)n * pixels * C * (sizeof(X) + (dx ? 2 : 1) * sizeof(Y)));
-                        return launch_cluster(k_gn_one_back<X, Y, V>, dim3((unsigned)(n * one.slabs * one.ks)), kGnThreads, one.ks, s, smem,
+                        return launch_cluster(k_gn_one_back<X, Y, V>, dim3(one.slabs * one.ks, n), kGnThreads, one.ks, s, smem,
                                               sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0), lddy, stride_dy, one,
                                               mean + (int64_t)s0 * h->groups, rstd + (int64_t)s0 * h->groups,
                                               dgamma || dbeta ? h->part_c : nullptr,
