@@ -1,9 +1,12 @@
 // The norm over many gradients, sqrt(sum x^2) over all values of all matrices, and the gradients scaled by
 // min(1, max_norm / norm).
 //
-// At creation the matrices are cut into pieces of about equal size, kept in a table on the device; CTA i takes pieces i,
-// i + CTAs, ...  A first pass leaves each CTA's sums, the last CTA adds them in 64 bits in the CTAs' order, and a second pass
-// scales.  Squares are summed three times, of x, of x 2^-80 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
+// At creation the matrices are cut into pieces, kept in a table on the device, so that each warp of one CTA an SM has about
+// the same bytes.  One cooperative launch: the warps sum their pieces' squares, every CTA waits for
+// all CTAs' sums and adds them in 64 bits in the same order, and the warps scale their pieces, last ones first (the second level cache
+// holds them).  A warp's first 13 KB stay in shared memory in between, so that up to 31 MB of
+// gradients are read once; where there are more, 7 KB, and the others come through a ring of places there.
+// Squares are summed three times, of x, of x 2^-80 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
 // loses values below 2^-75, and where its sum shows that, one of the others stands for it.
 #include <new>
 
@@ -17,165 +20,378 @@ using namespace nitro;
 namespace nitro {
 namespace {
 
-constexpr int kClipThreads = 256;
-constexpr int kClipCtas = 8;                       // an SM
-constexpr int64_t kMostPieces = (int64_t)1 << 22;
+constexpr int kClipThreads = 512, kClipWarps = kClipThreads / 32;
+constexpr int kClipPlaces = 27;                                   // vectors of a lane in shared memory
+constexpr int kClipGroups = 3, kClipGroup = 4;                    // of those the ones under way, in groups, where not all are to stay
+constexpr int kClipRing = kClipGroups * kClipGroup;
+constexpr int kClipSmem = kClipPlaces * kClipThreads * 16;
+constexpr int kClipNotes = 5;                                     // that a lane looks at together
+constexpr int64_t kMostPieces = (int64_t)1 << 26;
 
 // Rows of one matrix (of lone rows: a run of one).  vec: both sides' rows start at multiples of 16 bytes
 struct Piece {
     const void* in;
     void* out;             // or null
-    int64_t rows, cols, ld_in, ld_out;
+    int64_t ld_in, ld_out;
+    int rows, cols;
     int type, vec;
 };
 
+// What a warp does: its first piece, how many it has, and where the others are
+struct alignas(16) Work {
+    Piece first;
+    int n, rest;
+};
+
 struct Squares {
-    float mid = 0.0f, big = 0.0f, small = 0.0f;
-    __device__ __forceinline__ void add(float x) {
-        mid = fmaf(x, x, mid);
-        const float b = x * 0x1p-80f, s = x * 0x1p90f;
-        big = fmaf(b, b, big);
-        small = fmaf(s, s, small);
+    float2 mid = {0.0f, 0.0f}, big = {0.0f, 0.0f}, small = {0.0f, 0.0f};
+    __device__ __forceinline__ void add(float2 x) {
+        mid = fma2(x, x, mid);
+        const float2 b = mul2(x, pair(0x1p-80f)), s = mul2(x, pair(0x1p90f));
+        big = fma2(b, b, big);
+        small = fma2(s, s, small);
     }
 };
 
-__device__ __forceinline__ double warp_sum(double v) {
+template <typename T>
+__device__ __forceinline__ T warp_sum(T v) {
 #pragma unroll
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
 
+// A type's 16 bytes as pairs of fp32 and back, and one value
 template <typename T>
 struct Of;
 template <>
 struct Of<uint16_t> {
+    static constexpr int V = 8;
+    static __device__ __forceinline__ void get(const uint4& u, float2* v) {
+        const uint32_t w[4] = {u.x, u.y, u.z, u.w};
+#pragma unroll
+        for (int j = 0; j < 4; ++j) v[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    }
+    static __device__ __forceinline__ uint4 put(const float2* v) {
+        return make_uint4(pack_bf16(v[0].x, v[0].y), pack_bf16(v[1].x, v[1].y), pack_bf16(v[2].x, v[2].y), pack_bf16(v[3].x, v[3].y));
+    }
     static __device__ __forceinline__ float get(uint16_t v) { return __uint_as_float((uint32_t)v << 16); }
     static __device__ __forceinline__ uint16_t put(float v) { return __bfloat16_as_ushort(__float2bfloat16_rn(v)); }
 };
 template <>
 struct Of<float> {
+    static constexpr int V = 4;
+    static __device__ __forceinline__ void get(const uint4& u, float2* v) {
+        v[0] = make_float2(__uint_as_float(u.x), __uint_as_float(u.y));
+        v[1] = make_float2(__uint_as_float(u.z), __uint_as_float(u.w));
+    }
+    static __device__ __forceinline__ uint4 put(const float2* v) {
+        return make_uint4(__float_as_uint(v[0].x), __float_as_uint(v[0].y), __float_as_uint(v[1].x), __float_as_uint(v[1].y));
+    }
     static __device__ __forceinline__ float get(float v) { return v; }
     static __device__ __forceinline__ float put(float v) { return v; }
 };
 template <>
 struct Of<int64_t> {
+    static constexpr int V = 2;
+    static __device__ __forceinline__ void get(const uint4& u, float2* v) {
+        v[0] = make_float2((float)(int64_t)(u.x | (uint64_t)u.y << 32), (float)(int64_t)(u.z | (uint64_t)u.w << 32));
+    }
     static __device__ __forceinline__ float get(int64_t v) { return (float)v; }
-    static __device__ __forceinline__ int64_t put(float v) { return (int64_t)v; }
 };
 
-// f(values, valid ones, address in `out` of the first) for the vectors of a piece, or its values one by one
+// A piece's work: whole vectors, `items` of them in rows of `per`, and single values, the rows' ends or all of them.
+template <typename T>
+struct Parts {
+    static constexpr int V = Of<T>::V;
+    int per, tail;              // whole vectors of a row, and values after them
+    int items, singles;         // (a piece has at most 2^30 bytes)
+    __device__ __forceinline__ explicit Parts(const Piece& p) {
+        per = p.vec ? p.cols / V : 0;
+        tail = p.cols - per * V;
+        items = p.rows * per;
+        singles = p.rows * tail;
+    }
+    // steps that a warp takes for the vectors
+    __device__ __forceinline__ int steps() const { return (items + 31) / 32; }
+};
+// f(in, out) with the addresses of vector i
 template <typename T, class F>
-__device__ __forceinline__ void each(const Piece& p, F&& f) {
-    constexpr int V = 16 / (int)sizeof(T);
-    const T* in = static_cast<const T*>(p.in);
-    T* out = static_cast<T*>(p.out);
-    if (p.vec) {
-        const int64_t per = (p.cols + V - 1) / V, items = p.rows * per;
-        RowWalk at(threadIdx.x, kClipThreads, (int)per);
+__device__ __forceinline__ void at_vector(const Piece& p, const Parts<T>& q, int i, F&& f) {
+    int row = 0, c = i;
+    if (p.rows > 1) {
+        row = (uint32_t)i / (uint32_t)q.per;
+        c = i - row * q.per;
+    }
+    f(static_cast<const T*>(p.in) + row * p.ld_in + c * Of<T>::V, static_cast<T*>(p.out) + row * p.ld_out + c * Of<T>::V);
+}
+template <typename T, class F>
+__device__ __forceinline__ void singles(const Piece& p, const Parts<T>& q, int lane, F&& f) {
+    if (q.tail == 0) return;
+    RowWalk at(lane, 32, q.tail);
 #pragma unroll 4
-        for (int64_t i = threadIdx.x; i < items; i += kClipThreads, at.next()) {
-            const int64_t c = (int64_t)at.part * V;
-            const T* src = in + at.row * p.ld_in + c;
-            T* dst = out + at.row * p.ld_out + c;
-            T v[V];
-            if (c + V <= p.cols) {
-                *reinterpret_cast<uint4*>(v) = *reinterpret_cast<const uint4*>(src);
-                f(v, dst, std::integral_constant<int, V>{});
-            } else {
-                for (int j = 0; j < p.cols - c; ++j) {
-                    v[0] = src[j];
-                    f(v, dst + j, std::integral_constant<int, 1>{});
-                }
-            }
+    for (int i = lane; i < q.singles; i += 32, at.next()) {
+        const int c = q.per * Of<T>::V + at.part;
+        f(static_cast<const T*>(p.in) + at.row * p.ld_in + c, static_cast<T*>(p.out) + at.row * p.ld_out + c);
+    }
+}
+
+__device__ __forceinline__ void copy16(uint4* to, const void* from) {
+    asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(smem_u32(to)), "l"(from) : "memory");
+}
+
+// Starts the copies of a piece's vectors while of `keep` places some are left; `kept`: the lane's first place.
+// Steps of the piece.
+template <typename T>
+__device__ __forceinline__ int keep_piece(const Piece& p, int lane, uint4* kept, int keep, int slot) {
+    const Parts<T> q(p);
+    const int steps = q.steps(), n = min(steps, keep - slot);
+#pragma unroll 4
+    for (int k = 0; k < n; ++k) {
+        const int i = k * 32 + lane;
+        if (i < q.items) at_vector<T>(p, q, i, [&](const T* in, T*) { copy16(kept + (slot + k) * 32, in); });
+    }
+    return steps;
+}
+
+// f(vector, its place in `out`) for the steps from `from` on, last ones first, through a ring of the lane's places
+template <typename T, class F>
+__device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, int lane, uint4* ring, int from, F&& f) {
+    const auto fetch = [&](int last, uint4* to) {       // steps last, last - 1, ...
+#pragma unroll
+        for (int j = 0; j < kClipGroup; ++j) {
+            const int step = last - j, i = step * 32 + lane;
+            if (step >= from && i < q.items) at_vector<T>(p, q, i, [&](const T* in, T*) { copy16(to + j * 32, in); });
         }
-        return;
+        asm volatile("cp.async.commit_group;" ::: "memory");
+    };
+    int k = q.steps() - 1;
+#pragma unroll
+    for (int g = 0; g < kClipGroups; ++g) fetch(k - g * kClipGroup, ring + g * kClipGroup * 32);
+    for (int g = 0; k >= from; k -= kClipGroup) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kClipGroups - 1) : "memory");
+        uint4* at = ring + g * kClipGroup * 32;
+        uint4 u[kClipGroup];
+#pragma unroll
+        for (int j = 0; j < kClipGroup; ++j) u[j] = at[j * 32];
+#pragma unroll
+        for (int j = 0; j < kClipGroup; ++j) {
+            const int step = k - j, i = step * 32 + lane;
+            if (step >= from && i < q.items) at_vector<T>(p, q, i, [&](const T*, T* out) { f(u[j], out); });
+        }
+        fetch(k - kClipRing, at);
+        if (++g == kClipGroups) g = 0;
     }
-    const int64_t items = p.rows * p.cols;
-    RowWalk at(threadIdx.x, kClipThreads, (int)p.cols);
+}
+
+template <typename T>
+__device__ __forceinline__ void sum_vector(const uint4& u, Squares& sum) {
+    float2 v[Of<T>::V / 2];
+    Of<T>::get(u, v);
+#pragma unroll
+    for (int j = 0; j < Of<T>::V / 2; ++j) sum.add(v[j]);
+}
+
+// Squares of what is not kept of a piece
+template <typename T>
+__device__ __forceinline__ int sum_piece(const Piece& p, int lane, uint4* ring, int keep, int slot, Squares& sum) {
+    const Parts<T> q(p);
+    const int steps = q.steps(), from = max(0, keep - slot);
+    if (steps > from) stream_piece<T>(p, q, lane, ring, from, [&](const uint4& u, T*) { sum_vector<T>(u, sum); });
+    singles<T>(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); });
+    return steps;
+}
+
+// and of what is
+template <typename T>
+__device__ __forceinline__ int sum_kept(const Piece& p, int lane, const uint4* kept, int keep, int slot, Squares& sum) {
+    const Parts<T> q(p);
+    const int steps = q.steps(), n = min(steps, keep - slot);
 #pragma unroll 4
-    for (int64_t i = threadIdx.x; i < items; i += kClipThreads, at.next()) {
-        T v[1] = {in[at.row * p.ld_in + at.part]};
-        f(v, out + at.row * p.ld_out + at.part, std::integral_constant<int, 1>{});
+    for (int k = 0; k < n; ++k)
+        if (k * 32 + lane < q.items) sum_vector<T>(kept[(slot + k) * 32], sum);
+    return steps;
+}
+
+// A piece scaled, its last vectors first; `slot` as above
+template <typename T>
+__device__ __forceinline__ void scale_piece(const Piece& p, int lane, const uint4* kept, uint4* ring, int keep, int slot, float f) {
+    const Parts<T> q(p);
+    singles<T>(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); });
+    const float2 f2 = pair(f);
+    const auto one = [&](uint4 u, T* out) {
+        if (f != 1.0f) {
+            float2 v[Of<T>::V / 2];
+            Of<T>::get(u, v);
+#pragma unroll
+            for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(v[j], f2);
+            u = Of<T>::put(v);
+        }
+        *reinterpret_cast<uint4*>(out) = u;
+    };
+    const int steps = q.steps(), left = min(steps, max(0, keep - slot));         // steps that are kept
+    if (steps > left) stream_piece<T>(p, q, lane, ring, left, one);
+#pragma unroll 4
+    for (int k = 0; k < left; ++k) {
+        const int i = k * 32 + lane;
+        if (i < q.items) at_vector<T>(p, q, i, [&](const T*, T* out) { one(kept[(slot + k) * 32], out); });
     }
+}
+
+// f(type's value) for a piece's type
+template <class F>
+__device__ __forceinline__ int with_type(int type, F&& f) {
+    if (type == NITRO_BF16) return f((uint16_t)0);
+    if (type == NITRO_F32) return f(0.0f);
+    return f((int64_t)0);
+}
+
+// What a CTA hands to the others: a number and the turn that it belongs to, as one access of 16 bytes
+struct alignas(16) Note {
+    uint64_t bits, turn;
+};
+__device__ __forceinline__ void put_note(Note* to, uint64_t bits, uint64_t turn) {
+    asm volatile("{\n .reg .b128 t;\n mov.b128 t, {%1, %2};\n st.relaxed.gpu.global.b128 [%0], t;\n}" ::"l"(to), "l"(bits), "l"(turn) : "memory");
+}
+__device__ __forceinline__ Note get_note(const Note* from) {
+    Note n;
+    asm volatile("{\n .reg .b128 t;\n ld.relaxed.gpu.global.b128 t, [%2];\n mov.b128 {%0, %1}, t;\n}" : "=l"(n.bits), "=l"(n.turn) : "l"(from) : "memory");
+    return n;
 }
 
 struct ClipArgs {
+    const Work* work;      // [warps]
     const Piece* pieces;
-    int n;
-    double* sums;          // [CTAs][3]
-    uint32_t* ticket;      // zero before and after
-    float* factor;
+    Note* notes;           // [CTAs][2]: the middle range's sum, and the others'
+    uint64_t* turn;        // how often the handle has run
     float* norm;
     float limit;           // 0: the norm alone
+    int keep;              // vectors of a lane that stay in shared memory: all places, where they hold all of them
+    uint32_t* status;
 };
 
-__global__ void __launch_bounds__(kClipThreads) k_clip_norm(const ClipArgs a) {
-    __shared__ double sh[3][kClipThreads / 32];
-    __shared__ int last;
-    pdl_wait();
-    Squares q;
-    for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
-        const Piece p = a.pieces[i];
-        const auto sum = [&](auto* v, auto*, auto n) {
-#pragma unroll
-            for (int j = 0; j < decltype(n)::value; ++j) q.add(Of<std::remove_reference_t<decltype(v[0])>>::get(v[j]));
-        };
-        if (p.type == NITRO_BF16) each<uint16_t>(p, sum);
-        else if (p.type == NITRO_F32) each<float>(p, sum);
-        else each<int64_t>(p, sum);
-    }
+__global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
+    extern __shared__ uint4 stash[];      // [warps][places][32]
+    __shared__ double sh[kClipWarps];
+    __shared__ float sh_big[kClipWarps], sh_small[kClipWarps];
+    __shared__ float factor;
+    __shared__ int ok;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-    const double s[3] = {warp_sum(q.mid), warp_sum(q.big), warp_sum(q.small)};
-    if (lane == 0)
-        for (int k = 0; k < 3; ++k) sh[k][warp] = s[k];
-    __syncthreads();
-    if (threadIdx.x < 3) {
-        double v = 0.0;
-        for (int w = 0; w < kClipThreads / 32; ++w) v += sh[threadIdx.x][w];
-        a.sums[blockIdx.x * 3 + threadIdx.x] = v;
-        __threadfence();
+    const int keep = a.keep;
+    uint4 *kept = stash + warp * kClipPlaces * 32 + lane, *ring = kept + (kClipPlaces - kClipRing) * 32;
+    const Work work = a.work[blockIdx.x * kClipWarps + warp];
+    const auto piece = [&](int i) { return i == 0 ? work.first : a.pieces[work.rest + i - 1]; };
+    const uint64_t turn = *a.turn + 1;
+    int slot = 0;
+    for (int i = 0; i < work.n && slot < keep; ++i) {
+        const Piece p = piece(i);
+        slot += with_type(p.type, [&](auto t) { return keep_piece<decltype(t)>(p, lane, kept, keep, slot); });
     }
-    __syncthreads();
-    if (threadIdx.x == 0) {
-        last = atomicAdd(a.ticket, 1u) == gridDim.x - 1;
-        if (last) *a.ticket = 0;
+    Squares q;
+    slot = 0;
+    for (int i = 0; i < work.n; ++i) {
+        const Piece p = piece(i);
+        slot += with_type(p.type, [&](auto t) { return sum_piece<decltype(t)>(p, lane, ring, keep, slot, q); });
     }
-    __syncthreads();
-    if (!last) return;
-    __threadfence();
-    if (warp < 3) {
-        double v = 0.0;
-        for (int i = lane; i < gridDim.x; i += 32) v += __ldcg(a.sums + i * 3 + warp);
-        v = warp_sum(v);
-        if (lane == 0) sh[warp][0] = v;
+    const int end = slot;
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    slot = 0;
+    for (int i = 0; i < work.n && slot < keep; ++i) {
+        const Piece p = piece(i);
+        slot += with_type(p.type, [&](auto t) { return sum_kept<decltype(t)>(p, lane, kept, keep, slot, q); });
     }
+    {
+        const double mid = warp_sum((double)q.mid.x + (double)q.mid.y);
+        const float big = warp_sum(q.big.x + q.big.y), small = warp_sum(q.small.x + q.small.y);
+        if (lane == 0) sh[warp] = mid, sh_big[warp] = big, sh_small[warp] = small;
+    }
+    if (threadIdx.x == 0) ok = 1;
     __syncthreads();
-    if (threadIdx.x != 0) return;
-    const double mid = sh[0][0], big = sh[1][0], small = sh[2][0];
-    double norm = sqrt(mid);
-    if (!(mid <= 3e38)) norm = sqrt(big) * 0x1p80;
-    else if (mid < 0x1p-60) norm = sqrt(small) * 0x1p-90;
-    *a.norm = (float)norm;
-    *a.factor = norm > (double)a.limit && norm <= 1e300 ? (float)((double)a.limit / norm) : 1.0f;
-}
-
-__global__ void __launch_bounds__(kClipThreads) k_clip_scale(const ClipArgs a) {
-    pdl_wait();
-    const float f = *a.factor;
-    for (int i = blockIdx.x; i < a.n; i += gridDim.x) {
-        const Piece p = a.pieces[i];
-        if (!p.out || (f == 1.0f && p.out == p.in)) continue;
-        const auto scale = [&](auto* v, auto* dst, auto n) {
-            constexpr int V = decltype(n)::value;
-            using T = std::remove_reference_t<decltype(v[0])>;
-            T w[V];
+    if (warp == 0) {
+        const bool mine = lane < kClipWarps;
+        double mid = warp_sum(mine ? sh[lane] : 0.0);
+        double big = warp_sum(mine ? sh_big[lane] : 0.0f), small = warp_sum(mine ? sh_small[lane] : 0.0f);
+        if (gridDim.x > 1) {
+            // Every CTA takes all CTAs' notes of this turn (of the norm alone: the first one).
+            if (lane == 0) {
+                put_note(a.notes + 2 * blockIdx.x, __double_as_longlong(mid), turn);
+                put_note(a.notes + 2 * blockIdx.x + 1, __float_as_uint((float)big) | (uint64_t)__float_as_uint((float)small) << 32, turn);
+            }
+            if (a.limit == 0.0f && blockIdx.x != 0) return;
+            const uint64_t t0 = global_ns();
+            double all = 0.0;
+            float all_big = 0.0f, all_small = 0.0f;
+            bool in_time = true;
+            for (int i0 = lane; i0 < gridDim.x && in_time; i0 += 32 * kClipNotes) {
+                Note m[kClipNotes], o[kClipNotes];
+                for (uint32_t k = 1;; ++k) {
+                    bool here = true;
 #pragma unroll
-            for (int j = 0; j < V; ++j) w[j] = f == 1.0f ? v[j] : Of<T>::put(Of<T>::get(v[j]) * f);
-            if constexpr (V * sizeof(T) == 16) *reinterpret_cast<uint4*>(dst) = *reinterpret_cast<uint4*>(w);
-            else *dst = w[0];
-        };
-        if (p.type == NITRO_BF16) each<uint16_t>(p, scale);
-        else each<float>(p, scale);
+                    for (int j = 0; j < kClipNotes; ++j) {
+                        const int i = min(i0 + 32 * j, (int)gridDim.x - 1);
+                        m[j] = get_note(a.notes + 2 * i);
+                        o[j] = get_note(a.notes + 2 * i + 1);
+                    }
+#pragma unroll
+                    for (int j = 0; j < kClipNotes; ++j) here = here && m[j].turn == turn && o[j].turn == turn;
+                    if (here) break;
+                    if ((k & 63) == 0 && global_ns() - t0 > kWaitNs) {
+                        in_time = false;
+                        break;
+                    }
+                }
+#pragma unroll
+                for (int j = 0; j < kClipNotes; ++j) {
+                    if (i0 + 32 * j >= gridDim.x) continue;
+                    all += __longlong_as_double(m[j].bits);
+                    all_big += __uint_as_float((uint32_t)o[j].bits);
+                    all_small += __uint_as_float((uint32_t)(o[j].bits >> 32));
+                }
+            }
+            if (!__all_sync(0xffffffffu, in_time) && lane == 0) {
+                atomicOr(a.status, ST_TIMEOUT);
+                ok = 0;
+            }
+            mid = warp_sum(all);
+            if (!(mid <= 1e38 && mid >= 0x1p-60)) big = warp_sum((double)all_big), small = warp_sum((double)all_small);
+        }
+        if (lane == 0) {
+            double norm;
+            if (mid <= 1e38 && mid >= 0x1p-60) {
+                // the 32-bit root and one of Newton's steps (a double's root and quotients take a microsecond here)
+                const float y = sqrtf((float)mid);
+                norm = (double)y + (double)((float)(mid - (double)y * y) * (0.5f / y));
+            } else if (mid < 0x1p-60) {
+                norm = sqrt(small) * 0x1p-90;
+            } else {
+                norm = sqrt(big) * 0x1p80;
+            }
+            if (blockIdx.x == 0) {
+                *a.norm = (float)norm;
+                *a.turn = turn;              // every CTA has read it: its notes are there
+            }
+            float f = 1.0f;
+            if (norm > (double)a.limit && norm <= 1e300) {
+                f = a.limit / (float)norm;
+                if (norm < 1e38 && norm > 1e-30) f += (float)((double)a.limit - (double)f * norm) / (float)norm;
+                else f = (float)((double)a.limit / norm);
+            }
+            factor = f;
+        }
+    }
+    if (a.limit == 0.0f) return;
+    __syncthreads();
+    if (!ok) return;
+    const float f = factor;
+    slot = end;
+    for (int i = work.n - 1; i >= 0; --i) {
+        const Piece p = piece(i);
+        with_type(p.type, [&](auto t) {
+            using T = decltype(t);
+            slot -= Parts<T>(p).steps();
+            if constexpr (sizeof(T) < 8)
+                if (p.out && !(f == 1.0f && p.out == p.in)) scale_piece<T>(p, lane, kept, ring, keep, slot, f);
+            return 0;
+        });
     }
 }
 
@@ -204,23 +420,34 @@ bool overlap(const Range& a, const Range& b) {
 }  // namespace nitro
 
 struct nitro_clip {
-    int n = 0, ctas = 0;
+    int ctas = 0, keep = 0;
     bool writes = false;
     double bytes = 0.0;
     Piece* pieces = nullptr;
-    double* sums = nullptr;
-    float* factor = nullptr;
-    uint32_t* ticket = nullptr;
-    bool clean = false;              // the ticket, see clear_once
+    Work* work = nullptr;
+    Note* notes = nullptr;           // [CTAs][2], and the turn
+    bool clean = false;              // the notes, see clear_once
     StatusWord status;
     DeviceAllocs allocs;
 };
 
 namespace {
 
-// The pieces of all matrices into `to` (null: counted).  target: bytes of a piece
-int64_t cut(const nitro_clip_matrix* list, int count, int64_t target, Piece* to) {
-    int64_t n = 0;
+// Bytes that a piece costs beside its own: its description, and a step that it does not fill
+constexpr int64_t kPieceCost = 512;
+constexpr int64_t kLine = 512;       // a warp's vectors
+
+// All matrices as pieces, one warp's after another's: `share` of their cost to each.  to, first: null to count
+// last: the cost that was left for the last warp
+int64_t cut(const nitro_clip_matrix* list, int count, int64_t share, Piece* to, int* first, int warps, int64_t* last) {
+    int64_t n = 0, used = 0;
+    int w = 0;
+    if (first) first[0] = 0;
+    const auto next_warp = [&] {
+        used = 0;
+        ++w;
+        if (first && w <= warps) first[w] = (int)n;
+    };
     for (int i = 0; i < count; ++i) {
         nitro_clip_matrix m = list[i];
         if (m.rows == 0 || m.cols == 0) continue;
@@ -231,16 +458,30 @@ int64_t cut(const nitro_clip_matrix* list, int count, int64_t target, Piece* to)
         }
         const bool aligned = ((uintptr_t)m.in | (uintptr_t)m.out) % 16 == 0 &&
                              (m.rows == 1 || (m.ld_in * size % 16 == 0 && (!m.out || m.ld_out * size % 16 == 0)));
-        const int64_t per = std::max<int64_t>(16, target / size / 16 * 16);      // values: a multiple of 16 bytes
-        const int64_t wide = std::min(m.cols, per), tall = std::max<int64_t>(1, per / m.cols);
-        for (int64_t r = 0; r < m.rows; r += tall)
-            for (int64_t c = 0; c < m.cols; c += wide, ++n) {
-                if (!to) continue;
+        const int64_t wide = m.cols * size;
+        for (int64_t r = 0, c = 0; r < m.rows; ++n) {
+            // rows that are still the warp's; of rows longer than its share, whole lines; the last warp takes all that is left
+            const int64_t most = std::min<int64_t>(w + 1 < warps ? std::max(share - used - kPieceCost, kLine) : (int64_t)1 << 30, (int64_t)1 << 30);
+            int64_t rows = 1, cols = m.cols - c;
+            if (c == 0 && wide <= std::max(most, 4 * kLine)) rows = std::min(m.rows - r, std::max<int64_t>(1, most / wide));
+            else cols = std::min(cols, most / kLine * kLine / size);
+            if (to) {
                 const char* in = static_cast<const char*>(m.in) + (r * m.ld_in + c) * size;
                 char* out = m.out ? static_cast<char*>(m.out) + (r * m.ld_out + c) * size : nullptr;
-                to[n] = {in, out, std::min(tall, m.rows - r), std::min(wide, m.cols - c), m.ld_in, m.ld_out, m.type, aligned};
+                to[n] = {in, out, m.ld_in, m.ld_out, (int)rows, (int)cols, m.type, aligned};
             }
+            used += kPieceCost + rows * cols * size;
+            c += cols;
+            if (c == m.cols) c = 0, r += rows;
+            if (used + kPieceCost + kLine > share && w + 1 < warps) {
+                ++n;
+                next_warp();
+                --n;
+            }
+        }
     }
+    *last = w + 1 == warps ? used : 0;
+    while (w < warps) next_warp();
     return n;
 }
 
@@ -300,27 +541,52 @@ bool outs_apart(const nitro_clip_matrix* list, int count) {
 nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** out) {
     double bytes = 0.0;
     if (!clip_list_ok(list, count, &bytes) || !outs_apart(list, count)) return NITRO_ERR_ARG;
-    // Four pieces a CTA, so that none waits long for the last, of 4 to 64 KB
-    const int most = kClipCtas * sm_count();
-    int64_t target = std::min<int64_t>(65536, std::max<int64_t>(4096, (int64_t)(bytes / (4.0 * most))));
-    int64_t n = cut(list, count, target, nullptr);
-    while (n > kMostPieces && target < ((int64_t)1 << 30)) n = cut(list, count, target *= 4, nullptr);
-    if (n > ((int64_t)1 << 30)) return NITRO_ERR_ARG;
+    // an SM's worth of threads takes 16 KB at once: fewer CTAs where there is less, and a cheaper barrier
+    int64_t cost = 0;
+    for (int i = 0; i < count; ++i) {
+        const nitro_clip_matrix& m = list[i];
+        if (m.rows > 0 && m.cols > 0) cost += kPieceCost + m.rows * m.cols * value_size(m.type);
+    }
+    const int ctas = (int)std::max<int64_t>(1, std::min<int64_t>(sm_count(), (cost + 16383) / 16384)), warps = ctas * kClipWarps;
+    // (matrices that end inside a share, and rows, leave the others more than the mean)
+    int64_t share = std::max<int64_t>((cost + warps - 1) / warps + kLine, 2 * kPieceCost), last = 0, n = 0;
+    for (int tries = 0; tries < 64; ++tries, share += share / 64 + 64) {
+        n = cut(list, count, share, nullptr, nullptr, warps, &last);
+        if (last <= share) break;
+    }
+    if (n > kMostPieces) return NITRO_ERR_ARG;
     std::vector<Piece> host((size_t)n);
-    cut(list, count, target, host.data());
+    std::vector<int> first((size_t)warps + 1);
+    cut(list, count, share, host.data(), first.data(), warps, &last);
+    std::vector<Work> work((size_t)warps);
+    for (int w = 0; w < warps; ++w) {
+        work[w].n = first[w + 1] - first[w];
+        work[w].rest = first[w] + 1;
+        work[w].first = work[w].n ? host[first[w]] : Piece{};
+    }
     nitro_clip* h = new (std::nothrow) nitro_clip();
     if (!h) return NITRO_ERR_CUDA;
-    h->n = (int)n;
-    h->ctas = (int)std::max<int64_t>(1, std::min<int64_t>(n, most));
+    h->ctas = ctas;
+    int64_t most_steps = 0;
+    for (int w = 0; w < warps; ++w) {
+        int64_t steps = 0;
+        for (int i = first[w]; i < first[w + 1]; ++i) {
+            const Piece& p = host[i];
+            if (p.vec) steps += ((int64_t)p.rows * (p.cols * value_size(p.type) / 16) + 31) / 32;
+        }
+        most_steps = std::max(most_steps, steps);
+    }
+    h->keep = most_steps <= kClipPlaces ? kClipPlaces : kClipPlaces - kClipRing;
     h->bytes = bytes;
     for (int i = 0; i < count; ++i) h->writes = h->writes || (list[i].out && list[i].rows > 0 && list[i].cols > 0);
-    const bool ok = h->allocs.take(&h->pieces, std::max<int64_t>(n, 1)) && h->allocs.take(&h->sums, 3 * h->ctas) &&
-                    h->allocs.take(&h->factor, 1) && h->allocs.take(&h->ticket, 1) && h->status.take();
+    const bool ok = h->allocs.take(&h->pieces, std::max<int64_t>(n, 1)) && h->allocs.take(&h->work, warps) &&
+                    h->allocs.take(&h->notes, 2 * h->ctas + 1) && h->status.take();
     // (on a stream of its own: the default one may be busy, or part of a capture)
     cudaStream_t s = nullptr;
     bool copied = ok && cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking) == cudaSuccess;
     if (copied) {
         copied = (n == 0 || cudaMemcpyAsync(h->pieces, host.data(), sizeof(Piece) * (size_t)n, cudaMemcpyHostToDevice, s) == cudaSuccess) &&
+                 cudaMemcpyAsync(h->work, work.data(), sizeof(Work) * work.size(), cudaMemcpyHostToDevice, s) == cudaSuccess &&
                  cudaStreamSynchronize(s) == cudaSuccess;
         cudaStreamDestroy(s);
     }
@@ -350,16 +616,25 @@ nitro_status nitro_clip_create(const nitro_clip_matrix* list, int count, nitro_c
 nitro_status nitro_clip_run(nitro_clip* h, float max_norm, float* norm, void* stream) {
     if (!h || !norm || (uintptr_t)norm % 4 || !(max_norm >= 0.0f) || (max_norm > 0.0f && !h->writes)) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    TRY(clear_once(h->clean, h->ticket, sizeof(uint32_t), s));
-    const ClipArgs a{h->pieces, h->n, h->sums, h->ticket, h->factor, norm, max_norm};
-    {
-        ProfScope ps(K_CLIP, s, 0.0, h->bytes);
-        TRY(launch_k(k_clip_norm, dim3(h->ctas), dim3(kClipThreads), 0, s, a));
-    }
-    if (max_norm > 0.0f) {
-        ProfScope ps(K_CLIP, s, 0.0, 2.0 * h->bytes);
-        TRY(launch_k(k_clip_scale, dim3(h->ctas), dim3(kClipThreads), 0, s, a));
-    }
+    TRY(clear_once(h->clean, h->notes, (2 * h->ctas + 1) * sizeof(Note), s));
+    static std::atomic<uint64_t> ready{0};
+    int dev = 0;
+    sm_count(&dev);
+    TRY(once_per_device(ready, dev, [] { return cudaFuncSetAttribute(k_clip, cudaFuncAttributeMaxDynamicSharedMemorySize, kClipSmem); }));
+    const ClipArgs a{h->work, h->pieces, h->notes, &h->notes[2 * h->ctas].turn, norm, max_norm, h->keep, h->status.at};
+    ProfScope ps(K_CLIP, s, 0.0, (max_norm > 0.0f ? 2.0 : 1.0) * h->bytes);
+    // (its CTAs wait for one another)
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeCooperative;
+    attr[0].val.cooperative = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(h->ctas);
+    cfg.blockDim = dim3(kClipThreads);
+    cfg.dynamicSmemBytes = kClipSmem;
+    cfg.stream = s;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    TRY(cudaLaunchKernelEx(&cfg, k_clip, a));
     return NITRO_OK;
 }
 
