@@ -524,7 +524,7 @@ void nitro_glu_destroy(nitro_glu* h);
  * run: norm (fp32, one value) is written, and with max_norm > 0 every out = in min(1, max_norm / norm), rounded once;
  * with max_norm = 0 the norm alone is taken.  A sum of squares that is not finite (its norm is written: NaN or infinity)
  * scales by 1.  A norm beyond fp32 or the squares' range is no such sum: squares are taken in three ranges.  The sum is
- * in 64 bits over values' sums in 32, in an order that the handle's sizes fix.
+ * kept in pairs of 32-bit numbers over the threads, in an order that the handle's sizes fix.
  * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, 2^20], sizes below 0, strides below the columns
  * (with rows above 1), another type, int64 with an out, more than 2^40 values, an out that overlaps another
  * matrix, or in otherwise than by being it; max_norm below 0 or NaN, or above 0 where no matrix has an out. */

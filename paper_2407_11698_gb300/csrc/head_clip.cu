@@ -3,7 +3,7 @@
 //
 // At creation the matrices are cut into pieces, kept in a table on the device, so that each warp of one CTA an SM has about
 // the same bytes.  One cooperative launch: the warps sum their pieces' squares, every CTA waits for
-// all CTAs' sums and adds them in 64 bits in the same order, and the warps scale their pieces, last ones first (the second level cache
+// all CTAs' sums and adds them in the same order, and the warps scale their pieces, last ones first (the second level cache
 // holds them).  A warp's first 13 KB stay in shared memory in between, so that up to 31 MB of
 // gradients are read once; where there are more, 7 KB, and the others come through a ring of places there.
 // Squares are summed three times, of x, of x 2^-80 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
@@ -53,12 +53,26 @@ struct Squares {
     }
 };
 
-template <typename T>
-__device__ __forceinline__ T warp_sum(T v) {
-#pragma unroll
+__device__ __forceinline__ float warp_sum(float v) {
+#pragma unroll 1
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
     return v;
 }
+
+// A sum of 32-bit numbers with what its roundings leave over.  (64-bit additions would be as good, but one takes a warp
+// some hundred clocks here: the three sums over warps, CTAs and the grid took 2.5 us longer.)
+struct Exact {
+    float hi = 0.0f, lo = 0.0f;
+    __device__ __forceinline__ void add(float h, float l) {
+        const float s = hi + h, b = s - hi;
+        lo += l + ((hi - (s - b)) + (h - b));
+        hi = s;
+    }
+    __device__ __forceinline__ void over_warp() {
+#pragma unroll 1
+        for (int d = 16; d > 0; d >>= 1) add(__shfl_xor_sync(0xffffffffu, hi, d), __shfl_xor_sync(0xffffffffu, lo, d));
+    }
+};
 
 // A type's 16 bytes as pairs of fp32 and back, and one value
 template <typename T>
@@ -245,23 +259,56 @@ __device__ __forceinline__ int with_type(int type, F&& f) {
     return f((int64_t)0);
 }
 
-// What a CTA hands to the others: a number and the turn that it belongs to, as one access of 16 bytes
+// What a CTA hands to the others: two numbers and the turn that they belong to, as one access of 16 bytes
 struct alignas(16) Note {
-    uint64_t bits, turn;
+    float a, b;
+    uint64_t turn;
 };
-__device__ __forceinline__ void put_note(Note* to, uint64_t bits, uint64_t turn) {
+__device__ __forceinline__ void put_note(Note* to, float a, float b, uint64_t turn) {
+    const uint64_t bits = __float_as_uint(a) | (uint64_t)__float_as_uint(b) << 32;
     asm volatile("{\n .reg .b128 t;\n mov.b128 t, {%1, %2};\n st.relaxed.gpu.global.b128 [%0], t;\n}" ::"l"(to), "l"(bits), "l"(turn) : "memory");
 }
 __device__ __forceinline__ Note get_note(const Note* from) {
-    Note n;
-    asm volatile("{\n .reg .b128 t;\n ld.relaxed.gpu.global.b128 t, [%2];\n mov.b128 {%0, %1}, t;\n}" : "=l"(n.bits), "=l"(n.turn) : "l"(from) : "memory");
-    return n;
+    uint64_t bits, turn;
+    asm volatile("{\n .reg .b128 t;\n ld.relaxed.gpu.global.b128 t, [%2];\n mov.b128 {%0, %1}, t;\n}" : "=l"(bits), "=l"(turn) : "l"(from) : "memory");
+    return {__uint_as_float((uint32_t)bits), __uint_as_float((uint32_t)(bits >> 32)), turn};
 }
+// f(note) for every 32nd CTA's note, once it is of this turn; gives up after a while (in_time false)
+template <class F>
+__device__ __forceinline__ void take_notes(const Note* notes, uint64_t turn, int lane, uint64_t& t0, bool& in_time, F&& f) {
+    for (int i0 = lane; i0 < gridDim.x && in_time; i0 += 32 * kClipNotes) {
+        Note n[kClipNotes];
+        for (uint32_t k = 1;; ++k) {
+            bool here = true;
+#pragma unroll
+            for (int j = 0; j < kClipNotes; ++j)
+                if (i0 + 32 * j < gridDim.x) n[j] = get_note(notes + i0 + 32 * j);
+#pragma unroll
+            for (int j = 0; j < kClipNotes; ++j)
+                if (i0 + 32 * j < gridDim.x) here = here && n[j].turn == turn;
+            if (here) break;
+            if ((k & 63) == 0) {           // (a read of the timer takes longer than most waits)
+                const uint64_t now = global_ns();
+                if (t0 == 0) t0 = now;
+                if (now - t0 > kWaitNs) {
+                    in_time = false;
+                    break;
+                }
+            }
+        }
+#pragma unroll
+        for (int j = 0; j < kClipNotes; ++j)
+            if (i0 + 32 * j < gridDim.x) f(n[j]);
+    }
+}
+// Sums of plain squares that are right
+constexpr float kLeastMid = 0x1p-60f;
+__device__ __forceinline__ bool in_range(float mid) { return mid >= kLeastMid && mid <= 1e38f; }
 
 struct ClipArgs {
     const Work* work;      // [warps]
     const Piece* pieces;
-    Note* notes;           // [CTAs][2]: the middle range's sum, and the others'
+    Note* notes;           // [2][CTAs]: the plain squares' sum, and the others'
     uint64_t* turn;        // how often the handle has run
     float* norm;
     float limit;           // 0: the norm alone
@@ -271,8 +318,7 @@ struct ClipArgs {
 
 __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
     extern __shared__ uint4 stash[];      // [warps][places][32]
-    __shared__ double sh[kClipWarps];
-    __shared__ float sh_big[kClipWarps], sh_small[kClipWarps];
+    __shared__ float4 sh[kClipWarps];
     __shared__ float factor;
     __shared__ int ok;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -300,80 +346,65 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
         slot += with_type(p.type, [&](auto t) { return sum_kept<decltype(t)>(p, lane, kept, keep, slot, q); });
     }
     {
-        const double mid = warp_sum((double)q.mid.x + (double)q.mid.y);
+        Exact mid;
+        mid.add(q.mid.x, 0.0f);
+        mid.add(q.mid.y, 0.0f);
+        mid.over_warp();
         const float big = warp_sum(q.big.x + q.big.y), small = warp_sum(q.small.x + q.small.y);
-        if (lane == 0) sh[warp] = mid, sh_big[warp] = big, sh_small[warp] = small;
+        if (lane == 0) sh[warp] = make_float4(mid.hi, mid.lo, big, small);
     }
     if (threadIdx.x == 0) ok = 1;
     __syncthreads();
     if (warp == 0) {
-        const bool mine = lane < kClipWarps;
-        double mid = warp_sum(mine ? sh[lane] : 0.0);
-        double big = warp_sum(mine ? sh_big[lane] : 0.0f), small = warp_sum(mine ? sh_small[lane] : 0.0f);
+        const float4 mine = lane < kClipWarps ? sh[lane] : make_float4(0.0f, 0.0f, 0.0f, 0.0f);
+        Exact mid;
+        mid.add(mine.x, mine.y);
+        mid.over_warp();
+        float big = warp_sum(mine.z), small = warp_sum(mine.w);
         if (gridDim.x > 1) {
             // Every CTA takes all CTAs' notes of this turn (of the norm alone: the first one).
-            if (lane == 0) {
-                put_note(a.notes + 2 * blockIdx.x, __double_as_longlong(mid), turn);
-                put_note(a.notes + 2 * blockIdx.x + 1, __float_as_uint((float)big) | (uint64_t)__float_as_uint((float)small) << 32, turn);
-            }
+            Note* own = a.notes + blockIdx.x;
+            if (lane == 0) put_note(own, mid.hi, mid.lo, turn);
+            if (lane == 1) put_note(own + gridDim.x, big, small, turn);
             if (a.limit == 0.0f && blockIdx.x != 0) return;
-            const uint64_t t0 = global_ns();
-            double all = 0.0;
-            float all_big = 0.0f, all_small = 0.0f;
+            uint64_t t0 = 0;
             bool in_time = true;
-            for (int i0 = lane; i0 < gridDim.x && in_time; i0 += 32 * kClipNotes) {
-                Note m[kClipNotes], o[kClipNotes];
-                for (uint32_t k = 1;; ++k) {
-                    bool here = true;
-#pragma unroll
-                    for (int j = 0; j < kClipNotes; ++j) {
-                        const int i = min(i0 + 32 * j, (int)gridDim.x - 1);
-                        m[j] = get_note(a.notes + 2 * i);
-                        o[j] = get_note(a.notes + 2 * i + 1);
-                    }
-#pragma unroll
-                    for (int j = 0; j < kClipNotes; ++j) here = here && m[j].turn == turn && o[j].turn == turn;
-                    if (here) break;
-                    if ((k & 63) == 0 && global_ns() - t0 > kWaitNs) {
-                        in_time = false;
-                        break;
-                    }
-                }
-#pragma unroll
-                for (int j = 0; j < kClipNotes; ++j) {
-                    if (i0 + 32 * j >= gridDim.x) continue;
-                    all += __longlong_as_double(m[j].bits);
-                    all_big += __uint_as_float((uint32_t)o[j].bits);
-                    all_small += __uint_as_float((uint32_t)(o[j].bits >> 32));
-                }
+            mid = Exact();
+            take_notes(a.notes, turn, lane, t0, in_time, [&](const Note& n) { mid.add(n.a, n.b); });
+            mid.over_warp();
+            if (!in_range(mid.hi)) {
+                big = small = 0.0f;
+                take_notes(a.notes + gridDim.x, turn, lane, t0, in_time, [&](const Note& n) { big += n.a, small += n.b; });
+                big = warp_sum(big), small = warp_sum(small);
             }
             if (!__all_sync(0xffffffffu, in_time) && lane == 0) {
                 atomicOr(a.status, ST_TIMEOUT);
                 ok = 0;
             }
-            mid = warp_sum(all);
-            if (!(mid <= 1e38 && mid >= 0x1p-60)) big = warp_sum((double)all_big), small = warp_sum((double)all_small);
         }
         if (lane == 0) {
-            double norm;
-            if (mid <= 1e38 && mid >= 0x1p-60) {
-                // the 32-bit root and one of Newton's steps (a double's root and quotients take a microsecond here)
-                const float y = sqrtf((float)mid);
-                norm = (double)y + (double)((float)(mid - (double)y * y) * (0.5f / y));
-            } else if (mid < 0x1p-60) {
-                norm = sqrt(small) * 0x1p-90;
+            // root + rest of the sum in the range that holds it, and the norm over that: 1 / unit
+            float root, rest = 0.0f, unit = 1.0f;
+            if (in_range(mid.hi)) {
+                root = sqrtf(mid.hi);
+                rest = (fmaf(-root, root, mid.hi) + mid.lo) * (0.5f / root);
+            } else if (mid.hi < kLeastMid) {
+                root = sqrtf(small);
+                unit = 0x1p90f;
             } else {
-                norm = sqrt(big) * 0x1p80;
+                root = sqrtf(big);
+                unit = 0x1p-80f;
             }
+            const float norm = root + rest;
             if (blockIdx.x == 0) {
-                *a.norm = (float)norm;
+                *a.norm = norm / unit;
                 *a.turn = turn;              // every CTA has read it: its notes are there
             }
             float f = 1.0f;
-            if (norm > (double)a.limit && norm <= 1e300) {
-                f = a.limit / (float)norm;
-                if (norm < 1e38 && norm > 1e-30) f += (float)((double)a.limit - (double)f * norm) / (float)norm;
-                else f = (float)((double)a.limit / norm);
+            if (norm > a.limit * unit && norm <= 3e38f) {
+                f = a.limit / norm;
+                f += (fmaf(-f, root, a.limit) - f * rest) / norm;
+                f *= unit;
             }
             factor = f;
         }
@@ -425,7 +456,7 @@ struct nitro_clip {
     double bytes = 0.0;
     Piece* pieces = nullptr;
     Work* work = nullptr;
-    Note* notes = nullptr;           // [CTAs][2], and the turn
+    Note* notes = nullptr;           // [2][CTAs], and the turn
     bool clean = false;              // the notes, see clear_once
     StatusWord status;
     DeviceAllocs allocs;
