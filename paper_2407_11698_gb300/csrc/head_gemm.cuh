@@ -53,6 +53,7 @@ struct HgArgs {
     int upper;                 // symmetric D: only tiles that reach the diagonal or lie right of it
     int band;                  // row tiles that are walked together
     int fold;                  // K in two halves, an accumulator each (Epi::kFold only)
+    int stage;                 // bytes that a CTA's stage gets
     uint32_t* status;
 };
 
@@ -350,7 +351,7 @@ __global__ void __launch_bounds__(kHgThreads, 1)
                     if (!mbar_wait(empty_bar(st), ph, abort_flag, g.status)) goto producer_out;
                     const uint32_t a_dst = s0 + st * C::STAGE, b_dst = a_dst + HA * C::A_BYTES;
                     uint32_t fb = full_bar(st);
-                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * C::STAGE);
+                    if (CG == 1 || rank == 0) mbar_expect_tx(fb, CG * g.stage);
                     if constexpr (CG == 2) fb = remote_smem(fb, 0);
 #pragma unroll
                     for (int h = 0; h < HA; ++h) {
@@ -602,6 +603,9 @@ struct HgProblem {
     int64_t M, N, K;
     int batch = 1, planes_a = 1, planes_b = 1;
     bool upper = false, fold = false;
+    // few rows of A: a tile's stage gets these (a multiple of 8) and no rows past them, whose sums nobody takes.  128: all
+    int rows_a = 128;
+    int eights = 0;            // clusters of eight that run at once, where the caller has asked (hg_eights())
     uint32_t* status = nullptr;
     int prof = 0;
     double ops = 0, bytes = 0;
@@ -642,7 +646,7 @@ inline HgPick hg_pick(const HgProblem& p, int ha = 1, int hb = 1, int max_splits
     const int64_t kb = (p.K + kHgBK - 1) / kHgBK;
     for (const auto& f : kForms) {
         const int64_t tiles = hg_tiles(p, f.cg, f.bn), units = sms / f.cg;
-        const int64_t mma = 2 * f.bn * (ha + hb - 1), load = (ha * 16384 + hb * (f.bn / f.cg) * 128) / 53 + 30;
+        const int64_t mma = 2 * f.bn * (ha + hb - 1), load = (ha * (f.cg == 1 ? p.rows_a : 128) * 128 + hb * (f.bn / f.cg) * 128) / 53 + 30;
         const int64_t clocks = std::max(mma, load);
         const auto cost = [&](int s) {
             // and a tile's way through TMEM, most of it beside the next tile's MMAs; a pair's barriers
@@ -657,7 +661,7 @@ inline HgPick hg_pick(const HgProblem& p, int ha = 1, int hb = 1, int max_splits
         for (int s = 1; s <= max_splits && s <= kb; ++s)
             if (hg_splits(p.K, s) == s)
                 take(cost(s) + (s > 1 ? 4000 + (int64_t)s * p.M * p.N * p.batch * 8 / 3500 : 0), {f.cg, f.bn, s});
-        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 8 && (s < 8 || 8 * tiles <= sms / 8 * 7); s *= 2)
+        for (int s = 2; f.cg == 1 && f.bn == 128 && s <= 8 && (s < 8 || (p.eights ? tiles <= p.eights : 8 * tiles <= sms / 8 * 7)); s *= 2)
             if (hg_splits(p.K, s) == s) take(cost(s) + 6000 + (s == 8 ? 1000 : 0), {1, 128, 1, s});
     }
     return best;
@@ -669,7 +673,8 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     using C = HgCfg<CG, BN, HA, HB>;
     CUtensorMap ma, mb;
     static_assert(!hg_pairs<Epi> || (!BMN && HB == 1), "pairs of planes go along K");
-    if (!hg_map(&ma, a, F16, AMN ? 64 : 128)) return cudaErrorInvalidValue;
+    const int rows_a = CG == 1 && !AMN && p.M <= p.rows_a ? p.rows_a : 128;
+    if (!hg_map(&ma, a, F16, AMN ? 64 : rows_a)) return cudaErrorInvalidValue;
     if (!(hg_pairs<Epi> ? hg_map(&mb, b, F16, 16, 2) : hg_map(&mb, b, F16, BMN ? 64 : C::B_ROWS))) return cudaErrorInvalidValue;
     HgArgs g{};
     g.M = (int)p.M;
@@ -688,6 +693,7 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     // row tiles whose A stays in L2 while B goes past them once: 40 MB (8192 x 64000 x 2048 in
     // bands of 2048 rows read B, 262 MB, four times: a step 5.55 ms, with these 5.48, under the power limit)
     g.band = (int)std::min<int64_t>(64, std::max<int64_t>(4, ((int64_t)40 << 20) / ((int64_t)128 * CG * HA * 2 * p.K)));
+    g.stage = HA * rows_a * 128 + HB * C::B_BYTES;
     g.status = p.status;
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
@@ -702,6 +708,35 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     if constexpr (KS > 1) return launch_cluster(kernel, dim3(g.total), kHgThreads, KS, s, C::SMEM, ma, mb, g, ea);
     else if constexpr (CG == 2) return launch_cluster(kernel, dim3(grid), kHgThreads, 2, s, C::SMEM, ma, mb, g, ea);
     else return launch_k(kernel, dim3(grid), dim3(kHgThreads), C::SMEM, s, ma, mb, g, ea);
+}
+
+// Clusters of eight CTAs, one an SM, that the device runs at once: as many as its parts hold whole ones (152 SMs
+// do not hold 16 of them: 64 x 2048 x 1024 took 16.6 us with 16 and 7.4 in clusters of four).  0: unknown.
+template <class Epi, bool AMN, bool BMN, bool F16>
+int hg_eights() {
+    static std::atomic<int> known{-1};
+    int n = known.load(std::memory_order_relaxed);
+    if (n >= 0) return n;
+    using C = HgCfg<1, 128, 1, 1>;
+    const auto kernel = k_head_gemm<Epi, 1, 128, AMN, BMN, F16, 1, 1, 8>;
+    cudaLaunchAttribute attr[1];
+    attr[0].id = cudaLaunchAttributeClusterDimension;
+    attr[0].val.clusterDim.x = 8;
+    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
+    cudaLaunchConfig_t cfg = {};
+    cfg.gridDim = dim3(8);
+    cfg.blockDim = dim3(kHgThreads);
+    cfg.dynamicSmemBytes = C::SMEM;
+    cfg.attrs = attr;
+    cfg.numAttrs = 1;
+    n = 0;
+    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
+        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
+        cudaGetLastError();
+        n = 0;
+    }
+    known.store(n, std::memory_order_relaxed);
+    return n;
 }
 
 // D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K; HA, HB:

@@ -164,67 +164,80 @@ __global__ void __launch_bounds__(256, 2) k_glu_few(const T* x, const uint16_t* 
 
 // ------------------------------------------------------------------ elementwise
 // Rows as bf16 with a stride of ldp (a multiple of 8): int8 activations are exact in bf16.
+struct PackJob {
+    const void* x;
+    int64_t ldx, rows, ldp;
+    uint16_t* out;
+    int cols, i8;
+    int ctas;              // 0: nothing to do
+};
 template <typename T>
-__global__ void __launch_bounds__(256) k_glu_pack(const T* x, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp) {
-    pdl_wait();
-    const int per = (int)(ldp / 8);
-    const int64_t words = rows * per, step = (int64_t)gridDim.x * 256, first = blockIdx.x * (int64_t)256 + threadIdx.x;
-    const bool vec = (((uintptr_t)x | (uintptr_t)(ldx * sizeof(T))) & (8 * sizeof(T) - 1)) == 0;
+__device__ __forceinline__ void pack_rows(const PackJob& j, int cta) {
+    const T* x = static_cast<const T*>(j.x);
+    const int per = (int)(j.ldp / 8);
+    const int64_t words = j.rows * per, step = (int64_t)j.ctas * 256, first = cta * (int64_t)256 + threadIdx.x;
+    const bool vec = (((uintptr_t)x | (uintptr_t)(j.ldx * sizeof(T))) & (8 * sizeof(T) - 1)) == 0;
     RowWalk at(first, step, per);
     for (int64_t i = first; i < words; i += step, at.next()) {
         const int c = at.part * 8;
-        const T* src = x + at.row * ldx + c;
+        const T* src = x + at.row * j.ldx + c;
         uint32_t w[4] = {0, 0, 0, 0};
         if constexpr (sizeof(T) == 2) {
-            if (vec && c + 8 <= cols) {
+            if (vec && c + 8 <= j.cols) {
                 *reinterpret_cast<uint4*>(w) = *reinterpret_cast<const uint4*>(src);
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < cols) w[j >> 1] |= (uint32_t)src[j] << (16 * (j & 1));
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < j.cols) w[k >> 1] |= (uint32_t)src[k] << (16 * (k & 1));
             }
         } else {
             uint32_t b[2] = {0x80808080u, 0x80808080u};   // bytes hold x + 128
-            if (vec && c + 8 <= cols) {
+            if (vec && c + 8 <= j.cols) {
                 const uint2 r = *reinterpret_cast<const uint2*>(src);
                 b[0] ^= r.x;
                 b[1] ^= r.y;
             } else {
 #pragma unroll
-                for (int j = 0; j < 8; ++j)
-                    if (c + j < cols) b[j >> 2] ^= (uint32_t)(uint8_t)src[j] << (8 * (j & 3));
+                for (int k = 0; k < 8; ++k)
+                    if (c + k < j.cols) b[k >> 2] ^= (uint32_t)(uint8_t)src[k] << (8 * (k & 3));
             }
 #pragma unroll
-            for (int j = 0; j < 4; ++j) w[j] = bf16x2(b[j >> 1], 2 * (j & 1));
+            for (int k = 0; k < 4; ++k) w[k] = bf16x2(b[k >> 1], 2 * (k & 1));
         }
-        reinterpret_cast<uint4*>(out)[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        reinterpret_cast<uint4*>(j.out)[i] = make_uint4(w[0], w[1], w[2], w[3]);
     }
 }
 
 // D [rows][ldd] from saved and dout, and what its rounding left over `low` elements on (0: not kept): four units a
-// thread where rows are aligned (VEC), else one.
+// thread where rows are aligned (vec), else one.
+struct GradJob {
+    const float* saved;
+    const uint16_t* dout;
+    int64_t lddout, rows, ldd, low;
+    uint16_t* D;
+    int hidden, act, vec;
+    int ctas;
+};
 template <bool VEC>
-__global__ void __launch_bounds__(256) k_glu_grad(const float* saved, const uint16_t* dout, int64_t lddout, int64_t rows, int hidden,
-                                                  int act, uint16_t* D, int64_t ldd, int64_t low) {
-    pdl_wait();
+__device__ __forceinline__ void grad_rows(const GradJob& job, int cta) {
     constexpr int E = VEC ? 4 : 1;
-    const int per = hidden / E;
-    const int64_t items = rows * per, step = (int64_t)gridDim.x * 256, first = blockIdx.x * (int64_t)256 + threadIdx.x;
+    const int hidden = job.hidden, per = hidden / E;
+    const int64_t items = job.rows * per, step = (int64_t)job.ctas * 256, first = cta * (int64_t)256 + threadIdx.x;
     RowWalk at(first, step, per);
     for (int64_t i = first; i < items; i += step, at.next()) {
         const int c = at.part * E;
-        const float* z = saved + at.row * 2 * hidden + c;
+        const float* z = job.saved + at.row * 2 * hidden + c;
         float a[E], b[E], g[E], da[E], db[E];
         if constexpr (VEC) {
             *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(z);
             *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(z + hidden);
-            const uint2 u = *reinterpret_cast<const uint2*>(dout + at.row * lddout + c);
+            const uint2 u = *reinterpret_cast<const uint2*>(job.dout + at.row * job.lddout + c);
             g[0] = __uint_as_float(u.x << 16), g[1] = __uint_as_float(u.x & 0xffff0000u);
             g[2] = __uint_as_float(u.y << 16), g[3] = __uint_as_float(u.y & 0xffff0000u);
         } else {
-            a[0] = z[0], b[0] = z[hidden], g[0] = __uint_as_float((uint32_t)dout[at.row * lddout + c] << 16);
+            a[0] = z[0], b[0] = z[hidden], g[0] = __uint_as_float((uint32_t)job.dout[at.row * job.lddout + c] << 16);
         }
-        with_act(act, [&](auto k) {
+        with_act(job.act, [&](auto k) {
 #pragma unroll
             for (int j = 0; j < E; j += 2) {
                 float2 v;
@@ -237,7 +250,7 @@ __global__ void __launch_bounds__(256) k_glu_grad(const float* saved, const uint
                 }
             }
         });
-        uint16_t* dst = D + at.row * ldd + c;
+        uint16_t* dst = job.D + at.row * job.ldd + c;
         for (int half = 0;; ++half) {
             uint16_t ha[E], hb[E];
 #pragma unroll
@@ -252,15 +265,31 @@ __global__ void __launch_bounds__(256) k_glu_grad(const float* saved, const uint
                 dst[0] = ha[0];
                 dst[hidden] = hb[0];
             }
-            if (low == 0 || half == 1) break;
+            if (job.low == 0 || half == 1) break;
 #pragma unroll
             for (int j = 0; j < E; ++j) {
                 da[j] -= __uint_as_float((uint32_t)ha[j] << 16);
                 db[j] -= __uint_as_float((uint32_t)hb[j] << 16);
             }
-            dst += low;
+            dst += job.low;
         }
     }
+}
+
+// All that goes before the products, each job on CTAs of its own: a launch costs as much as a small job.
+__global__ void __launch_bounds__(256) k_glu_prep(const PackJob x, const PackJob w, const GradJob g) {
+    pdl_wait();
+    int cta = blockIdx.x;
+    if (cta < g.ctas) {
+        if (g.vec) grad_rows<true>(g, cta);
+        else grad_rows<false>(g, cta);
+        return;
+    }
+    cta -= g.ctas;
+    const PackJob& j = cta < x.ctas ? x : w;
+    if (cta >= x.ctas) cta -= x.ctas;
+    if (j.i8) pack_rows<int8_t>(j, cta);
+    else pack_rows<uint16_t>(j, cta);
 }
 
 // Up to this many rows D is kept as two bf16 halves: the rounding of one entry, up to 2^-8 of
@@ -289,32 +318,39 @@ namespace {
 
 bool copies(const void* x, int type, int64_t ldx) { return type == NITRO_I8 || !tma_rows(x, ldx); }
 
-cudaError_t pack(const void* x, int type, int64_t ldx, int64_t rows, int cols, uint16_t* out, int64_t ldp, cudaStream_t s) {
-    static std::atomic<int> resident[2];
-    const int64_t words = rows * (ldp / 8);
-    const bool i8 = type == NITRO_I8;
-    const int grid = i8 ? one_wave(k_glu_pack<int8_t>, resident[0], words) : one_wave(k_glu_pack<uint16_t>, resident[1], words);
-    ProfScope ps(K_GLU_PACK, s, 0.0, (double)rows * cols * (i8 ? 3 : 4));
-    return i8 ? launch_k(k_glu_pack<int8_t>, dim3(grid), dim3(256), 0, s, (const int8_t*)x, ldx, rows, cols, out, ldp)
-              : launch_k(k_glu_pack<uint16_t>, dim3(grid), dim3(256), 0, s, (const uint16_t*)x, ldx, rows, cols, out, ldp);
-}
-
-// x and W as operands along K; copies where TMA cannot take their rows.
-cudaError_t operands(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
-                     cudaStream_t s, HgOperand* ox, HgOperand* ow) {
-    cudaError_t e = cudaSuccess;
+// x and W as operands along K, copies where TMA cannot take their rows, and D's job, if there is one (g.rows > 0).
+cudaError_t prepare(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows, GradJob g,
+                    cudaStream_t s, HgOperand* ox, HgOperand* ow) {
+    PackJob jx{}, jw{};
+    double bytes = 14.0 * g.rows * g.hidden;
     *ox = {x, h->features, rows, ldx, 1, 0};
     if (copies(x, x_type, ldx)) {
-        e = pack(x, x_type, ldx, rows, h->features, h->xp, h->ldp, s);
+        jx = {x, ldx, rows, h->ldp, h->xp, h->features, x_type == NITRO_I8, 1};
         *ox = {h->xp, h->features, rows, h->ldp, 1, 0};
+        bytes += (double)rows * h->features * (jx.i8 ? 3 : 4);
     }
-    *ow = {w, h->features, 2 * (int64_t)h->hidden, ldw, 1, 0};
-    if (e == cudaSuccess && copies(w, NITRO_BF16, ldw)) {
-        e = pack(w, NITRO_BF16, ldw, 2 * (int64_t)h->hidden, h->features, h->wp, h->ldp, s);
-        *ow = {h->wp, h->features, 2 * (int64_t)h->hidden, h->ldp, 1, 0};
+    const int64_t rows_w = 2 * (int64_t)h->hidden;
+    *ow = {w, h->features, rows_w, ldw, 1, 0};
+    if (copies(w, NITRO_BF16, ldw)) {
+        jw = {w, ldw, rows_w, h->ldp, h->wp, h->features, 0, 1};
+        *ow = {h->wp, h->features, rows_w, h->ldp, 1, 0};
+        bytes += 4.0 * rows_w * h->features;
     }
-    return e;
+    const int64_t items[3] = {g.rows * (g.hidden / (g.vec ? 4 : 1)), jx.ctas ? rows * (h->ldp / 8) : 0, jw.ctas ? rows_w * (h->ldp / 8) : 0};
+    const int64_t all = items[0] + items[1] + items[2];
+    if (all == 0) return cudaSuccess;
+    // one wave of CTAs, shared out by their threads' work
+    static std::atomic<int> resident{0};
+    const int64_t wave = one_wave(k_glu_prep, resident, INT32_MAX);
+    const auto share = [&](int64_t n) { return n ? (int)std::max<int64_t>(1, std::min<int64_t>((n + 255) / 256, wave * n / all)) : 0; };
+    g.ctas = share(items[0]);
+    jx.ctas = share(items[1]);
+    jw.ctas = share(items[2]);
+    ProfScope ps(K_GLU_PREP, s, 0.0, bytes);
+    return launch_k(k_glu_prep, dim3(g.ctas + jx.ctas + jw.ctas), dim3(256), 0, s, jx, jw, g);
 }
+
+int rows_in_stage(int rows) { return rows < 128 ? (rows + 7) / 8 * 8 : 128; }
 
 bool glu_args(const nitro_glu* h, const void* x, int x_type, int64_t ldx, const void* w, int64_t ldw, int rows, float scale,
               int act) {
@@ -386,13 +422,15 @@ nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t 
         return NITRO_OK;
     }
     HgOperand ox, ow;
-    TRY(operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow));
+    TRY(prepare(h, x, x_type, ldx, w, ldw, rows, GradJob{}, s, &ox, &ow));
     ow = {ow.base, ow.inner, h->hidden, ow.ld, 2, h->hidden * ow.ld};
     HgProblem p{rows, 2 * round_up(h->hidden, 16), h->features};
     p.status = h->status.at;
     p.prof = K_GLU_FWD;
     p.ops = 4.0 * rows * h->hidden * h->features;
     p.fold = h->features > kFoldFeatures;
+    p.rows_a = rows_in_stage(rows);
+    p.eights = hg_eights<EpiGlu, false, false, false>();
     const EpiGlu::Args ea{out, ldo, saved, tma_rows(out, ldo), ((uintptr_t)saved & 15) == 0 && h->hidden % 4 == 0, h->hidden, act, scale};
     TRY((hg_launch<EpiGlu, false, false, false>(hg_pick(p), p, ox, ow, ea, s)));
     return NITRO_OK;
@@ -421,21 +459,10 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
     if (!dx && !dw) return NITRO_OK;
     const int halves = rows <= kRowsWithLow ? 2 : 1;
     const int64_t plane = rows * h->ldd;
-    {
-        static std::atomic<int> resident[2];
-        const bool vec = h->hidden % 4 == 0 && ((uintptr_t)saved & 15) == 0 && ((uintptr_t)dout & 7) == 0 && lddout % 4 == 0;
-        const int64_t items = rows * (int64_t)(h->hidden / (vec ? 4 : 1));
-        ProfScope ps(K_GLU_GRAD, s, 0.0, 14.0 * rows * h->hidden);
-        const int64_t low = halves == 2 ? plane : 0;
-        if (vec)
-            TRY(launch_k(k_glu_grad<true>, dim3(one_wave(k_glu_grad<true>, resident[0], items)), dim3(256), 0, s, saved, dout, lddout,
-                         (int64_t)rows, h->hidden, act, h->D, h->ldd, low));
-        else
-            TRY(launch_k(k_glu_grad<false>, dim3(one_wave(k_glu_grad<false>, resident[1], items)), dim3(256), 0, s, saved, dout, lddout,
-                         (int64_t)rows, h->hidden, act, h->D, h->ldd, low));
-    }
+    const bool vec = h->hidden % 4 == 0 && ((uintptr_t)saved & 15) == 0 && ((uintptr_t)dout & 7) == 0 && lddout % 4 == 0;
+    const GradJob g{saved, dout, lddout, rows, h->ldd, halves == 2 ? plane : 0, h->D, h->hidden, act, vec, 0};
     HgOperand ox, ow;
-    TRY(operands(h, x, x_type, ldx, w, ldw, rows, s, &ox, &ow));
+    TRY(prepare(h, x, x_type, ldx, w, ldw, rows, g, s, &ox, &ow));
     const HgOperand D{h->D, H2, rows, h->ldd, halves, plane};
     if (dx) {
         HgProblem p{rows, F, H2};
@@ -443,6 +470,8 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
         p.status = h->status.at;
         p.prof = K_GLU_DX;
         p.ops = 4.0 * rows * h->hidden * F;
+        p.rows_a = rows_in_stage(rows);
+        p.eights = hg_eights<EpiBf16, false, true, false>();
         // in slices along the hidden units where its tiles leave SMs idle
         const int64_t ldc = round_up(F, 32);
         const HgPick t = hg_pick(p, halves, 1, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
@@ -466,6 +495,7 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
         p.status = h->status.at;
         p.prof = K_GLU_DW;
         p.ops = 4.0 * rows * h->hidden * F;
+        p.eights = hg_eights<EpiBf16, true, true, false>();
         const EpiBf16::Args eb{dw, lddw, tma_rows(dw, lddw), nullptr, 0, scale};
         if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p, 2), p, D, ox, eb, s)));
         else TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, D, ox, eb, s)));

@@ -47,7 +47,7 @@ const char* const kNames[K_COUNT] = {
     "xent_pack", "xent_logits", "xent_rows", "xent_dx", "xent_dw", "orth_pack", "orth_gram",
     "orth_square", "orth_update", "orth_small",
     "mx4_quantize", "mx4_dequantize", "mx4_linear",
-    "glu_pack", "glu_fwd", "glu_grad", "glu_dx", "glu_dw", "gnorm_fwd", "gnorm_bwd", "gnorm_params", "clip"};
+    "glu_fwd", "glu_prep", "glu_dx", "glu_dw", "gnorm_fwd", "gnorm_bwd", "gnorm_params", "clip"};
 
 }  // namespace
 

@@ -51,9 +51,8 @@ enum KernelId : int {
     K_MX4_QUANTIZE,
     K_MX4_DEQUANTIZE,
     K_MX4_LINEAR,
-    K_GLU_PACK,
     K_GLU_FWD,
-    K_GLU_GRAD,
+    K_GLU_PREP,
     K_GLU_DX,
     K_GLU_DW,
     K_GNORM_FWD,
