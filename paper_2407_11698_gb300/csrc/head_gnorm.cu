@@ -20,8 +20,8 @@ namespace {
 
 constexpr int kGnThreads = 256;
 constexpr int kGnBatch = 1024;                 // samples of a launch, at most
-constexpr int kGnCtas = 608;                   // CTAs of a launch of two passes, unless there are more samples (four an SM)
-constexpr int64_t kGnBatchBytes = (int64_t)64 << 20;
+constexpr int kGnCtas = 608;                   // CTAs of a launch of two passes, unless there are more samples: four an SM
+constexpr int64_t kGnBatchBytes = (int64_t)100 << 20;
 constexpr int kGnChannels = 8192;
 
 // V values of a row as fp32 pairs (of one value: itself and 0); rows are aligned to V values
@@ -211,6 +211,9 @@ struct Sums {
 };
 
 // ------------------------------------------------------------------ two passes
+// CTAs of a backward pass that an SM holds by their registers
+constexpr int gn_resident(int v) { return v == 8 ? 2 : 4; }
+
 // What is common to the four passes.
 struct GnShape {
     int pixels, channels, groups, per;   // per: channels of a group
@@ -365,7 +368,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
 // Sums over a chunk: of du and du h for each channel (part_c [sample][chunk][2][channels]), and over a sample's
 // groups of gamma du and gamma du h, divided by their count (means [sample][groups]).
 template <typename X, typename Y, int V>
-__global__ void __launch_bounds__(kGnThreads, 2) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
+__global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                            const GnShape s, const float* mean, const float* rstd, float* part_c,
                                                            float2* parts, uint32_t* ticket, float2* means) {
     __shared__ float red[2][kGnThreads * V];
@@ -449,7 +452,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_sums(const X* x, int64_t l
 }
 
 template <typename X, typename Y, int V>
-__global__ void __launch_bounds__(kGnThreads, 2) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
+__global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                          const GnShape s, const float* mean, const float* rstd, const float2* means,
                                                          Y* dx, int64_t lddx, int64_t sdx) {
     pdl_wait();
@@ -928,7 +931,8 @@ struct Map {
     }
 };
 
-GnShape shape(const nitro_gnorm* h, int pixels, int samples, int v, int act, const float* gamma, const float* beta) {
+// resident: CTAs an SM holds
+GnShape shape(const nitro_gnorm* h, int pixels, int samples, int v, int resident, int act, const float* gamma, const float* beta) {
     GnShape s{};
     s.pixels = pixels;
     s.channels = h->channels;
@@ -938,8 +942,9 @@ GnShape shape(const nitro_gnorm* h, int pixels, int samples, int v, int act, con
     s.slabs = (vecs + kGnThreads - 1) / kGnThreads;
     s.vecs = (vecs + s.slabs - 1) / s.slabs;
     s.rows = kGnThreads / s.vecs;
-    // four CTAs an SM in all, of eight steps at least
-    const int want = std::max(1, std::min(kGnCtas / samples, (pixels + 8 * s.rows - 1) / (8 * s.rows)));
+    // one wave of CTAs in all, of eight steps at least
+    const int wave = std::min(kGnCtas, resident * sm_count());
+    const int want = std::max(1, std::min(wave / samples, (pixels + 8 * s.rows - 1) / (8 * s.rows)));
     s.chunk = (pixels + want - 1) / want;
     s.chunks = (pixels + s.chunk - 1) / s.chunk;
     s.act = act;
@@ -987,7 +992,7 @@ const T* sample_at(const Map& m, int64_t i) {
     return static_cast<const T*>(m.p) + i * m.stride;
 }
 
-// samples of a batch: what two passes touch stays in L2
+// samples of a batch: what both passes read stays in L2 in between
 int batch_size(const nitro_gnorm* h, int pixels, int bytes_a_value) {
     const int64_t n = kGnBatchBytes / ((int64_t)pixels * h->channels * bytes_a_value);
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, h->batch));
@@ -1120,10 +1125,10 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
         }));
         return NITRO_OK;
     }
-    const int batch = batch_size(h, pixels, type_size(x_type) + type_size(y_type));
+    const int batch = batch_size(h, pixels, type_size(x_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
-        const GnShape sh = shape(h, pixels, n, v, act, gamma, beta);
+        const GnShape sh = shape(h, pixels, n, v, 4, act, gamma, beta);
         float* m = mean ? mean + (int64_t)s0 * h->groups : h->mean;
         float* r = rstd ? rstd + (int64_t)s0 * h->groups : h->rstd;
         const double values = (double)n * pixels * C;
@@ -1211,10 +1216,10 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
         }
         return NITRO_OK;
     }
-    const int batch = batch_size(h, pixels, type_size(x_type) + (dx ? 2 : 1) * type_size(y_type));
+    const int batch = batch_size(h, pixels, type_size(x_type) + type_size(y_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
-        const GnShape sh = shape(h, pixels, n, v, act, gamma, beta);
+        const GnShape sh = shape(h, pixels, n, v, gn_resident(v), act, gamma, beta);
         const float *m = mean + (int64_t)s0 * h->groups, *r = rstd + (int64_t)s0 * h->groups;
         const double values = (double)n * pixels * C;
         const dim3 grid(sh.chunks, n), block((sh.rows * sh.vecs + 31) / 32 * 32);

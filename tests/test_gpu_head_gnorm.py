@@ -175,10 +175,11 @@ def test_forward_without_statistics():
     h.close()
 
 
-def test_in_place():
-    x, dy, gamma, beta = inputs(3, 80, 64, seed=9)
+@pytest.mark.parametrize("p", [80, 30000])
+def test_in_place(p):
+    x, dy, gamma, beta = inputs(3, p, 64, seed=9)
     want = run(x, dy, gamma, beta, 8, 1e-5, "gelu")
-    h = nb.GroupNorm(3, 80, 64, 8)
+    h = nb.GroupNorm(3, p, 64, 8)
     a, b = x.clone(), dy.clone()
     mean, rstd = torch.empty(3, 8, device="cuda"), torch.empty(3, 8, device="cuda")
     h.backward(x, gamma, beta, want[1], want[2], b, b, act=nb.NITRO_ACT_GELU)
@@ -225,12 +226,17 @@ def test_empty_batch_and_a_smaller_one():
     h.close()
 
 
-# more than a launch's samples, more than the batches that L2 holds
-@pytest.mark.parametrize("n, p, c, groups, x", [(1500, 6, 16, 4, "i8"), (20, 5000, 128, 8, "bf16"), (3, 70001, 100, 5, "bf16")])
-def test_batches(n, p, c, groups, x):
-    t = inputs(n, p, c, x, seed=21)
-    out = run(*t, groups, 1e-5, "silu")
+# more than a launch's samples; slabs that no cluster holds, of one sample and of so many that CTAs take several; groups
+# of more channels than a warp's lanes take, and than a CTA's; the same without vectors; sums of more CTAs than are kept
+@pytest.mark.parametrize("n, p, c, groups, x, pad", [
+    (2500, 6, 16, 4, "i8", 0), (20, 5000, 128, 8, "bf16", 0), (3, 70001, 100, 5, "bf16", 0), (1, 70001, 33, 3, "bf16", 0), (40, 15000, 16, 1, "f32", 0),
+    (90, 15000, 16, 2, "i8", 0), (2, 900, 1024, 1, "bf16", 0), (1, 900, 2048, 2, "i8", 0), (1, 250, 4096, 1, "bf16", 0), (1, 900, 600, 2, "bf16", 3),
+    (2, 9000, 64, 1, "bf16", 3), (1, 40000, 1000, 250, "bf16", 0), (9, 50000, 8, 8, "f32", 0)])
+def test_batches(n, p, c, groups, x, pad):
+    t = inputs(n, p, c, x, "f32" if x == "f32" else "bf16", pad=pad, seed=21)
+    out = run(*t, groups, 1e-5, "silu", pad=pad)
     check(*t, groups, 1e-5, "silu", *out)
+    assert all(torch.equal(a, b) for a, b in zip(out, run(*t, groups, 1e-5, "silu", pad=pad)))
 
 
 def test_gradients_against_differences():
@@ -250,10 +256,11 @@ def test_gradients_against_differences():
         assert abs((v[0] - v[1]) / (2 * step) - grad[pos].item()) < 2e-7 * 0.5 / step + step ** 2 * 0.1
 
 
-def test_captured_and_replayed_on_another_stream():
-    x, dy, gamma, beta = inputs(2, 3000, 64, seed=5)
+@pytest.mark.parametrize("p", [3000, 40000])
+def test_captured_and_replayed_on_another_stream(p):
+    x, dy, gamma, beta = inputs(2, p, 64, seed=5)
     want = run(x, dy, gamma, beta, 8, 1e-5, "silu")
-    h = nb.GroupNorm(2, 3000, 64, 8)
+    h = nb.GroupNorm(2, p, 64, 8)
     y, dx = torch.empty_like(dy), torch.empty_like(dy)
     mean, rstd = torch.empty(2, 8, device="cuda"), torch.empty(2, 8, device="cuda")
     dg, db = torch.empty(64, device="cuda"), torch.empty(64, device="cuda")
