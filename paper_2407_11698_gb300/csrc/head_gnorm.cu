@@ -558,10 +558,12 @@ __device__ __forceinline__ void copies_landed(int stage) {
     else asm volatile("cp.async.wait_group 0;" ::: "memory");
 }
 
-__device__ __forceinline__ float ld_remote(const float* p, uint32_t rank) {
-    float v;
-    asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v) : "r"(remote_smem(smem_u32(p), rank)) : "memory");
-    return v;
+// p of the cluster's `ks` CTAs, all loads under way together
+__device__ __forceinline__ void ld_remote(const float* p, int ks, float* v) {
+    const uint32_t at = smem_u32(p);
+#pragma unroll
+    for (int r = 0; r < 8; ++r)
+        if (r < ks) asm volatile("ld.shared::cluster.f32 %0, [%1];" : "=f"(v[r]) : "r"(remote_smem(at, r)) : "memory");
 }
 // (nothing is handed over: peers learn that their shared memory has been read)
 __device__ __forceinline__ void cluster_arrive() { asm volatile("barrier.cluster.arrive.relaxed;" ::: "memory"); }
@@ -698,8 +700,15 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     for (int g = threadIdx.x; g < gs; g += kGnThreads) {
         Moments a;
         if (s.ks == 1) a.n = group[g], a.m = group[gs + g], a.q = group[2 * gs + g];
-        else
-            for (int r = 0; r < s.ks; ++r) a.add(ld_remote(group + g, r), ld_remote(group + gs + g, r), ld_remote(group + 2 * gs + g, r));
+        else {
+            float rn[8], rm[8], rq[8];
+            ld_remote(group + g, s.ks, rn);
+            ld_remote(group + gs + g, s.ks, rm);
+            ld_remote(group + 2 * gs + g, s.ks, rq);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < s.ks) a.add(rn[r], rm[r], rq[r]);
+        }
         const float mu = stat[g] + a.m, rs = 1.0f / sqrtf(a.q / a.n + eps);
         stat[g] = mu;
         stat[gs + g] = rs;
@@ -746,6 +755,7 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
     float* warp_s = reinterpret_cast<float*>(grads + s.steps * SD::STEP);      // [2][warps][width]
     float* chan = warp_s + 2 * kGnWarps * s.width;                             // [2][width]
     float* means = chan + 2 * s.width;                                         // [2][groups]
+    float* gamma = means + 2 * gs;                                             // [width]
     pdl_wait();
     const GnPart at(s, V);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
@@ -765,6 +775,8 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
             copies_group();
         }
     }
+    const int c0 = at.g0 * s.per;
+    for (int i = threadIdx.x; i < s.width; i += kGnThreads) gamma[i] = s.gamma ? s.gamma[c0 + i] : 1.0f;
     GnChannels<V> ch;
     float2 a[N], b[N];
 #pragma unroll
@@ -820,15 +832,17 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
         cluster_barrier();
         // all ranks' sums, in their order, to where the warps' were
         for (int i = threadIdx.x; i < 2 * s.width; i += kGnThreads) {
-            float v = 0.0f;
-            for (int r = 0; r < s.ks; ++r) v += ld_remote(chan + i, r);
+            float v = 0.0f, o[8];
+            ld_remote(chan + i, s.ks, o);
+#pragma unroll
+            for (int r = 0; r < 8; ++r)
+                if (r < s.ks) v += o[r];
             warp_s[i] = v;
         }
         cluster_arrive();          // this CTA has read its peers' shared memory
     }
     __syncthreads();
     const float* total = s.ks > 1 ? warp_s : chan;
-    const int c0 = at.g0 * s.per;
     if (sums && at.rank == 0)
         for (int i = threadIdx.x; i < 2 * s.width; i += kGnThreads) {
             const int half = i >= s.width;
@@ -842,9 +856,8 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
             if (g < gs)
                 for (int i = threadIdx.x % 8; i < s.per; i += 8) {
                     const int c = g * s.per + i;
-                    const float k = s.gamma ? s.gamma[c0 + c] : 1.0f;
-                    u = fmaf(k, total[c], u);
-                    v = fmaf(k, total[s.width + c], v);
+                    u = fmaf(gamma[c], total[c], u);
+                    v = fmaf(gamma[c], total[s.width + c], v);
                 }
 #pragma unroll
             for (int d = 4; d > 0; d >>= 1) u += __shfl_xor_sync(0xffffffffu, u, d), v += __shfl_xor_sync(0xffffffffu, v, d);
@@ -1025,7 +1038,7 @@ GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size,
         const int rows = kGnThreads >> s.lane_log;
         s.chunk = (pixels + ks - 1) / ks;
         s.steps = (s.chunk + rows - 1) / rows;
-        const int64_t bytes = (int64_t)s.steps * kGnThreads * v * value_bytes + 32 + 4 * (2 * kGnWarps + 2) * (int64_t)s.width + 20 * m;
+        const int64_t bytes = (int64_t)s.steps * kGnThreads * v * value_bytes + 32 + 4 * (2 * kGnWarps + 3) * (int64_t)s.width + 20 * m;
         *smem = (int)bytes;
         return bytes <= budget;
     };
