@@ -499,7 +499,8 @@ void nitro_gnorm_destroy(nitro_gnorm* h);
  * [2 hidden x features], the gate's rows first; with a = z's first `hidden` columns and b the others
  * out = act(a) b, bf16 [rows x hidden].  The projection back is the caller's next matrix (of nitro_xent_*, say).
  *
- * forward: saved, fp32 [rows x 2 hidden] without gaps, gets z for a backward (NULL: not kept).
+ * forward: saved, 2 rows hidden fp32 values at a multiple of 16 bytes, gets z for a backward of as many rows, in an
+ * order of the library's own (NULL: not kept).
  * backward, from saved and the gradient dout (bf16): D = [dout b act'(a), dout act(a)], dx = scale D W and
  * dw = scale D^T x, bf16; either may be NULL.  D is rounded to bf16 (up to 32 rows: kept as two
  * bf16 halves).  Sums are in 32 bits, in an order that the sizes fix.  With rows = 0 dw is cleared.

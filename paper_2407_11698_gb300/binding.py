@@ -795,7 +795,7 @@ class GatedLinear(_Handle):
         return n, (xp, xt, ldx, wp, ldw, n, scale, act)
 
     def forward(self, x, w, out, saved=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
-        """Writes out (bf16 [rows x hidden]) and, for a backward, z to saved (fp32 [rows x 2 hidden])."""
+        """Writes out (bf16 [rows x hidden]) and, for a backward, z to saved (fp32 [rows x 2 hidden], in an order of the library's own)."""
         n, a = self._inputs(x, w, scale, act)
         op, _, ldo = _matrix(out, n, self.hidden, _W, "out")
         st = lib().nitro_glu_forward(self.h, *a, op, ldo,

@@ -238,7 +238,20 @@ __device__ __forceinline__ void hg_store16(const HgPart& p, const uint32_t* w, u
     if (!vec) {
         // (eight values a lane at the lines' places are eight stores to 32 sectors each: the gradient of 6008 x 2337 took 76 us, now 33)
         p.stage.put(v);
-        const int rows = min(32, p.rows - p.row0), c = col + p.stage.lane;
+        const int rows = min(32, p.rows - p.row0);
+        if ((((uintptr_t)base | (uintptr_t)(ld * 2) | (uintptr_t)(col * 2)) & 3) == 0) {      // two values a lane, two rows an instruction
+            const int j = 2 * (p.stage.lane & 15), c = col + j;
+            uint16_t* dst = base + (int64_t)(p.row0 + (p.stage.lane >> 4)) * ld + c;
+#pragma unroll 4
+            for (int r = p.stage.lane >> 4; r < rows; r += 2, dst += 2 * ld) {
+                const uint32_t w = p.stage.value<uint32_t>(r, j >> 1);
+                if (c + 2 <= cols) *reinterpret_cast<uint32_t*>(dst) = w;
+                else if (c < cols) *dst = (uint16_t)w;
+            }
+            __syncwarp();
+            return;
+        }
+        const int c = col + p.stage.lane;
         uint16_t* dst = base + (int64_t)p.row0 * ld + c;
 #pragma unroll 4
         for (int r = 0; r < rows; ++r, dst += ld)

@@ -17,14 +17,34 @@ using namespace nitro;
 namespace nitro {
 namespace {
 
+// Where saved has z: of whole blocks of 16 units a line of 128 bytes for each row, gates first, row after row and block after
+// block, so that lines are aligned whatever `hidden` is; then the units that are left, gates and ups of a row together.
+struct Saved {
+    float* base;
+    int64_t rows;
+    int hidden;
+    __device__ __forceinline__ int blocks() const { return hidden >> 4; }
+    __device__ __forceinline__ float* line(int block, int64_t row) const { return base + (block * rows + row) * 32; }
+    // z of a unit past the whole blocks, its gate; *up: from there to its up
+    __device__ __forceinline__ float* rest(int unit, int64_t row, int* up) const {
+        *up = hidden & 15;
+        return base + blocks() * rows * 32 + row * 2 * *up + (unit & 15);
+    }
+    __device__ __forceinline__ float* at(int unit, int64_t row, int* up) const {
+        if (unit >> 4 == blocks()) return rest(unit, row, up);
+        *up = 16;
+        return line(unit >> 4, row) + (unit & 15);
+    }
+};
+
 // out and saved of a tile: columns come in turns of 16 gates and the 16 ups of the same units.
 struct EpiGlu {
     static constexpr bool kFold = true, kTail = false;
     struct Args {
         uint16_t* out;
         int64_t ldo;
-        float* saved;         // or null
-        int vec, vec_saved;   // rows are 16-byte aligned
+        Saved saved;          // base null: not kept
+        int vec;              // out's rows are 16-byte aligned
         int hidden, act;
         float scale;
     };
@@ -33,36 +53,38 @@ struct EpiGlu {
     uint32_t kept[8];         // 16 units' outputs, until the next 16 fill their line of 64 bytes
     __device__ __forceinline__ EpiGlu(const Args& a_, const HgArgs&, const HgTile&, const HgPart& p_) : a(a_), p(p_) {}
     __device__ __forceinline__ void fetch(int) {}
-    // 16 values of each row, a thread's in v, to columns col.. of saved
-    __device__ __forceinline__ void save(const float* v, int unit, float* base) const {
-        uint4 w[4];
+    __device__ __forceinline__ void save(const float* v, int unit) const {
+        if (unit + 16 > a.hidden) {           // the units past the whole blocks
+            int up;
+            float* dst = a.saved.rest(unit, p.row, &up);
+            if (p.row < p.rows)
 #pragma unroll
-        for (int j = 0; j < 4; ++j)
-            w[j] = make_uint4(__float_as_uint(v[4 * j]), __float_as_uint(v[4 * j + 1]), __float_as_uint(v[4 * j + 2]), __float_as_uint(v[4 * j + 3]));
-        const int64_t ld = 2 * (int64_t)a.hidden;
-        if (a.vec_saved) {
-            p.stage.to_lines(w);
-            const int c = unit + 4 * p.stage.line_chunk(), row = p.row0 + p.stage.line_row(0);
-#pragma unroll
-            for (int i = 0; i < 4; ++i)
-                if (row + 8 * i < p.rows && c < a.hidden) *reinterpret_cast<uint4*>(base + (row + 8 * i) * ld + c) = w[i];
+                for (int j = 0; j < 16; ++j)
+                    if (unit + j < a.hidden) dst[j] = v[j], dst[up + j] = v[16 + j];
             return;
         }
-        p.stage.put(w);
-        const int rows = min(32, p.rows - p.row0), c = unit + (p.stage.lane & 15);
-        for (int r = p.stage.lane >> 4; r < rows; r += 2)
-            if (c < a.hidden) base[(p.row0 + r) * ld + c] = p.stage.value<float>(r, p.stage.lane & 15);
-        __syncwarp();
+#pragma unroll
+        for (int half = 0; half < 2; ++half) {
+            uint4 w[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const float* f = v + 16 * half + 4 * j;
+                w[j] = make_uint4(__float_as_uint(f[0]), __float_as_uint(f[1]), __float_as_uint(f[2]), __float_as_uint(f[3]));
+            }
+            p.stage.to_lines(w);
+            const int row = p.row0 + p.stage.line_row(0);
+            uint4* dst = reinterpret_cast<uint4*>(a.saved.line(unit >> 4, row) + 16 * half + 4 * p.stage.line_chunk());
+#pragma unroll
+            for (int i = 0; i < 4; ++i)
+                if (row + 8 * i < p.rows) dst[8 * i * 8] = w[i];
+        }
     }
     __device__ __forceinline__ void cols(int c, float* v) {
         const int unit = (p.col0 + c) >> 1;
         if (unit < a.hidden) {
 #pragma unroll
             for (int j = 0; j < 32; ++j) v[j] *= a.scale;
-            if (a.saved) {
-                save(v, unit, a.saved);
-                save(v + 16, unit, a.saved + a.hidden);
-            }
+            if (a.saved.base) save(v, unit);
             with_act(a.act, [&](auto act) {
 #pragma unroll
                 for (int j = 0; j < 16; j += 2) {
@@ -107,7 +129,7 @@ struct FewGluArgs {
     int64_t ldx, ldw, ldo;
     int rows, features, hidden, ks, act;
     uint16_t* out;
-    float* saved;          // or null
+    Saved saved;           // base null: not kept
     float scale;
 };
 
@@ -152,7 +174,11 @@ __global__ void __launch_bounds__(256, 2) k_glu_few(const T* x, const uint16_t* 
         const int i = lane / kLanes, row = i / (2 * C), unit = first + i % C;
         if (sub == 0 && lane % kLanes == 0 && row < a.rows && unit < a.hidden) {
             const bool gate = i % (2 * C) < C;
-            if (a.saved) a.saved[(int64_t)row * 2 * a.hidden + (gate ? 0 : a.hidden) + unit] = z;
+            if (a.saved.base) {
+                int to_up;
+                float* dst = a.saved.at(unit, row, &to_up);
+                dst[gate ? 0 : to_up] = z;
+            }
             if (gate) {
                 float v = 0.0f;
                 with_act(a.act, [&](auto act) { v = act_value<decltype(act)::value>(z); });
@@ -209,69 +235,92 @@ __device__ __forceinline__ void pack_rows(const PackJob& j, int cta) {
 }
 
 // D [rows][ldd] from saved and dout, and what its rounding left over `low` elements on (0: not kept): four units a
-// thread where rows are aligned (vec), else one.
+// thread, past the whole blocks one.
 struct GradJob {
-    const float* saved;
+    Saved saved;
     const uint16_t* dout;
     int64_t lddout, rows, ldd, low;
     uint16_t* D;
-    int hidden, act, vec;
+    int hidden, act;
+    int align;             // units that dout's rows and D's second half start at multiples of: 4, 2 or 1
     int ctas;
 };
-template <bool VEC>
+// N values of 16 bits at an address that is a multiple of `align` of them
+template <int N>
+__device__ __forceinline__ void store16(uint16_t* dst, const uint32_t* w, int align) {
+    if (N == 4 && align >= 4) {
+        *reinterpret_cast<uint2*>(dst) = make_uint2(w[0], w[1]);
+    } else if (N == 4 && align == 2) {
+        reinterpret_cast<uint32_t*>(dst)[0] = w[0];
+        reinterpret_cast<uint32_t*>(dst)[1] = w[1];
+    } else {
+#pragma unroll
+        for (int j = 0; j < N; ++j) dst[j] = (uint16_t)(w[j >> 1] >> (16 * (j & 1)));
+    }
+}
+template <int N>
+__device__ __forceinline__ void grad_units(const GradJob& job, int64_t row, int unit, const float* gate, int up) {
+    constexpr int P = (N + 1) / 2;
+    float2 a[P], b[P], g[P];
+    const uint16_t* d = job.dout + row * job.lddout + unit;
+    if constexpr (N == 4) {
+        const float4 z = *reinterpret_cast<const float4*>(gate), y = *reinterpret_cast<const float4*>(gate + up);
+        a[0] = make_float2(z.x, z.y), a[1] = make_float2(z.z, z.w);
+        b[0] = make_float2(y.x, y.y), b[1] = make_float2(y.z, y.w);
+        uint32_t w[2];
+        if (job.align == 4) {
+            *reinterpret_cast<uint2*>(w) = *reinterpret_cast<const uint2*>(d);
+        } else if (job.align == 2) {
+            w[0] = reinterpret_cast<const uint32_t*>(d)[0];
+            w[1] = reinterpret_cast<const uint32_t*>(d)[1];
+        } else {
+            w[0] = d[0] | (uint32_t)d[1] << 16;
+            w[1] = d[2] | (uint32_t)d[3] << 16;
+        }
+#pragma unroll
+        for (int j = 0; j < 2; ++j) g[j] = make_float2(__uint_as_float(w[j] << 16), __uint_as_float(w[j] & 0xffff0000u));
+    } else {
+        a[0] = make_float2(gate[0], 0.0f), b[0] = make_float2(gate[up], 0.0f), g[0] = make_float2(__uint_as_float((uint32_t)d[0] << 16), 0.0f);
+    }
+    with_act(job.act, [&](auto k) {
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            float2 v;
+            const float2 slope = act_slope<decltype(k)::value>(a[j], &v);
+            a[j] = mul2(mul2(g[j], b[j]), slope);
+            b[j] = mul2(g[j], v);
+        }
+    });
+    uint16_t* dst = job.D + row * job.ldd + unit;
+    for (int half = 0;; ++half) {
+        uint32_t wa[P], wb[P];
+#pragma unroll
+        for (int j = 0; j < P; ++j) wa[j] = pack_bf16(a[j].x, a[j].y), wb[j] = pack_bf16(b[j].x, b[j].y);
+        store16<N>(dst, wa, 4);
+        store16<N>(dst + job.hidden, wb, job.align);
+        if (job.low == 0 || half == 1) break;
+#pragma unroll
+        for (int j = 0; j < P; ++j) {
+            a[j] = sub2(a[j], make_float2(__uint_as_float(wa[j] << 16), __uint_as_float(wa[j] & 0xffff0000u)));
+            b[j] = sub2(b[j], make_float2(__uint_as_float(wb[j] << 16), __uint_as_float(wb[j] & 0xffff0000u)));
+        }
+        dst += job.low;
+    }
+}
+// units of a row that a thread takes, as items
+__host__ __device__ __forceinline__ int grad_items(int hidden) { return hidden / 16 * 4 + hidden % 16; }
 __device__ __forceinline__ void grad_rows(const GradJob& job, int cta) {
-    constexpr int E = VEC ? 4 : 1;
-    const int hidden = job.hidden, per = hidden / E;
+    const int per = grad_items(job.hidden), quads = job.saved.blocks() * 4;
     const int64_t items = job.rows * per, step = (int64_t)job.ctas * 256, first = cta * (int64_t)256 + threadIdx.x;
     RowWalk at(first, step, per);
     for (int64_t i = first; i < items; i += step, at.next()) {
-        const int c = at.part * E;
-        const float* z = job.saved + at.row * 2 * hidden + c;
-        float a[E], b[E], g[E], da[E], db[E];
-        if constexpr (VEC) {
-            *reinterpret_cast<float4*>(a) = *reinterpret_cast<const float4*>(z);
-            *reinterpret_cast<float4*>(b) = *reinterpret_cast<const float4*>(z + hidden);
-            const uint2 u = *reinterpret_cast<const uint2*>(job.dout + at.row * job.lddout + c);
-            g[0] = __uint_as_float(u.x << 16), g[1] = __uint_as_float(u.x & 0xffff0000u);
-            g[2] = __uint_as_float(u.y << 16), g[3] = __uint_as_float(u.y & 0xffff0000u);
+        if (at.part < quads) {
+            grad_units<4>(job, at.row, 4 * at.part, job.saved.line(at.part >> 2, at.row) + 4 * (at.part & 3), 16);
         } else {
-            a[0] = z[0], b[0] = z[hidden], g[0] = __uint_as_float((uint32_t)job.dout[at.row * job.lddout + c] << 16);
-        }
-        with_act(job.act, [&](auto k) {
-#pragma unroll
-            for (int j = 0; j < E; j += 2) {
-                float2 v;
-                const float2 d = act_slope<decltype(k)::value>(make_float2(a[j], E > 1 ? a[j + 1] : 0.0f), &v);
-                da[j] = g[j] * b[j] * d.x;
-                db[j] = g[j] * v.x;
-                if (E > 1) {
-                    da[j + 1] = g[j + 1] * b[j + 1] * d.y;
-                    db[j + 1] = g[j + 1] * v.y;
-                }
-            }
-        });
-        uint16_t* dst = job.D + at.row * job.ldd + c;
-        for (int half = 0;; ++half) {
-            uint16_t ha[E], hb[E];
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                ha[j] = __bfloat16_as_ushort(__float2bfloat16_rn(da[j]));
-                hb[j] = __bfloat16_as_ushort(__float2bfloat16_rn(db[j]));
-            }
-            if constexpr (VEC) {
-                *reinterpret_cast<uint2*>(dst) = make_uint2(ha[0] | (uint32_t)ha[1] << 16, ha[2] | (uint32_t)ha[3] << 16);
-                *reinterpret_cast<uint2*>(dst + hidden) = make_uint2(hb[0] | (uint32_t)hb[1] << 16, hb[2] | (uint32_t)hb[3] << 16);
-            } else {
-                dst[0] = ha[0];
-                dst[hidden] = hb[0];
-            }
-            if (job.low == 0 || half == 1) break;
-#pragma unroll
-            for (int j = 0; j < E; ++j) {
-                da[j] -= __uint_as_float((uint32_t)ha[j] << 16);
-                db[j] -= __uint_as_float((uint32_t)hb[j] << 16);
-            }
-            dst += job.low;
+            int up;
+            const int unit = job.saved.blocks() * 16 + at.part - quads;
+            const float* gate = job.saved.rest(unit, at.row, &up);
+            grad_units<1>(job, at.row, unit, gate, up);
         }
     }
 }
@@ -281,8 +330,7 @@ __global__ void __launch_bounds__(256) k_glu_prep(const PackJob x, const PackJob
     pdl_wait();
     int cta = blockIdx.x;
     if (cta < g.ctas) {
-        if (g.vec) grad_rows<true>(g, cta);
-        else grad_rows<false>(g, cta);
+        grad_rows(g, cta);
         return;
     }
     cta -= g.ctas;
@@ -336,7 +384,7 @@ cudaError_t prepare(nitro_glu* h, const void* x, int x_type, int64_t ldx, const 
         *ow = {h->wp, h->features, rows_w, h->ldp, 1, 0};
         bytes += 4.0 * rows_w * h->features;
     }
-    const int64_t items[3] = {g.rows * (g.hidden / (g.vec ? 4 : 1)), jx.ctas ? rows * (h->ldp / 8) : 0, jw.ctas ? rows_w * (h->ldp / 8) : 0};
+    const int64_t items[3] = {g.rows * grad_items(g.hidden), jx.ctas ? rows * (h->ldp / 8) : 0, jw.ctas ? rows_w * (h->ldp / 8) : 0};
     const int64_t all = items[0] + items[1] + items[2];
     if (all == 0) return cudaSuccess;
     // one wave of CTAs, shared out by their threads' work
@@ -413,12 +461,12 @@ nitro_status nitro_glu_create(int max_rows, int features, int hidden, nitro_glu*
 nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t ldx, const uint16_t* w, int64_t ldw, int rows,
                                float scale, int act, uint16_t* out, int64_t ldo, float* saved, void* stream) {
     if (!glu_args(h, x, x_type, ldx, w, ldw, rows, scale, act) || ldo < h->hidden) return NITRO_ERR_ARG;
-    if (((uintptr_t)out & 1) || ((uintptr_t)saved & 3)) return NITRO_ERR_ARG;
+    if (((uintptr_t)out & 1) || ((uintptr_t)saved & 15)) return NITRO_ERR_ARG;
     if (rows == 0) return NITRO_OK;
     if (!out) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     if (rows <= kFewRows) {
-        TRY(forward_few(h, x, x_type, w, FewGluArgs{ldx, ldw, ldo, rows, h->features, h->hidden, 1, act, out, saved, scale}, s));
+        TRY(forward_few(h, x, x_type, w, FewGluArgs{ldx, ldw, ldo, rows, h->features, h->hidden, 1, act, out, Saved{saved, rows, h->hidden}, scale}, s));
         return NITRO_OK;
     }
     HgOperand ox, ow;
@@ -431,7 +479,7 @@ nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t 
     p.fold = h->features > kFoldFeatures;
     p.rows_a = rows_in_stage(rows);
     p.eights = hg_eights<EpiGlu, false, false, false>();
-    const EpiGlu::Args ea{out, ldo, saved, tma_rows(out, ldo), ((uintptr_t)saved & 15) == 0 && h->hidden % 4 == 0, h->hidden, act, scale};
+    const EpiGlu::Args ea{out, ldo, Saved{saved, rows, h->hidden}, tma_rows(out, ldo), h->hidden, act, scale};
     TRY((hg_launch<EpiGlu, false, false, false>(hg_pick(p), p, ox, ow, ea, s)));
     return NITRO_OK;
 }
@@ -442,7 +490,7 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
     if (!glu_args(h, x, x_type, ldx, w, ldw, rows, scale, act) || lddout < h->hidden) return NITRO_ERR_ARG;
     if ((dx && (lddx < h->features || ((uintptr_t)dx & 1))) || (dw && (lddw < h->features || ((uintptr_t)dw & 1))))
         return NITRO_ERR_ARG;
-    if (rows > 0 && (!saved || !dout || ((uintptr_t)saved & 3) || ((uintptr_t)dout & 1))) return NITRO_ERR_ARG;
+    if (rows > 0 && (!saved || !dout || ((uintptr_t)saved & 15) || ((uintptr_t)dout & 1))) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     const int F = h->features;
     const int64_t H2 = 2 * (int64_t)h->hidden;
@@ -459,8 +507,9 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
     if (!dx && !dw) return NITRO_OK;
     const int halves = rows <= kRowsWithLow ? 2 : 1;
     const int64_t plane = rows * h->ldd;
-    const bool vec = h->hidden % 4 == 0 && ((uintptr_t)saved & 15) == 0 && ((uintptr_t)dout & 7) == 0 && lddout % 4 == 0;
-    const GradJob g{saved, dout, lddout, rows, h->ldd, halves == 2 ? plane : 0, h->D, h->hidden, act, vec, 0};
+    const uintptr_t starts = (uintptr_t)dout | (uintptr_t)(lddout * 2) | (uintptr_t)h->hidden * 2;
+    const int align = starts % 8 == 0 ? 4 : starts % 4 == 0 ? 2 : 1;
+    const GradJob g{Saved{const_cast<float*>(saved), rows, h->hidden}, dout, lddout, rows, h->ldd, halves == 2 ? plane : 0, h->D, h->hidden, act, align, 0};
     HgOperand ox, ow;
     TRY(prepare(h, x, x_type, ldx, w, ldw, rows, g, s, &ox, &ow));
     const HgOperand D{h->D, H2, rows, h->ldd, halves, plane};
