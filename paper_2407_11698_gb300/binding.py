@@ -718,11 +718,13 @@ class Mx4Linear(_Handle):
 def _map(t, shape, allowed, what):
     """(address, type, pixel stride, sample stride) of a CUDA map [samples x pixels x channels] whose channels are
     contiguous."""
-    code = _code(t)
+    code = _codes.get(t.dtype) if _codes else _code(t)
     if code not in allowed or not t.is_cuda or t.shape != shape:
         raise ValueError("%s must be a CUDA tensor %s of a supported type, not %s %s on %s"
                          % (what, list(shape), tuple(t.shape), t.dtype, t.device))
     n, p, c = shape
+    if t.is_contiguous():
+        return t.data_ptr(), code, c, p * c
     stride, ld, step = t.stride()
     if step != 1 and c > 1:
         raise ValueError("the channels of %s must be contiguous" % what)
@@ -743,22 +745,20 @@ class GroupNorm(_Handle):
     def __init__(self, max_samples, max_pixels, channels, groups):
         self.channels, self.groups = int(channels), int(groups)
         self._create(max_samples, max_pixels, channels, groups)
-
-    def _param(self, t, what):
-        return None if t is None else _vector(t, self.channels, NITRO_F32, what)
-
-    def _stat(self, t, n, what):
-        return None if t is None else _vector(t, n * self.groups, NITRO_F32, what)
+        self._calls = lib().nitro_gnorm_forward, lib().nitro_gnorm_backward
 
     def forward(self, x, gamma, beta, y, mean=None, rstd=None, eps=1e-5, act=NITRO_ACT_NONE, stream=None):
         """Writes y (bf16 or fp32) and, if given, mean and rstd (fp32 [samples x groups]); x: int8, bf16 or fp32."""
-        n, p = x.shape[0], x.shape[1]
-        shape = (n, p, self.channels)
+        n, p = x.shape[:2]
+        c, m = self.channels, n * self.groups
+        shape = (n, p, c)
         xp, xt, ldx, sx = _map(x, shape, _GN_X, "x")
         yp, yt, ldy, sy = _map(y, shape, _GN_Y, "y")
-        st = lib().nitro_gnorm_forward(self.h, xp, xt, ldx, sx, n, p, self._param(gamma, "gamma"), self._param(beta, "beta"),
-                                       eps, act, yp, yt, ldy, sy, self._stat(mean, n, "mean"), self._stat(rstd, n, "rstd"),
-                                       _stream_int(stream))
+        st = self._calls[0](self.h, xp, xt, ldx, sx, n, p, None if gamma is None else _vector(gamma, c, NITRO_F32, "gamma"),
+                            None if beta is None else _vector(beta, c, NITRO_F32, "beta"), eps, act, yp, yt, ldy, sy,
+                            None if mean is None else _vector(mean, m, NITRO_F32, "mean"),
+                            None if rstd is None else _vector(rstd, m, NITRO_F32, "rstd"),
+                            _current_stream() if stream is None else _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_gnorm_forward")
         return y
@@ -766,14 +766,19 @@ class GroupNorm(_Handle):
     def backward(self, x, gamma, beta, mean, rstd, dy, dx=None, dgamma=None, dbeta=None, act=NITRO_ACT_NONE, stream=None):
         """Writes dx (of dy's type), dgamma and dbeta (fp32 [channels]), each unless None, from mean and rstd of a
         forward on the same inputs."""
-        n, p = x.shape[0], x.shape[1]
-        shape = (n, p, self.channels)
+        n, p = x.shape[:2]
+        c, m = self.channels, n * self.groups
+        shape = (n, p, c)
         xp, xt, ldx, sx = _map(x, shape, _GN_X, "x")
         gp, gt, ldg, sg = _map(dy, shape, _GN_Y, "dy")
         dp, _, ldd, sd = (None, gt, ldg, sg) if dx is None else _map(dx, shape, (gt,), "dx")
-        st = lib().nitro_gnorm_backward(self.h, xp, xt, ldx, sx, n, p, self._param(gamma, "gamma"), self._param(beta, "beta"),
-                                        self._stat(mean, n, "mean"), self._stat(rstd, n, "rstd"), act, gp, gt, ldg, sg, dp, ldd, sd,
-                                        self._param(dgamma, "dgamma"), self._param(dbeta, "dbeta"), _stream_int(stream))
+        st = self._calls[1](self.h, xp, xt, ldx, sx, n, p, None if gamma is None else _vector(gamma, c, NITRO_F32, "gamma"),
+                            None if beta is None else _vector(beta, c, NITRO_F32, "beta"),
+                            None if mean is None else _vector(mean, m, NITRO_F32, "mean"),
+                            None if rstd is None else _vector(rstd, m, NITRO_F32, "rstd"), act, gp, gt, ldg, sg, dp, ldd, sd,
+                            None if dgamma is None else _vector(dgamma, c, NITRO_F32, "dgamma"),
+                            None if dbeta is None else _vector(dbeta, c, NITRO_F32, "dbeta"),
+                            _current_stream() if stream is None else _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_gnorm_backward")
         return dx, dgamma, dbeta
@@ -787,20 +792,18 @@ class GatedLinear(_Handle):
     def __init__(self, max_rows, features, hidden):
         self.features, self.hidden = int(features), int(hidden)
         self._create(max_rows, features, hidden)
-
-    def _inputs(self, x, w, scale, act):
-        n = x.shape[0]
-        xp, xt, ldx = _matrix(x, n, self.features, _X, "x")
-        wp, _, ldw = _matrix(w, 2 * self.hidden, self.features, _W, "w")
-        return n, (xp, xt, ldx, wp, ldw, n, scale, act)
+        self._calls = lib().nitro_glu_forward, lib().nitro_glu_backward
 
     def forward(self, x, w, out, saved=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
-        """Writes out (bf16 [rows x hidden]) and, for a backward, z to saved (fp32 [rows x 2 hidden], in an order of the library's own)."""
-        n, a = self._inputs(x, w, scale, act)
-        op, _, ldo = _matrix(out, n, self.hidden, _W, "out")
-        st = lib().nitro_glu_forward(self.h, *a, op, ldo,
-                                     None if saved is None else _vector(saved, 2 * n * self.hidden, NITRO_F32, "saved"),
-                                     _stream_int(stream))
+        """Writes out (bf16 [rows x hidden]) and, for a backward, z to saved (fp32 [rows x 2 hidden], in an order of the
+        library's own)."""
+        n, f, hidden = x.shape[0], self.features, self.hidden
+        xp, xt, ldx = _matrix(x, n, f, _X, "x")
+        wp, _, ldw = _matrix(w, 2 * hidden, f, _W, "w")
+        op, _, ldo = _matrix(out, n, hidden, _W, "out")
+        st = self._calls[0](self.h, xp, xt, ldx, wp, ldw, n, scale, act, op, ldo,
+                            None if saved is None else _vector(saved, 2 * n * hidden, NITRO_F32, "saved"),
+                            _current_stream() if stream is None else _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_glu_forward")
         return out
@@ -808,16 +811,14 @@ class GatedLinear(_Handle):
     def backward(self, x, w, saved, dout, dx=None, dw=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
         """Writes dx [rows x features] and dw [2 hidden x features] (bf16; either may be None) from the
         gradient dout (bf16 [rows x hidden]) and the saved of a forward on the same inputs."""
-        n, a = self._inputs(x, w, scale, act)
-        gp, _, ldg = _matrix(dout, n, self.hidden, _W, "dout")
-        dxp = dwp = None
-        lddx = lddw = self.features
-        if dx is not None:
-            dxp, _, lddx = _matrix(dx, n, self.features, _W, "dx")
-        if dw is not None:
-            dwp, _, lddw = _matrix(dw, 2 * self.hidden, self.features, _W, "dw")
-        st = lib().nitro_glu_backward(self.h, *a, _vector(saved, 2 * n * self.hidden, NITRO_F32, "saved"), gp, ldg, dxp, lddx,
-                                      dwp, lddw, _stream_int(stream))
+        n, f, hidden = x.shape[0], self.features, self.hidden
+        xp, xt, ldx = _matrix(x, n, f, _X, "x")
+        wp, _, ldw = _matrix(w, 2 * hidden, f, _W, "w")
+        gp, _, ldg = _matrix(dout, n, hidden, _W, "dout")
+        dxp, _, lddx = (None, 0, f) if dx is None else _matrix(dx, n, f, _W, "dx")
+        dwp, _, lddw = (None, 0, f) if dw is None else _matrix(dw, 2 * hidden, f, _W, "dw")
+        st = self._calls[1](self.h, xp, xt, ldx, wp, ldw, n, scale, act, _vector(saved, 2 * n * hidden, NITRO_F32, "saved"), gp, ldg,
+                            dxp, lddx, dwp, lddw, _current_stream() if stream is None else _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_glu_backward")
         return dx, dw
