@@ -210,7 +210,64 @@ struct Sums {
     }
 };
 
+// A vector's place in shared memory: planes of 16 bytes a thread (or less, the vector itself)
+template <typename T, int V>
+struct Slots {
+    static constexpr int BYTES = V * (int)sizeof(T), PLANE = BYTES < 16 ? BYTES : 16, PLANES = BYTES / PLANE;
+    static constexpr int STEP = kGnThreads * BYTES;          // from a thread's vector to its next
+    static __device__ __forceinline__ uint8_t* first(uint8_t* base) { return base + (int)threadIdx.x * PLANE; }
+    // Place: whose places the vector takes, its own or those of wider values that replace it later
+    template <class Place = Slots>
+    static __device__ __forceinline__ void fetch(uint8_t* to, const T* src) {
+        if constexpr (PLANE < 4) {
+            *reinterpret_cast<T*>(to) = *src;
+        } else {
+#pragma unroll
+            for (int i = 0; i < PLANES; ++i) {
+                const uint32_t dst = smem_u32(to + i * kGnThreads * Place::PLANE);
+                const char* s = reinterpret_cast<const char*>(src) + i * PLANE;
+                if constexpr (PLANE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(s) : "memory");
+                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(s), "n"(PLANE) : "memory");
+            }
+        }
+    }
+    template <class Place = Slots>
+    static __device__ __forceinline__ void get(const uint8_t* from, float2* v) {
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i)
+            Vals<T, V / PLANES>::load(reinterpret_cast<const T*>(from + i * kGnThreads * Place::PLANE), v + i * (V / PLANES / 2));
+    }
+    static __device__ __forceinline__ void put(uint8_t* to, const float2* v) {
+#pragma unroll
+        for (int i = 0; i < PLANES; ++i)
+            Vals<T, V / PLANES>::store(reinterpret_cast<T*>(to + i * kGnThreads * PLANE), v + i * (V / PLANES / 2));
+    }
+};
+__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
+
 // ------------------------------------------------------------------ two passes
+// fetch(i, s) for i = 0 .. n - 1 starts the copies of a thread's step i to its place s of a ring, use(i, s) works on them.
+constexpr int kRingGroups = 3, kRingGroup = 2, kRing = kRingGroups * kRingGroup;
+template <class Fetch, class Use>
+__device__ __forceinline__ void through_ring(int n, Fetch&& fetch, Use&& use) {
+    const auto group = [&](int i, int s) {
+#pragma unroll
+        for (int k = 0; k < kRingGroup; ++k)
+            if (i + k < n) fetch(i + k, s + k);
+        copies_group();
+    };
+#pragma unroll
+    for (int g = 0; g < kRingGroups; ++g) group(g * kRingGroup, g * kRingGroup);
+    for (int i = 0, s = 0; i < n; i += kRingGroup) {
+        asm volatile("cp.async.wait_group %0;" ::"n"(kRingGroups - 1) : "memory");
+#pragma unroll
+        for (int k = 0; k < kRingGroup; ++k)
+            if (i + k < n) use(i + k, s + k);
+        group(i + kRing, s);
+        s = s + kRingGroup == kRing ? 0 : s + kRingGroup;
+    }
+}
+
 // CTAs of a backward pass that an SM holds by their registers
 constexpr int gn_resident(int v) { return v == 8 ? 2 : 4; }
 
@@ -239,6 +296,8 @@ struct GnPlace {
         const int c = (i * s.vecs + vec) * V;
         return live && c < s.channels ? c : -1;
     }
+    // pixels of np that the thread takes
+    __device__ __forceinline__ int steps(const GnShape& s, int np) const { return row < np ? (np - row + s.rows - 1) / s.rows : 0; }
     __device__ __forceinline__ GnGroup group(const GnShape& s, int c) const {
         const int g = c / s.per;
         return {g, c - g * s.per, s.per};
@@ -263,11 +322,13 @@ __device__ __forceinline__ bool gn_last(uint32_t* ticket, int chunks, int* word)
     return *word;
 }
 
-// mean and rstd of a sample's groups.  Dynamic shared memory: two values a channel.
+// mean and rstd of a sample's groups.  Dynamic shared memory: the ring, two values a channel.
 template <typename X, int V>
 __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx, int64_t sx, const GnShape s, float eps, float2* parts,
                                                          uint32_t* ticket, float* mean, float* rstd) {
-    extern __shared__ float chan[];                   // [channels] means, [channels] squared distances
+    using SX = Slots<X, V>;
+    extern __shared__ __align__(16) uint8_t data[];
+    float* chan = reinterpret_cast<float*>(data + kRing * SX::STEP);      // [channels] means, [channels] squared distances
     __shared__ float red[2][kGnThreads * V];          // [rows][slab's channels]
     __shared__ int word;
     pdl_wait();
@@ -287,13 +348,16 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
             const X* src = x + (int64_t)(p0 + at.row) * ldx + c;
             if (at.row < np) Vals<X, V>::load(src, t.k);
             const int64_t step = s.rows * ldx;
-#pragma unroll 8
-            for (int p = at.row; p < np; p += s.rows, src += step) {
-                float2 v[Sums<V>::N];
-                Vals<X, V>::load(src, v);
-                t.add(v);
-            }
-            t.finish((float)max(0, (np - at.row + s.rows - 1) / s.rows), at.group(s, c), s.per % V == 0, origin);      // 0 for rows past the chunk
+            const int n = at.steps(s, np);
+            uint8_t* slot = SX::first(data);
+            through_ring(
+                n, [&](int i, int k) { SX::fetch(slot + k * SX::STEP, src + i * step); },
+                [&](int, int k) {
+                    float2 v[Sums<V>::N];
+                    SX::get(slot + k * SX::STEP, v);
+                    t.add(v);
+                });
+            t.finish((float)n, at.group(s, c), s.per % V == 0, origin);      // 0 for rows past the chunk
 #pragma unroll
             for (int j = 0; j < V; ++j) {
                 red[0][at.row * width + at.vec * V + j] = at2(t.sum, j);
@@ -339,6 +403,8 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
 template <typename X, typename Y, int V>
 __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx, int64_t sx, const GnShape s, const float* mean,
                                                          const float* rstd, Y* y, int64_t ldy, int64_t sy) {
+    using SX = Slots<X, V>;
+    extern __shared__ __align__(16) uint8_t data[];
     pdl_wait();
     const int sample = blockIdx.y, p0 = blockIdx.x * s.chunk, p1 = min(s.pixels, p0 + s.chunk), np = p1 - p0;
     const GnPlace at(s);
@@ -354,13 +420,15 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
         Y* dst = y + sample * sy + (int64_t)(p0 + at.row) * ldy + c;
         const int64_t xs = s.rows * ldx, ys = s.rows * ldy;
         with_act(s.act, [&](auto act) {
-#pragma unroll 4
-            for (int p = at.row; p < np; p += s.rows, src += xs, dst += ys) {
-                float2 v[ch.N];
-                Vals<X, V>::load(src, v);
-                ch.template apply<decltype(act)::value>(v);
-                Vals<Y, V>::store(dst, v);
-            }
+            uint8_t* slot = SX::first(data);
+            through_ring(
+                at.steps(s, np), [&](int i, int k) { SX::fetch(slot + k * SX::STEP, src + i * xs); },
+                [&](int i, int k) {
+                    float2 v[ch.N];
+                    SX::get(slot + k * SX::STEP, v);
+                    ch.template apply<decltype(act)::value>(v);
+                    Vals<Y, V>::store(dst + i * ys, v);
+                });
         });
     }
 }
@@ -371,6 +439,10 @@ template <typename X, typename Y, int V>
 __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                            const GnShape s, const float* mean, const float* rstd, float* part_c,
                                                            float2* parts, uint32_t* ticket, float2* means) {
+    using SX = Slots<X, V>;
+    using SY = Slots<Y, V>;
+    extern __shared__ __align__(16) uint8_t data[];
+    uint8_t *xslot = SX::first(data), *gslot = SY::first(data + kRing * SX::STEP);
     __shared__ float red[2][kGnThreads * V];
     __shared__ int word;
     pdl_wait();
@@ -391,18 +463,23 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X*
             const Y* grad = dy + sample * sdy + (int64_t)(p0 + at.row) * lddy + c;
             const int64_t xs = s.rows * ldx, gs = s.rows * lddy;
             with_act(s.act, [&](auto act) {
-#pragma unroll 4
-                for (int p = at.row; p < np; p += s.rows, src += xs, grad += gs) {
-                    float2 v[ch.N], g[ch.N];
-                    Vals<X, V>::load(src, v);
-                    Vals<Y, V>::load(grad, g);
-                    ch.template slopes<decltype(act)::value>(v, g);
+                through_ring(
+                    at.steps(s, np),
+                    [&](int i, int k) {
+                        SX::fetch(xslot + k * SX::STEP, src + i * xs);
+                        SY::fetch(gslot + k * SY::STEP, grad + i * gs);
+                    },
+                    [&](int, int k) {
+                        float2 v[ch.N], g[ch.N];
+                        SX::get(xslot + k * SX::STEP, v);
+                        SY::get(gslot + k * SY::STEP, g);
+                        ch.template slopes<decltype(act)::value>(v, g);
 #pragma unroll
-                    for (int j = 0; j < ch.N; ++j) {
-                        a[j] = add2(a[j], g[j]);
-                        b[j] = fma2(g[j], v[j], b[j]);
-                    }
-                }
+                        for (int j = 0; j < ch.N; ++j) {
+                            a[j] = add2(a[j], g[j]);
+                            b[j] = fma2(g[j], v[j], b[j]);
+                        }
+                    });
             });
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -455,6 +532,10 @@ template <typename X, typename Y, int V>
 __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                          const GnShape s, const float* mean, const float* rstd, const float2* means,
                                                          Y* dx, int64_t lddx, int64_t sdx) {
+    using SX = Slots<X, V>;
+    using SY = Slots<Y, V>;
+    extern __shared__ __align__(16) uint8_t data[];
+    uint8_t *xslot = SX::first(data), *gslot = SY::first(data + kRing * SX::STEP);
     pdl_wait();
     const int sample = blockIdx.y, p0 = blockIdx.x * s.chunk, p1 = min(s.pixels, p0 + s.chunk), np = p1 - p0;
     const GnPlace at(s);
@@ -480,17 +561,22 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_dx(const X* x
         Y* dst = dx + sample * sdx + (int64_t)(p0 + at.row) * lddx + c;
         const int64_t xs = s.rows * ldx, gs = s.rows * lddy, ds = s.rows * lddx;
         with_act(s.act, [&](auto act) {
-#pragma unroll 4
-            for (int p = at.row; p < np; p += s.rows, src += xs, grad += gs, dst += ds) {
-                float2 v[ch.N], h[ch.N], g[ch.N];
-                Vals<X, V>::load(src, v);
-                Vals<Y, V>::load(grad, g);
+            through_ring(
+                at.steps(s, np),
+                [&](int i, int k) {
+                    SX::fetch(xslot + k * SX::STEP, src + i * xs);
+                    SY::fetch(gslot + k * SY::STEP, grad + i * gs);
+                },
+                [&](int i, int k) {
+                    float2 v[ch.N], h[ch.N], g[ch.N];
+                    SX::get(xslot + k * SX::STEP, v);
+                    SY::get(gslot + k * SY::STEP, g);
 #pragma unroll
-                for (int j = 0; j < ch.N; ++j) h[j] = v[j];
-                ch.template slopes<decltype(act)::value>(h, g);
-                to.dx(v, g);
-                Vals<Y, V>::store(dst, v);
-            }
+                    for (int j = 0; j < ch.N; ++j) h[j] = v[j];
+                    ch.template slopes<decltype(act)::value>(h, g);
+                    to.dx(v, g);
+                    Vals<Y, V>::store(dst + i * ds, v);
+                });
         });
     }
 }
@@ -515,42 +601,8 @@ struct GnOne {
     const float* beta;                   // or null
 };
 
-// A vector's place in shared memory: planes of 16 bytes a thread (or less, the vector itself)
-template <typename T, int V>
-struct Slots {
-    static constexpr int BYTES = V * (int)sizeof(T), PLANE = BYTES < 16 ? BYTES : 16, PLANES = BYTES / PLANE;
-    static constexpr int STEP = kGnThreads * BYTES;          // from a thread's vector to its next
-    static __device__ __forceinline__ uint8_t* first(uint8_t* base) { return base + (int)threadIdx.x * PLANE; }
-    // Place: whose places the vector takes, its own or those of wider values that replace it later
-    template <class Place = Slots>
-    static __device__ __forceinline__ void fetch(uint8_t* to, const T* src) {
-        if constexpr (PLANE < 4) {
-            *reinterpret_cast<T*>(to) = *src;
-        } else {
-#pragma unroll
-            for (int i = 0; i < PLANES; ++i) {
-                const uint32_t dst = smem_u32(to + i * kGnThreads * Place::PLANE);
-                const char* s = reinterpret_cast<const char*>(src) + i * PLANE;
-                if constexpr (PLANE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(s) : "memory");
-                else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(s), "n"(PLANE) : "memory");
-            }
-        }
-    }
-    template <class Place = Slots>
-    static __device__ __forceinline__ void get(const uint8_t* from, float2* v) {
-#pragma unroll
-        for (int i = 0; i < PLANES; ++i)
-            Vals<T, V / PLANES>::load(reinterpret_cast<const T*>(from + i * kGnThreads * Place::PLANE), v + i * (V / PLANES / 2));
-    }
-    static __device__ __forceinline__ void put(uint8_t* to, const float2* v) {
-#pragma unroll
-        for (int i = 0; i < PLANES; ++i)
-            Vals<T, V / PLANES>::store(reinterpret_cast<T*>(to + i * kGnThreads * PLANE), v + i * (V / PLANES / 2));
-    }
-};
 // A thread's copies go in up to kGnStages groups, so that the first are taken while the others are under way
 constexpr int kGnStages = 4;
-__device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 __device__ __forceinline__ void copies_landed(int stage) {
     if (stage == 0) asm volatile("cp.async.wait_group 3;" ::: "memory");
     else if (stage == 1) asm volatile("cp.async.wait_group 2;" ::: "memory");
@@ -1069,12 +1121,10 @@ GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size,
 }
 
 template <typename K>
-cudaError_t one_ready(K* kernel, std::atomic<uint64_t>& ready) {
+cudaError_t one_ready(K* kernel, std::atomic<uint64_t>& ready, int smem = 226 * 1024) {
     int dev = 0;
     sm_count(&dev);
-    return once_per_device(ready, dev, [kernel] {
-        return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, 226 * 1024);
-    });
+    return once_per_device(ready, dev, [kernel, smem] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
 }
 
 }  // namespace
@@ -1151,14 +1201,10 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
             return with_v(v, [&](auto vt) {
                 constexpr int V = decltype(vt)::value;
                 static std::atomic<uint64_t> ready{0};
-                int dev = 0;
-                sm_count(&dev);
-                const cudaError_t e = once_per_device(ready, dev, [] {
-                    return cudaFuncSetAttribute(k_gn_stats<X, V>, cudaFuncAttributeMaxDynamicSharedMemorySize, 8 * kGnChannels);
-                });
+                const cudaError_t e = one_ready(k_gn_stats<X, V>, ready, kRing * Slots<X, V>::STEP + 8 * kGnChannels);
                 if (e != cudaSuccess) return e;
                 ProfScope ps(K_GNORM_FWD, s, 0.0, values * sizeof(X));
-                return launch_k(k_gn_stats<X, V>, grid, block, 8 * C, s, sample_at<X>(mx, s0), ldx, stride_x, sh, eps, h->part,
+                return launch_k(k_gn_stats<X, V>, grid, block, kRing * Slots<X, V>::STEP + 8 * C, s, sample_at<X>(mx, s0), ldx, stride_x, sh, eps, h->part,
                                 h->ticket, m, r);
             });
         }));
@@ -1168,8 +1214,12 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
                 using Y = decltype(yt);
                 return with_v(v, [&](auto vt) {
                     constexpr int V = decltype(vt)::value;
+                    constexpr int kSmem = kRing * Slots<X, V>::STEP;
+                    static std::atomic<uint64_t> ready{0};
+                    const cudaError_t e = one_ready(k_gn_apply<X, Y, V>, ready, kSmem);
+                    if (e != cudaSuccess) return e;
                     ProfScope ps(K_GNORM_FWD, s, 0.0, values * (sizeof(X) + sizeof(Y)));
-                    return launch_k(k_gn_apply<X, Y, V>, grid, block, 0, s, sample_at<X>(mx, s0), ldx, stride_x, sh, (const float*)m,
+                    return launch_k(k_gn_apply<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sh, (const float*)m,
                                     (const float*)r, const_cast<Y*>(sample_at<Y>(my, s0)), ldy, stride_y);
                 });
             });
@@ -1242,8 +1292,12 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
                 using Y = decltype(yt);
                 return with_v(v, [&](auto vt) {
                     constexpr int V = decltype(vt)::value;
+                    constexpr int kSmem = kRing * (Slots<X, V>::STEP + Slots<Y, V>::STEP);
+                    static std::atomic<uint64_t> ready{0};
+                    const cudaError_t e = one_ready(k_gn_sums<X, Y, V>, ready, kSmem);
+                    if (e != cudaSuccess) return e;
                     ProfScope ps(K_GNORM_BWD, s, 0.0, values * (sizeof(X) + sizeof(Y)));
-                    return launch_k(k_gn_sums<X, Y, V>, grid, block, 0, s, sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0),
+                    return launch_k(k_gn_sums<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0),
                                     lddy, stride_dy, sh, m, r, h->part_c, h->part, h->ticket, dx ? h->means : nullptr);
                 });
             });
@@ -1255,8 +1309,12 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
                     using Y = decltype(yt);
                     return with_v(v, [&](auto vt) {
                         constexpr int V = decltype(vt)::value;
+                        constexpr int kSmem = kRing * (Slots<X, V>::STEP + Slots<Y, V>::STEP);
+                        static std::atomic<uint64_t> ready{0};
+                        const cudaError_t e = one_ready(k_gn_dx<X, Y, V>, ready, kSmem);
+                        if (e != cudaSuccess) return e;
                         ProfScope ps(K_GNORM_BWD, s, 0.0, values * (sizeof(X) + 2 * sizeof(Y)));
-                        return launch_k(k_gn_dx<X, Y, V>, grid, block, 0, s, sample_at<X>(mx, s0), ldx, stride_x,
+                        return launch_k(k_gn_dx<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x,
                                         sample_at<Y>(mdy, s0), lddy, stride_dy, sh, m, r, (const float2*)h->means,
                                         const_cast<Y*>(sample_at<Y>(mdx, s0)), lddx, stride_dx);
                     });
