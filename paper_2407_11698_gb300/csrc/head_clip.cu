@@ -43,16 +43,6 @@ struct alignas(16) Work {
     int n, rest;
 };
 
-struct Squares {
-    float2 mid = {0.0f, 0.0f}, big = {0.0f, 0.0f}, small = {0.0f, 0.0f};
-    __device__ __forceinline__ void add(float2 x) {
-        mid = fma2(x, x, mid);
-        const float2 b = mul2(x, pair(0x1p-80f)), s = mul2(x, pair(0x1p90f));
-        big = fma2(b, b, big);
-        small = fma2(s, s, small);
-    }
-};
-
 __device__ __forceinline__ float warp_sum(float v) {
 #pragma unroll 1
     for (int d = 16; d > 0; d >>= 1) v += __shfl_xor_sync(0xffffffffu, v, d);
@@ -71,6 +61,26 @@ struct Exact {
     __device__ __forceinline__ void over_warp() {
 #pragma unroll 1
         for (int d = 16; d > 0; d >>= 1) add(__shfl_xor_sync(0xffffffffu, hi, d), __shfl_xor_sync(0xffffffffu, lo, d));
+    }
+};
+
+// Sums of squares.  A lane's run is short before it goes to `mid`: many squares are far below a sum's last place and are
+// lost more often than they are rounded up (6700 values of bf16 in one sum: 3.5e-6 to 6.5e-6 too little).
+struct Squares {
+    float2 run = {0.0f, 0.0f}, run_big = {0.0f, 0.0f}, run_small = {0.0f, 0.0f};
+    Exact mid;
+    float big = 0.0f, small = 0.0f;
+    __device__ __forceinline__ void add(float2 x) {
+        run = fma2(x, x, run);
+        const float2 b = mul2(x, pair(0x1p-80f)), s = mul2(x, pair(0x1p90f));
+        run_big = fma2(b, b, run_big);
+        run_small = fma2(s, s, run_small);
+    }
+    __device__ __forceinline__ void end_run() {
+        mid.add(run.x + run.y, 0.0f);
+        big += run_big.x + run_big.y;
+        small += run_small.x + run_small.y;
+        run = run_big = run_small = pair(0.0f);
     }
 };
 
@@ -167,9 +177,10 @@ __device__ __forceinline__ int keep_piece(const Piece& p, int lane, uint4* kept,
     return steps;
 }
 
-// f(vector, its place in `out`) for the steps from `from` on, last ones first, through a ring of the lane's places
-template <typename T, class F>
-__device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, int lane, uint4* ring, int from, F&& f) {
+// f(vector, its place in `out`) for the steps from `from` on, last ones first, through a ring of the lane's places; end()
+// after every few
+template <typename T, class F, class End>
+__device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, int lane, uint4* ring, int from, F&& f, End&& end) {
     const auto fetch = [&](int last, uint4* to) {       // steps last, last - 1, ...
 #pragma unroll
         for (int j = 0; j < kClipGroup; ++j) {
@@ -192,6 +203,7 @@ __device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, 
             const int step = k - j, i = step * 32 + lane;
             if (step >= from && i < q.items) at_vector<T>(p, q, i, [&](const T*, T* out) { f(u[j], out); });
         }
+        end();
         fetch(k - kClipRing, at);
         if (++g == kClipGroups) g = 0;
     }
@@ -210,7 +222,7 @@ template <typename T>
 __device__ __forceinline__ int sum_piece(const Piece& p, int lane, uint4* ring, int keep, int slot, Squares& sum) {
     const Parts<T> q(p);
     const int steps = q.steps(), from = max(0, keep - slot);
-    if (steps > from) stream_piece<T>(p, q, lane, ring, from, [&](const uint4& u, T*) { sum_vector<T>(u, sum); });
+    if (steps > from) stream_piece<T>(p, q, lane, ring, from, [&](const uint4& u, T*) { sum_vector<T>(u, sum); }, [&] { sum.end_run(); });
     singles<T>(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); });
     return steps;
 }
@@ -243,7 +255,7 @@ __device__ __forceinline__ void scale_piece(const Piece& p, int lane, const uint
         *reinterpret_cast<uint4*>(out) = u;
     };
     const int steps = q.steps(), left = min(steps, max(0, keep - slot));         // steps that are kept
-    if (steps > left) stream_piece<T>(p, q, lane, ring, left, one);
+    if (steps > left) stream_piece<T>(p, q, lane, ring, left, one, [] {});
 #pragma unroll 4
     for (int k = 0; k < left; ++k) {
         const int i = k * 32 + lane;
@@ -346,11 +358,10 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
         slot += with_type(p.type, [&](auto t) { return sum_kept<decltype(t)>(p, lane, kept, keep, slot, q); });
     }
     {
-        Exact mid;
-        mid.add(q.mid.x, 0.0f);
-        mid.add(q.mid.y, 0.0f);
+        q.end_run();
+        Exact mid = q.mid;
         mid.over_warp();
-        const float big = warp_sum(q.big.x + q.big.y), small = warp_sum(q.small.x + q.small.y);
+        const float big = warp_sum(q.big), small = warp_sum(q.small);
         if (lane == 0) sh[warp] = make_float4(mid.hi, mid.lo, big, small);
     }
     if (threadIdx.x == 0) ok = 1;
