@@ -28,13 +28,19 @@ constexpr int kClipSmem = kClipPlaces * kClipThreads * 16;
 constexpr int kClipNotes = 5;                                     // that a lane looks at together
 constexpr int64_t kMostPieces = (int64_t)1 << 26;
 
-// Rows of one matrix (of lone rows: a run of one).  vec: both sides' rows start at multiples of 16 bytes
+// How a piece's values are reached: one by one; as vectors, where rows start at multiples of 16 bytes on both sides; or,
+// where they do not and the gaps between them are small, as all vectors from its first to its last value, of which
+// the gaps and what lies beside the piece in its first and last vector count for nothing (those 16 bytes hold a value of
+// the piece, so they are memory that is there).
+enum : int { kSingles = 0, kRows = 1, kSpan = 2 };
+
+// Rows of one matrix (of lone rows: a run of one)
 struct Piece {
     const void* in;
     void* out;             // or null
     int64_t ld_in, ld_out;
     int rows, cols;
-    int type, vec;
+    int type, how;
 };
 
 // What a warp does: its first piece, how many it has, and where the others are
@@ -123,33 +129,47 @@ struct Of<int64_t> {
     static __device__ __forceinline__ float get(int64_t v) { return (float)v; }
 };
 
-// A piece's work: whole vectors, `items` of them in rows of `per`, and single values, the rows' ends or all of them.
-template <typename T>
+// A piece's work: vectors, `items` of them, in rows of `per` where they are rows', and single values, the rows' ends or
+// all of them.
+template <typename T_, bool SPAN>
 struct Parts {
+    using T = T_;
+    static constexpr bool kSpan = SPAN;
     static constexpr int V = Of<T>::V;
-    int per, tail;              // whole vectors of a row, and values after them
-    int items, singles;         // (a piece has at most 2^30 bytes)
+    int per, tail;               // whole vectors of a row, and values after them
+    int items, singles;          // (a piece has at most 2^30 bytes)
+    int before;                  // values in the first vector that are not the piece's
     __device__ __forceinline__ explicit Parts(const Piece& p) {
-        per = p.vec ? p.cols / V : 0;
-        tail = p.cols - per * V;
-        items = p.rows * per;
-        singles = p.rows * tail;
+        before = 0;
+        if constexpr (SPAN) {
+            before = (int)((uintptr_t)p.in & 15) / (int)sizeof(T);
+            per = tail = singles = 0;
+            items = (before + (p.rows - 1) * (int)p.ld_in + p.cols + V - 1) / V;
+        } else {
+            per = p.how == kRows ? p.cols / V : 0;
+            tail = p.cols - per * V;
+            items = p.rows * per;
+            singles = p.rows * tail;
+        }
     }
     // steps that a warp takes for the vectors
     __device__ __forceinline__ int steps() const { return (items + 31) / 32; }
-};
-// f(in, out) with the addresses of vector i
-template <typename T, class F>
-__device__ __forceinline__ void at_vector(const Piece& p, const Parts<T>& q, int i, F&& f) {
-    int row = 0, c = i;
-    if (p.rows > 1) {
-        row = (uint32_t)i / (uint32_t)q.per;
-        c = i - row * q.per;
+    // the addresses of vector i in `in` and, of rows, in `out`
+    __device__ __forceinline__ const uint4* in(const Piece& p, int i) const {
+        if constexpr (SPAN) return reinterpret_cast<const uint4*>((uintptr_t)p.in & ~(uintptr_t)15) + i;
+        int row = 0;
+        if (p.rows > 1) row = (uint32_t)i / (uint32_t)per;
+        return reinterpret_cast<const uint4*>(static_cast<const T*>(p.in) + row * p.ld_in) + (i - row * per);
     }
-    f(static_cast<const T*>(p.in) + row * p.ld_in + c * Of<T>::V, static_cast<T*>(p.out) + row * p.ld_out + c * Of<T>::V);
-}
-template <typename T, class F>
-__device__ __forceinline__ void singles(const Piece& p, const Parts<T>& q, int lane, F&& f) {
+    __device__ __forceinline__ uint4* out(const Piece& p, int i) const {
+        int row = 0;
+        if (p.rows > 1) row = (uint32_t)i / (uint32_t)per;
+        return reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * p.ld_out) + (i - row * per);
+    }
+};
+template <class Q, class F>
+__device__ __forceinline__ void singles(const Piece& p, const Q& q, int lane, F&& f) {
+    using T = typename Q::T;
     if (q.tail == 0) return;
     RowWalk at(lane, 32, q.tail);
 #pragma unroll 4
@@ -165,27 +185,25 @@ __device__ __forceinline__ void copy16(uint4* to, const void* from) {
 
 // Starts the copies of a piece's vectors while of `keep` places some are left; `kept`: the lane's first place.
 // Steps of the piece.
-template <typename T>
+template <class Q>
 __device__ __forceinline__ int keep_piece(const Piece& p, int lane, uint4* kept, int keep, int slot) {
-    const Parts<T> q(p);
+    const Q q(p);
     const int steps = q.steps(), n = min(steps, keep - slot);
 #pragma unroll 4
-    for (int k = 0; k < n; ++k) {
-        const int i = k * 32 + lane;
-        if (i < q.items) at_vector<T>(p, q, i, [&](const T* in, T*) { copy16(kept + (slot + k) * 32, in); });
-    }
+    for (int k = 0; k < n; ++k)
+        if (k * 32 + lane < q.items) copy16(kept + (slot + k) * 32, q.in(p, k * 32 + lane));
     return steps;
 }
 
-// f(vector, its place in `out`) for the steps from `from` on, last ones first, through a ring of the lane's places; end()
-// after every few
-template <typename T, class F, class End>
-__device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, int lane, uint4* ring, int from, F&& f, End&& end) {
+// f(step, the lane's place of its vector), by all lanes, for the steps from `from` on, last ones first, through a ring of
+// places; end() after every few
+template <class Q, class F, class End>
+__device__ __forceinline__ void stream_piece(const Piece& p, const Q& q, int lane, uint4* ring, int from, F&& f, End&& end) {
     const auto fetch = [&](int last, uint4* to) {       // steps last, last - 1, ...
 #pragma unroll
         for (int j = 0; j < kClipGroup; ++j) {
             const int step = last - j, i = step * 32 + lane;
-            if (step >= from && i < q.items) at_vector<T>(p, q, i, [&](const T* in, T*) { copy16(to + j * 32, in); });
+            if (step >= from && i < q.items) copy16(to + j * 32, q.in(p, i));
         }
         asm volatile("cp.async.commit_group;" ::: "memory");
     };
@@ -195,80 +213,130 @@ __device__ __forceinline__ void stream_piece(const Piece& p, const Parts<T>& q, 
     for (int g = 0; k >= from; k -= kClipGroup) {
         asm volatile("cp.async.wait_group %0;" ::"n"(kClipGroups - 1) : "memory");
         uint4* at = ring + g * kClipGroup * 32;
-        uint4 u[kClipGroup];
 #pragma unroll
-        for (int j = 0; j < kClipGroup; ++j) u[j] = at[j * 32];
-#pragma unroll
-        for (int j = 0; j < kClipGroup; ++j) {
-            const int step = k - j, i = step * 32 + lane;
-            if (step >= from && i < q.items) at_vector<T>(p, q, i, [&](const T*, T* out) { f(u[j], out); });
-        }
+        for (int j = 0; j < kClipGroup; ++j)
+            if (k - j >= from) f(k - j, at + j * 32);
         end();
         fetch(k - kClipRing, at);
         if (++g == kClipGroups) g = 0;
     }
 }
 
-template <typename T>
-__device__ __forceinline__ void sum_vector(const uint4& u, Squares& sum) {
-    float2 v[Of<T>::V / 2];
-    Of<T>::get(u, v);
+// Vector i of a piece
+template <class Q>
+__device__ __forceinline__ void sum_vector(const Piece& p, const Q& q, int i, const uint4& u, Squares& sum) {
+    constexpr int V = Q::V;
+    if (i >= q.items) return;
+    float2 v[V / 2];
+    Of<typename Q::T>::get(u, v);
+    if constexpr (Q::kSpan) {
+        // values of the gaps, of the row's and beside the piece
+        const int e = i * V - q.before, ld = (int)p.ld_in, end = (p.rows - 1) * ld + p.cols;
+        int c = e < 0 ? e : (int)((uint32_t)e % (uint32_t)ld);
+        if (e < 0 || e + V > end || c + V > p.cols) {
 #pragma unroll
-    for (int j = 0; j < Of<T>::V / 2; ++j) sum.add(v[j]);
+            for (int j = 0; j < V; ++j, ++c) {
+                if (c >= ld) c = 0;
+                float& x = j & 1 ? v[j >> 1].y : v[j >> 1].x;
+                x = c >= 0 && c < p.cols && e + j < end ? x : 0.0f;
+            }
+        }
+    }
+#pragma unroll
+    for (int j = 0; j < V / 2; ++j) sum.add(v[j]);
 }
 
 // Squares of what is not kept of a piece
-template <typename T>
+template <class Q>
 __device__ __forceinline__ int sum_piece(const Piece& p, int lane, uint4* ring, int keep, int slot, Squares& sum) {
-    const Parts<T> q(p);
+    const Q q(p);
     const int steps = q.steps(), from = max(0, keep - slot);
-    if (steps > from) stream_piece<T>(p, q, lane, ring, from, [&](const uint4& u, T*) { sum_vector<T>(u, sum); }, [&] { sum.end_run(); });
-    singles<T>(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); });
+    if (steps > from)
+        stream_piece(p, q, lane, ring, from, [&](int step, uint4* at) { sum_vector(p, q, step * 32 + lane, *at, sum); },
+                        [&] { sum.end_run(); });
+    using T = typename Q::T;
+    singles(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); });
+    sum.end_run();
     return steps;
 }
 
 // and of what is
-template <typename T>
+template <class Q>
 __device__ __forceinline__ int sum_kept(const Piece& p, int lane, const uint4* kept, int keep, int slot, Squares& sum) {
-    const Parts<T> q(p);
+    const Q q(p);
     const int steps = q.steps(), n = min(steps, keep - slot);
 #pragma unroll 4
-    for (int k = 0; k < n; ++k)
-        if (k * 32 + lane < q.items) sum_vector<T>(kept[(slot + k) * 32], sum);
+    for (int k = 0; k < n; ++k) sum_vector(p, q, k * 32 + lane, kept[(slot + k) * 32], sum);
     return steps;
 }
 
-// A piece scaled, its last vectors first; `slot` as above
 template <typename T>
-__device__ __forceinline__ void scale_piece(const Piece& p, int lane, const uint4* kept, uint4* ring, int keep, int slot, float f) {
-    const Parts<T> q(p);
-    singles<T>(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); });
-    const float2 f2 = pair(f);
-    const auto one = [&](uint4 u, T* out) {
-        if (f != 1.0f) {
-            float2 v[Of<T>::V / 2];
-            Of<T>::get(u, v);
+__device__ __forceinline__ uint4 scaled(uint4 u, float f) {
+    if (f == 1.0f) return u;
+    float2 v[Of<T>::V / 2];
+    Of<T>::get(u, v);
 #pragma unroll
-            for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(v[j], f2);
-            u = Of<T>::put(v);
-        }
-        *reinterpret_cast<uint4*>(out) = u;
-    };
+    for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(v[j], pair(f));
+    return Of<T>::put(v);
+}
+
+// A step of a span: its 32 vectors, scaled, lie one after another at the lanes' places, and go out a value a lane, in
+// their order.
+template <class Q>
+__device__ __forceinline__ void store_span(const Piece& p, const Q& q, int lane, int step, uint4* at, float f) {
+    using T = typename Q::T;
+    constexpr int E = 32 * Q::V;
+    if (step * 32 + lane < q.items) *at = scaled<T>(*at, f);
+    __syncwarp();
+    const T* from = reinterpret_cast<const T*>(at - lane) + lane;
+    const int ld = (int)p.ld_in, end = (p.rows - 1) * ld + p.cols;
+    int e = step * E - q.before + lane;
+    int row = e > 0 ? (uint32_t)e / (uint32_t)ld : 0, c = e - row * ld;
+    T* to = static_cast<T*>(p.out) + row * p.ld_out + c;
+#pragma unroll
+    for (int k = 0; k < E; k += 32) {
+        if (c >= 0 && c < p.cols && e < end) *to = from[k];
+        e += 32, c += 32, to += 32;
+        while (c >= ld) c -= ld, to += p.ld_out - ld;
+    }
+    __syncwarp();
+}
+
+// A piece scaled, its last vectors first; `slot` as above
+template <class Q>
+__device__ __forceinline__ void scale_piece(const Piece& p, int lane, uint4* kept, uint4* ring, int keep, int slot, float f) {
+    const Q q(p);
+    using T = typename Q::T;
+    singles(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); });
     const int steps = q.steps(), left = min(steps, max(0, keep - slot));         // steps that are kept
-    if (steps > left) stream_piece<T>(p, q, lane, ring, left, one, [] {});
+    if constexpr (Q::kSpan) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncwarp();
+        if (steps > left)
+            stream_piece(p, q, lane, ring, left, [&](int step, uint4* at) { store_span(p, q, lane, step, at, f); }, [] {});
+        for (int k = 0; k < left; ++k) store_span(p, q, lane, k, kept + (slot + k) * 32, f);
+    } else {
+        const auto one = [&](int step, const uint4* at) {
+            const int i = step * 32 + lane;
+            if (i < q.items) *q.out(p, i) = scaled<T>(*at, f);
+        };
+        if (steps > left) stream_piece(p, q, lane, ring, left, one, [] {});
 #pragma unroll 4
-    for (int k = 0; k < left; ++k) {
-        const int i = k * 32 + lane;
-        if (i < q.items) at_vector<T>(p, q, i, [&](const T*, T* out) { one(kept[(slot + k) * 32], out); });
+        for (int k = 0; k < left; ++k) one(k, kept + (slot + k) * 32);
     }
 }
 
-// f(type's value) for a piece's type
+// f(the piece's kind of Parts)
+template <class Q>
+struct Kind {
+    using type = Q;
+};
 template <class F>
-__device__ __forceinline__ int with_type(int type, F&& f) {
-    if (type == NITRO_BF16) return f((uint16_t)0);
-    if (type == NITRO_F32) return f(0.0f);
-    return f((int64_t)0);
+__device__ __forceinline__ int with_kind(const Piece& p, F&& f) {
+    const bool span = p.how == kSpan;
+    if (p.type == NITRO_BF16) return span ? f(Kind<Parts<uint16_t, true>>()) : f(Kind<Parts<uint16_t, false>>());
+    if (p.type == NITRO_F32) return span ? f(Kind<Parts<float, true>>()) : f(Kind<Parts<float, false>>());
+    return span ? f(Kind<Parts<int64_t, true>>()) : f(Kind<Parts<int64_t, false>>());
 }
 
 // What a CTA hands to the others: two numbers and the turn that they belong to, as one access of 16 bytes
@@ -342,20 +410,20 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
     int slot = 0;
     for (int i = 0; i < work.n && slot < keep; ++i) {
         const Piece p = piece(i);
-        slot += with_type(p.type, [&](auto t) { return keep_piece<decltype(t)>(p, lane, kept, keep, slot); });
+        slot += with_kind(p, [&](auto t) { return keep_piece<typename decltype(t)::type>(p, lane, kept, keep, slot); });
     }
     Squares q;
     slot = 0;
     for (int i = 0; i < work.n; ++i) {
         const Piece p = piece(i);
-        slot += with_type(p.type, [&](auto t) { return sum_piece<decltype(t)>(p, lane, ring, keep, slot, q); });
+        slot += with_kind(p, [&](auto t) { return sum_piece<typename decltype(t)::type>(p, lane, ring, keep, slot, q); });
     }
     const int end = slot;
     asm volatile("cp.async.wait_all;" ::: "memory");
     slot = 0;
     for (int i = 0; i < work.n && slot < keep; ++i) {
         const Piece p = piece(i);
-        slot += with_type(p.type, [&](auto t) { return sum_kept<decltype(t)>(p, lane, kept, keep, slot, q); });
+        slot += with_kind(p, [&](auto t) { return sum_kept<typename decltype(t)::type>(p, lane, kept, keep, slot, q); });
     }
     {
         q.end_run();
@@ -427,11 +495,11 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
     slot = end;
     for (int i = work.n - 1; i >= 0; --i) {
         const Piece p = piece(i);
-        with_type(p.type, [&](auto t) {
-            using T = decltype(t);
-            slot -= Parts<T>(p).steps();
-            if constexpr (sizeof(T) < 8)
-                if (p.out && !(f == 1.0f && p.out == p.in)) scale_piece<T>(p, lane, kept, ring, keep, slot, f);
+        with_kind(p, [&](auto t) {
+            using Q = typename decltype(t)::type;
+            slot -= Q(p).steps();
+            if constexpr (sizeof(typename Q::T) < 8)
+                if (p.out && !(f == 1.0f && p.out == p.in)) scale_piece<Q>(p, lane, kept, ring, keep, slot, f);
             return 0;
         });
     }
@@ -478,6 +546,26 @@ namespace {
 // Bytes that a piece costs beside its own: its description, and a step that it does not fill
 constexpr int64_t kPieceCost = 512;
 constexpr int64_t kLine = 512;       // a warp's vectors
+constexpr int64_t kSpanGap = 64;     // bytes between rows that are read over
+
+// A matrix as its pieces are made of it: without gaps it is one row
+struct Whole {
+    int64_t rows, cols, ld_in, ld_out;
+    int size, how;
+    int64_t pitch;           // bytes that a row costs
+    explicit Whole(const nitro_clip_matrix& m) : rows(m.rows), cols(m.cols), ld_in(m.ld_in), ld_out(m.ld_out), size(value_size(m.type)) {
+        if (rows == 1 || (ld_in == cols && (!m.out || ld_out == cols))) {
+            cols *= rows;
+            rows = 1;
+        }
+        const bool aligned = ((uintptr_t)m.in | (uintptr_t)m.out) % 16 == 0 &&
+                             (rows == 1 || (ld_in * size % 16 == 0 && (!m.out || ld_out * size % 16 == 0)));
+        const bool span = rows == 1 || ((ld_in - cols) * size <= kSpanGap && ld_in < (1 << 28));
+        how = aligned ? kRows : span ? kSpan : kSingles;
+        pitch = (rows > 1 && how == kSpan ? ld_in : cols) * size;
+    }
+    int64_t cost() const { return rows > 0 && cols > 0 ? kPieceCost + rows * pitch : 0; }
+};
 
 // All matrices as pieces, one warp's after another's: `share` of their cost to each.  to, first: null to count
 // last: the cost that was left for the last warp
@@ -491,35 +579,24 @@ int64_t cut(const nitro_clip_matrix* list, int count, int64_t share, Piece* to, 
         if (first && w <= warps) first[w] = (int)n;
     };
     for (int i = 0; i < count; ++i) {
-        nitro_clip_matrix m = list[i];
+        const Whole m(list[i]);
         if (m.rows == 0 || m.cols == 0) continue;
-        const int size = value_size(m.type);
-        if (m.rows == 1 || (m.ld_in == m.cols && (!m.out || m.ld_out == m.cols))) {
-            m.cols *= m.rows;
-            m.rows = 1;
-        }
-        const bool aligned = ((uintptr_t)m.in | (uintptr_t)m.out) % 16 == 0 &&
-                             (m.rows == 1 || (m.ld_in * size % 16 == 0 && (!m.out || m.ld_out * size % 16 == 0)));
-        const int64_t wide = m.cols * size;
-        for (int64_t r = 0, c = 0; r < m.rows; ++n) {
+        for (int64_t r = 0, c = 0; r < m.rows;) {
             // rows that are still the warp's; of rows longer than its share, whole lines; the last warp takes all that is left
             const int64_t most = std::min<int64_t>(w + 1 < warps ? std::max(share - used - kPieceCost, kLine) : (int64_t)1 << 30, (int64_t)1 << 30);
             int64_t rows = 1, cols = m.cols - c;
-            if (c == 0 && wide <= std::max(most, 4 * kLine)) rows = std::min(m.rows - r, std::max<int64_t>(1, most / wide));
-            else cols = std::min(cols, most / kLine * kLine / size);
+            if (c == 0 && m.pitch <= std::max(most, 4 * kLine)) rows = std::min(m.rows - r, std::max<int64_t>(1, most / m.pitch));
+            else cols = std::min(cols, most / kLine * kLine / m.size);
             if (to) {
-                const char* in = static_cast<const char*>(m.in) + (r * m.ld_in + c) * size;
-                char* out = m.out ? static_cast<char*>(m.out) + (r * m.ld_out + c) * size : nullptr;
-                to[n] = {in, out, m.ld_in, m.ld_out, (int)rows, (int)cols, m.type, aligned};
+                const char* in = static_cast<const char*>(list[i].in) + (r * m.ld_in + c) * m.size;
+                char* out = list[i].out ? static_cast<char*>(list[i].out) + (r * m.ld_out + c) * m.size : nullptr;
+                to[n] = {in, out, rows > 1 ? m.ld_in : cols, rows > 1 ? m.ld_out : cols, (int)rows, (int)cols, list[i].type, m.how};
             }
-            used += kPieceCost + rows * cols * size;
+            ++n;
+            used += kPieceCost + (rows > 1 ? rows * m.pitch : cols * m.size);
             c += cols;
             if (c == m.cols) c = 0, r += rows;
-            if (used + kPieceCost + kLine > share && w + 1 < warps) {
-                ++n;
-                next_warp();
-                --n;
-            }
+            if (used + kPieceCost + kLine > share && w + 1 < warps) next_warp();
         }
     }
     *last = w + 1 == warps ? used : 0;
@@ -585,10 +662,7 @@ nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** 
     if (!clip_list_ok(list, count, &bytes) || !outs_apart(list, count)) return NITRO_ERR_ARG;
     // an SM's worth of threads takes 16 KB at once: fewer CTAs where there is less, and a cheaper barrier
     int64_t cost = 0;
-    for (int i = 0; i < count; ++i) {
-        const nitro_clip_matrix& m = list[i];
-        if (m.rows > 0 && m.cols > 0) cost += kPieceCost + m.rows * m.cols * value_size(m.type);
-    }
+    for (int i = 0; i < count; ++i) cost += Whole(list[i]).cost();
     const int ctas = (int)std::max<int64_t>(1, std::min<int64_t>(sm_count(), (cost + 16383) / 16384)), warps = ctas * kClipWarps;
     // (matrices that end inside a share, and rows, leave the others more than the mean)
     int64_t share = std::max<int64_t>((cost + warps - 1) / warps + kLine, 2 * kPieceCost), last = 0, n = 0;
@@ -614,7 +688,8 @@ nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** 
         int64_t steps = 0;
         for (int i = first[w]; i < first[w + 1]; ++i) {
             const Piece& p = host[i];
-            if (p.vec) steps += ((int64_t)p.rows * (p.cols * value_size(p.type) / 16) + 31) / 32;
+            const int64_t size = value_size(p.type), row = p.cols * size / 16, span = ((p.rows - 1) * p.ld_in + p.cols) * size / 16 + 2;
+            if (p.how != kSingles) steps += ((p.how == kRows ? p.rows * row : span) + 31) / 32;
         }
         most_steps = std::max(most_steps, steps);
     }

@@ -83,7 +83,8 @@ def test_some_are_counted_and_not_written():
 
 
 @pytest.mark.parametrize("t", [BF, F32])
-@pytest.mark.parametrize("rows, cols, ld", [(40, 33, 40), (5, 5000, 5003), (3000, 3, 8), (9, 64, 72), (1, 7, 9), (700, 1, 5)])
+@pytest.mark.parametrize("rows, cols, ld", [(40, 33, 40), (5, 5000, 5003), (3000, 3, 8), (9, 64, 72), (1, 7, 9), (700, 1, 5), (2000, 1000, 1003), (3, 400001, 400009),
+                                            (50000, 7, 9), (300, 129, 1000), (20000, 5, 6), (777, 2048, 2049)])
 def test_matrices_in_wider_buffers(rows, cols, ld, t):
     src, dst = grads([((rows, ld), t), ((rows, ld + 3), t)], seed=rows)
     keep = dst.clone()
@@ -91,6 +92,13 @@ def test_matrices_in_wider_buffers(rows, cols, ld, t):
     check([src[:, 1: 1 + cols]], outs, norm, 0.5)
     keep[:, 2: 2 + cols] = dst[:, 2: 2 + cols]
     assert torch.equal(keep, dst)          # what lies between the rows stays as it was
+    # in place, and into one without gaps
+    place, flat = src.clone(), torch.empty(rows, cols, dtype=t, device="cuda")
+    run([place[:, 1: 1 + cols]], 0.5, [place[:, 1: 1 + cols]])
+    run([src[:, 1: 1 + cols]], 0.5, [flat])
+    assert torch.equal(place[:, 1: 1 + cols], outs[0]) and torch.equal(flat, outs[0])
+    place[:, 1: 1 + cols] = src[:, 1: 1 + cols]
+    assert torch.equal(place, src)
 
 
 def test_columns_of_one_buffer():
