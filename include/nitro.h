@@ -475,12 +475,12 @@ typedef enum { NITRO_ACT_NONE = 0, NITRO_ACT_RELU = 1, NITRO_ACT_SILU = 2, NITRO
  * y may be x itself where type and strides are the same, and must not overlap it otherwise.
  * backward, from mean and rstd of a forward on the same inputs and dy (NITRO_BF16 or NITRO_F32, y_type, as is dx):
  * dx, dgamma and dbeta (fp32 [channels], summed over samples and pixels, overwritten); any may be NULL.
- * dx may be dy itself likewise, but not x.
+ * dx may be dy itself likewise, but not x.  No other output may overlap an input.
  * Statistics and sums are in 32 bits or more, in an order that the sizes fix.  With samples = 0 dgamma and dbeta are
  * cleared.  Errors: NITRO_ERR_ARG for null handles or pointers, samples outside [0, max_samples],
  * pixels outside [1, max_pixels], strides below the sizes (stride_x below pixels ldx with more than one sample), eps
  * that is not above 0 and finite, another type or activation; at create sizes below 1,
- * channels above 8192 or not a multiple of groups, more than 2^31 - 1 pixels, more than 65535 samples, or
+ * channels above 8192 or not a multiple of groups, more than 2^30 pixels, more than 65535 samples, or
  * more than 2^38 values. */
 typedef struct nitro_gnorm nitro_gnorm;
 nitro_status nitro_gnorm_create(int max_samples, int max_pixels, int channels, int groups, nitro_gnorm** out);

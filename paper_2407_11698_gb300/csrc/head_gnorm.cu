@@ -186,6 +186,16 @@ struct Sums {
 #pragma unroll
         for (int j = 0; j < N; ++j) k[j] = sum[j] = sq[j] = pair(0.0f);
     }
+    // a run's sums to these: long ones go by runs, as squares far below a sum's last place are lost
+    // more often than they are rounded up
+    __device__ __forceinline__ void take(Sums& run) {
+#pragma unroll
+        for (int j = 0; j < N; ++j) {
+            sum[j] = add2(sum[j], run.sum[j]);
+            sq[j] = add2(sq[j], run.sq[j]);
+            run.sum[j] = run.sq[j] = pair(0.0f);
+        }
+    }
     __device__ __forceinline__ void add(const float2* v) {
 #pragma unroll
         for (int j = 0; j < N; ++j) {
@@ -344,19 +354,23 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
     for (int slab = 0; slab < s.slabs; ++slab) {
         const int c = at.channel<V>(s, slab);
         if (c >= 0) {
-            Sums<V> t;
+            Sums<V> t, run;
             const X* src = x + (int64_t)(p0 + at.row) * ldx + c;
             if (at.row < np) Vals<X, V>::load(src, t.k);
+#pragma unroll
+            for (int j = 0; j < t.N; ++j) run.k[j] = t.k[j];
             const int64_t step = s.rows * ldx;
             const int n = at.steps(s, np);
             uint8_t* slot = SX::first(data);
             through_ring(
                 n, [&](int i, int k) { SX::fetch(slot + k * SX::STEP, src + i * step); },
-                [&](int, int k) {
+                [&](int i, int k) {
                     float2 v[Sums<V>::N];
                     SX::get(slot + k * SX::STEP, v);
-                    t.add(v);
+                    run.add(v);
+                    if ((i & 31) == 31) t.take(run);
                 });
+            t.take(run);
             t.finish((float)n, at.group(s, c), s.per % V == 0, origin);      // 0 for rows past the chunk
 #pragma unroll
             for (int j = 0; j < V; ++j) {
@@ -1134,7 +1148,7 @@ extern "C" {
 nitro_status nitro_gnorm_create(int max_samples, int max_pixels, int channels, int groups, nitro_gnorm** out) {
     if (!out) return NITRO_ERR_ARG;
     *out = nullptr;
-    if (max_samples < 1 || max_pixels < 1 || channels < 1 || groups < 1 || max_samples > 65535 || channels > kGnChannels ||
+    if (max_samples < 1 || max_pixels < 1 || channels < 1 || groups < 1 || max_samples > 65535 || max_pixels > (1 << 30) || channels > kGnChannels ||
         channels % groups != 0 || (int64_t)max_pixels * channels > ((int64_t)1 << 38) / max_samples)
         return NITRO_ERR_ARG;
     nitro_gnorm* h = new (std::nothrow) nitro_gnorm();
@@ -1267,8 +1281,7 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
                         return launch_cluster(k_gn_one_back<X, Y, V>, dim3(one.slabs * one.ks, n), kGnThreads, one.ks, s, smem,
                                               sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0), lddy, stride_dy, one,
                                               mean + (int64_t)s0 * h->groups, rstd + (int64_t)s0 * h->groups,
-                                              dgamma || dbeta ? h->part_c : nullptr,
-                                              dx ? const_cast<Y*>(sample_at<Y>(mdx, s0)) : nullptr, lddx, stride_dx);
+                                              dgamma || dbeta ? h->part_c : nullptr, dx ? const_cast<Y*>(sample_at<Y>(mdx, s0)) : nullptr, lddx, stride_dx);
                     });
                 });
             }));

@@ -23,7 +23,7 @@ def _create(fn, *shape):
 
 
 @pytest.mark.parametrize("shape", [(0, 8, 8, 2), (8, 0, 8, 2), (8, 8, 0, 1), (8, 8, 8, 0), (8, 8, 8, 3), (65536, 8, 8, 2), (8, 8, 8193, 1),
-                                   (8, 8, 2, 4), (1, (1 << 31) - 1, 8192, 1), (65535, 1 << 20, 8192, 1)])
+                                   (8, 8, 2, 4), (1, (1 << 30) + 1, 8, 1), (1, 1 << 30, 8192, 1), (65535, 1 << 20, 8192, 1)])
 def test_gnorm_sizes_refused(lib, shape):
     assert _create(lib.nitro_gnorm_create, *shape) == (A, None)
 
