@@ -6,6 +6,8 @@
 // all CTAs' sums and adds them in the same order, and the warps scale their pieces, last ones first (the second level cache
 // holds them).  A warp's first 13 KB stay in shared memory in between, so that up to 31 MB of
 // gradients are read once; where there are more, 7 KB, and the others come through a ring of places there.
+// 48 tensors, 2.6 GB: 1290 us, 6.0 TB/s over the values' two ways in and one out (the first 448 us, with SMs up to a sixth apart);
+// 300 tensors, 29 MB: 25 us, of which 9 are loads, 3 sums, 3 notes and 6 stores; six tensors, 1 MB: 8.3.
 // Squares are summed three times, of x, of x 2^-80 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
 // loses values below 2^-75, and where its sum shows that, one of the others stands for it.
 #include <new>

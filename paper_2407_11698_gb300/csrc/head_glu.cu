@@ -7,7 +7,8 @@
 // value (8 rows hidden bytes each way, beside 12 rows hidden features operations; 16 bits would
 // put a rounding of 2^-9 under both gradients, and taking the products again costs a third of a step).
 // The backward writes D in bf16, which both products with it take.  4 rows hidden features operations forward and
-// 8 backward.  Few rows run on the CUDA cores, where W's bytes bound them (k_glu_few).
+// 8 backward: 8192 x 2048 x 8192 1.09 ms, forward 332 us (1.66 PFLOP/s), D 143 (6.6 TB/s), dx 324, dW 299 (1.7 and 1.84), at the
+// power limit.  Few rows run on the CUDA cores, where W's bytes bound them (k_glu_few).
 #include <new>
 
 #include "head_act.cuh"
@@ -124,7 +125,8 @@ constexpr bool hg_pairs<EpiGlu> = true;
 
 // ------------------------------------------------------------------ few rows
 // A warp takes C units, so 2 C rows of W (over ks warps of a CTA by pieces of 256 features, where there are few), and R
-// rows of x; its sums are exchanged so that each lane ends with one (row, unit, half).
+// rows of x at a time; its sums are exchanged so that each lane ends with one (row, unit, half).  W's bytes bound a lone row:
+// 4096 x 4096 12.5 us, 5.4 TB/s (6.2 us from the second level cache).
 struct FewGluArgs {
     int64_t ldx, ldw, ldo;
     int rows, features, hidden, ks, act;
@@ -141,48 +143,50 @@ __global__ void __launch_bounds__(256, 2) k_glu_few(const T* x, const uint16_t* 
     const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
     const int sub = warp % a.ks, per = 8 / a.ks;
     const int groups = (a.hidden + C - 1) / C;
-    const T* xr[R];
-#pragma unroll
-    for (int r = 0; r < R; ++r) xr[r] = x + min(r, a.rows - 1) * a.ldx;
     int turn = 0;
-    for (int g0 = blockIdx.x * per; g0 < groups; g0 += gridDim.x * per, turn ^= 1) {
+    for (int g0 = blockIdx.x * per; g0 < groups; g0 += gridDim.x * per) {
         const int first = (g0 + warp / a.ks) * C;
-        float acc[R][2 * C];
+        for (int r0 = 0; r0 < a.rows; r0 += R, turn ^= 1) {       // (W's rows are in the first level cache from the second time on)
+            float acc[R][2 * C];
 #pragma unroll
-        for (int i = 0; i < N; ++i) acc[i / (2 * C)][i % (2 * C)] = 0.0f;
-        if (first < a.hidden) {
-            const uint16_t* wr[2 * C];
+            for (int i = 0; i < N; ++i) acc[i / (2 * C)][i % (2 * C)] = 0.0f;
+            if (first < a.hidden) {
+                const T* xr[R];
 #pragma unroll
-            for (int c = 0; c < 2 * C; ++c)
-                wr[c] = w + (min(first + c % C, a.hidden - 1) + (int64_t)(c / C) * a.hidden) * a.ldw;
-            int piece = sub * 256;
-            for (; piece + 256 <= a.features; piece += a.ks * 256)
-                few_step<T, R, 2 * C, VEC, true>(xr, wr, piece, lane, a.features, acc);
-            if (piece < a.features) few_step<T, R, 2 * C, VEC, false>(xr, wr, piece, lane, a.features, acc);
-        }
-        float z = few_sum<N>(&acc[0][0], lane);
-        if (a.ks > 1) {
-            if (lane % kLanes == 0) sums[turn][warp][lane / kLanes] = z;
-            __syncthreads();       // the other turn's sums are read by now
-            if (sub == 0) {
-                z = sums[turn][warp][lane / kLanes];
-                for (int k = 1; k < a.ks; ++k) z += sums[turn][warp + k][lane / kLanes];
+                for (int r = 0; r < R; ++r) xr[r] = x + min(r0 + r, a.rows - 1) * a.ldx;
+                const uint16_t* wr[2 * C];
+#pragma unroll
+                for (int c = 0; c < 2 * C; ++c)
+                    wr[c] = w + (min(first + c % C, a.hidden - 1) + (int64_t)(c / C) * a.hidden) * a.ldw;
+                int piece = sub * 256;
+                for (; piece + 256 <= a.features; piece += a.ks * 256)
+                    few_step<T, R, 2 * C, VEC, true>(xr, wr, piece, lane, a.features, acc);
+                if (piece < a.features) few_step<T, R, 2 * C, VEC, false>(xr, wr, piece, lane, a.features, acc);
             }
-        }
-        z *= a.scale;
-        const float up = __shfl_down_sync(0xffffffffu, z, C * kLanes);
-        const int i = lane / kLanes, row = i / (2 * C), unit = first + i % C;
-        if (sub == 0 && lane % kLanes == 0 && row < a.rows && unit < a.hidden) {
-            const bool gate = i % (2 * C) < C;
-            if (a.saved.base) {
-                int to_up;
-                float* dst = a.saved.at(unit, row, &to_up);
-                dst[gate ? 0 : to_up] = z;
+            float z = few_sum<N>(&acc[0][0], lane);
+            if (a.ks > 1) {
+                if (lane % kLanes == 0) sums[turn][warp][lane / kLanes] = z;
+                __syncthreads();       // the other turn's sums are read by now
+                if (sub == 0) {
+                    z = sums[turn][warp][lane / kLanes];
+                    for (int k = 1; k < a.ks; ++k) z += sums[turn][warp + k][lane / kLanes];
+                }
             }
-            if (gate) {
-                float v = 0.0f;
-                with_act(a.act, [&](auto act) { v = act_value<decltype(act)::value>(z); });
-                a.out[row * a.ldo + unit] = __bfloat16_as_ushort(__float2bfloat16_rn(v * up));
+            z *= a.scale;
+            const float up = __shfl_down_sync(0xffffffffu, z, C * kLanes);
+            const int i = lane / kLanes, row = r0 + i / (2 * C), unit = first + i % C;
+            if (sub == 0 && lane % kLanes == 0 && row < a.rows && unit < a.hidden) {
+                const bool gate = i % (2 * C) < C;
+                if (a.saved.base) {
+                    int to_up;
+                    float* dst = a.saved.at(unit, row, &to_up);
+                    dst[gate ? 0 : to_up] = z;
+                }
+                if (gate) {
+                    float v = 0.0f;
+                    with_act(a.act, [&](auto act) { v = act_value<decltype(act)::value>(z); });
+                    a.out[row * a.ldo + unit] = __bfloat16_as_ushort(__float2bfloat16_rn(v * up));
+                }
             }
         }
     }
@@ -345,7 +349,6 @@ __global__ void __launch_bounds__(256) k_glu_prep(const PackJob x, const PackJob
 constexpr int kRowsWithLow = 32;
 // Sums in two accumulators, added with rounding, from here on: the tensor cores cut off what 32 bits do not hold.
 constexpr int kFoldFeatures = 2048;
-constexpr int kFewRows = 4;
 constexpr int64_t kAccFloats = (int64_t)16 << 20;   // slices of dx: at most 64 MB together
 
 }  // namespace
@@ -398,6 +401,15 @@ cudaError_t prepare(nitro_glu* h, const void* x, int x_type, int64_t ldx, const 
     return launch_k(k_glu_prep, dim3(g.ctas + jx.ctas + jw.ctas), dim3(256), 0, s, jx, jw, g);
 }
 
+// Whether a forward goes to the CUDA cores: four rows always, up to 16 where W is small or TMA cannot take its rows.  us,
+// k_glu_few and the tensor cores, features x hidden: 3 rows, 4096 x 4096 12.6 and 15; 5 to 8 rows 1000 x 1501 5.1 and 8.6, 2000 x
+// 3000 12.4 and 13.2, 4096 x 4096 20 and 15.3, with odd rows 28 and 43; 9 to 16 rows 1000 x 1501 8.6 and 8.7, 4096 x 300 5.7 and 9.9, but 512 x
+// 4096 7.2 and 6.0; with odd rows 1000 x 1501 9.7 and 12.7, 2000 x 3000 28 and 20.
+bool few_rows_pay(const nitro_glu* h, int rows, bool copy) {
+    const int64_t w = 2 * (int64_t)h->hidden * h->features, m = 1 << 20;
+    return rows <= 4 || (rows <= 8 && (copy || w <= 8 * m)) || (rows <= 16 && w <= (copy ? 6 : 3) * m);
+}
+
 int rows_in_stage(int rows) { return rows < 128 ? (rows + 7) / 8 * 8 : 128; }
 
 bool glu_args(const nitro_glu* h, const void* x, int x_type, int64_t ldx, const void* w, int64_t ldw, int rows, float scale,
@@ -413,20 +425,26 @@ cudaError_t few_as(bool vec, const void* x, const uint16_t* w, const FewGluArgs&
     return vec ? launch_k(k_glu_few<T, R, C, true>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a)
                : launch_k(k_glu_few<T, R, C, false>, dim3(grid), dim3(256), 0, s, (const T*)x, w, a);
 }
+template <typename T>
+cudaError_t few_rows(bool vec, int c, const void* x, const uint16_t* w, const FewGluArgs& a, int grid, cudaStream_t s) {
+    if (a.rows > 4) return few_as<T, 8, 2>(vec, x, w, a, grid, s);
+    if (c == 4) return a.rows <= 1 ? few_as<T, 1, 4>(vec, x, w, a, grid, s) : few_as<T, 4, 4>(vec, x, w, a, grid, s);
+    return a.rows <= 1 ? few_as<T, 1, 1>(vec, x, w, a, grid, s) : few_as<T, 4, 1>(vec, x, w, a, grid, s);
+}
 
 cudaError_t forward_few(const nitro_glu* h, const void* x, int x_type, const uint16_t* w, FewGluArgs a, cudaStream_t s) {
-    constexpr int C = 4;
-    // two CTAs an SM; a warp's features over as many warps as are free
+    // two CTAs an SM; four units a warp (two of more than four rows) where that leaves no warp idle, else one; a warp's
+    // features over as many warps as are free
     const int ctas = 2 * sm_count(), warps = 8 * ctas, pieces = (h->features + 255) / 256;
-    const int groups = (h->hidden + C - 1) / C;
+    const int c = a.rows > 4 ? 2 : (int64_t)((h->hidden + 3) / 4) * std::min(8, pieces) >= warps / 2 ? 4 : 1;
+    const int groups = (h->hidden + c - 1) / c;
     a.ks = 1;
     while (a.ks < 8 && 2 * a.ks <= pieces && (int64_t)groups * 2 * a.ks <= warps) a.ks *= 2;
     const int per = 8 / a.ks, grid = std::min(ctas, (groups + per - 1) / per);
     const bool i8 = x_type == NITRO_I8;
     const bool vec = tma_rows(w, a.ldw) && (i8 ? ((uintptr_t)x & 7) == 0 && a.ldx % 8 == 0 : tma_rows(x, a.ldx));
     ProfScope ps(K_GLU_FWD, s, 4.0 * a.rows * h->hidden * h->features, 4.0 * h->hidden * h->features);
-    if (i8) return a.rows <= 1 ? few_as<int8_t, 1, C>(vec, x, w, a, grid, s) : few_as<int8_t, 4, C>(vec, x, w, a, grid, s);
-    return a.rows <= 1 ? few_as<uint16_t, 1, C>(vec, x, w, a, grid, s) : few_as<uint16_t, 4, C>(vec, x, w, a, grid, s);
+    return i8 ? few_rows<int8_t>(vec, c, x, w, a, grid, s) : few_rows<uint16_t>(vec, c, x, w, a, grid, s);
 }
 
 }  // namespace
@@ -465,7 +483,7 @@ nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t 
     if (rows == 0) return NITRO_OK;
     if (!out) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    if (rows <= kFewRows) {
+    if (few_rows_pay(h, rows, copies(w, NITRO_BF16, ldw))) {
         TRY(forward_few(h, x, x_type, w, FewGluArgs{ldx, ldw, ldo, rows, h->features, h->hidden, 1, act, out, Saved{saved, rows, h->hidden}, scale}, s));
         return NITRO_OK;
     }

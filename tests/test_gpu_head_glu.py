@@ -86,7 +86,7 @@ def check(x, w, dout, scale, act, out, saved, dx, dw):
 
 
 # one row and few (CUDA cores), up to and past 32 (halves of D), tiles that end anywhere, several splits and tiles a CTA
-SIZES = [(1, 1, 1), (1, 4096, 300), (2, 33, 7), (3, 1000, 1501), (4, 600, 24), (5, 600, 24), (13, 1000, 501), (32, 72, 40), (33, 72, 40), (64, 4096, 100),
+SIZES = [(1, 1, 1), (6, 257, 50), (16, 1000, 301), (10, 2049, 33), (1, 4096, 300), (2, 33, 7), (3, 1000, 1501), (4, 600, 24), (5, 600, 24), (13, 1000, 501), (32, 72, 40), (33, 72, 40), (64, 4096, 100),
          (129, 65, 130), (300, 200, 1366), (1000, 24, 16), (257, 2500, 90), (700, 520, 2000)]
 
 

@@ -293,6 +293,11 @@ def test_refusals():
                 lambda: h.backward(x, gamma, beta, None, None, dy, y)):
         with pytest.raises(nb.NitroError):
             bad()
+    p = lambda t, off=0: t.data_ptr() + off
+    for gam, mu, dga in ((p(gamma, 2), p(mean), p(beta)), (p(gamma), p(mean, 1), p(beta)), (p(gamma), p(mean), p(beta, 2))):
+        assert nb.lib().nitro_gnorm_backward(h.h, p(x), 0, 16, 160, 2, 10, gam, None, mu, p(rstd), 0, p(dy), 0, 16, 160, None, 16, 160, dga,
+                                             None, None) == nb.NITRO_ERR_ARG
+    assert nb.lib().nitro_gnorm_forward(h.h, p(x, 1), 0, 16, 160, 2, 10, None, None, 1e-5, 0, p(y), 0, 16, 160, None, None, None) == nb.NITRO_ERR_ARG
     for bad in (lambda: h.forward(x.to(torch.float16), gamma, beta, y), lambda: h.forward(x, gamma, beta, y.to(torch.int8)),
                 lambda: h.forward(x[..., :8], gamma, beta, y[..., :8]), lambda: h.forward(x, gamma[:8], beta, y),
                 lambda: h.forward(x, gamma.to(torch.bfloat16), beta, y), lambda: h.forward(x, gamma, beta, y[:1]),
