@@ -700,15 +700,11 @@ nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** 
     for (int i = 0; i < count; ++i) h->writes = h->writes || (list[i].out && list[i].rows > 0 && list[i].cols > 0);
     const bool ok = h->allocs.take(&h->pieces, std::max<int64_t>(n, 1)) && h->allocs.take(&h->work, warps) &&
                     h->allocs.take(&h->notes, 2 * h->ctas + 1) && h->status.take();
-    // (on a stream of its own: the default one may be busy, or part of a capture)
-    cudaStream_t s = nullptr;
-    bool copied = ok && cudaStreamCreateWithFlags(&s, cudaStreamNonBlocking) == cudaSuccess;
-    if (copied) {
-        copied = (n == 0 || cudaMemcpyAsync(h->pieces, host.data(), sizeof(Piece) * (size_t)n, cudaMemcpyHostToDevice, s) == cudaSuccess) &&
-                 cudaMemcpyAsync(h->work, work.data(), sizeof(Work) * work.size(), cudaMemcpyHostToDevice, s) == cudaSuccess &&
-                 cudaStreamSynchronize(s) == cudaSuccess;
-        cudaStreamDestroy(s);
-    }
+    const cudaStream_t s = cudaStreamPerThread;
+    const bool copied = ok &&
+                        (n == 0 || cudaMemcpyAsync(h->pieces, host.data(), sizeof(Piece) * (size_t)n, cudaMemcpyHostToDevice, s) == cudaSuccess) &&
+                        cudaMemcpyAsync(h->work, work.data(), sizeof(Work) * work.size(), cudaMemcpyHostToDevice, s) == cudaSuccess &&
+                        cudaStreamSynchronize(s) == cudaSuccess;
     if (!copied) {
         nitro_clip_destroy(h);
         return NITRO_ERR_CUDA;

@@ -618,7 +618,7 @@ struct HgProblem {
     bool upper = false, fold = false;
     // few rows of A: a tile's stage gets these (a multiple of 8) and no rows past them, whose sums nobody takes.  128: all
     int rows_a = 128;
-    int eights = 0;            // clusters of eight that run at once, where the caller has asked (hg_eights())
+    int eights = 0;            // clusters of eight that the caller takes at most (hg_eights()); 0: seven eighths of the SMs' worth
     uint32_t* status = nullptr;
     int prof = 0;
     double ops = 0, bytes = 0;
@@ -723,34 +723,9 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
     else return launch_k(kernel, dim3(grid), dim3(kHgThreads), C::SMEM, s, ma, mb, g, ea);
 }
 
-// Clusters of eight CTAs, one an SM, that the device runs at once: as many as its parts hold whole ones (152 SMs
-// do not hold 16 of them: 64 x 2048 x 1024 took 16.6 us with 16 and 7.4 in clusters of four).  0: unknown.
-template <class Epi, bool AMN, bool BMN, bool F16>
-int hg_eights() {
-    static std::atomic<int> known{-1};
-    int n = known.load(std::memory_order_relaxed);
-    if (n >= 0) return n;
-    using C = HgCfg<1, 128, 1, 1>;
-    const auto kernel = k_head_gemm<Epi, 1, 128, AMN, BMN, F16, 1, 1, 8>;
-    cudaLaunchAttribute attr[1];
-    attr[0].id = cudaLaunchAttributeClusterDimension;
-    attr[0].val.clusterDim.x = 8;
-    attr[0].val.clusterDim.y = attr[0].val.clusterDim.z = 1;
-    cudaLaunchConfig_t cfg = {};
-    cfg.gridDim = dim3(8);
-    cfg.blockDim = dim3(kHgThreads);
-    cfg.dynamicSmemBytes = C::SMEM;
-    cfg.attrs = attr;
-    cfg.numAttrs = 1;
-    n = 0;
-    if (cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, C::SMEM) != cudaSuccess ||
-        cudaOccupancyMaxActiveClusters(&n, kernel, &cfg) != cudaSuccess) {
-        cudaGetLastError();
-        n = 0;
-    }
-    known.store(n, std::memory_order_relaxed);
-    return n;
-}
+// Clusters of eight CTAs, one an SM, that surely run at once: half the SMs' worth.  (152 SMs do not hold 16 of them, as their
+// parts hold whole clusters only: 64 x 2048 x 1024 took 16.6 us with 16 and 7.4 in clusters of four; 8 run at once.)
+inline int hg_eights() { return std::max(1, sm_count() / 16); }
 
 // D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K; HA, HB:
 // halves of the operands.

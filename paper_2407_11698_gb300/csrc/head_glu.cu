@@ -496,7 +496,7 @@ nitro_status nitro_glu_forward(nitro_glu* h, const void* x, int x_type, int64_t 
     p.ops = 4.0 * rows * h->hidden * h->features;
     p.fold = h->features > kFoldFeatures;
     p.rows_a = rows_in_stage(rows);
-    p.eights = hg_eights<EpiGlu, false, false, false>();
+    p.eights = hg_eights();
     const EpiGlu::Args ea{out, ldo, Saved{saved, rows, h->hidden}, tma_rows(out, ldo), h->hidden, act, scale};
     TRY((hg_launch<EpiGlu, false, false, false>(hg_pick(p), p, ox, ow, ea, s)));
     return NITRO_OK;
@@ -538,7 +538,7 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
         p.prof = K_GLU_DX;
         p.ops = 4.0 * rows * h->hidden * F;
         p.rows_a = rows_in_stage(rows);
-        p.eights = hg_eights<EpiBf16, false, true, false>();
+        p.eights = hg_eights();
         // in slices along the hidden units where its tiles leave SMs idle
         const int64_t ldc = round_up(F, 32);
         const HgPick t = hg_pick(p, halves, 1, (int)std::max<int64_t>(1, std::min<int64_t>(16, h->acc_floats / (rows * ldc))));
@@ -562,7 +562,7 @@ nitro_status nitro_glu_backward(nitro_glu* h, const void* x, int x_type, int64_t
         p.status = h->status.at;
         p.prof = K_GLU_DW;
         p.ops = 4.0 * rows * h->hidden * F;
-        p.eights = hg_eights<EpiBf16, true, true, false>();
+        p.eights = hg_eights();
         const EpiBf16::Args eb{dw, lddw, tma_rows(dw, lddw), nullptr, 0, scale};
         if (halves == 2) TRY((hg_launch<EpiBf16, true, true, false, 2, 1>(hg_pick(p, 2), p, D, ox, eb, s)));
         else TRY((hg_launch<EpiBf16, true, true, false>(hg_pick(p), p, D, ox, eb, s)));
