@@ -5,8 +5,8 @@
 //   dx = r (t - sum_g t / N - h sum_g (t h) / N).
 //
 // A thread keeps V neighbouring channels and goes along the pixels.  Where a cluster's shared memory holds a slab of a sample, a
-// direction is one launch and one pass over memory (k_gn_one, k_gn_one_back): 128 x 4096 x 256 bf16 with silu 112 us forward,
-// 4.8 TB/s, and 244 backward, 3.3, where a pass for the sums and one for the result took 1092 together.  17 and 29 instructions a
+// direction is one launch and one pass over memory (k_gn_one, k_gn_one_back): 128 x 4096 x 256 bf16 with silu 106 us forward,
+// 5.0 TB/s, and 225 backward, 3.6, where a pass for the sums and one for the result took 1092 together.  Their instructions a
 // value bound them, a third to a half of those the joining of sums, and 24 and 16 warps an SM.  Larger slabs take the
 // two passes, over batches of samples that stay in L2 in between; the last CTA of a sample joins its chunks' sums.
 //
@@ -53,6 +53,7 @@ struct GnShape {
     int chunk, chunks;                   // pixels of a CTA, CTAs of a sample
     int vecs, slabs, rows;               // vectors of a pixel that a CTA takes at once, how often, pixels at once
     int act;
+    int whole;                           // what is written starts at multiples of a vector
     const float* gamma;                  // or null
     const float* beta;                   // or null
 };
@@ -99,10 +100,10 @@ __device__ __forceinline__ bool gn_last(uint32_t* ticket, int chunks, int* word)
 }
 
 // mean and rstd of a sample's groups.  Dynamic shared memory: the ring, two values a channel.
-template <typename X, int V>
+template <typename X, int V, bool W>
 __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx, int64_t sx, const GnShape s, float eps, float2* parts,
                                                          uint32_t* ticket, float* mean, float* rstd) {
-    using SX = Slots<X, V>;
+    using SX = Slots<X, V, W>;
     extern __shared__ __align__(16) uint8_t data[];
     float* chan = reinterpret_cast<float*>(data + kRing * SX::STEP);      // [channels] means, [channels] squared distances
     __shared__ float red[2][kGnThreads * V];          // [rows][slab's channels]
@@ -122,7 +123,18 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
         if (c >= 0) {
             Sums<V> t, run;
             const X* src = x + (int64_t)(p0 + at.row) * ldx + c;
-            if (at.row < np) Vals<X, V>::load(src, t.k);
+            if (at.row < np) {
+                if constexpr (W) {
+#pragma unroll
+                    for (int j = 0; j < V; ++j) {
+                        float2 one;
+                        Vals<X, 1>::load(src + j, &one);
+                        at2(t.k, j) = one.x;
+                    }
+                } else {
+                    Vals<X, V>::load(src, t.k);
+                }
+            }
 #pragma unroll
             for (int j = 0; j < t.N; ++j) run.k[j] = t.k[j];
             const int64_t step = s.rows * ldx;
@@ -132,7 +144,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
                 n, [&](int i, int k) { SX::fetch(slot + k * SX::STEP, src + i * step); },
                 [&](int i, int k) {
                     float2 v[Sums<V>::N];
-                    SX::get(slot + k * SX::STEP, v);
+                    SX::get(slot + k * SX::STEP, v, low_bits(src + i * step));
                     run.add(v);
                     if ((i & 31) == 31) t.take(run);
                 });
@@ -180,10 +192,10 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
     }
 }
 
-template <typename X, typename Y, int V>
+template <typename X, typename Y, int V, bool W>
 __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx, int64_t sx, const GnShape s, const float* mean,
                                                          const float* rstd, Y* y, int64_t ldy, int64_t sy) {
-    using SX = Slots<X, V>;
+    using SX = Slots<X, V, W>;
     extern __shared__ __align__(16) uint8_t data[];
     pdl_wait();
     const int sample = blockIdx.y, p0 = blockIdx.x * s.chunk, p1 = min(s.pixels, p0 + s.chunk), np = p1 - p0;
@@ -205,9 +217,9 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
                 at.steps(s, np), [&](int i, int k) { SX::fetch(slot + k * SX::STEP, src + i * xs); },
                 [&](int i, int k) {
                     float2 v[ch.N];
-                    SX::get(slot + k * SX::STEP, v);
+                    SX::get(slot + k * SX::STEP, v, low_bits(src + i * xs));
                     ch.template apply<decltype(act)::value>(v);
-                    Vals<Y, V>::store(dst + i * ys, v);
+                    store_row<Y, V, W>(dst + i * ys, v, s.whole);
                 });
         });
     }
@@ -215,12 +227,12 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_apply(const X* x, int64_t ldx
 
 // Sums over a chunk: of du and du h for each channel (part_c [sample][chunk][2][channels]), and over a sample's
 // groups of gamma du and gamma du h, divided by their count (means [sample][groups]).
-template <typename X, typename Y, int V>
+template <typename X, typename Y, int V, bool W>
 __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                            const GnShape s, const float* mean, const float* rstd, float* part_c,
                                                            float2* parts, uint32_t* ticket, float2* means) {
-    using SX = Slots<X, V>;
-    using SY = Slots<Y, V>;
+    using SX = Slots<X, V, W>;
+    using SY = Slots<Y, V, W>;
     extern __shared__ __align__(16) uint8_t data[];
     uint8_t *xslot = SX::first(data), *gslot = SY::first(data + kRing * SX::STEP);
     __shared__ float red[2][kGnThreads * V];
@@ -249,10 +261,10 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X*
                         SX::fetch(xslot + k * SX::STEP, src + i * xs);
                         SY::fetch(gslot + k * SY::STEP, grad + i * gs);
                     },
-                    [&](int, int k) {
+                    [&](int i, int k) {
                         float2 v[ch.N], g[ch.N];
-                        SX::get(xslot + k * SX::STEP, v);
-                        SY::get(gslot + k * SY::STEP, g);
+                        SX::get(xslot + k * SX::STEP, v, low_bits(src + i * xs));
+                        SY::get(gslot + k * SY::STEP, g, low_bits(grad + i * gs));
                         ch.template slopes<decltype(act)::value>(v, g);
 #pragma unroll
                         for (int j = 0; j < ch.N; ++j) {
@@ -308,12 +320,12 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X*
     }
 }
 
-template <typename X, typename Y, int V>
+template <typename X, typename Y, int V, bool W>
 __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_dx(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                          const GnShape s, const float* mean, const float* rstd, const float2* means,
                                                          Y* dx, int64_t lddx, int64_t sdx) {
-    using SX = Slots<X, V>;
-    using SY = Slots<Y, V>;
+    using SX = Slots<X, V, W>;
+    using SY = Slots<Y, V, W>;
     extern __shared__ __align__(16) uint8_t data[];
     uint8_t *xslot = SX::first(data), *gslot = SY::first(data + kRing * SX::STEP);
     pdl_wait();
@@ -349,13 +361,13 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_dx(const X* x
                 },
                 [&](int i, int k) {
                     float2 v[ch.N], h[ch.N], g[ch.N];
-                    SX::get(xslot + k * SX::STEP, v);
-                    SY::get(gslot + k * SY::STEP, g);
+                    SX::get(xslot + k * SX::STEP, v, low_bits(src + i * xs));
+                    SY::get(gslot + k * SY::STEP, g, low_bits(grad + i * gs));
 #pragma unroll
                     for (int j = 0; j < ch.N; ++j) h[j] = v[j];
                     ch.template slopes<decltype(act)::value>(h, g);
                     to.dx(v, g);
-                    Vals<Y, V>::store(dst + i * ds, v);
+                    store_row<Y, V, W>(dst + i * ds, v, s.whole);
                 });
         });
     }
@@ -422,13 +434,28 @@ GnShape shape(const nitro_gnorm* h, int pixels, int samples, int v, int resident
     return s;
 }
 
-int pick_v(const nitro_gnorm* h, int samples, std::initializer_list<Map> maps) {
-    for (int v : {8, 4}) {
-        bool ok = h->channels % v == 0;
-        for (const Map& m : maps) ok = ok && m.aligned(v, samples);
-        if (ok) return v;
-    }
-    return 1;
+// in: what is read, out: what is written; whole: whether that starts at multiples of a vector.  Rows that start anywhere are
+// copied by words, in vectors of eight values, of four where some are fp32 (lanes' words are nearer to each other): 64 x 1024 x 256, rows
+// 259 apart, forward and backward 62 us with int8 x, 80 with bf16, 118 with fp32 (the other width 66, 77, 144; two samples of
+// 100000 x 96: 86, 94, 174 against 105, 112, 181), where single values take 150, 150 and 134, and aligned rows 52, 52 and
+// 114.  Aligned vectors of four come before words of eight: rows 260 apart 57, 74 and 113 us against 60, 79 and 113.
+Width pick_v(const nitro_gnorm* h, int samples, std::initializer_list<Map> in, std::initializer_list<Map> out, int* whole) {
+    const auto aligned = [&](std::initializer_list<Map> maps, int v) {
+        for (const Map& m : maps)
+            if (!m.aligned(v, samples)) return false;
+        return true;
+    };
+    *whole = 1;
+    const int C = h->channels;
+    for (int v : {8, 4})
+        if (C % v == 0 && aligned(in, v) && aligned(out, v)) return {v, false};
+    if (C % 4 != 0) return {1, false};
+    bool wide = false;
+    for (const auto& maps : {in, out})
+        for (const Map& m : maps) wide = wide || m.type == NITRO_F32;
+    const int v = wide || C % 8 != 0 ? 4 : 8;
+    *whole = aligned(out, v);
+    return {v, true};
 }
 
 bool gn_args(const nitro_gnorm* h, const Map& x, int samples, int pixels, int act) {
@@ -449,10 +476,16 @@ int batch_size(const nitro_gnorm* h, int pixels, int bytes_a_value) {
     return (int)std::max<int64_t>(1, std::min<int64_t>(n, h->batch));
 }
 
-// How a call runs in one pass, or ks = 0: x_bytes, dy_bytes: of a value in shared memory; ctas: that an SM should hold.
+// bytes of a vector of x in shared memory
+int slot_bytes(int x_type, Width w) {
+    const int size = w.v * type_size(x_type);
+    return size + (w.words && type_size(x_type) < 4 ? 4 : 0);
+}
+
+// How a call runs in one pass, or ks = 0: slot: bytes of a vector in shared memory; ctas: that an SM should hold.
 // The narrowest slab of whole groups whose rows are lines of 64 bytes of x, or of 32 where there are few CTAs; the least CTAs that hold it; and more
 // of them while SMs are idle.
-GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size, int value_bytes, int ctas, int act, const float* gamma,
+GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size, int slot, int ctas, int act, const float* gamma,
                const float* beta, int* smem) {
     GnOne s{};
     s.pixels = pixels;
@@ -476,7 +509,7 @@ GnOne one_pass(const nitro_gnorm* h, int samples, int pixels, int v, int x_size,
         const int rows = kGnThreads >> s.lane_log;
         s.chunk = (pixels + ks - 1) / ks;
         s.steps = (s.chunk + rows - 1) / rows;
-        const int64_t bytes = (int64_t)s.steps * kGnThreads * v * value_bytes + 32 + 4 * (2 * kGnWarps + 3) * (int64_t)s.width + 20 * m;
+        const int64_t bytes = (int64_t)s.steps * kGnThreads * slot + 32 + 4 * (2 * kGnWarps + 3) * (int64_t)s.width + 20 * m;
         *smem = (int)bytes;
         return bytes <= budget;
     };
@@ -546,30 +579,35 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
     if (!y) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
     TRY(clear_once(h->clean, h->ticket, sizeof(uint32_t) * h->batch, s));
-    const int v = pick_v(h, samples, {mx, my}), C = h->channels;
+    int whole = 0;
+    const Width w = pick_v(h, samples, {mx}, {my}, &whole);
+    const int v = w.v, C = h->channels;
     int smem = 0;
-    const GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), type_size(x_type), 3, act, gamma, beta, &smem);
+    GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), slot_bytes(x_type, w), 3, act, gamma, beta, &smem);
+    one.whole = whole;
     if (one.ks) {
-        TRY(gn_one_forward(one, samples, smem, x, x_type, ldx, stride_x, eps, mean, rstd, y, y_type, ldy, stride_y, v, s));
+        TRY(gn_one_forward(one, samples, smem, x, x_type, ldx, stride_x, eps, mean, rstd, y, y_type, ldy, stride_y, w, s));
         return NITRO_OK;
     }
     const int batch = batch_size(h, pixels, type_size(x_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
-        const GnShape sh = shape(h, pixels, n, v, 4, act, gamma, beta);
+        GnShape sh = shape(h, pixels, n, v, 4, act, gamma, beta);
+        sh.whole = whole;
         float* m = mean ? mean + (int64_t)s0 * h->groups : h->mean;
         float* r = rstd ? rstd + (int64_t)s0 * h->groups : h->rstd;
         const double values = (double)n * pixels * C;
         const dim3 grid(sh.chunks, n), block((sh.rows * sh.vecs + 31) / 32 * 32);
         TRY(with_x(x_type, [&](auto xt) {
             using X = decltype(xt);
-            return with_v(v, [&](auto vt) {
+            return with_v<sizeof(X) == 4>(w, [&](auto vt, auto wt) {
                 constexpr int V = decltype(vt)::value;
+                constexpr bool W = decltype(wt)::value;
                 static std::atomic<uint64_t> ready{0};
-                const cudaError_t e = one_ready(k_gn_stats<X, V>, ready, kRing * Slots<X, V>::STEP + 8 * kGnChannels);
+                const cudaError_t e = one_ready(k_gn_stats<X, V, W>, ready, kRing * Slots<X, V, W>::STEP + 8 * kGnChannels);
                 if (e != cudaSuccess) return e;
                 ProfScope ps(K_GNORM_FWD, s, 0.0, values * sizeof(X));
-                return launch_k(k_gn_stats<X, V>, grid, block, kRing * Slots<X, V>::STEP + 8 * C, s, sample_at<X>(mx, s0), ldx, stride_x, sh, eps, h->part,
+                return launch_k(k_gn_stats<X, V, W>, grid, block, kRing * Slots<X, V, W>::STEP + 8 * C, s, sample_at<X>(mx, s0), ldx, stride_x, sh, eps, h->part,
                                 h->ticket, m, r);
             });
         }));
@@ -577,14 +615,15 @@ nitro_status nitro_gnorm_forward(nitro_gnorm* h, const void* x, int x_type, int6
             using X = decltype(xt);
             return with_y(y_type, [&](auto yt) {
                 using Y = decltype(yt);
-                return with_v(v, [&](auto vt) {
+                return with_v<sizeof(X) == 4 || sizeof(Y) == 4>(w, [&](auto vt, auto wt) {
                     constexpr int V = decltype(vt)::value;
-                    constexpr int kSmem = kRing * Slots<X, V>::STEP;
+                    constexpr bool W = decltype(wt)::value;
+                    constexpr int kSmem = kRing * Slots<X, V, W>::STEP;
                     static std::atomic<uint64_t> ready{0};
-                    const cudaError_t e = one_ready(k_gn_apply<X, Y, V>, ready, kSmem);
+                    const cudaError_t e = one_ready(k_gn_apply<X, Y, V, W>, ready, kSmem);
                     if (e != cudaSuccess) return e;
                     ProfScope ps(K_GNORM_FWD, s, 0.0, values * (sizeof(X) + sizeof(Y)));
-                    return launch_k(k_gn_apply<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sh, (const float*)m,
+                    return launch_k(k_gn_apply<X, Y, V, W>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sh, (const float*)m,
                                     (const float*)r, const_cast<Y*>(sample_at<Y>(my, s0)), ldy, stride_y);
                 });
             });
@@ -611,9 +650,12 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
     }
     if (!dx && !dgamma && !dbeta) return NITRO_OK;
     TRY(clear_once(h->clean, h->ticket, sizeof(uint32_t) * h->batch, s));
-    const int v = pick_v(h, samples, {mx, mdy, mdx});
+    int whole = 0;
+    const Width w = pick_v(h, samples, {mx, mdy}, {mdx}, &whole);
+    const int v = w.v;
     int smem = 0;
-    const GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), type_size(x_type) + 4, 2, act, gamma, beta, &smem);
+    GnOne one = one_pass(h, samples, pixels, v, type_size(x_type), slot_bytes(x_type, w) + 4 * v, 2, act, gamma, beta, &smem);
+    one.whole = whole;
     if (one.ks) {
         // the sums of at most a batch's samples are kept at a time
         const int most = dgamma || dbeta ? std::max(kGnCtas, kGnBatch) : samples;
@@ -621,7 +663,7 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
             const int n = std::min(most, samples - s0);
             TRY(gn_one_backward(one, n, smem, sample_at(mx, s0), x_type, ldx, stride_x, mean + (int64_t)s0 * h->groups,
                                 rstd + (int64_t)s0 * h->groups, sample_at(mdy, s0), y_type, lddy, stride_dy, dgamma || dbeta ? h->part_c : nullptr,
-                                dx ? const_cast<void*>(sample_at(mdx, s0)) : nullptr, lddx, stride_dx, v, s));
+                                dx ? const_cast<void*>(sample_at(mdx, s0)) : nullptr, lddx, stride_dx, w, s));
             if (dgamma || dbeta) {
                 ProfScope ps(K_GNORM_PARAMS, s, 0.0, 8.0 * n * C);
                 TRY(launch_k(k_gn_params, dim3((C + 31) / 32, 2), dim3(1024), 0, s, (const float*)h->part_c, n, C, dgamma, dbeta, (int)(s0 > 0)));
@@ -632,7 +674,8 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
     const int batch = batch_size(h, pixels, type_size(x_type) + type_size(y_type));
     for (int s0 = 0; s0 < samples; s0 += batch) {
         const int n = std::min(batch, samples - s0);
-        const GnShape sh = shape(h, pixels, n, v, gn_resident(v), act, gamma, beta);
+        GnShape sh = shape(h, pixels, n, v, gn_resident(v), act, gamma, beta);
+        sh.whole = whole;
         const float *m = mean + (int64_t)s0 * h->groups, *r = rstd + (int64_t)s0 * h->groups;
         const double values = (double)n * pixels * C;
         const dim3 grid(sh.chunks, n), block((sh.rows * sh.vecs + 31) / 32 * 32);
@@ -640,14 +683,15 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
             using X = decltype(xt);
             return with_y(y_type, [&](auto yt) {
                 using Y = decltype(yt);
-                return with_v(v, [&](auto vt) {
+                return with_v<sizeof(X) == 4 || sizeof(Y) == 4>(w, [&](auto vt, auto wt) {
                     constexpr int V = decltype(vt)::value;
-                    constexpr int kSmem = kRing * (Slots<X, V>::STEP + Slots<Y, V>::STEP);
+                    constexpr bool W = decltype(wt)::value;
+                    constexpr int kSmem = kRing * (Slots<X, V, W>::STEP + Slots<Y, V, W>::STEP);
                     static std::atomic<uint64_t> ready{0};
-                    const cudaError_t e = one_ready(k_gn_sums<X, Y, V>, ready, kSmem);
+                    const cudaError_t e = one_ready(k_gn_sums<X, Y, V, W>, ready, kSmem);
                     if (e != cudaSuccess) return e;
                     ProfScope ps(K_GNORM_BWD, s, 0.0, values * (sizeof(X) + sizeof(Y)));
-                    return launch_k(k_gn_sums<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0),
+                    return launch_k(k_gn_sums<X, Y, V, W>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x, sample_at<Y>(mdy, s0),
                                     lddy, stride_dy, sh, m, r, h->part_c, h->part, h->ticket, dx ? h->means : nullptr);
                 });
             });
@@ -657,14 +701,15 @@ nitro_status nitro_gnorm_backward(nitro_gnorm* h, const void* x, int x_type, int
                 using X = decltype(xt);
                 return with_y(y_type, [&](auto yt) {
                     using Y = decltype(yt);
-                    return with_v(v, [&](auto vt) {
+                    return with_v<sizeof(X) == 4 || sizeof(Y) == 4>(w, [&](auto vt, auto wt) {
                         constexpr int V = decltype(vt)::value;
-                        constexpr int kSmem = kRing * (Slots<X, V>::STEP + Slots<Y, V>::STEP);
+                        constexpr bool W = decltype(wt)::value;
+                        constexpr int kSmem = kRing * (Slots<X, V, W>::STEP + Slots<Y, V, W>::STEP);
                         static std::atomic<uint64_t> ready{0};
-                        const cudaError_t e = one_ready(k_gn_dx<X, Y, V>, ready, kSmem);
+                        const cudaError_t e = one_ready(k_gn_dx<X, Y, V, W>, ready, kSmem);
                         if (e != cudaSuccess) return e;
                         ProfScope ps(K_GNORM_BWD, s, 0.0, values * (sizeof(X) + 2 * sizeof(Y)));
-                        return launch_k(k_gn_dx<X, Y, V>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x,
+                        return launch_k(k_gn_dx<X, Y, V, W>, grid, block, kSmem, s, sample_at<X>(mx, s0), ldx, stride_x,
                                         sample_at<Y>(mdy, s0), lddy, stride_dy, sh, m, r, (const float2*)h->means,
                                         const_cast<Y*>(sample_at<Y>(mdx, s0)), lddx, stride_dx);
                     });

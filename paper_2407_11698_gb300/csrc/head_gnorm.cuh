@@ -13,11 +13,18 @@ struct GnOne {
     int width, gs, slabs, ks;            // channels and groups of a slab, slabs of a sample, CTAs of a cluster
     int vecs, lane_log;                  // vectors of a slab's pixel, and the lanes' logarithm
     int chunk, steps;                    // pixels of a CTA, of which a thread takes every (256 / lanes)th
+    int whole;                           // what is written starts at multiples of a vector
     int alike, entries;                  // vectors are of one group each; a group's vectors, or its channels where they are not
     FloorDiv32 by_per;
     int act;
     const float* gamma;                  // or null
     const float* beta;                   // or null
+};
+
+// How wide vectors are, and whether they start at any value (Slots)
+struct Width {
+    int v;
+    bool words;
 };
 
 namespace {
@@ -49,6 +56,11 @@ struct Vals {
             } else {
                 w[0] = *reinterpret_cast<const uint32_t*>(p);
             }
+            unpack(w, v);
+        }
+    }
+    static __device__ __forceinline__ void unpack(const uint32_t* w, float2* v) {
+        if constexpr (V > 1) {
 #pragma unroll
             for (int j = 0; j < N; ++j) {
                 if constexpr (sizeof(T) == 1) {        // 2^23 + (v + 128) as a float has v + 128 in its low byte
@@ -224,39 +236,85 @@ struct Sums {
     }
 };
 
-// A vector's place in shared memory: planes of 16 bytes a thread (or less, the vector itself)
-template <typename T, int V>
+// A vector's place in shared memory: planes of 16 bytes a thread (or less, the vector itself).  WORDS: vectors that start at any
+// value; the 32-bit words that they reach into are copied (each holds a byte of the vector, so it is memory
+// that is there), in planes of words, and shifted when they are read
+template <typename T, int V, bool WORDS>
 struct Slots {
-    static constexpr int BYTES = V * (int)sizeof(T), PLANE = BYTES < 16 ? BYTES : 16, PLANES = BYTES / PLANE;
+    static constexpr int SIZE = V * (int)sizeof(T);
+    static constexpr int BYTES = WORDS ? (SIZE + 3) / 4 * 4 + (sizeof(T) < 4 ? 4 : 0) : SIZE;
+    static constexpr int PLANE = WORDS ? 4 : BYTES < 16 ? BYTES : 16, PLANES = BYTES / PLANE;
     static constexpr int STEP = kGnThreads * BYTES;          // from a thread's vector to its next
     static __device__ __forceinline__ uint8_t* first(uint8_t* base) { return base + (int)threadIdx.x * PLANE; }
     // Place: whose places the vector takes, its own or those of wider values that replace it later
+    template <class Place>
+    static __device__ __forceinline__ int plane(int i) {
+        const int byte = i * PLANE;
+        return byte / Place::PLANE * kGnThreads * Place::PLANE + byte % Place::PLANE;
+    }
     template <class Place = Slots>
     static __device__ __forceinline__ void fetch(uint8_t* to, const T* src) {
-        if constexpr (PLANE < 4) {
+        if constexpr (WORDS) {
+            const uintptr_t at = (uintptr_t)src & ~(uintptr_t)3;
+            const int end = (int)((uintptr_t)src & 3) + SIZE;
+#pragma unroll
+            for (int i = 0; i < PLANES; ++i)
+                if (4 * i < end)
+                    asm volatile("cp.async.ca.shared.global [%0], [%1], 4;" ::"r"(smem_u32(to + plane<Place>(i))), "l"(at + 4 * i) : "memory");
+        } else if constexpr (PLANE < 4) {
             *reinterpret_cast<T*>(to) = *src;
         } else {
 #pragma unroll
             for (int i = 0; i < PLANES; ++i) {
-                const uint32_t dst = smem_u32(to + i * kGnThreads * Place::PLANE);
+                const uint32_t dst = smem_u32(to + plane<Place>(i));
                 const char* s = reinterpret_cast<const char*>(src) + i * PLANE;
                 if constexpr (PLANE == 16) asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(dst), "l"(s) : "memory");
                 else asm volatile("cp.async.ca.shared.global [%0], [%1], %2;" ::"r"(dst), "l"(s), "n"(PLANE) : "memory");
             }
         }
     }
+    // src: the vector's address, or its low bits
     template <class Place = Slots>
-    static __device__ __forceinline__ void get(const uint8_t* from, float2* v) {
+    static __device__ __forceinline__ void get(const uint8_t* from, float2* v, uint32_t src) {
+        if constexpr (WORDS) {
+            uint32_t w[PLANES + 1];
 #pragma unroll
-        for (int i = 0; i < PLANES; ++i)
-            Vals<T, V / PLANES>::load(reinterpret_cast<const T*>(from + i * kGnThreads * Place::PLANE), v + i * (V / PLANES / 2));
+            for (int i = 0; i < PLANES; ++i) w[i] = *reinterpret_cast<const uint32_t*>(from + plane<Place>(i));
+            if constexpr (sizeof(T) < 4) {
+#pragma unroll
+                for (int i = 0; i < SIZE / 4; ++i) w[i] = __funnelshift_r(w[i], w[i + 1], 8 * (src & 3));
+            }
+            Vals<T, V>::unpack(w, v);
+        } else {
+#pragma unroll
+            for (int i = 0; i < PLANES; ++i)
+                Vals<T, V / PLANES>::load(reinterpret_cast<const T*>(from + plane<Place>(i)), v + i * (V / PLANES / 2));
+        }
     }
     static __device__ __forceinline__ void put(uint8_t* to, const float2* v) {
+        static_assert(!WORDS, "values of the kernels' own are aligned");
 #pragma unroll
         for (int i = 0; i < PLANES; ++i)
             Vals<T, V / PLANES>::store(reinterpret_cast<T*>(to + i * kGnThreads * PLANE), v + i * (V / PLANES / 2));
     }
 };
+__device__ __forceinline__ uint32_t low_bits(const void* p) { return (uint32_t)(uintptr_t)p; }
+
+// V values of a row; whole: rows are aligned to V values
+template <typename T, int V, bool WORDS>
+__device__ __forceinline__ void store_row(T* p, const float2* v, bool whole) {
+    if constexpr (WORDS) {
+        if (!whole) {
+#pragma unroll
+            for (int j = 0; j < V; ++j) {
+                const float2 x = make_float2(j & 1 ? v[j >> 1].y : v[j >> 1].x, 0.0f);
+                Vals<T, 1>::store(p + j, &x);
+            }
+            return;
+        }
+    }
+    Vals<T, V>::store(p, v);
+}
 __device__ __forceinline__ void copies_group() { asm volatile("cp.async.commit_group;" ::: "memory"); }
 
 // ------------------------------------------------------------------ one pass
@@ -349,13 +407,18 @@ cudaError_t with_y(int type, F&& f) {
     if (type == NITRO_BF16) return f((uint16_t)0);
     return f(0.0f);
 }
-template <class F>
-cudaError_t with_v(int v, F&& f) {
-    if (v == 8) return f(std::integral_constant<int, 8>{});
-    if (v == 4) return f(std::integral_constant<int, 4>{});
-    return f(std::integral_constant<int, 1>{});
+// f(width, words); WIDE: for fp32 values, which take no words of eight
+template <bool WIDE, class F>
+cudaError_t with_v(Width w, F&& f) {
+    if (w.words) {
+        if constexpr (!WIDE)
+            if (w.v == 8) return f(std::integral_constant<int, 8>{}, std::true_type{});
+        return f(std::integral_constant<int, 4>{}, std::true_type{});
+    }
+    if (w.v == 8) return f(std::integral_constant<int, 8>{}, std::false_type{});
+    if (w.v == 4) return f(std::integral_constant<int, 4>{}, std::false_type{});
+    return f(std::integral_constant<int, 1>{}, std::false_type{});
 }
-
 template <typename K>
 cudaError_t one_ready(K* kernel, std::atomic<uint64_t>& ready, int smem = 226 * 1024) {
     int dev = 0;
@@ -363,21 +426,21 @@ cudaError_t one_ready(K* kernel, std::atomic<uint64_t>& ready, int smem = 226 * 
     return once_per_device(ready, dev, [kernel, smem] { return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem); });
 }
 
-
 // and whether vectors are of one group each (single values always are)
-template <class F>
-cudaError_t with_alike(int v, bool alike, F&& f) {
-    if (v == 1) return f(std::integral_constant<int, 1>{}, std::true_type{});
-    if (v == 8) return alike ? f(std::integral_constant<int, 8>{}, std::true_type{}) : f(std::integral_constant<int, 8>{}, std::false_type{});
-    return alike ? f(std::integral_constant<int, 4>{}, std::true_type{}) : f(std::integral_constant<int, 4>{}, std::false_type{});
+template <bool WIDE, class F>
+cudaError_t with_alike(Width w, bool alike, F&& f) {
+    return with_v<WIDE>(w, [&](auto v, auto words) {
+        if constexpr (decltype(v)::value == 1) return f(v, words, std::true_type{});
+        else return alike ? f(v, words, std::true_type{}) : f(v, words, std::false_type{});
+    });
 }
 
 }  // namespace
 
 // The one-pass launches.  mean, rstd: null where nobody wants them.  sums: [samples][2][channels] or null
 cudaError_t gn_one_forward(const GnOne& one, int samples, int smem, const void* x, int x_type, int64_t ldx, int64_t stride_x, float eps, float* mean,
-                           float* rstd, void* y, int y_type, int64_t ldy, int64_t stride_y, int v, cudaStream_t s);
+                           float* rstd, void* y, int y_type, int64_t ldy, int64_t stride_y, Width v, cudaStream_t s);
 cudaError_t gn_one_backward(const GnOne& one, int samples, int smem, const void* x, int x_type, int64_t ldx, int64_t stride_x, const float* mean,
                             const float* rstd, const void* dy, int y_type, int64_t lddy, int64_t stride_dy, float* sums, void* dx, int64_t lddx,
-                            int64_t stride_dx, int v, cudaStream_t s);
+                            int64_t stride_dx, Width v, cudaStream_t s);
 }  // namespace nitro

@@ -8,13 +8,13 @@ namespace {
 
 // The gradients: du replaces dy in shared memory, in 32 bits, so that the slopes are taken once.  sums: of du and
 // du h for each sample and channel [sample][2][channels], or null.  dx may be null.
-template <typename X, typename Y, int V, bool ALIKE>
+template <typename X, typename Y, int V, bool W, bool ALIKE>
 __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64_t ldx, int64_t sx, const Y* dy, int64_t lddy, int64_t sdy,
                                                                const GnOne s, const float* mean, const float* rstd, float* sums, Y* dx,
                                                                int64_t lddx, int64_t sdx) {
-    using SX = Slots<X, V>;
-    using SY = Slots<Y, V>;
-    using SD = Slots<float, V>;
+    using SX = Slots<X, V, W>;
+    using SY = Slots<Y, V, W>;
+    using SD = Slots<float, V, false>;
     constexpr int N = (V + 1) / 2;
     extern __shared__ __align__(16) uint8_t data[];
     const int xb = (s.steps * SX::STEP + 15) / 16 * 16, gs = s.gs;
@@ -27,6 +27,8 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
     const GnPart at(s, V);
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     uint8_t *xslot = SX::first(data), *gslot = SD::first(grads);
+    const uint32_t xlow0 = low_bits(x + at.sample * sx + (at.p0 + at.row) * ldx + at.c), xlow_step = (uint32_t)(at.rows * ldx * (int64_t)sizeof(X));
+    const uint32_t glow0 = low_bits(dy + at.sample * sdy + (at.p0 + at.row) * lddy + at.c), glow_step = (uint32_t)(at.rows * lddy * (int64_t)sizeof(Y));
     {
         const X* src = x + at.sample * sx + (at.p0 + at.row) * ldx + at.c;
         const Y* grad = dy + at.sample * sdy + (at.p0 + at.row) * lddy + at.c;
@@ -55,14 +57,15 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
     with_act(s.act, [&](auto act) {
         const uint8_t* tx = xslot;
         uint8_t* tg = gslot;
+        uint32_t xlow = xlow0, glow = glow0;
         for (int k = 0, i = 0; k < kGnStages; ++k) {
             copies_landed(k);
             const int end = min(at.count, (k + 1) * at.stage);
 #pragma unroll 2
-            for (; i < end; ++i, tx += SX::STEP, tg += SD::STEP) {
+            for (; i < end; ++i, tx += SX::STEP, tg += SD::STEP, xlow += xlow_step, glow += glow_step) {
                 float2 v[N], du[N];
-                SX::get(tx, v);
-                SY::template get<SD>(tg, du);
+                SX::get(tx, v, xlow);
+                SY::template get<SD>(tg, du, glow);
                 ch.template slopes<decltype(act)::value>(v, du);
 #pragma unroll
                 for (int j = 0; j < N; ++j) {
@@ -141,13 +144,14 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
             Y* dst = dx + at.sample * sdx + (at.p0 + at.row) * lddx + at.c;
             const int64_t step = at.rows * lddx;
             const uint8_t *tx = xslot, *tg = gslot;
+            uint32_t xlow = xlow0;
 #pragma unroll 4
-            for (int i = 0; i < at.count; ++i, tx += SX::STEP, tg += SD::STEP, dst += step) {
+            for (int i = 0; i < at.count; ++i, tx += SX::STEP, tg += SD::STEP, dst += step, xlow += xlow_step) {
                 float2 v[N], du[N];
-                SX::get(tx, v);
-                SD::get(tg, du);
+                SX::get(tx, v, xlow);
+                SD::get(tg, du, 0);
                 ch.dx(v, du);
-                Vals<Y, V>::store(dst, v);
+                store_row<Y, V, W>(dst, v, s.whole);
             }
         }
     }
@@ -158,19 +162,20 @@ __global__ void __launch_bounds__(kGnThreads, 2) k_gn_one_back(const X* x, int64
 
 cudaError_t gn_one_backward(const GnOne& one, int samples, int smem, const void* x, int x_type, int64_t ldx, int64_t stride_x, const float* mean,
                             const float* rstd, const void* dy, int y_type, int64_t lddy, int64_t stride_dy, float* sums, void* dx, int64_t lddx,
-                            int64_t stride_dx, int v, cudaStream_t s) {
+                            int64_t stride_dx, Width v, cudaStream_t s) {
     return with_x(x_type, [&](auto xt) {
         using X = decltype(xt);
         return with_y(y_type, [&](auto yt) {
             using Y = decltype(yt);
-            return with_alike(v, one.alike, [&](auto vt, auto alike) {
+            return with_alike<sizeof(X) == 4 || sizeof(Y) == 4>(v, one.alike, [&](auto vt, auto wt, auto alike) {
                 constexpr int V = decltype(vt)::value;
+                constexpr bool W = decltype(wt)::value;
                 constexpr bool A = decltype(alike)::value;
                 static std::atomic<uint64_t> ready{0};
-                const cudaError_t e = one_ready(k_gn_one_back<X, Y, V, A>, ready);
+                const cudaError_t e = one_ready(k_gn_one_back<X, Y, V, W, A>, ready);
                 if (e != cudaSuccess) return e;
                 ProfScope ps(K_GNORM_BWD, s, 0.0, (double)samples * one.pixels * one.channels * (sizeof(X) + (dx ? 2 : 1) * sizeof(Y)));
-                return launch_cluster(k_gn_one_back<X, Y, V, A>, dim3(one.slabs * one.ks, samples), kGnThreads, one.ks, s, smem, (const X*)x, ldx,
+                return launch_cluster(k_gn_one_back<X, Y, V, W, A>, dim3(one.slabs * one.ks, samples), kGnThreads, one.ks, s, smem, (const X*)x, ldx,
                                       stride_x, (const Y*)dy, lddy, stride_dy, one, mean, rstd, sums, (Y*)dx, lddx, stride_dx);
             });
         });

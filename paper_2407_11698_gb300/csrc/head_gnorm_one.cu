@@ -6,10 +6,10 @@ using namespace nitro;
 namespace nitro {
 namespace {
 
-template <typename X, typename Y, int V, bool ALIKE>
+template <typename X, typename Y, int V, bool W, bool ALIKE>
 __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ldx, int64_t sx, const GnOne s, float eps, float* mean,
                                                           float* rstd, Y* y, int64_t ldy, int64_t sy) {
-    using SX = Slots<X, V>;
+    using SX = Slots<X, V, W>;
     constexpr int N = (V + 1) / 2;
     extern __shared__ __align__(16) uint8_t data[];
     const int gs = s.gs, lanes = 1 << s.lane_log;
@@ -23,6 +23,7 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     x += at.sample * sx;
     uint8_t* slot = SX::first(data);
+    const uint32_t low0 = low_bits(x + (at.p0 + at.row) * ldx + at.c), low_step = (uint32_t)(at.rows * ldx * (int64_t)sizeof(X));
     {
         const X* src = x + (at.p0 + at.row) * ldx + at.c;
         const int64_t step = at.rows * ldx;
@@ -46,14 +47,15 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
     Sums<V> t;
     {
         const uint8_t* from = slot;
+        uint32_t low = low0;
         for (int k = 0, i = 0; k < kGnStages; ++k) {
             copies_landed(k);
-            if (k == 0 && at.count > 0) SX::get(slot, t.k);
+            if (k == 0 && at.count > 0) SX::get(slot, t.k, low0);
             const int end = min(at.count, (k + 1) * at.stage);
 #pragma unroll 4
-            for (; i < end; ++i, from += SX::STEP) {
+            for (; i < end; ++i, from += SX::STEP, low += low_step) {
                 float2 v[N];
-                SX::get(from, v);
+                SX::get(from, v, low);
                 t.add(v);
             }
         }
@@ -139,13 +141,14 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
         Y* dst = y + at.sample * sy + (at.p0 + at.row) * ldy + at.c;
         const int64_t step = at.rows * ldy;
         const uint8_t* from = slot;
+        uint32_t low = low0;
         with_act(s.act, [&](auto act) {
 #pragma unroll 4
-            for (int i = 0; i < at.count; ++i, from += SX::STEP, dst += step) {
+            for (int i = 0; i < at.count; ++i, from += SX::STEP, dst += step, low += low_step) {
                 float2 v[N];
-                SX::get(from, v);
+                SX::get(from, v, low);
                 ch.template apply<decltype(act)::value>(v);
-                Vals<Y, V>::store(dst, v);
+                store_row<Y, V, W>(dst, v, s.whole);
             }
         });
     }
@@ -155,19 +158,20 @@ __global__ void __launch_bounds__(kGnThreads, 3) k_gn_one(const X* x, int64_t ld
 }  // namespace
 
 cudaError_t gn_one_forward(const GnOne& one, int samples, int smem, const void* x, int x_type, int64_t ldx, int64_t stride_x, float eps, float* mean,
-                           float* rstd, void* y, int y_type, int64_t ldy, int64_t stride_y, int v, cudaStream_t s) {
+                           float* rstd, void* y, int y_type, int64_t ldy, int64_t stride_y, Width v, cudaStream_t s) {
     return with_x(x_type, [&](auto xt) {
         using X = decltype(xt);
         return with_y(y_type, [&](auto yt) {
             using Y = decltype(yt);
-            return with_alike(v, one.alike, [&](auto vt, auto alike) {
+            return with_alike<sizeof(X) == 4 || sizeof(Y) == 4>(v, one.alike, [&](auto vt, auto wt, auto alike) {
                 constexpr int V = decltype(vt)::value;
+                constexpr bool W = decltype(wt)::value;
                 constexpr bool A = decltype(alike)::value;
                 static std::atomic<uint64_t> ready{0};
-                const cudaError_t e = one_ready(k_gn_one<X, Y, V, A>, ready);
+                const cudaError_t e = one_ready(k_gn_one<X, Y, V, W, A>, ready);
                 if (e != cudaSuccess) return e;
                 ProfScope ps(K_GNORM_FWD, s, 0.0, (double)samples * one.pixels * one.channels * (sizeof(X) + sizeof(Y)));
-                return launch_cluster(k_gn_one<X, Y, V, A>, dim3(one.slabs * one.ks, samples), kGnThreads, one.ks, s, smem, (const X*)x, ldx,
+                return launch_cluster(k_gn_one<X, Y, V, W, A>, dim3(one.slabs * one.ks, samples), kGnThreads, one.ks, s, smem, (const X*)x, ldx,
                                       stride_x, one, eps, mean, rstd, (Y*)y, ldy, stride_y);
             });
         });

@@ -150,6 +150,29 @@ def test_buffers_that_start_anywhere(offset):
     check(*t, groups, 1e-5, "silu", *run(*t, groups, 1e-5, "silu"))
 
 
+# vectors of eight and of four values in rows that start anywhere: in one pass and in two, groups of whole vectors and of parts of
+# them, the last row at the buffer's end, and outputs that are aligned although the inputs are not
+@pytest.mark.parametrize("out_pad", [0, 1])
+@pytest.mark.parametrize("pad", [1, 2, 5])
+@pytest.mark.parametrize("x, y", [("i8", "bf16"), ("bf16", "bf16"), ("f32", "f32"), ("bf16", "f32"), ("i8", "f32")])
+@pytest.mark.parametrize("n, p, c, groups", [(3, 50, 64, 8), (2, 33, 48, 4), (1, 1, 8, 1), (1, 900, 1024, 1), (40, 3000, 16, 1),
+                                             (3, 50, 60, 6), (2, 33, 52, 4), (1, 1, 4, 2), (1, 900, 1028, 1), (30, 3000, 20, 1)])
+def test_vectors_that_start_anywhere(n, p, c, groups, x, y, pad, out_pad):
+    t = list(inputs(n, p, c, x, y, seed=pad + c))
+    for i in (0, 1):
+        ld = c + pad
+        buf = torch.full((pad + (n * p - 1) * ld + c,), 77, dtype=t[i].dtype, device="cuda")
+        v = buf.as_strided((n, p, c), (p * ld, ld, 1), pad)
+        v.copy_(t[i])
+        t[i] = v
+    out = run(*t, groups, 1e-5, "silu", pad=out_pad * pad)
+    check(*t, groups, 1e-5, "silu", *out)
+    if out_pad:
+        for o in (out[0], out[3]):
+            assert (o.as_strided((n, p, pad), o.stride(), o.storage_offset() + c) == 77).all()
+    assert all(torch.equal(a, b) for a, b in zip(out, run(*t, groups, 1e-5, "silu", pad=out_pad * pad)))
+
+
 def test_samples_apart_and_a_part_of_the_pixels():
     n, p, c, groups = 3, 40, 24, 3
     x, dy, gamma, beta = inputs(n, p, c, seed=8)
