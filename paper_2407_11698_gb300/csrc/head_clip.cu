@@ -70,14 +70,18 @@ struct Exact {
 #pragma unroll 1
         for (int d = 16; d > 0; d >>= 1) add(__shfl_xor_sync(0xffffffffu, hi, d), __shfl_xor_sync(0xffffffffu, lo, d));
     }
+    // (what an infinite sum leaves over is a NaN)
+    __device__ __forceinline__ float value() const { return hi <= 3e38f ? hi + lo : hi; }
 };
 
-// Sums of squares.  A lane's run is short before it goes to `mid`: many squares are far below a sum's last place and are
-// lost more often than they are rounded up (6700 values of bf16 in one sum: 3.5e-6 to 6.5e-6 too little).
+// Sums of squares.  A lane's run takes kRun pairs at most before it goes to sums that keep what their roundings leave over: many squares are
+// far below a long run's last place and are lost more often than they are rounded up, and equal ones are all rounded
+// the same way (1500 equal values in one run: a norm 1.2e-5 off).
+constexpr int kRun = 16;
+static_assert(kClipGroup * 8 / 2 <= kRun, "a run of vectors is a group");
 struct Squares {
     float2 run = {0.0f, 0.0f}, run_big = {0.0f, 0.0f}, run_small = {0.0f, 0.0f};
-    Exact mid;
-    float big = 0.0f, small = 0.0f;
+    Exact mid, big, small;
     __device__ __forceinline__ void add(float2 x) {
         run = fma2(x, x, run);
         const float2 b = mul2(x, pair(0x1p-80f)), s = mul2(x, pair(0x1p90f));
@@ -86,8 +90,8 @@ struct Squares {
     }
     __device__ __forceinline__ void end_run() {
         mid.add(run.x + run.y, 0.0f);
-        big += run_big.x + run_big.y;
-        small += run_small.x + run_small.y;
+        big.add(run_big.x + run_big.y, 0.0f);
+        small.add(run_small.x + run_small.y, 0.0f);
         run = run_big = run_small = pair(0.0f);
     }
 };
@@ -169,15 +173,20 @@ struct Parts {
         return reinterpret_cast<uint4*>(static_cast<T*>(p.out) + row * p.ld_out) + (i - row * per);
     }
 };
-template <class Q, class F>
-__device__ __forceinline__ void singles(const Piece& p, const Q& q, int lane, F&& f) {
+// f(address in `in`, address in `out`) for the lane's single values; end() after every kRun, and after the last
+template <class Q, class F, class End>
+__device__ __forceinline__ void singles(const Piece& p, const Q& q, int lane, F&& f, End&& end) {
     using T = typename Q::T;
     if (q.tail == 0) return;
     RowWalk at(lane, 32, q.tail);
+    for (int i = lane; i < q.singles;) {
+        const int to = min(q.singles, i + 32 * kRun);
 #pragma unroll 4
-    for (int i = lane; i < q.singles; i += 32, at.next()) {
-        const int c = q.per * Of<T>::V + at.part;
-        f(static_cast<const T*>(p.in) + at.row * p.ld_in + c, static_cast<T*>(p.out) + at.row * p.ld_out + c);
+        for (; i < to; i += 32, at.next()) {
+            const int c = q.per * Of<T>::V + at.part;
+            f(static_cast<const T*>(p.in) + at.row * p.ld_in + c, static_cast<T*>(p.out) + at.row * p.ld_out + c);
+        }
+        end();
     }
 }
 
@@ -257,8 +266,7 @@ __device__ __forceinline__ int sum_piece(const Piece& p, int lane, uint4* ring, 
         stream_piece(p, q, lane, ring, from, [&](int step, uint4* at) { sum_vector(p, q, step * 32 + lane, *at, sum); },
                         [&] { sum.end_run(); });
     using T = typename Q::T;
-    singles(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); });
-    sum.end_run();
+    singles(p, q, lane, [&](const T* in, T*) { sum.add(make_float2(Of<T>::get(*in), 0.0f)); }, [&] { sum.end_run(); });
     return steps;
 }
 
@@ -267,8 +275,12 @@ template <class Q>
 __device__ __forceinline__ int sum_kept(const Piece& p, int lane, const uint4* kept, int keep, int slot, Squares& sum) {
     const Q q(p);
     const int steps = q.steps(), n = min(steps, keep - slot);
-#pragma unroll 4
-    for (int k = 0; k < n; ++k) sum_vector(p, q, k * 32 + lane, kept[(slot + k) * 32], sum);
+    for (int k = 0; k < n; k += kClipGroup) {
+#pragma unroll
+        for (int j = 0; j < kClipGroup; ++j)
+            if (k + j < n) sum_vector(p, q, (k + j) * 32 + lane, kept[(slot + k + j) * 32], sum);
+        sum.end_run();
+    }
     return steps;
 }
 
@@ -309,7 +321,7 @@ template <class Q>
 __device__ __forceinline__ void scale_piece(const Piece& p, int lane, uint4* kept, uint4* ring, int keep, int slot, float f) {
     const Q q(p);
     using T = typename Q::T;
-    singles(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); });
+    singles(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); }, [] {});
     const int steps = q.steps(), left = min(steps, max(0, keep - slot));         // steps that are kept
     if constexpr (Q::kSpan) {
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -428,10 +440,9 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
         slot += with_kind(p, [&](auto t) { return sum_kept<typename decltype(t)::type>(p, lane, kept, keep, slot, q); });
     }
     {
-        q.end_run();
         Exact mid = q.mid;
         mid.over_warp();
-        const float big = warp_sum(q.big), small = warp_sum(q.small);
+        const float big = warp_sum(q.big.value()), small = warp_sum(q.small.value());
         if (lane == 0) sh[warp] = make_float4(mid.hi, mid.lo, big, small);
     }
     if (threadIdx.x == 0) ok = 1;
