@@ -8,8 +8,9 @@
 // gradients are read once; where there are more, 7 KB, and the others come through a ring of places there.
 // 48 tensors, 2.6 GB: 1290 us, 6.0 TB/s over the values' two ways in and one out (the first 448 us, with SMs up to a sixth apart);
 // 300 tensors, 29 MB: 25 us, of which 9 are loads, 3 sums, 3 notes and 6 stores; six tensors, 1 MB: 8.3.
-// Squares are summed three times, of x, of x 2^-80 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
-// loses values below 2^-75, and where its sum shows that, one of the others stands for it.
+// Squares are summed three times, of x, of x 2^-100 and of x 2^90: the first passes fp32 from |x| = 2^64 on and
+// loses values below 2^-75, and where its sum shows that, one of the others stands for it.  Of 2^40 values the largest have a sum of 2^96
+// in the second, and where the first passes 2^126 those that count are above 2^43, their squares in the second above 2^-114.
 #include <new>
 
 #include <cmath>
@@ -78,13 +79,14 @@ struct Exact {
 // far below a long run's last place and are lost more often than they are rounded up, and equal ones are all rounded
 // the same way (1500 equal values in one run: a norm 1.2e-5 off).
 constexpr int kRun = 16;
+constexpr float kBig = 0x1p-100f, kSmall = 0x1p90f;       // what values are scaled by in the other two sums
 static_assert(kClipGroup * 8 / 2 <= kRun, "a run of vectors is a group");
 struct Squares {
     float2 run = {0.0f, 0.0f}, run_big = {0.0f, 0.0f}, run_small = {0.0f, 0.0f};
     Exact mid, big, small;
     __device__ __forceinline__ void add(float2 x) {
         run = fma2(x, x, run);
-        const float2 b = mul2(x, pair(0x1p-80f)), s = mul2(x, pair(0x1p90f));
+        const float2 b = mul2(x, pair(kBig)), s = mul2(x, pair(kSmall));
         run_big = fma2(b, b, run_big);
         run_small = fma2(s, s, run_small);
     }
@@ -482,10 +484,10 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
                 rest = (fmaf(-root, root, mid.hi) + mid.lo) * (0.5f / root);
             } else if (mid.hi < kLeastMid) {
                 root = sqrtf(small);
-                unit = 0x1p90f;
+                unit = kSmall;
             } else {
                 root = sqrtf(big);
-                unit = 0x1p-80f;
+                unit = kBig;
             }
             const float norm = root + rest;
             if (blockIdx.x == 0) {
