@@ -286,20 +286,35 @@ __device__ __forceinline__ int sum_kept(const Piece& p, int lane, const uint4* k
     return steps;
 }
 
+// What values are scaled by.  A factor below 2^-100, which 32 bits hold with few digits or not at all, is f kTinyStep^2: values that
+// are not 0 once it has scaled them lose nothing in x kTinyStep, and (x kTinyStep) f passes neither end of the range.
+constexpr float kTinyStep = 0x1p-76f;
+struct Factor {
+    float f;
+    int tiny;
+    __device__ __forceinline__ bool one() const { return f == 1.0f && !tiny; }
+    __device__ __forceinline__ float times(float x) const { return tiny ? x * kTinyStep * f * kTinyStep : x * f; }
+};
+
 template <typename T>
-__device__ __forceinline__ uint4 scaled(uint4 u, float f) {
-    if (f == 1.0f) return u;
+__device__ __forceinline__ uint4 scaled(uint4 u, const Factor& f) {
+    if (f.one()) return u;
     float2 v[Of<T>::V / 2];
     Of<T>::get(u, v);
+    if (f.tiny) {
 #pragma unroll
-    for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(v[j], pair(f));
+        for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(mul2(mul2(v[j], pair(kTinyStep)), pair(f.f)), pair(kTinyStep));
+    } else {
+#pragma unroll
+        for (int j = 0; j < Of<T>::V / 2; ++j) v[j] = mul2(v[j], pair(f.f));
+    }
     return Of<T>::put(v);
 }
 
 // A step of a span: its 32 vectors, scaled, lie one after another at the lanes' places, and go out a value a lane, in
 // their order.
 template <class Q>
-__device__ __forceinline__ void store_span(const Piece& p, const Q& q, int lane, int step, uint4* at, float f) {
+__device__ __forceinline__ void store_span(const Piece& p, const Q& q, int lane, int step, uint4* at, const Factor& f) {
     using T = typename Q::T;
     constexpr int E = 32 * Q::V;
     if (step * 32 + lane < q.items) *at = scaled<T>(*at, f);
@@ -320,10 +335,10 @@ __device__ __forceinline__ void store_span(const Piece& p, const Q& q, int lane,
 
 // A piece scaled, its last vectors first; `slot` as above
 template <class Q>
-__device__ __forceinline__ void scale_piece(const Piece& p, int lane, uint4* kept, uint4* ring, int keep, int slot, float f) {
+__device__ __forceinline__ void scale_piece(const Piece& p, int lane, uint4* kept, uint4* ring, int keep, int slot, const Factor& f) {
     const Q q(p);
     using T = typename Q::T;
-    singles(p, q, lane, [&](const T* in, T* out) { *out = f == 1.0f ? *in : Of<T>::put(Of<T>::get(*in) * f); }, [] {});
+    singles(p, q, lane, [&](const T* in, T* out) { *out = f.one() ? *in : Of<T>::put(f.times(Of<T>::get(*in))); }, [] {});
     const int steps = q.steps(), left = min(steps, max(0, keep - slot));         // steps that are kept
     if constexpr (Q::kSpan) {
         asm volatile("cp.async.wait_all;" ::: "memory");
@@ -415,7 +430,7 @@ struct ClipArgs {
 __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
     extern __shared__ uint4 stash[];      // [warps][places][32]
     __shared__ float4 sh[kClipWarps];
-    __shared__ float factor;
+    __shared__ Factor factor;
     __shared__ int ok;
     const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
     const int keep = a.keep;
@@ -477,28 +492,35 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
             }
         }
         if (lane == 0) {
-            // root + rest of the sum in the range that holds it, and the norm over that: 1 / unit
-            float root, rest = 0.0f, unit = 1.0f;
+            // root + rest of the sum in the range that holds it, and the norm over that: 1 / unit.  The factor is limit unit / norm,
+            // where the products are powers of two of `limit` without loss; step: 2^76 sqrt(unit), a tiny one's other part
+            float root, rest = 0.0f, unit = 1.0f, step = 1.0f / kTinyStep;
+            const bool large = !in_range(mid.hi) && !(mid.hi < kLeastMid);
             if (in_range(mid.hi)) {
                 root = sqrtf(mid.hi);
                 rest = (fmaf(-root, root, mid.hi) + mid.lo) * (0.5f / root);
             } else if (mid.hi < kLeastMid) {
                 root = sqrtf(small);
                 unit = kSmall;
+                step = 0x1p121f;
             } else {
                 root = sqrtf(big);
                 unit = kBig;
+                step = 0x1p26f;
             }
             const float norm = root + rest;
             if (blockIdx.x == 0) {
                 *a.norm = norm / unit;
                 *a.turn = turn;              // every CTA has read it: its notes are there
             }
-            float f = 1.0f;
+            Factor f{1.0f, 0};
             if (norm > a.limit * unit && norm <= 3e38f) {
-                f = a.limit / norm;
-                f += (fmaf(-f, root, a.limit) - f * rest) / norm;
-                f *= unit;
+                f.tiny = a.limit * unit < norm * 0x1p-100f;
+                // (limit kBig may lose digits: of large norms that is the last product)
+                const float limit = f.tiny ? a.limit * step * step : large ? a.limit : a.limit * unit;
+                f.f = limit / norm;
+                f.f += (fmaf(-f.f, root, limit) - f.f * rest) / norm;
+                if (large && !f.tiny) f.f *= unit;
             }
             factor = f;
         }
@@ -506,7 +528,7 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
     if (a.limit == 0.0f) return;
     __syncthreads();
     if (!ok) return;
-    const float f = factor;
+    const Factor f = factor;
     slot = end;
     for (int i = work.n - 1; i >= 0; --i) {
         const Piece p = piece(i);
@@ -514,7 +536,7 @@ __global__ void __launch_bounds__(kClipThreads) k_clip(const ClipArgs a) {
             using Q = typename decltype(t)::type;
             slot -= Q(p).steps();
             if constexpr (sizeof(typename Q::T) < 8)
-                if (p.out && !(f == 1.0f && p.out == p.in)) scale_piece<Q>(p, lane, kept, ring, keep, slot, f);
+                if (p.out && !(f.one() && p.out == p.in)) scale_piece<Q>(p, lane, kept, ring, keep, slot, f);
             return 0;
         });
     }
