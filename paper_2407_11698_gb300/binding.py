@@ -866,9 +866,10 @@ class GradClip(_Handle):
 
     def run(self, norm, max_norm=None, stream=None):
         """Writes the norm (fp32, one value) and with max_norm (above 0) the outs; returns norm."""
-        if max_norm is not None and not max_norm > 0:
-            raise ValueError("max_norm must be above 0")
-        st = lib().nitro_clip_run(self.h, 0.0 if max_norm is None else max_norm, _vector(norm, 1, NITRO_F32, "norm"),
+        limit = 0.0 if max_norm is None else ctypes.c_float(max_norm).value
+        if max_norm is not None and not limit > 0:
+            raise ValueError("max_norm must be above 0 (in fp32)")
+        st = lib().nitro_clip_run(self.h, limit, _vector(norm, 1, NITRO_F32, "norm"),
                                   _stream_int(stream))
         if st != NITRO_OK:
             raise NitroError(st, "nitro_clip_run")
