@@ -547,20 +547,22 @@ int value_size(int type) { return type == NITRO_BF16 ? 2 : type == NITRO_F32 ? 4
 // The bytes between a matrix's first and last value, and its rows within them
 struct Range {
     uintptr_t at, end;
-    int64_t pitch, width;      // bytes from row to row (0: a run without gaps), bytes of a row
+    int64_t pitch, width;      // bytes from row to row (0: a run without gaps), bytes of a row, or of the run
 };
 Range range(const void* p, int64_t rows, int64_t cols, int64_t ld, int size) {
     const bool run = rows <= 1 || ld == cols;
     const uintptr_t at = (uintptr_t)p;
-    return {at, at + (uintptr_t)(((rows - 1) * ld + cols) * size), run ? 0 : ld * size, cols * size};
+    const int64_t bytes = ((rows - 1) * ld + cols) * size;
+    return {at, at + (uintptr_t)bytes, run ? 0 : ld * size, run ? bytes : cols * size};
 }
 bool overlap(const Range& a, const Range& b) {
     if (a.end <= b.at || b.end <= a.at) return false;
-    if (a.pitch == 0 || a.pitch != b.pitch) return true;
-    // columns of one wider buffer
-    const int64_t d = (int64_t)((b.at > a.at ? b.at - a.at : a.at - b.at) % (uintptr_t)a.pitch);
+    const int64_t pitch = std::max(a.pitch, b.pitch);
+    if (pitch == 0 || (a.pitch != b.pitch && a.pitch != 0 && b.pitch != 0)) return true;
+    // columns of one wider buffer, or of it and of one of its rows
+    const int64_t d = (int64_t)((b.at > a.at ? b.at - a.at : a.at - b.at) % (uintptr_t)pitch);
     const int64_t first = b.at > a.at ? a.width : b.width, second = b.at > a.at ? b.width : a.width;
-    return d < first || d + second > a.pitch;
+    return d < first || d + second > pitch;
 }
 
 }  // namespace
