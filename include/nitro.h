@@ -517,8 +517,8 @@ nitro_status nitro_glu_status(nitro_glu* h, int clear);
 void nitro_glu_destroy(nitro_glu* h);
 
 /* The norm over many gradients, sqrt of the sum of the squares of all their values, and the gradients scaled by
- * min(1, max_norm / norm).  The matrices are named at create, which lays out the work on the device; their
- * values are read by every run.  (Creation waits for what the default stream has queued.)  in: [rows x cols], NITRO_BF16, NITRO_F32 or NITRO_I64 (nitro_block_grad_device), rows ld_in
+ * min(1, max_norm / norm).  The matrices are named at create, which lays out the work; the first run copies it to the device (as does every replay of a run that was captured before
+ * one that was not).  Their values are read by every run.  in: [rows x cols], NITRO_BF16, NITRO_F32 or NITRO_I64 (nitro_block_grad_device), rows ld_in
  * elements apart; out (NULL: this one is not written): the same type, ld_out apart, may be `in` itself with the
  * same ld.  The pointers must stay valid while the handle runs.
  *

@@ -14,6 +14,7 @@
 #include <new>
 
 #include <cmath>
+#include <cstring>
 #include <vector>
 
 #include "head_act.cuh"
@@ -572,10 +573,15 @@ struct nitro_clip {
     int ctas = 0, keep = 0;
     bool writes = false;
     double bytes = 0.0;
-    Piece* pieces = nullptr;
+    Note* notes = nullptr;           // [2][CTAs], and the turn; then work and pieces
     Work* work = nullptr;
-    Note* notes = nullptr;           // [2][CTAs], and the turn
-    bool clean = false;              // the notes, see clear_once
+    Piece* pieces = nullptr;
+    // What all of them hold before the first run, page-locked, and whether they do.  The first run copies it, on its own stream:
+    // a copy at creation would wait behind what the default stream has queued.  A captured run holds the copy too
+    // and does not count as the first (see clear_once).
+    uint8_t* start = nullptr;
+    int64_t start_bytes = 0;
+    bool started = false;
     StatusWord status;
     DeviceAllocs allocs;
 };
@@ -696,6 +702,17 @@ bool outs_apart(const nitro_clip_matrix* list, int count) {
     return true;
 }
 
+static_assert(sizeof(Note) % alignof(Work) == 0 && sizeof(Work) % alignof(Piece) == 0, "they follow one another");
+
+cudaError_t start_once(nitro_clip* h, cudaStream_t s) {
+    if (h->started) return cudaSuccess;
+    cudaStreamCaptureStatus capture = cudaStreamCaptureStatusNone;
+    cudaError_t e = cudaStreamIsCapturing(s, &capture);
+    if (e == cudaSuccess) e = cudaMemcpyAsync(h->notes, h->start, (size_t)h->start_bytes, cudaMemcpyHostToDevice, s);
+    if (e == cudaSuccess && capture == cudaStreamCaptureStatusNone) h->started = true;
+    return e;
+}
+
 nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** out) {
     double bytes = 0.0;
     if (!clip_list_ok(list, count, &bytes) || !outs_apart(list, count)) return NITRO_ERR_ARG;
@@ -735,17 +752,21 @@ nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** 
     h->keep = most_steps <= kClipPlaces ? kClipPlaces : kClipPlaces - kClipRing;
     h->bytes = bytes;
     for (int i = 0; i < count; ++i) h->writes = h->writes || (list[i].out && list[i].rows > 0 && list[i].cols > 0);
-    const bool ok = h->allocs.take(&h->pieces, std::max<int64_t>(n, 1)) && h->allocs.take(&h->work, warps) &&
-                    h->allocs.take(&h->notes, 2 * h->ctas + 1) && h->status.take();
-    const cudaStream_t s = cudaStreamPerThread;
-    const bool copied = ok &&
-                        (n == 0 || cudaMemcpyAsync(h->pieces, host.data(), sizeof(Piece) * (size_t)n, cudaMemcpyHostToDevice, s) == cudaSuccess) &&
-                        cudaMemcpyAsync(h->work, work.data(), sizeof(Work) * work.size(), cudaMemcpyHostToDevice, s) == cudaSuccess &&
-                        cudaStreamSynchronize(s) == cudaSuccess;
-    if (!copied) {
+    const int64_t notes = sizeof(Note) * (2 * ctas + 1), works = sizeof(Work) * work.size(), all = notes + works + sizeof(Piece) * n;
+    uint8_t* block = nullptr;
+    void* start = nullptr;
+    if (!h->allocs.take(&block, all) || !h->status.take() || !allocated(cudaMallocHost(&start, (size_t)all))) {
         nitro_clip_destroy(h);
         return NITRO_ERR_CUDA;
     }
+    h->start = static_cast<uint8_t*>(start);
+    h->start_bytes = all;
+    memset(h->start, 0, (size_t)notes);
+    memcpy(h->start + notes, work.data(), (size_t)works);
+    if (n) memcpy(h->start + notes + works, host.data(), sizeof(Piece) * (size_t)n);
+    h->notes = reinterpret_cast<Note*>(block);
+    h->work = reinterpret_cast<Work*>(block + notes);
+    h->pieces = reinterpret_cast<Piece*>(block + notes + works);
     *out = h;
     return NITRO_OK;
 }
@@ -768,7 +789,7 @@ nitro_status nitro_clip_create(const nitro_clip_matrix* list, int count, nitro_c
 nitro_status nitro_clip_run(nitro_clip* h, float max_norm, float* norm, void* stream) {
     if (!h || !norm || (uintptr_t)norm % 4 || !(max_norm >= 0.0f) || (max_norm > 0.0f && !h->writes)) return NITRO_ERR_ARG;
     const cudaStream_t s = static_cast<cudaStream_t>(stream);
-    TRY(clear_once(h->clean, h->notes, (2 * h->ctas + 1) * sizeof(Note), s));
+    TRY(start_once(h, s));
     static std::atomic<uint64_t> ready{0};
     int dev = 0;
     sm_count(&dev);
@@ -802,6 +823,7 @@ void nitro_clip_destroy(nitro_clip* h) {
     cudaDeviceSynchronize();
     h->allocs.free();
     h->status.free();
+    if (h->start) cudaFreeHost(h->start);
     delete h;
 }
 
