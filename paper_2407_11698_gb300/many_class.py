@@ -162,8 +162,10 @@ class GatedHead:
         pair = lambda t: t.view(2, self.hidden, self.features)      # the gate and the up matrix, each by itself
         self.orth_ops[0].run(pair(self.m[0]), pair(self.updates[0]))
         self.orth_ops[1].run(self.m[1], self.updates[1])
-        for master, w, u in zip(self.masters, self.w, self.updates):
-            master.add_(u, alpha=-self.lr * math.sqrt(max(w.shape)))
+        # an entry of an orthogonal rows x cols matrix is 1 / sqrt(max(rows, cols)) in the mean square: times lr, here
+        longest = max(self.hidden, self.features), max(self.classes, self.hidden)
+        for master, w, u, n in zip(self.masters, self.w, self.updates, longest):
+            master.add_(u, alpha=-self.lr * math.sqrt(n))
             w.copy_(master)
         for p, m in zip((self.gamma, self.beta), self.m[2:]):
             p.add_(m, alpha=-self.lr)
