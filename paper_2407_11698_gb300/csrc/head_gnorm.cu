@@ -44,6 +44,10 @@ __device__ __forceinline__ void through_ring(int n, Fetch&& fetch, Use&& use) {
     }
 }
 
+// Sums of many values go in runs, of a thread's and of the threads', which are then added up: equal values are all rounded the same way in
+// one sum (2^28 equal dy in one channel: dbeta 1.9e-5 off).
+constexpr int kValueRun = 32, kRowRun = 16;
+
 // CTAs of a backward pass that an SM holds by their registers
 constexpr int gn_resident(int v) { return v == 8 ? 2 : 4; }
 
@@ -146,7 +150,7 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
                     float2 v[Sums<V>::N];
                     SX::get(slot + k * SX::STEP, v, low_bits(src + i * step));
                     run.add(v);
-                    if ((i & 31) == 31) t.take(run);
+                    if (i % kValueRun == kValueRun - 1) t.take(run);
                 });
             t.take(run);
             t.finish((float)n, at.group(s, c), s.per % V == 0, origin);      // 0 for rows past the chunk
@@ -161,8 +165,12 @@ __global__ void __launch_bounds__(kGnThreads) k_gn_stats(const X* x, int64_t ldx
             const int ch = slab * width + i;
             if (ch >= s.channels) break;
             Moments a;
-            for (int r = 0; r < min(s.rows, np); ++r)
-                a.add((float)((np - r + s.rows - 1) / s.rows), red[0][r * width + i], red[1][r * width + i]);
+            for (int r = 0; r < min(s.rows, np);) {
+                Moments run;
+                for (const int to = min(min(s.rows, np), r + kRowRun); r < to; ++r)
+                    run.add((float)((np - r + s.rows - 1) / s.rows), red[0][r * width + i], red[1][r * width + i]);
+                a.add(run.n, run.m, run.q);
+            }
             chan[ch] = a.m;
             chan[s.channels + ch] = a.q;
         }
@@ -251,6 +259,18 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X*
             float2 a[ch.N], b[ch.N];
 #pragma unroll
             for (int j = 0; j < ch.N; ++j) a[j] = b[j] = pair(0.0f);
+            // (runs are added up where the sums are wanted in the end, which takes no registers)
+            float *suma = red[0] + at.row * width + at.vec * V, *sumb = red[1] + at.row * width + at.vec * V;
+#pragma unroll
+            for (int j = 0; j < V; ++j) suma[j] = sumb[j] = 0.0f;
+            const auto end_run = [&] {
+#pragma unroll
+                for (int j = 0; j < V; ++j) {
+                    suma[j] += at2(a, j);
+                    sumb[j] += at2(b, j);
+                    at2(a, j) = at2(b, j) = 0.0f;
+                }
+            };
             const X* src = x + sample * sx + (int64_t)(p0 + at.row) * ldx + c;
             const Y* grad = dy + sample * sdy + (int64_t)(p0 + at.row) * lddy + c;
             const int64_t xs = s.rows * ldx, gs = s.rows * lddy;
@@ -271,20 +291,21 @@ __global__ void __launch_bounds__(kGnThreads, gn_resident(V)) k_gn_sums(const X*
                             a[j] = add2(a[j], g[j]);
                             b[j] = fma2(g[j], v[j], b[j]);
                         }
+                        if (i % kValueRun == kValueRun - 1) end_run();
                     });
             });
-#pragma unroll
-            for (int j = 0; j < V; ++j) {
-                red[0][at.row * width + at.vec * V + j] = at2(a, j);
-                red[1][at.row * width + at.vec * V + j] = at2(b, j);
-            }
+            end_run();
         }
         __syncthreads();
         for (int i = threadIdx.x; i < 2 * width; i += blockDim.x) {
             const int half = i >= width, k = i - half * width, chn = slab * width + k;
             if (chn >= s.channels) continue;
             float v = 0.0f;
-            for (int r = 0; r < s.rows; ++r) v += red[half][r * width + k];
+            for (int r = 0; r < s.rows;) {
+                float run = 0.0f;
+                for (const int to = min(s.rows, r + kRowRun); r < to; ++r) run += red[half][r * width + k];
+                v += run;
+            }
             out[half * s.channels + chn] = v;
         }
         __syncthreads();
