@@ -528,7 +528,8 @@ void nitro_glu_destroy(nitro_glu* h);
  * kept in pairs of 32-bit numbers over the threads, in an order that the handle's sizes fix.
  * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, 2^20], sizes below 0, strides below the columns
  * (with rows above 1), another type, int64 with an out, more than 2^40 values, an out that overlaps another
- * matrix (interleaved matrices of two different strides count as such), or in otherwise than by being it; max_norm below 0 or NaN, or above 0 where no matrix has an out. */
+ * matrix (interleaved matrices of two different strides count as such), or in otherwise than by being it; max_norm below 0 or NaN, or above 0 where there are values and no matrix that
+ * has any has an out. */
 typedef struct nitro_clip nitro_clip;
 typedef struct {
     const void* in;

@@ -571,7 +571,7 @@ bool overlap(const Range& a, const Range& b) {
 
 struct nitro_clip {
     int ctas = 0, keep = 0;
-    bool writes = false;
+    bool writes = true;              // an out, or there are no values
     double bytes = 0.0;
     Note* notes = nullptr;           // [2][CTAs], and the turn; then work and pieces
     Work* work = nullptr;
@@ -751,6 +751,7 @@ nitro_status clip_create(const nitro_clip_matrix* list, int count, nitro_clip** 
     }
     h->keep = most_steps <= kClipPlaces ? kClipPlaces : kClipPlaces - kClipRing;
     h->bytes = bytes;
+    for (int i = 0; i < count; ++i) h->writes = h->writes && (list[i].rows == 0 || list[i].cols == 0);
     for (int i = 0; i < count; ++i) h->writes = h->writes || (list[i].out && list[i].rows > 0 && list[i].cols > 0);
     const int64_t notes = sizeof(Note) * (2 * ctas + 1), works = sizeof(Work) * work.size(), all = notes + works + sizeof(Piece) * n;
     uint8_t* block = nullptr;
