@@ -477,7 +477,7 @@ typedef enum { NITRO_ACT_NONE = 0, NITRO_ACT_RELU = 1, NITRO_ACT_SILU = 2, NITRO
  * dx, dgamma and dbeta (fp32 [channels], summed over samples and pixels, overwritten); any may be NULL.
  * dx may be dy itself likewise, but not x.  No other output may overlap an input.
  * Statistics and sums are in 32 bits or more, in an order that the sizes fix.  With samples = 0 dgamma and dbeta are
- * cleared.  Errors: NITRO_ERR_ARG for null handles or pointers, samples outside [0, max_samples],
+ * cleared.  Workspace: 8 KB a channel and a group, and 16 bytes for each group of up to 1024 samples.  Errors: NITRO_ERR_ARG for null handles or pointers, samples outside [0, max_samples],
  * pixels outside [1, max_pixels], strides below the sizes (stride_x below pixels ldx with more than one sample), eps
  * that is not above 0 and finite, another type or activation; at create sizes below 1,
  * channels above 8192 or not a multiple of groups, more than 2^30 pixels, more than 65535 samples, or
@@ -504,6 +504,8 @@ void nitro_gnorm_destroy(nitro_gnorm* h);
  * backward, from saved and the gradient dout (bf16): D = [dout b act'(a), dout act(a)], dx = scale D W and
  * dw = scale D^T x, bf16; either may be NULL.  D is rounded to bf16 (up to 32 rows: kept as two
  * bf16 halves).  Sums are in 32 bits, in an order that the sizes fix.  With rows = 0 dw is cleared.
+ * Workspace: copies of x and W as bf16 (used where they are int8 or their rows are no multiples of 16 bytes), D,
+ * and at most 64 MB of sums.
  * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], strides below the sizes, another type
  * or activation, or a scale that is not above 0 (1e30 at most). */
 typedef struct nitro_glu nitro_glu;
@@ -517,19 +519,21 @@ nitro_status nitro_glu_status(nitro_glu* h, int clear);
 void nitro_glu_destroy(nitro_glu* h);
 
 /* The norm over many gradients, sqrt of the sum of the squares of all their values, and the gradients scaled by
- * min(1, max_norm / norm).  The matrices are named at create, which lays out the work; the first run copies it to the device (as does every replay of a run that was captured before
- * one that was not).  Their values are read by every run.  in: [rows x cols], NITRO_BF16, NITRO_F32 or NITRO_I64 (nitro_block_grad_device), rows ld_in
+ * min(1, max_norm / norm).  The matrices are named at create, which lays out the work; the first run copies that to the
+ * device (so does every replay of a run that was captured before one that was not).  Their values are read by
+ * every run.  in: [rows x cols], NITRO_BF16, NITRO_F32 or NITRO_I64 (nitro_block_grad_device), rows ld_in
  * elements apart; out (NULL: this one is not written): the same type, ld_out apart, may be `in` itself with the
  * same ld.  The pointers must stay valid while the handle runs.
  *
  * run: norm (fp32, one value) is written, and with max_norm > 0 every out = in min(1, max_norm / norm), rounded once;
  * with max_norm = 0 the norm alone is taken.  A sum of squares that is not finite (its norm is written: NaN or infinity)
- * scales by 1.  A norm beyond fp32 or the squares' range is no such sum: squares are taken in three ranges.  The sum is
- * kept in pairs of 32-bit numbers over the threads, in an order that the handle's sizes fix.
+ * scales by 1.  A norm beyond fp32 or the squares' range is no such sum: squares are taken in three ranges, and the factor
+ * may be of any size.  The sum is kept in pairs of 32-bit numbers over the threads, in an order that the handle's sizes fix.
+ * Workspace: 64 bytes a matrix and up to 1 MB, on the device and page-locked on the host.
  * Errors: NITRO_ERR_ARG for null handles or pointers, count outside [0, 2^20], sizes below 0, strides below the columns
  * (with rows above 1), another type, int64 with an out, more than 2^40 values, an out that overlaps another
- * matrix (interleaved matrices of two different strides count as such), or in otherwise than by being it; max_norm below 0 or NaN, or above 0 where there are values and no matrix that
- * has any has an out. */
+ * matrix (interleaved matrices of two different strides count as such), or in otherwise than by being it; max_norm below 0
+ * or NaN, or above 0 where there are values and no matrix that has any has an out. */
 typedef struct nitro_clip nitro_clip;
 typedef struct {
     const void* in;
