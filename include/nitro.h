@@ -503,7 +503,8 @@ void nitro_gnorm_destroy(nitro_gnorm* h);
  * order of the library's own (NULL: not kept).
  * backward, from saved and the gradient dout (bf16): D = [dout b act'(a), dout act(a)], dx = scale D W and
  * dw = scale D^T x, bf16; either may be NULL.  D is rounded to bf16 (up to 32 rows: kept as two
- * bf16 halves).  Sums are in 32 bits, in an order that the sizes fix.  With rows = 0 dw is cleared.
+ * bf16 halves).  Sums are in 32 bits, in an order that the sizes fix.  With rows = 0 dw is cleared.  No output of either
+ * call may overlap an input or another output.
  * Workspace: copies of x and W as bf16 (used where they are int8 or their rows are no multiples of 16 bytes), D,
  * and at most 64 MB of sums.
  * Errors: NITRO_ERR_ARG for null handles or pointers, rows outside [0, max_rows], strides below the sizes, another type

@@ -810,7 +810,8 @@ class GatedLinear(_Handle):
 
     def backward(self, x, w, saved, dout, dx=None, dw=None, act=NITRO_ACT_SILU, scale=1.0, stream=None):
         """Writes dx [rows x features] and dw [2 hidden x features] (bf16; either may be None) from the
-        gradient dout (bf16 [rows x hidden]) and the saved of a forward on the same inputs."""
+        gradient dout (bf16 [rows x hidden]) and the saved of a forward on the same inputs.  The gradient of z is
+        rounded to bf16 on the way (up to 32 rows: kept as two bf16 halves)."""
         n, f, hidden = x.shape[0], self.features, self.hidden
         xp, xt, ldx = _matrix(x, n, f, _X, "x")
         wp, _, ldw = _matrix(w, 2 * hidden, f, _W, "w")
@@ -827,8 +828,8 @@ class GatedLinear(_Handle):
 class GradClip(_Handle):
     """The norm over the values of all `grads` (bf16, fp32, or int64 where it is not scaled), and each scaled by
     min(1, max_norm / norm) into its tensor of `outs` (None: not written; grads themselves: in
-    place).  Tensors are contiguous, or matrices with contiguous rows.  The handle keeps them and reads their
-    values at every run."""
+    place).  Where a value is infinite or NaN, so is the norm, and the outs are the grads as they are.  Tensors are
+    contiguous, or matrices with contiguous rows.  The handle keeps them and reads their values at every run."""
     _op = "clip"
 
     def __init__(self, grads, outs=None):

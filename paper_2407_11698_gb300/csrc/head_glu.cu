@@ -7,8 +7,8 @@
 // value (8 rows hidden bytes each way, beside 12 rows hidden features operations; 16 bits would
 // put a rounding of 2^-9 under both gradients, and taking the products again costs a third of a step).
 // The backward writes D in bf16, which both products with it take.  4 rows hidden features operations forward and
-// 8 backward: 8192 x 2048 x 8192 1.09 ms, forward 332 us (1.66 PFLOP/s), D 143 (6.6 TB/s), dx 324, dW 299 (1.7 and 1.84), at the
-// power limit.  Few rows run on the CUDA cores, where W's bytes bound them (k_glu_few).
+// 8 backward: 8192 x 2048 x 8192 1.09 to 1.17 ms at the power limit, forward 332 to 348 us (1.66 to 1.58 PFLOP/s), D 143 (6.6 TB/s), dx 324
+// to 340, dW 299 to 307 (1.7 and 1.84).  Few rows run on the CUDA cores, where W's bytes bound them (k_glu_few).
 #include <new>
 
 #include "head_act.cuh"

@@ -96,8 +96,9 @@ class GatedHead:
     """logits = (act(n Wg^T) * (n Wu^T)) Wc^T with n = act(group norm of x), on int8 maps x [rows x pixels x channels].
 
     Wg and Wu are one matrix w1 [2 hidden x features], features = pixels * channels; Wc is w2 [classes x hidden], both bf16
-    with an fp32 master.  step() scales all gradients so that their norm together is at most max_norm, and takes the
-    matrices by orthogonal updates as ManyClassHead does, the norm's scales and shifts by lr times their momentum."""
+    with an fp32 master.  step() scales all gradients so that their norm together is at most max_norm (gradients whose norm, kept in
+    self.norm, is infinite or NaN go on as they are), and takes the matrices by orthogonal updates as ManyClassHead does,
+    the gate and the up matrix each by itself, the norm's scales and shifts by lr times their momentum."""
 
     def __init__(self, pixels, channels, groups, hidden, classes, max_rows, lr=0.002, momentum=0.9, max_norm=1.0, seed=0, device="cuda"):
         g = torch.Generator(device="cpu").manual_seed(seed)
