@@ -461,7 +461,7 @@ nitro_status nitro_mx4_linear(nitro_mx4* h, const void* x, int x_type, int64_t l
 nitro_status nitro_mx4_status(nitro_mx4* h, int clear);
 void nitro_mx4_destroy(nitro_mx4* h);
 
-/* Activations of the two operators below: u, max(u, 0), u / (1 + exp(-u)), and u times the
+/* Activations of the two operators below: u, max(u, 0) (slope 0 at 0), u / (1 + exp(-u)), and u times the
  * normal distribution at u. */
 typedef enum { NITRO_ACT_NONE = 0, NITRO_ACT_RELU = 1, NITRO_ACT_SILU = 2, NITRO_ACT_GELU = 3 } nitro_act;
 
