@@ -724,7 +724,8 @@ cudaError_t hg_launch_as(int splits, const HgProblem& p, const HgOperand& a, con
 }
 
 // Clusters of eight CTAs, one an SM, that surely run at once: half the SMs' worth.  (152 SMs do not hold 16 of them, as their
-// parts hold whole clusters only: 64 x 2048 x 1024 took 16.6 us with 16 and 7.4 in clusters of four; 8 run at once.)
+// parts hold whole clusters only: 64 x 2048 x 1024 took 16.6 us with 16 and 7.4 in clusters of four.  15 run at once, but 10 to 15 tiles
+// gain by them along 8192 features only, 15.6 to 13.5 us with 64 rows, and lose along 4096, 10.7 to 11.1, and 2048, 8.2 to 9.7.)
 inline int hg_eights() { return std::max(1, sm_count() / 16); }
 
 // D = A B^T through Epi; AMN / BMN: the operand's inner dimension is M / N, else K; HA, HB:
